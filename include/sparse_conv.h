@@ -330,6 +330,95 @@ int sparse_conv_get_launch(sparse_conv_t h, int N, int H, int W, int stride, int
 int sparse_conv_probe_lds_read(void* sink, int workgroups, int iterations, void* stream, long long* bytes_read);
 int sparse_conv_probe_copy(void* dst, const void* src, long long bytes, void* stream);
 
+/*
+ * Operators around the convolutions of a text model (section 9's "CNN-non-static": sentences of word
+ * vectors that are trained with the network, 1-D convolutions, a classifier): rows of a table of vectors
+ * for tokens, the gradient of that table, and a fully connected layer in 8-bit integers (section 6's linear
+ * quantisation).  They have no handle: all operands are DEVICE memory of the current device, calls are
+ * asynchronous on `stream`, allocate nothing, keep nothing from one call for the next and may be recorded
+ * into a HIP graph.  A call that needs scratch memory takes it from the caller (`workspace`, of the size that
+ * its _workspace function reports, at a multiple of 16 bytes, its contents unspecified before and after);
+ * two calls must not use one workspace at the same time.  Arguments are checked before anything is enqueued.
+ */
+
+/* Further storage types, for the operators below only: bfloat16, and 8-bit integers with a scale for each row. */
+enum { SC_BF16 = 2, SC_I8 = 3 };
+
+/* sparse_conv_embed, sparse_conv_embed_backward: vectors are [sentences][dim][words], as a 1-D convolution layer
+ * reads and writes them (H = 1, W = words), instead of [sentences][words][dim]; tokens are 64-bit integers instead of
+ * 32-bit ones; the gradient is added to what table_grad holds. */
+enum { SC_EMBED_CHANNELS_FIRST = 1u, SC_EMBED_TOKENS_64 = 2u, SC_EMBED_ACCUMULATE = 4u };
+
+/*
+ * sparse_conv_embed - word vectors: out[n][t][:] = scale * table[tokens[n][t]][:].
+ *   table    [vocab][dim] of dtype (SC_F32, SC_F16 or SC_BF16).
+ *   tokens   [sentences][words], signed 32-bit integers (64-bit with SC_EMBED_TOKENS_64).  A token outside
+ *            0..vocab-1 reads as a row of zeros.
+ *   out      [sentences][words][dim] of dtype, or [sentences][dim][words] with SC_EMBED_CHANNELS_FIRST; must not
+ *            overlap the table or the tokens.
+ *   flags    0 or any of SC_EMBED_CHANNELS_FIRST, SC_EMBED_TOKENS_64.
+ * The product with scale is formed in fp32 and rounded once.  sentences or words may be 0 (no-op).
+ * SC_EINVAL: a null or misaligned pointer (to its own element size), vocab or dim below 1, a negative count, an unknown
+ * type or flag.  SC_EUNSUPPORTED: vocab or sentences * words of 2^31 or more.
+ */
+int sparse_conv_embed(const void* table, const void* tokens, void* out, long long vocab, int dim, int sentences, int words,
+                      int dtype, float scale, unsigned flags, void* stream);
+
+/*
+ * sparse_conv_embed_backward - gradient of the table: table_grad[v][:] = scale * the sum of grad[n][t][:] over
+ * all (n, t) with tokens[n][t] = v; rows that no token names are set to zero (with SC_EMBED_ACCUMULATE the sum is
+ * added to what table_grad holds, and such rows are left alone).
+ *   grad        [sentences][words][dim] of grad_dtype (SC_F32, SC_F16, SC_BF16), or [sentences][dim][words] with
+ *               SC_EMBED_CHANNELS_FIRST.
+ *   tokens      as for sparse_conv_embed; a token outside 0..vocab-1 adds to no row.
+ *   table_grad  [vocab][dim] of table_dtype: SC_F32 or grad_dtype.  Must not overlap the other arrays.
+ *   padding     a token whose row has no gradient (it adds to no row), or -1.
+ *   workspace   of at least the bytes that sparse_conv_embed_backward_workspace reports for the same arguments.
+ * Sums are formed in fp32, each row's in an order that depends on the tokens alone, and rounded once: the same
+ * arguments give the same bits.  Status codes as for sparse_conv_embed; SC_EINVAL for a workspace that is too small.
+ */
+int sparse_conv_embed_backward_workspace(long long vocab, int dim, int sentences, int words, int grad_dtype, unsigned flags,
+                                         long long* bytes);
+int sparse_conv_embed_backward(const void* grad, const void* tokens, void* table_grad, long long vocab, int dim, int sentences,
+                               int words, int grad_dtype, int table_dtype, float scale, long long padding, unsigned flags,
+                               void* workspace, long long workspace_bytes, void* stream);
+
+/* Bytes from one row of 8-bit integers to the next: a whole number of 128, the bytes past K zero. */
+#define SC_INT8_PITCH(K) (((long long)(K) + 127) / 128 * 128)
+
+/*
+ * sparse_conv_int8_quantize - rows of numbers as 8-bit integers with a scale each: with a the largest |x| of a row,
+ * scale = a / 127 and q = x * (127 / a) rounded to the nearest whole number (ties to even), both in fp32; -127 <= q <= 127.
+ * Tokens of an activation matrix and output channels of a weight matrix are both such rows.
+ *   x        [rows][K] of dtype (SC_F32, SC_F16, SC_BF16), ldx elements from one row to the next (ldx >= K).
+ *   q        [rows][SC_INT8_PITCH(K)], at a multiple of 16 bytes; bytes past K are set to zero.
+ *   scale    fp32 [rows].
+ * A row whose a is below 2^-100 counts as zeros: q = 0, scale = 0.  A row that holds an infinity or a NaN has q = 0 and
+ * scale = NaN.
+ */
+int sparse_conv_int8_quantize(const void* x, signed char* q, float* scale, int rows, int K, long long ldx, int dtype, void* stream);
+
+/*
+ * sparse_conv_int8_linear - fully connected layer in 8-bit integers:
+ *   out[m][n] = act(x_scale[m] * w_scale[n] * sum_k x[m][k] * w[n][k] + bias[n]).
+ *   x        [M][K], ldx elements from one row to the next.  in_dtype SC_F32, SC_F16 or SC_BF16: each row is quantised
+ *            within the call as sparse_conv_int8_quantize does it (x_scale is not read and may be NULL).  SC_I8: rows as
+ *            that function leaves them (ldx = SC_INT8_PITCH(K), at a multiple of 16 bytes, zeros past K), x_scale fp32 [M].
+ *   w        [N][SC_INT8_PITCH(K)] 8-bit integers at a multiple of 16 bytes, zeros past K; w_scale fp32 [N].
+ *   bias     fp32 [N] or NULL.
+ *   out      [M][N] of out_dtype (SC_F32, SC_F16, SC_BF16), ldo elements from one row to the next (ldo >= N).
+ *   flags    0 or SC_EPILOGUE_RELU (a NaN stays one).
+ *   workspace  of at least the bytes that sparse_conv_int8_linear_workspace reports for the same sizes and types.
+ * Sums are exact (32-bit integers, hence K <= 131071); scales, bias and activation are applied in fp32 and the result is
+ * rounded once, to out_dtype.  An output row whose scale is NaN is NaN; no other row is touched by it.  M may be 0 (no-op).
+ * SC_EINVAL: a null or misaligned pointer, a size below 1, ldx or ldo too small, an unknown type or flag, a workspace that is
+ * too small.  SC_EUNSUPPORTED: K above 131071, M or N of 2^24 or more.
+ */
+int sparse_conv_int8_linear_workspace(int M, int N, int K, int in_dtype, int out_dtype, long long* bytes);
+int sparse_conv_int8_linear(const void* x, const float* x_scale, const signed char* w, const float* w_scale, const float* bias,
+                            void* out, int M, int N, int K, long long ldx, long long ldo, int in_dtype, int out_dtype,
+                            unsigned flags, void* workspace, long long workspace_bytes, void* stream);
+
 /* HIP error code of the last failing runtime call made through this handle (0 if none). */
 int sparse_conv_last_hip_error(sparse_conv_t h);
 

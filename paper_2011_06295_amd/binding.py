@@ -15,10 +15,11 @@ import numpy as np
 
 SC_OK, SC_EINVAL, SC_EUNSUPPORTED, SC_ENOMEM, SC_EHIP, SC_ETOOBIG = 0, -1, -2, -3, -4, -5
 SC_STATIC_SCRATCH_BYTES = 16 << 20
-SC_F32, SC_F16 = 0, 1
+SC_F32, SC_F16, SC_BF16, SC_I8 = 0, 1, 2, 3
 SC_FLAG_UNIFY_NNZ = 1
 SC_EPILOGUE_RELU = 1
 SC_EPILOGUE_MAXPOOL2 = 2
+SC_EMBED_CHANNELS_FIRST, SC_EMBED_TOKENS_64, SC_EMBED_ACCUMULATE = 1, 2, 4
 
 # SPARSECONV_LIBRARY names another build of the same library (e.g. an instrumented one)
 LIB_PATH = os.environ.get("SPARSECONV_LIBRARY") or os.path.join(
@@ -30,6 +31,8 @@ EXPORTS = (
     "sparse_conv_create_codebook", "sparse_conv_get_codebook", "sparse_conv_check_plan", "sparse_conv_rank_launches", "sparse_conv_get_kernel",
     "sparse_conv_get_matrix_plan", "sparse_conv_get_matrix_runs", "sparse_conv_get_matrix_out_runs",
     "sparse_conv_probe_lds_read", "sparse_conv_probe_copy",
+    "sparse_conv_embed", "sparse_conv_embed_backward_workspace", "sparse_conv_embed_backward",
+    "sparse_conv_int8_quantize", "sparse_conv_int8_linear_workspace", "sparse_conv_int8_linear",
     "sparse_conv_last_hip_error", "sparse_conv_strerror", "sparse_conv_destroy",
 )
 
@@ -74,6 +77,13 @@ def _load():
                                          C.POINTER(C.c_float)]
     lib.sparse_conv_probe_lds_read.argtypes = [vp, C.c_int, C.c_int, vp, C.POINTER(C.c_longlong)]
     lib.sparse_conv_probe_copy.argtypes = [vp, vp, C.c_longlong, vp]
+    n, ll, f32, flags = C.c_int, C.c_longlong, C.c_float, C.c_uint
+    lib.sparse_conv_embed.argtypes = [vp, vp, vp, ll, n, n, n, n, f32, flags, vp]
+    lib.sparse_conv_embed_backward_workspace.argtypes = [ll, n, n, n, n, flags, C.POINTER(ll)]
+    lib.sparse_conv_embed_backward.argtypes = [vp, vp, vp, ll, n, n, n, n, n, f32, ll, flags, vp, ll, vp]
+    lib.sparse_conv_int8_quantize.argtypes = [vp, vp, vp, n, n, ll, n, vp]
+    lib.sparse_conv_int8_linear_workspace.argtypes = [n, n, n, n, n, C.POINTER(ll)]
+    lib.sparse_conv_int8_linear.argtypes = [vp, vp, vp, vp, vp, vp, n, n, n, ll, ll, n, n, flags, vp, ll, vp]
     lib.sparse_conv_last_hip_error.argtypes = [vp]
     lib.sparse_conv_strerror.argtypes = [C.c_int]
     lib.sparse_conv_strerror.restype = C.c_char_p
@@ -260,6 +270,56 @@ def sparse_conv_probe_lds_read(sink_ptr: int, workgroups: int, iterations: int, 
 def sparse_conv_probe_copy(dst_ptr: int, src_ptr: int, nbytes: int, stream: int = 0) -> None:
     """Enqueues the copy probe (nbytes read, nbytes written)."""
     _check(_lib.sparse_conv_probe_copy(dst_ptr, src_ptr, nbytes, stream or None), "sparse_conv_probe_copy")
+
+
+def sparse_conv_embed(table_ptr: int, tokens_ptr: int, out_ptr: int, vocab: int, dim: int, sentences: int, words: int, dtype: int,
+                      scale: float = 1.0, flags: int = 0, stream: int = 0) -> None:
+    """Enqueue the lookup of DEVICE tokens [sentences][words] in DEVICE table [vocab][dim]."""
+    _check(_lib.sparse_conv_embed(table_ptr, tokens_ptr, out_ptr, vocab, dim, sentences, words, dtype, scale, flags, stream or None),
+           "sparse_conv_embed")
+
+
+def sparse_conv_embed_backward_workspace(vocab: int, dim: int, sentences: int, words: int, grad_dtype: int, flags: int = 0) -> int:
+    """Bytes of scratch memory that sparse_conv_embed_backward needs for these sizes."""
+    n = C.c_longlong(0)
+    _check(_lib.sparse_conv_embed_backward_workspace(vocab, dim, sentences, words, grad_dtype, flags, C.byref(n)),
+           "sparse_conv_embed_backward_workspace")
+    return int(n.value)
+
+
+def sparse_conv_embed_backward(grad_ptr: int, tokens_ptr: int, table_grad_ptr: int, vocab: int, dim: int, sentences: int, words: int,
+                               grad_dtype: int, table_dtype: int, scale: float = 1.0, padding: int = -1, flags: int = 0,
+                               workspace_ptr: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    """Enqueue the gradient of the table: DEVICE grad and tokens to DEVICE table_grad [vocab][dim]."""
+    _check(_lib.sparse_conv_embed_backward(grad_ptr, tokens_ptr, table_grad_ptr, vocab, dim, sentences, words, grad_dtype, table_dtype,
+                                           scale, padding, flags, workspace_ptr or None, workspace_bytes, stream or None),
+           "sparse_conv_embed_backward")
+
+
+def sparse_conv_int8_quantize(x_ptr: int, q_ptr: int, scale_ptr: int, rows: int, K: int, ldx: int, dtype: int, stream: int = 0) -> None:
+    """Enqueue the quantisation of DEVICE rows [rows][K] to 8-bit integers [rows][int8_pitch(K)] with a scale each."""
+    _check(_lib.sparse_conv_int8_quantize(x_ptr, q_ptr, scale_ptr, rows, K, ldx, dtype, stream or None), "sparse_conv_int8_quantize")
+
+
+def int8_pitch(K: int) -> int:
+    """Bytes from one row of 8-bit integers to the next (SC_INT8_PITCH)."""
+    return -(-K // 128) * 128
+
+
+def sparse_conv_int8_linear_workspace(M: int, N: int, K: int, in_dtype: int, out_dtype: int) -> int:
+    """Bytes of scratch memory that sparse_conv_int8_linear needs for these sizes."""
+    n = C.c_longlong(0)
+    _check(_lib.sparse_conv_int8_linear_workspace(M, N, K, in_dtype, out_dtype, C.byref(n)), "sparse_conv_int8_linear_workspace")
+    return int(n.value)
+
+
+def sparse_conv_int8_linear(x_ptr: int, x_scale_ptr: int, w_ptr: int, w_scale_ptr: int, bias_ptr: int, out_ptr: int, M: int, N: int, K: int,
+                            ldx: int, ldo: int, in_dtype: int, out_dtype: int, flags: int = 0, workspace_ptr: int = 0,
+                            workspace_bytes: int = 0, stream: int = 0) -> None:
+    """Enqueue the fully connected layer on DEVICE x [M][K] and 8-bit weights [N][int8_pitch(K)] into DEVICE out [M][N]."""
+    _check(_lib.sparse_conv_int8_linear(x_ptr, x_scale_ptr or None, w_ptr, w_scale_ptr, bias_ptr or None, out_ptr, M, N, K, ldx, ldo,
+                                        in_dtype, out_dtype, flags, workspace_ptr or None, workspace_bytes, stream or None),
+           "sparse_conv_int8_linear")
 
 
 def sparse_conv_destroy(handle: Optional[int]) -> None:

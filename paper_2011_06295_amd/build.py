@@ -9,7 +9,8 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsparseconv.so")
-SOURCES = ["kernels.hip", "matrix_f32.hip", "matrix_f16.hip", "probes.hip", "api.cpp", "plan.cpp", "matrix_plan.cpp", "host_csr.cpp"]
+SOURCES = ["kernels.hip", "matrix_f32.hip", "matrix_f16.hip", "probes.hip", "api.cpp", "plan.cpp", "matrix_plan.cpp", "host_csr.cpp",
+           "embed.hip", "int8.hip", "text_api.cpp"]
 
 # packed fp32 VALU forms are switched off for the device pass (the host pass
 # prints a harmless "not a recognized feature" note for the same flag)

@@ -1,0 +1,51 @@
+// Internal declarations of the text model's operators: word vectors, their gradient, products in 8-bit integers.
+// Nothing here is part of the public ABI.
+#pragma once
+
+#include <cstdint>
+
+namespace sc {
+
+struct EmbedArgs {
+    const void* table;     // [vocab][dim]
+    const void* tokens;    // [sentences][words]
+    void* out;             // [sentences][words][dim] or [sentences][dim][words]
+    long long vocab;
+    int dim, sentences, words;
+    float scale;
+    bool channels_first, wide;   // wide: 64-bit tokens
+};
+int launch_embed(int dtype, const EmbedArgs& a, void* stream);
+
+struct EmbedGradArgs {
+    const void* grad;      // as EmbedArgs::out
+    const void* tokens;
+    void* table_grad;      // [vocab][dim]
+    long long vocab, padding;
+    int dim, sentences, words;
+    float scale;
+    bool channels_first, wide, accumulate;
+    char* workspace;
+};
+long long embed_grad_workspace(const EmbedGradArgs& a, int grad_dtype);
+int launch_embed_grad(int grad_dtype, int table_dtype, const EmbedGradArgs& a, void* stream);
+
+int launch_int8_quantize(int dtype, const void* x, int8_t* q, float* scale, int rows, int K, long long ldx, void* stream);
+
+struct Int8Args {
+    const void* x;         // [M][ldx], of in_dtype
+    const float* x_scale;
+    const int8_t* w;       // [N][pitch]
+    const float* w_scale;
+    const float* bias;     // or null
+    void* out;             // [M][ldo]
+    int M, N, K;
+    int pitch;             // bytes of a row of w (and of x, where it is 8-bit)
+    long long ldx, ldo;
+    bool relu;
+    char* workspace;
+};
+long long int8_workspace(int M, int N, int K, int in_dtype, int out_dtype);
+int launch_int8_linear(int in_dtype, int out_dtype, const Int8Args& a, void* stream);
+
+}  // namespace sc

@@ -1,0 +1,433 @@
+"""Word vectors, their gradient and the fully connected layer in 8-bit integers against plain statements in 64 bits.
+
+Bounds: u is half a unit in the last place of the output type (2^-24 fp32, 2^-11 binary16, 2^-8 bfloat16), `tiny` half its
+smallest step.  lookup: one fp32 product, one rounding: (2^-24 + u) |y| + tiny.  gradient: a sum of m fp32 terms in any order and
+a product: (m + 1) 2^-24 times the sum of sizes, then u |y| + tiny.  layer: the sum is exact; its conversion, two scales and the
+bias round once each: 4 * 2^-24 (|product| + |bias|), then u |y| + tiny."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+U = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+TINY = {"f32": 2.0 ** -149, "f16": 2.0 ** -25, "bf16": 2.0 ** -134}
+
+
+def _types():
+    import torch
+    return {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+
+
+def _wide(t):
+    return t.detach().cpu().double().numpy()
+
+
+def _within(got, ref, bound, what):
+    got = _wide(got)
+    assert got.shape == ref.shape, (what, got.shape, ref.shape)
+    err = np.abs(got - ref)
+    bad = ~(err <= bound)
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.size} outside, worst {float((err - bound)[bad].max())}, first at {np.argwhere(bad)[0]}"
+
+
+def _tokens(rng, shape, vocab, kind):
+    if kind == "same":
+        return np.full(shape, vocab // 2, np.int64)
+    if kind == "outside":          # nothing of the table, at both ends and far away
+        return rng.choice(np.array([-1, -7, vocab, vocab + 3, -2 ** 31, 2 ** 31 - 1]), shape)
+    if kind == "skewed":
+        return np.minimum((vocab + 1.0) ** rng.random(shape) - 1.0, vocab - 1).astype(np.int64)
+    t = rng.integers(0, vocab, shape)
+    if kind == "mixed":            # some outside, runs of one token
+        t[rng.random(shape) < 0.2] = -1
+        t[rng.random(shape) < 0.3] = vocab - 1
+    return t
+
+
+# ---------------------------------------------------------------- lookup
+
+LOOKUPS = [  # sentences, words, vocab, dim
+    (1, 1, 5, 1), (1, 1, 7, 2048), (1, 3, 1, 7), (2, 5, 11, 8), (3, 7, 100, 300), (1, 64, 50, 33), (5, 1, 9, 16), (128, 64, 77, 300),
+    (2, 129, 33, 130), (7, 67, 500, 1001), (1, 2048, 300, 64), (3, 65, 40, 4096)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("first", [False, True])
+def test_lookup(dtype, first):
+    import torch
+    from paper_2011_06295_amd import text
+    rng = np.random.default_rng(11)
+    for i, (n, t, vocab, dim) in enumerate(LOOKUPS):
+        wide, kind = i % 2 == 0, ("uniform", "mixed", "skewed", "outside")[i % 4]
+        print(f"lookup {dtype} first={first} {n}x{t} of {vocab}x{dim} {kind} wide={wide}", flush=True)
+        table = torch.from_numpy(rng.standard_normal((vocab, dim)).astype(np.float32)).cuda().to(_types()[dtype])
+        tok = _tokens(rng, (n, t), vocab, kind)
+        scale = float(np.float32(rng.choice([1.0, 0.37, 45.25])))
+        tokens = torch.from_numpy(tok).cuda().to(torch.int64 if wide else torch.int32)
+        y = text.Embedding(table, scale=scale).forward(tokens, channels_first=first)
+        known = (tok >= 0) & (tok < vocab)
+        ref = np.where(known[..., None], _wide(table)[np.where(known, tok, 0)] * scale, 0.0)
+        if first:
+            ref = ref.transpose(0, 2, 1)[:, :, None]
+        _within(y, ref, np.abs(ref) * (U[dtype] + 2.0 ** -24) + TINY[dtype], (n, t, vocab, dim))
+
+
+def test_lookup_of_rows_and_outputs_at_odd_addresses():
+    """Table and output start one element past a multiple of 16 bytes; what lies around the output stays."""
+    import torch
+    from paper_2011_06295_amd import text
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    for dtype in _types().values():
+        for first in (False, True):
+            for dim in (8, 64, 77):
+                n, t, vocab = 3, 21, 19
+                store = torch.randn(vocab * dim + 1, generator=gen, device="cuda").to(dtype)
+                table = store[1:].reshape(vocab, dim)
+                tokens = torch.randint(0, vocab, (n, t), generator=gen, device="cuda")
+                room = torch.full((n * t * dim + 2,), 9.0, dtype=dtype, device="cuda")
+                out = room[1:-1].reshape((n, dim, 1, t) if first else (n, t, dim))
+                text.Embedding(table, scale=3.0).forward(tokens, channels_first=first, out=out)
+                want = (table.float()[tokens] * 3.0).to(dtype)
+                assert torch.equal(out, want.transpose(1, 2)[:, :, None] if first else want), (dtype, first, dim)
+                assert room[0] == 9.0 and room[-1] == 9.0
+
+
+def test_lookup_past_32_bits():
+    """Rows of a table of more than 2^32 bytes and 2^31 elements."""
+    import torch
+    from paper_2011_06295_amd import text
+    vocab, dim = 600_011, 4096
+    table = torch.zeros((vocab, dim), dtype=torch.float16, device="cuda")
+    rows = torch.tensor([0, 1, 262_144, 524_289, vocab - 1], device="cuda")
+    table[rows] = torch.arange(1, 6, device="cuda", dtype=torch.float16)[:, None]
+    for first in (False, True):
+        y = text.Embedding(table).forward(rows[None], channels_first=first)
+        y = y[:, :, 0].transpose(1, 2) if first else y
+        assert torch.equal(y, table[rows][None])
+
+
+# ---------------------------------------------------------------- gradient
+
+GRADIENTS = [  # sentences, words, vocab, dim, kind of tokens
+    (1, 1, 5, 1, "uniform"), (1, 1, 600, 2048, "uniform"), (1, 37, 100, 128, "mixed"), (2, 5, 11, 8, "outside"), (128, 64, 2000, 300, "skewed"),
+    (3, 341, 501, 101, "mixed"), (1, 700, 3, 16, "same"), (4, 1024, 513, 40, "skewed"), (5, 1000, 100, 36, "same"), (9, 1111, 70000, 12, "skewed"),
+    (2, 4097, 1025, 24, "mixed"), (1, 20000, 300, 9, "skewed"), (1, 9000, 7, 130, "uniform"), (3, 3000, 40000, 5, "outside")]
+
+
+def _gradient_reference(g, tok, vocab, dim, scale, padding):
+    """(sums, bound on the fp32 error) [vocab][dim] of token-major g."""
+    rows, tok = g.reshape(-1, dim), tok.reshape(-1)
+    keep = (tok >= 0) & (tok < vocab) & (tok != padding)
+    ref, size, count = np.zeros((vocab, dim)), np.zeros((vocab, dim)), np.zeros((vocab, 1))
+    np.add.at(ref, tok[keep], rows[keep])
+    np.add.at(size, tok[keep], np.abs(rows[keep]))
+    np.add.at(count, tok[keep], 1.0)
+    return ref * scale, (count + 1.0) * 2.0 ** -24 * size * abs(scale)
+
+
+@pytest.mark.parametrize("types", [("f32", "f32"), ("f16", "f16"), ("f16", "f32"), ("bf16", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("first", [False, True])
+def test_gradient(types, first):
+    import torch
+    from paper_2011_06295_amd import text
+    rng = np.random.default_rng(12)
+    for i, (n, t, vocab, dim, kind) in enumerate(GRADIENTS):
+        wide, padding = i % 2 == 1, None if i % 3 else vocab // 2
+        print(f"gradient {types} first={first} {n}x{t} to {vocab}x{dim} {kind} wide={wide} padding={padding}", flush=True)
+        tok = _tokens(rng, (n, t), vocab, kind)
+        g = torch.from_numpy(rng.standard_normal((n, t, dim)).astype(np.float32)).to(_types()[types[0]])
+        scale = float(np.float32(rng.choice([1.0, 0.37, 45.25])))
+        ref, bound = _gradient_reference(_wide(g), tok, vocab, dim, scale, -1 if padding is None else padding)
+        tokens = torch.from_numpy(tok).cuda().to(torch.int64 if wide else torch.int32)
+        grad = (g.transpose(1, 2)[:, :, None] if first else g).contiguous().cuda()
+        layer = text.Embedding(torch.empty((vocab, dim), dtype=_types()[types[1]], device="cuda"), scale=scale, padding=padding)
+        out = layer.backward(grad, tokens, channels_first=first)
+        _within(out, ref, bound + U[types[1]] * (np.abs(ref) + bound) + TINY[types[1]], (n, t, vocab, dim))
+        again = layer.backward(grad, tokens, channels_first=first, out=torch.full_like(out, float("nan")))
+        assert torch.equal(out, again)       # every element written, sums in one order
+
+
+@pytest.mark.parametrize("first", [False, True])
+def test_gradient_is_added(first):
+    """accumulate: rows that a token names grow, the others keep their bits (a NaN among them)."""
+    import torch
+    from paper_2011_06295_amd import text
+    rng = np.random.default_rng(13)
+    for n, t, vocab, dim in [(1, 1, 40, 8), (3, 50, 200, 77), (2, 4100, 3000, 20)]:
+        for types in (("f32", "f32"), ("f16", "f16"), ("bf16", "f32")):
+            tok = _tokens(rng, (n, t), vocab, "skewed")
+            g = torch.from_numpy(rng.standard_normal((n, t, dim)).astype(np.float32)).to(_types()[types[0]])
+            held = torch.from_numpy(rng.standard_normal((vocab, dim)).astype(np.float32)).to(_types()[types[1]])
+            ref, bound = _gradient_reference(_wide(g), tok, vocab, dim, 2.0, 1)
+            named = np.isin(np.arange(vocab), tok) & (np.arange(vocab) != 1)
+            held[torch.from_numpy(~named)] = float("nan")
+            out = held.cuda()
+            layer = text.Embedding(torch.empty_like(out), scale=2.0, padding=1)
+            layer.backward((g.transpose(1, 2)[:, :, None] if first else g).contiguous().cuda(), torch.from_numpy(tok).cuda(),
+                           channels_first=first, out=out, accumulate=True)
+            assert np.isnan(_wide(out)[~named]).all()
+            ref, bound = (ref + _wide(held))[named], bound[named]
+            bound = bound + 2.0 ** -24 * (np.abs(ref) + bound)
+            _within(out[torch.from_numpy(named).cuda()], ref, bound + U[types[1]] * (np.abs(ref) + bound) + TINY[types[1]], (n, t))
+
+
+def test_gradient_against_differences():
+    """The gradient of sum(c * lookup) by steps of the table: both are linear, so a step of one is exact up to rounding."""
+    import torch
+    from paper_2011_06295_amd import text
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    vocab, dim, n, t = 6, 5, 2, 9
+    tokens = torch.randint(0, vocab, (n, t), generator=gen, device="cuda")
+    table = torch.zeros((vocab, dim), device="cuda")
+    layer = text.Embedding(table, scale=1.5)
+    for first in (False, True):
+        c = torch.randn((n, dim, 1, t) if first else (n, t, dim), generator=gen, device="cuda")
+        grad = layer.backward(c, tokens, channels_first=first)
+        for v in range(vocab):
+            for d in range(dim):
+                table.zero_()
+                table[v, d] = 1.0
+                step = float((c.double() * layer.forward(tokens, channels_first=first).double()).sum())
+                assert abs(step - float(grad[v, d])) <= 20 * 2.0 ** -24 * 1.5 * float(c.abs().sum())
+
+
+def test_gradient_of_no_tokens_is_zero():
+    import torch
+    from paper_2011_06295_amd import text
+    layer = text.Embedding(torch.full((5, 3), 2.0, device="cuda"))
+    out = layer.backward(torch.empty((0, 3), device="cuda"), torch.empty(0, dtype=torch.int64, device="cuda"), out=torch.full((5, 3), 7.0, device="cuda"))
+    assert torch.equal(out, torch.zeros(5, 3, device="cuda"))
+    assert layer.forward(torch.empty(0, dtype=torch.int32, device="cuda")).shape == (0, 3)
+    held = torch.full((5, 3), 7.0, device="cuda")
+    layer.backward(torch.empty((0, 3), device="cuda"), torch.empty(0, dtype=torch.int64, device="cuda"), out=held, accumulate=True)
+    assert (held == 7.0).all()
+
+
+def test_infinities_and_nan_stay_in_their_row():
+    import torch
+    from paper_2011_06295_amd import text
+    for t in (30, 6000):
+        tok = torch.arange(t, device="cuda") % 10
+        g = torch.ones((t, 8), device="cuda")
+        g[3, 2], g[14, 5], g[5, 0], g[15, 0] = float("nan"), float("inf"), float("inf"), float("-inf")
+        out = text.Embedding(torch.empty((10, 8), device="cuda"), padding=3).backward(g, tok)
+        assert out[4, 5] == float("inf") and torch.isnan(out[5, 0])
+        out[4, 5] = out[5, 0] = t // 10
+        want = torch.full((10, 8), float(t // 10), device="cuda")
+        want[3] = 0.0                       # the padding's row, whose gradient holds the NaN
+        assert torch.equal(out, want), t
+
+
+# ---------------------------------------------------------------- 8-bit integers
+
+def _quantised(x):
+    """q and scale by the definition, in numpy's fp32."""
+    x = x.astype(np.float32)
+    q, scale = np.zeros(x.shape, np.int64), np.zeros(len(x), np.float32)
+    for i, row in enumerate(x):
+        a = np.abs(row).max()
+        if not np.isfinite(a):
+            scale[i] = np.nan
+        elif a >= 2.0 ** -100:
+            scale[i] = a / np.float32(127.0)
+            q[i] = np.rint(row * (np.float32(127.0) / a))
+    return q, scale
+
+
+def _rows(rng, rows, K, dtype):
+    """Rows of all sizes; among them zeros, a row below the smallest size that counts, values at ties."""
+    import torch
+    x = rng.standard_normal((rows, K)) * np.exp(rng.uniform(-9, 9, (rows, 1)))
+    x[:, rng.random(K) < 0.02] *= 20.0
+    if rows > 2:
+        x[rows // 3] = 0.0
+    if rows > 4:
+        x[rows // 2] = rng.integers(-127, 128, K) / 2.0 + 0.25
+        x[rows // 2, 0] = 127.0
+        x[rows - 1] = 1e-38 * rng.integers(-3, 4, K)
+    return torch.from_numpy(np.clip(x, -6e4, 6e4).astype(np.float32)).to(_types()[dtype])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_quantize(dtype):
+    import torch
+    from paper_2011_06295_amd import text
+    rng = np.random.default_rng(14)
+    for rows, K in [(1, 1), (3, 7), (5, 128), (6, 129), (17, 1000), (33, 4096), (7, 8200), (5, 20000), (2000, 64)]:
+        x = _rows(rng, rows, K, dtype)
+        print(f"quantize {dtype} {rows}x{K}", flush=True)
+        room = torch.zeros((rows, K + 3), dtype=x.dtype, device="cuda")
+        room[:, 1:K + 1] = x.cuda()
+        for xt in (x.cuda(), room[:, 1:K + 1]):           # whole rows; rows at odd addresses
+            q, scale = text.quantize(xt)
+            want, wscale = _quantised(x.float().numpy())
+            assert q.shape == (rows, -(-K // 128) * 128) and not q[:, K:].any()
+            assert np.array_equal(scale.cpu().numpy(), wscale) and np.array_equal(q[:, :K].cpu().numpy(), want)
+
+
+LAYERS = [  # M, K, N
+    (1, 1, 1), (1, 64, 10), (1, 1000, 129), (1, 4096, 512), (2, 127, 33), (3, 128, 300), (4, 300, 2), (5, 2048, 65), (7, 129, 1000), (8, 640, 48),
+    (13, 2900, 100), (16, 256, 256), (17, 512, 31), (24, 1024, 96), (32, 100, 640), (33, 2000, 129), (48, 384, 500), (64, 1024, 128), (65, 130, 257),
+    (100, 777, 100), (127, 512, 384), (128, 896, 255), (200, 1100, 190), (256, 256, 256), (257, 640, 513), (300, 2300, 640), (513, 200, 1025),
+    (1000, 128, 8), (1025, 1030, 270), (2048, 64, 64)]
+
+
+def _layer_reference(x, w, w_scale, bias, relu):
+    q, scale = _quantised(x)
+    product = (q.astype(np.float64) @ w.astype(np.float64).T) * scale.astype(np.float64)[:, None] * w_scale.astype(np.float64)
+    y = product + bias
+    bound = 4 * 2.0 ** -24 * (np.abs(product) + np.abs(bias))
+    return (np.maximum(y, 0.0) if relu else y), bound
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_layer(dtype):
+    import torch
+    from paper_2011_06295_amd import text
+    rng = np.random.default_rng(15)
+    for i, (M, K, N) in enumerate(LAYERS):
+        relu, biased = i % 2 == 1, i % 3 != 0
+        print(f"layer {dtype} {M}x{K} -> {N} relu={relu} bias={biased}", flush=True)
+        w = rng.integers(-128, 128, (N, K))
+        w_scale = np.exp(rng.uniform(-8, -3, N)).astype(np.float32)
+        bias = rng.standard_normal(N).astype(np.float32) if biased else np.zeros(N, np.float32)
+        x = torch.from_numpy((rng.standard_normal((M, K)) * np.exp(rng.uniform(-3, 3, (M, 1)))).astype(np.float32)).to(_types()[dtype])
+        layer = text.Int8Linear.from_quantized(torch.from_numpy(w).to(torch.int8).cuda(), torch.from_numpy(w_scale).cuda(),
+                                               torch.from_numpy(bias).cuda() if biased else None, relu=relu)
+        ref, bound = _layer_reference(x.float().numpy(), w, w_scale, bias, relu)
+        xt = x.cuda()
+        out = {"f32": "f16", "f16": "bf16", "bf16": "f32"}[dtype] if i % 5 == 4 else dtype
+        y = layer.forward(xt, dtype=_types()[out])
+        assert np.isfinite(ref[np.abs(ref) < 6e4]).all()
+        with np.errstate(over="ignore", invalid="ignore"):
+            full = bound + U[out] * (np.abs(ref) + bound) + TINY[out]
+        over = np.abs(ref) >= (65504.0 if out == "f16" else np.inf)      # past the type's largest value
+        _within(torch.where(torch.from_numpy(over).cuda(), 0.0, y.float()), np.where(over, 0.0, ref), full, (M, K, N))
+        q, scale = text.quantize(xt)
+        assert torch.equal(layer.forward_quantized(q, scale, dtype=_types()[out]), y)
+        # rows of a wider matrix, in and out; what lies between the rows stays
+        room = torch.zeros((M, K + 5), dtype=xt.dtype, device="cuda")
+        room[:, 3:K + 3] = xt
+        wide = torch.full((M, N + 3), 7.0, dtype=y.dtype, device="cuda")
+        layer.forward(room[:, 3:K + 3], out=wide[:, 1:N + 1])
+        assert torch.equal(wide[:, 1:N + 1], y) and (wide[:, :1] == 7.0).all() and (wide[:, N + 1:] == 7.0).all()
+
+
+@pytest.mark.parametrize("shape", [(1, 131071, 40), (40, 131071, 70), (300, 131071, 260)])
+def test_layer_of_the_longest_sums(shape):
+    """127 * -128 in every product: the sum nearly fills 32 bits."""
+    import torch
+    from paper_2011_06295_amd import text
+    M, K, N = shape
+    layer = text.Int8Linear.from_quantized(torch.full((N, K), -128, dtype=torch.int8, device="cuda"), torch.ones(N, device="cuda"))
+    y = layer.forward(torch.ones((M, K), device="cuda"))
+    ref = -128.0 * 127.0 * K * float(np.float32(1.0) / np.float32(127.0))
+    assert bool((y - ref).abs().max() <= 4 * 2.0 ** -24 * abs(ref))
+
+
+def test_layer_rows_that_hold_infinities_and_nan():
+    import torch
+    from paper_2011_06295_amd import text
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    for M, K, N in [(1, 200, 30), (3, 200, 30), (40, 300, 70), (150, 256, 200), (600, 256, 300)]:
+        for relu in (False, True):
+            layer = text.Int8Linear(torch.randn((N, K), generator=gen, device="cuda"), torch.randn(N, generator=gen, device="cuda"), relu=relu)
+            for dtype in _types().values():
+                x = torch.randn((M, K), generator=gen, device="cuda").to(dtype)
+                want = layer.forward(x)
+                for bad, value in ((0, float("nan")), (M // 2, float("inf")), (M - 1, float("-inf"))):
+                    x2 = x.clone()
+                    x2[bad, K // 2] = value
+                    y = layer.forward(x2)
+                    assert torch.isnan(y[bad]).all()
+                    y[bad] = want[bad]
+                    assert torch.equal(y, want)
+                if M > 2:
+                    x[1] = 0.0
+                    y = layer.forward(x)[1].float()
+                    assert torch.equal(y, (layer.bias.clamp(min=0.0) if relu else layer.bias).to(dtype).float())
+
+
+def test_layer_shapes_and_empty_batches():
+    import torch
+    from paper_2011_06295_amd import text
+    layer = text.Int8Linear(torch.randn(6, 40, device="cuda"))
+    x = torch.randn(2, 3, 40, device="cuda")
+    assert torch.equal(layer.forward(x).reshape(6, 6), layer.forward(x.reshape(6, 40)))
+    assert layer.forward(x[0, 0]).shape == (6,)
+    assert layer.forward(torch.empty((0, 40), device="cuda")).shape == (0, 6)
+
+
+# ---------------------------------------------------------------- streams, graphs, refusals
+
+def test_operators_on_another_stream_and_in_a_graph():
+    import torch
+    from paper_2011_06295_amd import text
+    gen = torch.Generator(device="cuda").manual_seed(21)
+    table = torch.randn((3000, 96), generator=gen, device="cuda")
+    emb = text.Embedding(table, scale=2.0, padding=0)
+    for n, t in ((1, 1), (4, 30), (8, 800)):
+        lin = text.Int8Linear(torch.randn((70, 96), generator=gen, device="cuda"), relu=True)
+        tokens = torch.randint(0, 3000, (n, t), generator=gen, device="cuda")
+
+        def step():
+            y = emb.forward(tokens)
+            return lin.forward(y), emb.backward(y, tokens), emb.backward(emb.forward(tokens, channels_first=True), tokens, channels_first=True)
+
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            other = step()
+            step()
+        torch.cuda.synchronize()
+        for a, b in zip(other, step()):
+            assert torch.equal(a, b)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            recorded = step()
+        for seed in range(4):
+            tokens.copy_(torch.randint(0, 3000, (n, t), generator=gen, device="cuda"))
+            graph.replay()
+            torch.cuda.synchronize()
+            want = step()
+            torch.cuda.synchronize()
+            for a, b in zip(recorded, want):
+                assert torch.equal(a, b), seed
+
+
+def test_wrappers_refuse_what_they_cannot_run():
+    import torch
+    from paper_2011_06295_amd import text
+    table = torch.zeros((10, 4), device="cuda")
+    for bad in (torch.zeros((10, 4)), table.t(), table.double(), table[0]):
+        with pytest.raises(ValueError):
+            text.Embedding(bad)
+    with pytest.raises(ValueError):
+        text.Embedding(table, padding=10)
+    emb = text.Embedding(table)
+    tokens = torch.zeros((2, 3), dtype=torch.int64, device="cuda")
+    for bad in (tokens.t(), tokens.cpu(), tokens.short(), tokens.float()):
+        with pytest.raises(ValueError):
+            emb.forward(bad)
+    with pytest.raises(ValueError):
+        emb.forward(tokens[0].contiguous(), channels_first=True)
+    with pytest.raises(ValueError):
+        emb.forward(tokens, out=torch.empty((2, 3, 5), device="cuda"))
+    for bad in (torch.zeros((2, 3, 5), device="cuda"), torch.zeros((2, 3, 4)), torch.zeros((2, 4, 3), device="cuda").transpose(1, 2)):
+        with pytest.raises(ValueError):
+            emb.backward(bad, tokens)
+    grad = torch.zeros((2, 3, 4), device="cuda")
+    with pytest.raises(ValueError):
+        emb.backward(grad, tokens, accumulate=True)
+    with pytest.raises(ValueError):
+        emb.backward(grad, tokens, out=torch.empty((10, 4), device="cuda", dtype=torch.float16))
+    layer = text.Int8Linear(torch.ones((3, 8), device="cuda"))
+    for bad in (torch.ones((2, 9), device="cuda"), torch.ones((2, 8)), torch.ones((8, 2), device="cuda").t(), torch.ones((2, 8), device="cuda").int()):
+        with pytest.raises(ValueError):
+            layer.forward(bad)
+    with pytest.raises(ValueError):
+        layer.forward(torch.ones((2, 8), device="cuda"), out=torch.empty((2, 4), device="cuda"))
+    with pytest.raises(ValueError):
+        layer.forward_quantized(torch.zeros((2, 8), dtype=torch.int8, device="cuda"), torch.ones(2, device="cuda"))
+    with pytest.raises(ValueError):
+        text.Int8Linear(torch.ones((3, 8), device="cuda"), bias=torch.ones(4, device="cuda"))
