@@ -10,44 +10,337 @@ namespace {
 
 enum { kF32 = 0, kF16 = 1, kBF16 = 2, kI8 = 3 };   // SC_F32, SC_F16, SC_BF16, SC_I8
 
-constexpr int kThreads = 256;
 constexpr float kTiny = 0x1p-100f;   // a row whose largest size is below this counts as zeros (127 / a would overflow from 2^-121)
 
-// One row a workgroup.  The largest |x| is found on the bit patterns: they order as the sizes do, and a NaN lies above all.
+// ---------------------------------------------------------------- rows to 8-bit integers
+
 template <class T>
-__global__ __launch_bounds__(kThreads) void quantize_kernel(const T* x, int8_t* q, float* scale, int K, int pitch, long long ldx)
+struct Piece {     // what one load of 16 bytes holds
+    static constexpr int kCount = 16 / sizeof(T);
+    typedef T type __attribute__((ext_vector_type(16 / sizeof(T))));
+};
+
+// Elements k .. k + kCount - 1 of a row; zeros past its end.
+template <class T>
+__device__ __forceinline__ typename Piece<T>::type load_piece(const T* row, int k, int K, bool aligned)
 {
-    __shared__ unsigned largest;
-    const size_t row = blockIdx.x;
-    x += row * ldx;
-    q += row * pitch;
-    if (threadIdx.x == 0) largest = 0;
-    __syncthreads();
-    unsigned most = 0;
-    for (int k = threadIdx.x; k < K; k += kThreads) most = max(most, __float_as_uint((float)x[k]) & 0x7fffffffu);
-    atomicMax(&largest, most);
-    __syncthreads();
-    const float a = __uint_as_float(largest);
-    const bool counts = a >= kTiny && a < INFINITY;
-    const float inv = counts ? 127.f / a : 0.f;
-    if (threadIdx.x == 0) scale[row] = counts ? a / 127.f : a < kTiny ? 0.f : NAN;
-    for (int k = threadIdx.x; k < pitch; k += kThreads) q[k] = counts && k < K ? (int8_t)(int)rintf((float)x[k] * inv) : 0;
+    typedef typename Piece<T>::type V;
+    if (aligned && k + Piece<T>::kCount <= K) return *reinterpret_cast<const V*>(row + k);
+    V v;
+#pragma unroll
+    for (int e = 0; e < Piece<T>::kCount; ++e) v[e] = k + e < K ? row[k + e] : (T)0.f;
+    return v;
 }
 
-// One output a thread.
+// The sizes of a piece as bit patterns: they order as the sizes do, and a NaN lies above all.
 template <class T>
-__global__ __launch_bounds__(kThreads) void product_kernel(Int8Args a, const int8_t* x, const float* x_scale)
+__device__ __forceinline__ unsigned largest_of(typename Piece<T>::type v, unsigned most)
 {
-    const int across = (a.N + 15) / 16;
-    const int n = (int)(blockIdx.x % across) * 16 + (threadIdx.x & 15), m = (int)(blockIdx.x / across) * 16 + (threadIdx.x >> 4);
-    if (n >= a.N || m >= a.M) return;
-    const int* xr = reinterpret_cast<const int*>(x + (size_t)m * a.pitch);
-    const int* wr = reinterpret_cast<const int*>(a.w + (size_t)n * a.pitch);
-    int sum = 0;
-    for (int k = 0; k < a.pitch / 4; ++k) sum = __builtin_amdgcn_sdot4(xr[k], wr[k], sum, false);
-    float y = (float)sum * x_scale[m] * a.w_scale[n] + (a.bias ? a.bias[n] : 0.f);
-    if (a.relu && y < 0.f) y = 0.f;
-    static_cast<T*>(a.out)[m * a.ldo + n] = (T)y;
+#pragma unroll
+    for (int e = 0; e < Piece<T>::kCount; ++e) most = max(most, __float_as_uint((float)v[e]) & 0x7fffffffu);
+    return most;
+}
+
+// The factor that takes a row to whole numbers, and its scale, from its largest size.
+__device__ __forceinline__ float scale_of(unsigned largest, float& scale)
+{
+    const float a = __uint_as_float(largest);
+    const bool counts = a >= kTiny && a < INFINITY;
+    scale = counts ? a / 127.f : a < kTiny ? 0.f : NAN;
+    return counts ? 127.f / a : 0.f;
+}
+
+// The whole numbers of a piece, four to a word.  A row that does not count has the factor 0 and gives zeros, NaN and infinities too.
+template <class T>
+__device__ __forceinline__ void quantize_piece(typename Piece<T>::type v, float factor, int (&word)[Piece<T>::kCount / 4])
+{
+#pragma unroll
+    for (int e = 0; e < Piece<T>::kCount; e += 4) {
+        int w = 0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const float y = rintf((float)v[e + c] * factor);
+            w |= (factor > 0.f ? ((int)y & 255) : 0) << (8 * c);
+        }
+        word[e / 4] = w;
+    }
+}
+
+__device__ __forceinline__ unsigned largest_in_wavefront(unsigned most)
+{
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) most = max(most, (unsigned)__shfl_xor((int)most, d));
+    return most;
+}
+
+// A row for kLanes threads (several rows a workgroup where that is one wavefront).  Up to kKept pieces a thread stay in registers
+// between the search for the largest size and the rounding; longer rows are read again.
+template <class T, int kLanes>
+__global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void quantize_kernel(const T* x, int8_t* q, float* scale, int rows, int K, int pitch, long long ldx, bool aligned)
+{
+    typedef typename Piece<T>::type V;
+    constexpr int kKept = 4, kCount = Piece<T>::kCount, kRows = kLanes < 256 ? 256 / kLanes : 1, kWaves = kLanes / 64;
+    const int t = threadIdx.x % kLanes;
+    const long long row = (long long)blockIdx.x * kRows + threadIdx.x / kLanes;
+    if (kRows > 1 && row >= rows) return;       // (a whole wavefront: no barrier follows where rows share a workgroup)
+    x += row * ldx;
+    q += row * pitch;
+    V kept[kKept];
+    unsigned most = 0;
+#pragma unroll
+    for (int p = 0; p < kKept; ++p) kept[p] = load_piece<T>(x, (p * kLanes + t) * kCount, K, aligned);
+#pragma unroll
+    for (int p = 0; p < kKept; ++p) most = largest_of<T>(kept[p], most);
+    for (int k = (kKept * kLanes + t) * kCount; k < K; k += kLanes * kCount) most = largest_of<T>(load_piece<T>(x, k, K, aligned), most);
+    most = largest_in_wavefront(most);
+    if (kWaves > 1) {
+        __shared__ unsigned of_wave[kWaves];
+        if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6] = most;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) most = max(most, of_wave[w]);
+    }
+    float s;
+    const float factor = scale_of(most, s);
+    if (t == 0) scale[row] = s;
+    auto store = [&](V v, int k) {
+        int word[kCount / 4];
+        quantize_piece<T>(v, factor, word);
+        if (kCount == 8) *reinterpret_cast<int2*>(q + k) = make_int2(word[0], word[kCount / 4 - 1]);
+        else *reinterpret_cast<int*>(q + k) = word[0];
+    };
+#pragma unroll
+    for (int p = 0; p < kKept; ++p) {
+        const int k = (p * kLanes + t) * kCount;
+        if (k < pitch) store(kept[p], k);
+    }
+    for (int k = (kKept * kLanes + t) * kCount; k < pitch; k += kLanes * kCount) store(load_piece<T>(x, k, K, aligned), k);
+}
+
+template <class T>
+int launch_quantize(const void* x, int8_t* q, float* scale, int rows, int K, long long ldx, hipStream_t s)
+{
+    const int pitch = (K + 127) / 128 * 128, pieces = pitch / Piece<T>::kCount;
+    const bool aligned = ldx * sizeof(T) % 16 == 0 && reinterpret_cast<uintptr_t>(x) % 16 == 0;
+    const T* in = static_cast<const T*>(x);
+    // one wavefront a row where a lane's pieces fit its registers; few long rows by as many threads as have a piece each
+    if (pieces <= 128 || (pieces <= 256 && rows >= 1024))
+        hipLaunchKernelGGL((quantize_kernel<T, 64>), dim3((rows + 3) / 4), dim3(256), 0, s, in, q, scale, rows, K, pitch, ldx, aligned);
+    else if (pieces <= 512 || rows >= 512)
+        hipLaunchKernelGGL((quantize_kernel<T, 256>), dim3(rows), dim3(256), 0, s, in, q, scale, rows, K, pitch, ldx, aligned);
+    else
+        hipLaunchKernelGGL((quantize_kernel<T, 1024>), dim3(rows), dim3(1024), 0, s, in, q, scale, rows, K, pitch, ldx, aligned);
+    return (int)hipGetLastError();
+}
+
+// ---------------------------------------------------------------- product, tiles through LDS
+
+typedef int int4v __attribute__((ext_vector_type(4)));
+#define SC_LDS __attribute__((address_space(3)))
+
+// 16 bytes a lane from memory to LDS at `lds` + 16 * lane; bytes past the descriptor's end arrive as zeros.  Not the builtin:
+// the compiler waits for every load of that kind before any later read of LDS, here the reads wait where they have to.
+__device__ __forceinline__ void load_to_lds(int4v descriptor, unsigned offset, unsigned base, unsigned lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" :: "s"(lds), "v"(offset), "s"(descriptor), "s"(base) : "memory");
+}
+
+// c += a * b over 16 x 16 outputs and 64 bytes: lane l holds bytes 16 * (l / 16) .. + 15 of row l % 16 of a and of b, and rows
+// 4 * (l / 16) .. + 3 of c at column l % 16.  The sums stay in accumulation registers (as a builtin they were copied and spilled).
+__device__ __forceinline__ void multiply(int4v& c, int4v a, int4v b)
+{
+    asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+}
+
+// The tile that a workgroup takes: workgroups go round the eight XCDs, so each gets a run of tiles of its own, in which eight by eight
+// tiles that share rows of x and of w are at work together.
+__device__ __forceinline__ void tile_of(unsigned block, unsigned tiles, int down, int across, int& tm, int& tn)
+{
+    const unsigned xcd = block % 8, share = tiles / 8, rest = tiles % 8;
+    const unsigned tile = xcd * share + (xcd < rest ? xcd : rest) + block / 8;
+    constexpr int kGroup = 4;
+    const unsigned per_group = kGroup * (unsigned)across, group = tile / per_group, in = tile % per_group;
+    const int rows = min(kGroup, down - (int)group * kGroup);
+    tm = (int)group * kGroup + (int)(in % (unsigned)rows);
+    tn = (int)(in / (unsigned)rows);
+}
+
+// A tile of 16 MB WM rows of x by 16 NB WN rows of w, 128 bytes of each a step; WM x WN wavefronts with MB x NB blocks of 16 x 16 sums.
+template <class T, int MB, int NB, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_product_kernel(Int8Args a, const int8_t* x, const float* x_scale, bool aligned)
+{
+    constexpr int TM = 16 * MB * WM, TN = 16 * NB * WN, W = WM * WN;
+    constexpr int kLoadsX = TM / 8 / W, kLoadsW = TN / 8 / W, kLoads = kLoadsX + kLoadsW;
+    constexpr int kX = TM * 128, kW = TN * 128, kHalf = MB / 2;
+    static_assert(MB % 2 == 0 && NB % 2 == 0, "blocks come in pairs");
+    __shared__ __attribute__((aligned(256))) char lds[2 * kX + 2 * kW];
+    __shared__ __attribute__((aligned(16))) float channel_scale[TN], channel_bias[TN], token_scale[TM];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int down = (a.M + TM - 1) / TM, across = (a.N + TN - 1) / TN;
+    int tm, tn;
+    tile_of(blockIdx.x, gridDim.x, down, across, tm, tn);
+    const int m0 = tm * TM, n0 = tn * TN;
+
+    const uint64_t xb = (uint64_t)(x + (size_t)m0 * a.pitch), wb = (uint64_t)(a.w + (size_t)n0 * a.pitch);
+    int4v from_x = {(int)xb, (int)(xb >> 32) & 0xffff, min(TM, a.M - m0) * a.pitch, 0x00020000};
+    int4v from_w = {(int)wb, (int)(wb >> 32) & 0xffff, min(TN, a.N - n0) * a.pitch, 0x00020000};
+    // A row of LDS is the 128 bytes of a row's step; its eight pieces of 16 bytes are permuted by the row, so that the 16 rows that a
+    // read takes one piece of lie in 16 different groups of four banks.  A lane's load fetches the piece that belongs where it lands.
+    unsigned offset[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        const int row = (wave * (i < kLoadsX ? kLoadsX : kLoadsW) + (i < kLoadsX ? i : i - kLoadsX)) * 8 + (lane >> 3);
+        const int turn = i < kLoadsX ? (row >> 1) & 7 : ((row >> 1) & 1) | ((row >> 3) & 3) << 1;
+        offset[i] = (unsigned)row * a.pitch + (((lane & 7) ^ turn) << 4);
+    }
+    const unsigned lds0 = (unsigned)(uintptr_t)(SC_LDS char*)lds;
+    unsigned at = 0, xdst = lds0, wdst = lds0 + 2 * kX;
+    auto load = [&](int i) {
+        if (i < kLoadsX) load_to_lds(from_x, offset[i], at, xdst + (wave * kLoadsX + i) * 1024);
+        else load_to_lds(from_w, offset[i], at, wdst + (wave * kLoadsW + i - kLoadsX) * 1024);
+    };
+    const int steps = a.pitch / 128;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load(i);
+    at += 128;
+    if (steps == 1) from_x[2] = from_w[2] = 0;      // past the last step: zeros, and nothing is fetched
+    xdst += kX;
+    wdst += kW;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load(i);
+    xdst -= kX;
+    wdst -= kW;
+
+    int4v acc[MB][NB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            acc[i][j] = int4v{0, 0, 0, 0};
+            asm volatile("" : "+a"(acc[i][j]));
+        }
+
+    // Where a lane reads: its row of block 0 and its piece; the second 64 bytes of a step are four pieces on (an exclusive or).
+    // Row r of a wavefront's block j of w stands for channel 32 (j / 2) + 8 (r / 4) + 4 (j % 2) + r % 4, so that a lane's sums of
+    // two blocks are eight channels in a row.
+    const int wm = wave % WM, wn = wave / WM, r = lane & 15, q = lane >> 4;
+    int xa0 = (wm * 16 * MB + r) * 128 + ((q ^ (r >> 1)) << 4), xa1 = xa0 ^ 64;
+    int wa0 = 2 * kX + (wn * 16 * NB + (r >> 2) * 8 + (r & 3)) * 128 + ((q ^ (r >> 1)) << 4), wa1 = wa0 ^ 64;
+    int4v wf[2][NB], xf[MB];
+    auto read_w = [&](int h, int j) { wf[h][j] = *reinterpret_cast<const int4v*>(lds + (h ? wa1 : wa0) + ((j >> 1) * 32 + (j & 1) * 4) * 128); };
+    auto read_x = [&](int h, int i) { xf[i] = *reinterpret_cast<const int4v*>(lds + (h ? xa1 : xa0) + i * 2048); };
+    asm volatile("s_waitcnt vmcnt(%0)" :: "n"(kLoads) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int j = 0; j < NB; ++j) read_w(0, j);
+#pragma unroll
+    for (int i = 0; i < kHalf; ++i) read_x(0, i);
+    __builtin_amdgcn_sched_barrier(0);
+
+    // A step is 2 MB groups of NB products, half its bytes in the first MB.  Reads run kHalf groups of x and one half of w ahead; before
+    // the last kHalf groups all that the step needs of its buffer is in registers: the next step's bytes are waited for, and the
+    // buffer is loaded again with those of the step after it.
+    int dx = kX, dw = kW;
+    for (int k = 0; k < steps; ++k) {
+        at += 128;
+        if (k + 2 >= steps) from_x[2] = from_w[2] = 0;
+#pragma unroll
+        for (int g = 0; g < 2 * MB; ++g) {
+            constexpr int kTurn = 2 * MB - kHalf;
+            const int h = g / MB, i = g % MB;
+            if (g == kTurn) {
+                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+                xa0 += dx;
+                xa1 += dx;
+                wa0 += dw;
+                wa1 += dw;
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            read_x(g < kTurn ? (g + kHalf) / MB : 0, (g + kHalf) % MB);
+            if (g < MB)
+#pragma unroll
+                for (int j = g * NB / MB; j < (g + 1) * NB / MB; ++j) read_w(1, j);
+            if (g >= kTurn) {
+#pragma unroll
+                for (int j = (g - kTurn) * NB / kHalf; j < (g - kTurn + 1) * NB / kHalf; ++j) read_w(0, j);
+#pragma unroll
+                for (int l = (g - kTurn) * kLoads / kHalf; l < (g - kTurn + 1) * kLoads / kHalf; ++l) load(l);
+            }
+#pragma unroll
+            for (int j = 0; j < NB; ++j) multiply(acc[i][j], wf[h][j], xf[i]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        xdst += dx;
+        wdst += dw;
+        dx = -dx;
+        dw = -dw;
+    }
+
+    // Scales, bias and activation.
+    for (int i = threadIdx.x; i < TN; i += 64 * W) {
+        const int n = min(n0 + i, a.N - 1);
+        channel_scale[i] = a.w_scale[n];
+        channel_bias[i] = a.bias ? a.bias[n] : 0.f;
+    }
+    for (int i = threadIdx.x; i < TM; i += 64 * W) token_scale[i] = x_scale[min(m0 + i, a.M - 1)];
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");      // (the last products are read below)
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < MB; ++i) {
+        const int tile_m = (wm * MB + i) * 16 + r, m = m0 + tile_m;
+        const float xs = token_scale[tile_m];
+        T* out = static_cast<T*>(a.out) + (size_t)m * a.ldo;
+#pragma unroll
+        for (int j = 0; j < NB; j += 2) {
+            const int tile_n = wn * 16 * NB + j * 16 + q * 8, n = n0 + tile_n;
+            T y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                asm volatile("" : "+a"(acc[i][j + e / 4]));
+                float v = (float)acc[i][j + e / 4][e % 4] * xs * channel_scale[tile_n + e] + channel_bias[tile_n + e];
+                if (a.relu && v < 0.f) v = 0.f;
+                y[e] = (T)v;
+            }
+            if (m >= a.M) continue;
+            if (aligned && n + 8 <= a.N) {
+                typedef typename Piece<T>::type V;
+                constexpr int kV = 16 / sizeof(T);
+#pragma unroll
+                for (int e = 0; e < 8; e += kV) {
+                    V v;
+#pragma unroll
+                    for (int c = 0; c < kV; ++c) v[c] = y[e + c];
+                    *reinterpret_cast<V*>(out + n + e) = v;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (n + e < a.N) out[n + e] = y[e];
+            }
+        }
+    }
+}
+
+template <class T, int MB, int NB, int WM, int WN>
+int launch_tile_product(const Int8Args& a, const int8_t* x, const float* x_scale, hipStream_t s)
+{
+    const long long tiles = ((a.M + 16ll * MB * WM - 1) / (16 * MB * WM)) * ((a.N + 16ll * NB * WN - 1) / (16 * NB * WN));
+    if (tiles >= (1ll << 31)) return (int)hipErrorInvalidValue;
+    const bool aligned = a.ldo * sizeof(T) % 16 == 0 && reinterpret_cast<uintptr_t>(a.out) % 16 == 0;
+    hipLaunchKernelGGL((tile_product_kernel<T, MB, NB, WM, WN>), dim3((unsigned)tiles), dim3(64 * WM * WN), 0, s, a, x, x_scale, aligned);
+    return (int)hipGetLastError();
+}
+
+template <class T>
+int launch_product(const Int8Args& a, const int8_t* x, const float* x_scale, hipStream_t s)
+{
+    const long long large = ((a.M + 255ll) / 256) * ((a.N + 255) / 256);
+    if (large >= 256) return launch_tile_product<T, 8, 8, 2, 2>(a, x, x_scale, s);
+    return launch_tile_product<T, 4, 4, 2, 2>(a, x, x_scale, s);
 }
 
 }  // namespace
@@ -55,14 +348,9 @@ __global__ __launch_bounds__(kThreads) void product_kernel(Int8Args a, const int
 int launch_int8_quantize(int dtype, const void* x, int8_t* q, float* scale, int rows, int K, long long ldx, void* stream)
 {
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    const int pitch = (K + 127) / 128 * 128;
-    if (dtype == kF32)
-        hipLaunchKernelGGL(quantize_kernel<float>, dim3(rows), dim3(kThreads), 0, s, static_cast<const float*>(x), q, scale, K, pitch, ldx);
-    else if (dtype == kF16)
-        hipLaunchKernelGGL(quantize_kernel<_Float16>, dim3(rows), dim3(kThreads), 0, s, static_cast<const _Float16*>(x), q, scale, K, pitch, ldx);
-    else
-        hipLaunchKernelGGL(quantize_kernel<__bf16>, dim3(rows), dim3(kThreads), 0, s, static_cast<const __bf16*>(x), q, scale, K, pitch, ldx);
-    return (int)hipGetLastError();
+    if (dtype == kF32) return launch_quantize<float>(x, q, scale, rows, K, ldx, s);
+    if (dtype == kF16) return launch_quantize<_Float16>(x, q, scale, rows, K, ldx, s);
+    return launch_quantize<__bf16>(x, q, scale, rows, K, ldx, s);
 }
 
 // The quantised input, then its scales.
@@ -84,13 +372,9 @@ int launch_int8_linear(int in_dtype, int out_dtype, const Int8Args& a, void* str
         x = q;
         x_scale = scale;
     }
-    const long long tiles = ((a.N + 15ll) / 16) * ((a.M + 15) / 16);
-    if (tiles >= (1ll << 31)) return (int)hipErrorInvalidValue;
-    const dim3 grid((unsigned)tiles);
-    if (out_dtype == kF32) hipLaunchKernelGGL(product_kernel<float>, grid, dim3(kThreads), 0, s, a, x, x_scale);
-    else if (out_dtype == kF16) hipLaunchKernelGGL(product_kernel<_Float16>, grid, dim3(kThreads), 0, s, a, x, x_scale);
-    else hipLaunchKernelGGL(product_kernel<__bf16>, grid, dim3(kThreads), 0, s, a, x, x_scale);
-    return (int)hipGetLastError();
+    if (out_dtype == kF32) return launch_product<float>(a, x, x_scale, s);
+    if (out_dtype == kF16) return launch_product<_Float16>(a, x, x_scale, s);
+    return launch_product<__bf16>(a, x, x_scale, s);
 }
 
 }  // namespace sc
