@@ -2,6 +2,8 @@
 // sparse_conv_int8_linear).
 #include <hip/hip_runtime.h>
 
+#include <utility>
+
 #include "text_ops.h"
 
 namespace sc {
@@ -138,11 +140,29 @@ int launch_quantize(const void* x, int8_t* q, float* scale, int rows, int K, lon
 typedef int int4v __attribute__((ext_vector_type(4)));
 #define SC_LDS __attribute__((address_space(3)))
 
+template <class F, int... I>
+__device__ __forceinline__ void each_of(F&& f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
+// f(0) .. f(N - 1), each with its number as a constant: loops that have to be unrolled whole, however long.
+template <int N, class F>
+__device__ __forceinline__ void each(F&& f) { each_of(f, std::make_integer_sequence<int, N>{}); }
+
 // 16 bytes a lane from memory to LDS at `lds` + 16 * lane; bytes past the descriptor's end arrive as zeros.  Not the builtin:
 // the compiler waits for every load of that kind before any later read of LDS, here the reads wait where they have to.
 __device__ __forceinline__ void load_to_lds(int4v descriptor, unsigned offset, unsigned base, unsigned lds)
 {
     asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" :: "s"(lds), "v"(offset), "s"(descriptor), "s"(base) : "memory");
+}
+
+// The same, 4 bytes a lane.
+__device__ __forceinline__ void load_word_to_lds(int4v descriptor, unsigned offset, unsigned lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dword %1, %2, 0 offen lds" :: "s"(lds), "v"(offset), "s"(descriptor) : "memory");
+}
+
+__device__ __forceinline__ int4v descriptor_of(const void* p, long long bytes)
+{
+    const uint64_t b = reinterpret_cast<uint64_t>(p);
+    return int4v{(int)b, (int)(b >> 32) & 0xffff, (int)bytes, 0x00020000};
 }
 
 // c += a * b over 16 x 16 outputs and 64 bytes: lane l holds bytes 16 * (l / 16) .. + 15 of row l % 16 of a and of b, and rows
@@ -173,6 +193,7 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_prod
     constexpr int kLoadsX = TM / 8 / W, kLoadsW = TN / 8 / W, kLoads = kLoadsX + kLoadsW;
     constexpr int kX = TM * 128, kW = TN * 128, kHalf = MB / 2;
     static_assert(MB % 2 == 0 && NB % 2 == 0, "blocks come in pairs");
+    static_assert(TM % 64 == 0 && TN % 64 == 0 && TM <= 64 * W && TN <= 64 * W, "a scale a thread");
     __shared__ __attribute__((aligned(256))) char lds[2 * kX + 2 * kW];
     __shared__ __attribute__((aligned(16))) float channel_scale[TN], channel_bias[TN], token_scale[TM];
 
@@ -182,9 +203,8 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_prod
     tile_of(blockIdx.x, gridDim.x, down, across, tm, tn);
     const int m0 = tm * TM, n0 = tn * TN;
 
-    const uint64_t xb = (uint64_t)(x + (size_t)m0 * a.pitch), wb = (uint64_t)(a.w + (size_t)n0 * a.pitch);
-    int4v from_x = {(int)xb, (int)(xb >> 32) & 0xffff, min(TM, a.M - m0) * a.pitch, 0x00020000};
-    int4v from_w = {(int)wb, (int)(wb >> 32) & 0xffff, min(TN, a.N - n0) * a.pitch, 0x00020000};
+    int4v from_x = descriptor_of(x + (size_t)m0 * a.pitch, (long long)min(TM, a.M - m0) * a.pitch);
+    int4v from_w = descriptor_of(a.w + (size_t)n0 * a.pitch, (long long)min(TN, a.N - n0) * a.pitch);
     // A row of LDS is the 128 bytes of a row's step; its eight pieces of 16 bytes are permuted by the row, so that the 16 rows that a
     // read takes one piece of lie in 16 different groups of four banks.  A lane's load fetches the piece that belongs where it lands.
     unsigned offset[kLoads];
@@ -201,6 +221,13 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_prod
         else load_to_lds(from_w, offset[i], at, wdst + (wave * kLoadsW + i - kLoadsX) * 1024);
     };
     const int steps = a.pitch / 128;
+    if (wave * 64 < TN) {
+        load_word_to_lds(descriptor_of(a.w_scale + n0, min(TN, a.N - n0) * 4ll), threadIdx.x * 4, (unsigned)(uintptr_t)(SC_LDS float*)channel_scale + wave * 256);
+        if (a.bias) load_word_to_lds(descriptor_of(a.bias + n0, min(TN, a.N - n0) * 4ll), threadIdx.x * 4, (unsigned)(uintptr_t)(SC_LDS float*)channel_bias + wave * 256);
+        else channel_bias[threadIdx.x] = 0.f;
+    }
+    if (wave * 64 < TM)
+        load_word_to_lds(descriptor_of(x_scale + m0, min(TM, a.M - m0) * 4ll), threadIdx.x * 4, (unsigned)(uintptr_t)(SC_LDS float*)token_scale + wave * 256);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) load(i);
     at += 128;
@@ -227,9 +254,9 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_prod
     const int wm = wave % WM, wn = wave / WM, r = lane & 15, q = lane >> 4;
     int xa0 = (wm * 16 * MB + r) * 128 + ((q ^ (r >> 1)) << 4), xa1 = xa0 ^ 64;
     int wa0 = 2 * kX + (wn * 16 * NB + (r >> 2) * 8 + (r & 3)) * 128 + ((q ^ (r >> 1)) << 4), wa1 = wa0 ^ 64;
-    int4v wf[2][NB], xf[MB];
+    int4v wf[2][NB], xf[2][MB];
     auto read_w = [&](int h, int j) { wf[h][j] = *reinterpret_cast<const int4v*>(lds + (h ? wa1 : wa0) + ((j >> 1) * 32 + (j & 1) * 4) * 128); };
-    auto read_x = [&](int h, int i) { xf[i] = *reinterpret_cast<const int4v*>(lds + (h ? xa1 : xa0) + i * 2048); };
+    auto read_x = [&](int h, int i) { xf[h][i] = *reinterpret_cast<const int4v*>(lds + (h ? xa1 : xa0) + i * 2048); };
     asm volatile("s_waitcnt vmcnt(%0)" :: "n"(kLoads) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
@@ -239,19 +266,39 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_prod
     for (int i = 0; i < kHalf; ++i) read_x(0, i);
     __builtin_amdgcn_sched_barrier(0);
 
-    // A step is 2 MB groups of NB products, half its bytes in the first MB.  Reads run kHalf groups of x and one half of w ahead; before
-    // the last kHalf groups all that the step needs of its buffer is in registers: the next step's bytes are waited for, and the
-    // buffer is loaded again with those of the step after it.
+    // A step is two halves of MB x NB products, 64 bytes each.  In the first, all that the second needs is read, one read every few
+    // products (a wavefront is alone on its SIMD and issues in order: reads or loads in a row leave the matrix unit without work).
+    // Then nothing reads this buffer any more and, spread over the second half, it is loaded with the bytes of the step after the next.
+    // Halfway through, those of the next step (loaded in the step before) are waited for, and the first half's operands are read.
     int dx = kX, dw = kW;
     for (int k = 0; k < steps; ++k) {
         at += 128;
         if (k + 2 >= steps) from_x[2] = from_w[2] = 0;
-#pragma unroll
-        for (int g = 0; g < 2 * MB; ++g) {
-            constexpr int kTurn = 2 * MB - kHalf;
-            const int h = g / MB, i = g % MB;
-            if (g == kTurn) {
-                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        constexpr int kSlots = MB * NB, kTurn = kSlots / 2;
+        each<kSlots>([&](auto slot) {
+            constexpr int t = slot, i = t / NB, j = t % NB, kOps = kHalf + NB + MB;
+            multiply(acc[i][j], wf[0][j], xf[0][i]);
+            constexpr int first = (t * kOps + kSlots - 1) / kSlots, last = ((t + 1) * kOps + kSlots - 1) / kSlots;
+            each<last - first>([&](auto n) {
+                constexpr int o = first + n;
+                if constexpr (o < 2 * kHalf && o % 2 == 0) read_x(0, kHalf + o / 2);
+                else {
+                    constexpr int u = o < 2 * kHalf ? o / 2 : o - kHalf;
+                    if constexpr (u < NB) read_w(1, u);
+                    else read_x(1, u - NB);
+                }
+            });
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        each<kSlots>([&](auto slot) {
+            constexpr int t = slot, i = t / NB, j = t % NB;
+            if constexpr (t == kTurn) {
+                constexpr int kIssued = (kTurn * kLoads + kSlots - 1) / kSlots;
+                asm volatile("s_waitcnt vmcnt(%0)" :: "n"(kIssued) : "memory");
                 __builtin_amdgcn_s_barrier();
                 asm volatile("" ::: "memory");
                 xa0 += dx;
@@ -260,69 +307,70 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_prod
                 wa1 += dw;
                 __builtin_amdgcn_sched_barrier(0);
             }
-            read_x(g < kTurn ? (g + kHalf) / MB : 0, (g + kHalf) % MB);
-            if (g < MB)
-#pragma unroll
-                for (int j = g * NB / MB; j < (g + 1) * NB / MB; ++j) read_w(1, j);
-            if (g >= kTurn) {
-#pragma unroll
-                for (int j = (g - kTurn) * NB / kHalf; j < (g - kTurn + 1) * NB / kHalf; ++j) read_w(0, j);
-#pragma unroll
-                for (int l = (g - kTurn) * kLoads / kHalf; l < (g - kTurn + 1) * kLoads / kHalf; ++l) load(l);
+            multiply(acc[i][j], wf[1][j], xf[1][i]);
+            constexpr int first = (t * kLoads + kSlots - 1) / kSlots, last = ((t + 1) * kLoads + kSlots - 1) / kSlots;
+            each<last - first>([&](auto n) { load(first + n); });
+            if constexpr (t >= kTurn) {
+                constexpr int kReads = NB + kHalf, kRoom = kSlots - kTurn, v = t - kTurn;
+                constexpr int from = (v * kReads + kRoom - 1) / kRoom, to = ((v + 1) * kReads + kRoom - 1) / kRoom;
+                each<to - from>([&](auto n) {
+                    constexpr int o = from + n;
+                    if constexpr (o < NB) read_w(0, o);
+                    else read_x(0, o - NB);
+                });
             }
-#pragma unroll
-            for (int j = 0; j < NB; ++j) multiply(acc[i][j], wf[h][j], xf[i]);
             __builtin_amdgcn_sched_barrier(0);
-        }
+        });
         xdst += dx;
         wdst += dw;
         dx = -dx;
         dw = -dw;
     }
 
-    // Scales, bias and activation.
-    for (int i = threadIdx.x; i < TN; i += 64 * W) {
-        const int n = min(n0 + i, a.N - 1);
-        channel_scale[i] = a.w_scale[n];
-        channel_bias[i] = a.bias ? a.bias[n] : 0.f;
-    }
-    for (int i = threadIdx.x; i < TM; i += 64 * W) token_scale[i] = x_scale[min(m0 + i, a.M - 1)];
-    asm volatile("s_waitcnt vmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");      // (the last products are read below)
-    __syncthreads();
+    // Scales, bias and activation.  The last products are read: the matrix unit's results need 18 clocks.
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");
+    float xs[MB];
 #pragma unroll
-    for (int i = 0; i < MB; ++i) {
-        const int tile_m = (wm * MB + i) * 16 + r, m = m0 + tile_m;
-        const float xs = token_scale[tile_m];
-        T* out = static_cast<T*>(a.out) + (size_t)m * a.ldo;
-#pragma unroll
-        for (int j = 0; j < NB; j += 2) {
+    for (int i = 0; i < MB; ++i) xs[i] = token_scale[(wm * MB + i) * 16 + r];
+    typedef typename Piece<T>::type V;
+    constexpr int kV = Piece<T>::kCount;
+    auto finish = [&](auto inside) {      // inside: the tile lies whole within the output, whose rows start at multiples of 16 bytes
+        each<NB / 2>([&](auto pair) {
+            constexpr int j = 2 * pair;
             const int tile_n = wn * 16 * NB + j * 16 + q * 8, n = n0 + tile_n;
-            T y[8];
+            float cs[8], cb[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                asm volatile("" : "+a"(acc[i][j + e / 4]));
-                float v = (float)acc[i][j + e / 4][e % 4] * xs * channel_scale[tile_n + e] + channel_bias[tile_n + e];
-                if (a.relu && v < 0.f) v = 0.f;
-                y[e] = (T)v;
+                cs[e] = channel_scale[tile_n + e];
+                cb[e] = channel_bias[tile_n + e];
             }
-            if (m >= a.M) continue;
-            if (aligned && n + 8 <= a.N) {
-                typedef typename Piece<T>::type V;
-                constexpr int kV = 16 / sizeof(T);
+            each<MB>([&](auto block) {
+                constexpr int i = block;
+                const int m = m0 + (wm * MB + i) * 16 + r;
+                asm volatile("" : "+a"(acc[i][j]), "+a"(acc[i][j + 1]));
+                float v[8];
 #pragma unroll
-                for (int e = 0; e < 8; e += kV) {
-                    V v;
+                for (int e = 0; e < 8; ++e) v[e] = fmaf((float)acc[i][j + e / 4][e % 4] * xs[i], cs[e], cb[e]);
+                if (a.relu)
 #pragma unroll
-                    for (int c = 0; c < kV; ++c) v[c] = y[e + c];
-                    *reinterpret_cast<V*>(out + n + e) = v;
+                    for (int e = 0; e < 8; ++e) v[e] = v[e] < 0.f ? 0.f : v[e];
+                V y[8 / kV];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e / kV][e % kV] = (T)v[e];
+                T* out = static_cast<T*>(a.out) + (size_t)m * a.ldo + n;
+                if constexpr (inside) {
+#pragma unroll
+                    for (int c = 0; c < 8 / kV; ++c) reinterpret_cast<V*>(out)[c] = y[c];
+                } else if (m < a.M) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (n + e < a.N) out[e] = y[e / kV][e % kV];
                 }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (n + e < a.N) out[n + e] = y[e];
-            }
-        }
-    }
+            });
+        });
+    };
+    if (aligned && m0 + TM <= a.M && n0 + TN <= a.N) finish(std::true_type{});
+    else finish(std::false_type{});
 }
 
 template <class T, int MB, int NB, int WM, int WN>
