@@ -383,12 +383,207 @@ int launch_tile_product(const Int8Args& a, const int8_t* x, const float* x_scale
     return (int)hipGetLastError();
 }
 
+// ---------------------------------------------------------------- product, few tokens
+
+template <class T>
+struct IsByte { static constexpr bool value = false; };
+template <>
+struct IsByte<int8_t> { static constexpr bool value = true; };
+
+// The input is quantised by every workgroup for itself where that is little beside its weights: up to this many bytes of rows.
+constexpr int kOwnBytes = 16384;
+bool quantises_itself(int M, int pitch) { return M <= 16 && (long long)M * pitch <= kOwnBytes; }
+
+// 16 MB tokens by 16 NB channels a workgroup, whose W wavefronts go round the 128-byte units of the rows and add their sums up at
+// the end.  A wavefront loads its units to a part of LDS of its own, D of them in flight, and waits for its own loads alone.  (Loads
+// in the order that the products take would touch 16 rows with 16 lanes in a row, at a quarter of the rate.)  X is int8_t, x then
+// comes the same way as w; or the type of an input that every workgroup quantises for itself while its first weights are on their way.
+template <class T, class X, int MB, int NB, int W, int D>
+__global__ __launch_bounds__(64 * W) void row_product_kernel(Int8Args a, const int8_t* x8, const float* x_scale)
+{
+    constexpr bool kGiven = IsByte<X>::value;
+    constexpr int kTokens = 16 * MB, kChannels = 16 * NB, kThreads = 64 * W;
+    constexpr int kLoadsX = kGiven ? 2 * MB : 0, kLoads = kLoadsX + 2 * NB, kUnit = 1024 * kLoads;
+    static_assert(kGiven || MB == 1, "rows that are quantised here are 16 at most");
+    static_assert(D * kUnit >= kTokens * kChannels * 4, "the sums take the place of the units");
+    __shared__ __attribute__((aligned(256))) char lds[W * D * kUnit];
+    __shared__ __attribute__((aligned(16))) char rows_of_x[kGiven ? 16 : kOwnBytes];
+    __shared__ float own_scale[16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, q = lane >> 4;
+    const int across = (a.N + kChannels - 1) / kChannels;
+    const int m0 = (int)(blockIdx.x / across) * kTokens, n0 = (int)(blockIdx.x % across) * kChannels;
+    const int units = a.pitch / 128;
+
+    // the scales and the bias of a thread's first output (most have one or none)
+    const int first_m = min(m0 + (int)threadIdx.x / kChannels, a.M - 1), first_n = min(n0 + (int)threadIdx.x % kChannels, a.N - 1);
+    const float first_scale = a.w_scale[first_n], first_bias = a.bias ? a.bias[first_n] : 0.f, first_token = kGiven ? x_scale[first_m] : 0.f;
+
+    // A thread's pieces of x, of any rows, stay in registers (their number a row is a multiple of 16: 16 lanes share a row).
+    typedef typename Piece<typename std::conditional<kGiven, float, X>::type>::type P;
+    constexpr int kCount = kGiven ? 4 : 16 / sizeof(X), kKept = kGiven ? 1 : (kOwnBytes / kCount + kThreads - 1) / kThreads;
+    P kept[kKept];
+    int m_of[kKept];
+    const int per_row = a.pitch / kCount, pieces = min(kTokens, a.M - m0) * per_row;
+    __shared__ unsigned largest[16];
+    if constexpr (!kGiven) {
+        const bool aligned = a.ldx * sizeof(X) % 16 == 0 && reinterpret_cast<uintptr_t>(a.x) % 16 == 0;
+        const X* x = static_cast<const X*>(a.x) + (size_t)m0 * a.ldx;
+        if (threadIdx.x < 16) largest[threadIdx.x] = 0;
+#pragma unroll
+        for (int i = 0; i < kKept; ++i) {
+            const int p = i * kThreads + threadIdx.x;
+            m_of[i] = p / per_row;
+            if (p < pieces) kept[i] = load_piece<X>(x + m_of[i] * a.ldx, p % per_row * kCount, a.K, aligned);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (the compiler would wait for the weights as well)
+        __syncthreads();
+    }
+
+    // Pieces of 16 bytes are permuted within the 128 bytes of a row as in the tile kernel.
+    int4v from_w = descriptor_of(a.w + (size_t)n0 * a.pitch, (long long)min(kChannels, a.N - n0) * a.pitch);
+    int4v from_x = kGiven ? descriptor_of(x8 + (size_t)m0 * a.pitch, (long long)min(kTokens, a.M - m0) * a.pitch) : from_w;
+    const int bytes_w = from_w[2], bytes_x = from_x[2];
+    const unsigned lds0 = (unsigned)(uintptr_t)(SC_LDS char*)lds + wave * D * kUnit;
+    unsigned offset[2];      // of the rows lane / 8 of an even and an odd load: their permutations differ
+#pragma unroll
+    for (int o = 0; o < 2; ++o) offset[o] = (unsigned)(o * 8 + (lane >> 3)) * a.pitch + (((lane & 7) ^ ((o * 4 + (lane >> 4)) & 7)) << 4);
+    auto load = [&](int slot, int unit) {
+        from_w[2] = unit < units ? bytes_w : 0;
+        from_x[2] = unit < units ? bytes_x : 0;
+        each<kLoads>([&](auto load) {
+            constexpr int l = load, block = l < kLoadsX ? l / 2 : (l - kLoadsX) / 2;
+            load_to_lds(l < kLoadsX ? from_x : from_w, offset[l & 1] + block * 16u * a.pitch, unit * 128, lds0 + slot * kUnit + l * 1024);
+        });
+    };
+    each<D>([&](auto d) { load(d, wave + d * W); });
+
+    if constexpr (!kGiven) {
+#pragma unroll
+        for (int i = 0; i < kKept; ++i) {
+            if ((int)(i * kThreads + threadIdx.x) >= pieces) continue;
+            unsigned most = largest_of<X>(kept[i], 0);
+#pragma unroll
+            for (int d = 8; d > 0; d /= 2) most = max(most, (unsigned)__shfl_xor((int)most, d));
+            if (r == 0) atomicMax(&largest[m_of[i]], most);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < kKept; ++i) {
+            const int p = i * kThreads + threadIdx.x;
+            if (p >= pieces) continue;
+            float s;
+            const float factor = scale_of(largest[m_of[i]], s);
+            if (p % per_row == 0) own_scale[m_of[i]] = s;
+            int word[kCount / 4];
+            quantize_piece<X>(kept[i], factor, word);
+            int* to = reinterpret_cast<int*>(rows_of_x + p * kCount);
+#pragma unroll
+            for (int c = 0; c < kCount / 4; ++c) to[c] = word[c];
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    }
+
+    int4v acc[MB][NB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[i][j] = int4v{0, 0, 0, 0};
+    const char* mine = lds + wave * D * kUnit + r * 128;
+    const int piece[2] = {(q ^ (r >> 1)) << 4, ((q + 4) ^ (r >> 1)) << 4};
+    const int my_row = min(r, a.M - m0 - 1);      // (the columns of tokens that are not there are never stored)
+    int slot = 0;
+    for (int unit = wave; unit < units; unit += W) {
+        asm volatile("s_waitcnt vmcnt(%0)" :: "n"((D - 1) * kLoads) : "memory");
+        const char* from = mine + slot * kUnit;
+        int4v wf[2][NB], xf[2][MB];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int i = 0; i < MB; ++i) {
+                if constexpr (kGiven) xf[h][i] = *reinterpret_cast<const int4v*>(from + i * 2048 + piece[h]);
+                else xf[h][i] = *reinterpret_cast<const int4v*>(rows_of_x + my_row * a.pitch + unit * 128 + h * 64 + q * 16);
+            }
+#pragma unroll
+            for (int j = 0; j < NB; ++j) wf[h][j] = *reinterpret_cast<const int4v*>(from + kLoadsX * 1024 + j * 2048 + piece[h]);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        load(slot, unit + D * W);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[h][j], xf[h][i], acc[i][j], 0, 0, 0);
+        slot = slot + 1 == D ? 0 : slot + 1;
+    }
+
+    // Sums of each wavefront where its units were: [token][channel].
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+            *reinterpret_cast<int4v*>(lds + wave * D * kUnit + ((i * 16 + r) * kChannels + j * 16 + q * 4) * 4) = acc[i][j];
+    __syncthreads();
+    auto finish = [&](int o, int m, int n, float xs, float ws, float b) {
+        int sum = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) sum += *reinterpret_cast<const int*>(lds + w * D * kUnit + o * 4);
+        float v = fmaf((float)sum * xs, ws, b);
+        if (a.relu && v < 0.f) v = 0.f;
+        static_cast<T*>(a.out)[m * a.ldo + n] = (T)v;
+    };
+    for (int o = threadIdx.x; o < kTokens * kChannels; o += kThreads) {
+        const int m = m0 + o / kChannels, n = n0 + o % kChannels;
+        if (m >= a.M || n >= a.N) continue;
+        if (o == (int)threadIdx.x) finish(o, m, n, kGiven ? first_token : own_scale[m - m0], first_scale, first_bias);
+        else finish(o, m, n, kGiven ? x_scale[m] : own_scale[m - m0], a.w_scale[n], a.bias ? a.bias[n] : 0.f);
+    }
+}
+
+template <class T, class X, int MB, int NB, int W, int D>
+int launch_row_product(const Int8Args& a, const int8_t* x, const float* x_scale, hipStream_t s)
+{
+    const long long groups = ((a.M + 16ll * MB - 1) / (16 * MB)) * ((a.N + 16ll * NB - 1) / (16 * NB));
+    if (groups >= (1ll << 31)) return (int)hipErrorInvalidValue;
+    hipLaunchKernelGGL((row_product_kernel<T, X, MB, NB, W, D>), dim3((unsigned)groups), dim3(64 * W), 0, s, a, x, x_scale);
+    return (int)hipGetLastError();
+}
+
 template <class T>
 int launch_product(const Int8Args& a, const int8_t* x, const float* x_scale, hipStream_t s)
 {
     const long long large = ((a.M + 255ll) / 256) * ((a.N + 255) / 256);
     if (large >= 256) return launch_tile_product<T, 8, 8, 2, 2>(a, x, x_scale, s);
-    return launch_tile_product<T, 4, 4, 2, 2>(a, x, x_scale, s);
+    const long long middle = ((a.M + 127ll) / 128) * ((a.N + 127) / 128);
+    if (middle >= 128 && a.M > 64) return launch_tile_product<T, 4, 4, 2, 2>(a, x, x_scale, s);
+    if (a.M <= 16) return launch_row_product<T, int8_t, 1, 1, 8, 4>(a, x, x_scale, s);
+    if (a.M <= 32) return launch_row_product<T, int8_t, 2, 1, 8, 2>(a, x, x_scale, s);
+    if (a.M <= 64) return launch_row_product<T, int8_t, 4, 1, 8, 1>(a, x, x_scale, s);
+    if (a.M <= 128) return launch_row_product<T, int8_t, 4, 2, 8, 1>(a, x, x_scale, s);
+    return launch_row_product<T, int8_t, 4, 4, 4, 2>(a, x, x_scale, s);
+}
+
+template <class T, class X>
+int launch_own(const Int8Args& a, hipStream_t s)
+{
+    if (a.N >= 16 * 1024) return launch_row_product<T, X, 1, 4, 8, 2>(a, nullptr, nullptr, s);
+    if (a.N >= 8 * 1024) return launch_row_product<T, X, 1, 2, 8, 4>(a, nullptr, nullptr, s);
+    return launch_row_product<T, X, 1, 1, 16, 4>(a, nullptr, nullptr, s);
+}
+
+template <class T>
+int launch_own(int in_dtype, const Int8Args& a, hipStream_t s)
+{
+    if (in_dtype == kF32) return launch_own<T, float>(a, s);
+    if (in_dtype == kF16) return launch_own<T, _Float16>(a, s);
+    return launch_own<T, __bf16>(a, s);
 }
 
 }  // namespace
@@ -404,7 +599,8 @@ int launch_int8_quantize(int dtype, const void* x, int8_t* q, float* scale, int 
 // The quantised input, then its scales.
 long long int8_workspace(int M, int, int K, int in_dtype, int)
 {
-    return in_dtype == kI8 ? 0 : (long long)M * ((K + 127) / 128 * 128) + (M * 4ll + 15) / 16 * 16;
+    if (in_dtype == kI8 || quantises_itself(M, (K + 127) / 128 * 128)) return 0;
+    return (long long)M * ((K + 127) / 128 * 128) + (M * 4ll + 15) / 16 * 16;
 }
 
 int launch_int8_linear(int in_dtype, int out_dtype, const Int8Args& a, void* stream)
@@ -412,6 +608,11 @@ int launch_int8_linear(int in_dtype, int out_dtype, const Int8Args& a, void* str
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const int8_t* x = static_cast<const int8_t*>(a.x);
     const float* x_scale = a.x_scale;
+    if (in_dtype != kI8 && quantises_itself(a.M, a.pitch)) {
+        if (out_dtype == kF32) return launch_own<float>(in_dtype, a, s);
+        if (out_dtype == kF16) return launch_own<_Float16>(in_dtype, a, s);
+        return launch_own<__bf16>(in_dtype, a, s);
+    }
     if (in_dtype != kI8) {
         int8_t* q = reinterpret_cast<int8_t*>(a.workspace);
         float* scale = reinterpret_cast<float*>(a.workspace + (size_t)a.M * a.pitch);
