@@ -34,13 +34,32 @@ __device__ __forceinline__ typename Piece<T>::type load_piece(const T* row, int 
     return v;
 }
 
-// The sizes of a piece as bit patterns: they order as the sizes do, and a NaN lies above all.
+// The largest size of a piece and of what came before, as a bit pattern: patterns order as the sizes do, and a NaN lies above all.
+// 16-bit types go two by two (two patterns a word until size_of).
 template <class T>
 __device__ __forceinline__ unsigned largest_of(typename Piece<T>::type v, unsigned most)
 {
+    typedef unsigned words __attribute__((ext_vector_type(4)));
+    typedef unsigned short two __attribute__((ext_vector_type(2)));
+    const words w = __builtin_bit_cast(words, v);
 #pragma unroll
-    for (int e = 0; e < Piece<T>::kCount; ++e) most = max(most, __float_as_uint((float)v[e]) & 0x7fffffffu);
+    for (int c = 0; c < 4; ++c) {
+        if constexpr (sizeof(T) == 4) most = max(most, w[c] & 0x7fffffffu);
+        else most = __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(two, w[c] & 0x7fff7fffu), __builtin_bit_cast(two, most)));
+    }
     return most;
+}
+
+// The fp32 pattern of the largest of largest_of.
+template <class T>
+__device__ __forceinline__ unsigned size_of(unsigned most)
+{
+    if constexpr (sizeof(T) == 4) {
+        return most;
+    } else {
+        const unsigned short one = (unsigned short)max(most & 0xffffu, most >> 16);
+        return __float_as_uint((float)__builtin_bit_cast(T, one));
+    }
 }
 
 // The factor that takes a row to whole numbers, and its scale, from its largest size.
@@ -52,19 +71,19 @@ __device__ __forceinline__ float scale_of(unsigned largest, float& scale)
     return counts ? 127.f / a : 0.f;
 }
 
-// The whole numbers of a piece, four to a word.  A row that does not count has the factor 0 and gives zeros, NaN and infinities too.
+// The whole numbers of a piece, four to a word.  1.5 * 2^23 added to a product of at most 127 rounds it to a whole number, ties to
+// even, and leaves that number in the low bits.  A row that does not count has the factor 0 and gives zeros.
 template <class T>
 __device__ __forceinline__ void quantize_piece(typename Piece<T>::type v, float factor, int (&word)[Piece<T>::kCount / 4])
 {
+#pragma clang fp contract(off)      // (the product is rounded before it is added to)
 #pragma unroll
     for (int e = 0; e < Piece<T>::kCount; e += 4) {
-        int w = 0;
+        unsigned y[4];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const float y = rintf((float)v[e + c] * factor);
-            w |= (factor > 0.f ? ((int)y & 255) : 0) << (8 * c);
-        }
-        word[e / 4] = w;
+        for (int c = 0; c < 4; ++c) y[c] = __float_as_uint((float)v[e + c] * factor + 0x1.8p23f);
+        const unsigned low = __builtin_amdgcn_perm(y[1], y[0], 0x0c0c0400u), high = __builtin_amdgcn_perm(y[3], y[2], 0x04000c0cu);
+        word[e / 4] = factor > 0.f ? (int)(low | high) : 0;
     }
 }
 
@@ -94,7 +113,7 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void quantize_kernel(c
 #pragma unroll
     for (int p = 0; p < kKept; ++p) most = largest_of<T>(kept[p], most);
     for (int k = (kKept * kLanes + t) * kCount; k < K; k += kLanes * kCount) most = largest_of<T>(load_piece<T>(x, k, K, aligned), most);
-    most = largest_in_wavefront(most);
+    most = largest_in_wavefront(size_of<T>(most));
     if (kWaves > 1) {
         __shared__ unsigned of_wave[kWaves];
         if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6] = most;
@@ -408,16 +427,12 @@ __global__ __launch_bounds__(64 * W) void row_product_kernel(Int8Args a, const i
     static_assert(D * kUnit >= kTokens * kChannels * 4, "the sums take the place of the units");
     __shared__ __attribute__((aligned(256))) char lds[W * D * kUnit];
     __shared__ __attribute__((aligned(16))) char rows_of_x[kGiven ? 16 : kOwnBytes];
-    __shared__ float own_scale[16];
+    __shared__ __attribute__((aligned(16))) float channel_scale[64], channel_bias[64], token_scale[64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, q = lane >> 4;
     const int across = (a.N + kChannels - 1) / kChannels;
     const int m0 = (int)(blockIdx.x / across) * kTokens, n0 = (int)(blockIdx.x % across) * kChannels;
     const int units = a.pitch / 128;
-
-    // the scales and the bias of a thread's first output (most have one or none)
-    const int first_m = min(m0 + (int)threadIdx.x / kChannels, a.M - 1), first_n = min(n0 + (int)threadIdx.x % kChannels, a.N - 1);
-    const float first_scale = a.w_scale[first_n], first_bias = a.bias ? a.bias[first_n] : 0.f, first_token = kGiven ? x_scale[first_m] : 0.f;
 
     // A thread's pieces of x, of any rows, stay in registers (their number a row is a multiple of 16: 16 lanes share a row).
     typedef typename Piece<typename std::conditional<kGiven, float, X>::type>::type P;
@@ -448,6 +463,13 @@ __global__ __launch_bounds__(64 * W) void row_product_kernel(Int8Args a, const i
     unsigned offset[2];      // of the rows lane / 8 of an even and an odd load: their permutations differ
 #pragma unroll
     for (int o = 0; o < 2; ++o) offset[o] = (unsigned)(o * 8 + (lane >> 3)) * a.pitch + (((lane & 7) ^ ((o * 4 + (lane >> 4)) & 7)) << 4);
+    if (wave == 0) load_word_to_lds(descriptor_of(a.w_scale + n0, min(kChannels, a.N - n0) * 4ll), lane * 4, (unsigned)(uintptr_t)(SC_LDS float*)channel_scale);
+    if (wave == 1) {
+        if (a.bias) load_word_to_lds(descriptor_of(a.bias + n0, min(kChannels, a.N - n0) * 4ll), lane * 4, (unsigned)(uintptr_t)(SC_LDS float*)channel_bias);
+        else channel_bias[lane] = 0.f;
+    }
+    if (kGiven && wave == 2)
+        load_word_to_lds(descriptor_of(x_scale + m0, min(kTokens, a.M - m0) * 4ll), lane * 4, (unsigned)(uintptr_t)(SC_LDS float*)token_scale);
     auto load = [&](int slot, int unit) {
         from_w[2] = unit < units ? bytes_w : 0;
         from_x[2] = unit < units ? bytes_x : 0;
@@ -462,7 +484,7 @@ __global__ __launch_bounds__(64 * W) void row_product_kernel(Int8Args a, const i
 #pragma unroll
         for (int i = 0; i < kKept; ++i) {
             if ((int)(i * kThreads + threadIdx.x) >= pieces) continue;
-            unsigned most = largest_of<X>(kept[i], 0);
+            unsigned most = size_of<X>(largest_of<X>(kept[i], 0));
 #pragma unroll
             for (int d = 8; d > 0; d /= 2) most = max(most, (unsigned)__shfl_xor((int)most, d));
             if (r == 0) atomicMax(&largest[m_of[i]], most);
@@ -476,7 +498,7 @@ __global__ __launch_bounds__(64 * W) void row_product_kernel(Int8Args a, const i
             if (p >= pieces) continue;
             float s;
             const float factor = scale_of(largest[m_of[i]], s);
-            if (p % per_row == 0) own_scale[m_of[i]] = s;
+            if (p % per_row == 0) token_scale[m_of[i]] = s;
             int word[kCount / 4];
             quantize_piece<X>(kept[i], factor, word);
             int* to = reinterpret_cast<int*>(rows_of_x + p * kCount);
@@ -531,19 +553,27 @@ __global__ __launch_bounds__(64 * W) void row_product_kernel(Int8Args a, const i
         for (int j = 0; j < NB; ++j)
             *reinterpret_cast<int4v*>(lds + wave * D * kUnit + ((i * 16 + r) * kChannels + j * 16 + q * 4) * 4) = acc[i][j];
     __syncthreads();
-    auto finish = [&](int o, int m, int n, float xs, float ws, float b) {
-        int sum = 0;
+    typedef T four __attribute__((ext_vector_type(4)));
+    const bool whole = a.ldo % 4 == 0 && reinterpret_cast<uintptr_t>(a.out) % sizeof(four) == 0 && n0 + kChannels <= a.N;
+    for (int o = threadIdx.x; o < kTokens * kChannels / 4; o += kThreads) {
+        const int token = o / (kChannels / 4), channel = o % (kChannels / 4) * 4, m = m0 + token, n = n0 + channel;
+        if (m >= a.M) continue;
+        int4v sum = {0, 0, 0, 0};
 #pragma unroll
-        for (int w = 0; w < W; ++w) sum += *reinterpret_cast<const int*>(lds + w * D * kUnit + o * 4);
-        float v = fmaf((float)sum * xs, ws, b);
-        if (a.relu && v < 0.f) v = 0.f;
-        static_cast<T*>(a.out)[m * a.ldo + n] = (T)v;
-    };
-    for (int o = threadIdx.x; o < kTokens * kChannels; o += kThreads) {
-        const int m = m0 + o / kChannels, n = n0 + o % kChannels;
-        if (m >= a.M || n >= a.N) continue;
-        if (o == (int)threadIdx.x) finish(o, m, n, kGiven ? first_token : own_scale[m - m0], first_scale, first_bias);
-        else finish(o, m, n, kGiven ? x_scale[m] : own_scale[m - m0], a.w_scale[n], a.bias ? a.bias[n] : 0.f);
+        for (int w = 0; w < W; ++w) sum += *reinterpret_cast<const int4v*>(lds + w * D * kUnit + o * 16);
+        four y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float v = fmaf((float)sum[e] * token_scale[token], channel_scale[channel + e], channel_bias[channel + e]);
+            if (a.relu && v < 0.f) v = 0.f;
+            y[e] = (T)v;
+        }
+        T* out = static_cast<T*>(a.out) + m * a.ldo + n;
+        if (whole) *reinterpret_cast<four*>(out) = y;
+        else
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (n + e < a.N) out[e] = y[e];
     }
 }
 
