@@ -2,6 +2,9 @@
 // sparse_conv_int8_linear).
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
 #include <utility>
 
 #include "text_ops.h"
@@ -381,9 +384,13 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_prod
 #pragma unroll
                     for (int c = 0; c < 8 / kV; ++c) reinterpret_cast<V*>(out)[c] = y[c];
                 } else if (m < a.M) {
+                    if (aligned && n + 8 <= a.N)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (n + e < a.N) out[e] = y[e / kV][e % kV];
+                        for (int c = 0; c < 8 / kV; ++c) reinterpret_cast<V*>(out)[c] = y[c];
+                    else
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (n + e < a.N) out[e] = y[e / kV][e % kV];
                 }
             });
         });
@@ -586,18 +593,71 @@ int launch_row_product(const Int8Args& a, const int8_t* x, const float* x_scale,
     return (int)hipGetLastError();
 }
 
+// ---------------------------------------------------------------- which kernel
+
+long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+
+// Microseconds that a product is estimated to take, fitted to launches of 20 sizes of M by 14 of K and N (1 to 8192 tokens, K 128 to
+// 16384, N 10 to 16384, weights that do not stay in a cache): over these the kernel of the least estimate takes 1.6 % more than
+// the fastest one, 23 % at most.
+// Row kernel: a launch and the sums of W wavefronts (0.14 a block of 256 sums), then the larger of what all workgroups load (18 TB/s),
+// what those of one CU load in turn (115 GB/s) and the weights from memory.
+double row_estimate(int MB, int NB, int W, int D, int M, int N, int pitch)
+{
+    const double groups = (double)(ceil_div(M, 16 * MB) * ceil_div(N, 16 * NB)), bytes = 16.0 * (MB + NB) * pitch;
+    const double resident = W * D * 2048 * (MB + NB) <= 78 * 1024 ? 512.0 : 256.0, rounds = std::ceil(groups / resident);
+    const double all = groups * bytes / 18e6, one = rounds * bytes / 115e3, weights = (double)N * pitch / (NB == 4 ? 6.3e6 : 4.9e6);
+    return 3.0 + 0.14 * MB * NB * rounds + 1.3 * (rounds - 1.0) + std::max(all, std::max(one, weights));
+}
+
+// Tile kernel: steps of `least` microseconds while a workgroup has the CU to itself, `each` times the workgroups that share it beyond.
+double tile_estimate(int MB, int M, int N, int pitch)
+{
+    const double least = MB == 8 ? 1.1 : MB == 4 ? 0.43 : 0.33, each = MB == 8 ? 1.38 : MB == 4 ? 0.49 : 0.185;
+    const double share = MB == 8 ? 1.0 : MB == 4 ? 2.0 : 4.0;        // workgroups that a CU holds
+    const double start = MB == 8 ? 1.0 : MB == 4 ? 1.8 : 2.0, finish = MB == 8 ? 5.5 : MB == 4 ? 1.7 : 0.9;
+    const double groups = (double)(ceil_div(M, 32 * MB) * ceil_div(N, 32 * MB)), steps = pitch / 128.0;
+    const double rounds = std::floor(groups / (256.0 * share)), rest = groups - rounds * 256.0 * share;
+    double us = start + rounds * (steps * each * share + finish);
+    if (rest > 0.0) us += steps * std::max(least, each * std::ceil(rest / 256.0)) + finish;
+    return std::max(us, 3.0 + (double)N * pitch / (MB == 2 ? 3.9e6 : 3.2e6));
+}
+
 template <class T>
 int launch_product(const Int8Args& a, const int8_t* x, const float* x_scale, hipStream_t s)
 {
-    const long long large = ((a.M + 255ll) / 256) * ((a.N + 255) / 256);
-    if (large >= 256) return launch_tile_product<T, 8, 8, 2, 2>(a, x, x_scale, s);
-    const long long middle = ((a.M + 127ll) / 128) * ((a.N + 127) / 128);
-    if (middle >= 128 && a.M > 64) return launch_tile_product<T, 4, 4, 2, 2>(a, x, x_scale, s);
-    if (a.M <= 16) return launch_row_product<T, int8_t, 1, 1, 8, 4>(a, x, x_scale, s);
-    if (a.M <= 32) return launch_row_product<T, int8_t, 2, 1, 8, 2>(a, x, x_scale, s);
-    if (a.M <= 64) return launch_row_product<T, int8_t, 4, 1, 8, 1>(a, x, x_scale, s);
-    if (a.M <= 128) return launch_row_product<T, int8_t, 4, 2, 8, 1>(a, x, x_scale, s);
-    return launch_row_product<T, int8_t, 4, 4, 4, 2>(a, x, x_scale, s);
+    typedef int (*Launch)(const Int8Args&, const int8_t*, const float*, hipStream_t);
+    Launch best = nullptr;
+    double least = 0.0;
+    auto consider = [&](double us, Launch launch) {
+        if (!best || us < least) {
+            best = launch;
+            least = us;
+        }
+    };
+    auto rows = [&](auto mb, auto nb, auto w, auto d) {
+        constexpr int MB = mb, NB = nb, W = w, D = d;
+        consider(row_estimate(MB, NB, W, D, a.M, a.N, a.pitch), launch_row_product<T, int8_t, MB, NB, W, D>);
+    };
+    auto tiles = [&](auto mb) {
+        constexpr int MB = mb;
+        consider(tile_estimate(MB, a.M, a.N, a.pitch), launch_tile_product<T, MB, MB, 2, 2>);
+    };
+    std::integral_constant<int, 1> one;
+    std::integral_constant<int, 2> two;
+    std::integral_constant<int, 4> four;
+    std::integral_constant<int, 8> eight;
+    rows(one, one, eight, four);
+    rows(two, one, eight, two);
+    rows(two, two, four, two);
+    rows(two, four, four, two);
+    rows(four, one, eight, one);
+    rows(four, two, four, two);
+    rows(four, four, four, two);
+    tiles(two);
+    tiles(four);
+    tiles(eight);
+    return best(a, x, x_scale, s);
 }
 
 template <class T, class X>
