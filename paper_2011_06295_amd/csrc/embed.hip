@@ -176,20 +176,25 @@ int launch_lookup(const EmbedArgs& a, hipStream_t s)
 
 // ---------------------------------------------------------------- gradient: rows of the table
 
-// A wavefront sums 512 columns of rows of grad, lane l columns 4 l .. + 3 and 256 + 4 l .. + 3 of them.
+// A wavefront sums 512 columns of rows of grad, lane l columns 4 l .. + 3 and 256 + 4 l .. + 3 of them.  A lane whose four are not all
+// there reads the last four of the row (its loads need no branch then) and stores those that are its own.
 constexpr int kColumns = 512;
 
 struct Columns {
-    int first[2], count[2];      // the lane's columns: where they start, how many of the four are there
+    int offset[2], count[2];      // where the lane reads; how many columns are its own, the last ones of those it reads
+    bool both, narrow;            // the second 256 are there; rows of less than four columns
 };
 
 __device__ __forceinline__ Columns columns_of(int block, int lane, int dim)
 {
     Columns c;
+    c.both = dim - block * kColumns > 256;
+    c.narrow = dim < 4;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-        c.first[s] = block * kColumns + s * 256 + lane * 4;
-        c.count[s] = min(max(dim - c.first[s], 0), 4);
+        const int first = block * kColumns + s * 256 + lane * 4;
+        c.count[s] = min(max(dim - first, 0), 4);
+        c.offset[s] = c.narrow ? 0 : min(first, dim - 4);
     }
     return c;
 }
@@ -214,208 +219,263 @@ struct Row {
 template <class G>
 __device__ __forceinline__ Row<G> load_row(const G* row, const Columns& c)
 {
+    typedef typename Piece<G, 4>::type V;
     Row<G> r;
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-        r.v[s] = typename Piece<G, 4>::type{};
-        if (c.count[s] > 0) r.v[s] = load_some<G, 4>(row + c.first[s], c.count[s]);
+    if (c.narrow) {
+        r.v[0] = load_some<G, 4>(row, c.count[0]);
+    } else {
+        r.v[0] = *reinterpret_cast<const V*>(row + c.offset[0]);
+        if (c.both) r.v[1] = *reinterpret_cast<const V*>(row + c.offset[1]);
     }
     return r;
 }
 
 template <class G>
-__device__ __forceinline__ void add(Sums& sums, const Row<G>& r)
+__device__ __forceinline__ void add(Sums& sums, const Row<G>& r, const Columns& c)
 {
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+    for (int e = 0; e < 4; ++e) sums.v[0][e] += (float)r.v[0][e];
+    if (c.both)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sums.v[s][e] += (float)r.v[s][e];
-}
-
-// Adds rows at(0) .. at(count - 1) in that order, eight loads ahead.
-template <class G, class At>
-__device__ __forceinline__ void add_rows(Sums& sums, int count, const Columns& c, At at)
-{
-    constexpr int kAhead = 8;
-    int i = 0;
-#pragma unroll 1
-    for (; i + kAhead <= count; i += kAhead) {
-        Row<G> r[kAhead];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) r[u] = load_row<G>(at(i + u), c);
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) add(sums, r[u]);
-    }
-    if (i < count) {
-        Row<G> r[kAhead];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (i + u < count) r[u] = load_row<G>(at(i + u), c);
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (i + u < count) add(sums, r[u]);
-    }
+        for (int e = 0; e < 4; ++e) sums.v[1][e] += (float)r.v[1][e];
 }
 
 template <class W>
 __device__ __forceinline__ void store_row(W* row, const Sums& sums, const Columns& c, float scale, bool accumulate)
 {
+    typedef typename Piece<W, 4>::type V;
     Row<W> held;
     if (accumulate) held = load_row<W>(row, c);
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-        if (c.count[s] <= 0) continue;
-        typename Piece<W, 4>::type v;
+        if (s == 1 && !c.both) break;
+        V v;
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = (W)(accumulate ? (float)held.v[s][e] + sums.v[s][e] * scale : sums.v[s][e] * scale);
-        store_some<W, 4>(row + c.first[s], v, c.count[s]);
+        W* out = row + c.offset[s];
+        if (c.count[s] == 4) {
+            *reinterpret_cast<V*>(out) = v;
+        } else if (c.count[s] > 0) {
+            const int skip = c.narrow ? 0 : 4 - c.count[s];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e >= skip && e < skip + c.count[s]) out[e] = v[e];
+        }
     }
 }
 
-// ---------------------------------------------------------------- gradient of few tokens: one launch
+constexpr int kAhead = 8;       // rows that a wavefront loads before it adds the first of them
 
-// Workgroup (b, c) owns rows b, b + gridDim.x, ... of the table (frequent tokens are often neighbours) and column block c.  It looks
-// through all tokens, keeps those of its rows in their order, and each wavefront sums the rows of its turn; a row of many tokens is
-// shared by all wavefronts, each a run of them, and joined in their order.
-constexpr int kFewTokens = 8192, kFewThreads = 1024, kFewWaves = kFewThreads / 64, kShared = 32;
-
-template <class G, class W>
-__global__ __launch_bounds__(kFewThreads) void embed_grad_few_kernel(EmbedGradArgs a, const G* grad)
+// Adds the rows that begin at grad + place_at(0) * dim .. grad + place_at(count - 1) * dim, in that order.
+template <class G, class PlaceAt>
+__device__ __forceinline__ void add_rows(Sums& sums, const G* grad, int dim, int count, const Columns& c, PlaceAt place_at)
 {
-    __shared__ int row_of[kFewTokens], place_of[kFewTokens];
-    __shared__ int counts[kFewWaves + 1];
-    __shared__ float part[kFewWaves][kColumns];
-    __shared__ int long_rows[kFewTokens / kShared + 1], long_count;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int tokens = a.sentences * a.words, groups = gridDim.x;
-    constexpr int kPasses = kFewTokens / kFewThreads;
-    const int per_wave = (tokens + kFewThreads - 1) / kFewThreads * 64;      // tokens of a wavefront, in 64s
-    // Rows are numbered within the workgroup: v = b + number * groups.
-    int number[kPasses];
-    unsigned long long mine[kPasses];
-    int count = 0;
+    const int lane = threadIdx.x & 63;
+#pragma unroll 1
+    for (int start = 0; start < count; start += 64) {
+        const int place = start + lane < count ? place_at(start + lane) : 0, here = min(count - start, 64);
+#pragma unroll 1
+        for (int i = 0; i < here; i += kAhead) {
+            Row<G> r[kAhead];
 #pragma unroll
-    for (int i = 0; i < kPasses; ++i) {
-        const int t = wave * per_wave + i * 64 + lane;
-        number[i] = -1;
-        if (i * 64 < per_wave && t < tokens) {
-            const long long v = token_at(a.tokens, a.wide, t);
-            if (v >= 0 && v < a.vocab && v != a.padding && (unsigned)v % (unsigned)groups == blockIdx.x) number[i] = (int)((unsigned)v / (unsigned)groups);
+            for (int u = 0; u < kAhead; ++u)
+                if (i + u < here) r[u] = load_row<G>(grad + (size_t)(unsigned)__builtin_amdgcn_readlane(place, i + u) * dim, c);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                if (i + u < here) add(sums, r[u], c);
         }
     }
-#pragma unroll
-    for (int i = 0; i < kPasses; ++i) {
-        mine[i] = __ballot(number[i] >= 0);
-        count += __popcll(mine[i]);
-    }
-    if (lane == 0) counts[wave] = count;
-    if (threadIdx.x == 0) long_count = 0;
-    __syncthreads();
-    int at = 0, total = 0;
-#pragma unroll
-    for (int w = 0; w < kFewWaves; ++w) {
-        at += w < wave ? counts[w] : 0;
-        total += counts[w];
-    }
-#pragma unroll
-    for (int i = 0; i < kPasses; ++i) {
-        if (number[i] >= 0) {
-            const int to = at + __popcll(mine[i] & ((1ull << lane) - 1));
-            row_of[to] = number[i];
-            place_of[to] = wave * per_wave + i * 64 + lane;
-        }
-        at += __popcll(mine[i]);
-    }
-    __syncthreads();
+}
 
-    const Columns c = columns_of(blockIdx.y, lane, a.dim);
-    W* table_grad = static_cast<W*>(a.table_grad);
-    const int rows = (int)((a.vocab - blockIdx.x + groups - 1) / groups);
-    for (int r = wave; r < rows; r += kFewWaves) {
-        int found = 0;
-        for (int j = 0; j < total; j += 64) found += __popcll(__ballot(j + lane < total && row_of[j + lane] == r));
-        if (found > kShared) {
-            if (lane == 0) long_rows[atomicAdd(&long_count, 1)] = r;
-            continue;
-        }
-        if (found == 0 && a.accumulate) continue;
-        Sums sums;
-        clear(sums);
-        for (int j = 0; found > 0; j += 64) {
-            unsigned long long match = __ballot(j + lane < total && row_of[j + lane] == r);
-            const int here = __popcll(match);
-            add_rows<G>(sums, here, c, [&](int) {
-                const int bit = __ffsll((long long)match) - 1;
-                match &= match - 1;
-                return grad + (size_t)__builtin_amdgcn_readfirstlane(place_of[j + bit]) * a.dim;
-            });
-            found -= here;
-        }
-        store_row<W>(table_grad + ((size_t)blockIdx.x + (size_t)r * groups) * a.dim, sums, c, a.scale, a.accumulate);
+// One past the last of the sorted keys that equals that of `from`: 64 probes at a time, further apart until one differs, then closer.
+template <class KeyAt>
+__device__ __forceinline__ unsigned end_of_run(KeyAt key_at, unsigned from, unsigned count)
+{
+    const int lane = threadIdx.x & 63;
+    const unsigned key = key_at(from);
+    unsigned long long last = from, step = 1;
+    auto probe = [&]() {
+        const unsigned long long at = last + (unsigned long long)(lane + 1) * step;
+        const int same = __popcll(__ballot(at < count && key_at((unsigned)min(at, (unsigned long long)count - 1)) == key));
+        last += (unsigned long long)same * step;
+        return same;
+    };
+    while (probe() == 64) step *= 64;
+    while (step > 1) {
+        step /= 64;
+        probe();
     }
+    return __builtin_amdgcn_readfirstlane((unsigned)last + 1);
+}
+
+// The runs of equal keys that begin among sorted tokens first .. first + kSlot - 1 (of `count`; keys from `none` on are no rows): their
+// rows are loaded kAhead at a time, whatever runs they belong to.  done(key, sums) for each, but longer(its first token) for one
+// of more than kLong tokens.
+constexpr int kSlot = 8, kLong = 32;
+
+template <class G, class KeyAt, class PlaceAt, class Done, class Longer>
+__device__ __forceinline__ void add_slot(const G* grad, int dim, const Columns& c, unsigned first, unsigned count, unsigned none, KeyAt key_at, PlaceAt place_at, Done done,
+                                         Longer longer)
+{
+    const int lane = threadIdx.x & 63;
+    const unsigned at = first + lane;
+    const bool there = at < count;
+    const unsigned key = there ? key_at(at) : none;
+    const int place = there ? place_at(at) : 0;
+    unsigned before = (unsigned)__shfl_up((int)key, 1);
+    if (lane == 0) before = first > 0 ? key_at(first - 1) : ~key;
+    const unsigned long long begins = __ballot(key != before), heads = begins & __ballot(key < none) & ((1ull << kSlot) - 1);
+    if (!heads) return;
+    const int from = __ffsll((long long)heads) - 1, last = 63 - __clzll((long long)heads);
+    const unsigned long long above = begins & ~((2ull << last) - 1);
+    int to = above ? __ffsll((long long)above) - 1 : 64;
+    if (!above || to - last > kLong) {
+        longer(first + last);
+        to = last;
+    }
+    Sums sums;
+    clear(sums);
+#pragma unroll 1
+    for (int i = from; i < to; i += kAhead) {
+        Row<G> r[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (i + u < to) r[u] = load_row<G>(grad + (size_t)(unsigned)__builtin_amdgcn_readlane(place, i + u) * dim, c);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (i + u < to) {
+                if (i + u > from && (begins >> (i + u) & 1)) {
+                    done((unsigned)__builtin_amdgcn_readlane((int)key, i + u - 1), sums);
+                    clear(sums);
+                }
+                add(sums, r[u], c);
+            }
+    }
+    if (from < to) done((unsigned)__builtin_amdgcn_readlane((int)key, to - 1), sums);
+}
+
+// Adds up what the wavefronts of a workgroup left in `part`, in their order; wavefront 0 goes on with the sum.
+template <int WAVES>
+__device__ __forceinline__ void join(Sums& sums, float (*part)[kColumns])
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     __syncthreads();
-    const int shared_rows = long_count;
-    for (int l = 0; l < shared_rows; ++l) {
-        const int r = long_rows[l];
-        int found = 0;
-        for (int j = 0; j < total; j += 64) found += __popcll(__ballot(j + lane < total && row_of[j + lane] == r));
-        // this wavefront's run of the row's tokens
-        const int from = (int)((long long)found * wave / kFewWaves), to = (int)((long long)found * (wave + 1) / kFewWaves);
-        Sums sums;
-        clear(sums);
-        int seen = 0;
-        for (int j = 0; j < total && seen < to; j += 64) {
-            unsigned long long match = __ballot(j + lane < total && row_of[j + lane] == r);
-            const int here = __popcll(match), skip = max(0, from - seen), keep = min(here, to - seen) - skip;
-            for (int k = 0; k < skip && match; ++k) match &= match - 1;
-            if (keep > 0)
-                add_rows<G>(sums, keep, c, [&](int) {
-                    const int bit = __ffsll((long long)match) - 1;
-                    match &= match - 1;
-                    return grad + (size_t)__builtin_amdgcn_readfirstlane(place_of[j + bit]) * a.dim;
-                });
-            seen += here;
-        }
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) part[wave][s * 256 + lane * 4 + e] = sums.v[s][e];
+    __syncthreads();
+    if (wave > 0) return;
+    clear(sums);
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w)
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) part[wave][s * 256 + lane * 4 + e] = sums.v[s][e];
-        __syncthreads();
-        if (wave == 0) {
-            clear(sums);
-            for (int w = 0; w < kFewWaves; ++w)
+            for (int e = 0; e < 4; ++e) sums.v[s][e] += part[w][s * 256 + lane * 4 + e];
+}
+
+// ---------------------------------------------------------------- gradient: channels first
+
+// [sentence][dimension][word] to rows of vectors: tile number `tile`, by the first kThreads threads of a workgroup.
+template <class G>
+__device__ __forceinline__ void turn_tile(const EmbedGradArgs& a, G* rows, unsigned number, G* tile)
+{
+    typedef Turn<G> U;
+    typedef typename U::V V;
+    size_t n;
+    int w0, d0;
+    tile_at(number, a.words, a.dim, U::kWords, U::kDims, n, w0, d0);
+    const G* grad = static_cast<const G*>(a.grad);
+    constexpr int kAlong = U::kWords / U::kVec;
+    const bool works = threadIdx.x < kThreads;
+    if (works) {
+        V piece[U::kPasses];
 #pragma unroll
-                for (int s = 0; s < 2; ++s)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) sums.v[s][e] += part[w][s * 256 + lane * 4 + e];
-            store_row<W>(table_grad + ((size_t)blockIdx.x + (size_t)r * groups) * a.dim, sums, c, a.scale, a.accumulate);
+        for (int i = 0; i < U::kPasses; ++i) {
+            const int at = i * kThreads + threadIdx.x, row = at / kAlong, w = at % kAlong * U::kVec;
+            piece[i] = V{};
+            if (d0 + row < a.dim && w0 + w < a.words) piece[i] = load_some<G, U::kVec>(grad + (n * a.dim + d0 + row) * a.words + w0 + w, a.words - w0 - w);
         }
-        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < U::kPasses; ++i) {
+            const int at = i * kThreads + threadIdx.x, row = at / kAlong, w = at % kAlong * U::kVec;
+#pragma unroll
+            for (int e = 0; e < U::kVec; ++e) tile[row * U::kPitch + w + e] = piece[i][e];
+        }
+    }
+    __syncthreads();
+    if (works) {
+        const int p = threadIdx.x & 15, d = d0 + p * U::kVec;
+#pragma unroll
+        for (int i = 0; i < U::kPasses; ++i) {
+            const int w = i * (kThreads / 16) + (threadIdx.x >> 4);
+            if (w0 + w >= a.words || d >= a.dim) continue;
+            V v;
+#pragma unroll
+            for (int e = 0; e < U::kVec; ++e) v[e] = tile[(p * U::kVec + e) * U::kPitch + w];
+            store_some<G, U::kVec>(rows + (n * a.words + w0 + w) * a.dim + d, v, a.dim - d);
+        }
     }
 }
 
-// ---------------------------------------------------------------- gradient of many tokens: a sort, then rows
+// What else a launch of the sort does, in workgroups of its own beside those that sort: it takes the few CUs of a sort a while, and
+// most of the table's gradient is zeros, which need nothing of it.
+struct Beside {
+    unsigned tiles;                       // to turn, from number 0 on
+    unsigned long long fill_from, fill;   // elements of the table's gradient to set to zero (all rows: those with tokens are written later)
+    unsigned fill_each;                   // stores of 16 bytes a thread
+};
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 
-// A stable sort of (token, place) by the token, kDigit bits a pass from the lowest on: each workgroup counts the digits of its run
-// of tokens; then each finds, from all counts, where its tokens of each digit go, and takes them there in their order.  Tokens that
-// add to no row get the number `vocab` and end up last.
-constexpr int kMaxDigit = 10, kSortThreads = 1024, kSortWaves = kSortThreads / 64;
+template <class G, class W>
+__device__ __forceinline__ void do_beside(const EmbedGradArgs& a, G* rows, const Beside& b, unsigned number, char* room)
+{
+    if (number < b.tiles) {
+        turn_tile<G>(a, rows, number, reinterpret_cast<G*>(room));
+        return;
+    }
+    constexpr int kVec = 16 / sizeof(W);
+    typedef typename Piece<W, kVec>::type V;
+    W* out = static_cast<W*>(a.table_grad) + b.fill_from;
+    const unsigned long long first = (unsigned long long)(number - b.tiles) * (kSortThreads * b.fill_each * kVec);
+    if (first + kSortThreads * b.fill_each * kVec <= b.fill) {
+#pragma unroll 4
+        for (unsigned i = 0; i < b.fill_each; ++i) *reinterpret_cast<V*>(out + first + (i * kSortThreads + threadIdx.x) * kVec) = V{};
+    } else {
+        for (unsigned i = 0; i < b.fill_each; ++i) {
+            const unsigned long long at = first + (i * kSortThreads + threadIdx.x) * kVec;
+            if (at < b.fill) store_some<W, kVec>(out + at, V{}, (int)min(b.fill - at, (unsigned long long)kVec));
+        }
+    }
+}
+
+// Workgroups for that; about two a CU fill, with 16 KB of stores each at least.
+template <class W>
+unsigned beside_blocks(Beside& b)
+{
+    const unsigned long long once = (unsigned long long)kSortThreads * (16 / sizeof(W));
+    b.fill_each = (unsigned)std::min<unsigned long long>(std::max<unsigned long long>(b.fill / (once * 512), 1), 64);
+    return b.tiles + (unsigned)((b.fill + once * b.fill_each - 1) / (once * b.fill_each));
+}
+
+// A stable sort of (token, place) by the token, `digit` bits a pass from the lowest on.  Tokens that add to no row get the number
+// `vocab` and end up last.
+constexpr int kMaxDigit = 10, kMoveEach = 2;      // tokens of a thread
 
 struct SortPlan {
-    int passes, digit, per_group, groups;     // bits a digit, tokens a workgroup
+    int passes, digit;      // bits a digit
+    int groups;             // workgroups
 };
 
-SortPlan sort_plan(long long vocab, long long tokens)
+SortPlan sort_plan(long long last, int most, long long tokens)      // of keys 0 .. last, by digits of at most `most` bits
 {
     int bits = 1;
-    while (vocab >> bits) ++bits;             // of the numbers 0 .. vocab
+    while (last >> bits) ++bits;
     SortPlan p;
-    p.passes = (bits + kMaxDigit - 1) / kMaxDigit;
+    p.passes = (bits + most - 1) / most;
     p.digit = (bits + p.passes - 1) / p.passes;
-    long long each = kSortThreads;
-    while (tokens > each * 256) each *= 2;    // (every workgroup reads the counts of all)
-    p.per_group = (int)each;
-    p.groups = (int)((tokens + each - 1) / each);
+    p.groups = (int)((tokens + kMoveEach * kSortThreads - 1) / (kMoveEach * kSortThreads));
     return p;
 }
 
@@ -425,189 +485,355 @@ __device__ __forceinline__ unsigned sort_key(const EmbedGradArgs& a, unsigned t)
     return v >= 0 && v < a.vocab && v != a.padding ? (unsigned)v : (unsigned)a.vocab;
 }
 
-// keys: null in the first pass, which reads the tokens.
-__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(EmbedGradArgs a, const unsigned* keys, int* counts, SortPlan plan, int shift)
+// The tokens of a workgroup: `each` runs of 64 a wavefront, in order.
+__device__ __forceinline__ unsigned own_token(int each, int i) { return ((threadIdx.x >> 6) * each + i) * 64 + (threadIdx.x & 63); }
+
+// rank[i]: how many tokens of this wavefront with the same digit come before token i; of_wave[wavefront][digit]: how many it has.
+template <int EACH, int BITS>
+__device__ __forceinline__ void rank_tokens(const unsigned (&key)[EACH], const bool (&there)[EACH], int each, int shift, int bits, int (*of_wave)[1 << BITS], int (&rank)[EACH])
 {
-    __shared__ int bins[1 << kMaxDigit];
-    const int size = 1 << plan.digit, tokens = a.sentences * a.words;
-    for (int d = threadIdx.x; d < size; d += kSortThreads) bins[d] = 0;
-    __syncthreads();
-    const unsigned from = blockIdx.x * (unsigned)plan.per_group, to = min((unsigned)tokens, from + (unsigned)plan.per_group);
-    for (unsigned t = from + threadIdx.x; t < to; t += kSortThreads) atomicAdd(&bins[((keys ? keys[t] : sort_key(a, t)) >> shift) & (size - 1)], 1);
-    __syncthreads();
-    for (int d = threadIdx.x; d < size; d += kSortThreads) counts[(size_t)blockIdx.x * size + d] = bins[d];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, size = 1 << bits;
+    for (int d = lane; d < size; d += 64) of_wave[wave][d] = 0;
+    volatile int* mine = of_wave[wave];       // (this wavefront's alone until the next barrier; its LDS accesses stay in order)
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        if (i >= each) break;
+        const int digit = (int)((key[i] >> shift) & (unsigned)(size - 1));
+        unsigned long long same = __ballot(there[i]);
+        for (int b = 0; b < bits; ++b) {
+            const unsigned long long set = __ballot(digit >> b & 1);
+            same &= digit >> b & 1 ? set : ~set;
+        }
+        const int before = __popcll(same & ((1ull << lane) - 1)), held = mine[digit];
+        rank[i] = held + before;
+        if (there[i] && before == 0) mine[digit] = held + __popcll(same);
+    }
 }
 
-__global__ __launch_bounds__(kSortThreads) void sort_move_kernel(EmbedGradArgs a, const unsigned* keys, const int* places, const int* counts,
-                                                                 unsigned* keys_out, int* places_out, SortPlan plan, int shift)
+// Sum of the values of the threads before this one.
+__device__ __forceinline__ int sum_before(int value, int* of_wave)
 {
-    static_assert(kSortThreads >= 1 << kMaxDigit, "a digit a thread");
-    __shared__ int of_wave[kSortWaves][1 << kMaxDigit];
-    __shared__ int wave_total[kSortWaves];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int size = 1 << plan.digit, tokens = a.sentences * a.words, digit = threadIdx.x;
-
-    // where this workgroup's first token of `digit` goes: all smaller digits, then the same digit in the workgroups before
-    int before = 0, total = 0;
-    if (digit < size)
-        for (int g = 0; g < plan.groups; ++g) {
-            const int n = counts[(size_t)g * size + digit];
-            before += g < (int)blockIdx.x ? n : 0;
-            total += n;
-        }
-    int sum = total;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int sum = value;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
         const int n = __shfl_up(sum, d);
         sum += lane >= d ? n : 0;
     }
-    if (lane == 63) wave_total[wave] = sum;
+    if (lane == 63) of_wave[wave] = sum;
     __syncthreads();
-    int base = sum - total + before;
-    for (int w = 0; w < wave; ++w) base += wave_total[w];
+    int before = sum - value;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) before += w < wave ? of_wave[w] : 0;
+    return before;
+}
 
-    const unsigned from = blockIdx.x * (unsigned)plan.per_group, to = min((unsigned)tokens, from + (unsigned)plan.per_group);
-    for (unsigned start = from; start < to; start += kSortThreads) {
-        const unsigned t = start + threadIdx.x;
-        const bool there = t < to;
-        const unsigned key = !there ? 0u : keys ? keys[t] : sort_key(a, t);
-        const int place = !there ? 0 : keys ? places[t] : (int)t;
-        const int mine = (int)((key >> shift) & (unsigned)(size - 1));
-        // the lanes of this wavefront with the same digit
-        unsigned long long same = __ballot(there);
-        for (int b = 0; b < plan.digit; ++b) {
-            const unsigned long long set = __ballot(mine >> b & 1);
-            same &= mine >> b & 1 ? set : ~set;
+// Turns the counts of a digit's wavefronts into where each begins, from `base` on.
+template <int BITS>
+__device__ __forceinline__ void spread(int (*of_wave)[1 << BITS], int digit, int base)
+{
+    int n[kSortWaves];
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) n[w] = of_wave[w][digit];
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+        of_wave[w][digit] = base;
+        base += n[w];
+    }
+}
+
+struct Sorted {
+    unsigned* keys;
+    int* places;
+};
+
+// ---------------------------------------------------------------- gradient of few tokens: one launch
+
+// Workgroup (b, c) owns the rows of the table whose number ends in b (kBuckets of them: frequent tokens are often neighbours) and
+// column block c.  It looks through all tokens, keeps those of its rows in their order, sets the rows without any to zero and sorts
+// what it kept by the row; each wavefront then takes slots of the sorted tokens, and a run of many tokens is shared by all.
+constexpr int kFewTokens = 8192, kBuckets = 256, kBucketBits = 8, kBucketDigit = 9, kMarks = 1 << 15;
+constexpr int kFewEach = kFewTokens / kSortThreads;
+
+template <class G, class W>
+__global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, const G* grad, SortPlan plan)
+{
+    __shared__ unsigned keys[kFewTokens];                  // number of the row within the bucket
+    __shared__ unsigned short places[kFewTokens];
+    __shared__ union {
+        int of_wave[kSortWaves][1 << kBucketDigit];
+        float part[kSortWaves][kColumns];
+    } room;
+    __shared__ unsigned marks[kMarks / 32];                // rows of the bucket that have tokens
+    __shared__ int counts[kSortWaves];
+    __shared__ unsigned long_runs[kFewTokens / kLong + 1];
+    __shared__ int long_count;
+    static_assert(kFewTokens <= 1 << 16, "places of 16 bits");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned tokens = (unsigned)a.sentences * a.words;
+    const int each = (int)((tokens + kSortThreads - 1) / kSortThreads);
+    const long long rows = (a.vocab - blockIdx.x + kBuckets - 1) >> kBucketBits;      // of this bucket
+
+    unsigned key[kFewEach], place[kFewEach];
+    bool there[kFewEach];
+    unsigned long long mine[kFewEach];
+    int count = 0;
+#pragma unroll
+    for (int i = 0; i < kFewEach; ++i) {
+        place[i] = own_token(each, i);
+        there[i] = i < each && place[i] < tokens;
+        key[i] = there[i] ? sort_key(a, place[i]) : (unsigned)a.vocab;
+        there[i] = key[i] < (unsigned)a.vocab && (key[i] & (kBuckets - 1)) == blockIdx.x;
+    }
+    if (threadIdx.x == 0) long_count = 0;
+    if (!a.accumulate)
+        for (int i = threadIdx.x; i < kMarks / 32; i += kSortThreads) marks[i] = 0;
+#pragma unroll
+    for (int i = 0; i < kFewEach; ++i) {
+        mine[i] = __ballot(there[i]);
+        count += __popcll(mine[i]);
+    }
+    if (lane == 0) counts[wave] = count;
+    __syncthreads();
+    int at = 0;
+    unsigned total = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+        at += w < wave ? counts[w] : 0;
+        total += counts[w];
+    }
+#pragma unroll
+    for (int i = 0; i < kFewEach; ++i) {
+        if (there[i]) {
+            const int to = at + __popcll(mine[i] & ((1ull << lane) - 1));
+            keys[to] = key[i] >> kBucketBits;
+            places[to] = (unsigned short)place[i];
+            if (!a.accumulate && (key[i] >> kBucketBits) < kMarks) atomicOr(&marks[key[i] >> (kBucketBits + 5)], 1u << (key[i] >> kBucketBits & 31));
         }
-        const int rank = __popcll(same & ((1ull << lane) - 1));
-        for (int w = 0; w < kSortWaves; ++w)
-            if (digit < size) of_wave[w][digit] = 0;
+        at += __popcll(mine[i]);
+    }
+    __syncthreads();
+
+    const Columns c = columns_of(blockIdx.y, lane, a.dim);
+    W* table_grad = static_cast<W*>(a.table_grad) + (size_t)blockIdx.x * a.dim;
+    const size_t apart = (size_t)kBuckets * a.dim;         // elements from one row of the bucket to the next
+    Sums sums;
+    if (!a.accumulate) {
+        clear(sums);
+        const int marked = (int)min(rows, (long long)kMarks);      // (more rows than marks are set to zero before this launch)
+        for (int r = wave; r < marked; r += kSortWaves)
+            if (!(marks[r >> 5] >> (r & 31) & 1)) store_row<W>(table_grad + r * apart, sums, c, 1.f, false);
+    }
+
+    // A stable sort by the key, in LDS.
+    const int kept = (int)((total + kSortThreads - 1) / kSortThreads);
+#pragma unroll
+    for (int i = 0; i < kFewEach; ++i) {
+        const unsigned t = own_token(kept, i);
+        there[i] = i < kept && t < total;
+        key[i] = there[i] ? keys[t] : 0u;
+        place[i] = there[i] ? places[t] : 0u;
+    }
+    for (int pass = 0; pass < plan.passes; ++pass) {
+        const int shift = pass * plan.digit, digit = threadIdx.x, size = 1 << plan.digit;
+        int rank[kFewEach];
+        rank_tokens<kFewEach, kBucketDigit>(key, there, kept, shift, plan.digit, room.of_wave, rank);
         __syncthreads();
-        if (there && rank == 0) of_wave[wave][mine] = __popcll(same);
-        __syncthreads();
+        int here = 0;
         if (digit < size)
-            for (int w = 0; w < kSortWaves; ++w) {
-                const int n = of_wave[w][digit];
-                of_wave[w][digit] = base;
-                base += n;
+#pragma unroll
+            for (int w = 0; w < kSortWaves; ++w) here += room.of_wave[w][digit];
+        const int base = sum_before(here, counts);
+        if (digit < size) spread<kBucketDigit>(room.of_wave, digit, base);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kFewEach; ++i)
+            if (there[i]) {
+                const int to = room.of_wave[wave][(key[i] >> shift) & (unsigned)(size - 1)] + rank[i];
+                keys[to] = key[i];
+                places[to] = (unsigned short)place[i];
             }
         __syncthreads();
-        if (there) {
-            const int at = of_wave[wave][mine] + rank;
-            keys_out[at] = key;
-            places_out[at] = place;
-        }
-        __syncthreads();
+        if (pass + 1 < plan.passes)
+#pragma unroll
+            for (int i = 0; i < kFewEach; ++i)
+                if (there[i]) {
+                    key[i] = keys[own_token(kept, i)];
+                    place[i] = places[own_token(kept, i)];
+                }
     }
+
+    auto key_at = [&](unsigned i) { return keys[i]; };
+    auto done = [&](unsigned k, const Sums& of_row) { store_row<W>(table_grad + k * apart, of_row, c, a.scale, a.accumulate); };
+    for (unsigned first = wave * kSlot; first < total; first += kSortWaves * kSlot)
+        add_slot<G>(grad, a.dim, c, first, total, ~0u, key_at, [&](unsigned i) { return (int)places[i]; }, done, [&](unsigned from) {
+            if (lane == 0) long_runs[atomicAdd(&long_count, 1)] = from;
+        });
+    __syncthreads();
+    const int shared_runs = long_count;
+    for (int l = 0; l < shared_runs; ++l) {
+        const unsigned from = __builtin_amdgcn_readfirstlane(long_runs[l]), length = end_of_run(key_at, from, total) - from;
+        const unsigned p0 = length * wave / kSortWaves, p1 = length * (wave + 1) / kSortWaves;
+        clear(sums);
+        add_rows<G>(sums, grad, a.dim, (int)(p1 - p0), c, [&](int i) { return (int)places[from + p0 + i]; });
+        join<kSortWaves>(sums, room.part);
+        if (wave == 0) done(keys[from], sums);
+    }
+}
+
+// ---------------------------------------------------------------- gradient of many tokens: a sort, windows, runs
+
+// A pass of the sort is two launches.  Each workgroup counts the digits of its run of tokens ...  (from.keys: null in the first pass, which
+// reads the tokens.)
+template <class G, class W>
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(EmbedGradArgs a, G* rows, Beside beside, SortPlan plan, int shift, Sorted from, int* counts)
+{
+    __shared__ __attribute__((aligned(16))) int bins[(sizeof(G) * Turn<G>::kDims * Turn<G>::kPitch + 3) / 4];
+    static_assert(sizeof(bins) >= sizeof(int) << kMaxDigit, "a count for each digit fits");
+    if ((int)blockIdx.x >= plan.groups) {
+        do_beside<G, W>(a, rows, beside, blockIdx.x - plan.groups, reinterpret_cast<char*>(bins));
+        return;
+    }
+    const int size = 1 << plan.digit;
+    const unsigned tokens = (unsigned)a.sentences * a.words, first = blockIdx.x * (unsigned)(kMoveEach * kSortThreads);
+    for (int d = threadIdx.x; d < size; d += kSortThreads) bins[d] = 0;
+    __syncthreads();
+    for (int i = 0; i < kMoveEach; ++i) {
+        const unsigned t = first + own_token(kMoveEach, i);
+        if (t < tokens) atomicAdd(&bins[((from.keys ? from.keys[t] : sort_key(a, t)) >> shift) & (unsigned)(size - 1)], 1);
+    }
+    __syncthreads();
+    for (int d = threadIdx.x; d < size; d += kSortThreads) counts[(size_t)blockIdx.x * size + d] = bins[d];
+}
+
+// ... then each finds, from the counts of all, where its tokens of each digit go, and takes them there in their order.
+template <class G, class W>
+__global__ __launch_bounds__(kSortThreads) void sort_move_kernel(EmbedGradArgs a, Beside beside, SortPlan plan, int shift, Sorted from, const int* counts, Sorted to)
+{
+    __shared__ int of_wave[kSortWaves][1 << kMaxDigit];
+    __shared__ int wave_sums[kSortWaves];
+    if ((int)blockIdx.x >= plan.groups) {
+        do_beside<G, W>(a, nullptr, beside, blockIdx.x - plan.groups, nullptr);
+        return;
+    }
+    constexpr int kEach = kMoveEach;
+    const int wave = threadIdx.x >> 6, size = 1 << plan.digit, digit = threadIdx.x;
+    const unsigned tokens = (unsigned)a.sentences * a.words, first = blockIdx.x * (unsigned)(kEach * kSortThreads);
+    unsigned key[kEach];
+    int place[kEach], rank[kEach];
+    bool there[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const unsigned t = first + own_token(kEach, i);
+        there[i] = t < tokens;
+        key[i] = !there[i] ? 0u : from.keys ? from.keys[t] : sort_key(a, t);
+        place[i] = !there[i] ? 0 : from.keys ? from.places[t] : (int)t;
+    }
+    // where this workgroup's first token of `digit` goes: all smaller digits, then the same digit in the workgroups before
+    int before = 0, total = 0;
+    if (digit < size) {
+        int g = 0;
+        for (; g + 16 <= plan.groups; g += 16) {
+            int n[16];
+#pragma unroll
+            for (int u = 0; u < 16; ++u) n[u] = counts[(size_t)(g + u) * size + digit];
+#pragma unroll
+            for (int u = 0; u < 16; ++u) {
+                before += g + u < (int)blockIdx.x ? n[u] : 0;
+                total += n[u];
+            }
+        }
+        for (; g < plan.groups; ++g) {
+            const int n = counts[(size_t)g * size + digit];
+            before += g < (int)blockIdx.x ? n : 0;
+            total += n;
+        }
+    }
+    rank_tokens<kEach, kMaxDigit>(key, there, kEach, shift, plan.digit, of_wave, rank);
+    const int base = sum_before(total, wave_sums) + before;
+    if (digit < size) spread<kMaxDigit>(of_wave, digit, base);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+        if (there[i]) {
+            const int at = of_wave[wave][(key[i] >> shift) & (unsigned)(size - 1)] + rank[i];
+            to.keys[at] = key[i];
+            to.places[at] = place[i];
+        }
 }
 
 // Sums of kWindow sorted tokens in a row, where they are of one row of the table.
 constexpr int kWindow = 32;
 
 template <class G>
-__global__ __launch_bounds__(kThreads) void window_kernel(EmbedGradArgs a, const G* grad, const unsigned* keys, const int* places, float* windows, int column_blocks)
+__global__ __launch_bounds__(kThreads) void window_kernel(EmbedGradArgs a, const G* grad, Sorted sorted, float* windows, int column_blocks)
 {
     const int lane = threadIdx.x & 63;
     const long long unit = (long long)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const long long w = unit / column_blocks, first = w * kWindow;
     if (first + kWindow > (long long)a.sentences * a.words) return;
-    const unsigned key = keys[first];
-    if (key != keys[first + kWindow - 1] || key >= (unsigned)a.vocab) return;
+    const unsigned key = sorted.keys[first];
+    if (key != sorted.keys[first + kWindow - 1] || key >= (unsigned)a.vocab) return;
     const Columns c = columns_of((int)(unit % column_blocks), lane, a.dim);
     Sums sums;
     clear(sums);
-    add_rows<G>(sums, kWindow, c, [&](int i) { return grad + (size_t)places[first + i] * a.dim; });
+    add_rows<G>(sums, grad, a.dim, kWindow, c, [&](int i) { return sorted.places[first + i]; });
     store_row<float>(windows + w * a.dim, sums, c, 1.f, false);
 }
 
-// The first of `count` sorted keys that is not below v.
-__device__ __forceinline__ int lower_bound(const unsigned* keys, int count, unsigned v)
-{
-    int from = 0, length = count;
-    while (length > 0) {
-        const int half = length / 2;
-        const bool below = keys[from + half] < v;
-        from = below ? from + half + 1 : from;
-        length = below ? length - half - 1 : half;
-    }
-    return from;
-}
-
-// A wavefront takes kRows rows of the table and one column block: lane l looks for the tokens of row l, then the rows go one by one.
-// Its rows are `sets` apart: frequent tokens are often neighbours.
-constexpr int kRows = 32;
+// The rows of the table that have tokens.  A wavefront takes a slot of sorted tokens; a run of many rows to add (tokens, and sums of
+// whole windows) is shared by the wavefronts of the workgroup, each a part of either, and joined in their order.
+constexpr int kRunThreads = 512, kRunWaves = kRunThreads / 64;
 
 template <class G, class W>
-__global__ __launch_bounds__(kThreads) void rows_kernel(EmbedGradArgs a, const G* grad, const unsigned* keys, const int* places, const float* windows, int column_blocks,
-                                                        unsigned sets)
+__global__ __launch_bounds__(kRunThreads) void runs_kernel(EmbedGradArgs a, const G* grad, Sorted sorted, const float* windows, int column_blocks)
 {
-    const int lane = threadIdx.x & 63, tokens = a.sentences * a.words;
-    const long long unit = (long long)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const unsigned set = (unsigned)(unit / column_blocks);
-    if (set >= sets) return;
-    // lanes 0 .. 31: where the tokens of row l begin; lanes 32 .. 63: where they end
-    const long long row = (long long)set + (long long)(lane % kRows) * sets;
-    const int bound = row < a.vocab ? lower_bound(keys, tokens, (unsigned)row + lane / kRows) : 0;
-    const Columns c = columns_of((int)(unit % column_blocks), lane, a.dim);
+    __shared__ unsigned long_runs[kRunWaves];
+    __shared__ int long_count;
+    __shared__ float part[kRunWaves][kColumns];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned tokens = (unsigned)a.sentences * a.words;
+    const unsigned first = (unsigned)(blockIdx.x / column_blocks) * (kRunWaves * kSlot) + wave * kSlot;
+    const Columns c = columns_of((int)(blockIdx.x % column_blocks), lane, a.dim);
     W* table_grad = static_cast<W*>(a.table_grad);
-    for (int r = 0; r < kRows; ++r) {
-        const long long v = (long long)set + (long long)r * sets;
-        if (v >= a.vocab) break;
-        const int from = __builtin_amdgcn_readlane(bound, r), to = __builtin_amdgcn_readlane(bound, r + kRows);
-        if (from == to && a.accumulate) continue;
+    if (threadIdx.x == 0) long_count = 0;
+    __syncthreads();
+    auto key_at = [&](unsigned i) { return sorted.keys[i]; };
+    auto done = [&](unsigned k, const Sums& of_row) { store_row<W>(table_grad + (size_t)k * a.dim, of_row, c, a.scale, a.accumulate); };
+    if (first < tokens)
+        add_slot<G>(grad, a.dim, c, first, tokens, (unsigned)a.vocab, key_at, [&](unsigned i) { return sorted.places[i]; }, done, [&](unsigned from) {
+            if (lane == 0) long_runs[atomicAdd(&long_count, 1)] = from;
+        });
+    __syncthreads();
+    const int shared_runs = long_count;
+    for (int l = 0; l < shared_runs; ++l) {
+        const unsigned from = __builtin_amdgcn_readfirstlane(long_runs[l]), to = end_of_run(key_at, from, tokens);
+        // tokens before the first whole window, whole windows, tokens after the last
+        unsigned w0 = (from + kWindow - 1) / kWindow, w1 = to / kWindow, lead = w0 * kWindow - from, rest = w1 * kWindow;
+        if (w0 >= w1) {
+            w0 = w1 = 0;
+            lead = to - from;
+            rest = to;
+        }
+        auto share = [&](unsigned n, int w) { return (unsigned)((unsigned long long)n * w / kRunWaves); };
         Sums sums;
         clear(sums);
-        const int first = (from + kWindow - 1) / kWindow, last = to / kWindow;
-        auto row_at = [&](int i) { return grad + (size_t)places[i] * a.dim; };
-        if (first < last) {
-            add_rows<G>(sums, first * kWindow - from, c, [&](int i) { return row_at(from + i); });
-            add_rows<float>(sums, last - first, c, [&](int i) { return windows + (size_t)(first + i) * a.dim; });
-            add_rows<G>(sums, to - last * kWindow, c, [&](int i) { return row_at(last * kWindow + i); });
-        } else {
-            add_rows<G>(sums, to - from, c, [&](int i) { return row_at(from + i); });
-        }
-        store_row<W>(table_grad + (size_t)v * a.dim, sums, c, a.scale, a.accumulate);
+        const unsigned l0 = share(lead, wave), l1 = share(lead, wave + 1), m0 = share(w1 - w0, wave), m1 = share(w1 - w0, wave + 1), t0 = share(to - rest, wave),
+                       t1 = share(to - rest, wave + 1);
+        add_rows<G>(sums, grad, a.dim, (int)(l1 - l0), c, [&](int i) { return sorted.places[from + l0 + i]; });
+        add_rows<float>(sums, windows, a.dim, (int)(m1 - m0), c, [&](int i) { return (int)(w0 + m0 + i); });
+        add_rows<G>(sums, grad, a.dim, (int)(t1 - t0), c, [&](int i) { return sorted.places[rest + t0 + i]; });
+        join<kRunWaves>(sums, part);
+        if (wave == 0) done(sorted.keys[from], sums);
     }
 }
 
-// ---------------------------------------------------------------- gradient: channels first
-
-// [sentence][dimension][word] to rows of vectors.
-template <class G>
-__global__ __launch_bounds__(kThreads) void turn_kernel(EmbedGradArgs a, G* rows)
+// Before a launch of few tokens: what has to be turned or, where the rows are too many to be marked, set to zero.
+template <class G, class W>
+__global__ __launch_bounds__(kSortThreads) void beside_kernel(EmbedGradArgs a, G* rows, Beside beside)
 {
-    typedef Turn<G> U;
-    typedef typename U::V V;
-    __shared__ G tile[U::kDims * U::kPitch];
-    size_t n;
-    int w0, d0;
-    tile_at(blockIdx.x, a.words, a.dim, U::kWords, U::kDims, n, w0, d0);
-    const G* grad = static_cast<const G*>(a.grad);
-    constexpr int kAlong = U::kWords / U::kVec;
-    V piece[U::kPasses];
-#pragma unroll
-    for (int i = 0; i < U::kPasses; ++i) {
-        const int at = i * kThreads + threadIdx.x, row = at / kAlong, w = at % kAlong * U::kVec;
-        piece[i] = V{};
-        if (d0 + row < a.dim && w0 + w < a.words) piece[i] = load_some<G, U::kVec>(grad + (n * a.dim + d0 + row) * a.words + w0 + w, a.words - w0 - w);
-    }
-#pragma unroll
-    for (int i = 0; i < U::kPasses; ++i) {
-        const int at = i * kThreads + threadIdx.x, row = at / kAlong, w = at % kAlong * U::kVec;
-#pragma unroll
-        for (int e = 0; e < U::kVec; ++e) tile[row * U::kPitch + w + e] = piece[i][e];
-    }
-    __syncthreads();
-    const int p = threadIdx.x & 15, d = d0 + p * U::kVec;
-#pragma unroll
-    for (int i = 0; i < U::kPasses; ++i) {
-        const int w = i * (kThreads / 16) + (threadIdx.x >> 4);
-        if (w0 + w >= a.words || d >= a.dim) continue;
-        V v;
-#pragma unroll
-        for (int e = 0; e < U::kVec; ++e) v[e] = tile[(p * U::kVec + e) * U::kPitch + w];
-        store_some<G, U::kVec>(rows + (n * a.words + w0 + w) * a.dim + d, v, a.dim - d);
-    }
+    __shared__ __attribute__((aligned(16))) char room[sizeof(G) * Turn<G>::kDims * Turn<G>::kPitch];
+    do_beside<G, W>(a, rows, beside, blockIdx.x, room);
 }
 
 int type_bytes(int dtype) { return dtype == kF32 ? 4 : 2; }
@@ -615,7 +841,7 @@ long long rounded(long long bytes) { return (bytes + 255) / 256 * 256; }
 
 // What the workspace holds, in this order.
 struct Parts {
-    long long rows, keys, counts, windows, total;      // bytes; keys: of each of two pairs of (token, place)
+    long long rows, keys, counts, windows, total;      // bytes; keys: of each of two pairs of arrays, tokens and places
 };
 
 Parts parts_of(const EmbedGradArgs& a, int grad_dtype)
@@ -624,7 +850,7 @@ Parts parts_of(const EmbedGradArgs& a, int grad_dtype)
     Parts p{};
     if (a.channels_first && a.words > 1) p.rows = rounded(tokens * a.dim * type_bytes(grad_dtype));
     if (tokens > kFewTokens) {
-        const SortPlan plan = sort_plan(a.vocab, tokens);
+        const SortPlan plan = sort_plan(a.vocab, kMaxDigit, tokens);
         p.keys = rounded(tokens * 4);
         p.counts = rounded((long long)plan.groups * (1 << plan.digit) * 4);
         p.windows = rounded(tokens / kWindow * a.dim * 4);
@@ -636,50 +862,61 @@ Parts parts_of(const EmbedGradArgs& a, int grad_dtype)
 template <class G, class W>
 int launch_grad(const EmbedGradArgs& a, const Parts& parts, hipStream_t s)
 {
-    const long long tokens = (long long)a.sentences * a.words;
+    const long long tokens = (long long)a.sentences * a.words, column_blocks = ((long long)a.dim + kColumns - 1) / kColumns;
     const G* grad = static_cast<const G*>(a.grad);
+    G* rows = reinterpret_cast<G*>(a.workspace);
+    long long tiles = 0;
     if (parts.rows) {
         typedef Turn<G> U;
-        const long long tiles = (long long)a.sentences * ((a.words + U::kWords - 1) / U::kWords) * ((a.dim + U::kDims - 1) / U::kDims);
-        if (tiles >= (1ll << 31)) return (int)hipErrorInvalidValue;
-        G* rows = reinterpret_cast<G*>(a.workspace);
-        hipLaunchKernelGGL(turn_kernel<G>, dim3((unsigned)tiles), dim3(kThreads), 0, s, a, rows);
+        tiles = (long long)a.sentences * ((a.words + U::kWords - 1) / U::kWords) * ((a.dim + U::kDims - 1) / U::kDims);
+        if (tiles >= (1ll << 30)) return (int)hipErrorInvalidValue;
         grad = rows;
     }
-    const long long column_blocks = ((long long)a.dim + kColumns - 1) / kColumns;
+    const unsigned long long elements = a.accumulate ? 0 : (unsigned long long)a.vocab * a.dim;
+    Beside beside{(unsigned)tiles, 0, elements, 1};
     if (tokens <= kFewTokens) {
         if (column_blocks > 65535) return (int)hipErrorInvalidValue;
-        const unsigned groups = (unsigned)std::min<long long>(a.vocab, 256);
-        hipLaunchKernelGGL((embed_grad_few_kernel<G, W>), dim3(groups, (unsigned)column_blocks), dim3(kFewThreads), 0, s, a, grad);
+        if (a.vocab <= (long long)kMarks * kBuckets) beside.fill = 0;
+        const unsigned blocks = beside_blocks<W>(beside);
+        if (blocks) hipLaunchKernelGGL((beside_kernel<G, W>), dim3(blocks), dim3(kSortThreads), 0, s, a, rows, beside);
+        const SortPlan plan = sort_plan((a.vocab - 1) >> kBucketBits, kBucketDigit, tokens);
+        const unsigned groups = (unsigned)std::min<long long>(a.vocab, kBuckets);
+        hipLaunchKernelGGL((bucket_kernel<G, W>), dim3(groups, (unsigned)column_blocks), dim3(kSortThreads), 0, s, a, grad, plan);
         return (int)hipGetLastError();
     }
-    const SortPlan plan = sort_plan(a.vocab, tokens);
+    const SortPlan plan = sort_plan(a.vocab, kMaxDigit, tokens);
+    const long long run_blocks = ((tokens + kRunWaves * kSlot - 1) / (kRunWaves * kSlot)) * column_blocks;
+    if (run_blocks >= (1ll << 31)) return (int)hipErrorInvalidValue;
     char* at = a.workspace + parts.rows;
-    unsigned* keys[2];
-    int* places[2];
+    Sorted sorted[2];
     for (int i = 0; i < 2; ++i) {
-        keys[i] = reinterpret_cast<unsigned*>(at);
-        places[i] = reinterpret_cast<int*>(at + parts.keys);
+        sorted[i].keys = reinterpret_cast<unsigned*>(at);
+        sorted[i].places = reinterpret_cast<int*>(at + parts.keys);
         at += 2 * parts.keys;
     }
     int* counts = reinterpret_cast<int*>(at);
     float* windows = reinterpret_cast<float*>(at + parts.counts);
-    const unsigned *from = nullptr;
-    const int* from_places = nullptr;
-    for (int pass = 0; pass < plan.passes; ++pass) {
-        hipLaunchKernelGGL(sort_count_kernel, dim3(plan.groups), dim3(kSortThreads), 0, s, a, from, counts, plan, pass * plan.digit);
-        hipLaunchKernelGGL(sort_move_kernel, dim3(plan.groups), dim3(kSortThreads), 0, s, a, from, from_places, counts, keys[pass & 1], places[pass & 1], plan,
-                           pass * plan.digit);
-        from = keys[pass & 1];
-        from_places = places[pass & 1];
+    Sorted from{nullptr, nullptr};
+    const int launches = 2 * plan.passes;
+    for (int l = 0; l < launches; ++l) {
+        const unsigned long long kVec = 16 / sizeof(W), end = l + 1 == launches ? elements : elements * (l + 1) / launches / kVec * kVec;
+        beside.fill = end - beside.fill_from;
+        const int shift = l / 2 * plan.digit;
+        const dim3 grid(plan.groups + beside_blocks<W>(beside));
+        if (l % 2 == 0) {
+            hipLaunchKernelGGL((sort_count_kernel<G, W>), grid, dim3(kSortThreads), 0, s, a, rows, beside, plan, shift, from, counts);
+        } else {
+            hipLaunchKernelGGL((sort_move_kernel<G, W>), grid, dim3(kSortThreads), 0, s, a, beside, plan, shift, from, counts, sorted[l / 2 & 1]);
+            from = sorted[l / 2 & 1];
+        }
+        beside.tiles = 0;
+        beside.fill_from = end;
     }
     constexpr int kWaves = kThreads / 64;
-    const long long window_units = tokens / kWindow * column_blocks, sets = (a.vocab + kRows - 1) / kRows, row_units = sets * column_blocks;
-    if ((window_units + kWaves - 1) / kWaves >= (1ll << 31) || (row_units + kWaves - 1) / kWaves >= (1ll << 31)) return (int)hipErrorInvalidValue;
-    hipLaunchKernelGGL(window_kernel<G>, dim3((unsigned)((window_units + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, a, grad, from, from_places, windows,
-                       (int)column_blocks);
-    hipLaunchKernelGGL((rows_kernel<G, W>), dim3((unsigned)((row_units + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, a, grad, from, from_places, windows,
-                       (int)column_blocks, (unsigned)sets);
+    const long long window_blocks = (tokens / kWindow * column_blocks + kWaves - 1) / kWaves;
+    if (window_blocks >= (1ll << 31)) return (int)hipErrorInvalidValue;
+    hipLaunchKernelGGL(window_kernel<G>, dim3((unsigned)window_blocks), dim3(kThreads), 0, s, a, grad, from, windows, (int)column_blocks);
+    hipLaunchKernelGGL((runs_kernel<G, W>), dim3((unsigned)run_blocks), dim3(kRunThreads), 0, s, a, grad, from, static_cast<const float*>(windows), (int)column_blocks);
     return (int)hipGetLastError();
 }
 
