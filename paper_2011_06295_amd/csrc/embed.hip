@@ -28,6 +28,12 @@ __device__ __forceinline__ long long token_at(const void* tokens, bool wide, siz
     return wide ? static_cast<const long long*>(tokens)[i] : static_cast<const int*>(tokens)[i];
 }
 
+// A barrier for what the wavefronts of a workgroup exchange through LDS; stores to memory may still be on their way.
+__device__ __forceinline__ void lds_barrier()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
 template <class T, int VEC>
 __device__ __forceinline__ typename Piece<T, VEC>::type scaled(typename Piece<T, VEC>::type v, float scale)
 {
@@ -359,12 +365,12 @@ template <int WAVES>
 __device__ __forceinline__ void join(Sums& sums, float (*part)[kColumns])
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    __syncthreads();
+    lds_barrier();
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int e = 0; e < 4; ++e) part[wave][s * 256 + lane * 4 + e] = sums.v[s][e];
-    __syncthreads();
+    lds_barrier();
     if (wave > 0) return;
     clear(sums);
 #pragma unroll
@@ -377,39 +383,41 @@ __device__ __forceinline__ void join(Sums& sums, float (*part)[kColumns])
 
 // ---------------------------------------------------------------- gradient: channels first
 
-// [sentence][dimension][word] to rows of vectors: tile number `tile`, by the first kThreads threads of a workgroup.
+// [sentence][dimension][word] to rows of vectors: each kThreads threads of a workgroup turn a tile, number, number + 1, ... (of `tiles`).
 template <class G>
-__device__ __forceinline__ void turn_tile(const EmbedGradArgs& a, G* rows, unsigned number, G* tile)
+__device__ __forceinline__ void turn_tiles(const EmbedGradArgs& a, G* rows, unsigned number, unsigned tiles, G* room)
 {
     typedef Turn<G> U;
     typedef typename U::V V;
+    const int thread = threadIdx.x % kThreads, part = threadIdx.x / kThreads;
+    G* tile = room + part * U::kDims * U::kPitch;
+    const bool works = number + part < tiles;
     size_t n;
     int w0, d0;
-    tile_at(number, a.words, a.dim, U::kWords, U::kDims, n, w0, d0);
+    tile_at(number + part, a.words, a.dim, U::kWords, U::kDims, n, w0, d0);
     const G* grad = static_cast<const G*>(a.grad);
     constexpr int kAlong = U::kWords / U::kVec;
-    const bool works = threadIdx.x < kThreads;
     if (works) {
         V piece[U::kPasses];
 #pragma unroll
         for (int i = 0; i < U::kPasses; ++i) {
-            const int at = i * kThreads + threadIdx.x, row = at / kAlong, w = at % kAlong * U::kVec;
+            const int at = i * kThreads + thread, row = at / kAlong, w = at % kAlong * U::kVec;
             piece[i] = V{};
             if (d0 + row < a.dim && w0 + w < a.words) piece[i] = load_some<G, U::kVec>(grad + (n * a.dim + d0 + row) * a.words + w0 + w, a.words - w0 - w);
         }
 #pragma unroll
         for (int i = 0; i < U::kPasses; ++i) {
-            const int at = i * kThreads + threadIdx.x, row = at / kAlong, w = at % kAlong * U::kVec;
+            const int at = i * kThreads + thread, row = at / kAlong, w = at % kAlong * U::kVec;
 #pragma unroll
             for (int e = 0; e < U::kVec; ++e) tile[row * U::kPitch + w + e] = piece[i][e];
         }
     }
-    __syncthreads();
+    lds_barrier();
     if (works) {
-        const int p = threadIdx.x & 15, d = d0 + p * U::kVec;
+        const int p = thread & 15, d = d0 + p * U::kVec;
 #pragma unroll
         for (int i = 0; i < U::kPasses; ++i) {
-            const int w = i * (kThreads / 16) + (threadIdx.x >> 4);
+            const int w = i * (kThreads / 16) + (thread >> 4);
             if (w0 + w >= a.words || d >= a.dim) continue;
             V v;
 #pragma unroll
@@ -422,41 +430,37 @@ __device__ __forceinline__ void turn_tile(const EmbedGradArgs& a, G* rows, unsig
 // What else a launch of the sort does, in workgroups of its own beside those that sort: it takes the few CUs of a sort a while, and
 // most of the table's gradient is zeros, which need nothing of it.
 struct Beside {
-    unsigned tiles;                       // to turn, from number 0 on
+    unsigned tiles;                       // to turn
     unsigned long long fill_from, fill;   // elements of the table's gradient to set to zero (all rows: those with tokens are written later)
-    unsigned fill_each;                   // stores of 16 bytes a thread
 };
-constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kTiles = kSortThreads / kThreads;      // tiles a workgroup
 
-template <class G, class W>
-__device__ __forceinline__ void do_beside(const EmbedGradArgs& a, G* rows, const Beside& b, unsigned number, char* room)
+template <class G>
+constexpr int tiles_room() { return kTiles * Turn<G>::kDims * Turn<G>::kPitch * (int)sizeof(G); }
+
+// 16 bytes a thread: zeros go out fastest (6.4 TB/s; with 16 stores a thread 6.1, with 4 5.6) as many short workgroups in order.
+template <class W>
+__device__ __forceinline__ void fill_part(const EmbedGradArgs& a, const Beside& b, unsigned number)
 {
-    if (number < b.tiles) {
-        turn_tile<G>(a, rows, number, reinterpret_cast<G*>(room));
-        return;
-    }
     constexpr int kVec = 16 / sizeof(W);
     typedef typename Piece<W, kVec>::type V;
-    W* out = static_cast<W*>(a.table_grad) + b.fill_from;
-    const unsigned long long first = (unsigned long long)(number - b.tiles) * (kSortThreads * b.fill_each * kVec);
-    if (first + kSortThreads * b.fill_each * kVec <= b.fill) {
-#pragma unroll 4
-        for (unsigned i = 0; i < b.fill_each; ++i) *reinterpret_cast<V*>(out + first + (i * kSortThreads + threadIdx.x) * kVec) = V{};
-    } else {
-        for (unsigned i = 0; i < b.fill_each; ++i) {
-            const unsigned long long at = first + (i * kSortThreads + threadIdx.x) * kVec;
-            if (at < b.fill) store_some<W, kVec>(out + at, V{}, (int)min(b.fill - at, (unsigned long long)kVec));
-        }
-    }
+    const unsigned long long at = ((unsigned long long)number * kSortThreads + threadIdx.x) * kVec;
+    if (at < b.fill) store_some<W, kVec>(static_cast<W*>(a.table_grad) + b.fill_from + at, V{}, (int)min(b.fill - at, (unsigned long long)kVec));
 }
 
-// Workgroups for that; about two a CU fill, with 16 KB of stores each at least.
+template <class G, class W>
+__device__ __forceinline__ void do_beside(const EmbedGradArgs& a, G* rows, const Beside& b, unsigned number, void* room)
+{
+    const unsigned turning = (b.tiles + kTiles - 1) / kTiles;
+    if (number < turning) turn_tiles<G>(a, rows, number * kTiles, b.tiles, static_cast<G*>(room));
+    else fill_part<W>(a, b, number - turning);
+}
+
 template <class W>
-unsigned beside_blocks(Beside& b)
+unsigned long long beside_blocks(const Beside& b)
 {
     const unsigned long long once = (unsigned long long)kSortThreads * (16 / sizeof(W));
-    b.fill_each = (unsigned)std::min<unsigned long long>(std::max<unsigned long long>(b.fill / (once * 512), 1), 64);
-    return b.tiles + (unsigned)((b.fill + once * b.fill_each - 1) / (once * b.fill_each));
+    return (b.tiles + kTiles - 1) / kTiles + (b.fill + once - 1) / once;
 }
 
 // A stable sort of (token, place) by the token, `digit` bits a pass from the lowest on.  Tokens that add to no row get the number
@@ -521,7 +525,7 @@ __device__ __forceinline__ int sum_before(int value, int* of_wave)
         sum += lane >= d ? n : 0;
     }
     if (lane == 63) of_wave[wave] = sum;
-    __syncthreads();
+    lds_barrier();
     int before = sum - value;
 #pragma unroll
     for (int w = 0; w < kSortWaves; ++w) before += w < wave ? of_wave[w] : 0;
@@ -550,13 +554,14 @@ struct Sorted {
 // ---------------------------------------------------------------- gradient of few tokens: one launch
 
 // Workgroup (b, c) owns the rows of the table whose number ends in b (kBuckets of them: frequent tokens are often neighbours) and
-// column block c.  It looks through all tokens, keeps those of its rows in their order, sets the rows without any to zero and sorts
-// what it kept by the row; each wavefront then takes slots of the sorted tokens, and a run of many tokens is shared by all.
+// column block c.  It looks through all tokens, keeps those of its rows in their order, sets the rows without any to zero (`zeros`;
+// beyond kOwnZeros bytes a launch before this one does that for all, at a higher rate) and sorts what it kept by the row; each wavefront then takes slots of the sorted tokens, and a run of many tokens is shared by all.
 constexpr int kFewTokens = 8192, kBuckets = 256, kBucketBits = 8, kBucketDigit = 9, kMarks = 1 << 15;
 constexpr int kFewEach = kFewTokens / kSortThreads;
+constexpr unsigned long long kOwnZeros = 32ull << 20;
 
 template <class G, class W>
-__global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, const G* grad, SortPlan plan)
+__global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, const G* grad, SortPlan plan, bool zeros)
 {
     __shared__ unsigned keys[kFewTokens];                  // number of the row within the bucket
     __shared__ unsigned short places[kFewTokens];
@@ -586,7 +591,7 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
         there[i] = key[i] < (unsigned)a.vocab && (key[i] & (kBuckets - 1)) == blockIdx.x;
     }
     if (threadIdx.x == 0) long_count = 0;
-    if (!a.accumulate)
+    if (zeros)
         for (int i = threadIdx.x; i < kMarks / 32; i += kSortThreads) marks[i] = 0;
 #pragma unroll
     for (int i = 0; i < kFewEach; ++i) {
@@ -594,7 +599,7 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
         count += __popcll(mine[i]);
     }
     if (lane == 0) counts[wave] = count;
-    __syncthreads();
+    lds_barrier();
     int at = 0;
     unsigned total = 0;
 #pragma unroll
@@ -608,20 +613,19 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
             const int to = at + __popcll(mine[i] & ((1ull << lane) - 1));
             keys[to] = key[i] >> kBucketBits;
             places[to] = (unsigned short)place[i];
-            if (!a.accumulate && (key[i] >> kBucketBits) < kMarks) atomicOr(&marks[key[i] >> (kBucketBits + 5)], 1u << (key[i] >> kBucketBits & 31));
+            if (zeros) atomicOr(&marks[key[i] >> (kBucketBits + 5)], 1u << (key[i] >> kBucketBits & 31));
         }
         at += __popcll(mine[i]);
     }
-    __syncthreads();
+    lds_barrier();
 
     const Columns c = columns_of(blockIdx.y, lane, a.dim);
     W* table_grad = static_cast<W*>(a.table_grad) + (size_t)blockIdx.x * a.dim;
     const size_t apart = (size_t)kBuckets * a.dim;         // elements from one row of the bucket to the next
     Sums sums;
-    if (!a.accumulate) {
+    if (zeros) {
         clear(sums);
-        const int marked = (int)min(rows, (long long)kMarks);      // (more rows than marks are set to zero before this launch)
-        for (int r = wave; r < marked; r += kSortWaves)
+        for (int r = wave; r < (int)rows; r += kSortWaves)
             if (!(marks[r >> 5] >> (r & 31) & 1)) store_row<W>(table_grad + r * apart, sums, c, 1.f, false);
     }
 
@@ -638,14 +642,14 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
         const int shift = pass * plan.digit, digit = threadIdx.x, size = 1 << plan.digit;
         int rank[kFewEach];
         rank_tokens<kFewEach, kBucketDigit>(key, there, kept, shift, plan.digit, room.of_wave, rank);
-        __syncthreads();
+        lds_barrier();
         int here = 0;
         if (digit < size)
 #pragma unroll
             for (int w = 0; w < kSortWaves; ++w) here += room.of_wave[w][digit];
         const int base = sum_before(here, counts);
         if (digit < size) spread<kBucketDigit>(room.of_wave, digit, base);
-        __syncthreads();
+        lds_barrier();
 #pragma unroll
         for (int i = 0; i < kFewEach; ++i)
             if (there[i]) {
@@ -653,7 +657,7 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
                 keys[to] = key[i];
                 places[to] = (unsigned short)place[i];
             }
-        __syncthreads();
+        lds_barrier();
         if (pass + 1 < plan.passes)
 #pragma unroll
             for (int i = 0; i < kFewEach; ++i)
@@ -669,7 +673,7 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
         add_slot<G>(grad, a.dim, c, first, total, ~0u, key_at, [&](unsigned i) { return (int)places[i]; }, done, [&](unsigned from) {
             if (lane == 0) long_runs[atomicAdd(&long_count, 1)] = from;
         });
-    __syncthreads();
+    lds_barrier();
     const int shared_runs = long_count;
     for (int l = 0; l < shared_runs; ++l) {
         const unsigned from = __builtin_amdgcn_readfirstlane(long_runs[l]), length = end_of_run(key_at, from, total) - from;
@@ -688,32 +692,32 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
 template <class G, class W>
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(EmbedGradArgs a, G* rows, Beside beside, SortPlan plan, int shift, Sorted from, int* counts)
 {
-    __shared__ __attribute__((aligned(16))) int bins[(sizeof(G) * Turn<G>::kDims * Turn<G>::kPitch + 3) / 4];
+    __shared__ __attribute__((aligned(16))) int bins[tiles_room<G>() / 4];
     static_assert(sizeof(bins) >= sizeof(int) << kMaxDigit, "a count for each digit fits");
     if ((int)blockIdx.x >= plan.groups) {
-        do_beside<G, W>(a, rows, beside, blockIdx.x - plan.groups, reinterpret_cast<char*>(bins));
+        do_beside<G, W>(a, rows, beside, blockIdx.x - plan.groups, bins);
         return;
     }
     const int size = 1 << plan.digit;
     const unsigned tokens = (unsigned)a.sentences * a.words, first = blockIdx.x * (unsigned)(kMoveEach * kSortThreads);
     for (int d = threadIdx.x; d < size; d += kSortThreads) bins[d] = 0;
-    __syncthreads();
+    lds_barrier();
     for (int i = 0; i < kMoveEach; ++i) {
         const unsigned t = first + own_token(kMoveEach, i);
         if (t < tokens) atomicAdd(&bins[((from.keys ? from.keys[t] : sort_key(a, t)) >> shift) & (unsigned)(size - 1)], 1);
     }
-    __syncthreads();
+    lds_barrier();
     for (int d = threadIdx.x; d < size; d += kSortThreads) counts[(size_t)blockIdx.x * size + d] = bins[d];
 }
 
 // ... then each finds, from the counts of all, where its tokens of each digit go, and takes them there in their order.
-template <class G, class W>
+template <class W>
 __global__ __launch_bounds__(kSortThreads) void sort_move_kernel(EmbedGradArgs a, Beside beside, SortPlan plan, int shift, Sorted from, const int* counts, Sorted to)
 {
     __shared__ int of_wave[kSortWaves][1 << kMaxDigit];
     __shared__ int wave_sums[kSortWaves];
     if ((int)blockIdx.x >= plan.groups) {
-        do_beside<G, W>(a, nullptr, beside, blockIdx.x - plan.groups, nullptr);
+        fill_part<W>(a, beside, blockIdx.x - plan.groups);
         return;
     }
     constexpr int kEach = kMoveEach;
@@ -752,7 +756,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_move_kernel(EmbedGradArgs a
     rank_tokens<kEach, kMaxDigit>(key, there, kEach, shift, plan.digit, of_wave, rank);
     const int base = sum_before(total, wave_sums) + before;
     if (digit < size) spread<kMaxDigit>(of_wave, digit, base);
-    __syncthreads();
+    lds_barrier();
 #pragma unroll
     for (int i = 0; i < kEach; ++i)
         if (there[i]) {
@@ -797,14 +801,14 @@ __global__ __launch_bounds__(kRunThreads) void runs_kernel(EmbedGradArgs a, cons
     const Columns c = columns_of((int)(blockIdx.x % column_blocks), lane, a.dim);
     W* table_grad = static_cast<W*>(a.table_grad);
     if (threadIdx.x == 0) long_count = 0;
-    __syncthreads();
+    lds_barrier();
     auto key_at = [&](unsigned i) { return sorted.keys[i]; };
     auto done = [&](unsigned k, const Sums& of_row) { store_row<W>(table_grad + (size_t)k * a.dim, of_row, c, a.scale, a.accumulate); };
     if (first < tokens)
         add_slot<G>(grad, a.dim, c, first, tokens, (unsigned)a.vocab, key_at, [&](unsigned i) { return sorted.places[i]; }, done, [&](unsigned from) {
             if (lane == 0) long_runs[atomicAdd(&long_count, 1)] = from;
         });
-    __syncthreads();
+    lds_barrier();
     const int shared_runs = long_count;
     for (int l = 0; l < shared_runs; ++l) {
         const unsigned from = __builtin_amdgcn_readfirstlane(long_runs[l]), to = end_of_run(key_at, from, tokens);
@@ -828,11 +832,11 @@ __global__ __launch_bounds__(kRunThreads) void runs_kernel(EmbedGradArgs a, cons
     }
 }
 
-// Before a launch of few tokens: what has to be turned or, where the rows are too many to be marked, set to zero.
+// Before a launch of few tokens: what has to be turned and, where that is much, set to zero.
 template <class G, class W>
 __global__ __launch_bounds__(kSortThreads) void beside_kernel(EmbedGradArgs a, G* rows, Beside beside)
 {
-    __shared__ __attribute__((aligned(16))) char room[sizeof(G) * Turn<G>::kDims * Turn<G>::kPitch];
+    __shared__ __attribute__((aligned(16))) char room[tiles_room<G>()];
     do_beside<G, W>(a, rows, beside, blockIdx.x, room);
 }
 
@@ -873,15 +877,17 @@ int launch_grad(const EmbedGradArgs& a, const Parts& parts, hipStream_t s)
         grad = rows;
     }
     const unsigned long long elements = a.accumulate ? 0 : (unsigned long long)a.vocab * a.dim;
-    Beside beside{(unsigned)tiles, 0, elements, 1};
+    Beside beside{(unsigned)tiles, 0, elements};
     if (tokens <= kFewTokens) {
         if (column_blocks > 65535) return (int)hipErrorInvalidValue;
-        if (a.vocab <= (long long)kMarks * kBuckets) beside.fill = 0;
-        const unsigned blocks = beside_blocks<W>(beside);
-        if (blocks) hipLaunchKernelGGL((beside_kernel<G, W>), dim3(blocks), dim3(kSortThreads), 0, s, a, rows, beside);
+        const bool zeros = !a.accumulate && elements * sizeof(W) <= kOwnZeros && a.vocab <= (long long)kMarks * kBuckets;
+        if (zeros) beside.fill = 0;
+        const unsigned long long blocks = beside_blocks<W>(beside);
+        if (blocks >= (1ull << 31)) return (int)hipErrorInvalidValue;
+        if (blocks) hipLaunchKernelGGL((beside_kernel<G, W>), dim3((unsigned)blocks), dim3(kSortThreads), 0, s, a, rows, beside);
         const SortPlan plan = sort_plan((a.vocab - 1) >> kBucketBits, kBucketDigit, tokens);
         const unsigned groups = (unsigned)std::min<long long>(a.vocab, kBuckets);
-        hipLaunchKernelGGL((bucket_kernel<G, W>), dim3(groups, (unsigned)column_blocks), dim3(kSortThreads), 0, s, a, grad, plan);
+        hipLaunchKernelGGL((bucket_kernel<G, W>), dim3(groups, (unsigned)column_blocks), dim3(kSortThreads), 0, s, a, grad, plan, zeros);
         return (int)hipGetLastError();
     }
     const SortPlan plan = sort_plan(a.vocab, kMaxDigit, tokens);
@@ -902,11 +908,13 @@ int launch_grad(const EmbedGradArgs& a, const Parts& parts, hipStream_t s)
         const unsigned long long kVec = 16 / sizeof(W), end = l + 1 == launches ? elements : elements * (l + 1) / launches / kVec * kVec;
         beside.fill = end - beside.fill_from;
         const int shift = l / 2 * plan.digit;
-        const dim3 grid(plan.groups + beside_blocks<W>(beside));
+        const unsigned long long blocks = plan.groups + beside_blocks<W>(beside);
+        if (blocks >= (1ull << 31)) return (int)hipErrorInvalidValue;
+        const dim3 grid((unsigned)blocks);
         if (l % 2 == 0) {
             hipLaunchKernelGGL((sort_count_kernel<G, W>), grid, dim3(kSortThreads), 0, s, a, rows, beside, plan, shift, from, counts);
         } else {
-            hipLaunchKernelGGL((sort_move_kernel<G, W>), grid, dim3(kSortThreads), 0, s, a, beside, plan, shift, from, counts, sorted[l / 2 & 1]);
+            hipLaunchKernelGGL((sort_move_kernel<W>), grid, dim3(kSortThreads), 0, s, a, beside, plan, shift, from, counts, sorted[l / 2 & 1]);
             from = sorted[l / 2 & 1];
         }
         beside.tiles = 0;
