@@ -12,6 +12,7 @@ namespace {
 enum { kF32 = 0, kF16 = 1, kBF16 = 2 };   // SC_F32, SC_F16, SC_BF16
 
 constexpr int kThreads = 256;
+constexpr unsigned long long kCacheBytes = 256ull << 20;      // of the last-level cache
 
 // VEC elements that may start at any element (the hardware splits what crosses a line).
 template <class T, int VEC>
@@ -46,7 +47,8 @@ __device__ __forceinline__ typename Piece<T, VEC>::type scaled(typename Piece<T,
 
 // Rows as they are, in pieces of VEC elements, kEach a thread; the last piece of a row ends with the row (where that does not hold
 // a whole number of pieces it overlaps the one before, with the same values).
-template <class T, int VEC>
+// PASSING: the output is larger than the caches and goes past them (64k rows of 4096 in bfloat16: 139 us instead of 149).
+template <class T, int VEC, bool PASSING>
 __global__ __launch_bounds__(kThreads) void embed_rows_kernel(EmbedArgs a, unsigned per_row, unsigned long long pieces)
 {
     typedef typename Piece<T, VEC>::type V;
@@ -74,7 +76,11 @@ __global__ __launch_bounds__(kThreads) void embed_rows_kernel(EmbedArgs a, unsig
     }
 #pragma unroll
     for (int i = 0; i < kEach; ++i)
-        if (base + i * kThreads + threadIdx.x < pieces) *reinterpret_cast<V*>(out + place[i] * a.dim + d[i]) = scaled<T, VEC>(piece[i], a.scale);
+        if (base + i * kThreads + threadIdx.x < pieces) {
+            V* to = reinterpret_cast<V*>(out + place[i] * a.dim + d[i]);
+            if (PASSING) __builtin_nontemporal_store(scaled<T, VEC>(piece[i], a.scale), to);
+            else *to = scaled<T, VEC>(piece[i], a.scale);
+        }
 }
 
 // A tile of kWords words by kDims dimensions, turned in LDS between rows of vectors and rows of words.  Pieces of 16 bytes on either
@@ -175,8 +181,9 @@ int launch_lookup(const EmbedArgs& a, hipStream_t s)
     const unsigned per_row = a.dim >= kVec ? (a.dim + kVec - 1) / kVec : a.dim;
     const unsigned long long pieces = (unsigned long long)a.sentences * a.words * per_row, blocks = (pieces + 4 * kThreads - 1) / (4 * kThreads);
     if (blocks >= (1ull << 31)) return (int)hipErrorInvalidValue;
-    if (a.dim >= kVec) hipLaunchKernelGGL((embed_rows_kernel<T, kVec>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a, per_row, pieces);
-    else hipLaunchKernelGGL((embed_rows_kernel<T, 1>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a, per_row, pieces);
+    const bool passing = pieces * 16 > kCacheBytes;
+    auto kernel = a.dim < kVec ? embed_rows_kernel<T, 1, false> : passing ? embed_rows_kernel<T, kVec, true> : embed_rows_kernel<T, kVec, false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kThreads), 0, s, a, per_row, pieces);
     return (int)hipGetLastError();
 }
 
@@ -360,9 +367,9 @@ __device__ __forceinline__ void add_slot(const G* grad, int dim, const Columns& 
     if (from < to) done((unsigned)__builtin_amdgcn_readlane((int)key, to - 1), sums);
 }
 
-// Adds up what the wavefronts of a workgroup left in `part`, in their order; wavefront 0 goes on with the sum.
-template <int WAVES>
-__device__ __forceinline__ void join(Sums& sums, float (*part)[kColumns])
+// Adds up the sums of `parts` wavefronts in a row, `first` the first of them, in their order: it goes on with the sum.  Every wavefront
+// of the workgroup calls this.
+__device__ __forceinline__ void join(Sums& sums, float (*part)[kColumns], int first, int parts)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     lds_barrier();
@@ -371,14 +378,12 @@ __device__ __forceinline__ void join(Sums& sums, float (*part)[kColumns])
 #pragma unroll
         for (int e = 0; e < 4; ++e) part[wave][s * 256 + lane * 4 + e] = sums.v[s][e];
     lds_barrier();
-    if (wave > 0) return;
-    clear(sums);
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w)
+    if (wave != first) return;
+    for (int w = 1; w < parts; ++w)
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sums.v[s][e] += part[w][s * 256 + lane * 4 + e];
+            for (int e = 0; e < 4; ++e) sums.v[s][e] += part[first + w][s * 256 + lane * 4 + e];
 }
 
 // ---------------------------------------------------------------- gradient: channels first
@@ -553,17 +558,18 @@ struct Sorted {
 
 // ---------------------------------------------------------------- gradient of few tokens: one launch
 
-// Workgroup (b, c) owns the rows of the table whose number ends in b (kBuckets of them: frequent tokens are often neighbours) and
-// column block c.  It looks through all tokens, keeps those of its rows in their order, sets the rows without any to zero (`zeros`;
+// Workgroup (b, y) owns the rows of the table whose number ends in b (kBuckets of them: frequent tokens are often neighbours), and
+// column blocks y, y + gridDim.y, ...  It looks through all tokens, keeps those of its rows in their order, sets the rows without any to zero (`zeros`;
 // beyond kOwnZeros bytes a launch before this one does that for all, at a higher rate) and sorts what it kept by the row; each wavefront then takes slots of the sorted tokens, and a run of many tokens is shared by all.
 constexpr int kFewTokens = 8192, kBuckets = 256, kBucketBits = 8, kBucketDigit = 9, kMarks = 1 << 15;
 constexpr int kFewEach = kFewTokens / kSortThreads;
 constexpr unsigned long long kOwnZeros = 32ull << 20;
+constexpr unsigned kPairs = 256;
 
 template <class G, class W>
-__global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, const G* grad, SortPlan plan, bool zeros)
+__global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, const G* grad, SortPlan plan, int column_blocks, bool zeros)
 {
-    __shared__ unsigned keys[kFewTokens];                  // number of the row within the bucket
+    __shared__ __attribute__((aligned(16))) unsigned keys[kFewTokens];      // number of the row within the bucket
     __shared__ unsigned short places[kFewTokens];
     __shared__ union {
         int of_wave[kSortWaves][1 << kBucketDigit];
@@ -619,69 +625,98 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
     }
     lds_barrier();
 
-    const Columns c = columns_of(blockIdx.y, lane, a.dim);
+    const int own_blocks = (column_blocks - (int)blockIdx.y + (int)gridDim.y - 1) / (int)gridDim.y;
+    auto columns = [&](int block) { return columns_of((int)(blockIdx.y + block * gridDim.y), lane, a.dim); };
     W* table_grad = static_cast<W*>(a.table_grad) + (size_t)blockIdx.x * a.dim;
     const size_t apart = (size_t)kBuckets * a.dim;         // elements from one row of the bucket to the next
     Sums sums;
     if (zeros) {
         clear(sums);
-        for (int r = wave; r < (int)rows; r += kSortWaves)
-            if (!(marks[r >> 5] >> (r & 31) & 1)) store_row<W>(table_grad + r * apart, sums, c, 1.f, false);
+        for (int block = 0; block < own_blocks; ++block) {
+            const Columns c = columns(block);
+            for (int r = wave; r < (int)rows; r += kSortWaves)
+                if (!(marks[r >> 5] >> (r & 31) & 1)) store_row<W>(table_grad + r * apart, sums, c, 1.f, false);
+        }
     }
 
-    // A stable sort by the key, in LDS.
-    const int kept = (int)((total + kSortThreads - 1) / kSortThreads);
-#pragma unroll
-    for (int i = 0; i < kFewEach; ++i) {
-        const unsigned t = own_token(kept, i);
-        there[i] = i < kept && t < total;
-        key[i] = there[i] ? keys[t] : 0u;
-        place[i] = there[i] ? places[t] : 0u;
-    }
-    for (int pass = 0; pass < plan.passes; ++pass) {
-        const int shift = pass * plan.digit, digit = threadIdx.x, size = 1 << plan.digit;
-        int rank[kFewEach];
-        rank_tokens<kFewEach, kBucketDigit>(key, there, kept, shift, plan.digit, room.of_wave, rank);
+    // A stable sort by the key, in LDS: few tokens by counting those that go before each, more by digits.
+    if (total <= kPairs) {
+        const unsigned t = threadIdx.x, own = t < total ? keys[t] : 0u;
+        const unsigned short own_place = t < total ? places[t] : 0;
+        unsigned before = 0;
+        if (t < total)
+            for (unsigned j = 0; j < total; ++j) before += keys[j] < own || (keys[j] == own && j < t);
         lds_barrier();
-        int here = 0;
-        if (digit < size)
-#pragma unroll
-            for (int w = 0; w < kSortWaves; ++w) here += room.of_wave[w][digit];
-        const int base = sum_before(here, counts);
-        if (digit < size) spread<kBucketDigit>(room.of_wave, digit, base);
+        if (t < total) {
+            keys[before] = own;
+            places[before] = own_place;
+        }
         lds_barrier();
+    } else {
+        const int kept = (int)((total + kSortThreads - 1) / kSortThreads);
 #pragma unroll
-        for (int i = 0; i < kFewEach; ++i)
-            if (there[i]) {
-                const int to = room.of_wave[wave][(key[i] >> shift) & (unsigned)(size - 1)] + rank[i];
-                keys[to] = key[i];
-                places[to] = (unsigned short)place[i];
-            }
-        lds_barrier();
-        if (pass + 1 < plan.passes)
+        for (int i = 0; i < kFewEach; ++i) {
+            const unsigned t = own_token(kept, i);
+            there[i] = i < kept && t < total;
+            key[i] = there[i] ? keys[t] : 0u;
+            place[i] = there[i] ? places[t] : 0u;
+        }
+        for (int pass = 0; pass < plan.passes; ++pass) {
+            const int shift = pass * plan.digit, digit = threadIdx.x, size = 1 << plan.digit;
+            int rank[kFewEach];
+            rank_tokens<kFewEach, kBucketDigit>(key, there, kept, shift, plan.digit, room.of_wave, rank);
+            lds_barrier();
+            int here = 0;
+            if (digit < size)
+#pragma unroll
+                for (int w = 0; w < kSortWaves; ++w) here += room.of_wave[w][digit];
+            const int base = sum_before(here, counts);
+            if (digit < size) spread<kBucketDigit>(room.of_wave, digit, base);
+            lds_barrier();
 #pragma unroll
             for (int i = 0; i < kFewEach; ++i)
                 if (there[i]) {
-                    key[i] = keys[own_token(kept, i)];
-                    place[i] = places[own_token(kept, i)];
+                    const int to = room.of_wave[wave][(key[i] >> shift) & (unsigned)(size - 1)] + rank[i];
+                    keys[to] = key[i];
+                    places[to] = (unsigned short)place[i];
                 }
+            lds_barrier();
+            if (pass + 1 < plan.passes)
+#pragma unroll
+                for (int i = 0; i < kFewEach; ++i)
+                    if (there[i]) {
+                        key[i] = keys[own_token(kept, i)];
+                        place[i] = places[own_token(kept, i)];
+                    }
+        }
     }
 
     auto key_at = [&](unsigned i) { return keys[i]; };
-    auto done = [&](unsigned k, const Sums& of_row) { store_row<W>(table_grad + k * apart, of_row, c, a.scale, a.accumulate); };
-    for (unsigned first = wave * kSlot; first < total; first += kSortWaves * kSlot)
-        add_slot<G>(grad, a.dim, c, first, total, ~0u, key_at, [&](unsigned i) { return (int)places[i]; }, done, [&](unsigned from) {
-            if (lane == 0) long_runs[atomicAdd(&long_count, 1)] = from;
-        });
+    auto store = [&](unsigned k, const Sums& of_row, const Columns& c) { store_row<W>(table_grad + k * apart, of_row, c, a.scale, a.accumulate); };
+    const int slots = (int)((total + kSlot - 1) / kSlot);
+    for (int unit = wave; unit < slots * own_blocks; unit += kSortWaves) {
+        const int block = unit / slots;
+        const Columns c = columns(block);
+        add_slot<G>(grad, a.dim, c, (unsigned)(unit % slots) * kSlot, total, ~0u, key_at, [&](unsigned i) { return (int)places[i]; },
+                    [&](unsigned k, const Sums& of_row) { store(k, of_row, c); }, [&](unsigned from) {
+                        if (lane == 0 && block == 0) long_runs[atomicAdd(&long_count, 1)] = from;
+                    });
+    }
     lds_barrier();
-    const int shared_runs = long_count;
+    // A long run: as many wavefronts to a column block as there are for each, some tokens each.
+    const int shared_runs = long_count, parts = max(kSortWaves / own_blocks, 1);
     for (int l = 0; l < shared_runs; ++l) {
         const unsigned from = __builtin_amdgcn_readfirstlane(long_runs[l]), length = end_of_run(key_at, from, total) - from;
-        const unsigned p0 = length * wave / kSortWaves, p1 = length * (wave + 1) / kSortWaves;
-        clear(sums);
-        add_rows<G>(sums, grad, a.dim, (int)(p1 - p0), c, [&](int i) { return (int)places[from + p0 + i]; });
-        join<kSortWaves>(sums, room.part);
-        if (wave == 0) done(keys[from], sums);
+        for (int first = 0; first < own_blocks; first += kSortWaves / parts) {
+            const int block = first + wave / parts, part = wave % parts;
+            const bool works = wave / parts < kSortWaves / parts && block < own_blocks;
+            const Columns c = columns(works ? block : 0);
+            const unsigned p0 = length * part / parts, p1 = length * (part + 1) / parts;
+            clear(sums);
+            if (works) add_rows<G>(sums, grad, a.dim, (int)(p1 - p0), c, [&](int i) { return (int)places[from + p0 + i]; });
+            join(sums, room.part, wave - part, works ? parts : 0);
+            if (works && part == 0) store(keys[from], sums, c);
+        }
     }
 }
 
@@ -827,7 +862,7 @@ __global__ __launch_bounds__(kRunThreads) void runs_kernel(EmbedGradArgs a, cons
         add_rows<G>(sums, grad, a.dim, (int)(l1 - l0), c, [&](int i) { return sorted.places[from + l0 + i]; });
         add_rows<float>(sums, windows, a.dim, (int)(m1 - m0), c, [&](int i) { return (int)(w0 + m0 + i); });
         add_rows<G>(sums, grad, a.dim, (int)(t1 - t0), c, [&](int i) { return sorted.places[rest + t0 + i]; });
-        join<kRunWaves>(sums, part);
+        join(sums, part, 0, kRunWaves);
         if (wave == 0) done(sorted.keys[from], sums);
     }
 }
@@ -879,7 +914,6 @@ int launch_grad(const EmbedGradArgs& a, const Parts& parts, hipStream_t s)
     const unsigned long long elements = a.accumulate ? 0 : (unsigned long long)a.vocab * a.dim;
     Beside beside{(unsigned)tiles, 0, elements};
     if (tokens <= kFewTokens) {
-        if (column_blocks > 65535) return (int)hipErrorInvalidValue;
         const bool zeros = !a.accumulate && elements * sizeof(W) <= kOwnZeros && a.vocab <= (long long)kMarks * kBuckets;
         if (zeros) beside.fill = 0;
         const unsigned long long blocks = beside_blocks<W>(beside);
@@ -887,7 +921,8 @@ int launch_grad(const EmbedGradArgs& a, const Parts& parts, hipStream_t s)
         if (blocks) hipLaunchKernelGGL((beside_kernel<G, W>), dim3((unsigned)blocks), dim3(kSortThreads), 0, s, a, rows, beside);
         const SortPlan plan = sort_plan((a.vocab - 1) >> kBucketBits, kBucketDigit, tokens);
         const unsigned groups = (unsigned)std::min<long long>(a.vocab, kBuckets);
-        hipLaunchKernelGGL((bucket_kernel<G, W>), dim3(groups, (unsigned)column_blocks), dim3(kSortThreads), 0, s, a, grad, plan, zeros);
+        const unsigned shares = (unsigned)std::min<long long>(column_blocks, kBuckets / groups);      // of the column blocks: a workgroup a CU
+        hipLaunchKernelGGL((bucket_kernel<G, W>), dim3(groups, shares), dim3(kSortThreads), 0, s, a, grad, plan, (int)column_blocks, zeros);
         return (int)hipGetLastError();
     }
     const SortPlan plan = sort_plan(a.vocab, kMaxDigit, tokens);
