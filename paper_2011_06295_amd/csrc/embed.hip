@@ -645,7 +645,14 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
         const unsigned short own_place = t < total ? places[t] : 0;
         unsigned before = 0;
         if (t < total)
-            for (unsigned j = 0; j < total; ++j) before += keys[j] < own || (keys[j] == own && j < t);
+#pragma unroll 2
+            for (unsigned j = 0; j < total; j += 4) {
+                const uint4 k = *reinterpret_cast<const uint4*>(keys + j);      // (what lies past the last one does not count)
+                before += j < total && (k.x < own || (k.x == own && j < t));
+                before += j + 1 < total && (k.y < own || (k.y == own && j + 1 < t));
+                before += j + 2 < total && (k.z < own || (k.z == own && j + 2 < t));
+                before += j + 3 < total && (k.w < own || (k.w == own && j + 3 < t));
+            }
         lds_barrier();
         if (t < total) {
             keys[before] = own;
