@@ -367,23 +367,26 @@ __device__ __forceinline__ void add_slot(const G* grad, int dim, const Columns& 
     if (from < to) done((unsigned)__builtin_amdgcn_readlane((int)key, to - 1), sums);
 }
 
-// Adds up the sums of `parts` wavefronts in a row, `first` the first of them, in their order: it goes on with the sum.  Every wavefront
-// of the workgroup calls this.
-__device__ __forceinline__ void join(Sums& sums, float (*part)[kColumns], int first, int parts)
+// What the wavefronts of a workgroup leave to be joined.
+__device__ __forceinline__ void leave(const Sums& sums, float (*part)[kColumns])
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    lds_barrier();
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int e = 0; e < 4; ++e) part[wave][s * 256 + lane * 4 + e] = sums.v[s][e];
-    lds_barrier();
-    if (wave != first) return;
-    for (int w = 1; w < parts; ++w)
+}
+
+// The sum of what `count` wavefronts in a row left, `first` the first of them, in their order.
+__device__ __forceinline__ void join(Sums& sums, float (*part)[kColumns], int first, int count)
+{
+    const int lane = threadIdx.x & 63;
+    clear(sums);
+    for (int w = first; w < first + count; ++w)
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sums.v[s][e] += part[first + w][s * 256 + lane * 4 + e];
+            for (int e = 0; e < 4; ++e) sums.v[s][e] += part[w][s * 256 + lane * 4 + e];
 }
 
 // ---------------------------------------------------------------- gradient: channels first
@@ -565,21 +568,24 @@ constexpr int kFewTokens = 8192, kBuckets = 256, kBucketBits = 8, kBucketDigit =
 constexpr int kFewEach = kFewTokens / kSortThreads;
 constexpr unsigned long long kOwnZeros = 32ull << 20;
 constexpr unsigned kPairs = 256;
+constexpr int kFewBits = 13;
 
 template <class G, class W>
 __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, const G* grad, SortPlan plan, int column_blocks, bool zeros)
 {
-    __shared__ __attribute__((aligned(16))) unsigned keys[kFewTokens];      // number of the row within the bucket
+    __shared__ unsigned keys[kFewTokens];                  // number of the row within the bucket
     __shared__ unsigned short places[kFewTokens];
-    __shared__ union {
+    __shared__ __attribute__((aligned(16))) union {
+        unsigned pairs[kPairs];
         int of_wave[kSortWaves][1 << kBucketDigit];
         float part[kSortWaves][kColumns];
     } room;
     __shared__ unsigned marks[kMarks / 32];                // rows of the bucket that have tokens
     __shared__ int counts[kSortWaves];
-    __shared__ unsigned long_runs[kFewTokens / kLong + 1];
+    __shared__ unsigned long_from[kFewTokens / kLong], long_to[kFewTokens / kLong];
     __shared__ int long_count;
     static_assert(kFewTokens <= 1 << 16, "places of 16 bits");
+    static_assert(kFewTokens == 1 << kFewBits && kPairs % 4 == 0, "numbers of tokens; four at a time");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const unsigned tokens = (unsigned)a.sentences * a.words;
     const int each = (int)((tokens + kSortThreads - 1) / kSortThreads);
@@ -640,22 +646,20 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
     }
 
     // A stable sort by the key, in LDS: few tokens by counting those that go before each, more by digits.
-    if (total <= kPairs) {
-        const unsigned t = threadIdx.x, own = t < total ? keys[t] : 0u;
+    if (total <= kPairs && rows <= 1ll << (32 - kFewBits)) {
+        // (key, number) as one number: all differ
+        const unsigned t = threadIdx.x, k = t < total ? keys[t] : 0u, own = t < total ? k << kFewBits | t : ~0u;
         const unsigned short own_place = t < total ? places[t] : 0;
-        unsigned before = 0;
-        if (t < total)
-#pragma unroll 2
-            for (unsigned j = 0; j < total; j += 4) {
-                const uint4 k = *reinterpret_cast<const uint4*>(keys + j);      // (what lies past the last one does not count)
-                before += j < total && (k.x < own || (k.x == own && j < t));
-                before += j + 1 < total && (k.y < own || (k.y == own && j + 1 < t));
-                before += j + 2 < total && (k.z < own || (k.z == own && j + 2 < t));
-                before += j + 3 < total && (k.w < own || (k.w == own && j + 3 < t));
-            }
+        if (t < kPairs) room.pairs[t] = own;
         lds_barrier();
         if (t < total) {
-            keys[before] = own;
+            unsigned before = 0;
+#pragma unroll 4
+            for (unsigned j = 0; j < total; j += 4) {
+                const uint4 n = *reinterpret_cast<const uint4*>(room.pairs + j);
+                before += (n.x < own) + (n.y < own) + (n.z < own) + (n.w < own);
+            }
+            keys[before] = k;
             places[before] = own_place;
         }
         lds_barrier();
@@ -698,32 +702,55 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
         }
     }
 
-    auto key_at = [&](unsigned i) { return keys[i]; };
-    auto store = [&](unsigned k, const Sums& of_row, const Columns& c) { store_row<W>(table_grad + k * apart, of_row, c, a.scale, a.accumulate); };
-    const int slots = (int)((total + kSlot - 1) / kSlot);
-    for (int unit = wave; unit < slots * own_blocks; unit += kSortWaves) {
-        const int block = unit / slots;
-        const Columns c = columns(block);
-        add_slot<G>(grad, a.dim, c, (unsigned)(unit % slots) * kSlot, total, ~0u, key_at, [&](unsigned i) { return (int)places[i]; },
-                    [&](unsigned k, const Sums& of_row) { store(k, of_row, c); }, [&](unsigned from) {
-                        if (lane == 0 && block == 0) long_runs[atomicAdd(&long_count, 1)] = from;
-                    });
+    // The long runs, and where they end.
+    for (unsigned t = threadIdx.x; t + kLong < total; t += kSortThreads) {
+        const unsigned k = keys[t];
+        if (keys[t + kLong] != k || (t > 0 && keys[t - 1] == k)) continue;
+        unsigned same = t + kLong, other = total;      // a token of the run, one past it
+        while (other - same > 1) {
+            const unsigned middle = (same + other) / 2;
+            if (keys[middle] == k) same = middle;
+            else other = middle;
+        }
+        const int l = atomicAdd(&long_count, 1);
+        long_from[l] = t;
+        long_to[l] = other;
     }
     lds_barrier();
-    // A long run: as many wavefronts to a column block as there are for each, some tokens each.
-    const int shared_runs = long_count, parts = max(kSortWaves / own_blocks, 1);
-    for (int l = 0; l < shared_runs; ++l) {
-        const unsigned from = __builtin_amdgcn_readfirstlane(long_runs[l]), length = end_of_run(key_at, from, total) - from;
-        for (int first = 0; first < own_blocks; first += kSortWaves / parts) {
-            const int block = first + wave / parts, part = wave % parts;
-            const bool works = wave / parts < kSortWaves / parts && block < own_blocks;
-            const Columns c = columns(works ? block : 0);
-            const unsigned p0 = length * part / parts, p1 = length * (part + 1) / parts;
-            clear(sums);
-            if (works) add_rows<G>(sums, grad, a.dim, (int)(p1 - p0), c, [&](int i) { return (int)places[from + p0 + i]; });
-            join(sums, room.part, wave - part, works ? parts : 0);
-            if (works && part == 0) store(keys[from], sums, c);
+
+    // A long run and a column block are shared by `parts` wavefronts; a round is as many such pairs as there are wavefronts for.
+    const int shared_runs = long_count, parts = max(kSortWaves / own_blocks, 1), together = kSortWaves / parts;
+    const int pairs = shared_runs * own_blocks;
+    auto store = [&](unsigned k, const Sums& of_row, const Columns& c) { store_row<W>(table_grad + k * apart, of_row, c, a.scale, a.accumulate); };
+    auto add_pairs = [&](int first) {
+        const int pair = first + wave / parts, part = wave % parts;
+        clear(sums);
+        if (wave / parts >= together || pair >= pairs) return;
+        const unsigned from = __builtin_amdgcn_readfirstlane(long_from[pair / own_blocks]), length = __builtin_amdgcn_readfirstlane(long_to[pair / own_blocks]) - from;
+        const unsigned p0 = length * part / parts, p1 = length * (part + 1) / parts;
+        add_rows<G>(sums, grad, a.dim, (int)(p1 - p0), columns(pair % own_blocks), [&](int i) { return (int)places[from + p0 + i]; });
+        leave(sums, room.part);
+    };
+    auto finish_pairs = [&](int first) {
+        lds_barrier();
+        const int pair = first + wave / parts;
+        if (wave / parts < together && pair < pairs && wave % parts == 0) {
+            join(sums, room.part, wave, parts);
+            store(keys[long_from[pair / own_blocks]], sums, columns(pair % own_blocks));
         }
+    };
+    if (pairs) add_pairs(0);
+    const int slots = (int)((total + kSlot - 1) / kSlot);
+    for (int unit = wave; unit < slots * own_blocks; unit += kSortWaves) {
+        const Columns c = columns(unit / slots);
+        add_slot<G>(grad, a.dim, c, (unsigned)(unit % slots) * kSlot, total, ~0u, [&](unsigned i) { return keys[i]; }, [&](unsigned i) { return (int)places[i]; },
+                    [&](unsigned k, const Sums& of_row) { store(k, of_row, c); }, [](unsigned) {});
+    }
+    if (pairs) finish_pairs(0);
+    for (int first = together; first < pairs; first += together) {
+        lds_barrier();
+        add_pairs(first);
+        finish_pairs(first);
     }
 }
 
@@ -869,8 +896,13 @@ __global__ __launch_bounds__(kRunThreads) void runs_kernel(EmbedGradArgs a, cons
         add_rows<G>(sums, grad, a.dim, (int)(l1 - l0), c, [&](int i) { return sorted.places[from + l0 + i]; });
         add_rows<float>(sums, windows, a.dim, (int)(m1 - m0), c, [&](int i) { return (int)(w0 + m0 + i); });
         add_rows<G>(sums, grad, a.dim, (int)(t1 - t0), c, [&](int i) { return sorted.places[rest + t0 + i]; });
-        join(sums, part, 0, kRunWaves);
-        if (wave == 0) done(sorted.keys[from], sums);
+        leave(sums, part);
+        lds_barrier();
+        if (wave == 0) {
+            join(sums, part, 0, kRunWaves);
+            done(sorted.keys[from], sums);
+        }
+        lds_barrier();
     }
 }
 
