@@ -391,15 +391,23 @@ __device__ __forceinline__ void join(Sums& sums, float (*part)[kColumns], int fi
 
 // ---------------------------------------------------------------- gradient: channels first
 
-// [sentence][dimension][word] to rows of vectors: each kThreads threads of a workgroup turn a tile, number, number + 1, ... (of `tiles`).
+// grad of the shape [sentence][dimension][word] to rows of vectors.
+struct TurnArgs {
+    const void* grad;
+    void* rows;
+    int dim, sentences, words;
+    unsigned tiles;
+};
+
+// Each kThreads threads of a workgroup turn a tile: number, number + 1, ...
 template <class G>
-__device__ __forceinline__ void turn_tiles(const EmbedGradArgs& a, G* rows, unsigned number, unsigned tiles, G* room)
+__device__ __forceinline__ void turn_tiles(const TurnArgs& a, unsigned number, G* room)
 {
     typedef Turn<G> U;
     typedef typename U::V V;
     const int thread = threadIdx.x % kThreads, part = threadIdx.x / kThreads;
     G* tile = room + part * U::kDims * U::kPitch;
-    const bool works = number + part < tiles;
+    const bool works = number + part < a.tiles;
     size_t n;
     int w0, d0;
     tile_at(number + part, a.words, a.dim, U::kWords, U::kDims, n, w0, d0);
@@ -430,17 +438,19 @@ __device__ __forceinline__ void turn_tiles(const EmbedGradArgs& a, G* rows, unsi
             V v;
 #pragma unroll
             for (int e = 0; e < U::kVec; ++e) v[e] = tile[(p * U::kVec + e) * U::kPitch + w];
-            store_some<G, U::kVec>(rows + (n * a.words + w0 + w) * a.dim + d, v, a.dim - d);
+            store_some<G, U::kVec>(static_cast<G*>(a.rows) + (n * a.words + w0 + w) * a.dim + d, v, a.dim - d);
         }
     }
 }
 
-// What else a launch of the sort does, in workgroups of its own beside those that sort: it takes the few CUs of a sort a while, and
-// most of the table's gradient is zeros, which need nothing of it.
-struct Beside {
-    unsigned tiles;                       // to turn
-    unsigned long long fill_from, fill;   // elements of the table's gradient to set to zero (all rows: those with tokens are written later)
+// Elements of the table's gradient to set to zero.
+struct Fill {
+    void* to;
+    unsigned long long count;
 };
+
+// The launches of the sort turn tiles and fill in workgroups of their own beside those that sort: it takes the few CUs of a sort a
+// while, and most of the table's gradient is zeros, which need nothing of it (rows with tokens are written later).
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kTiles = kSortThreads / kThreads;      // tiles a workgroup
 
 template <class G>
@@ -448,27 +458,27 @@ constexpr int tiles_room() { return kTiles * Turn<G>::kDims * Turn<G>::kPitch * 
 
 // 16 bytes a thread: zeros go out fastest (6.4 TB/s; with 16 stores a thread 6.1, with 4 5.6) as many short workgroups in order.
 template <class W>
-__device__ __forceinline__ void fill_part(const EmbedGradArgs& a, const Beside& b, unsigned number)
+__device__ __forceinline__ void fill_part(const Fill& f, unsigned number)
 {
     constexpr int kVec = 16 / sizeof(W);
     typedef typename Piece<W, kVec>::type V;
     const unsigned long long at = ((unsigned long long)number * kSortThreads + threadIdx.x) * kVec;
-    if (at < b.fill) store_some<W, kVec>(static_cast<W*>(a.table_grad) + b.fill_from + at, V{}, (int)min(b.fill - at, (unsigned long long)kVec));
+    if (at < f.count) store_some<W, kVec>(static_cast<W*>(f.to) + at, V{}, (int)min(f.count - at, (unsigned long long)kVec));
 }
 
 template <class G, class W>
-__device__ __forceinline__ void do_beside(const EmbedGradArgs& a, G* rows, const Beside& b, unsigned number, void* room)
+__device__ __forceinline__ void turn_or_fill(const TurnArgs& t, const Fill& f, unsigned number, void* room)
 {
-    const unsigned turning = (b.tiles + kTiles - 1) / kTiles;
-    if (number < turning) turn_tiles<G>(a, rows, number * kTiles, b.tiles, static_cast<G*>(room));
-    else fill_part<W>(a, b, number - turning);
+    const unsigned turning = (t.tiles + kTiles - 1) / kTiles;
+    if (number < turning) turn_tiles<G>(t, number * kTiles, static_cast<G*>(room));
+    else fill_part<W>(f, number - turning);
 }
 
 template <class W>
-unsigned long long beside_blocks(const Beside& b)
+unsigned long long blocks_of(unsigned tiles, const Fill& f)
 {
     const unsigned long long once = (unsigned long long)kSortThreads * (16 / sizeof(W));
-    return (b.tiles + kTiles - 1) / kTiles + (b.fill + once - 1) / once;
+    return (tiles + kTiles - 1) / kTiles + (f.count + once - 1) / once;
 }
 
 // A stable sort of (token, place) by the token, `digit` bits a pass from the lowest on.  Tokens that add to no row get the number
@@ -491,7 +501,14 @@ SortPlan sort_plan(long long last, int most, long long tokens)      // of keys 0
     return p;
 }
 
-__device__ __forceinline__ unsigned sort_key(const EmbedGradArgs& a, unsigned t)
+struct TokenArgs {
+    const void* tokens;
+    long long vocab, padding;
+    unsigned count;
+    bool wide;
+};
+
+__device__ __forceinline__ unsigned sort_key(const TokenArgs& a, unsigned t)
 {
     const long long v = token_at(a.tokens, a.wide, t);
     return v >= 0 && v < a.vocab && v != a.padding ? (unsigned)v : (unsigned)a.vocab;
@@ -562,7 +579,7 @@ struct Sorted {
 // ---------------------------------------------------------------- gradient of few tokens: one launch
 
 // Workgroup (b, y) owns the rows of the table whose number ends in b (kBuckets of them: frequent tokens are often neighbours), and
-// column blocks y, y + gridDim.y, ...  It looks through all tokens, keeps those of its rows in their order, sets the rows without any to zero (`zeros`;
+// column blocks y, y + shares, ...  It looks through all tokens, keeps those of its rows in their order, sets the rows without any to zero (`zeros`;
 // beyond kOwnZeros bytes a launch before this one does that for all, at a higher rate) and sorts what it kept by the row; each wavefront then takes slots of the sorted tokens, and a run of many tokens is shared by all.
 constexpr int kFewTokens = 8192, kBuckets = 256, kBucketBits = 8, kBucketDigit = 9, kMarks = 1 << 15;
 constexpr int kFewEach = kFewTokens / kSortThreads;
@@ -571,7 +588,7 @@ constexpr unsigned kPairs = 256;
 constexpr int kFewBits = 13;
 
 template <class G, class W>
-__global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, const G* grad, SortPlan plan, int column_blocks, bool zeros)
+__global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, const G* grad, int passes, int digit_bits, int column_blocks, int shares, bool zeros)
 {
     __shared__ unsigned keys[kFewTokens];                  // number of the row within the bucket
     __shared__ unsigned short places[kFewTokens];
@@ -591,6 +608,7 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
     const int each = (int)((tokens + kSortThreads - 1) / kSortThreads);
     const long long rows = (a.vocab - blockIdx.x + kBuckets - 1) >> kBucketBits;      // of this bucket
 
+    const TokenArgs named{a.tokens, a.vocab, a.padding, tokens, a.wide};
     unsigned key[kFewEach], place[kFewEach];
     bool there[kFewEach];
     unsigned long long mine[kFewEach];
@@ -599,7 +617,7 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
     for (int i = 0; i < kFewEach; ++i) {
         place[i] = own_token(each, i);
         there[i] = i < each && place[i] < tokens;
-        key[i] = there[i] ? sort_key(a, place[i]) : (unsigned)a.vocab;
+        key[i] = there[i] ? sort_key(named, place[i]) : (unsigned)a.vocab;
         there[i] = key[i] < (unsigned)a.vocab && (key[i] & (kBuckets - 1)) == blockIdx.x;
     }
     if (threadIdx.x == 0) long_count = 0;
@@ -631,8 +649,8 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
     }
     lds_barrier();
 
-    const int own_blocks = (column_blocks - (int)blockIdx.y + (int)gridDim.y - 1) / (int)gridDim.y;
-    auto columns = [&](int block) { return columns_of((int)(blockIdx.y + block * gridDim.y), lane, a.dim); };
+    const int own_blocks = (column_blocks - (int)blockIdx.y + shares - 1) / shares;
+    auto columns = [&](int block) { return columns_of((int)(blockIdx.y + block * shares), lane, a.dim); };
     W* table_grad = static_cast<W*>(a.table_grad) + (size_t)blockIdx.x * a.dim;
     const size_t apart = (size_t)kBuckets * a.dim;         // elements from one row of the bucket to the next
     Sums sums;
@@ -672,10 +690,10 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
             key[i] = there[i] ? keys[t] : 0u;
             place[i] = there[i] ? places[t] : 0u;
         }
-        for (int pass = 0; pass < plan.passes; ++pass) {
-            const int shift = pass * plan.digit, digit = threadIdx.x, size = 1 << plan.digit;
+        for (int pass = 0; pass < passes; ++pass) {
+            const int shift = pass * digit_bits, digit = threadIdx.x, size = 1 << digit_bits;
             int rank[kFewEach];
-            rank_tokens<kFewEach, kBucketDigit>(key, there, kept, shift, plan.digit, room.of_wave, rank);
+            rank_tokens<kFewEach, kBucketDigit>(key, there, kept, shift, digit_bits, room.of_wave, rank);
             lds_barrier();
             int here = 0;
             if (digit < size)
@@ -692,7 +710,7 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
                     places[to] = (unsigned short)place[i];
                 }
             lds_barrier();
-            if (pass + 1 < plan.passes)
+            if (pass + 1 < passes)
 #pragma unroll
                 for (int i = 0; i < kFewEach; ++i)
                     if (there[i]) {
@@ -756,24 +774,24 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
 
 // ---------------------------------------------------------------- gradient of many tokens: a sort, windows, runs
 
-// A pass of the sort is two launches.  Each workgroup counts the digits of its run of tokens ...  (from.keys: null in the first pass, which
-// reads the tokens.)
+// A pass of the sort is two launches.  Each workgroup counts the digits of its run of tokens ...  (from: null in the first pass, which reads
+// the tokens.)
 template <class G, class W>
-__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(EmbedGradArgs a, G* rows, Beside beside, SortPlan plan, int shift, Sorted from, int* counts)
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(TokenArgs a, TurnArgs turn, Fill fill, const unsigned* from, int* counts, int groups, short shift, short bits)
 {
     __shared__ __attribute__((aligned(16))) int bins[tiles_room<G>() / 4];
     static_assert(sizeof(bins) >= sizeof(int) << kMaxDigit, "a count for each digit fits");
-    if ((int)blockIdx.x >= plan.groups) {
-        do_beside<G, W>(a, rows, beside, blockIdx.x - plan.groups, bins);
+    if ((int)blockIdx.x >= groups) {
+        turn_or_fill<G, W>(turn, fill, blockIdx.x - groups, bins);
         return;
     }
-    const int size = 1 << plan.digit;
-    const unsigned tokens = (unsigned)a.sentences * a.words, first = blockIdx.x * (unsigned)(kMoveEach * kSortThreads);
+    const int size = 1 << bits;
+    const unsigned first = blockIdx.x * (unsigned)(kMoveEach * kSortThreads);
     for (int d = threadIdx.x; d < size; d += kSortThreads) bins[d] = 0;
     lds_barrier();
     for (int i = 0; i < kMoveEach; ++i) {
         const unsigned t = first + own_token(kMoveEach, i);
-        if (t < tokens) atomicAdd(&bins[((from.keys ? from.keys[t] : sort_key(a, t)) >> shift) & (unsigned)(size - 1)], 1);
+        if (t < a.count) atomicAdd(&bins[((from ? from[t] : sort_key(a, t)) >> shift) & (unsigned)(size - 1)], 1);
     }
     lds_barrier();
     for (int d = threadIdx.x; d < size; d += kSortThreads) counts[(size_t)blockIdx.x * size + d] = bins[d];
@@ -781,24 +799,24 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(EmbedGradArgs 
 
 // ... then each finds, from the counts of all, where its tokens of each digit go, and takes them there in their order.
 template <class W>
-__global__ __launch_bounds__(kSortThreads) void sort_move_kernel(EmbedGradArgs a, Beside beside, SortPlan plan, int shift, Sorted from, const int* counts, Sorted to)
+__global__ __launch_bounds__(kSortThreads) void sort_move_kernel(TokenArgs a, Fill fill, Sorted from, Sorted to, const int* counts, int groups, short shift, short bits)
 {
     __shared__ int of_wave[kSortWaves][1 << kMaxDigit];
     __shared__ int wave_sums[kSortWaves];
-    if ((int)blockIdx.x >= plan.groups) {
-        fill_part<W>(a, beside, blockIdx.x - plan.groups);
+    if ((int)blockIdx.x >= groups) {
+        fill_part<W>(fill, blockIdx.x - groups);
         return;
     }
     constexpr int kEach = kMoveEach;
-    const int wave = threadIdx.x >> 6, size = 1 << plan.digit, digit = threadIdx.x;
-    const unsigned tokens = (unsigned)a.sentences * a.words, first = blockIdx.x * (unsigned)(kEach * kSortThreads);
+    const int wave = threadIdx.x >> 6, size = 1 << bits, digit = threadIdx.x;
+    const unsigned first = blockIdx.x * (unsigned)(kEach * kSortThreads);
     unsigned key[kEach];
     int place[kEach], rank[kEach];
     bool there[kEach];
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
         const unsigned t = first + own_token(kEach, i);
-        there[i] = t < tokens;
+        there[i] = t < a.count;
         key[i] = !there[i] ? 0u : from.keys ? from.keys[t] : sort_key(a, t);
         place[i] = !there[i] ? 0 : from.keys ? from.places[t] : (int)t;
     }
@@ -806,7 +824,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_move_kernel(EmbedGradArgs a
     int before = 0, total = 0;
     if (digit < size) {
         int g = 0;
-        for (; g + 16 <= plan.groups; g += 16) {
+        for (; g + 16 <= groups; g += 16) {
             int n[16];
 #pragma unroll
             for (int u = 0; u < 16; ++u) n[u] = counts[(size_t)(g + u) * size + digit];
@@ -816,13 +834,13 @@ __global__ __launch_bounds__(kSortThreads) void sort_move_kernel(EmbedGradArgs a
                 total += n[u];
             }
         }
-        for (; g < plan.groups; ++g) {
+        for (; g < groups; ++g) {
             const int n = counts[(size_t)g * size + digit];
             before += g < (int)blockIdx.x ? n : 0;
             total += n;
         }
     }
-    rank_tokens<kEach, kMaxDigit>(key, there, kEach, shift, plan.digit, of_wave, rank);
+    rank_tokens<kEach, kMaxDigit>(key, there, kEach, shift, bits, of_wave, rank);
     const int base = sum_before(total, wave_sums) + before;
     if (digit < size) spread<kMaxDigit>(of_wave, digit, base);
     lds_barrier();
@@ -908,10 +926,10 @@ __global__ __launch_bounds__(kRunThreads) void runs_kernel(EmbedGradArgs a, cons
 
 // Before a launch of few tokens: what has to be turned and, where that is much, set to zero.
 template <class G, class W>
-__global__ __launch_bounds__(kSortThreads) void beside_kernel(EmbedGradArgs a, G* rows, Beside beside)
+__global__ __launch_bounds__(kSortThreads) void turn_or_fill_kernel(TurnArgs turn, Fill fill)
 {
     __shared__ __attribute__((aligned(16))) char room[tiles_room<G>()];
-    do_beside<G, W>(a, rows, beside, blockIdx.x, room);
+    turn_or_fill<G, W>(turn, fill, blockIdx.x, room);
 }
 
 int type_bytes(int dtype) { return dtype == kF32 ? 4 : 2; }
@@ -938,11 +956,11 @@ Parts parts_of(const EmbedGradArgs& a, int grad_dtype)
 }
 
 template <class G, class W>
-int launch_grad(const EmbedGradArgs& a, const Parts& parts, hipStream_t s)
+int launch_grad(const EmbedGradArgs& a, const Parts& parts, char* workspace, hipStream_t s)
 {
     const long long tokens = (long long)a.sentences * a.words, column_blocks = ((long long)a.dim + kColumns - 1) / kColumns;
     const G* grad = static_cast<const G*>(a.grad);
-    G* rows = reinterpret_cast<G*>(a.workspace);
+    G* rows = reinterpret_cast<G*>(workspace);
     long long tiles = 0;
     if (parts.rows) {
         typedef Turn<G> U;
@@ -951,23 +969,24 @@ int launch_grad(const EmbedGradArgs& a, const Parts& parts, hipStream_t s)
         grad = rows;
     }
     const unsigned long long elements = a.accumulate ? 0 : (unsigned long long)a.vocab * a.dim;
-    Beside beside{(unsigned)tiles, 0, elements};
+    const TurnArgs turn{a.grad, rows, a.dim, a.sentences, a.words, (unsigned)tiles};
     if (tokens <= kFewTokens) {
         const bool zeros = !a.accumulate && elements * sizeof(W) <= kOwnZeros && a.vocab <= (long long)kMarks * kBuckets;
-        if (zeros) beside.fill = 0;
-        const unsigned long long blocks = beside_blocks<W>(beside);
+        const Fill fill{a.table_grad, zeros ? 0 : elements};
+        const unsigned long long blocks = blocks_of<W>(turn.tiles, fill);
         if (blocks >= (1ull << 31)) return (int)hipErrorInvalidValue;
-        if (blocks) hipLaunchKernelGGL((beside_kernel<G, W>), dim3((unsigned)blocks), dim3(kSortThreads), 0, s, a, rows, beside);
+        if (blocks) hipLaunchKernelGGL((turn_or_fill_kernel<G, W>), dim3((unsigned)blocks), dim3(kSortThreads), 0, s, turn, fill);
         const SortPlan plan = sort_plan((a.vocab - 1) >> kBucketBits, kBucketDigit, tokens);
         const unsigned groups = (unsigned)std::min<long long>(a.vocab, kBuckets);
         const unsigned shares = (unsigned)std::min<long long>(column_blocks, kBuckets / groups);      // of the column blocks: a workgroup a CU
-        hipLaunchKernelGGL((bucket_kernel<G, W>), dim3(groups, shares), dim3(kSortThreads), 0, s, a, grad, plan, (int)column_blocks, zeros);
+        hipLaunchKernelGGL((bucket_kernel<G, W>), dim3(groups, shares), dim3(kSortThreads), 0, s, a, grad, plan.passes, plan.digit, (int)column_blocks,
+                           (int)shares, zeros);
         return (int)hipGetLastError();
     }
     const SortPlan plan = sort_plan(a.vocab, kMaxDigit, tokens);
     const long long run_blocks = ((tokens + kRunWaves * kSlot - 1) / (kRunWaves * kSlot)) * column_blocks;
     if (run_blocks >= (1ll << 31)) return (int)hipErrorInvalidValue;
-    char* at = a.workspace + parts.rows;
+    char* at = workspace + parts.rows;
     Sorted sorted[2];
     for (int i = 0; i < 2; ++i) {
         sorted[i].keys = reinterpret_cast<unsigned*>(at);
@@ -977,22 +996,24 @@ int launch_grad(const EmbedGradArgs& a, const Parts& parts, hipStream_t s)
     int* counts = reinterpret_cast<int*>(at);
     float* windows = reinterpret_cast<float*>(at + parts.counts);
     Sorted from{nullptr, nullptr};
+    const TokenArgs named{a.tokens, a.vocab, a.padding, (unsigned)tokens, a.wide};
     const int launches = 2 * plan.passes;
+    unsigned long long filled = 0;
     for (int l = 0; l < launches; ++l) {
         const unsigned long long kVec = 16 / sizeof(W), end = l + 1 == launches ? elements : elements * (l + 1) / launches / kVec * kVec;
-        beside.fill = end - beside.fill_from;
-        const int shift = l / 2 * plan.digit;
-        const unsigned long long blocks = plan.groups + beside_blocks<W>(beside);
+        const Fill fill{static_cast<W*>(a.table_grad) + filled, end - filled};
+        filled = end;
+        const short shift = (short)(l / 2 * plan.digit), bits = (short)plan.digit;
+        const unsigned long long blocks = plan.groups + blocks_of<W>(l == 0 ? turn.tiles : 0, fill);
         if (blocks >= (1ull << 31)) return (int)hipErrorInvalidValue;
-        const dim3 grid((unsigned)blocks);
         if (l % 2 == 0) {
-            hipLaunchKernelGGL((sort_count_kernel<G, W>), grid, dim3(kSortThreads), 0, s, a, rows, beside, plan, shift, from, counts);
+            TurnArgs here = turn;
+            if (l > 0) here.tiles = 0;
+            hipLaunchKernelGGL((sort_count_kernel<G, W>), dim3((unsigned)blocks), dim3(kSortThreads), 0, s, named, here, fill, from.keys, counts, plan.groups, shift, bits);
         } else {
-            hipLaunchKernelGGL((sort_move_kernel<W>), grid, dim3(kSortThreads), 0, s, a, beside, plan, shift, from, counts, sorted[l / 2 & 1]);
+            hipLaunchKernelGGL(sort_move_kernel<W>, dim3((unsigned)blocks), dim3(kSortThreads), 0, s, named, fill, from, sorted[l / 2 & 1], counts, plan.groups, shift, bits);
             from = sorted[l / 2 & 1];
         }
-        beside.tiles = 0;
-        beside.fill_from = end;
     }
     constexpr int kWaves = kThreads / 64;
     const long long window_blocks = (tokens / kWindow * column_blocks + kWaves - 1) / kWaves;
@@ -1004,9 +1025,19 @@ int launch_grad(const EmbedGradArgs& a, const Parts& parts, hipStream_t s)
 
 // No tokens: all rows are zero.
 template <class W>
-__global__ __launch_bounds__(kThreads) void zero_kernel(W* out, unsigned long long count)
+__global__ __launch_bounds__(kSortThreads) void zero_kernel(Fill fill)
 {
-    for (unsigned long long i = (unsigned long long)blockIdx.x * kThreads + threadIdx.x; i < count; i += (unsigned long long)gridDim.x * kThreads) out[i] = (W)0.f;
+    fill_part<W>(fill, blockIdx.x);
+}
+
+template <class W>
+int launch_zero(const EmbedGradArgs& a, hipStream_t s)
+{
+    const Fill fill{a.table_grad, (unsigned long long)a.vocab * a.dim};
+    const unsigned long long blocks = blocks_of<W>(0, fill);
+    if (blocks >= (1ull << 31)) return (int)hipErrorInvalidValue;
+    hipLaunchKernelGGL(zero_kernel<W>, dim3((unsigned)blocks), dim3(kSortThreads), 0, s, fill);
+    return (int)hipGetLastError();
 }
 
 }  // namespace
@@ -1021,20 +1052,14 @@ int launch_embed(int dtype, const EmbedArgs& a, void* stream)
 
 long long embed_grad_workspace(const EmbedGradArgs& a, int grad_dtype) { return parts_of(a, grad_dtype).total; }
 
-int launch_embed_grad(int grad_dtype, int table_dtype, const EmbedGradArgs& a, void* stream)
+int launch_embed_grad(int grad_dtype, int table_dtype, const EmbedGradArgs& a, char* workspace, void* stream)
 {
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    if ((long long)a.sentences * a.words == 0) {
-        const unsigned long long count = (unsigned long long)a.vocab * a.dim;
-        const dim3 grid((unsigned)std::min<unsigned long long>((count + kThreads - 1) / kThreads, 16384));
-        if (table_dtype == kF32) hipLaunchKernelGGL(zero_kernel<float>, grid, dim3(kThreads), 0, s, static_cast<float*>(a.table_grad), count);
-        else hipLaunchKernelGGL(zero_kernel<_Float16>, grid, dim3(kThreads), 0, s, static_cast<_Float16*>(a.table_grad), count);
-        return (int)hipGetLastError();
-    }
+    if ((long long)a.sentences * a.words == 0) return table_dtype == kF32 ? launch_zero<float>(a, s) : launch_zero<_Float16>(a, s);      // (zeros of 16 bits)
     const Parts parts = parts_of(a, grad_dtype);
-    if (grad_dtype == kF32) return launch_grad<float, float>(a, parts, s);
-    if (grad_dtype == kF16) return table_dtype == kF32 ? launch_grad<_Float16, float>(a, parts, s) : launch_grad<_Float16, _Float16>(a, parts, s);
-    return table_dtype == kF32 ? launch_grad<__bf16, float>(a, parts, s) : launch_grad<__bf16, __bf16>(a, parts, s);
+    if (grad_dtype == kF32) return launch_grad<float, float>(a, parts, workspace, s);
+    if (grad_dtype == kF16) return table_dtype == kF32 ? launch_grad<_Float16, float>(a, parts, workspace, s) : launch_grad<_Float16, _Float16>(a, parts, workspace, s);
+    return table_dtype == kF32 ? launch_grad<__bf16, float>(a, parts, workspace, s) : launch_grad<__bf16, __bf16>(a, parts, workspace, s);
 }
 
 }  // namespace sc

@@ -209,8 +209,10 @@ __device__ __forceinline__ void tile_of(unsigned block, unsigned tiles, int down
 
 // A tile of 16 MB WM rows of x by 16 NB WN rows of w, 128 bytes of each a step; WM x WN wavefronts with MB x NB blocks of 16 x 16 sums.
 template <class T, int MB, int NB, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_product_kernel(Int8Args a, const int8_t* x, const float* x_scale, bool aligned)
+__global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_product_kernel(Int8Args a, unsigned tiles, bool aligned)
 {
+    const int8_t* x = static_cast<const int8_t*>(a.x);
+    const float* x_scale = a.x_scale;
     constexpr int TM = 16 * MB * WM, TN = 16 * NB * WN, W = WM * WN;
     constexpr int kLoadsX = TM / 8 / W, kLoadsW = TN / 8 / W, kLoads = kLoadsX + kLoadsW;
     constexpr int kX = TM * 128, kW = TN * 128, kHalf = MB / 2;
@@ -222,7 +224,7 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_prod
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int down = (a.M + TM - 1) / TM, across = (a.N + TN - 1) / TN;
     int tm, tn;
-    tile_of(blockIdx.x, gridDim.x, down, across, tm, tn);
+    tile_of(blockIdx.x, tiles, down, across, tm, tn);
     const int m0 = tm * TM, n0 = tn * TN;
 
     int4v from_x = descriptor_of(x + (size_t)m0 * a.pitch, (long long)min(TM, a.M - m0) * a.pitch);
@@ -400,12 +402,12 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_prod
 }
 
 template <class T, int MB, int NB, int WM, int WN>
-int launch_tile_product(const Int8Args& a, const int8_t* x, const float* x_scale, hipStream_t s)
+int launch_tile_product(const Int8Args& a, hipStream_t s)
 {
     const long long tiles = ((a.M + 16ll * MB * WM - 1) / (16 * MB * WM)) * ((a.N + 16ll * NB * WN - 1) / (16 * NB * WN));
     if (tiles >= (1ll << 31)) return (int)hipErrorInvalidValue;
     const bool aligned = a.ldo * sizeof(T) % 16 == 0 && reinterpret_cast<uintptr_t>(a.out) % 16 == 0;
-    hipLaunchKernelGGL((tile_product_kernel<T, MB, NB, WM, WN>), dim3((unsigned)tiles), dim3(64 * WM * WN), 0, s, a, x, x_scale, aligned);
+    hipLaunchKernelGGL((tile_product_kernel<T, MB, NB, WM, WN>), dim3((unsigned)tiles), dim3(64 * WM * WN), 0, s, a, (unsigned)tiles, aligned);
     return (int)hipGetLastError();
 }
 
@@ -425,7 +427,7 @@ bool quantises_itself(int M, int pitch) { return M <= 16 && (long long)M * pitch
 // in the order that the products take would touch 16 rows with 16 lanes in a row, at a quarter of the rate.)  X is int8_t, x then
 // comes the same way as w; or the type of an input that every workgroup quantises for itself while its first weights are on their way.
 template <class T, class X, int MB, int NB, int W, int D>
-__global__ __launch_bounds__(64 * W) void row_product_kernel(Int8Args a, const int8_t* x8, const float* x_scale)
+__global__ __launch_bounds__(64 * W) void row_product_kernel(Int8Args a)
 {
     constexpr bool kGiven = IsByte<X>::value;
     constexpr int kTokens = 16 * MB, kChannels = 16 * NB, kThreads = 64 * W;
@@ -464,7 +466,7 @@ __global__ __launch_bounds__(64 * W) void row_product_kernel(Int8Args a, const i
 
     // Pieces of 16 bytes are permuted within the 128 bytes of a row as in the tile kernel.
     int4v from_w = descriptor_of(a.w + (size_t)n0 * a.pitch, (long long)min(kChannels, a.N - n0) * a.pitch);
-    int4v from_x = kGiven ? descriptor_of(x8 + (size_t)m0 * a.pitch, (long long)min(kTokens, a.M - m0) * a.pitch) : from_w;
+    int4v from_x = kGiven ? descriptor_of(static_cast<const int8_t*>(a.x) + (size_t)m0 * a.pitch, (long long)min(kTokens, a.M - m0) * a.pitch) : from_w;
     const int bytes_w = from_w[2], bytes_x = from_x[2];
     const unsigned lds0 = (unsigned)(uintptr_t)(SC_LDS char*)lds + wave * D * kUnit;
     unsigned offset[2];      // of the rows lane / 8 of an even and an odd load: their permutations differ
@@ -476,7 +478,7 @@ __global__ __launch_bounds__(64 * W) void row_product_kernel(Int8Args a, const i
         else channel_bias[lane] = 0.f;
     }
     if (kGiven && wave == 2)
-        load_word_to_lds(descriptor_of(x_scale + m0, min(kTokens, a.M - m0) * 4ll), lane * 4, (unsigned)(uintptr_t)(SC_LDS float*)token_scale);
+        load_word_to_lds(descriptor_of(a.x_scale + m0, min(kTokens, a.M - m0) * 4ll), lane * 4, (unsigned)(uintptr_t)(SC_LDS float*)token_scale);
     auto load = [&](int slot, int unit) {
         from_w[2] = unit < units ? bytes_w : 0;
         from_x[2] = unit < units ? bytes_x : 0;
@@ -585,11 +587,11 @@ __global__ __launch_bounds__(64 * W) void row_product_kernel(Int8Args a, const i
 }
 
 template <class T, class X, int MB, int NB, int W, int D>
-int launch_row_product(const Int8Args& a, const int8_t* x, const float* x_scale, hipStream_t s)
+int launch_row_product(const Int8Args& a, hipStream_t s)
 {
     const long long groups = ((a.M + 16ll * MB - 1) / (16 * MB)) * ((a.N + 16ll * NB - 1) / (16 * NB));
     if (groups >= (1ll << 31)) return (int)hipErrorInvalidValue;
-    hipLaunchKernelGGL((row_product_kernel<T, X, MB, NB, W, D>), dim3((unsigned)groups), dim3(64 * W), 0, s, a, x, x_scale);
+    hipLaunchKernelGGL((row_product_kernel<T, X, MB, NB, W, D>), dim3((unsigned)groups), dim3(64 * W), 0, s, a);
     return (int)hipGetLastError();
 }
 
@@ -624,9 +626,9 @@ double tile_estimate(int MB, int M, int N, int pitch)
 }
 
 template <class T>
-int launch_product(const Int8Args& a, const int8_t* x, const float* x_scale, hipStream_t s)
+int launch_product(const Int8Args& a, hipStream_t s)
 {
-    typedef int (*Launch)(const Int8Args&, const int8_t*, const float*, hipStream_t);
+    typedef int (*Launch)(const Int8Args&, hipStream_t);
     Launch best = nullptr;
     double least = 0.0;
     auto consider = [&](double us, Launch launch) {
@@ -657,15 +659,15 @@ int launch_product(const Int8Args& a, const int8_t* x, const float* x_scale, hip
     tiles(two);
     tiles(four);
     tiles(eight);
-    return best(a, x, x_scale, s);
+    return best(a, s);
 }
 
 template <class T, class X>
 int launch_own(const Int8Args& a, hipStream_t s)
 {
-    if (a.N >= 16 * 1024) return launch_row_product<T, X, 1, 4, 8, 2>(a, nullptr, nullptr, s);
-    if (a.N >= 8 * 1024) return launch_row_product<T, X, 1, 2, 8, 4>(a, nullptr, nullptr, s);
-    return launch_row_product<T, X, 1, 1, 16, 4>(a, nullptr, nullptr, s);
+    if (a.N >= 16 * 1024) return launch_row_product<T, X, 1, 4, 8, 2>(a, s);
+    if (a.N >= 8 * 1024) return launch_row_product<T, X, 1, 2, 8, 4>(a, s);
+    return launch_row_product<T, X, 1, 1, 16, 4>(a, s);
 }
 
 template <class T>
@@ -693,27 +695,26 @@ long long int8_workspace(int M, int, int K, int in_dtype, int)
     return (long long)M * ((K + 127) / 128 * 128) + (M * 4ll + 15) / 16 * 16;
 }
 
-int launch_int8_linear(int in_dtype, int out_dtype, const Int8Args& a, void* stream)
+int launch_int8_linear(int in_dtype, int out_dtype, const Int8Args& given, char* workspace, void* stream)
 {
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    const int8_t* x = static_cast<const int8_t*>(a.x);
-    const float* x_scale = a.x_scale;
+    Int8Args a = given;
     if (in_dtype != kI8 && quantises_itself(a.M, a.pitch)) {
         if (out_dtype == kF32) return launch_own<float>(in_dtype, a, s);
         if (out_dtype == kF16) return launch_own<_Float16>(in_dtype, a, s);
         return launch_own<__bf16>(in_dtype, a, s);
     }
     if (in_dtype != kI8) {
-        int8_t* q = reinterpret_cast<int8_t*>(a.workspace);
-        float* scale = reinterpret_cast<float*>(a.workspace + (size_t)a.M * a.pitch);
+        int8_t* q = reinterpret_cast<int8_t*>(workspace);
+        float* scale = reinterpret_cast<float*>(workspace + (size_t)a.M * a.pitch);
         const int e = launch_int8_quantize(in_dtype, a.x, q, scale, a.M, a.K, a.ldx, stream);
         if (e != 0) return e;
-        x = q;
-        x_scale = scale;
+        a.x = q;
+        a.x_scale = scale;
     }
-    if (out_dtype == kF32) return launch_product<float>(a, x, x_scale, s);
-    if (out_dtype == kF16) return launch_product<_Float16>(a, x, x_scale, s);
-    return launch_product<__bf16>(a, x, x_scale, s);
+    if (out_dtype == kF32) return launch_product<float>(a, s);
+    if (out_dtype == kF16) return launch_product<_Float16>(a, s);
+    return launch_product<__bf16>(a, s);
 }
 
 }  // namespace sc

@@ -89,7 +89,7 @@ int sparse_conv_embed_backward(const void* grad, const void* tokens, void* table
     if (!table_grad || !aligned(table_grad, b2)) return SC_EINVAL;
     sc::EmbedGradArgs a{grad, tokens, table_grad, vocab, padding, dim, sentences, words, scale,
                         (flags & SC_EMBED_CHANNELS_FIRST) != 0, (flags & SC_EMBED_TOKENS_64) != 0,
-                        (flags & SC_EMBED_ACCUMULATE) != 0, static_cast<char*>(workspace)};
+                        (flags & SC_EMBED_ACCUMULATE) != 0};
     if (count > 0) {
         if (!grad || !tokens || !aligned(grad, b) || !aligned(tokens, tb)) return SC_EINVAL;
         const long long need = sc::embed_grad_workspace(a, grad_dtype), table_bytes = vocab * dim * b2;
@@ -100,7 +100,7 @@ int sparse_conv_embed_backward(const void* grad, const void* tokens, void* table
     } else if (flags & SC_EMBED_ACCUMULATE) {
         return SC_OK;
     }
-    return sc::launch_embed_grad(grad_dtype, table_dtype, a, stream) == 0 ? SC_OK : SC_EHIP;
+    return sc::launch_embed_grad(grad_dtype, table_dtype, a, static_cast<char*>(workspace), stream) == 0 ? SC_OK : SC_EHIP;
 }
 
 int sparse_conv_int8_quantize(const void* x, signed char* q, float* scale, int rows, int K, long long ldx, int dtype, void* stream)
@@ -145,8 +145,8 @@ int sparse_conv_int8_linear(const void* x, const float* x_scale, const signed ch
     if (need > 0 && (overlap(workspace, need, x, x_bytes) || overlap(workspace, need, w, N * pitch) || overlap(workspace, need, out, out_bytes)))
         return SC_EINVAL;
     const sc::Int8Args a{x, x_scale, reinterpret_cast<const int8_t*>(w), w_scale, bias, out, M, N, K, (int)pitch, ldx, ldo,
-                         (flags & SC_EPILOGUE_RELU) != 0, static_cast<char*>(workspace)};
-    return sc::launch_int8_linear(in_dtype, out_dtype, a, stream) == 0 ? SC_OK : SC_EHIP;
+                         (flags & SC_EPILOGUE_RELU) != 0};
+    return sc::launch_int8_linear(in_dtype, out_dtype, a, static_cast<char*>(workspace), stream) == 0 ? SC_OK : SC_EHIP;
 }
 
 }  // extern "C"

@@ -6,6 +6,9 @@
 
 namespace sc {
 
+// (A launch whose arguments take more than 112 bytes, the block counts of the grid among them where a kernel asks for them, keeps the
+// host 3.5 us instead of 2.75: the structures below hold what the kernels need and nothing else.)
+
 struct EmbedArgs {
     const void* table;     // [vocab][dim]
     const void* tokens;    // [sentences][words]
@@ -25,10 +28,9 @@ struct EmbedGradArgs {
     int dim, sentences, words;
     float scale;
     bool channels_first, wide, accumulate;
-    char* workspace;
 };
 long long embed_grad_workspace(const EmbedGradArgs& a, int grad_dtype);
-int launch_embed_grad(int grad_dtype, int table_dtype, const EmbedGradArgs& a, void* stream);
+int launch_embed_grad(int grad_dtype, int table_dtype, const EmbedGradArgs& a, char* workspace, void* stream);
 
 int launch_int8_quantize(int dtype, const void* x, int8_t* q, float* scale, int rows, int K, long long ldx, void* stream);
 
@@ -43,9 +45,8 @@ struct Int8Args {
     int pitch;             // bytes of a row of w (and of x, where it is 8-bit)
     long long ldx, ldo;
     bool relu;
-    char* workspace;
 };
 long long int8_workspace(int M, int N, int K, int in_dtype, int out_dtype);
-int launch_int8_linear(int in_dtype, int out_dtype, const Int8Args& a, void* stream);
+int launch_int8_linear(int in_dtype, int out_dtype, const Int8Args& a, char* workspace, void* stream);
 
 }  // namespace sc
