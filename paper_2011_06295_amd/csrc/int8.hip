@@ -20,17 +20,17 @@ constexpr float kTiny = 0x1p-100f;   // a row whose largest size is below this c
 // ---------------------------------------------------------------- rows to 8-bit integers
 
 template <class T>
-struct Piece {     // what one load of 16 bytes holds
+struct Piece {     // what one load of 16 bytes holds, from any element on (the hardware splits what crosses a line)
     static constexpr int kCount = 16 / sizeof(T);
-    typedef T type __attribute__((ext_vector_type(16 / sizeof(T))));
+    typedef T type __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
 };
 
 // Elements k .. k + kCount - 1 of a row; zeros past its end.
 template <class T>
-__device__ __forceinline__ typename Piece<T>::type load_piece(const T* row, int k, int K, bool aligned)
+__device__ __forceinline__ typename Piece<T>::type load_piece(const T* row, int k, int K)
 {
     typedef typename Piece<T>::type V;
-    if (aligned && k + Piece<T>::kCount <= K) return *reinterpret_cast<const V*>(row + k);
+    if (k + Piece<T>::kCount <= K) return *reinterpret_cast<const V*>(row + k);
     V v;
 #pragma unroll
     for (int e = 0; e < Piece<T>::kCount; ++e) v[e] = k + e < K ? row[k + e] : (T)0.f;
@@ -100,7 +100,7 @@ __device__ __forceinline__ unsigned largest_in_wavefront(unsigned most)
 // A row for kLanes threads (several rows a workgroup where that is one wavefront).  Up to kKept pieces a thread stay in registers
 // between the search for the largest size and the rounding; longer rows are read again.
 template <class T, int kLanes>
-__global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void quantize_kernel(const T* x, int8_t* q, float* scale, int rows, int K, int pitch, long long ldx, bool aligned)
+__global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void quantize_kernel(const T* x, int8_t* q, float* scale, int rows, int K, int pitch, long long ldx)
 {
     typedef typename Piece<T>::type V;
     constexpr int kKept = 4, kCount = Piece<T>::kCount, kRows = kLanes < 256 ? 256 / kLanes : 1, kWaves = kLanes / 64;
@@ -112,10 +112,10 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void quantize_kernel(c
     V kept[kKept];
     unsigned most = 0;
 #pragma unroll
-    for (int p = 0; p < kKept; ++p) kept[p] = load_piece<T>(x, (p * kLanes + t) * kCount, K, aligned);
+    for (int p = 0; p < kKept; ++p) kept[p] = load_piece<T>(x, (p * kLanes + t) * kCount, K);
 #pragma unroll
     for (int p = 0; p < kKept; ++p) most = largest_of<T>(kept[p], most);
-    for (int k = (kKept * kLanes + t) * kCount; k < K; k += kLanes * kCount) most = largest_of<T>(load_piece<T>(x, k, K, aligned), most);
+    for (int k = (kKept * kLanes + t) * kCount; k < K; k += kLanes * kCount) most = largest_of<T>(load_piece<T>(x, k, K), most);
     most = largest_in_wavefront(size_of<T>(most));
     if (kWaves > 1) {
         __shared__ unsigned of_wave[kWaves];
@@ -138,22 +138,21 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void quantize_kernel(c
         const int k = (p * kLanes + t) * kCount;
         if (k < pitch) store(kept[p], k);
     }
-    for (int k = (kKept * kLanes + t) * kCount; k < pitch; k += kLanes * kCount) store(load_piece<T>(x, k, K, aligned), k);
+    for (int k = (kKept * kLanes + t) * kCount; k < pitch; k += kLanes * kCount) store(load_piece<T>(x, k, K), k);
 }
 
 template <class T>
 int launch_quantize(const void* x, int8_t* q, float* scale, int rows, int K, long long ldx, hipStream_t s)
 {
     const int pitch = (K + 127) / 128 * 128, pieces = pitch / Piece<T>::kCount;
-    const bool aligned = ldx * sizeof(T) % 16 == 0 && reinterpret_cast<uintptr_t>(x) % 16 == 0;
     const T* in = static_cast<const T*>(x);
     // one wavefront a row where a lane's pieces fit its registers; few long rows by as many threads as have a piece each
     if (pieces <= 128 || (pieces <= 256 && rows >= 1024))
-        hipLaunchKernelGGL((quantize_kernel<T, 64>), dim3((rows + 3) / 4), dim3(256), 0, s, in, q, scale, rows, K, pitch, ldx, aligned);
+        hipLaunchKernelGGL((quantize_kernel<T, 64>), dim3((rows + 3) / 4), dim3(256), 0, s, in, q, scale, rows, K, pitch, ldx);
     else if (pieces <= 512 || rows >= 512)
-        hipLaunchKernelGGL((quantize_kernel<T, 256>), dim3(rows), dim3(256), 0, s, in, q, scale, rows, K, pitch, ldx, aligned);
+        hipLaunchKernelGGL((quantize_kernel<T, 256>), dim3(rows), dim3(256), 0, s, in, q, scale, rows, K, pitch, ldx);
     else
-        hipLaunchKernelGGL((quantize_kernel<T, 1024>), dim3(rows), dim3(1024), 0, s, in, q, scale, rows, K, pitch, ldx, aligned);
+        hipLaunchKernelGGL((quantize_kernel<T, 1024>), dim3(rows), dim3(1024), 0, s, in, q, scale, rows, K, pitch, ldx);
     return (int)hipGetLastError();
 }
 
@@ -209,7 +208,7 @@ __device__ __forceinline__ void tile_of(unsigned block, unsigned tiles, int down
 
 // A tile of 16 MB WM rows of x by 16 NB WN rows of w, 128 bytes of each a step; WM x WN wavefronts with MB x NB blocks of 16 x 16 sums.
 template <class T, int MB, int NB, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_product_kernel(Int8Args a, unsigned tiles, bool aligned)
+__global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_product_kernel(Int8Args a, unsigned tiles)
 {
     const int8_t* x = static_cast<const int8_t*>(a.x);
     const float* x_scale = a.x_scale;
@@ -358,7 +357,7 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_prod
     for (int i = 0; i < MB; ++i) xs[i] = token_scale[(wm * MB + i) * 16 + r];
     typedef typename Piece<T>::type V;
     constexpr int kV = Piece<T>::kCount;
-    auto finish = [&](auto inside) {      // inside: the tile lies whole within the output, whose rows start at multiples of 16 bytes
+    auto finish = [&](auto inside) {      // inside: the tile lies whole within the output
         each<NB / 2>([&](auto pair) {
             constexpr int j = 2 * pair;
             const int tile_n = wn * 16 * NB + j * 16 + q * 8, n = n0 + tile_n;
@@ -386,7 +385,7 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_prod
 #pragma unroll
                     for (int c = 0; c < 8 / kV; ++c) reinterpret_cast<V*>(out)[c] = y[c];
                 } else if (m < a.M) {
-                    if (aligned && n + 8 <= a.N)
+                    if (n + 8 <= a.N)
 #pragma unroll
                         for (int c = 0; c < 8 / kV; ++c) reinterpret_cast<V*>(out)[c] = y[c];
                     else
@@ -397,7 +396,7 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_prod
             });
         });
     };
-    if (aligned && m0 + TM <= a.M && n0 + TN <= a.N) finish(std::true_type{});
+    if (m0 + TM <= a.M && n0 + TN <= a.N) finish(std::true_type{});
     else finish(std::false_type{});
 }
 
@@ -406,8 +405,7 @@ int launch_tile_product(const Int8Args& a, hipStream_t s)
 {
     const long long tiles = ((a.M + 16ll * MB * WM - 1) / (16 * MB * WM)) * ((a.N + 16ll * NB * WN - 1) / (16 * NB * WN));
     if (tiles >= (1ll << 31)) return (int)hipErrorInvalidValue;
-    const bool aligned = a.ldo * sizeof(T) % 16 == 0 && reinterpret_cast<uintptr_t>(a.out) % 16 == 0;
-    hipLaunchKernelGGL((tile_product_kernel<T, MB, NB, WM, WN>), dim3((unsigned)tiles), dim3(64 * WM * WN), 0, s, a, (unsigned)tiles, aligned);
+    hipLaunchKernelGGL((tile_product_kernel<T, MB, NB, WM, WN>), dim3((unsigned)tiles), dim3(64 * WM * WN), 0, s, a, (unsigned)tiles);
     return (int)hipGetLastError();
 }
 
@@ -451,14 +449,13 @@ __global__ __launch_bounds__(64 * W) void row_product_kernel(Int8Args a)
     const int per_row = a.pitch / kCount, pieces = min(kTokens, a.M - m0) * per_row;
     __shared__ unsigned largest[16];
     if constexpr (!kGiven) {
-        const bool aligned = a.ldx * sizeof(X) % 16 == 0 && reinterpret_cast<uintptr_t>(a.x) % 16 == 0;
         const X* x = static_cast<const X*>(a.x) + (size_t)m0 * a.ldx;
         if (threadIdx.x < 16) largest[threadIdx.x] = 0;
 #pragma unroll
         for (int i = 0; i < kKept; ++i) {
             const int p = i * kThreads + threadIdx.x;
             m_of[i] = p / per_row;
-            if (p < pieces) kept[i] = load_piece<X>(x + m_of[i] * a.ldx, p % per_row * kCount, a.K, aligned);
+            if (p < pieces) kept[i] = load_piece<X>(x + m_of[i] * a.ldx, p % per_row * kCount, a.K);
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (the compiler would wait for the weights as well)
         __syncthreads();
@@ -562,8 +559,7 @@ __global__ __launch_bounds__(64 * W) void row_product_kernel(Int8Args a)
         for (int j = 0; j < NB; ++j)
             *reinterpret_cast<int4v*>(lds + wave * D * kUnit + ((i * 16 + r) * kChannels + j * 16 + q * 4) * 4) = acc[i][j];
     __syncthreads();
-    typedef T four __attribute__((ext_vector_type(4)));
-    const bool whole = a.ldo % 4 == 0 && reinterpret_cast<uintptr_t>(a.out) % sizeof(four) == 0 && n0 + kChannels <= a.N;
+    typedef T four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
     for (int o = threadIdx.x; o < kTokens * kChannels / 4; o += kThreads) {
         const int token = o / (kChannels / 4), channel = o % (kChannels / 4) * 4, m = m0 + token, n = n0 + channel;
         if (m >= a.M) continue;
@@ -578,7 +574,7 @@ __global__ __launch_bounds__(64 * W) void row_product_kernel(Int8Args a)
             y[e] = (T)v;
         }
         T* out = static_cast<T*>(a.out) + m * a.ldo + n;
-        if (whole) *reinterpret_cast<four*>(out) = y;
+        if (n + 4 <= a.N) *reinterpret_cast<four*>(out) = y;
         else
 #pragma unroll
             for (int e = 0; e < 4; ++e)
