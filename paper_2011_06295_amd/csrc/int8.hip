@@ -206,9 +206,15 @@ __device__ __forceinline__ void tile_of(unsigned block, unsigned tiles, int down
     tn = (int)(in / (unsigned)rows);
 }
 
+// Large tiles: a workgroup has a CU to itself, so it walks over tiles, `stride` apart, and loads the next one's first steps before it
+// finishes one.  (Three steps a tile at least: a barrier lies between what reads a set of scales and what loads over it.)
+template <int MB, int NB>
+constexpr bool kWalks = MB * NB >= 64;
+constexpr int kWalkSteps = 3;
+
 // A tile of 16 MB WM rows of x by 16 NB WN rows of w, 128 bytes of each a step; WM x WN wavefronts with MB x NB blocks of 16 x 16 sums.
 template <class T, int MB, int NB, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_product_kernel(Int8Args a, unsigned tiles)
+__global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_product_kernel(Int8Args a, unsigned tiles, unsigned stride)
 {
     const int8_t* x = static_cast<const int8_t*>(a.x);
     const float* x_scale = a.x_scale;
@@ -218,16 +224,11 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_prod
     static_assert(MB % 2 == 0 && NB % 2 == 0, "blocks come in pairs");
     static_assert(TM % 64 == 0 && TN % 64 == 0 && TM <= 64 * W && TN <= 64 * W, "a scale a thread");
     __shared__ __attribute__((aligned(256))) char lds[2 * kX + 2 * kW];
-    __shared__ __attribute__((aligned(16))) float channel_scale[TN], channel_bias[TN], token_scale[TM];
+    constexpr int kSets = kWalks<MB, NB> ? 2 : 1;      // the tile that is finished, and the next one
+    __shared__ __attribute__((aligned(16))) float channel_scale[kSets][TN], channel_bias[kSets][TN], token_scale[kSets][TM];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int down = (a.M + TM - 1) / TM, across = (a.N + TN - 1) / TN;
-    int tm, tn;
-    tile_of(blockIdx.x, tiles, down, across, tm, tn);
-    const int m0 = tm * TM, n0 = tn * TN;
-
-    int4v from_x = descriptor_of(x + (size_t)m0 * a.pitch, (long long)min(TM, a.M - m0) * a.pitch);
-    int4v from_w = descriptor_of(a.w + (size_t)n0 * a.pitch, (long long)min(TN, a.N - n0) * a.pitch);
+    const int down = (a.M + TM - 1) / TM, across = (a.N + TN - 1) / TN, steps = a.pitch / 128;
     // A row of LDS is the 128 bytes of a row's step; its eight pieces of 16 bytes are permuted by the row, so that the 16 rows that a
     // read takes one piece of lie in 16 different groups of four banks.  A lane's load fetches the piece that belongs where it lands.
     unsigned offset[kLoads];
@@ -238,23 +239,45 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_prod
         offset[i] = (unsigned)row * a.pitch + (((lane & 7) ^ turn) << 4);
     }
     const unsigned lds0 = (unsigned)(uintptr_t)(SC_LDS char*)lds;
-    unsigned at = 0, xdst = lds0, wdst = lds0 + 2 * kX;
-    auto load = [&](int i) {
-        if (i < kLoadsX) load_to_lds(from_x, offset[i], at, xdst + (wave * kLoadsX + i) * 1024);
-        else load_to_lds(from_w, offset[i], at, wdst + (wave * kLoadsW + i - kLoadsX) * 1024);
+    int4v from_x, from_w;
+    unsigned xdst = lds0, wdst = lds0 + 2 * kX, tile = blockIdx.x;
+    int next_m = 0, next_n = 0, step = 0, set = 0;      // what is loaded: a step of a tile, whose scales go to `set`
+    auto enter = [&]() {
+        int tm, tn;
+        tile_of(tile, tiles, down, across, tm, tn);
+        next_m = tm * TM;
+        next_n = tn * TN;
+        from_x = descriptor_of(x + (size_t)next_m * a.pitch, (long long)min(TM, a.M - next_m) * a.pitch);
+        from_w = descriptor_of(a.w + (size_t)next_n * a.pitch, (long long)min(TN, a.N - next_n) * a.pitch);
+        const long long ws = min(TN, a.N - next_n) * 4ll, xs = min(TM, a.M - next_m) * 4ll;
+        if (wave * 64 < TN) {
+            load_word_to_lds(descriptor_of(a.w_scale + next_n, ws), threadIdx.x * 4, (unsigned)(uintptr_t)(SC_LDS float*)channel_scale[set] + wave * 256);
+            if (a.bias) load_word_to_lds(descriptor_of(a.bias + next_n, ws), threadIdx.x * 4, (unsigned)(uintptr_t)(SC_LDS float*)channel_bias[set] + wave * 256);
+            else channel_bias[set][threadIdx.x] = 0.f;
+        }
+        if (wave * 64 < TM)
+            load_word_to_lds(descriptor_of(x_scale + next_m, xs), threadIdx.x * 4, (unsigned)(uintptr_t)(SC_LDS float*)token_scale[set] + wave * 256);
     };
-    const int steps = a.pitch / 128;
-    if (wave * 64 < TN) {
-        load_word_to_lds(descriptor_of(a.w_scale + n0, min(TN, a.N - n0) * 4ll), threadIdx.x * 4, (unsigned)(uintptr_t)(SC_LDS float*)channel_scale + wave * 256);
-        if (a.bias) load_word_to_lds(descriptor_of(a.bias + n0, min(TN, a.N - n0) * 4ll), threadIdx.x * 4, (unsigned)(uintptr_t)(SC_LDS float*)channel_bias + wave * 256);
-        else channel_bias[threadIdx.x] = 0.f;
-    }
-    if (wave * 64 < TM)
-        load_word_to_lds(descriptor_of(x_scale + m0, min(TM, a.M - m0) * 4ll), threadIdx.x * 4, (unsigned)(uintptr_t)(SC_LDS float*)token_scale + wave * 256);
+    auto advance = [&]() {
+        if (++step < steps) return;
+        tile += stride;
+        if (kWalks<MB, NB> && tile < tiles) {
+            step = 0;
+            set ^= 1;
+            enter();
+        } else {
+            from_x[2] = from_w[2] = 0;      // past the last step: zeros, and nothing is fetched
+        }
+    };
+    auto load = [&](int i) {
+        if (i < kLoadsX) load_to_lds(from_x, offset[i], step * 128, xdst + (wave * kLoadsX + i) * 1024);
+        else load_to_lds(from_w, offset[i], step * 128, wdst + (wave * kLoadsW + i - kLoadsX) * 1024);
+    };
+    enter();
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) load(i);
-    at += 128;
-    if (steps == 1) from_x[2] = from_w[2] = 0;      // past the last step: zeros, and nothing is fetched
+    int m0 = next_m, n0 = next_n, done = set;
+    advance();
     xdst += kX;
     wdst += kW;
 #pragma unroll
@@ -294,110 +317,118 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_prod
     // Then nothing reads this buffer any more and, spread over the second half, it is loaded with the bytes of the step after the next.
     // Halfway through, those of the next step (loaded in the step before) are waited for, and the first half's operands are read.
     int dx = kX, dw = kW;
-    for (int k = 0; k < steps; ++k) {
-        at += 128;
-        if (k + 2 >= steps) from_x[2] = from_w[2] = 0;
-        constexpr int kSlots = MB * NB, kTurn = kSlots / 2;
-        each<kSlots>([&](auto slot) {
-            constexpr int t = slot, i = t / NB, j = t % NB, kOps = kHalf + NB + MB;
-            multiply(acc[i][j], wf[0][j], xf[0][i]);
-            constexpr int first = (t * kOps + kSlots - 1) / kSlots, last = ((t + 1) * kOps + kSlots - 1) / kSlots;
-            each<last - first>([&](auto n) {
-                constexpr int o = first + n;
-                if constexpr (o < 2 * kHalf && o % 2 == 0) read_x(0, kHalf + o / 2);
-                else {
-                    constexpr int u = o < 2 * kHalf ? o / 2 : o - kHalf;
-                    if constexpr (u < NB) read_w(1, u);
-                    else read_x(1, u - NB);
-                }
-            });
-            __builtin_amdgcn_sched_barrier(0);
-        });
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_sched_barrier(0);
-        each<kSlots>([&](auto slot) {
-            constexpr int t = slot, i = t / NB, j = t % NB;
-            if constexpr (t == kTurn) {
-                constexpr int kIssued = (kTurn * kLoads + kSlots - 1) / kSlots;
-                asm volatile("s_waitcnt vmcnt(%0)" :: "n"(kIssued) : "memory");
-                __builtin_amdgcn_s_barrier();
-                asm volatile("" ::: "memory");
-                xa0 += dx;
-                xa1 += dx;
-                wa0 += dw;
-                wa1 += dw;
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            multiply(acc[i][j], wf[1][j], xf[1][i]);
-            constexpr int first = (t * kLoads + kSlots - 1) / kSlots, last = ((t + 1) * kLoads + kSlots - 1) / kSlots;
-            each<last - first>([&](auto n) { load(first + n); });
-            if constexpr (t >= kTurn) {
-                constexpr int kReads = NB + kHalf, kRoom = kSlots - kTurn, v = t - kTurn;
-                constexpr int from = (v * kReads + kRoom - 1) / kRoom, to = ((v + 1) * kReads + kRoom - 1) / kRoom;
-                each<to - from>([&](auto n) {
-                    constexpr int o = from + n;
-                    if constexpr (o < NB) read_w(0, o);
-                    else read_x(0, o - NB);
+    for (unsigned current = blockIdx.x; current < tiles; current += stride) {
+        for (int k = 0; k < steps; ++k) {
+            advance();
+            constexpr int kSlots = MB * NB, kTurn = kSlots / 2;
+            each<kSlots>([&](auto slot) {
+                constexpr int t = slot, i = t / NB, j = t % NB, kOps = kHalf + NB + MB;
+                multiply(acc[i][j], wf[0][j], xf[0][i]);
+                constexpr int first = (t * kOps + kSlots - 1) / kSlots, last = ((t + 1) * kOps + kSlots - 1) / kSlots;
+                each<last - first>([&](auto n) {
+                    constexpr int o = first + n;
+                    if constexpr (o < 2 * kHalf && o % 2 == 0) read_x(0, kHalf + o / 2);
+                    else {
+                        constexpr int u = o < 2 * kHalf ? o / 2 : o - kHalf;
+                        if constexpr (u < NB) read_w(1, u);
+                        else read_x(1, u - NB);
+                    }
                 });
-            }
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
             __builtin_amdgcn_sched_barrier(0);
-        });
-        xdst += dx;
-        wdst += dw;
-        dx = -dx;
-        dw = -dw;
-    }
+            each<kSlots>([&](auto slot) {
+                constexpr int t = slot, i = t / NB, j = t % NB;
+                if constexpr (t == kTurn) {
+                    constexpr int kIssued = (kTurn * kLoads + kSlots - 1) / kSlots;
+                    asm volatile("s_waitcnt vmcnt(%0)" :: "n"(kIssued) : "memory");
+                    __builtin_amdgcn_s_barrier();
+                    asm volatile("" ::: "memory");
+                    xa0 += dx;
+                    xa1 += dx;
+                    wa0 += dw;
+                    wa1 += dw;
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                multiply(acc[i][j], wf[1][j], xf[1][i]);
+                constexpr int first = (t * kLoads + kSlots - 1) / kSlots, last = ((t + 1) * kLoads + kSlots - 1) / kSlots;
+                each<last - first>([&](auto n) { load(first + n); });
+                if constexpr (t >= kTurn) {
+                    constexpr int kReads = NB + kHalf, kRoom = kSlots - kTurn, v = t - kTurn;
+                    constexpr int from = (v * kReads + kRoom - 1) / kRoom, to = ((v + 1) * kReads + kRoom - 1) / kRoom;
+                    each<to - from>([&](auto n) {
+                        constexpr int o = from + n;
+                        if constexpr (o < NB) read_w(0, o);
+                        else read_x(0, o - NB);
+                    });
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            xdst += dx;
+            wdst += dw;
+            dx = -dx;
+            dw = -dw;
+        }
 
-    // Scales, bias and activation.  The last products are read: the matrix unit's results need 18 clocks.
-    asm volatile("s_waitcnt vmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");
-    float xs[MB];
+        // Scales, bias and activation, while the first steps of the next tile are on their way.  The last products are read: the matrix
+        // unit's results need 18 clocks.
+        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+        float xs[MB];
 #pragma unroll
-    for (int i = 0; i < MB; ++i) xs[i] = token_scale[(wm * MB + i) * 16 + r];
-    typedef typename Piece<T>::type V;
-    constexpr int kV = Piece<T>::kCount;
-    auto finish = [&](auto inside) {      // inside: the tile lies whole within the output
-        each<NB / 2>([&](auto pair) {
-            constexpr int j = 2 * pair;
-            const int tile_n = wn * 16 * NB + j * 16 + q * 8, n = n0 + tile_n;
-            float cs[8], cb[8];
+        for (int i = 0; i < MB; ++i) xs[i] = token_scale[done][(wm * MB + i) * 16 + r];
+        typedef typename Piece<T>::type V;
+        constexpr int kV = Piece<T>::kCount;
+        auto finish = [&](auto inside) {      // inside: the tile lies whole within the output
+            each<NB / 2>([&](auto pair) {
+                constexpr int j = 2 * pair;
+                const int tile_n = wn * 16 * NB + j * 16 + q * 8, n = n0 + tile_n;
+                float cs[8], cb[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                cs[e] = channel_scale[tile_n + e];
-                cb[e] = channel_bias[tile_n + e];
-            }
-            each<MB>([&](auto block) {
-                constexpr int i = block;
-                const int m = m0 + (wm * MB + i) * 16 + r;
-                asm volatile("" : "+a"(acc[i][j]), "+a"(acc[i][j + 1]));
-                float v[8];
+                for (int e = 0; e < 8; ++e) {
+                    cs[e] = channel_scale[done][tile_n + e];
+                    cb[e] = channel_bias[done][tile_n + e];
+                }
+                each<MB>([&](auto block) {
+                    constexpr int i = block;
+                    const int m = m0 + (wm * MB + i) * 16 + r;
+                    asm volatile("" : "+a"(acc[i][j]), "+a"(acc[i][j + 1]));
+                    float v[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = fmaf((float)acc[i][j + e / 4][e % 4] * xs[i], cs[e], cb[e]);
-                if (a.relu)
+                    for (int e = 0; e < 8; ++e) v[e] = fmaf((float)acc[i][j + e / 4][e % 4] * xs[i], cs[e], cb[e]);
+                    acc[i][j] = acc[i][j + 1] = int4v{0, 0, 0, 0};
+                    if (a.relu)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = v[e] < 0.f ? 0.f : v[e];
-                V y[8 / kV];
+                        for (int e = 0; e < 8; ++e) v[e] = v[e] < 0.f ? 0.f : v[e];
+                    V y[8 / kV];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e / kV][e % kV] = (T)v[e];
-                T* out = static_cast<T*>(a.out) + (size_t)m * a.ldo + n;
-                if constexpr (inside) {
-#pragma unroll
-                    for (int c = 0; c < 8 / kV; ++c) reinterpret_cast<V*>(out)[c] = y[c];
-                } else if (m < a.M) {
-                    if (n + 8 <= a.N)
+                    for (int e = 0; e < 8; ++e) y[e / kV][e % kV] = (T)v[e];
+                    T* out = static_cast<T*>(a.out) + (size_t)m * a.ldo + n;
+                    if constexpr (inside) {
 #pragma unroll
                         for (int c = 0; c < 8 / kV; ++c) reinterpret_cast<V*>(out)[c] = y[c];
-                    else
+                    } else if (m < a.M) {
+                        if (n + 8 <= a.N)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (n + e < a.N) out[e] = y[e / kV][e % kV];
-                }
+                            for (int c = 0; c < 8 / kV; ++c) reinterpret_cast<V*>(out)[c] = y[c];
+                        else
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                if (n + e < a.N) out[e] = y[e / kV][e % kV];
+                    }
+                });
             });
-        });
-    };
-    if (m0 + TM <= a.M && n0 + TN <= a.N) finish(std::true_type{});
-    else finish(std::false_type{});
+        };
+        if (m0 + TM <= a.M && n0 + TN <= a.N) finish(std::true_type{});
+        else finish(std::false_type{});
+        if (!kWalks<MB, NB>) break;
+        m0 = next_m;
+        n0 = next_n;
+        done = set;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (loads of zeros that nothing reads)
 }
 
 template <class T, int MB, int NB, int WM, int WN>
@@ -405,7 +436,8 @@ int launch_tile_product(const Int8Args& a, hipStream_t s)
 {
     const long long tiles = ((a.M + 16ll * MB * WM - 1) / (16 * MB * WM)) * ((a.N + 16ll * NB * WN - 1) / (16 * NB * WN));
     if (tiles >= (1ll << 31)) return (int)hipErrorInvalidValue;
-    hipLaunchKernelGGL((tile_product_kernel<T, MB, NB, WM, WN>), dim3((unsigned)tiles), dim3(64 * WM * WN), 0, s, a, (unsigned)tiles);
+    const unsigned blocks = kWalks<MB, NB> && a.pitch >= 128 * kWalkSteps ? (unsigned)std::min(tiles, 256ll) : (unsigned)tiles;
+    hipLaunchKernelGGL((tile_product_kernel<T, MB, NB, WM, WN>), dim3(blocks), dim3(64 * WM * WN), 0, s, a, (unsigned)tiles, blocks);
     return (int)hipGetLastError();
 }
 
@@ -595,9 +627,9 @@ int launch_row_product(const Int8Args& a, hipStream_t s)
 
 long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
-// Microseconds that a product is estimated to take, fitted to launches of 20 sizes of M by 14 of K and N (1 to 8192 tokens, K 128 to
-// 16384, N 10 to 16384, weights that do not stay in a cache): over these the kernel of the least estimate takes 1.6 % more than
-// the fastest one, 23 % at most.
+// Microseconds that a product is estimated to take, fitted to launches of 20 sizes of M by 16 of K and N (1 to 8192 tokens, K 128 to
+// 16384, N 10 to 16384, weights that do not stay in a cache): over these the kernel of the least estimate takes 1.4 % more than
+// the fastest one, 26 % at most.
 // Row kernel: a launch and the sums of W wavefronts (0.14 a block of 256 sums), then the larger of what all workgroups load (18 TB/s),
 // what those of one CU load in turn (115 GB/s) and the weights from memory.
 double row_estimate(int MB, int NB, int W, int D, int M, int N, int pitch)
@@ -621,41 +653,31 @@ double tile_estimate(int MB, int M, int N, int pitch)
     return std::max(us, 3.0 + (double)N * pitch / (MB == 2 ? 3.9e6 : 3.2e6));
 }
 
+enum Kernel { kRow11, kRow21, kRow22, kRow24, kRow41, kRow42, kRow44, kTile2, kTile4, kTile8, kKernels };
+
+Kernel choose(int M, int N, int pitch)
+{
+    const double us[kKernels] = {row_estimate(1, 1, 8, 4, M, N, pitch), row_estimate(2, 1, 8, 2, M, N, pitch), row_estimate(2, 2, 4, 2, M, N, pitch),
+                                 row_estimate(2, 4, 4, 2, M, N, pitch), row_estimate(4, 1, 8, 1, M, N, pitch), row_estimate(4, 2, 4, 2, M, N, pitch),
+                                 row_estimate(4, 4, 4, 2, M, N, pitch), tile_estimate(2, M, N, pitch), tile_estimate(4, M, N, pitch), tile_estimate(8, M, N, pitch)};
+    return (Kernel)(std::min_element(us, us + kKernels) - us);
+}
+
 template <class T>
 int launch_product(const Int8Args& a, hipStream_t s)
 {
-    typedef int (*Launch)(const Int8Args&, hipStream_t);
-    Launch best = nullptr;
-    double least = 0.0;
-    auto consider = [&](double us, Launch launch) {
-        if (!best || us < least) {
-            best = launch;
-            least = us;
-        }
-    };
-    auto rows = [&](auto mb, auto nb, auto w, auto d) {
-        constexpr int MB = mb, NB = nb, W = w, D = d;
-        consider(row_estimate(MB, NB, W, D, a.M, a.N, a.pitch), launch_row_product<T, int8_t, MB, NB, W, D>);
-    };
-    auto tiles = [&](auto mb) {
-        constexpr int MB = mb;
-        consider(tile_estimate(MB, a.M, a.N, a.pitch), launch_tile_product<T, MB, MB, 2, 2>);
-    };
-    std::integral_constant<int, 1> one;
-    std::integral_constant<int, 2> two;
-    std::integral_constant<int, 4> four;
-    std::integral_constant<int, 8> eight;
-    rows(one, one, eight, four);
-    rows(two, one, eight, two);
-    rows(two, two, four, two);
-    rows(two, four, four, two);
-    rows(four, one, eight, one);
-    rows(four, two, four, two);
-    rows(four, four, four, two);
-    tiles(two);
-    tiles(four);
-    tiles(eight);
-    return best(a, s);
+    switch (choose(a.M, a.N, a.pitch)) {
+        case kRow11: return launch_row_product<T, int8_t, 1, 1, 8, 4>(a, s);
+        case kRow21: return launch_row_product<T, int8_t, 2, 1, 8, 2>(a, s);
+        case kRow22: return launch_row_product<T, int8_t, 2, 2, 4, 2>(a, s);
+        case kRow24: return launch_row_product<T, int8_t, 2, 4, 4, 2>(a, s);
+        case kRow41: return launch_row_product<T, int8_t, 4, 1, 8, 1>(a, s);
+        case kRow42: return launch_row_product<T, int8_t, 4, 2, 4, 2>(a, s);
+        case kRow44: return launch_row_product<T, int8_t, 4, 4, 4, 2>(a, s);
+        case kTile2: return launch_tile_product<T, 2, 2, 2, 2>(a, s);
+        case kTile4: return launch_tile_product<T, 4, 4, 2, 2>(a, s);
+        default: return launch_tile_product<T, 8, 8, 2, 2>(a, s);
+    }
 }
 
 template <class T, class X>
@@ -683,6 +705,8 @@ int launch_int8_quantize(int dtype, const void* x, int8_t* q, float* scale, int 
     if (dtype == kF16) return launch_quantize<_Float16>(x, q, scale, rows, K, ldx, s);
     return launch_quantize<__bf16>(x, q, scale, rows, K, ldx, s);
 }
+
+int int8_kernel(int M, int N, int K) { return choose(M, N, (K + 127) / 128 * 128); }
 
 // The quantised input, then its scales.
 long long int8_workspace(int M, int, int K, int in_dtype, int)

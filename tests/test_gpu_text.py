@@ -269,7 +269,11 @@ LAYERS = [  # M, K, N
     (1, 1, 1), (1, 64, 10), (1, 1000, 129), (1, 4096, 512), (2, 127, 33), (3, 128, 300), (4, 300, 2), (5, 2048, 65), (7, 129, 1000), (8, 640, 48),
     (13, 2900, 100), (16, 256, 256), (17, 512, 31), (24, 1024, 96), (32, 100, 640), (33, 2000, 129), (48, 384, 500), (64, 1024, 128), (65, 130, 257),
     (100, 777, 100), (127, 512, 384), (128, 896, 255), (200, 1100, 190), (256, 256, 256), (257, 640, 513), (300, 2300, 640), (513, 200, 1025),
-    (1000, 128, 8), (1025, 1030, 270), (2048, 64, 64)]
+    (1000, 128, 8), (1025, 1030, 270), (2048, 64, 64), (250, 300, 300), (600, 1500, 700), (3616, 272, 33), (300, 1500, 1500),
+    (601, 2000, 1003), (130, 100, 500), (603, 300, 5001)]
+
+
+LARGE_LAYERS = [(8100, 2000, 8150), (4300, 2900, 8333), (2048, 8192, 8192)]
 
 
 def _layer_reference(x, w, w_scale, bias, relu):
@@ -346,6 +350,30 @@ def test_layer_rows_that_hold_infinities_and_nan():
                     x[1] = 0.0
                     y = layer.forward(x)[1].float()
                     assert torch.equal(y, (layer.bias.clamp(min=0.0) if relu else layer.bias).to(dtype).float())
+
+
+def test_layer_of_large_tiles():
+    """Workgroups that walk over several tiles, ragged at both ends: rows of the first, of the last and of all between, every column."""
+    import torch
+    from paper_2011_06295_amd import text
+    for (M, K, N), dtype in zip(LARGE_LAYERS, ("bf16", "f32", "f16")):
+        gen = torch.Generator(device="cuda").manual_seed(M)
+        w = torch.randint(-128, 128, (N, K), generator=gen, device="cuda", dtype=torch.int8)
+        scale = torch.rand(N, generator=gen, device="cuda") * 0.01 + 1e-3
+        bias = torch.randn(N, generator=gen, device="cuda")
+        x = torch.randn((M, K), generator=gen, device="cuda").to(_types()[dtype])
+        print(f"layer {dtype} {M}x{K} -> {N}", flush=True)
+        layer = text.Int8Linear.from_quantized(w, scale, bias, relu=M == 4300)
+        y = layer.forward(x)
+        assert torch.equal(layer.forward(x), y)
+        rows = torch.cat([torch.arange(0, M, 97, device="cuda"), torch.arange(M - 5, M, device="cuda")])
+        q, xs = text.quantize(x[rows].contiguous())
+        product = (q[:, :K].double() @ w.double().t().contiguous()) * xs.double()[:, None] * scale.double()
+        ref, bound = product + bias.double(), 4 * 2.0 ** -24 * (product.abs() + bias.double().abs())
+        if M == 4300:
+            ref = ref.clamp(min=0.0)
+        err = (y[rows].double() - ref).abs()
+        assert bool((err <= bound + U[dtype] * (ref.abs() + bound) + TINY[dtype]).all()), float(err.max())
 
 
 def test_layer_shapes_and_empty_batches():

@@ -97,3 +97,14 @@ def test_convolution_layers_refuse_the_operators_types():
     w, m, h = np.ones((2, 3, 3, 3), np.float32), np.ones((2, 3, 3, 3), np.uint8), C.c_void_p()
     for dtype in (B.SC_BF16, B.SC_I8):
         assert LIB.sparse_conv_create(C.byref(h), w.ctypes.data, m.ctypes.data, 2, 3, 3, 3, dtype, 0) == B.SC_EINVAL
+
+
+def test_every_product_kernel_has_a_layer_in_the_tests():
+    from test_gpu_text import LARGE_LAYERS, LAYERS
+    choice = LIB["_ZN2sc11int8_kernelEiii"]        # sc::int8_kernel(M, N, K)
+    choice.argtypes = [C.c_int] * 3
+    reached = {}
+    for M, K, N in LAYERS + LARGE_LAYERS:
+        reached.setdefault(choice(M, N, K), []).append((M, K, N))
+    assert set(reached) == set(range(10)), reached
+    assert any(m * n > 256 for m, n in [(-(-M // 256), -(-N // 256)) for M, _, N in reached[9]])      # a workgroup takes several tiles
