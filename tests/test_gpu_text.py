@@ -111,7 +111,8 @@ def test_lookup_past_32_bits():
 GRADIENTS = [  # sentences, words, vocab, dim, kind of tokens
     (1, 1, 5, 1, "uniform"), (1, 1, 600, 2048, "uniform"), (1, 37, 100, 128, "mixed"), (2, 5, 11, 8, "outside"), (128, 64, 2000, 300, "skewed"),
     (3, 341, 501, 101, "mixed"), (1, 700, 3, 16, "same"), (4, 1024, 513, 40, "skewed"), (5, 1000, 100, 36, "same"), (9, 1111, 70000, 12, "skewed"),
-    (2, 4097, 1025, 24, "mixed"), (1, 20000, 300, 9, "skewed"), (1, 9000, 7, 130, "uniform"), (3, 3000, 40000, 5, "outside")]
+    (2, 4097, 1025, 24, "mixed"), (1, 20000, 300, 9, "skewed"), (1, 9000, 7, 130, "uniform"), (3, 3000, 40000, 5, "outside"),
+    (2, 200, 700, 1100, "skewed"), (1, 9000, 60, 1030, "mixed")]
 
 
 def _gradient_reference(g, tok, vocab, dim, scale, padding):
@@ -189,6 +190,49 @@ def test_gradient_against_differences():
                 table[v, d] = 1.0
                 step = float((c.double() * layer.forward(tokens, channels_first=first).double()).sum())
                 assert abs(step - float(grad[v, d])) <= 20 * 2.0 ** -24 * 1.5 * float(c.abs().sum())
+
+
+LARGE_TABLES = [  # tokens, vocab, dim, types: rows past what a workgroup marks, keys of three digits, past 27 bits, zeros in a launch of their own
+    (500, 9_000_001, 3, ("f32", "f32")), (20_000, 3_000_001, 2, ("bf16", "f32")), (700, 140_000_003, 1, ("f16", "f16")), (9000, 70_001, 130, ("f32", "f32")),
+    (3000, 70_001, 130, ("f32", "f32")), (40_000, 1500, 700, ("f16", "f32"))]
+
+
+@pytest.mark.parametrize("case", LARGE_TABLES)
+def test_gradient_of_large_tables(case):
+    import torch
+    from paper_2011_06295_amd import text
+    t, vocab, dim, types = case
+    gen = torch.Generator(device="cuda").manual_seed(t)
+    tokens = torch.randint(0, vocab, (t,), generator=gen, device="cuda")
+    tokens[: t // 4] = tokens[t // 4 : t // 4 + 30].repeat(t // 120 + 1)[: t // 4]      # some rows have many tokens
+    tokens[-1], tokens[-2] = vocab - 1, 0
+    grad = torch.randn((t, dim), generator=gen, device="cuda").to(_types()[types[0]])
+    out = text.Embedding(torch.empty((vocab, dim), dtype=_types()[types[1]], device="cuda")).backward(grad, tokens)
+    names, row = torch.unique(tokens, return_inverse=True)
+    ref, size, count = (torch.zeros((len(names), dim), dtype=torch.float64) for _ in range(3))
+    g, row = grad.double().cpu(), row.cpu()
+    ref.index_add_(0, row, g)
+    size.index_add_(0, row, g.abs())
+    count.index_add_(0, row, torch.ones_like(g))
+    bound = ((count + 1) * 2.0 ** -24 * size).numpy()
+    _within(out[names], ref.numpy(), bound + U[types[1]] * (np.abs(ref.numpy()) + bound) + TINY[types[1]], case)
+    out[names] = 0
+    assert int(torch.count_nonzero(out)) == 0
+
+
+def test_gradient_of_one_bucket_of_rows():
+    """All tokens in rows that lie 256 apart, so that one workgroup sorts them all: few, more than it compares pair by pair, as many as
+    it takes; over one column block and over more than it has wavefronts."""
+    import torch
+    from paper_2011_06295_amd import text
+    rng = np.random.default_rng(17)
+    for t, dim, spread in ((200, 8, 3), (257, 40, 60), (8192, 12, 2000), (8192, 600, 7), (2000, 8300, 40), (100, 9000, 1)):
+        vocab = 256 * spread + 5
+        tok = 3 + 256 * rng.integers(0, spread, t)
+        g = rng.standard_normal((t, dim)).astype(np.float32)
+        ref, bound = _gradient_reference(g.astype(np.float64), tok, vocab, dim, 1.0, -1)
+        out = text.Embedding(torch.full((vocab, dim), float("nan"), device="cuda")).backward(torch.from_numpy(g).cuda(), torch.from_numpy(tok).cuda())
+        _within(out, ref, bound + U["f32"] * (np.abs(ref) + bound) + TINY["f32"], (t, dim, spread))
 
 
 def test_gradient_of_no_tokens_is_zero():
