@@ -151,6 +151,10 @@ class Int8Linear:
         self._flags = B.SC_EPILOGUE_RELU if relu else 0
         self._workspaces = {}
 
+    def dequantized(self) -> torch.Tensor:
+        """The weights that the 8-bit integers stand for: fp32 [N][K]."""
+        return self.weight[:, :self.K].float() * self.scale[:, None]
+
     def _call(self, x, x_scale, in_dtype, M, ldx, lead, dtype, out):
         if out is None:
             out = x.new_empty((*lead, self.N), dtype=dtype)

@@ -503,3 +503,61 @@ def test_wrappers_refuse_what_they_cannot_run():
         layer.forward_quantized(torch.zeros((2, 8), dtype=torch.int8, device="cuda"), torch.ones(2, device="cuda"))
     with pytest.raises(ValueError):
         text.Int8Linear(torch.ones((3, 8), device="cuda"), bias=torch.ones(4, device="cuda"))
+
+
+# ---------------------------------------------------------------- the model that runs them together
+
+def _model_in_64_bits(model, filters, tokens):
+    """(features, their gradient towards the vectors as a function) of the model in double on the CPU."""
+    import torch
+    table = model.words.table.double().cpu()
+    x = table[tokens.cpu()].permute(0, 2, 1)[:, :, None].contiguous().requires_grad_(True)
+    features = []
+    for weights, mask, bias in filters:
+        y = torch.nn.functional.conv2d(x, torch.from_numpy(weights * mask).double(), torch.from_numpy(bias).double())
+        features.append(torch.relu(y).squeeze(2).amax(2))
+    return x, torch.cat(features, 1)
+
+
+def test_model_against_64_bits():
+    """Logits: fp32 features (bounded by 1e-5 of their largest, the convolutions' own tolerance), each then at most half a step of
+    its row's scale off, through weights that the integers stand for.  Gradient: the same path backwards, 1e-5 of the largest."""
+    import torch
+    from paper_2011_06295_amd import text_model
+    rng = np.random.default_rng(31)
+    gen = torch.Generator(device="cuda").manual_seed(31)
+    vocab, dim, classes, n, t = 500, 40, 5, 9, 21
+    filters = [((rng.standard_normal((12, dim, 1, s)) * 0.3).astype(np.float32), (rng.random((12, dim, 1, s)) < 0.3).astype(np.uint8),
+                (rng.standard_normal(12) * 0.1).astype(np.float32)) for s in (2, 3)]
+    table = torch.randn((vocab, dim), generator=gen, device="cuda")
+    model = text_model.TextModel(table, filters, torch.randn((classes, 24), generator=gen, device="cuda"), torch.randn(classes, generator=gen, device="cuda"))
+    tokens, _ = text_model.sentences(n, t, vocab, classes)
+    x, features = _model_in_64_bits(model, filters, tokens)
+    weights = model.classifier.dequantized().double().cpu()
+    logits = model.forward(tokens)
+    ref = features @ weights.t() + model.classifier.bias.double().cpu()
+    step = features.abs().amax(1, keepdim=True) / 127.0
+    bound = (0.5 * step * 1.001 + 1e-5 * features.abs().max()) * weights.abs().sum(1) + 1e-5 * ref.abs().max()
+    assert bool(((logits.double().cpu() - ref).abs() <= bound).all())
+    g = torch.randn((n, classes), generator=gen, device="cuda")
+    (features @ weights.t() * g.double().cpu()).sum().backward()
+    want = torch.zeros((vocab, dim), dtype=torch.float64).index_add_(0, tokens.cpu().reshape(-1), x.grad[:, :, 0].permute(0, 2, 1).reshape(-1, dim))
+    want[0] = 0.0
+    got = model.table_gradient(g).double().cpu()
+    assert float((got - want).abs().max()) <= 1e-5 * float(want.abs().max())
+    model.close()
+
+
+def test_model_learns_and_touches_only_its_words():
+    import torch
+    from paper_2011_06295_amd import text_model
+    model = text_model.TextModel.synthetic(vocab=3000)
+    tokens, labels = text_model.sentences(32, 64, 3000)
+    before = model.words.table.clone()
+    losses = [float(model.train_step(tokens, labels, rate=20.0)) for _ in range(12)]
+    assert losses[-1] < 0.5 * losses[0], losses
+    named = torch.zeros(3000, dtype=torch.bool, device="cuda")
+    named[tokens.reshape(-1)] = True
+    named[0] = False
+    assert torch.equal(before[~named], model.words.table[~named]) and not torch.equal(before[named], model.words.table[named])
+    model.close()
