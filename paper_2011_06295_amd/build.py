@@ -9,6 +9,7 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsparseconv.so")
+TORCH_LIB = os.path.join(HERE, "_text_torch.so")
 SOURCES = ["kernels.hip", "matrix_f32.hip", "matrix_f16.hip", "probes.hip", "api.cpp", "plan.cpp", "matrix_plan.cpp", "host_csr.cpp",
            "embed.hip", "int8.hip", "text_api.cpp"]
 
@@ -26,7 +27,8 @@ def build(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     with tempfile.TemporaryDirectory() as objects:
         cmds = [[hipcc] + HIPCC_FLAGS + ["-c", "-o", os.path.join(objects, s + ".o"), os.path.join(CSRC, s)] for s in SOURCES]
-        link = [hipcc] + HIPCC_FLAGS + ["-shared", "-o", LIB] + [c[-2] for c in cmds]
+        cmds.append(torch_command())
+        link = [hipcc] + HIPCC_FLAGS + ["-shared", "-o", LIB] + [c[-2] for c in cmds[:len(SOURCES)]]
         running = [(c, subprocess.Popen(c, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)) for c in cmds]
         done = [(c, p.communicate()[0], p.returncode) for c, p in running]
         if all(rc == 0 for _, _, rc in done):
@@ -41,6 +43,17 @@ def build(verbose: bool = False) -> str:
         if verbose and out.strip():
             print(out)
     return LIB
+
+
+def torch_command() -> list:
+    """The compiler's call for the Python side of the text model's operators (checks and allocation on PyTorch tensors, host code)."""
+    import sysconfig
+    import torch
+    from torch.utils import cpp_extension
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    return ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+            f"-I{sysconfig.get_paths()['include']}", *[f"-I{p}" for p in cpp_extension.include_paths()],
+            "-o", TORCH_LIB, os.path.join(CSRC, "text_torch.cpp"), f"-L{lib}", f"-Wl,-rpath,{lib}", "-ltorch_python", "-ltorch_cpu", "-lc10"]
 
 
 def build_sanitize(verbose: bool = False) -> str:

@@ -924,7 +924,15 @@ __global__ __launch_bounds__(kRunThreads) void runs_kernel(EmbedGradArgs a, cons
     }
 }
 
-// Before a launch of few tokens: what has to be turned and, where that is much, set to zero.
+// Before a launch of few tokens: what has to be turned and, where that is much, set to zero.  Tiles alone by workgroups of one: 640 of
+// them spread over the CUs better than 160 of four (6.0 us instead of 7.1).
+template <class G>
+__global__ __launch_bounds__(kThreads) void turn_kernel(TurnArgs turn)
+{
+    __shared__ __attribute__((aligned(16))) char room[tiles_room<G>() / kTiles];
+    turn_tiles<G>(turn, blockIdx.x, reinterpret_cast<G*>(room));
+}
+
 template <class G, class W>
 __global__ __launch_bounds__(kSortThreads) void turn_or_fill_kernel(TurnArgs turn, Fill fill)
 {
@@ -975,7 +983,8 @@ int launch_grad(const EmbedGradArgs& a, const Parts& parts, char* workspace, hip
         const Fill fill{a.table_grad, zeros ? 0 : elements};
         const unsigned long long blocks = blocks_of<W>(turn.tiles, fill);
         if (blocks >= (1ull << 31)) return (int)hipErrorInvalidValue;
-        if (blocks) hipLaunchKernelGGL((turn_or_fill_kernel<G, W>), dim3((unsigned)blocks), dim3(kSortThreads), 0, s, turn, fill);
+        if (fill.count) hipLaunchKernelGGL((turn_or_fill_kernel<G, W>), dim3((unsigned)blocks), dim3(kSortThreads), 0, s, turn, fill);
+        else if (tiles) hipLaunchKernelGGL(turn_kernel<G>, dim3((unsigned)tiles), dim3(kThreads), 0, s, turn);
         const SortPlan plan = sort_plan((a.vocab - 1) >> kBucketBits, kBucketDigit, tokens);
         const unsigned groups = (unsigned)std::min<long long>(a.vocab, kBuckets);
         const unsigned shares = (unsigned)std::min<long long>(column_blocks, kBuckets / groups);      // of the column blocks: a workgroup a CU

@@ -108,3 +108,29 @@ def test_every_product_kernel_has_a_layer_in_the_tests():
         reached.setdefault(choice(M, N, K), []).append((M, K, N))
     assert set(reached) == set(range(10)), reached
     assert any(m * n > 256 for m, n in [(-(-M // 256), -(-N // 256)) for M, _, N in reached[9]])      # a workgroup takes several tiles
+
+
+def test_tensor_calls_refuse_before_they_touch_anything():
+    """The compiled side of text.py, given what is no CUDA tensor, no tensor, too few arguments."""
+    import torch
+    from paper_2011_06295_amd import text
+    calls = text._calls
+    table, tokens = torch.zeros(4, 3), torch.zeros(2, dtype=torch.int64)
+    for args in [(table, tokens, None, False, 1.0, 0), (3, tokens, None, False, 1.0, 0), (table, None, None, False, 1.0, 0), (table, tokens, None, False, 1, 0), (table,), ()]:
+        with pytest.raises(ValueError):
+            calls.embed(*args)
+    for args in [(table, table, tokens, None, False, False, 1.0, -1, 0), (table, None, tokens, None, False, False, 1.0, -1, 0), (table,)]:
+        with pytest.raises(ValueError):
+            calls.embed_backward(*args)
+    weight, scale = torch.zeros((2, 128), dtype=torch.int8), torch.zeros(2)
+    for args in [(torch.zeros(2, 5), None, weight, scale, None, 4, False, None, None, 0), (torch.zeros((1, 4), dtype=torch.int32), None, weight, scale, None, 4, False, None, None, 0),
+                 (torch.zeros(2, 4), None, weight, scale, None, 4, False, torch.zeros(2, 3), None, 0), (torch.zeros(2, 4), None, weight, scale, None, 4, False, None, "f32", 0),
+                 (torch.zeros(2, 4), scale, weight, scale, None, 4, False, None, None, 0), (5, None, weight, scale, None, 4, False, None, None, 0), ()]:
+        with pytest.raises(ValueError):
+            calls.linear(*args)
+    with pytest.raises(ValueError):
+        text.Embedding(table)
+    with pytest.raises(ValueError):
+        text.Int8Linear(table)
+    with pytest.raises(TypeError):
+        calls.bind(1, 2)
