@@ -193,6 +193,15 @@ __device__ __forceinline__ void multiply(int4v& c, int4v a, int4v b)
     asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
 }
 
+// An output from its sum, alike in every kernel: rounded to 32 bits before anything else (the compiler would fuse the last addition
+// into a conversion to float16, which then rounds once, and not everywhere: a token's outputs would depend on the kernel).
+__device__ __forceinline__ float output_of(int sum, float x_scale, float w_scale, float bias, int relu)
+{
+    float v = fmaf((float)sum * x_scale, w_scale, bias);
+    asm("" : "+v"(v));
+    return relu && v < 0.f ? 0.f : v;
+}
+
 // The tile that a workgroup takes: workgroups go round the eight XCDs, so each gets a run of tiles of its own, in which eight by eight
 // tiles that share rows of x and of w are at work together.
 __device__ __forceinline__ void tile_of(unsigned block, unsigned tiles, int down, int across, int& tm, int& tn)
@@ -213,8 +222,9 @@ constexpr bool kWalks = MB * NB >= 64;
 constexpr int kWalkSteps = 3;
 
 // A tile of 16 MB WM rows of x by 16 NB WN rows of w, 128 bytes of each a step; WM x WN wavefronts with MB x NB blocks of 16 x 16 sums.
-template <class T, int MB, int NB, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_product_kernel(Int8Args a, unsigned tiles, unsigned stride)
+// S steps are in LDS or on their way there.
+template <class T, int MB, int NB, int WM, int WN, int S>
+__global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 || S > 2 ? 1 : 2) void tile_product_kernel(Int8Args a, unsigned tiles, unsigned stride)
 {
     const int8_t* x = static_cast<const int8_t*>(a.x);
     const float* x_scale = a.x_scale;
@@ -223,7 +233,7 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_prod
     constexpr int kX = TM * 128, kW = TN * 128, kHalf = MB / 2;
     static_assert(MB % 2 == 0 && NB % 2 == 0, "blocks come in pairs");
     static_assert(TM % 64 == 0 && TN % 64 == 0 && TM <= 64 * W && TN <= 64 * W, "a scale a thread");
-    __shared__ __attribute__((aligned(256))) char lds[2 * kX + 2 * kW];
+    __shared__ __attribute__((aligned(256))) char lds[S * (kX + kW)];
     constexpr int kSets = kWalks<MB, NB> ? 2 : 1;      // the tile that is finished, and the next one
     __shared__ __attribute__((aligned(16))) float channel_scale[kSets][TN], channel_bias[kSets][TN], token_scale[kSets][TM];
 
@@ -240,7 +250,7 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_prod
     }
     const unsigned lds0 = (unsigned)(uintptr_t)(SC_LDS char*)lds;
     int4v from_x, from_w;
-    unsigned xdst = lds0, wdst = lds0 + 2 * kX, tile = blockIdx.x;
+    unsigned xdst = lds0, wdst = lds0 + S * kX, tile = blockIdx.x;
     int next_m = 0, next_n = 0, step = 0, set = 0;      // what is loaded: a step of a tile, whose scales go to `set`
     auto enter = [&]() {
         int tm, tn;
@@ -274,16 +284,16 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_prod
         else load_to_lds(from_w, offset[i], step * 128, wdst + (wave * kLoadsW + i - kLoadsX) * 1024);
     };
     enter();
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) load(i);
     int m0 = next_m, n0 = next_n, done = set;
-    advance();
-    xdst += kX;
-    wdst += kW;
+    each<S>([&](auto stage) {
+        if constexpr (stage > 0) advance();
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) load(i);
-    xdst -= kX;
-    wdst -= kW;
+        for (int i = 0; i < kLoads; ++i) load(i);
+        xdst += kX;
+        wdst += kW;
+    });
+    xdst -= S * kX;
+    wdst -= S * kW;
 
     int4v acc[MB][NB];
 #pragma unroll
@@ -299,11 +309,11 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_prod
     // two blocks are eight channels in a row.
     const int wm = wave % WM, wn = wave / WM, r = lane & 15, q = lane >> 4;
     int xa0 = (wm * 16 * MB + r) * 128 + ((q ^ (r >> 1)) << 4), xa1 = xa0 ^ 64;
-    int wa0 = 2 * kX + (wn * 16 * NB + (r >> 2) * 8 + (r & 3)) * 128 + ((q ^ (r >> 1)) << 4), wa1 = wa0 ^ 64;
+    int wa0 = S * kX + (wn * 16 * NB + (r >> 2) * 8 + (r & 3)) * 128 + ((q ^ (r >> 1)) << 4), wa1 = wa0 ^ 64;
     int4v wf[2][NB], xf[2][MB];
     auto read_w = [&](int h, int j) { wf[h][j] = *reinterpret_cast<const int4v*>(lds + (h ? wa1 : wa0) + ((j >> 1) * 32 + (j & 1) * 4) * 128); };
     auto read_x = [&](int h, int i) { xf[h][i] = *reinterpret_cast<const int4v*>(lds + (h ? xa1 : xa0) + i * 2048); };
-    asm volatile("s_waitcnt vmcnt(%0)" :: "n"(kLoads) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0)" :: "n"((S - 1) * kLoads) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 #pragma unroll
@@ -314,12 +324,14 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_prod
 
     // A step is two halves of MB x NB products, 64 bytes each.  In the first, all that the second needs is read, one read every few
     // products (a wavefront is alone on its SIMD and issues in order: reads or loads in a row leave the matrix unit without work).
-    // Then nothing reads this buffer any more and, spread over the second half, it is loaded with the bytes of the step after the next.
-    // Halfway through, those of the next step (loaded in the step before) are waited for, and the first half's operands are read.
-    int dx = kX, dw = kW;
+    // Then nothing reads this buffer any more and, spread over the second half, it is loaded with the bytes of the step that is S on.
+    // Halfway through, those of the next step (loaded S - 1 steps before) are waited for, and the first half's operands are read.
+    int buffer = 0;
     for (unsigned current = blockIdx.x; current < tiles; current += stride) {
         for (int k = 0; k < steps; ++k) {
             advance();
+            const int dx = buffer == S - 1 ? (1 - S) * kX : kX, dw = buffer == S - 1 ? (1 - S) * kW : kW;      // to the next step's buffer
+            buffer = buffer == S - 1 ? 0 : buffer + 1;
             constexpr int kSlots = MB * NB, kTurn = kSlots / 2;
             each<kSlots>([&](auto slot) {
                 constexpr int t = slot, i = t / NB, j = t % NB, kOps = kHalf + NB + MB;
@@ -344,7 +356,7 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_prod
                 constexpr int t = slot, i = t / NB, j = t % NB;
                 if constexpr (t == kTurn) {
                     constexpr int kIssued = (kTurn * kLoads + kSlots - 1) / kSlots;
-                    asm volatile("s_waitcnt vmcnt(%0)" :: "n"(kIssued) : "memory");
+                    asm volatile("s_waitcnt vmcnt(%0)" :: "n"(kIssued + (S - 2) * kLoads) : "memory");
                     __builtin_amdgcn_s_barrier();
                     asm volatile("" ::: "memory");
                     xa0 += dx;
@@ -369,8 +381,6 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_prod
             });
             xdst += dx;
             wdst += dw;
-            dx = -dx;
-            dw = -dw;
         }
 
         // Scales, bias and activation, while the first steps of the next tile are on their way.  The last products are read: the matrix
@@ -397,11 +407,8 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_prod
                     asm volatile("" : "+a"(acc[i][j]), "+a"(acc[i][j + 1]));
                     float v[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = fmaf((float)acc[i][j + e / 4][e % 4] * xs[i], cs[e], cb[e]);
+                    for (int e = 0; e < 8; ++e) v[e] = output_of(acc[i][j + e / 4][e % 4], xs[i], cs[e], cb[e], a.relu);
                     acc[i][j] = acc[i][j + 1] = int4v{0, 0, 0, 0};
-                    if (a.relu)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] = v[e] < 0.f ? 0.f : v[e];
                     V y[8 / kV];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) y[e / kV][e % kV] = (T)v[e];
@@ -431,13 +438,13 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 ? 1 : 2) void tile_prod
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (loads of zeros that nothing reads)
 }
 
-template <class T, int MB, int NB, int WM, int WN>
+template <class T, int MB, int NB, int WM, int WN, int S>
 int launch_tile_product(const Int8Args& a, hipStream_t s)
 {
     const long long tiles = ((a.M + 16ll * MB * WM - 1) / (16 * MB * WM)) * ((a.N + 16ll * NB * WN - 1) / (16 * NB * WN));
     if (tiles >= (1ll << 31)) return (int)hipErrorInvalidValue;
     const unsigned blocks = kWalks<MB, NB> && a.pitch >= 128 * kWalkSteps ? (unsigned)std::min(tiles, 256ll) : (unsigned)tiles;
-    hipLaunchKernelGGL((tile_product_kernel<T, MB, NB, WM, WN>), dim3(blocks), dim3(64 * WM * WN), 0, s, a, (unsigned)tiles, blocks);
+    hipLaunchKernelGGL((tile_product_kernel<T, MB, NB, WM, WN, S>), dim3(blocks), dim3(64 * WM * WN), 0, s, a, (unsigned)tiles, blocks);
     return (int)hipGetLastError();
 }
 
@@ -601,9 +608,7 @@ __global__ __launch_bounds__(64 * W) void row_product_kernel(Int8Args a)
         four y;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            float v = fmaf((float)sum[e] * token_scale[token], channel_scale[channel + e], channel_bias[channel + e]);
-            if (a.relu && v < 0.f) v = 0.f;
-            y[e] = (T)v;
+            y[e] = (T)output_of(sum[e], token_scale[token], channel_scale[channel + e], channel_bias[channel + e], a.relu);
         }
         T* out = static_cast<T*>(a.out) + m * a.ldo + n;
         if (n + 4 <= a.N) *reinterpret_cast<four*>(out) = y;
@@ -625,42 +630,65 @@ int launch_row_product(const Int8Args& a, hipStream_t s)
 
 // ---------------------------------------------------------------- which kernel
 
+// Microseconds that a product is estimated to take.  The constants are fitted to launches of 20 sizes of M by 16 of K and N (1 to
+// 8192 tokens, K 128 to 16384, N 10 to 16384, weights that do not stay in a cache), each to what is near the fastest there: over
+// these the kernel of the least estimate takes 1.3 % more than the fastest one, 16 % at most.  Depth pays where a CU has a tile or two
+// (64 x 64 at 256 x 4096 -> 4096: 14.5 us by two steps, 10.0 by four), two steps where workgroups that share a CU hide each other's waits
+// (128 x 128 at 2048 x 4096 -> 4096: 32.7 by two, 35.2 by three).
+
 long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
-// Microseconds that a product is estimated to take, fitted to launches of 20 sizes of M by 16 of K and N (1 to 8192 tokens, K 128 to
-// 16384, N 10 to 16384, weights that do not stay in a cache): over these the kernel of the least estimate takes 1.4 % more than
-// the fastest one, 26 % at most.
-// Row kernel: a launch and the sums of W wavefronts (0.14 a block of 256 sums), then the larger of what all workgroups load (18 TB/s),
-// what those of one CU load in turn (115 GB/s) and the weights from memory.
-double row_estimate(int MB, int NB, int W, int D, int M, int N, int pitch)
+enum Kernel { kRow11, kRow21, kRow22, kRow41, kRow42, kTile22, kTile44, kTile88, kDeep22, kDeep42, kDeep44, kKernels };
+
+// Row kernel: a launch, the sums of the wavefronts and the further rounds of workgroups, then the largest of what all workgroups load,
+// what those of one CU load in turn, and the weights.
+struct RowRule {
+    int MB, NB, resident;            // blocks; workgroups that the chip holds at a time
+    double join, round;              // us
+    double all, one, weights;        // MB/us of all, KB/us of one, MB/us of the weights
+};
+constexpr RowRule kRowRules[] = {{1, 1, 256, 0.24, 1.34, 14.8, 137.0, 6.8}, {2, 1, 256, 0.17, 1.42, 20.3, 134.0, 5.9}, {2, 2, 512, 0.08, 2.23, 15.0, 139.0, 5.4},
+                                 {4, 1, 256, 0.32, 1.50, 24.3, 136.0, 4.7}, {4, 2, 256, 0.88, 1.58, 19.1, 134.0, 5.1}};
+
+double row_estimate(const RowRule& r, int M, int N, int pitch)
 {
-    const double groups = (double)(ceil_div(M, 16 * MB) * ceil_div(N, 16 * NB)), bytes = 16.0 * (MB + NB) * pitch;
-    const double resident = W * D * 2048 * (MB + NB) <= 78 * 1024 ? 512.0 : 256.0, rounds = std::ceil(groups / resident);
-    const double all = groups * bytes / 18e6, one = rounds * bytes / 115e3, weights = (double)N * pitch / (NB == 4 ? 6.3e6 : 4.9e6);
-    return 3.0 + 0.14 * MB * NB * rounds + 1.3 * (rounds - 1.0) + std::max(all, std::max(one, weights));
+    const double groups = (double)(ceil_div(M, 16 * r.MB) * ceil_div(N, 16 * r.NB)), bytes = 16.0 * (r.MB + r.NB) * pitch;
+    const double rounds = std::ceil(groups / r.resident);
+    const double load = std::max({groups * bytes / (r.all * 1e6), rounds * bytes / (r.one * 1e3), (double)N * pitch / (r.weights * 1e6)});
+    return 3.0 + r.join * rounds + r.round * (rounds - 1.0) + load;
 }
 
-// Tile kernel: steps of `least` microseconds while a workgroup has the CU to itself, `each` times the workgroups that share it beyond.
-double tile_estimate(int MB, int M, int N, int pitch)
-{
-    const double least = MB == 8 ? 1.1 : MB == 4 ? 0.43 : 0.33, each = MB == 8 ? 1.38 : MB == 4 ? 0.49 : 0.185;
-    const double share = MB == 8 ? 1.0 : MB == 4 ? 2.0 : 4.0;        // workgroups that a CU holds
-    const double start = MB == 8 ? 1.0 : MB == 4 ? 1.8 : 2.0, finish = MB == 8 ? 5.5 : MB == 4 ? 1.7 : 0.9;
-    const double groups = (double)(ceil_div(M, 32 * MB) * ceil_div(N, 32 * MB)), steps = pitch / 128.0;
-    const double rounds = std::floor(groups / (256.0 * share)), rest = groups - rounds * 256.0 * share;
-    double us = start + rounds * (steps * each * share + finish);
-    if (rest > 0.0) us += steps * std::max(least, each * std::ceil(rest / 256.0)) + finish;
-    return std::max(us, 3.0 + (double)N * pitch / (MB == 2 ? 3.9e6 : 3.2e6));
-}
+// Tile kernel: steps of `least` us while a workgroup has the CU to itself, `each` times the workgroups that share it beyond; the weights
+// from memory at least.
+struct TileRule {
+    int MB, NB, share;               // blocks of a wavefront; workgroups that a CU holds
+    double least, each, start, finish;
+    double weights;                  // MB/us
+};
+constexpr TileRule kTileRules[] = {{2, 2, 4, 0.261, 0.211, 0.2, 2.4, 3.5}, {4, 4, 2, 0.189, 0.448, 0.2, 3.9, 3.3}, {8, 8, 1, 0.94, 1.152, 1.4, 8.9, 2.2},
+                                   {2, 2, 2, 0.142, 0.192, 1.1, 1.9, 7.1}, {4, 2, 1, 0.0, 0.266, 1.1, 2.4, 6.6}, {4, 4, 1, 0.0, 0.397, 0.9, 3.2, 4.8}};
 
-enum Kernel { kRow11, kRow21, kRow22, kRow24, kRow41, kRow42, kRow44, kTile2, kTile4, kTile8, kKernels };
+double tile_estimate(const TileRule& r, int M, int N, int pitch)
+{
+    const double groups = (double)(ceil_div(M, 32 * r.MB) * ceil_div(N, 32 * r.NB)), steps = pitch / 128.0, held = 256.0 * r.share;
+    const double rounds = std::floor(groups / held), rest = groups - rounds * held;
+    double us = r.start + rounds * (steps * r.each * r.share + r.finish);
+    if (rest > 0.0) us += steps * std::max(r.least, r.each * std::ceil(rest / 256.0)) + r.finish;
+    return std::max(us, 3.0 + (double)N * pitch / (r.weights * 1e6));
+}
 
 Kernel choose(int M, int N, int pitch)
 {
-    const double us[kKernels] = {row_estimate(1, 1, 8, 4, M, N, pitch), row_estimate(2, 1, 8, 2, M, N, pitch), row_estimate(2, 2, 4, 2, M, N, pitch),
-                                 row_estimate(2, 4, 4, 2, M, N, pitch), row_estimate(4, 1, 8, 1, M, N, pitch), row_estimate(4, 2, 4, 2, M, N, pitch),
-                                 row_estimate(4, 4, 4, 2, M, N, pitch), tile_estimate(2, M, N, pitch), tile_estimate(4, M, N, pitch), tile_estimate(8, M, N, pitch)};
-    return (Kernel)(std::min_element(us, us + kKernels) - us);
+    int best = 0;
+    double least = 0.0;
+    for (int k = 0; k < kKernels; ++k) {
+        const double us = k < kTile22 ? row_estimate(kRowRules[k], M, N, pitch) : tile_estimate(kTileRules[k - kTile22], M, N, pitch);
+        if (k == 0 || us < least) {
+            best = k;
+            least = us;
+        }
+    }
+    return (Kernel)best;
 }
 
 template <class T>
@@ -670,13 +698,14 @@ int launch_product(const Int8Args& a, hipStream_t s)
         case kRow11: return launch_row_product<T, int8_t, 1, 1, 8, 4>(a, s);
         case kRow21: return launch_row_product<T, int8_t, 2, 1, 8, 2>(a, s);
         case kRow22: return launch_row_product<T, int8_t, 2, 2, 4, 2>(a, s);
-        case kRow24: return launch_row_product<T, int8_t, 2, 4, 4, 2>(a, s);
         case kRow41: return launch_row_product<T, int8_t, 4, 1, 8, 1>(a, s);
         case kRow42: return launch_row_product<T, int8_t, 4, 2, 4, 2>(a, s);
-        case kRow44: return launch_row_product<T, int8_t, 4, 4, 4, 2>(a, s);
-        case kTile2: return launch_tile_product<T, 2, 2, 2, 2>(a, s);
-        case kTile4: return launch_tile_product<T, 4, 4, 2, 2>(a, s);
-        default: return launch_tile_product<T, 8, 8, 2, 2>(a, s);
+        case kTile22: return launch_tile_product<T, 2, 2, 2, 2, 2>(a, s);
+        case kTile44: return launch_tile_product<T, 4, 4, 2, 2, 2>(a, s);
+        case kTile88: return launch_tile_product<T, 8, 8, 2, 2, 2>(a, s);
+        case kDeep22: return launch_tile_product<T, 2, 2, 2, 2, 4>(a, s);
+        case kDeep42: return launch_tile_product<T, 4, 2, 2, 2, 4>(a, s);
+        default: return launch_tile_product<T, 4, 4, 2, 2, 3>(a, s);
     }
 }
 
