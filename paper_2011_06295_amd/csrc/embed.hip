@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "text_ops.h"
 
@@ -190,24 +191,33 @@ int launch_lookup(const EmbedArgs& a, hipStream_t s)
 // ---------------------------------------------------------------- gradient: rows of the table
 
 // A wavefront sums 512 columns of rows of grad, lane l columns 4 l .. + 3 and 256 + 4 l .. + 3 of them.  A lane whose four are not all
-// there reads the last four of the row (its loads need no branch then) and stores those that are its own.
+// there takes the last four of the block instead: loads and stores need no branch for it, and it writes the same values as its
+// neighbours.  Rows of less than four columns: a column a lane.
 constexpr int kColumns = 512;
 
 struct Columns {
-    int offset[2], count[2];      // where the lane reads; how many columns are its own, the last ones of those it reads
+    int offset[2];                // where the lane reads and writes
+    bool own[2];                  // some of these columns are its own
     bool both, narrow;            // the second 256 are there; rows of less than four columns
 };
 
 __device__ __forceinline__ Columns columns_of(int block, int lane, int dim)
 {
     Columns c;
-    c.both = dim - block * kColumns > 256;
+    int begin = block * kColumns, end = min(begin + kColumns, dim);
     c.narrow = dim < 4;
+    if (end < dim && dim - end < 4) end = dim - 4;            // (a last block of less than four columns takes some of the one before)
+    if (block > 0 && dim - begin < 4) begin = dim - 4;
+    c.both = end - begin > 256;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-        const int first = block * kColumns + s * 256 + lane * 4;
-        c.count[s] = min(max(dim - first, 0), 4);
-        c.offset[s] = c.narrow ? 0 : min(first, dim - 4);
+        const int first = begin + s * 256 + lane * 4;
+        c.own[s] = first < end;
+        c.offset[s] = min(first, end - 4);
+    }
+    if (c.narrow) {
+        c.own[0] = lane < dim;
+        c.offset[0] = min(lane, dim - 1);
     }
     return c;
 }
@@ -235,7 +245,8 @@ __device__ __forceinline__ Row<G> load_row(const G* row, const Columns& c)
     typedef typename Piece<G, 4>::type V;
     Row<G> r;
     if (c.narrow) {
-        r.v[0] = load_some<G, 4>(row, c.count[0]);
+        r.v[0] = V{};
+        r.v[0][0] = row[c.offset[0]];
     } else {
         r.v[0] = *reinterpret_cast<const V*>(row + c.offset[0]);
         if (c.both) r.v[1] = *reinterpret_cast<const V*>(row + c.offset[1]);
@@ -265,15 +276,9 @@ __device__ __forceinline__ void store_row(W* row, const Sums& sums, const Column
         V v;
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = (W)(accumulate ? (float)held.v[s][e] + sums.v[s][e] * scale : sums.v[s][e] * scale);
-        W* out = row + c.offset[s];
-        if (c.count[s] == 4) {
-            *reinterpret_cast<V*>(out) = v;
-        } else if (c.count[s] > 0) {
-            const int skip = c.narrow ? 0 : 4 - c.count[s];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (e >= skip && e < skip + c.count[s]) out[e] = v[e];
-        }
+        if (!c.own[s]) continue;
+        if (s == 0 && c.narrow) row[c.offset[0]] = v[0];
+        else *reinterpret_cast<V*>(row + c.offset[s]) = v;
     }
 }
 
@@ -377,11 +382,11 @@ __device__ __forceinline__ void leave(const Sums& sums, float (*part)[kColumns])
         for (int e = 0; e < 4; ++e) part[wave][s * 256 + lane * 4 + e] = sums.v[s][e];
 }
 
-// The sum of what `count` wavefronts in a row left, `first` the first of them, in their order.
+// Adds what `count` wavefronts in a row left, `first` the first of them, in their order.
 __device__ __forceinline__ void join(Sums& sums, float (*part)[kColumns], int first, int count)
 {
     const int lane = threadIdx.x & 63;
-    clear(sums);
+#pragma unroll 4
     for (int w = first; w < first + count; ++w)
 #pragma unroll
         for (int s = 0; s < 2; ++s)
@@ -508,11 +513,12 @@ struct TokenArgs {
     bool wide;
 };
 
-__device__ __forceinline__ unsigned sort_key(const TokenArgs& a, unsigned t)
+__device__ __forceinline__ unsigned key_of(const TokenArgs& a, long long token)
 {
-    const long long v = token_at(a.tokens, a.wide, t);
-    return v >= 0 && v < a.vocab && v != a.padding ? (unsigned)v : (unsigned)a.vocab;
+    return token >= 0 && token < a.vocab && token != a.padding ? (unsigned)token : (unsigned)a.vocab;
 }
+
+__device__ __forceinline__ unsigned sort_key(const TokenArgs& a, unsigned t) { return key_of(a, token_at(a.tokens, a.wide, t)); }
 
 // The tokens of a workgroup: `each` runs of 64 a wavefront, in order.
 __device__ __forceinline__ unsigned own_token(int each, int i) { return ((threadIdx.x >> 6) * each + i) * 64 + (threadIdx.x & 63); }
@@ -579,13 +585,17 @@ struct Sorted {
 // ---------------------------------------------------------------- gradient of few tokens: one launch
 
 // Workgroup (b, y) owns the rows of the table whose number ends in b (kBuckets of them: frequent tokens are often neighbours), and
-// column blocks y, y + shares, ...  It looks through all tokens, keeps those of its rows in their order, sets the rows without any to zero (`zeros`;
-// beyond kOwnZeros bytes a launch before this one does that for all, at a higher rate) and sorts what it kept by the row; each wavefront then takes slots of the sorted tokens, and a run of many tokens is shared by all.
+// column blocks y, y + shares, ...  It looks through all tokens, keeps those of its rows in their order, sets the rows without any to
+// zero (`zeros`; beyond kOwnZeros bytes, or where a launch turns the gradient first, that launch does it for all rows, at a higher rate),
+// sorts what it kept by the row and deals it out to its wavefronts evenly.  Latency bounds it, and the instructions that it fetches: at
+// 8192 tokens of 20000 x 300 (148 in the fullest workgroup) 2.5 us to look through the tokens, 2 to sort, 4 for the first rows, 3 to
+// end the runs and join; the median workgroup takes half as long.
 constexpr int kFewTokens = 8192, kBuckets = 256, kBucketBits = 8, kBucketDigit = 9, kMarks = 1 << 15;
 constexpr int kFewEach = kFewTokens / kSortThreads;
 constexpr unsigned long long kOwnZeros = 32ull << 20;
 constexpr unsigned kPairs = 256;
 constexpr int kFewBits = 13;
+constexpr int kFewAhead = 10;      // rows that a wavefront has in flight (as registers go)
 
 template <class G, class W>
 __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, const G* grad, int passes, int digit_bits, int column_blocks, int shares, bool zeros)
@@ -599,35 +609,42 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
     } room;
     __shared__ unsigned marks[kMarks / 32];                // rows of the bucket that have tokens
     __shared__ int counts[kSortWaves];
-    __shared__ unsigned long_from[kFewTokens / kLong], long_to[kFewTokens / kLong];
-    __shared__ int long_count;
     static_assert(kFewTokens <= 1 << 16, "places of 16 bits");
-    static_assert(kFewTokens == 1 << kFewBits && kPairs % 4 == 0, "numbers of tokens; four at a time");
+    static_assert(kFewTokens == 1 << kFewBits && kPairs % 4 == 0 && kPairs * 4 == kSortThreads, "numbers of tokens; four at a time");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const unsigned tokens = (unsigned)a.sentences * a.words;
     const int each = (int)((tokens + kSortThreads - 1) / kSortThreads);
     const long long rows = (a.vocab - blockIdx.x + kBuckets - 1) >> kBucketBits;      // of this bucket
 
     const TokenArgs named{a.tokens, a.vocab, a.padding, tokens, a.wide};
-    unsigned key[kFewEach], place[kFewEach];
-    bool there[kFewEach];
-    unsigned long long mine[kFewEach];
-    int count = 0;
-#pragma unroll
-    for (int i = 0; i < kFewEach; ++i) {
-        place[i] = own_token(each, i);
-        there[i] = i < each && place[i] < tokens;
-        key[i] = there[i] ? sort_key(named, place[i]) : (unsigned)a.vocab;
-        there[i] = key[i] < (unsigned)a.vocab && (key[i] & (kBuckets - 1)) == blockIdx.x;
-    }
-    if (threadIdx.x == 0) long_count = 0;
     if (zeros)
         for (int i = threadIdx.x; i < kMarks / 32; i += kSortThreads) marks[i] = 0;
+    unsigned key[kFewEach], place[kFewEach];
+    unsigned long long mine[kFewEach];
+    int count = 0;
+    // All loads before the first use.  Of 64 tokens one in four has a token of this workgroup's, so the others get one look at their low
+    // bits.  Code that a size has no use for is jumped over (it would be fetched).
+    auto look = [&](auto* from) {
+        typename std::remove_const<typename std::remove_pointer<decltype(from)>::type>::type token[kFewEach];
 #pragma unroll
-    for (int i = 0; i < kFewEach; ++i) {
-        mine[i] = __ballot(there[i]);
-        count += __popcll(mine[i]);
-    }
+        for (int i = 0; i < kFewEach; ++i) {
+            if (i >= each) break;
+            place[i] = own_token(each, i);
+            token[i] = from[min(place[i], tokens - 1)];
+        }
+#pragma unroll
+        for (int i = 0; i < kFewEach; ++i) {
+            if (i >= each) break;
+            key[i] = (unsigned)token[i];
+            mine[i] = __ballot((key[i] & (kBuckets - 1)) == blockIdx.x);
+            if (mine[i]) {
+                mine[i] &= __ballot(place[i] < tokens && key_of(named, token[i]) < (unsigned)a.vocab);
+                count += __popcll(mine[i]);
+            }
+        }
+    };
+    if (a.wide) look(static_cast<const long long*>(a.tokens));
+    else look(static_cast<const int*>(a.tokens));
     if (lane == 0) counts[wave] = count;
     lds_barrier();
     int at = 0;
@@ -639,7 +656,9 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
     }
 #pragma unroll
     for (int i = 0; i < kFewEach; ++i) {
-        if (there[i]) {
+        if (i >= each) break;
+        if (!mine[i]) continue;
+        if (mine[i] >> lane & 1) {
             const int to = at + __popcll(mine[i] & ((1ull << lane) - 1));
             keys[to] = key[i] >> kBucketBits;
             places[to] = (unsigned short)place[i];
@@ -665,24 +684,30 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
 
     // A stable sort by the key, in LDS: few tokens by counting those that go before each, more by digits.
     if (total <= kPairs && rows <= 1ll << (32 - kFewBits)) {
-        // (key, number) as one number: all differ
-        const unsigned t = threadIdx.x, k = t < total ? keys[t] : 0u, own = t < total ? k << kFewBits | t : ~0u;
-        const unsigned short own_place = t < total ? places[t] : 0;
-        if (t < kPairs) room.pairs[t] = own;
+        // (key, number) as one number: all differ.  Four lanes a token.
+        const unsigned t = threadIdx.x, i = t / 4, k = i < total ? keys[i] : 0u;
+        const unsigned short own_place = i < total ? places[i] : 0;
+        if (t < kPairs) room.pairs[t] = t < total ? keys[t] << kFewBits | t : ~0u;
         lds_barrier();
-        if (t < total) {
+        if (i < total) {
+            const unsigned own = k << kFewBits | i;
             unsigned before = 0;
-#pragma unroll 4
-            for (unsigned j = 0; j < total; j += 4) {
+#pragma unroll 2
+            for (unsigned j = t % 4 * 4; j < total; j += 16) {
                 const uint4 n = *reinterpret_cast<const uint4*>(room.pairs + j);
                 before += (n.x < own) + (n.y < own) + (n.z < own) + (n.w < own);
             }
-            keys[before] = k;
-            places[before] = own_place;
+            before += (unsigned)__shfl_xor((int)before, 1);
+            before += (unsigned)__shfl_xor((int)before, 2);
+            if (t % 4 == 0) {
+                keys[before] = k;
+                places[before] = own_place;
+            }
         }
         lds_barrier();
     } else {
         const int kept = (int)((total + kSortThreads - 1) / kSortThreads);
+        bool there[kFewEach];
 #pragma unroll
         for (int i = 0; i < kFewEach; ++i) {
             const unsigned t = own_token(kept, i);
@@ -720,55 +745,59 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
         }
     }
 
-    // The long runs, and where they end.
-    for (unsigned t = threadIdx.x; t + kLong < total; t += kSortThreads) {
-        const unsigned k = keys[t];
-        if (keys[t + kLong] != k || (t > 0 && keys[t - 1] == k)) continue;
-        unsigned same = t + kLong, other = total;      // a token of the run, one past it
-        while (other - same > 1) {
-            const unsigned middle = (same + other) / 2;
-            if (keys[middle] == k) same = middle;
-            else other = middle;
-        }
-        const int l = atomicAdd(&long_count, 1);
-        long_from[l] = t;
-        long_to[l] = other;
-    }
-    lds_barrier();
-
-    // A long run and a column block are shared by `parts` wavefronts; a round is as many such pairs as there are wavefronts for.
-    const int shared_runs = long_count, parts = max(kSortWaves / own_blocks, 1), together = kSortWaves / parts;
-    const int pairs = shared_runs * own_blocks;
-    auto store = [&](unsigned k, const Sums& of_row, const Columns& c) { store_row<W>(table_grad + k * apart, of_row, c, a.scale, a.accumulate); };
-    auto add_pairs = [&](int first) {
-        const int pair = first + wave / parts, part = wave % parts;
+    // The sorted tokens are dealt out evenly, whatever rows they belong to: `parts` wavefronts share a column block and take `share`
+    // tokens in a row each.  What a wavefront has of a run that began before its tokens it leaves in LDS; the wavefront in which the
+    // run begins adds that up.
+    const int parts = max(kSortWaves / own_blocks, 1), together = kSortWaves / parts;
+    const unsigned share = (total + parts - 1) / parts, part = wave % parts, from = min(part * share, total), to = min(from + share, total);
+    for (int first = 0; first < own_blocks; first += together) {
+        const int block = first + wave / parts;
+        const Columns c = columns(block);
+        const bool works = wave / parts < together && block < own_blocks && from < to;
+        unsigned k = 0;
+        bool before = false, open = false;      // the run at hand began before; it has not ended here
+        auto store = [&]() { store_row<W>(table_grad + k * apart, sums, c, a.scale, a.accumulate); };
         clear(sums);
-        if (wave / parts >= together || pair >= pairs) return;
-        const unsigned from = __builtin_amdgcn_readfirstlane(long_from[pair / own_blocks]), length = __builtin_amdgcn_readfirstlane(long_to[pair / own_blocks]) - from;
-        const unsigned p0 = length * part / parts, p1 = length * (part + 1) / parts;
-        add_rows<G>(sums, grad, a.dim, (int)(p1 - p0), columns(pair % own_blocks), [&](int i) { return (int)places[from + p0 + i]; });
-        leave(sums, room.part);
-    };
-    auto finish_pairs = [&](int first) {
-        lds_barrier();
-        const int pair = first + wave / parts;
-        if (wave / parts < together && pair < pairs && wave % parts == 0) {
-            join(sums, room.part, wave, parts);
-            store(keys[long_from[pair / own_blocks]], sums, columns(pair % own_blocks));
+        if (works) {
+            before = from > 0 && keys[from - 1] == keys[from];
+#pragma unroll 1
+            for (unsigned start = from; start < to; start += 64) {
+                const unsigned t = start + lane, here = min(to - start, 64u);
+                const unsigned own = t < to ? keys[t] : 0u;
+                const int own_place = t < to ? places[t] : 0;
+                const unsigned long long ends = __ballot(t < to && (t + 1 == total || keys[min(t + 1, total - 1)] != own));
+#pragma unroll 1
+                for (unsigned i = 0; i < here; i += kFewAhead) {
+                    Row<G> r[kFewAhead];
+#pragma unroll
+                    for (int u = 0; u < kFewAhead; ++u)
+                        if (i + u < here) r[u] = load_row<G>(grad + (size_t)(unsigned)__builtin_amdgcn_readlane(own_place, i + u) * a.dim, c);
+#pragma unroll
+                    for (int u = 0; u < kFewAhead; ++u) {
+                        if (i + u >= here) break;
+                        add(sums, r[u], c);
+                        open = !(ends >> (i + u) & 1);
+                        if (open) continue;
+                        k = (unsigned)__builtin_amdgcn_readlane((int)own, i + u);
+                        if (before) leave(sums, room.part);
+                        else store();
+                        before = false;
+                        clear(sums);
+                    }
+                }
+                k = (unsigned)__builtin_amdgcn_readlane((int)own, here - 1);
+            }
+            if (open && before) leave(sums, room.part);
         }
-    };
-    if (pairs) add_pairs(0);
-    const int slots = (int)((total + kSlot - 1) / kSlot);
-    for (int unit = wave; unit < slots * own_blocks; unit += kSortWaves) {
-        const Columns c = columns(unit / slots);
-        add_slot<G>(grad, a.dim, c, (unsigned)(unit % slots) * kSlot, total, ~0u, [&](unsigned i) { return keys[i]; }, [&](unsigned i) { return (int)places[i]; },
-                    [&](unsigned k, const Sums& of_row) { store(k, of_row, c); }, [](unsigned) {});
-    }
-    if (pairs) finish_pairs(0);
-    for (int first = together; first < pairs; first += together) {
+        if (parts == 1) continue;
         lds_barrier();
-        add_pairs(first);
-        finish_pairs(first);
+        if (open && !before) {
+            const unsigned t = lane * share;
+            const int more = __popcll(__ballot(lane > (int)part && lane < parts && t < total && keys[min(t, total - 1)] == k));
+            join(sums, room.part, wave + 1, more);
+            store();
+        }
+        if (first + together < own_blocks) lds_barrier();
     }
 }
 
@@ -917,7 +946,7 @@ __global__ __launch_bounds__(kRunThreads) void runs_kernel(EmbedGradArgs a, cons
         leave(sums, part);
         lds_barrier();
         if (wave == 0) {
-            join(sums, part, 0, kRunWaves);
+            join(sums, part, 1, kRunWaves - 1);
             done(sorted.keys[from], sums);
         }
         lds_barrier();
@@ -979,7 +1008,7 @@ int launch_grad(const EmbedGradArgs& a, const Parts& parts, char* workspace, hip
     const unsigned long long elements = a.accumulate ? 0 : (unsigned long long)a.vocab * a.dim;
     const TurnArgs turn{a.grad, rows, a.dim, a.sentences, a.words, (unsigned)tiles};
     if (tokens <= kFewTokens) {
-        const bool zeros = !a.accumulate && elements * sizeof(W) <= kOwnZeros && a.vocab <= (long long)kMarks * kBuckets;
+        const bool zeros = !a.accumulate && !tiles && elements * sizeof(W) <= kOwnZeros && a.vocab <= (long long)kMarks * kBuckets;
         const Fill fill{a.table_grad, zeros ? 0 : elements};
         const unsigned long long blocks = blocks_of<W>(turn.tiles, fill);
         if (blocks >= (1ull << 31)) return (int)hipErrorInvalidValue;

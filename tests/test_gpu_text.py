@@ -235,6 +235,31 @@ def test_gradient_of_one_bucket_of_rows():
         _within(out, ref, bound + U["f32"] * (np.abs(ref) + bound) + TINY["f32"], (t, dim, spread))
 
 
+@pytest.mark.parametrize("types", [("f32", "f32"), ("f16", "f16")])
+def test_gradient_at_the_ends_of_column_blocks(types):
+    """Rows about as long as 512 columns and of fewer than four: set and added, and nothing around the table's gradient is written."""
+    import torch
+    from paper_2011_06295_amd import text
+    rng = np.random.default_rng(31)
+    for t in (40, 8300):
+        for dim in (1, 2, 3, 4, 5, 255, 257, 511, 512, 513, 514, 515, 516, 769, 1025):
+            vocab = 23
+            print(f"column blocks {types} {t} tokens, {dim} columns", flush=True)
+            tok = rng.integers(0, vocab, t)
+            g = torch.from_numpy(rng.standard_normal((t, dim)).astype(np.float32)).to(_types()[types[0]])
+            ref, bound = _gradient_reference(_wide(g), tok, vocab, dim, 1.0, -1)
+            room = torch.full((vocab * dim + 16,), 5.0, dtype=_types()[types[1]], device="cuda")
+            out = room[8:-8].reshape(vocab, dim)
+            layer = text.Embedding(torch.empty_like(out))
+            layer.backward(g.cuda(), torch.from_numpy(tok).cuda(), out=out)
+            once = bound + U[types[1]] * (np.abs(ref) + bound) + TINY[types[1]]
+            _within(out, ref, once, (t, dim))
+            layer.backward(g.cuda(), torch.from_numpy(tok).cuda(), out=out, accumulate=True)
+            twice = once + bound + 2.0 ** -24 * (2 * np.abs(ref) + once + bound)
+            _within(out, 2 * ref, twice + U[types[1]] * (2 * np.abs(ref) + twice) + TINY[types[1]], (t, dim, "added"))
+            assert bool((room[:8] == 5.0).all()) and bool((room[-8:] == 5.0).all())
+
+
 def test_gradient_of_no_tokens_is_zero():
     import torch
     from paper_2011_06295_amd import text
