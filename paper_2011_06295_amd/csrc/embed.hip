@@ -582,14 +582,8 @@ struct Sorted {
     int* places;
 };
 
-// ---------------------------------------------------------------- gradient of few tokens: one launch
+// ---------------------------------------------------------------- gradient of few tokens: one launch, two with a turn or many zeros
 
-// Workgroup (b, y) owns the rows of the table whose number ends in b (kBuckets of them: frequent tokens are often neighbours), and
-// column blocks y, y + shares, ...  It looks through all tokens, keeps those of its rows in their order, sets the rows without any to
-// zero (`zeros`; beyond kOwnZeros bytes, or where a launch turns the gradient first, that launch does it for all rows, at a higher rate),
-// sorts what it kept by the row and deals it out to its wavefronts evenly.  Latency bounds it, and the instructions that it fetches: at
-// 8192 tokens of 20000 x 300 (148 in the fullest workgroup) 2.5 us to look through the tokens, 2 to sort, 4 for the first rows, 3 to
-// end the runs and join; the median workgroup takes half as long.
 constexpr int kFewTokens = 8192, kBuckets = 256, kBucketBits = 8, kBucketDigit = 9, kMarks = 1 << 15;
 constexpr int kFewEach = kFewTokens / kSortThreads;
 constexpr unsigned long long kOwnZeros = 32ull << 20;
@@ -597,31 +591,33 @@ constexpr unsigned kPairs = 256;
 constexpr int kFewBits = 13;
 constexpr int kFewAhead = 10;      // rows that a wavefront has in flight (as registers go)
 
-template <class G, class W>
-__global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, const G* grad, int passes, int digit_bits, int column_blocks, int shares, bool zeros)
-{
-    __shared__ unsigned keys[kFewTokens];                  // number of the row within the bucket
-    __shared__ unsigned short places[kFewTokens];
-    __shared__ __attribute__((aligned(16))) union {
-        unsigned pairs[kPairs];
-        int of_wave[kSortWaves][1 << kBucketDigit];
-        float part[kSortWaves][kColumns];
-    } room;
-    __shared__ unsigned marks[kMarks / 32];                // rows of the bucket that have tokens
-    __shared__ int counts[kSortWaves];
-    static_assert(kFewTokens <= 1 << 16, "places of 16 bits");
-    static_assert(kFewTokens == 1 << kFewBits && kPairs % 4 == 0 && kPairs * 4 == kSortThreads, "numbers of tokens; four at a time");
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const unsigned tokens = (unsigned)a.sentences * a.words;
-    const int each = (int)((tokens + kSortThreads - 1) / kSortThreads);
-    const long long rows = (a.vocab - blockIdx.x + kBuckets - 1) >> kBucketBits;      // of this bucket
+__device__ __forceinline__ long long rows_of(long long vocab, unsigned bucket) { return (vocab - bucket + kBuckets - 1) >> kBucketBits; }
 
-    const TokenArgs named{a.tokens, a.vocab, a.padding, tokens, a.wide};
-    if (zeros)
-        for (int i = threadIdx.x; i < kMarks / 32; i += kSortThreads) marks[i] = 0;
+template <int BITS>
+struct BucketRoom {
+    unsigned keys[kFewTokens];                  // number of the row within the bucket
+    unsigned short places[kFewTokens];
+    union {
+        __attribute__((aligned(16))) unsigned pairs[kPairs];
+        int of_wave[kSortWaves][1 << BITS];
+    };
+    int counts[kSortWaves], earlier[kSortWaves];
+};
+static_assert(kFewTokens <= 1 << 16, "places of 16 bits");
+static_assert(kFewTokens == 1 << kFewBits && kPairs % 4 == 0 && kPairs * 4 == kSortThreads, "numbers of tokens; four at a time, by four lanes");
+
+// Leaves the tokens of a bucket in room.keys and .places, sorted, and returns their number; `marks` (if there) gets a bit for each of
+// their rows; start: with EARLIER, the number of tokens of the buckets before.  between() runs when the marks are whole.
+template <int BITS, bool EARLIER, class Between>
+__device__ __forceinline__ unsigned sort_bucket(const TokenArgs& a, unsigned bucket, int passes, int digit_bits, BucketRoom<BITS>& room, unsigned* marks, unsigned& start,
+                                                Between between)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int each = (int)((a.count + kSortThreads - 1) / kSortThreads);
+    const long long rows = rows_of(a.vocab, bucket);
     unsigned key[kFewEach], place[kFewEach];
     unsigned long long mine[kFewEach];
-    int count = 0;
+    int count = 0, before = 0;
     // All loads before the first use.  Of 64 tokens one in four has a token of this workgroup's, so the others get one look at their low
     // bits.  Code that a size has no use for is jumped over (it would be fetched).
     auto look = [&](auto* from) {
@@ -630,29 +626,37 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
         for (int i = 0; i < kFewEach; ++i) {
             if (i >= each) break;
             place[i] = own_token(each, i);
-            token[i] = from[min(place[i], tokens - 1)];
+            token[i] = from[min(place[i], a.count - 1)];
         }
 #pragma unroll
         for (int i = 0; i < kFewEach; ++i) {
             if (i >= each) break;
             key[i] = (unsigned)token[i];
-            mine[i] = __ballot((key[i] & (kBuckets - 1)) == blockIdx.x);
-            if (mine[i]) {
-                mine[i] &= __ballot(place[i] < tokens && key_of(named, token[i]) < (unsigned)a.vocab);
-                count += __popcll(mine[i]);
+            mine[i] = __ballot((key[i] & (kBuckets - 1)) == bucket);
+            if (EARLIER) {
+                const bool valid = place[i] < a.count && key_of(a, token[i]) < (unsigned)a.vocab;
+                mine[i] &= __ballot(valid);
+                before += __popcll(__ballot(valid && (key[i] & (kBuckets - 1)) < bucket));
+            } else if (mine[i]) {
+                mine[i] &= __ballot(place[i] < a.count && key_of(a, token[i]) < (unsigned)a.vocab);
             }
+            count += __popcll(mine[i]);
         }
     };
     if (a.wide) look(static_cast<const long long*>(a.tokens));
     else look(static_cast<const int*>(a.tokens));
-    if (lane == 0) counts[wave] = count;
+    if (lane == 0) {
+        room.counts[wave] = count;
+        if (EARLIER) room.earlier[wave] = before;
+    }
     lds_barrier();
     int at = 0;
     unsigned total = 0;
 #pragma unroll
     for (int w = 0; w < kSortWaves; ++w) {
-        at += w < wave ? counts[w] : 0;
-        total += counts[w];
+        at += w < wave ? room.counts[w] : 0;
+        total += room.counts[w];
+        if (EARLIER) start += room.earlier[w];
     }
 #pragma unroll
     for (int i = 0; i < kFewEach; ++i) {
@@ -660,34 +664,21 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
         if (!mine[i]) continue;
         if (mine[i] >> lane & 1) {
             const int to = at + __popcll(mine[i] & ((1ull << lane) - 1));
-            keys[to] = key[i] >> kBucketBits;
-            places[to] = (unsigned short)place[i];
-            if (zeros) atomicOr(&marks[key[i] >> (kBucketBits + 5)], 1u << (key[i] >> kBucketBits & 31));
+            room.keys[to] = key[i] >> kBucketBits;
+            room.places[to] = (unsigned short)place[i];
+            if (marks) atomicOr(&marks[key[i] >> (kBucketBits + 5)], 1u << (key[i] >> kBucketBits & 31));
         }
         at += __popcll(mine[i]);
     }
     lds_barrier();
-
-    const int own_blocks = (column_blocks - (int)blockIdx.y + shares - 1) / shares;
-    auto columns = [&](int block) { return columns_of((int)(blockIdx.y + block * shares), lane, a.dim); };
-    W* table_grad = static_cast<W*>(a.table_grad) + (size_t)blockIdx.x * a.dim;
-    const size_t apart = (size_t)kBuckets * a.dim;         // elements from one row of the bucket to the next
-    Sums sums;
-    if (zeros) {
-        clear(sums);
-        for (int block = 0; block < own_blocks; ++block) {
-            const Columns c = columns(block);
-            for (int r = wave; r < (int)rows; r += kSortWaves)
-                if (!(marks[r >> 5] >> (r & 31) & 1)) store_row<W>(table_grad + r * apart, sums, c, 1.f, false);
-        }
-    }
+    between();
 
     // A stable sort by the key, in LDS: few tokens by counting those that go before each, more by digits.
     if (total <= kPairs && rows <= 1ll << (32 - kFewBits)) {
         // (key, number) as one number: all differ.  Four lanes a token.
-        const unsigned t = threadIdx.x, i = t / 4, k = i < total ? keys[i] : 0u;
-        const unsigned short own_place = i < total ? places[i] : 0;
-        if (t < kPairs) room.pairs[t] = t < total ? keys[t] << kFewBits | t : ~0u;
+        const unsigned t = threadIdx.x, i = t / 4, k = i < total ? room.keys[i] : 0u;
+        const unsigned short own_place = i < total ? room.places[i] : 0;
+        if (t < kPairs) room.pairs[t] = t < total ? room.keys[t] << kFewBits | t : ~0u;
         lds_barrier();
         if (i < total) {
             const unsigned own = k << kFewBits | i;
@@ -700,8 +691,8 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
             before += (unsigned)__shfl_xor((int)before, 1);
             before += (unsigned)__shfl_xor((int)before, 2);
             if (t % 4 == 0) {
-                keys[before] = k;
-                places[before] = own_place;
+                room.keys[before] = k;
+                room.places[before] = own_place;
             }
         }
         lds_barrier();
@@ -712,37 +703,123 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
         for (int i = 0; i < kFewEach; ++i) {
             const unsigned t = own_token(kept, i);
             there[i] = i < kept && t < total;
-            key[i] = there[i] ? keys[t] : 0u;
-            place[i] = there[i] ? places[t] : 0u;
+            key[i] = there[i] ? room.keys[t] : 0u;
+            place[i] = there[i] ? room.places[t] : 0u;
         }
         for (int pass = 0; pass < passes; ++pass) {
             const int shift = pass * digit_bits, digit = threadIdx.x, size = 1 << digit_bits;
             int rank[kFewEach];
-            rank_tokens<kFewEach, kBucketDigit>(key, there, kept, shift, digit_bits, room.of_wave, rank);
+            rank_tokens<kFewEach, BITS>(key, there, kept, shift, digit_bits, room.of_wave, rank);
             lds_barrier();
             int here = 0;
             if (digit < size)
 #pragma unroll
                 for (int w = 0; w < kSortWaves; ++w) here += room.of_wave[w][digit];
-            const int base = sum_before(here, counts);
-            if (digit < size) spread<kBucketDigit>(room.of_wave, digit, base);
+            const int base = sum_before(here, room.counts);
+            if (digit < size) spread<BITS>(room.of_wave, digit, base);
             lds_barrier();
 #pragma unroll
             for (int i = 0; i < kFewEach; ++i)
                 if (there[i]) {
                     const int to = room.of_wave[wave][(key[i] >> shift) & (unsigned)(size - 1)] + rank[i];
-                    keys[to] = key[i];
-                    places[to] = (unsigned short)place[i];
+                    room.keys[to] = key[i];
+                    room.places[to] = (unsigned short)place[i];
                 }
             lds_barrier();
             if (pass + 1 < passes)
 #pragma unroll
                 for (int i = 0; i < kFewEach; ++i)
                     if (there[i]) {
-                        key[i] = keys[own_token(kept, i)];
-                        place[i] = places[own_token(kept, i)];
+                        key[i] = room.keys[own_token(kept, i)];
+                        place[i] = room.places[own_token(kept, i)];
                     }
         }
+    }
+    return total;
+}
+
+// Where a launch goes before that of the sums, it sorts the tokens: lists of all buckets, one after another, and where each begins.
+struct Lists {
+    unsigned start[kBuckets], count[kBuckets];
+    // the rows' numbers within their bucket, then the places
+
+    __device__ unsigned* keys() { return count + kBuckets; }
+    __device__ unsigned short* places(unsigned tokens) { return reinterpret_cast<unsigned short*>(keys() + tokens); }
+};
+constexpr long long lists_bytes(long long tokens) { return (long long)sizeof(Lists) + tokens * 6; }
+
+// Turns, then sorts in `groups` workgroups, one a bucket, then sets to zero: in this order, for the sort takes a while and zeros go out
+// beside it (two workgroups to a CU: digits of 8 bits leave the room for it).
+constexpr int kListDigit = 8;
+
+template <class G, class W>
+__global__ __launch_bounds__(kSortThreads, 8) void lists_kernel(TokenArgs a, TurnArgs turn, Fill fill, Lists* lists, int groups, short passes, short digit_bits)
+{
+    typedef BucketRoom<kListDigit> Room;
+    __shared__ __attribute__((aligned(16))) char bytes[sizeof(Room) > tiles_room<G>() ? sizeof(Room) : tiles_room<G>()];
+    const unsigned turning = (turn.tiles + kTiles - 1) / kTiles, bucket = blockIdx.x - turning;
+    if (bucket >= (unsigned)groups) {
+        turn_or_fill<G, W>(turn, fill, blockIdx.x < turning ? blockIdx.x : blockIdx.x - groups, bytes);
+        return;
+    }
+    Room& room = *reinterpret_cast<Room*>(bytes);
+    unsigned start = 0;
+    const unsigned total = sort_bucket<kListDigit, true>(a, bucket, passes, digit_bits, room, nullptr, start, [] {});
+    for (unsigned t = threadIdx.x; t < total; t += kSortThreads) {
+        lists->keys()[start + t] = room.keys[t];
+        lists->places(a.count)[start + t] = room.places[t];
+    }
+    if (threadIdx.x == 0) {
+        lists->start[bucket] = start;
+        lists->count[bucket] = total;
+    }
+}
+
+// Workgroup (b, y) owns the rows of the table whose number ends in b (kBuckets of them: frequent tokens are often neighbours), and
+// column blocks y, y + shares, ...  It takes the sorted tokens of its rows from the launch before, or looks through all tokens and sorts
+// them itself, sets the rows without any to zero (`zeros`; a launch before does that at a higher rate, so beyond kOwnZeros bytes
+// there is one) and deals the sorted tokens out to its wavefronts evenly.  Latency bounds it, and the instructions that it fetches:
+// 9.0 us at 8192 tokens of 20000 x 300 with the fullest workgroup's 148 tokens sorted before (the launch before takes 10.1, 8.1 without the
+// sort; sorting here took 3.9), 4.2 at 37 tokens.
+template <class G, class W>
+__global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, const G* grad, Lists* lists, short passes, short digit_bits, int column_blocks, int shares, bool zeros)
+{
+    __shared__ __attribute__((aligned(16))) BucketRoom<kBucketDigit> room;
+    __shared__ unsigned marks[kMarks / 32];                // rows of the bucket that have tokens
+    unsigned* const keys = room.keys;
+    unsigned short* const places = room.places;
+    float (*const part_sums)[kColumns] = reinterpret_cast<float (*)[kColumns]>(room.of_wave);      // (the sort is over when these are written)
+    static_assert(sizeof(room.of_wave) >= sizeof(float) * kSortWaves * kColumns, "a part of each wavefront fits");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const TokenArgs named{a.tokens, a.vocab, a.padding, (unsigned)a.sentences * a.words, a.wide};
+    const int own_blocks = (column_blocks - (int)blockIdx.y + shares - 1) / shares;
+    auto columns = [&](int block) { return columns_of((int)(blockIdx.y + block * shares), lane, a.dim); };
+    W* table_grad = static_cast<W*>(a.table_grad) + (size_t)blockIdx.x * a.dim;
+    const size_t apart = (size_t)kBuckets * a.dim;         // elements from one row of the bucket to the next
+    Sums sums;
+    unsigned total;
+    if (lists) {
+        const unsigned start = lists->start[blockIdx.x];
+        total = lists->count[blockIdx.x];
+        for (unsigned t = threadIdx.x; t < total; t += kSortThreads) {
+            keys[t] = lists->keys()[start + t];
+            places[t] = lists->places(named.count)[start + t];
+        }
+        lds_barrier();
+    } else {
+        if (zeros)
+            for (int i = threadIdx.x; i < kMarks / 32; i += kSortThreads) marks[i] = 0;
+        unsigned start;
+        total = sort_bucket<kBucketDigit, false>(named, blockIdx.x, passes, digit_bits, room, zeros ? marks : nullptr, start, [&] {
+            if (!zeros) return;
+            clear(sums);
+            const int rows = (int)rows_of(a.vocab, blockIdx.x);
+            for (int block = 0; block < own_blocks; ++block) {
+                const Columns c = columns(block);
+                for (int r = wave; r < rows; r += kSortWaves)
+                    if (!(marks[r >> 5] >> (r & 31) & 1)) store_row<W>(table_grad + r * apart, sums, c, 1.f, false);
+            }
+        });
     }
 
     // The sorted tokens are dealt out evenly, whatever rows they belong to: `parts` wavefronts share a column block and take `share`
@@ -779,7 +856,7 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
                         open = !(ends >> (i + u) & 1);
                         if (open) continue;
                         k = (unsigned)__builtin_amdgcn_readlane((int)own, i + u);
-                        if (before) leave(sums, room.part);
+                        if (before) leave(sums, part_sums);
                         else store();
                         before = false;
                         clear(sums);
@@ -787,14 +864,14 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
                 }
                 k = (unsigned)__builtin_amdgcn_readlane((int)own, here - 1);
             }
-            if (open && before) leave(sums, room.part);
+            if (open && before) leave(sums, part_sums);
         }
         if (parts == 1) continue;
         lds_barrier();
         if (open && !before) {
             const unsigned t = lane * share;
             const int more = __popcll(__ballot(lane > (int)part && lane < parts && t < total && keys[min(t, total - 1)] == k));
-            join(sums, room.part, wave + 1, more);
+            join(sums, part_sums, wave + 1, more);
             store();
         }
         if (first + together < own_blocks) lds_barrier();
@@ -955,27 +1032,19 @@ __global__ __launch_bounds__(kRunThreads) void runs_kernel(EmbedGradArgs a, cons
 
 // Before a launch of few tokens: what has to be turned and, where that is much, set to zero.  Tiles alone by workgroups of one: 640 of
 // them spread over the CUs better than 160 of four (6.0 us instead of 7.1).
-template <class G>
-__global__ __launch_bounds__(kThreads) void turn_kernel(TurnArgs turn)
-{
-    __shared__ __attribute__((aligned(16))) char room[tiles_room<G>() / kTiles];
-    turn_tiles<G>(turn, blockIdx.x, reinterpret_cast<G*>(room));
-}
-
-template <class G, class W>
-__global__ __launch_bounds__(kSortThreads) void turn_or_fill_kernel(TurnArgs turn, Fill fill)
-{
-    __shared__ __attribute__((aligned(16))) char room[tiles_room<G>()];
-    turn_or_fill<G, W>(turn, fill, blockIdx.x, room);
-}
-
 int type_bytes(int dtype) { return dtype == kF32 ? 4 : 2; }
 long long rounded(long long bytes) { return (bytes + 255) / 256 * 256; }
 
 // What the workspace holds, in this order.
 struct Parts {
-    long long rows, keys, counts, windows, total;      // bytes; keys: of each of two pairs of arrays, tokens and places
+    long long rows, keys, counts, windows, lists, total;      // bytes; keys: of each of two pairs of arrays, tokens and places
 };
+
+// Few tokens: whether the launch that sums sets the rows without tokens to zero.
+bool sets_own_zeros(const EmbedGradArgs& a, int table_bytes)
+{
+    return (unsigned long long)a.vocab * a.dim * table_bytes <= kOwnZeros && a.vocab <= (long long)kMarks * kBuckets;
+}
 
 Parts parts_of(const EmbedGradArgs& a, int grad_dtype)
 {
@@ -987,8 +1056,10 @@ Parts parts_of(const EmbedGradArgs& a, int grad_dtype)
         p.keys = rounded(tokens * 4);
         p.counts = rounded((long long)plan.groups * (1 << plan.digit) * 4);
         p.windows = rounded(tokens / kWindow * a.dim * 4);
+    } else if (p.rows || (!a.accumulate && !sets_own_zeros(a, 4))) {
+        p.lists = rounded(lists_bytes(tokens));
     }
-    p.total = p.rows + 4 * p.keys + p.counts + p.windows;
+    p.total = p.rows + 4 * p.keys + p.counts + p.windows + p.lists;
     return p;
 }
 
@@ -1008,17 +1079,23 @@ int launch_grad(const EmbedGradArgs& a, const Parts& parts, char* workspace, hip
     const unsigned long long elements = a.accumulate ? 0 : (unsigned long long)a.vocab * a.dim;
     const TurnArgs turn{a.grad, rows, a.dim, a.sentences, a.words, (unsigned)tiles};
     if (tokens <= kFewTokens) {
-        const bool zeros = !a.accumulate && !tiles && elements * sizeof(W) <= kOwnZeros && a.vocab <= (long long)kMarks * kBuckets;
+        const bool zeros = !a.accumulate && !tiles && sets_own_zeros(a, sizeof(W));
         const Fill fill{a.table_grad, zeros ? 0 : elements};
-        const unsigned long long blocks = blocks_of<W>(turn.tiles, fill);
-        if (blocks >= (1ull << 31)) return (int)hipErrorInvalidValue;
-        if (fill.count) hipLaunchKernelGGL((turn_or_fill_kernel<G, W>), dim3((unsigned)blocks), dim3(kSortThreads), 0, s, turn, fill);
-        else if (tiles) hipLaunchKernelGGL(turn_kernel<G>, dim3((unsigned)tiles), dim3(kThreads), 0, s, turn);
-        const SortPlan plan = sort_plan((a.vocab - 1) >> kBucketBits, kBucketDigit, tokens);
         const unsigned groups = (unsigned)std::min<long long>(a.vocab, kBuckets);
         const unsigned shares = (unsigned)std::min<long long>(column_blocks, kBuckets / groups);      // of the column blocks: a workgroup a CU
-        hipLaunchKernelGGL((bucket_kernel<G, W>), dim3(groups, shares), dim3(kSortThreads), 0, s, a, grad, plan.passes, plan.digit, (int)column_blocks,
-                           (int)shares, zeros);
+        Lists* lists = nullptr;
+        if (tiles || fill.count) {
+            const unsigned long long blocks = groups + blocks_of<W>(turn.tiles, fill);
+            if (blocks >= (1ull << 31)) return (int)hipErrorInvalidValue;
+            const TokenArgs named{a.tokens, a.vocab, a.padding, (unsigned)tokens, a.wide};
+            const SortPlan plan = sort_plan((a.vocab - 1) >> kBucketBits, kListDigit, tokens);
+            lists = reinterpret_cast<Lists*>(workspace + parts.rows);
+            hipLaunchKernelGGL((lists_kernel<G, W>), dim3((unsigned)blocks), dim3(kSortThreads), 0, s, named, turn, fill, lists, (int)groups, (short)plan.passes,
+                               (short)plan.digit);
+        }
+        const SortPlan plan = sort_plan((a.vocab - 1) >> kBucketBits, kBucketDigit, tokens);
+        hipLaunchKernelGGL((bucket_kernel<G, W>), dim3(groups, shares), dim3(kSortThreads), 0, s, a, grad, lists, (short)plan.passes, (short)plan.digit,
+                           (int)column_blocks, (int)shares, zeros);
         return (int)hipGetLastError();
     }
     const SortPlan plan = sort_plan(a.vocab, kMaxDigit, tokens);
