@@ -812,12 +812,16 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
         unsigned start;
         total = sort_bucket<kBucketDigit, false>(named, blockIdx.x, passes, digit_bits, room, zeros ? marks : nullptr, start, [&] {
             if (!zeros) return;
-            clear(sums);
-            const int rows = (int)rows_of(a.vocab, blockIdx.x);
-            for (int block = 0; block < own_blocks; ++block) {
-                const Columns c = columns(block);
-                for (int r = wave; r < rows; r += kSortWaves)
-                    if (!(marks[r >> 5] >> (r & 31) & 1)) store_row<W>(table_grad + r * apart, sums, c, 1.f, false);
+            // pieces of 16 bytes of all rows, one after another: a row may be a few lanes wide
+            constexpr int kVec = 16 / sizeof(W);
+            typedef typename Piece<W, kVec>::type V;
+            const unsigned per_row = a.dim < kVec ? a.dim : (a.dim + kVec - 1) / kVec, pieces = (unsigned)rows_of(a.vocab, blockIdx.x) * per_row;
+            for (unsigned f = blockIdx.y * kSortThreads + threadIdx.x; f < pieces; f += shares * kSortThreads) {
+                const unsigned r = f / per_row, p = f % per_row;
+                if (marks[r >> 5] >> (r & 31) & 1) continue;
+                W* row = table_grad + r * apart;
+                if (a.dim < kVec) row[p] = (W)0.f;
+                else *reinterpret_cast<V*>(row + min((int)p * kVec, a.dim - kVec)) = V{};
             }
         });
     }
