@@ -455,9 +455,8 @@ struct IsByte { static constexpr bool value = false; };
 template <>
 struct IsByte<int8_t> { static constexpr bool value = true; };
 
-// The input is quantised by every workgroup for itself where that is little beside its weights: up to this many bytes of rows.
+// Rows of 8-bit integers that a workgroup can quantise for itself, in bytes.
 constexpr int kOwnBytes = 16384;
-bool quantises_itself(int M, int pitch) { return M <= 16 && (long long)M * pitch <= kOwnBytes; }
 
 // 16 MB tokens by 16 NB channels a workgroup, whose W wavefronts go round the 128-byte units of the rows and add their sums up at
 // the end.  A wavefront loads its units to a part of LDS of its own, D of them in flight, and waits for its own loads alone.  (Loads
@@ -636,7 +635,9 @@ int launch_row_product(const Int8Args& a, hipStream_t s)
 // (64 x 64 at 256 x 4096 -> 4096: 14.5 us by two steps, 10.0 by four), two steps where workgroups that share a CU hide each other's waits
 // (128 x 128 at 2048 x 4096 -> 4096: 32.7 by two, 35.2 by three).
 
-long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+// Pieces of `size` (a power of two) that n is cut into.  (The host looks at 14 kernels a call: 0.1 us without divisions of 64 bits, 0.25 with.)
+double pieces_of(int n, int size) { return (double)(((unsigned)n + (unsigned)size - 1) >> __builtin_ctz((unsigned)size)); }
+double rounds_of(double groups, double held) { return (double)(long long)((groups + held - 1.0) / held); }
 
 enum Kernel { kRow11, kRow21, kRow22, kRow41, kRow42, kTile22, kTile44, kTile88, kDeep22, kDeep42, kDeep44, kKernels };
 
@@ -652,8 +653,8 @@ constexpr RowRule kRowRules[] = {{1, 1, 256, 0.24, 1.34, 14.8, 137.0, 6.8}, {2, 
 
 double row_estimate(const RowRule& r, int M, int N, int pitch)
 {
-    const double groups = (double)(ceil_div(M, 16 * r.MB) * ceil_div(N, 16 * r.NB)), bytes = 16.0 * (r.MB + r.NB) * pitch;
-    const double rounds = std::ceil(groups / r.resident);
+    const double groups = pieces_of(M, 16 * r.MB) * pieces_of(N, 16 * r.NB), bytes = 16.0 * (r.MB + r.NB) * pitch;
+    const double rounds = rounds_of(groups, r.resident);
     const double load = std::max({groups * bytes / (r.all * 1e6), rounds * bytes / (r.one * 1e3), (double)N * pitch / (r.weights * 1e6)});
     return 3.0 + r.join * rounds + r.round * (rounds - 1.0) + load;
 }
@@ -670,17 +671,17 @@ constexpr TileRule kTileRules[] = {{2, 2, 4, 0.261, 0.211, 0.2, 2.4, 3.5}, {4, 4
 
 double tile_estimate(const TileRule& r, int M, int N, int pitch)
 {
-    const double groups = (double)(ceil_div(M, 32 * r.MB) * ceil_div(N, 32 * r.NB)), steps = pitch / 128.0, held = 256.0 * r.share;
-    const double rounds = std::floor(groups / held), rest = groups - rounds * held;
+    const double groups = pieces_of(M, 32 * r.MB) * pieces_of(N, 32 * r.NB), steps = pitch / 128.0, held = 256.0 * r.share;
+    const double rounds = (double)(long long)(groups / held), rest = groups - rounds * held;
     double us = r.start + rounds * (steps * r.each * r.share + r.finish);
-    if (rest > 0.0) us += steps * std::max(r.least, r.each * std::ceil(rest / 256.0)) + r.finish;
+    if (rest > 0.0) us += steps * std::max(r.least, r.each * rounds_of(rest, 256.0)) + r.finish;
     return std::max(us, 3.0 + (double)N * pitch / (r.weights * 1e6));
 }
 
-Kernel choose(int M, int N, int pitch)
+Kernel choose(int M, int N, int pitch, double& least)
 {
     int best = 0;
-    double least = 0.0;
+    least = 0.0;
     for (int k = 0; k < kKernels; ++k) {
         const double us = k < kTile22 ? row_estimate(kRowRules[k], M, N, pitch) : tile_estimate(kTileRules[k - kTile22], M, N, pitch);
         if (k == 0 || us < least) {
@@ -692,9 +693,9 @@ Kernel choose(int M, int N, int pitch)
 }
 
 template <class T>
-int launch_product(const Int8Args& a, hipStream_t s)
+int launch_product(Kernel kernel, const Int8Args& a, hipStream_t s)
 {
-    switch (choose(a.M, a.N, a.pitch)) {
+    switch (kernel) {
         case kRow11: return launch_row_product<T, int8_t, 1, 1, 8, 4>(a, s);
         case kRow21: return launch_row_product<T, int8_t, 2, 1, 8, 2>(a, s);
         case kRow22: return launch_row_product<T, int8_t, 2, 2, 4, 2>(a, s);
@@ -709,20 +710,68 @@ int launch_product(const Int8Args& a, hipStream_t s)
     }
 }
 
-template <class T, class X>
-int launch_own(const Int8Args& a, hipStream_t s)
+// An input that is not quantised yet takes a launch of its own, 2.5 to 3.9 us more on the GPU and 2.75 on the host (kQuantise counts
+// some of that), or every workgroup of a row kernel quantises its 16 rows for itself while its first weights are on their way.  Fitted to
+// 114 sizes (1 to 593 tokens, K 128 to 4096, N 10 to 12288), the rule takes 0.5 % more than the fastest one call after another, 1.6 % in
+// a graph.  1 x 2048 -> 4288 5.7 us against 8.9, 1 x 4096 -> 12288 12.5 against 15.3, 101 x 384 -> 256 5.0 against 8.9;
+// 593 x 384 -> 1280 would take 11.3 against 8.7.
+enum Own { kOwn16, kOwn4, kOwn4Wide, kOwns, kTwoLaunches = kOwns };
+
+struct Choice {
+    Own own;
+    Kernel product;      // after another launch
+};
+
+struct OwnRule {
+    int NB, resident;                                  // blocks of channels; workgroups that a CU holds
+    double start, round, each, more, weights, one;     // us; us a round; us for 1000 values a round, a further workgroup on a CU; MB/us; KB/us
+};
+constexpr OwnRule kOwnRules[] = {{1, 1, 3.7, 3.1, 0.145, 0.0, 7.7, 53.6}, {1, 4, 2.8, 1.46, 0.312, 0.041, 5.4, 29.5}, {2, 3, 3.05, 2.44, 0.327, 0.071, 4.6, 56.5}};
+constexpr double kQuantise = 4.5, kTwoAtLeast = 3.0 + kQuantise;
+
+double own_estimate(const OwnRule& r, int M, int N, int pitch, int in_dtype)
 {
-    if (a.N >= 16 * 1024) return launch_row_product<T, X, 1, 4, 8, 2>(a, s);
-    if (a.N >= 8 * 1024) return launch_row_product<T, X, 1, 2, 8, 4>(a, s);
-    return launch_row_product<T, X, 1, 1, 16, 4>(a, s);
+    const double groups = pieces_of(M, 16) * pieces_of(N, 16 * r.NB), on_a_cu = rounds_of(groups, 256.0), rounds = rounds_of(groups, 256.0 * r.resident);
+    const double values = std::min(M, 16) * (double)pitch * (in_dtype == kF32 ? 1.35e-3 : 1e-3);
+    return r.start + (rounds - 1.0) * r.round + rounds * r.each * values + (on_a_cu - 1.0) * r.more * values +
+           std::max((double)N * pitch / (r.weights * 1e6), on_a_cu * 16 * r.NB * pitch / (r.one * 1e3));
+}
+
+Choice choose(int M, int N, int pitch, int in_dtype)
+{
+    double least = 0.0, product;
+    int best = kTwoLaunches;
+    if (in_dtype != kI8 && (long long)std::min(M, 16) * pitch <= kOwnBytes) {
+        for (int k = 0; k < kOwns; ++k) {
+            const double us = own_estimate(kOwnRules[k], M, N, pitch, in_dtype);
+            if (k == 0 || us < least) {
+                best = k;
+                least = us;
+            }
+        }
+        if (least <= kTwoAtLeast) return {(Own)best, kKernels};      // (no product takes less than 3 us)
+    }
+    const Kernel kernel = choose(M, N, pitch, product);
+    if (best != kTwoLaunches && least <= product + kQuantise) return {(Own)best, kKernels};
+    return {kTwoLaunches, kernel};
+}
+
+template <class T, class X>
+int launch_own(Own kernel, const Int8Args& a, hipStream_t s)
+{
+    switch (kernel) {
+        case kOwn16: return launch_row_product<T, X, 1, 1, 16, 4>(a, s);
+        case kOwn4: return launch_row_product<T, X, 1, 1, 4, 2>(a, s);
+        default: return launch_row_product<T, X, 1, 2, 4, 2>(a, s);
+    }
 }
 
 template <class T>
-int launch_own(int in_dtype, const Int8Args& a, hipStream_t s)
+int launch_own(Own kernel, int in_dtype, const Int8Args& a, hipStream_t s)
 {
-    if (in_dtype == kF32) return launch_own<T, float>(a, s);
-    if (in_dtype == kF16) return launch_own<T, _Float16>(a, s);
-    return launch_own<T, __bf16>(a, s);
+    if (in_dtype == kF32) return launch_own<T, float>(kernel, a, s);
+    if (in_dtype == kF16) return launch_own<T, _Float16>(kernel, a, s);
+    return launch_own<T, __bf16>(kernel, a, s);
 }
 
 }  // namespace
@@ -735,12 +784,18 @@ int launch_int8_quantize(int dtype, const void* x, int8_t* q, float* scale, int 
     return launch_quantize<__bf16>(x, q, scale, rows, K, ldx, s);
 }
 
-int int8_kernel(int M, int N, int K) { return choose(M, N, (K + 127) / 128 * 128); }
+int int8_kernel(int M, int N, int K) { return choose(M, N, (K + 127) / 128 * 128, kI8).product; }
+
+int int8_own_kernel(int M, int N, int K, int in_dtype)
+{
+    const Own own = choose(M, N, (K + 127) / 128 * 128, in_dtype).own;
+    return own == kTwoLaunches ? -1 : own;
+}
 
 // The quantised input, then its scales.
-long long int8_workspace(int M, int, int K, int in_dtype, int)
+long long int8_workspace(int M, int N, int K, int in_dtype, int)
 {
-    if (in_dtype == kI8 || quantises_itself(M, (K + 127) / 128 * 128)) return 0;
+    if (in_dtype == kI8 || int8_own_kernel(M, N, K, in_dtype) >= 0) return 0;
     return (long long)M * ((K + 127) / 128 * 128) + (M * 4ll + 15) / 16 * 16;
 }
 
@@ -748,10 +803,11 @@ int launch_int8_linear(int in_dtype, int out_dtype, const Int8Args& given, char*
 {
     const hipStream_t s = static_cast<hipStream_t>(stream);
     Int8Args a = given;
-    if (in_dtype != kI8 && quantises_itself(a.M, a.pitch)) {
-        if (out_dtype == kF32) return launch_own<float>(in_dtype, a, s);
-        if (out_dtype == kF16) return launch_own<_Float16>(in_dtype, a, s);
-        return launch_own<__bf16>(in_dtype, a, s);
+    const Choice choice = choose(a.M, a.N, a.pitch, in_dtype);
+    if (choice.own != kTwoLaunches) {
+        if (out_dtype == kF32) return launch_own<float>(choice.own, in_dtype, a, s);
+        if (out_dtype == kF16) return launch_own<_Float16>(choice.own, in_dtype, a, s);
+        return launch_own<__bf16>(choice.own, in_dtype, a, s);
     }
     if (in_dtype != kI8) {
         int8_t* q = reinterpret_cast<int8_t*>(workspace);
@@ -761,9 +817,9 @@ int launch_int8_linear(int in_dtype, int out_dtype, const Int8Args& given, char*
         a.x = q;
         a.x_scale = scale;
     }
-    if (out_dtype == kF32) return launch_product<float>(a, s);
-    if (out_dtype == kF16) return launch_product<_Float16>(a, s);
-    return launch_product<__bf16>(a, s);
+    if (out_dtype == kF32) return launch_product<float>(choice.product, a, s);
+    if (out_dtype == kF16) return launch_product<_Float16>(choice.product, a, s);
+    return launch_product<__bf16>(choice.product, a, s);
 }
 
 }  // namespace sc

@@ -47,6 +47,7 @@ struct Int8Args {
     bool relu;
 };
 int int8_kernel(int M, int N, int K);      // number of the kernel that multiplies (for tests: all are to be reached)
+int int8_own_kernel(int M, int N, int K, int in_dtype);      // of the kernel that quantises its input itself, or -1: a launch does that before
 long long int8_workspace(int M, int N, int K, int in_dtype, int out_dtype);
 int launch_int8_linear(int in_dtype, int out_dtype, const Int8Args& a, char* workspace, void* stream);
 

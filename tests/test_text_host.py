@@ -110,6 +110,21 @@ def test_every_product_kernel_has_a_layer_in_the_tests():
     assert any(m * n > 256 for m, n in [(-(-M // 256), -(-N // 256)) for M, _, N in reached[7]])      # a workgroup takes several tiles
 
 
+def test_every_kernel_that_quantises_has_a_layer_in_the_tests():
+    from test_gpu_text import LAYERS
+    choice = LIB["_ZN2sc15int8_own_kernelEiiii"]        # sc::int8_own_kernel(M, N, K, in_dtype)
+    choice.argtypes = [C.c_int] * 4
+    n = C.c_longlong()
+    for dtype in (B.SC_F32, B.SC_F16, B.SC_BF16):
+        reached = {}
+        for M, K, N in LAYERS:
+            kernel = choice(M, N, K, dtype)
+            reached.setdefault(kernel, []).append(M)
+            assert LIB.sparse_conv_int8_linear_workspace(M, N, K, dtype, dtype, C.byref(n)) == B.SC_OK and (n.value > 0) == (kernel < 0)
+        assert set(reached) == {-1, 0, 1, 2}, reached
+        assert all(min(reached[k]) <= 16 < max(reached[k]) for k in (0, 1, 2)), reached
+
+
 def test_tensor_calls_refuse_before_they_touch_anything():
     """The compiled side of text.py, given what is no CUDA tensor, no tensor, too few arguments."""
     import torch
