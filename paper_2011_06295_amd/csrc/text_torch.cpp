@@ -44,6 +44,10 @@ const at::Tensor& tensor(PyObject* o, const char* what)
 // A status other than SC_OK goes back as a number (text.py raises the library's error from it).
 PyObject* result(int rc, const at::Tensor& out) { return rc == SC_OK ? THPVariable_Wrap(out) : PyLong_FromLong(rc); }
 
+// Scratch memory of the current device and stream (text.py calls with the tensors' device as the current one), as at::empty gets it, but
+// without a tensor around it.
+c10::DataPtr workspace(long long bytes) { return bytes > 0 ? c10::GetAllocator(c10::DeviceType::CUDA)->allocate((size_t)bytes) : c10::DataPtr(); }
+
 // The truth of an argument.
 bool is_true(PyObject* o)
 {
@@ -181,12 +185,11 @@ PyObject* py_embed_backward(PyObject*, PyObject* const* args, Py_ssize_t count)
         const unsigned flags = s.flags | (accumulate ? SC_EMBED_ACCUMULATE : 0u);
         long long bytes = 0;
         int rc = embed_backward_workspace(table.size(0), (int)table.size(1), s.count, s.words, g, flags, &bytes);
-        at::Tensor work;
-        if (rc == SC_OK && bytes > 0) work = at::empty({bytes}, table.options().dtype(at::kByte).requires_grad(false));
+        const c10::DataPtr work = rc == SC_OK ? workspace(bytes) : c10::DataPtr();
         if (rc == SC_OK)
             rc = embed_backward(grad.data_ptr(), tokens.data_ptr(), out.data_ptr(), table.size(0), (int)table.size(1), s.count, s.words, g,
                                 type_of(out.scalar_type()), (float)PyFloat_AS_DOUBLE(args[6]), PyLong_AsLongLong(args[7]), flags,
-                                bytes > 0 ? work.data_ptr() : nullptr, bytes, PyLong_AsVoidPtr(args[8]));
+                                work.get(), bytes, PyLong_AsVoidPtr(args[8]));
         return result(rc, out);
     });
 }
@@ -254,12 +257,11 @@ PyObject* py_linear(PyObject*, PyObject* const* args, Py_ssize_t count)
         const int o = type_of(out.scalar_type());
         long long bytes = 0;
         int rc = int8_linear_workspace((int)M, (int)N, (int)K, in, o, &bytes);
-        at::Tensor work;
-        if (rc == SC_OK && bytes > 0) work = at::empty({bytes}, weight.options());
+        const c10::DataPtr work = rc == SC_OK ? workspace(bytes) : c10::DataPtr();
         if (rc == SC_OK)
             rc = int8_linear(x.data_ptr(), x_scale, static_cast<const signed char*>(weight.data_ptr()), w_scale.data_ptr<float>(),
                              args[4] == Py_None ? nullptr : THPVariable_Unpack(args[4]).data_ptr<float>(), out.data_ptr(), (int)M, (int)N, (int)K, ldx, ldo,
-                             in, o, is_true(args[6]) ? SC_EPILOGUE_RELU : 0u, bytes > 0 ? work.data_ptr() : nullptr, bytes, PyLong_AsVoidPtr(args[9]));
+                             in, o, is_true(args[6]) ? SC_EPILOGUE_RELU : 0u, work.get(), bytes, PyLong_AsVoidPtr(args[9]));
         return result(rc, out);
     });
 }
