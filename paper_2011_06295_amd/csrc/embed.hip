@@ -586,7 +586,7 @@ struct Sorted {
 
 constexpr int kFewTokens = 8192, kBuckets = 256, kBucketBits = 8, kBucketDigit = 9, kMarks = 1 << 15;
 constexpr int kFewEach = kFewTokens / kSortThreads;
-constexpr unsigned long long kOwnZeros = 32ull << 20;
+constexpr unsigned long long kOwnZeros = 64ull << 20;
 constexpr unsigned kPairs = 256;
 constexpr int kFewBits = 13;
 constexpr int kFewAhead = 10;      // rows that a wavefront has in flight (as registers go)
@@ -618,7 +618,7 @@ __device__ __forceinline__ unsigned sort_bucket(const TokenArgs& a, unsigned buc
     unsigned key[kFewEach], place[kFewEach];
     unsigned long long mine[kFewEach];
     int count = 0, before = 0;
-    // All loads before the first use.  Of 64 tokens one in four has a token of this workgroup's, so the others get one look at their low
+    // All loads before the first use.  Most groups of 64 tokens have none of this workgroup's and get one look at their low
     // bits.  Code that a size has no use for is jumped over (it would be fetched).
     auto look = [&](auto* from) {
         typename std::remove_const<typename std::remove_pointer<decltype(from)>::type>::type token[kFewEach];
@@ -777,10 +777,11 @@ __global__ __launch_bounds__(kSortThreads, 8) void lists_kernel(TokenArgs a, Tur
 
 // Workgroup (b, y) owns the rows of the table whose number ends in b (kBuckets of them: frequent tokens are often neighbours), and
 // column blocks y, y + shares, ...  It takes the sorted tokens of its rows from the launch before, or looks through all tokens and sorts
-// them itself, sets the rows without any to zero (`zeros`; a launch before does that at a higher rate, so beyond kOwnZeros bytes
-// there is one) and deals the sorted tokens out to its wavefronts evenly.  Latency bounds it, and the instructions that it fetches:
-// 9.0 us at 8192 tokens of 20000 x 300 with the fullest workgroup's 148 tokens sorted before (the launch before takes 10.1, 8.1 without the
-// sort; sorting here took 3.9); 37 tokens of 8192 x 128 5.2 us a call, the launch included.
+// them itself, sets the rows without any to zero (`zeros`; beyond kOwnZeros bytes a launch before does that, in order: 60000 x 250 floats
+// 13.9 us a call here and 14.7 there, 100000 x 250, whose rows share cache lines, 31.6 and 22.9) and deals the sorted tokens out to its
+// wavefronts evenly.  Latency bounds it, and the instructions that it fetches: 9.0 us at 8192 tokens of 20000 x 300 with the fullest
+// workgroup's 148 tokens sorted before (the launch before takes 10.1, 8.1 without the sort; sorting here took 3.9); 37 tokens of
+// 8192 x 128 5.2 us a call, the launch included.
 template <class G, class W>
 __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, const G* grad, Lists* lists, short passes, short digit_bits, int column_blocks, int shares, bool zeros)
 {

@@ -194,7 +194,8 @@ def test_gradient_against_differences():
 
 LARGE_TABLES = [  # tokens, vocab, dim, types: rows past what a workgroup marks, keys of three digits, past 27 bits, zeros in a launch of their own
     (500, 9_000_001, 3, ("f32", "f32")), (20_000, 3_000_001, 2, ("bf16", "f32")), (700, 140_000_003, 1, ("f16", "f16")), (9000, 70_001, 130, ("f32", "f32")),
-    (3000, 70_001, 130, ("f32", "f32")), (40_000, 1500, 700, ("f16", "f32"))]
+    (3000, 70_001, 130, ("f32", "f32")), (40_000, 1500, 700, ("f16", "f32")), (3000, 70_001, 260, ("f32", "f32")),
+    (3000, 70_001, 260, ("f16", "f16"))]
 
 
 @pytest.mark.parametrize("case", LARGE_TABLES)
