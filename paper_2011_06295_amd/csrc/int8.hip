@@ -631,9 +631,9 @@ int launch_row_product(const Int8Args& a, hipStream_t s)
 
 // Microseconds that a product is estimated to take.  The constants are fitted to launches of 20 sizes of M by 16 of K and N (1 to
 // 8192 tokens, K 128 to 16384, N 10 to 16384, weights that do not stay in a cache), each to what is near the fastest there: over
-// these the kernel of the least estimate takes 1.3 % more than the fastest one, 16 % at most.  Depth pays where a CU has a tile or two
-// (64 x 64 at 256 x 4096 -> 4096: 14.5 us by two steps, 10.0 by four), two steps where workgroups that share a CU hide each other's waits
-// (128 x 128 at 2048 x 4096 -> 4096: 32.7 by two, 35.2 by three).
+// these the kernel of the least estimate takes 1.0 % more than the fastest one, 26 % at most
+// (512 x 16384 -> 512).  Depth pays where a CU has a tile or two (64 x 64 at 256 x 4096 -> 4096: 14.5 us by two steps, 10.0 by four),
+// two steps where workgroups that share a CU hide each other's waits (128 x 128 at 2048 x 4096 -> 4096: 32.7 by two, 35.2 by three).
 
 // Pieces of `size` (a power of two) that n is cut into.  (The host looks at 14 kernels a call: 0.1 us without divisions of 64 bits, 0.25 with.)
 double pieces_of(int n, int size) { return (double)(((unsigned)n + (unsigned)size - 1) >> __builtin_ctz((unsigned)size)); }
@@ -641,22 +641,22 @@ double rounds_of(double groups, double held) { return (double)(long long)((group
 
 enum Kernel { kRow11, kRow21, kRow22, kRow41, kRow42, kTile22, kTile44, kTile88, kDeep22, kDeep42, kDeep44, kKernels };
 
-// Row kernel: a launch, the sums of the wavefronts and the further rounds of workgroups, then the largest of what all workgroups load,
-// what those of one CU load in turn, and the weights.
+// Row kernel: a launch, the sums of the wavefronts and the further workgroups of a CU, then the largest of what all workgroups load,
+// what those of one CU load, and the weights.
 struct RowRule {
-    int MB, NB, resident;            // blocks; workgroups that the chip holds at a time
-    double join, round;              // us
+    int MB, NB;                      // blocks
+    double join, more;               // us
     double all, one, weights;        // MB/us of all, KB/us of one, MB/us of the weights
 };
-constexpr RowRule kRowRules[] = {{1, 1, 256, 0.24, 1.34, 14.8, 137.0, 6.8}, {2, 1, 256, 0.17, 1.42, 20.3, 134.0, 5.9}, {2, 2, 512, 0.08, 2.23, 15.0, 139.0, 5.4},
-                                 {4, 1, 256, 0.32, 1.50, 24.3, 136.0, 4.7}, {4, 2, 256, 0.88, 1.58, 19.1, 134.0, 5.1}};
+constexpr RowRule kRowRules[] = {{1, 1, 0.36, 1.39, 21.1, 144.0, 7.2}, {2, 1, 0.24, 1.42, 22.5, 135.0, 6.0}, {2, 2, 0.12, 0.83, 19.2, 136.0, 5.6},
+                                 {4, 1, 0.33, 1.54, 24.6, 133.0, 4.75}, {4, 2, 0.91, 1.64, 19.8, 132.0, 5.05}};
 
 double row_estimate(const RowRule& r, int M, int N, int pitch)
 {
     const double groups = pieces_of(M, 16 * r.MB) * pieces_of(N, 16 * r.NB), bytes = 16.0 * (r.MB + r.NB) * pitch;
-    const double rounds = rounds_of(groups, r.resident);
-    const double load = std::max({groups * bytes / (r.all * 1e6), rounds * bytes / (r.one * 1e3), (double)N * pitch / (r.weights * 1e6)});
-    return 3.0 + r.join * rounds + r.round * (rounds - 1.0) + load;
+    const double on_a_cu = rounds_of(groups, 256.0);
+    const double load = std::max({groups * bytes / (r.all * 1e6), on_a_cu * bytes / (r.one * 1e3), (double)N * pitch / (r.weights * 1e6)});
+    return 3.0 + r.join * on_a_cu + r.more * (on_a_cu - 1.0) + load;
 }
 
 // Tile kernel: steps of `least` us while a workgroup has the CU to itself, `each` times the workgroups that share it beyond; the weights
@@ -666,8 +666,8 @@ struct TileRule {
     double least, each, start, finish;
     double weights;                  // MB/us
 };
-constexpr TileRule kTileRules[] = {{2, 2, 4, 0.261, 0.211, 0.2, 2.4, 3.5}, {4, 4, 2, 0.189, 0.448, 0.2, 3.9, 3.3}, {8, 8, 1, 0.94, 1.152, 1.4, 8.9, 2.2},
-                                   {2, 2, 2, 0.142, 0.192, 1.1, 1.9, 7.1}, {4, 2, 1, 0.0, 0.266, 1.1, 2.4, 6.6}, {4, 4, 1, 0.0, 0.397, 0.9, 3.2, 4.8}};
+constexpr TileRule kTileRules[] = {{2, 2, 4, 0.268, 0.213, 0.28, 2.35, 3.5}, {4, 4, 2, 0.063, 0.446, 0.40, 4.07, 3.2}, {8, 8, 1, 0.0, 1.16, 2.66, 9.15, 6.7},
+                                   {2, 2, 2, 0.049, 0.194, 1.20, 1.90, 7.0}, {4, 2, 1, 0.0, 0.271, 1.12, 2.48, 6.6}, {4, 4, 1, 0.0, 0.396, 0.99, 3.39, 4.7}};
 
 double tile_estimate(const TileRule& r, int M, int N, int pitch)
 {

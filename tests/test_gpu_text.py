@@ -341,7 +341,8 @@ LAYERS = [  # M, K, N
     (100, 777, 100), (127, 512, 384), (128, 896, 255), (200, 1100, 190), (256, 256, 256), (257, 640, 513), (300, 2300, 640), (513, 200, 1025),
     (1000, 128, 8), (1025, 1030, 270), (2048, 64, 64), (250, 300, 300), (600, 1500, 700), (3616, 272, 33), (300, 1500, 1500),
     (601, 2000, 1003), (130, 100, 500), (603, 300, 5001), (954, 1429, 289), (521, 2, 7263), (2567, 171, 1569), (1, 1, 5251), (37, 131, 5257),
-    (44, 292, 5286), (583, 676, 601), (1006, 647, 1224), (2487, 414, 1226), (15, 416, 4177), (2, 256, 8200)]
+    (44, 292, 5286), (583, 676, 601), (1006, 647, 1224), (2487, 414, 1226), (15, 416, 4177), (2, 256, 8200), (183, 1100, 232), (946, 552, 264),
+    (906, 903, 1203)]
 
 
 LARGE_LAYERS = [(8100, 2000, 8150), (4300, 2900, 8333), (2048, 8192, 8192)]
