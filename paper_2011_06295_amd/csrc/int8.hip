@@ -169,16 +169,21 @@ __device__ __forceinline__ void each(F&& f) { each_of(f, std::make_integer_seque
 
 // 16 bytes a lane from memory to LDS at `lds` + 16 * lane; bytes past the descriptor's end arrive as zeros.  Not the builtin:
 // the compiler waits for every load of that kind before any later read of LDS, here the reads wait where they have to.
+// A load to LDS may read m0 one wait state after a scalar instruction wrote it at the earliest; the compiler adds none inside an asm block.
+// (It notes that it keeps m0 for itself, which it does not across an operation that needs it.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_to_lds(int4v descriptor, unsigned offset, unsigned base, unsigned lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" :: "s"(lds), "v"(offset), "s"(descriptor), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" :: "s"(lds), "v"(offset), "s"(descriptor), "s"(base) : "m0", "memory");
 }
 
 // The same, 4 bytes a lane.
 __device__ __forceinline__ void load_word_to_lds(int4v descriptor, unsigned offset, unsigned lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dword %1, %2, 0 offen lds" :: "s"(lds), "v"(offset), "s"(descriptor) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" :: "s"(lds), "v"(offset), "s"(descriptor) : "m0", "memory");
 }
+#pragma clang diagnostic pop
 
 __device__ __forceinline__ int4v descriptor_of(const void* p, long long bytes)
 {
