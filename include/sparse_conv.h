@@ -359,7 +359,8 @@ enum { SC_EMBED_CHANNELS_FIRST = 1u, SC_EMBED_TOKENS_64 = 2u, SC_EMBED_ACCUMULAT
  *   flags    0 or any of SC_EMBED_CHANNELS_FIRST, SC_EMBED_TOKENS_64.
  * The product with scale is formed in fp32 and rounded once.  sentences or words may be 0 (no-op).
  * SC_EINVAL: a null or misaligned pointer (to its own element size), vocab or dim below 1, a negative count, an unknown
- * type or flag.  SC_EUNSUPPORTED: vocab or sentences * words of 2^31 or more.
+ * type or flag.  SC_EUNSUPPORTED: vocab or sentences * words of 2^31 or more; what no launch can hold: an output of about 256 GB
+ * or more, or (channels first) 2^24 or more tiles, of 64 words of a sentence by 256 bytes of their vectors, each begun tile whole.
  */
 int sparse_conv_embed(const void* table, const void* tokens, void* out, long long vocab, int dim, int sentences, int words,
                       int dtype, float scale, unsigned flags, void* stream);
@@ -375,7 +376,8 @@ int sparse_conv_embed(const void* table, const void* tokens, void* out, long lon
  *   padding     a token whose row has no gradient (it adds to no row), or -1.
  *   workspace   of at least the bytes that sparse_conv_embed_backward_workspace reports for the same arguments.
  * Sums are formed in fp32, each row's in an order that depends on the tokens alone, and rounded once: the same
- * arguments give the same bits.  Status codes as for sparse_conv_embed; SC_EINVAL for a workspace that is too small.
+ * arguments give the same bits.  Status codes as for sparse_conv_embed; SC_EINVAL for a workspace that is too small;
+ * SC_EUNSUPPORTED for 2^23 or more tiles (channels first) and for sentences * words * (dim / 512, rounded up) of about 2^29 or more.
  */
 int sparse_conv_embed_backward_workspace(long long vocab, int dim, int sentences, int words, int grad_dtype, unsigned flags,
                                          long long* bytes);

@@ -174,14 +174,14 @@ int launch_lookup(const EmbedArgs& a, hipStream_t s)
     if (a.channels_first && a.words > 1) {
         typedef Turn<T> U;
         const long long tiles = (long long)a.sentences * ((a.words + U::kWords - 1) / U::kWords) * ((a.dim + U::kDims - 1) / U::kDims);
-        if (tiles >= (1ll << 31)) return (int)hipErrorInvalidValue;
+        if ((unsigned long long)tiles > most_groups(kThreads)) return kTooLarge;
         hipLaunchKernelGGL(embed_turned_kernel<T>, dim3((unsigned)tiles), dim3(kThreads), 0, s, a);
         return (int)hipGetLastError();
     }
     constexpr int kVec = 16 / sizeof(T);
     const unsigned per_row = a.dim >= kVec ? (a.dim + kVec - 1) / kVec : a.dim;
     const unsigned long long pieces = (unsigned long long)a.sentences * a.words * per_row, blocks = (pieces + 4 * kThreads - 1) / (4 * kThreads);
-    if (blocks >= (1ull << 31)) return (int)hipErrorInvalidValue;
+    if (blocks > most_groups(kThreads)) return kTooLarge;
     const bool passing = pieces * 16 > kCacheBytes;
     auto kernel = a.dim < kVec ? embed_rows_kernel<T, 1, false> : passing ? embed_rows_kernel<T, kVec, true> : embed_rows_kernel<T, kVec, false>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kThreads), 0, s, a, per_row, pieces);
@@ -1068,6 +1068,29 @@ Parts parts_of(const EmbedGradArgs& a, int grad_dtype)
     return p;
 }
 
+template <class W>
+__global__ __launch_bounds__(kSortThreads) void zero_kernel(Fill fill)
+{
+    fill_part<W>(fill, blockIdx.x);
+}
+
+// Elements that one launch sets to zero at most (16 GB).
+template <class W>
+constexpr unsigned long long kFillAtOnce = (1ull << 20) * kSortThreads * (16 / sizeof(W));
+
+// Sets all but at most `left` of `count` elements to zero, in launches of their own; returns how many.
+template <class W>
+unsigned long long set_ahead(void* to, unsigned long long count, unsigned long long left, hipStream_t s)
+{
+    unsigned long long done = 0;
+    while (count - done > left) {
+        const Fill fill{static_cast<W*>(to) + done, std::min(count - done, kFillAtOnce<W>)};
+        hipLaunchKernelGGL(zero_kernel<W>, dim3((unsigned)blocks_of<W>(0, fill)), dim3(kSortThreads), 0, s, fill);
+        done += fill.count;
+    }
+    return done;
+}
+
 template <class G, class W>
 int launch_grad(const EmbedGradArgs& a, const Parts& parts, char* workspace, hipStream_t s)
 {
@@ -1078,20 +1101,20 @@ int launch_grad(const EmbedGradArgs& a, const Parts& parts, char* workspace, hip
     if (parts.rows) {
         typedef Turn<G> U;
         tiles = (long long)a.sentences * ((a.words + U::kWords - 1) / U::kWords) * ((a.dim + U::kDims - 1) / U::kDims);
-        if (tiles >= (1ll << 30)) return (int)hipErrorInvalidValue;
         grad = rows;
     }
     const unsigned long long elements = a.accumulate ? 0 : (unsigned long long)a.vocab * a.dim;
+    if (tiles >= (1ll << 23)) return kTooLarge;        // (turned, set to zero and sorted in one launch: 2^21, 2^20 and, below, at most 2^18 workgroups)
     const TurnArgs turn{a.grad, rows, a.dim, a.sentences, a.words, (unsigned)tiles};
     if (tokens <= kFewTokens) {
         const bool zeros = !a.accumulate && !tiles && sets_own_zeros(a, sizeof(W));
-        const Fill fill{a.table_grad, zeros ? 0 : elements};
         const unsigned groups = (unsigned)std::min<long long>(a.vocab, kBuckets);
         const unsigned shares = (unsigned)std::min<long long>(column_blocks, kBuckets / groups);      // of the column blocks: a workgroup a CU
         Lists* lists = nullptr;
-        if (tiles || fill.count) {
+        if (tiles || (elements && !zeros)) {
+            const unsigned long long filled = set_ahead<W>(a.table_grad, elements, kFillAtOnce<W>, s);
+            const Fill fill{static_cast<W*>(a.table_grad) + filled, elements - filled};
             const unsigned long long blocks = groups + blocks_of<W>(turn.tiles, fill);
-            if (blocks >= (1ull << 31)) return (int)hipErrorInvalidValue;
             const TokenArgs named{a.tokens, a.vocab, a.padding, (unsigned)tokens, a.wide};
             const SortPlan plan = sort_plan((a.vocab - 1) >> kBucketBits, kListDigit, tokens);
             lists = reinterpret_cast<Lists*>(workspace + parts.rows);
@@ -1105,7 +1128,9 @@ int launch_grad(const EmbedGradArgs& a, const Parts& parts, char* workspace, hip
     }
     const SortPlan plan = sort_plan(a.vocab, kMaxDigit, tokens);
     const long long run_blocks = ((tokens + kRunWaves * kSlot - 1) / (kRunWaves * kSlot)) * column_blocks;
-    if (run_blocks >= (1ll << 31)) return (int)hipErrorInvalidValue;
+    constexpr int kWaves = kThreads / 64;
+    const long long window_blocks = (tokens / kWindow * column_blocks + kWaves - 1) / kWaves;
+    if ((unsigned long long)run_blocks > most_groups(kRunThreads) || (unsigned long long)window_blocks > most_groups(kThreads)) return kTooLarge;
     char* at = workspace + parts.rows;
     Sorted sorted[2];
     for (int i = 0; i < 2; ++i) {
@@ -1118,14 +1143,14 @@ int launch_grad(const EmbedGradArgs& a, const Parts& parts, char* workspace, hip
     Sorted from{nullptr, nullptr};
     const TokenArgs named{a.tokens, a.vocab, a.padding, (unsigned)tokens, a.wide};
     const int launches = 2 * plan.passes;
-    unsigned long long filled = 0;
+    const unsigned long long ahead = set_ahead<W>(a.table_grad, elements, launches * kFillAtOnce<W>, s);
+    unsigned long long filled = ahead;
     for (int l = 0; l < launches; ++l) {
-        const unsigned long long kVec = 16 / sizeof(W), end = l + 1 == launches ? elements : elements * (l + 1) / launches / kVec * kVec;
+        const unsigned long long kVec = 16 / sizeof(W), end = l + 1 == launches ? elements : ahead + (elements - ahead) * (l + 1) / launches / kVec * kVec;
         const Fill fill{static_cast<W*>(a.table_grad) + filled, end - filled};
         filled = end;
         const short shift = (short)(l / 2 * plan.digit), bits = (short)plan.digit;
         const unsigned long long blocks = plan.groups + blocks_of<W>(l == 0 ? turn.tiles : 0, fill);
-        if (blocks >= (1ull << 31)) return (int)hipErrorInvalidValue;
         if (l % 2 == 0) {
             TurnArgs here = turn;
             if (l > 0) here.tiles = 0;
@@ -1135,28 +1160,8 @@ int launch_grad(const EmbedGradArgs& a, const Parts& parts, char* workspace, hip
             from = sorted[l / 2 & 1];
         }
     }
-    constexpr int kWaves = kThreads / 64;
-    const long long window_blocks = (tokens / kWindow * column_blocks + kWaves - 1) / kWaves;
-    if (window_blocks >= (1ll << 31)) return (int)hipErrorInvalidValue;
     hipLaunchKernelGGL(window_kernel<G>, dim3((unsigned)window_blocks), dim3(kThreads), 0, s, a, grad, from, windows, (int)column_blocks);
     hipLaunchKernelGGL((runs_kernel<G, W>), dim3((unsigned)run_blocks), dim3(kRunThreads), 0, s, a, grad, from, static_cast<const float*>(windows), (int)column_blocks);
-    return (int)hipGetLastError();
-}
-
-// No tokens: all rows are zero.
-template <class W>
-__global__ __launch_bounds__(kSortThreads) void zero_kernel(Fill fill)
-{
-    fill_part<W>(fill, blockIdx.x);
-}
-
-template <class W>
-int launch_zero(const EmbedGradArgs& a, hipStream_t s)
-{
-    const Fill fill{a.table_grad, (unsigned long long)a.vocab * a.dim};
-    const unsigned long long blocks = blocks_of<W>(0, fill);
-    if (blocks >= (1ull << 31)) return (int)hipErrorInvalidValue;
-    hipLaunchKernelGGL(zero_kernel<W>, dim3((unsigned)blocks), dim3(kSortThreads), 0, s, fill);
     return (int)hipGetLastError();
 }
 
@@ -1175,7 +1180,12 @@ long long embed_grad_workspace(const EmbedGradArgs& a, int grad_dtype) { return 
 int launch_embed_grad(int grad_dtype, int table_dtype, const EmbedGradArgs& a, char* workspace, void* stream)
 {
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    if ((long long)a.sentences * a.words == 0) return table_dtype == kF32 ? launch_zero<float>(a, s) : launch_zero<_Float16>(a, s);      // (zeros of 16 bits)
+    if ((long long)a.sentences * a.words == 0) {       // all rows are zero
+        const unsigned long long elements = (unsigned long long)a.vocab * a.dim;
+        if (table_dtype == kF32) set_ahead<float>(a.table_grad, elements, 0, s);
+        else set_ahead<_Float16>(a.table_grad, elements, 0, s);      // (zeros of 16 bits)
+        return (int)hipGetLastError();
+    }
     const Parts parts = parts_of(a, grad_dtype);
     if (grad_dtype == kF32) return launch_grad<float, float>(a, parts, workspace, s);
     if (grad_dtype == kF16) return table_dtype == kF32 ? launch_grad<_Float16, float>(a, parts, workspace, s) : launch_grad<_Float16, _Float16>(a, parts, workspace, s);

@@ -447,8 +447,9 @@ template <class T, int MB, int NB, int WM, int WN, int S>
 int launch_tile_product(const Int8Args& a, hipStream_t s)
 {
     const long long tiles = ((a.M + 16ll * MB * WM - 1) / (16 * MB * WM)) * ((a.N + 16ll * NB * WN - 1) / (16 * NB * WN));
-    if (tiles >= (1ll << 31)) return (int)hipErrorInvalidValue;
-    const unsigned blocks = kWalks<MB, NB> && a.pitch >= 128 * kWalkSteps ? (unsigned)std::min(tiles, 256ll) : (unsigned)tiles;
+    const bool walks = kWalks<MB, NB> && a.pitch >= 128 * kWalkSteps;
+    if (tiles >= (1ll << 31) || (!walks && (unsigned long long)tiles > most_groups(64 * WM * WN))) return kTooLarge;
+    const unsigned blocks = walks ? (unsigned)std::min(tiles, 256ll) : (unsigned)tiles;
     hipLaunchKernelGGL((tile_product_kernel<T, MB, NB, WM, WN, S>), dim3(blocks), dim3(64 * WM * WN), 0, s, a, (unsigned)tiles, blocks);
     return (int)hipGetLastError();
 }
@@ -627,7 +628,7 @@ template <class T, class X, int MB, int NB, int W, int D>
 int launch_row_product(const Int8Args& a, hipStream_t s)
 {
     const long long groups = ((a.M + 16ll * MB - 1) / (16 * MB)) * ((a.N + 16ll * NB - 1) / (16 * NB));
-    if (groups >= (1ll << 31)) return (int)hipErrorInvalidValue;
+    if ((unsigned long long)groups > most_groups(64 * W)) return kTooLarge;
     hipLaunchKernelGGL((row_product_kernel<T, X, MB, NB, W, D>), dim3((unsigned)groups), dim3(64 * W), 0, s, a);
     return (int)hipGetLastError();
 }

@@ -43,6 +43,8 @@ int check_int8(int M, int N, int K, int in_dtype, int out_dtype)
     return SC_OK;
 }
 
+int status(int launched) { return launched == 0 ? SC_OK : launched == sc::kTooLarge ? SC_EUNSUPPORTED : SC_EHIP; }
+
 }  // namespace
 
 extern "C" {
@@ -60,7 +62,7 @@ int sparse_conv_embed(const void* table, const void* tokens, void* out, long lon
     if (overlap(out, out_bytes, table, vocab * dim * b) || overlap(out, out_bytes, tokens, count * tb)) return SC_EINVAL;
     const sc::EmbedArgs a{table, tokens, out, vocab, dim, sentences, words, scale,
                           (flags & SC_EMBED_CHANNELS_FIRST) != 0, (flags & SC_EMBED_TOKENS_64) != 0};
-    return sc::launch_embed(dtype, a, stream) == 0 ? SC_OK : SC_EHIP;
+    return status(sc::launch_embed(dtype, a, stream));
 }
 
 int sparse_conv_embed_backward_workspace(long long vocab, int dim, int sentences, int words, int grad_dtype, unsigned flags,
@@ -100,7 +102,7 @@ int sparse_conv_embed_backward(const void* grad, const void* tokens, void* table
     } else if (flags & SC_EMBED_ACCUMULATE) {
         return SC_OK;
     }
-    return sc::launch_embed_grad(grad_dtype, table_dtype, a, static_cast<char*>(workspace), stream) == 0 ? SC_OK : SC_EHIP;
+    return status(sc::launch_embed_grad(grad_dtype, table_dtype, a, static_cast<char*>(workspace), stream));
 }
 
 int sparse_conv_int8_quantize(const void* x, signed char* q, float* scale, int rows, int K, long long ldx, int dtype, void* stream)
@@ -112,7 +114,7 @@ int sparse_conv_int8_quantize(const void* x, signed char* q, float* scale, int r
     if (!x || !q || !scale || !aligned(x, b) || !aligned(q, 16) || !aligned(scale, 4)) return SC_EINVAL;
     const long long x_bytes = ((rows - 1ll) * ldx + K) * b, q_bytes = rows * SC_INT8_PITCH(K);
     if (overlap(x, x_bytes, q, q_bytes) || overlap(x, x_bytes, scale, rows * 4ll) || overlap(q, q_bytes, scale, rows * 4ll)) return SC_EINVAL;
-    return sc::launch_int8_quantize(dtype, x, reinterpret_cast<int8_t*>(q), scale, rows, K, ldx, stream) == 0 ? SC_OK : SC_EHIP;
+    return status(sc::launch_int8_quantize(dtype, x, reinterpret_cast<int8_t*>(q), scale, rows, K, ldx, stream));
 }
 
 int sparse_conv_int8_linear_workspace(int M, int N, int K, int in_dtype, int out_dtype, long long* bytes)
@@ -146,7 +148,7 @@ int sparse_conv_int8_linear(const void* x, const float* x_scale, const signed ch
         return SC_EINVAL;
     const sc::Int8Args a{x, x_scale, reinterpret_cast<const int8_t*>(w), w_scale, bias, out, M, N, K, (int)pitch, ldx, ldo,
                          (flags & SC_EPILOGUE_RELU) != 0};
-    return sc::launch_int8_linear(in_dtype, out_dtype, a, static_cast<char*>(workspace), stream) == 0 ? SC_OK : SC_EHIP;
+    return status(sc::launch_int8_linear(in_dtype, out_dtype, a, static_cast<char*>(workspace), stream));
 }
 
 }  // extern "C"

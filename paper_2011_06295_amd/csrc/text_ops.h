@@ -9,6 +9,11 @@ namespace sc {
 // (A launch whose arguments take more than 112 bytes, the block counts of the grid among them where a kernel asks for them, keeps the
 // host 3.5 us instead of 2.75: the structures below hold what the kernels need and nothing else.)
 
+// A launch counts its threads in 32 bits, and cuts off what is above that without an error: the workgroups that it can have.
+constexpr unsigned long long most_groups(int threads) { return 0xffffffffull / (unsigned)threads; }
+// What a launch function returns, with nothing enqueued, for sizes past that (else 0, or the HIP error).
+constexpr int kTooLarge = -1;
+
 struct EmbedArgs {
     const void* table;     // [vocab][dim]
     const void* tokens;    // [sentences][words]

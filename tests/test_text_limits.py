@@ -1,0 +1,20 @@
+"""Sizes at the ends of what the text model's entry points take (no kernel is launched: every call is refused)."""
+import pytest
+
+from paper_2011_06295_amd import binding as B
+
+LIB = B.raw_library()
+A, X, Y, W = 1 << 42, 1 << 43, 1 << 44, 1 << 46        # addresses that are never read
+
+
+@pytest.mark.parametrize("n, t, dim, dtype, flags", [
+    (1 << 25, 2, 1, B.SC_F32, B.SC_EMBED_CHANNELS_FIRST), (1 << 23, 65, 1, B.SC_F16, B.SC_EMBED_CHANNELS_FIRST), (1 << 21, 2, 513, B.SC_F32, B.SC_EMBED_CHANNELS_FIRST),
+    (1, (1 << 31) - 1, 64, B.SC_F16, 0), (1 << 15, (1 << 16) - 1, 36, B.SC_F32, 0)])
+def test_lookup_of_more_than_a_launch_holds_is_refused(n, t, dim, dtype, flags):
+    assert LIB.sparse_conv_embed(A, X, Y, 1000, dim, n, t, dtype, 1.0, flags, None) == B.SC_EUNSUPPORTED
+
+
+@pytest.mark.parametrize("n, t, dim, flags", [
+    (1 << 25, 2, 1, B.SC_EMBED_CHANNELS_FIRST), (1 << 30, 1, 1, 0), (1 << 27, 4, 16, 0), (1 << 25, 8, 513, 0), (1 << 25, 8, 513, B.SC_EMBED_ACCUMULATE)])
+def test_gradient_of_more_than_a_launch_holds_is_refused(n, t, dim, flags):
+    assert LIB.sparse_conv_embed_backward(A, X, Y, 1000, dim, n, t, B.SC_F32, B.SC_F32, 1.0, -1, flags, W, 1 << 46, None) == B.SC_EUNSUPPORTED
