@@ -489,10 +489,13 @@ unsigned long long blocks_of(unsigned tiles, const Fill& f)
 // A stable sort of (token, place) by the token, `digit` bits a pass from the lowest on.  Tokens that add to no row get the number
 // `vocab` and end up last.
 constexpr int kMaxDigit = 10, kMoveEach = 2;      // tokens of a thread
+// Every workgroup that moves tokens reads the counts of all, so that there is a most of them: work grows with the tokens, not their square.
+// (2^20 tokens to 131072 x 16: 211 us a call, by twice as many 264, by half 215; 2^24 to 131072 x 4: 3.1 ms, 3.1, 3.4.)
+constexpr int kMostGroups = 256;
 
 struct SortPlan {
     int passes, digit;      // bits a digit
-    int groups;             // workgroups
+    int groups, rounds;     // workgroups, and how many times kMoveEach * kSortThreads tokens in a row each takes
 };
 
 SortPlan sort_plan(long long last, int most, long long tokens)      // of keys 0 .. last, by digits of at most `most` bits
@@ -502,7 +505,9 @@ SortPlan sort_plan(long long last, int most, long long tokens)      // of keys 0
     SortPlan p;
     p.passes = (bits + most - 1) / most;
     p.digit = (bits + p.passes - 1) / p.passes;
-    p.groups = (int)((tokens + kMoveEach * kSortThreads - 1) / (kMoveEach * kSortThreads));
+    const long long runs = (tokens + kMoveEach * kSortThreads - 1) / (kMoveEach * kSortThreads);
+    p.rounds = (int)((runs + kMostGroups - 1) / kMostGroups);
+    p.groups = (int)((runs + p.rounds - 1) / p.rounds);
     return p;
 }
 
@@ -563,9 +568,9 @@ __device__ __forceinline__ int sum_before(int value, int* of_wave)
     return before;
 }
 
-// Turns the counts of a digit's wavefronts into where each begins, from `base` on.
+// Turns the counts of a digit's wavefronts into where each begins, from `base` on, and returns where the last ends.
 template <int BITS>
-__device__ __forceinline__ void spread(int (*of_wave)[1 << BITS], int digit, int base)
+__device__ __forceinline__ int spread(int (*of_wave)[1 << BITS], int digit, int base)
 {
     int n[kSortWaves];
 #pragma unroll
@@ -575,6 +580,7 @@ __device__ __forceinline__ void spread(int (*of_wave)[1 << BITS], int digit, int
         of_wave[w][digit] = base;
         base += n[w];
     }
+    return base;
 }
 
 struct Sorted {
@@ -888,7 +894,7 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(EmbedGradArgs a, c
 // A pass of the sort is two launches.  Each workgroup counts the digits of its run of tokens ...  (from: null in the first pass, which reads
 // the tokens.)
 template <class G, class W>
-__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(TokenArgs a, TurnArgs turn, Fill fill, const unsigned* from, int* counts, int groups, short shift, short bits)
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(TokenArgs a, TurnArgs turn, Fill fill, const unsigned* from, int* counts, int groups, short rounds, short shift, short bits)
 {
     __shared__ __attribute__((aligned(16))) int bins[tiles_room<G>() / 4];
     static_assert(sizeof(bins) >= sizeof(int) << kMaxDigit, "a count for each digit fits");
@@ -897,11 +903,12 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(TokenArgs a, T
         return;
     }
     const int size = 1 << bits;
-    const unsigned first = blockIdx.x * (unsigned)(kMoveEach * kSortThreads);
+    const int each = kMoveEach * rounds;
+    const unsigned first = blockIdx.x * (unsigned)(each * kSortThreads);
     for (int d = threadIdx.x; d < size; d += kSortThreads) bins[d] = 0;
     lds_barrier();
-    for (int i = 0; i < kMoveEach; ++i) {
-        const unsigned t = first + own_token(kMoveEach, i);
+    for (int i = 0; i < each; ++i) {
+        const unsigned t = first + own_token(each, i);
         if (t < a.count) atomicAdd(&bins[((from ? from[t] : sort_key(a, t)) >> shift) & (unsigned)(size - 1)], 1);
     }
     lds_barrier();
@@ -910,7 +917,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(TokenArgs a, T
 
 // ... then each finds, from the counts of all, where its tokens of each digit go, and takes them there in their order.
 template <class W>
-__global__ __launch_bounds__(kSortThreads) void sort_move_kernel(TokenArgs a, Fill fill, Sorted from, Sorted to, const int* counts, int groups, short shift, short bits)
+__global__ __launch_bounds__(kSortThreads) void sort_move_kernel(TokenArgs a, Fill fill, Sorted from, Sorted to, const int* counts, int groups, short rounds, short shift, short bits)
 {
     __shared__ int of_wave[kSortWaves][1 << kMaxDigit];
     __shared__ int wave_sums[kSortWaves];
@@ -920,17 +927,20 @@ __global__ __launch_bounds__(kSortThreads) void sort_move_kernel(TokenArgs a, Fi
     }
     constexpr int kEach = kMoveEach;
     const int wave = threadIdx.x >> 6, size = 1 << bits, digit = threadIdx.x;
-    const unsigned first = blockIdx.x * (unsigned)(kEach * kSortThreads);
+    unsigned first = blockIdx.x * (unsigned)(kEach * kSortThreads * rounds);
     unsigned key[kEach];
     int place[kEach], rank[kEach];
     bool there[kEach];
+    auto fetch = [&]() {
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        const unsigned t = first + own_token(kEach, i);
-        there[i] = t < a.count;
-        key[i] = !there[i] ? 0u : from.keys ? from.keys[t] : sort_key(a, t);
-        place[i] = !there[i] ? 0 : from.keys ? from.places[t] : (int)t;
-    }
+        for (int i = 0; i < kEach; ++i) {
+            const unsigned t = first + own_token(kEach, i);
+            there[i] = t < a.count;
+            key[i] = !there[i] ? 0u : from.keys ? from.keys[t] : sort_key(a, t);
+            place[i] = !there[i] ? 0 : from.keys ? from.places[t] : (int)t;
+        }
+    };
+    fetch();
     // where this workgroup's first token of `digit` goes: all smaller digits, then the same digit in the workgroups before
     int before = 0, total = 0;
     if (digit < size) {
@@ -951,17 +961,23 @@ __global__ __launch_bounds__(kSortThreads) void sort_move_kernel(TokenArgs a, Fi
             total += n;
         }
     }
-    rank_tokens<kEach, kMaxDigit>(key, there, kEach, shift, bits, of_wave, rank);
-    const int base = sum_before(total, wave_sums) + before;
-    if (digit < size) spread<kMaxDigit>(of_wave, digit, base);
-    lds_barrier();
+    int base = 0;
+    for (int round = 0; round < rounds; ++round) {
+        rank_tokens<kEach, kMaxDigit>(key, there, kEach, shift, bits, of_wave, rank);
+        if (round == 0) base = sum_before(total, wave_sums) + before;      // (waits for the counts of all wavefronts)
+        else lds_barrier();
+        if (digit < size) base = spread<kMaxDigit>(of_wave, digit, base);
+        lds_barrier();
 #pragma unroll
-    for (int i = 0; i < kEach; ++i)
-        if (there[i]) {
-            const int at = of_wave[wave][(key[i] >> shift) & (unsigned)(size - 1)] + rank[i];
-            to.keys[at] = key[i];
-            to.places[at] = place[i];
-        }
+        for (int i = 0; i < kEach; ++i)
+            if (there[i]) {
+                const int at = of_wave[wave][(key[i] >> shift) & (unsigned)(size - 1)] + rank[i];
+                to.keys[at] = key[i];
+                to.places[at] = place[i];
+            }
+        first += kEach * kSortThreads;
+        if (round + 1 < rounds) fetch();
+    }
 }
 
 // Sums of kWindow sorted tokens in a row, where they are of one row of the table.
@@ -1154,9 +1170,9 @@ int launch_grad(const EmbedGradArgs& a, const Parts& parts, char* workspace, hip
         if (l % 2 == 0) {
             TurnArgs here = turn;
             if (l > 0) here.tiles = 0;
-            hipLaunchKernelGGL((sort_count_kernel<G, W>), dim3((unsigned)blocks), dim3(kSortThreads), 0, s, named, here, fill, from.keys, counts, plan.groups, shift, bits);
+            hipLaunchKernelGGL((sort_count_kernel<G, W>), dim3((unsigned)blocks), dim3(kSortThreads), 0, s, named, here, fill, from.keys, counts, plan.groups, (short)plan.rounds, shift, bits);
         } else {
-            hipLaunchKernelGGL(sort_move_kernel<W>, dim3((unsigned)blocks), dim3(kSortThreads), 0, s, named, fill, from, sorted[l / 2 & 1], counts, plan.groups, shift, bits);
+            hipLaunchKernelGGL(sort_move_kernel<W>, dim3((unsigned)blocks), dim3(kSortThreads), 0, s, named, fill, from, sorted[l / 2 & 1], counts, plan.groups, (short)plan.rounds, shift, bits);
             from = sorted[l / 2 & 1];
         }
     }

@@ -1,4 +1,6 @@
 """Sizes at the ends of what the text model's entry points take (no kernel is launched: every call is refused)."""
+import ctypes as C
+
 import pytest
 
 from paper_2011_06295_amd import binding as B
@@ -18,3 +20,13 @@ def test_lookup_of_more_than_a_launch_holds_is_refused(n, t, dim, dtype, flags):
     (1 << 25, 2, 1, B.SC_EMBED_CHANNELS_FIRST), (1 << 30, 1, 1, 0), (1 << 27, 4, 16, 0), (1 << 25, 8, 513, 0), (1 << 25, 8, 513, B.SC_EMBED_ACCUMULATE)])
 def test_gradient_of_more_than_a_launch_holds_is_refused(n, t, dim, flags):
     assert LIB.sparse_conv_embed_backward(A, X, Y, 1000, dim, n, t, B.SC_F32, B.SC_F32, 1.0, -1, flags, W, 1 << 46, None) == B.SC_EUNSUPPORTED
+
+
+@pytest.mark.parametrize("tokens", [1 << 17, (1 << 20) + 3, 1 << 24, (1 << 29) - 64])
+@pytest.mark.parametrize("vocab", [9, 1000, 131072, (1 << 31) - 1])
+def test_scratch_memory_of_the_sort_grows_with_the_tokens(tokens, vocab):
+    """Keys and places twice, a window of sums for 32 tokens, and counts of a bounded number of workgroups (of 1024 digits at most), for
+    every workgroup reads them all."""
+    n = C.c_longlong(-1)
+    assert LIB.sparse_conv_embed_backward_workspace(vocab, 1, 1, tokens, B.SC_F32, 0, C.byref(n)) == B.SC_OK
+    assert 16 * tokens <= n.value <= 16 * tokens + tokens // 8 + 512 * 1024 * 4 + 8 * 256
