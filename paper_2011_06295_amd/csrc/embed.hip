@@ -122,10 +122,17 @@ __device__ __forceinline__ void store_some(T* p, typename Piece<T, VEC>::type v,
 // Tile number -> sentence, first word, first dimension.
 __device__ __forceinline__ void tile_at(unsigned tile, int words, int dim, int per_words, int per_dims, size_t& n, int& w0, int& d0)
 {
-    const unsigned across = (dim + per_dims - 1) / per_dims, along = (words + per_words - 1) / per_words;
+    const unsigned across = ((unsigned)dim + per_dims - 1) / per_dims, along = ((unsigned)words + per_words - 1) / per_words;
     d0 = (int)(tile % across) * per_dims;
     w0 = (int)(tile / across % along) * per_words;
     n = tile / across / along;
+}
+
+// (Sizes go up to 2^31 - 1: what rounds them up does not do so in int.)
+template <class U>
+long long tiles_of(int sentences, int words, int dim)
+{
+    return (long long)sentences * ((words + (U::kWords - 1ll)) / U::kWords) * ((dim + (U::kDims - 1ll)) / U::kDims);
 }
 
 // Vectors channels first: [sentence][dimension][word].
@@ -172,14 +179,13 @@ template <class T>
 int launch_lookup(const EmbedArgs& a, hipStream_t s)
 {
     if (a.channels_first && a.words > 1) {
-        typedef Turn<T> U;
-        const long long tiles = (long long)a.sentences * ((a.words + U::kWords - 1) / U::kWords) * ((a.dim + U::kDims - 1) / U::kDims);
+        const long long tiles = tiles_of<Turn<T>>(a.sentences, a.words, a.dim);
         if ((unsigned long long)tiles > most_groups(kThreads)) return kTooLarge;
         hipLaunchKernelGGL(embed_turned_kernel<T>, dim3((unsigned)tiles), dim3(kThreads), 0, s, a);
         return (int)hipGetLastError();
     }
     constexpr int kVec = 16 / sizeof(T);
-    const unsigned per_row = a.dim >= kVec ? (a.dim + kVec - 1) / kVec : a.dim;
+    const unsigned per_row = a.dim >= kVec ? ((unsigned)a.dim + kVec - 1) / kVec : a.dim;
     const unsigned long long pieces = (unsigned long long)a.sentences * a.words * per_row, blocks = (pieces + 4 * kThreads - 1) / (4 * kThreads);
     if (blocks > most_groups(kThreads)) return kTooLarge;
     const bool passing = pieces * 16 > kCacheBytes;
@@ -204,7 +210,7 @@ struct Columns {
 __device__ __forceinline__ Columns columns_of(int block, int lane, int dim)
 {
     Columns c;
-    int begin = block * kColumns, end = min(begin + kColumns, dim);
+    int begin = block * kColumns, end = begin + min(kColumns, dim - begin);
     c.narrow = dim < 4;
     if (end < dim && dim - end < 4) end = dim - 4;            // (a last block of less than four columns takes some of the one before)
     if (block > 0 && dim - begin < 4) begin = dim - 4;
@@ -1115,8 +1121,7 @@ int launch_grad(const EmbedGradArgs& a, const Parts& parts, char* workspace, hip
     G* rows = reinterpret_cast<G*>(workspace);
     long long tiles = 0;
     if (parts.rows) {
-        typedef Turn<G> U;
-        tiles = (long long)a.sentences * ((a.words + U::kWords - 1) / U::kWords) * ((a.dim + U::kDims - 1) / U::kDims);
+        tiles = tiles_of<Turn<G>>(a.sentences, a.words, a.dim);
         grad = rows;
     }
     const unsigned long long elements = a.accumulate ? 0 : (unsigned long long)a.vocab * a.dim;

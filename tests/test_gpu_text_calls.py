@@ -45,3 +45,24 @@ def test_gradient_of_more_tokens_than_workgroups_sort_at_once(case, first):
         total.index_add_(0, tok[keep], terms[keep])
     bound = (count + 1) * 2.0 ** -24 * size
     assert bool(((out.double().cpu() - ref).abs() <= bound + 2.0 ** -24 * (ref.abs() + bound) + 2.0 ** -149).all())
+
+
+@pytest.mark.parametrize("dim", [2 ** 31 - 1, 2 ** 31 - 300, 2 ** 31 - 514])
+def test_vectors_of_nearly_2_to_the_31(dim):
+    """The longest rows: their last pieces and column blocks end next to what an int holds."""
+    import torch
+    from paper_2011_06295_amd import text
+    dtype = torch.float16
+    table = torch.full((1, dim), 3.0, dtype=dtype, device="cuda")
+    places = torch.tensor([0, 1, 4095, dim // 2, dim - 514, dim - 9, dim - 2, dim - 1], device="cuda")
+    table[0, places] = torch.arange(1, 9, device="cuda", dtype=dtype)
+    layer = text.Embedding(table, scale=2.0)
+    tokens = torch.zeros(1, dtype=torch.int64, device="cuda")
+
+    def is_twice_the_table(y):
+        return all(torch.equal(a, b * 2.0) for a, b in zip(y.split(1 << 28), table[0].split(1 << 28)))
+
+    y = layer.forward(tokens)
+    assert is_twice_the_table(y[0])
+    g = layer.backward(table, tokens, out=y)
+    assert is_twice_the_table(g[0])
