@@ -359,8 +359,9 @@ enum { SC_EMBED_CHANNELS_FIRST = 1u, SC_EMBED_TOKENS_64 = 2u, SC_EMBED_ACCUMULAT
  *   flags    0 or any of SC_EMBED_CHANNELS_FIRST, SC_EMBED_TOKENS_64.
  * The product with scale is formed in fp32 and rounded once.  sentences or words may be 0 (no-op).
  * SC_EINVAL: a null or misaligned pointer (to its own element size), vocab or dim below 1, a negative count, an unknown
- * type or flag.  SC_EUNSUPPORTED: vocab or sentences * words of 2^31 or more; what no launch can hold: an output of about 256 GB
- * or more, or (channels first) 2^24 or more tiles, of 64 words of a sentence by 256 bytes of their vectors, each begun tile whole.
+ * type or flag.  SC_EUNSUPPORTED: vocab or sentences * words of 2^31 or more, an array of more than 2^46 elements;
+ * what no launch can hold: an output of about 256 GB or more, or (channels first) 2^24 or more tiles, of 64 words of a
+ * sentence by 256 bytes of their vectors, each begun tile whole.
  */
 int sparse_conv_embed(const void* table, const void* tokens, void* out, long long vocab, int dim, int sentences, int words,
                       int dtype, float scale, unsigned flags, void* stream);
@@ -396,7 +397,7 @@ int sparse_conv_embed_backward(const void* grad, const void* tokens, void* table
  *   q        [rows][SC_INT8_PITCH(K)], at a multiple of 16 bytes; bytes past K are set to zero.
  *   scale    fp32 [rows].
  * A row whose a is below 2^-100 counts as zeros: q = 0, scale = 0.  A row that holds an infinity or a NaN has q = 0 and
- * scale = NaN.
+ * scale = NaN.  SC_EUNSUPPORTED: rows of 2^24 or more, K above 2^24, rows * ldx above 2^46.
  */
 int sparse_conv_int8_quantize(const void* x, signed char* q, float* scale, int rows, int K, long long ldx, int dtype, void* stream);
 
@@ -414,7 +415,7 @@ int sparse_conv_int8_quantize(const void* x, signed char* q, float* scale, int r
  * Sums are exact (32-bit integers, hence K <= 131071); scales, bias and activation are applied in fp32 and the result is
  * rounded once, to out_dtype.  An output row whose scale is NaN is NaN; no other row is touched by it.  M may be 0 (no-op).
  * SC_EINVAL: a null or misaligned pointer, a size below 1, ldx or ldo too small, an unknown type or flag, a workspace that is
- * too small.  SC_EUNSUPPORTED: K above 131071, M or N of 2^24 or more.
+ * too small.  SC_EUNSUPPORTED: K above 131071, M or N of 2^24 or more, M * ldx or M * ldo above 2^46.
  */
 int sparse_conv_int8_linear_workspace(int M, int N, int K, int in_dtype, int out_dtype, long long* bytes);
 int sparse_conv_int8_linear(const void* x, const float* x_scale, const signed char* w, const float* w_scale, const float* bias,

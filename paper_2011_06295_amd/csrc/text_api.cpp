@@ -24,12 +24,17 @@ bool overlap(const void* a, long long na, const void* b, long long nb)
 }
 
 constexpr long long kMaxCount = 1ll << 31;
+constexpr long long kMaxElements = 1ll << 46;      // of an array: past any memory, and numbers of bytes stay within 64 bits
+
+// `rows` rows, `apart` elements from one to the next, are more than an array can be.
+bool too_many(long long rows, long long apart) { return rows > 1 && apart > kMaxElements / rows; }
 
 // Sizes that both directions of the lookup share.
 int check_embed(long long vocab, int dim, int sentences, int words, int dtype, unsigned flags, unsigned known)
 {
     if (vocab < 1 || dim < 1 || sentences < 0 || words < 0 || !is_float(dtype) || (flags & ~known)) return SC_EINVAL;
-    if (vocab >= kMaxCount || (long long)sentences * words >= kMaxCount) return SC_EUNSUPPORTED;
+    const long long count = (long long)sentences * words;
+    if (vocab >= kMaxCount || count >= kMaxCount || too_many(vocab, dim) || too_many(count, dim)) return SC_EUNSUPPORTED;
     return SC_OK;
 }
 
@@ -108,7 +113,7 @@ int sparse_conv_embed_backward(const void* grad, const void* tokens, void* table
 int sparse_conv_int8_quantize(const void* x, signed char* q, float* scale, int rows, int K, long long ldx, int dtype, void* stream)
 {
     if (rows < 0 || K < 1 || ldx < K || !is_float(dtype)) return SC_EINVAL;
-    if (rows >= (1 << 24) || K > (1 << 24)) return SC_EUNSUPPORTED;
+    if (rows >= (1 << 24) || K > (1 << 24) || too_many(rows, ldx)) return SC_EUNSUPPORTED;
     if (rows == 0) return SC_OK;
     const int b = type_bytes(dtype);
     if (!x || !q || !scale || !aligned(x, b) || !aligned(q, 16) || !aligned(scale, 4)) return SC_EINVAL;
@@ -134,6 +139,7 @@ int sparse_conv_int8_linear(const void* x, const float* x_scale, const signed ch
     if (rc != SC_OK) return rc;
     const long long pitch = SC_INT8_PITCH(K);
     if ((flags & ~static_cast<unsigned>(SC_EPILOGUE_RELU)) || ldo < N || (in_dtype == SC_I8 ? ldx != pitch : ldx < K)) return SC_EINVAL;
+    if (too_many(M, ldx) || too_many(M, ldo)) return SC_EUNSUPPORTED;
     if (M == 0) return SC_OK;
     const int b = type_bytes(in_dtype), b2 = type_bytes(out_dtype);
     if (!x || !w || !w_scale || !out || !aligned(x, in_dtype == SC_I8 ? 16 : b) || !aligned(w, 16) || !aligned(w_scale, 4) || !aligned(out, b2))

@@ -30,3 +30,17 @@ def test_scratch_memory_of_the_sort_grows_with_the_tokens(tokens, vocab):
     n = C.c_longlong(-1)
     assert LIB.sparse_conv_embed_backward_workspace(vocab, 1, 1, tokens, B.SC_F32, 0, C.byref(n)) == B.SC_OK
     assert 16 * tokens <= n.value <= 16 * tokens + tokens // 8 + 512 * 1024 * 4 + 8 * 256
+
+
+def test_sizes_whose_bytes_pass_64_bits_are_refused():
+    big = (1 << 31) - 1
+    assert LIB.sparse_conv_embed(A, X, Y, big, big, 1, 1, B.SC_F32, 1.0, 0, None) == B.SC_EUNSUPPORTED
+    assert LIB.sparse_conv_embed(A, X, Y, 1, big, 1, big, B.SC_F32, 1.0, 0, None) == B.SC_EUNSUPPORTED
+    n = C.c_longlong(-1)
+    for vocab, dim, words in ((big, big, 1), (1, big, big)):
+        assert LIB.sparse_conv_embed_backward(A, X, Y, vocab, dim, 1, words, B.SC_F32, B.SC_F32, 1.0, -1, 0, W, 1 << 46, None) == B.SC_EUNSUPPORTED
+        assert LIB.sparse_conv_embed_backward_workspace(vocab, dim, 1, words, B.SC_F32, 0, C.byref(n)) == B.SC_EUNSUPPORTED and n.value == -1
+    for apart in (1 << 62, 1 << 61, (1 << 45) - 1):
+        assert LIB.sparse_conv_int8_quantize(A, X, Y, 3, 100, apart, B.SC_F32, None) == B.SC_EUNSUPPORTED
+        for ldx, ldo in ((apart, 5), (100, apart)):
+            assert LIB.sparse_conv_int8_linear(A, None, X, Y, None, 1 << 45, 3, 5, 100, ldx, ldo, B.SC_F32, B.SC_F32, 0, W, 1 << 40, None) == B.SC_EUNSUPPORTED
