@@ -56,34 +56,51 @@ def torch_command() -> list:
             "-o", TORCH_LIB, os.path.join(CSRC, "text_torch.cpp"), f"-L{lib}", f"-Wl,-rpath,{lib}", "-ltorch_python", "-ltorch_cpu", "-lc10"]
 
 
-def build_sanitize(verbose: bool = False) -> str:
-    """Host-only build for the sanitizer check: CSR encoder, planner and the C ABI (no kernels; the launch
-    functions are stand-ins that report "not supported"), the CPU oracle and tests/sanitize/driver.cpp in one
-    executable compiled with -fsanitize=address,undefined.  Returns its path; needs no GPU."""
-    root = os.path.dirname(HERE)
-    out_dir = os.path.join(root, "_build")
-    os.makedirs(out_dir, exist_ok=True)
-    exe = os.path.join(out_dir, "sanitize_driver")
-    oracle_o = os.path.join(out_dir, "oracle_sanitize.o")
-    san = ["-fsanitize=address,undefined", "-fno-sanitize-recover=undefined", "-fno-omit-frame-pointer", "-g", "-O1"]
-    cmds = [
-        ["gcc", "-std=c11", "-ffp-contract=off", "-c", *san, "-o", oracle_o, os.path.join(root, "oracle", "sparse_conv_oracle.c")],
-        ["g++", "-std=c++17", *san, "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include", "-o", exe,
-         os.path.join(root, "tests", "sanitize", "driver.cpp"), oracle_o,
-         *[os.path.join(CSRC, f) for f in ("api.cpp", "plan.cpp", "matrix_plan.cpp", "host_csr.cpp", "no_device.cpp")],
-         "-L/opt/rocm/lib", "-Wl,-rpath,/opt/rocm/lib", "-lamdhip64", "-lm"],
-    ]
+_SANITIZE = ["-fsanitize=address,undefined", "-fno-sanitize-recover=undefined", "-fno-omit-frame-pointer", "-g", "-O1"]
+
+
+def _build_dir() -> str:
+    path = os.path.join(os.path.dirname(HERE), "_build")
+    os.makedirs(path, exist_ok=True)
+    return path
+
+
+def _sanitized(driver: str, exe: str, sources, objects=()) -> list:
+    """The compiler's call for a sanitizer driver of tests/sanitize, linked with host sources of the library."""
+    return ["g++", "-std=c++17", *_SANITIZE, "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include", "-o", exe,
+            os.path.join(os.path.dirname(HERE), "tests", "sanitize", driver), *objects, *[os.path.join(CSRC, f) for f in sources],
+            "-L/opt/rocm/lib", "-Wl,-rpath,/opt/rocm/lib", "-lamdhip64", "-lm"]
+
+
+def _run_all(cmds, verbose: bool) -> None:
     for cmd in cmds:
         if verbose:
             print(" ".join(cmd), flush=True)
         res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
         if res.returncode != 0:
             raise RuntimeError("sanitizer build failed:\n" + res.stdout)
+
+
+def build_sanitize(verbose: bool = False) -> str:
+    """Host-only build for the sanitizer check: CSR encoder, planner and the C ABI (no kernels; the launch
+    functions are stand-ins that report "not supported"), the CPU oracle and tests/sanitize/driver.cpp in one
+    executable compiled with -fsanitize=address,undefined.  Returns its path; needs no GPU."""
+    exe, oracle_o = os.path.join(_build_dir(), "sanitize_driver"), os.path.join(_build_dir(), "oracle_sanitize.o")
+    _run_all([["gcc", "-std=c11", "-ffp-contract=off", "-c", *_SANITIZE, "-o", oracle_o, os.path.join(os.path.dirname(HERE), "oracle", "sparse_conv_oracle.c")],
+              _sanitized("driver.cpp", exe, ("api.cpp", "plan.cpp", "matrix_plan.cpp", "host_csr.cpp", "no_device.cpp"), [oracle_o])], verbose)
+    return exe
+
+
+def build_sanitize_text(verbose: bool = False) -> str:
+    """The same for the text model's entry points (text_api.cpp) and tests/sanitize/text_driver.cpp."""
+    exe = os.path.join(_build_dir(), "sanitize_text_driver")
+    _run_all([_sanitized("text_driver.cpp", exe, ("text_api.cpp", "no_device.cpp"))], verbose)
     return exe
 
 
 if __name__ == "__main__":
     if "--sanitize" in sys.argv[1:]:
         print(build_sanitize(verbose=True))
+        print(build_sanitize_text(verbose=True))
     else:
         print(build(verbose=True))
