@@ -396,6 +396,7 @@ int sparse_conv_embed_backward(const void* grad, const void* tokens, void* table
  *   x        [rows][K] of dtype (SC_F32, SC_F16, SC_BF16), ldx elements from one row to the next (ldx >= K).
  *   q        [rows][SC_INT8_PITCH(K)], at a multiple of 16 bytes; bytes past K are set to zero.
  *   scale    fp32 [rows].
+ * The three must not overlap (what lies between the rows of x counts as theirs).
  * A row whose a is below 2^-100 counts as zeros: q = 0, scale = 0.  A row that holds an infinity or a NaN has q = 0 and
  * scale = NaN.  SC_EUNSUPPORTED: rows of 2^24 or more, K above 2^24, rows * ldx above 2^46.
  */
@@ -409,7 +410,8 @@ int sparse_conv_int8_quantize(const void* x, signed char* q, float* scale, int r
  *            that function leaves them (ldx = SC_INT8_PITCH(K), at a multiple of 16 bytes, zeros past K), x_scale fp32 [M].
  *   w        [N][SC_INT8_PITCH(K)] 8-bit integers at a multiple of 16 bytes, zeros past K; w_scale fp32 [N].
  *   bias     fp32 [N] or NULL.
- *   out      [M][N] of out_dtype (SC_F32, SC_F16, SC_BF16), ldo elements from one row to the next (ldo >= N).
+ *   out      [M][N] of out_dtype (SC_F32, SC_F16, SC_BF16), ldo elements from one row to the next (ldo >= N).  Neither it nor the
+ *            workspace may overlap another array; what lies between the rows of x and of out counts as theirs.
  *   flags    0 or SC_EPILOGUE_RELU (a NaN stays one).
  *   workspace  of at least the bytes that sparse_conv_int8_linear_workspace reports for the same sizes and types.
  * Sums are exact (32-bit integers, hence K <= 131071); scales, bias and activation are applied in fp32 and the result is

@@ -150,8 +150,8 @@ int sparse_conv_int8_linear(const void* x, const float* x_scale, const signed ch
     const long long out_bytes = ((M - 1ll) * ldo + N) * b2, x_bytes = ((M - 1ll) * ldx + K) * b;
     if (overlap(out, out_bytes, x, x_bytes) || overlap(out, out_bytes, w, N * pitch) || overlap(out, out_bytes, w_scale, N * 4ll) ||
         (bias && overlap(out, out_bytes, bias, N * 4ll)) || (in_dtype == SC_I8 && overlap(out, out_bytes, x_scale, M * 4ll))) return SC_EINVAL;
-    if (need > 0 && (overlap(workspace, need, x, x_bytes) || overlap(workspace, need, w, N * pitch) || overlap(workspace, need, out, out_bytes)))
-        return SC_EINVAL;
+    if (need > 0 && (overlap(workspace, need, x, x_bytes) || overlap(workspace, need, w, N * pitch) || overlap(workspace, need, w_scale, N * 4ll) ||
+                     (bias && overlap(workspace, need, bias, N * 4ll)) || overlap(workspace, need, out, out_bytes))) return SC_EINVAL;
     const sc::Int8Args a{x, x_scale, reinterpret_cast<const int8_t*>(w), w_scale, bias, out, M, N, K, (int)pitch, ldx, ldo,
                          (flags & SC_EPILOGUE_RELU) != 0};
     return status(sc::launch_int8_linear(in_dtype, out_dtype, a, static_cast<char*>(workspace), stream));

@@ -162,7 +162,8 @@ void layer(int t)
         else if (M == 0) want = SC_OK;
         else if (refused(x) || refused(w) || refused(ws) || refused(y) || (in == SC_I8 && refused(xs)) || (bias.at && refused(bias))) want = SC_EINVAL;
         else if (overlap(y, x) || overlap(y, w) || overlap(y, ws) || (bias.at && overlap(y, bias)) || (in == SC_I8 && overlap(y, xs))) want = SC_EINVAL;
-        else if (need > 0 && (refused(work) || given < need || overlap(work, x) || overlap(work, w) || overlap(work, y))) want = SC_EINVAL;
+        else if (need > 0 && (refused(work) || given < need || overlap(work, x) || overlap(work, w) || overlap(work, ws) ||
+                              (bias.at && overlap(work, bias)) || overlap(work, y))) want = SC_EINVAL;
     }
     check("layer", t, sparse_conv_int8_linear(at(x), static_cast<const float*>(at(xs)), static_cast<const signed char*>(at(w)), static_cast<const float*>(at(ws)),
                                               static_cast<const float*>(at(bias)), at(y), M, N, K, ldx, ldo, in, out, flags, at(work), given, nullptr), want);

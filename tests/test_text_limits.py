@@ -44,3 +44,16 @@ def test_sizes_whose_bytes_pass_64_bits_are_refused():
         assert LIB.sparse_conv_int8_quantize(A, X, Y, 3, 100, apart, B.SC_F32, None) == B.SC_EUNSUPPORTED
         for ldx, ldo in ((apart, 5), (100, apart)):
             assert LIB.sparse_conv_int8_linear(A, None, X, Y, None, 1 << 45, 3, 5, 100, ldx, ldo, B.SC_F32, B.SC_F32, 0, W, 1 << 40, None) == B.SC_EUNSUPPORTED
+
+
+def test_layer_s_scratch_memory_overlaps_no_scales_and_no_bias():
+    n = C.c_longlong()
+    M, N, K = 1000, 70, 1000
+    assert LIB.sparse_conv_int8_linear_workspace(M, N, K, B.SC_F16, B.SC_F16, C.byref(n)) == B.SC_OK and n.value > 4096
+
+    def call(scale=Y, bias=None):
+        return LIB.sparse_conv_int8_linear(A, None, X, scale, bias, 1 << 45, M, N, K, K, N, B.SC_F16, B.SC_F16, 0, W, n.value, None)
+
+    for inside in (W, W + 4096, W + n.value - 4, W - 4 * N + 4):
+        assert call(scale=inside) == B.SC_EINVAL
+        assert call(bias=inside) == B.SC_EINVAL
