@@ -1,7 +1,8 @@
-"""Builds libsparseconv.so (HIP kernels + C ABI) in-tree for gfx950."""
+"""Builds libsparseconv.so (HIP kernels + C ABI) in-tree for gfx950, and the Python side of the text model's operators."""
 from __future__ import annotations
 
 import os
+import shutil
 import subprocess
 import sys
 import tempfile
@@ -23,37 +24,48 @@ HIPCC_FLAGS = [
 
 
 def build(verbose: bool = False) -> str:
-    """Compiles every source (side by side) and links them."""
+    """Compiles every source (side by side) and links them.  The Python side of the text model's operators is built as well where PyTorch
+    is there; the library needs neither it nor its compiler."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     with tempfile.TemporaryDirectory() as objects:
         cmds = [[hipcc] + HIPCC_FLAGS + ["-c", "-o", os.path.join(objects, s + ".o"), os.path.join(CSRC, s)] for s in SOURCES]
-        cmds.append(torch_command())
-        link = [hipcc] + HIPCC_FLAGS + ["-shared", "-o", LIB] + [c[-2] for c in cmds[:len(SOURCES)]]
-        running = [(c, subprocess.Popen(c, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)) for c in cmds]
+        torch_lib = os.path.join(objects, os.path.basename(TORCH_LIB))
+        torch_side = torch_command(torch_lib)
+        if torch_side is None and verbose:
+            print("PyTorch is not there: the library without " + os.path.basename(TORCH_LIB), flush=True)
+        link = [hipcc] + HIPCC_FLAGS + ["-shared", "-o", LIB] + [c[-2] for c in cmds]
+        running = [(c, subprocess.Popen(c, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)) for c in cmds + ([torch_side] if torch_side else [])]
         done = [(c, p.communicate()[0], p.returncode) for c, p in running]
-        if all(rc == 0 for _, _, rc in done):
+        if all(rc == 0 for _, _, rc in done[:len(cmds)]):
             res = subprocess.run(link, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-            done.append((link, res.stdout, res.returncode))
+            done.insert(len(cmds), (link, res.stdout, res.returncode))
+        if torch_side and done[-1][2] == 0:      # moved into place whole: another process may be about to load it
+            shutil.copyfile(torch_lib, TORCH_LIB + ".new")
+            os.replace(TORCH_LIB + ".new", TORCH_LIB)
     for cmd, text, rc in done:
         if verbose:
             print(" ".join(cmd), flush=True)
         out = "\n".join(l for l in text.splitlines() if "packed-fp32-ops" not in l)
         if rc != 0:
-            raise RuntimeError("hipcc failed:\n" + out)
+            raise RuntimeError(os.path.basename(cmd[0]) + " failed:\n" + out)
         if verbose and out.strip():
             print(out)
     return LIB
 
 
-def torch_command() -> list:
-    """The compiler's call for the Python side of the text model's operators (checks and allocation on PyTorch tensors, host code)."""
+def torch_command(path: str):
+    """The compiler's call that makes `path`, the Python side of the text model's operators (checks and allocation on PyTorch tensors, host
+    code), or None where PyTorch is not there."""
+    try:
+        import torch
+        from torch.utils import cpp_extension
+    except ImportError:
+        return None
     import sysconfig
-    import torch
-    from torch.utils import cpp_extension
     lib = os.path.join(os.path.dirname(torch.__file__), "lib")
     return ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
             f"-I{sysconfig.get_paths()['include']}", *[f"-I{p}" for p in cpp_extension.include_paths()],
-            "-o", TORCH_LIB, os.path.join(CSRC, "text_torch.cpp"), f"-L{lib}", f"-Wl,-rpath,{lib}", "-ltorch_python", "-ltorch_cpu", "-lc10"]
+            "-o", path, os.path.join(CSRC, "text_torch.cpp"), f"-L{lib}", f"-Wl,-rpath,{lib}", "-ltorch_python", "-ltorch_cpu", "-lc10"]
 
 
 _SANITIZE = ["-fsanitize=address,undefined", "-fno-sanitize-recover=undefined", "-fno-omit-frame-pointer", "-g", "-O1"]
