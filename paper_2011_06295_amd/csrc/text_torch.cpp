@@ -57,6 +57,16 @@ bool is_true(PyObject* o)
     return t != 0;
 }
 
+// torch.OutOfMemoryError, as every other allocation of the caller's raises it.
+void set_out_of_memory(const char* what)
+{
+    PyObject* torch = PyImport_ImportModule("torch");
+    PyObject* type = torch ? PyObject_GetAttrString(torch, "OutOfMemoryError") : nullptr;
+    if (type) PyErr_SetString(type, what);
+    Py_XDECREF(type);
+    Py_XDECREF(torch);
+}
+
 template <class F>
 PyObject* guarded(F&& f)
 {
@@ -65,7 +75,7 @@ PyObject* guarded(F&& f)
     } catch (const Refused& r) {
         PyErr_SetString(PyExc_ValueError, r.what);
     } catch (const c10::OutOfMemoryError& e) {
-        PyErr_SetString(PyExc_MemoryError, e.what_without_backtrace());
+        set_out_of_memory(e.what_without_backtrace());
     } catch (const std::exception& e) {
         PyErr_SetString(PyExc_RuntimeError, e.what());
     } catch (...) {

@@ -4,6 +4,13 @@ import pytest
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(autouse=True)
+def _memory_goes_back():
+    yield
+    import torch
+    torch.cuda.empty_cache()
+
+
 def test_gradient_of_a_table_of_more_than_64_gb():
     """More zeros than one launch can write (2^32 threads of 16 bytes): few tokens, and none."""
     import torch
@@ -66,3 +73,17 @@ def test_vectors_of_nearly_2_to_the_31(dim):
     assert is_twice_the_table(y[0])
     g = layer.backward(table, tokens, out=y)
     assert is_twice_the_table(g[0])
+
+
+def test_out_of_memory_is_pytorch_s_own_exception():
+    """Outputs and scratch memory of more bytes than the card has: the allocator refuses them before anything is enqueued."""
+    import torch
+    from paper_2011_06295_amd import text
+    tokens = torch.zeros(1 << 20, dtype=torch.int32, device="cuda")
+    wide = text.Embedding(torch.zeros((2, 1 << 20), dtype=torch.float16, device="cuda"))
+    with pytest.raises(torch.OutOfMemoryError):
+        wide.forward(tokens)
+    layer = text.Int8Linear.from_quantized(torch.zeros((1 << 20, 1), dtype=torch.int8, device="cuda"), torch.ones(1 << 20, device="cuda"))
+    with pytest.raises(torch.OutOfMemoryError):
+        layer.forward(torch.zeros((1 << 20, 1), device="cuda"))
+    assert wide.forward(tokens[:1]).shape == (1, 1 << 20)       # the next call runs
