@@ -41,8 +41,13 @@ const at::Tensor& tensor(PyObject* o, const char* what)
     return THPVariable_Unpack(o);
 }
 
-// A status other than SC_OK goes back as a number (text.py raises the library's error from it).
-PyObject* result(int rc, const at::Tensor& out) { return rc == SC_OK ? THPVariable_Wrap(out) : PyLong_FromLong(rc); }
+// A status other than SC_OK goes back as a number (text.py raises the library's error from it).  given: `out` is the caller's, whose
+// version counts what is written into it (autograd refuses to read what it saved once that has changed).
+PyObject* result(int rc, const at::Tensor& out, bool given)
+{
+    if (given && !out.is_inference()) out.unsafeGetTensorImpl()->bump_version();
+    return rc == SC_OK ? THPVariable_Wrap(out) : PyLong_FromLong(rc);
+}
 
 // Scratch memory of the current device and stream (text.py calls with the tensors' device as the current one), as at::empty gets it, but
 // without a tensor around it.
@@ -163,7 +168,7 @@ PyObject* py_embed(PyObject*, PyObject* const* args, Py_ssize_t count)
         }
         return result(embed(table.data_ptr(), tokens.data_ptr(), out.data_ptr(), table.size(0), (int)table.size(1), s.count, s.words,
                             type_of(table.scalar_type()), (float)PyFloat_AS_DOUBLE(args[4]), s.flags, PyLong_AsVoidPtr(args[5])),
-                      out);
+                      out, args[2] != Py_None);
     });
 }
 
@@ -200,7 +205,7 @@ PyObject* py_embed_backward(PyObject*, PyObject* const* args, Py_ssize_t count)
             rc = embed_backward(grad.data_ptr(), tokens.data_ptr(), out.data_ptr(), table.size(0), (int)table.size(1), s.count, s.words, g,
                                 type_of(out.scalar_type()), (float)PyFloat_AS_DOUBLE(args[6]), PyLong_AsLongLong(args[7]), flags,
                                 work.get(), bytes, PyLong_AsVoidPtr(args[8]));
-        return result(rc, out);
+        return result(rc, out, args[3] != Py_None);
     });
 }
 
@@ -272,7 +277,7 @@ PyObject* py_linear(PyObject*, PyObject* const* args, Py_ssize_t count)
             rc = int8_linear(x.data_ptr(), x_scale, static_cast<const signed char*>(weight.data_ptr()), w_scale.data_ptr<float>(),
                              args[4] == Py_None ? nullptr : THPVariable_Unpack(args[4]).data_ptr<float>(), out.data_ptr(), (int)M, (int)N, (int)K, ldx, ldo,
                              in, o, is_true(args[6]) ? SC_EPILOGUE_RELU : 0u, work.get(), bytes, PyLong_AsVoidPtr(args[9]));
-        return result(rc, out);
+        return result(rc, out, args[7] != Py_None);
     });
 }
 

@@ -2,6 +2,9 @@
 
 `Embedding` and `Int8Linear` call the library's operators (include/sparse_conv.h) on PyTorch tensors.  A call's tensors are checked,
 and its output and scratch memory allocated, by csrc/text_torch.cpp: calls of few tokens are bound by the host.  There is no fallback.
+
+Autograd does not record these calls: their outputs have no gradient function, also where a table or an input requires a gradient.
+`Embedding.backward` is called by the program itself.  A write into a given `out` raises that tensor's version.
 """
 from __future__ import annotations
 
@@ -34,7 +37,8 @@ _bind()
 
 class Embedding:
     """Rows of a table [vocab][dim] (fp32, binary16 or bfloat16) for tokens, times `scale`, and the gradient of the table.
-    A token outside 0..vocab-1 reads as zeros and has no gradient; the row of token `padding` has no gradient."""
+    A token outside 0..vocab-1 reads as zeros and has no gradient; the row of token `padding` has no gradient.  `backward` computes
+    that gradient when it is called: autograd does not record `forward`."""
 
     def __init__(self, table: torch.Tensor, scale: float = 1.0, padding: Optional[int] = None):
         if not table.is_cuda or table.dtype not in _DTYPES or table.dim() != 2 or not table.is_contiguous():
@@ -87,7 +91,8 @@ def quantize(x: torch.Tensor):
 
 class Int8Linear:
     """Fully connected layer whose weights are 8-bit integers with a scale for each output channel; the input is quantised
-    within the call, with a scale for each token (row)."""
+    within the call, with a scale for each token (row).  Autograd does not record it; `dequantized` gives the weights that a
+    gradient of the input goes through."""
 
     def __init__(self, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, relu: bool = False):
         """weight: CUDA tensor [N][K] of fp32, binary16 or bfloat16, quantised here; bias: [N] or None."""

@@ -87,3 +87,29 @@ def test_out_of_memory_is_pytorch_s_own_exception():
     with pytest.raises(torch.OutOfMemoryError):
         layer.forward(torch.zeros((1 << 20, 1), device="cuda"))
     assert wide.forward(tokens[:1]).shape == (1, 1 << 20)       # the next call runs
+
+
+def test_writes_into_a_given_tensor_raise_its_version():
+    import torch
+    from paper_2011_06295_amd import text
+    emb = text.Embedding(torch.ones((10, 4), device="cuda"))
+    tokens = torch.zeros(3, dtype=torch.int64, device="cuda")
+    out = torch.zeros((3, 4), device="cuda")
+    layer = text.Int8Linear(torch.ones((5, 4), device="cuda"))
+    y = torch.zeros((3, 5), device="cuda")
+    for tensor, call in ((out, lambda: emb.forward(tokens, out=out)), (emb.table, lambda: emb.backward(out, tokens, out=emb.table, accumulate=True)),
+                         (y, lambda: layer.forward(out, out=y))):
+        before = tensor._version
+        call()
+        assert tensor._version > before
+    # what autograd has saved and a call overwrites: noticed by backward
+    x = torch.ones((3, 4), device="cuda", requires_grad=True)
+    kept = torch.ones((3, 4), device="cuda")
+    product = (x * kept).sum()
+    emb.forward(tokens, out=kept)
+    with pytest.raises(RuntimeError):
+        product.backward()
+    with torch.inference_mode():
+        held = torch.zeros((3, 4), device="cuda")
+        emb.forward(tokens, out=held)
+    assert torch.equal(emb.forward(tokens, out=held), emb.forward(tokens))      # an inference tensor has no version
