@@ -16,7 +16,8 @@ from . import workloads as wl
 
 
 class TextModel:
-    """Filters are pruned and fixed, the classifier is quantised; the word vectors can be trained."""
+    """Filters are pruned and fixed, the classifier is quantised; the word vectors can be trained.  A gradient is that of the last
+    forward: threads that train need a model each."""
 
     def __init__(self, table: torch.Tensor, filters, classifier: torch.Tensor, bias: torch.Tensor, padding: int = 0):
         """table: word vectors [vocab][dim], fp32.  filters: (weights [K][dim][1][S], mask, bias [K]) of each convolution, numpy
@@ -44,9 +45,9 @@ class TextModel:
         return cls(table, filters, torch.randn((classes, features), generator=gen, device=device) / features ** 0.5, torch.zeros(classes, device=device))
 
     def forward(self, tokens: torch.Tensor) -> torch.Tensor:
-        """Logits [sentences][classes] of tokens [sentences][words]; what backward needs is kept."""
+        """Logits [sentences][classes] of tokens [sentences][words]; what the gradient needs is kept, the tokens as they are now."""
         x = self.words.forward(tokens, channels_first=True)
-        self._tokens = tokens
+        self._tokens = tokens.clone()
         self._maps = [layer.forward(x) for layer in self.convs]
         best = [m.squeeze(2).max(2) for m in self._maps]
         self._places = [b.indices for b in best]

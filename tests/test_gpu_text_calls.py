@@ -113,3 +113,19 @@ def test_writes_into_a_given_tensor_raise_its_version():
         held = torch.zeros((3, 4), device="cuda")
         emb.forward(tokens, out=held)
     assert torch.equal(emb.forward(tokens, out=held), emb.forward(tokens))      # an inference tensor has no version
+
+
+def test_model_s_gradient_is_of_the_tokens_that_forward_saw():
+    import torch
+    from paper_2011_06295_amd import text_model
+    model = text_model.TextModel.synthetic(vocab=500)
+    tokens, _ = text_model.sentences(8, 64, 500)
+    other, _ = text_model.sentences(8, 64, 500, seed=3)
+    g = torch.ones((8, 6), device="cuda")
+    model.forward(tokens)
+    want = model.table_gradient(g)
+    batch = tokens.clone()                  # a buffer that the program fills anew for each batch
+    model.forward(batch)
+    batch.copy_(other)
+    assert torch.equal(model.table_gradient(g), want)
+    model.close()
