@@ -129,3 +129,43 @@ def test_model_s_gradient_is_of_the_tokens_that_forward_saw():
     batch.copy_(other)
     assert torch.equal(model.table_gradient(g), want)
     model.close()
+
+
+@pytest.mark.parametrize("first", [False, True])
+@pytest.mark.parametrize("count", [1, 60, 5000, 9000])
+def test_64_bit_tokens_whose_low_32_bits_name_a_row(first, count):
+    """They lie outside the table: zeros, and no gradient, on every path (one look at a token's low bits among them)."""
+    import torch
+    from paper_2011_06295_amd import text
+    vocab, dim = 600, 24
+    gen = torch.Generator(device="cuda").manual_seed(count)
+    table = torch.randn((vocab, dim), generator=gen, device="cuda")
+    inside = torch.randint(0, vocab, (2, count), generator=gen, device="cuda")
+    far = torch.tensor([1 << 32, -(1 << 32), 1 << 40, -(1 << 63), (1 << 63) - (1 << 32), -(1 << 31) * 2 * 3], device="cuda")
+    tokens = inside + far[torch.randint(0, len(far), inside.shape, generator=gen, device="cuda")]
+    assert bool(((tokens & 0xffffffff) == inside).all())
+    layer = text.Embedding(table)
+    assert int(torch.count_nonzero(layer.forward(tokens, channels_first=first))) == 0
+    kept = torch.rand(inside.shape, generator=gen, device="cuda") < 0.5
+    kept[0, 0] = True
+    tokens = torch.where(kept, inside, tokens)
+    y = layer.forward(tokens, channels_first=first)
+    want = table[inside] * kept[..., None]
+    assert torch.equal(y, want.transpose(1, 2)[:, :, None] if first else want)
+    g = torch.ones_like(y)
+    named = torch.zeros(vocab, device="cuda").index_add_(0, inside[kept], torch.ones(int(kept.sum()), device="cuda"))
+    out = layer.backward(g, tokens, channels_first=first)
+    assert torch.equal(out, named[:, None].expand(vocab, dim))         # whole numbers: exact in fp32
+
+
+@pytest.mark.parametrize("relu", [False, True])
+def test_layer_s_outputs_past_the_largest_binary16(relu):
+    """They are infinities of the right sign (zero below, with ReLU), whichever kernel multiplies."""
+    import torch
+    from paper_2011_06295_amd import text
+    for M, K, N in ((1, 256, 64), (3, 4096, 70), (40, 1000, 300), (300, 1000, 260), (2048, 512, 2048)):
+        sign = torch.where(torch.arange(N, device="cuda") % 2 == 0, 1.0, -1.0)
+        layer = text.Int8Linear.from_quantized(torch.full((N, K), 100, dtype=torch.int8, device="cuda"), sign * 1e3, relu=relu)
+        y = layer.forward(torch.ones((M, K), device="cuda"), dtype=torch.float16)
+        want = sign * float("inf")
+        assert torch.equal(y, (want.clamp(min=0.0) if relu else want).to(torch.float16).expand(M, N)), (M, K, N)

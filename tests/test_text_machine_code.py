@@ -6,7 +6,7 @@ import subprocess
 import pytest
 
 from paper_2011_06295_amd import build
-from test_kernel_resources import LLVM, _code_objects
+from test_kernel_resources import LLVM, _code_objects, _metadata
 
 
 @pytest.fixture(scope="module")
@@ -85,3 +85,13 @@ def test_no_vector_instruction_writes_a_product_s_operands_right_before_it(produ
     early = [(kernel, code[at], i) for kernel, code in product_code.items() for at in range(len(code)) if code[at][0].startswith("v_mfma")
              for i in _before(code, at, 2) if i[0].startswith("v_") and not i[0].startswith("v_mfma") and _written(*i) & _named(code[at][1])]
     assert not early, early[:4]
+
+
+def test_no_kernel_of_the_text_operators_uses_scratch(tmp_path):
+    """(Their loads to LDS are waited for by number: a spilled register would be one more.)"""
+    with open(build.LIB, "rb") as f:
+        images = [elf for elf in _code_objects(f.read()) if b"row_product_kernel" in elf or b"embed_rows_kernel" in elf]
+    kernels = [k for elf in images for k in _metadata(elf, tmp_path / "object") if ".name" in k]
+    assert len(images) == 2 and len(kernels) > 60
+    used = {k[".name"]: (k[".private_segment_fixed_size"], k[".vgpr_spill_count"]) for k in kernels if k[".private_segment_fixed_size"] != "0" or k[".vgpr_spill_count"] != "0"}
+    assert not used, used
