@@ -376,7 +376,7 @@ int sparse_conv_embed(const void* table, const void* tokens, void* out, long lon
  *   table_grad  [vocab][dim] of table_dtype: SC_F32 or grad_dtype.  Must not overlap the other arrays.
  *   padding     a token whose row has no gradient (it adds to no row), or -1.
  *   workspace   of at least the bytes that sparse_conv_embed_backward_workspace reports for the same arguments.
- * Sums are formed in fp32, each row's in an order that depends on the tokens alone, and rounded once: the same
+ * Sums are formed in fp32, each row's in an order that depends on tokens and sizes alone, and rounded once: the same
  * arguments give the same bits.  Status codes as for sparse_conv_embed; SC_EINVAL for a workspace that is too small;
  * SC_EUNSUPPORTED for 2^23 or more tiles (channels first) and for sentences * words * (dim / 512, rounded up) of about 2^29 or more.
  */

@@ -207,8 +207,8 @@ __device__ __forceinline__ float output_of(int sum, float x_scale, float w_scale
     return relu && v < 0.f ? 0.f : v;
 }
 
-// The tile that a workgroup takes: workgroups go round the eight XCDs, so each gets a run of tiles of its own, in which eight by eight
-// tiles that share rows of x and of w are at work together.
+// The tile that a workgroup takes: workgroups go round the eight XCDs, so each gets a run of tiles of its own, which goes down kGroup
+// tiles before it goes across: the 32 that an XCD's CUs hold at one a CU are 4 by 8 tiles that share rows of x and of w.
 __device__ __forceinline__ void tile_of(unsigned block, unsigned tiles, int down, int across, int& tm, int& tn)
 {
     const unsigned xcd = block % 8, share = tiles / 8, rest = tiles % 8;
@@ -467,7 +467,7 @@ constexpr int kOwnBytes = 16384;
 // 16 MB tokens by 16 NB channels a workgroup, whose W wavefronts go round the 128-byte units of the rows and add their sums up at
 // the end.  A wavefront loads its units to a part of LDS of its own, D of them in flight, and waits for its own loads alone.  (Loads
 // in the order that the products take would touch 16 rows with 16 lanes in a row, at a quarter of the rate.)  X is int8_t, x then
-// comes the same way as w; or the type of an input that every workgroup quantises for itself while its first weights are on their way.
+// comes the same way as w; or the type of an input that every workgroup loads and then quantises while its first weights are on their way.
 template <class T, class X, int MB, int NB, int W, int D>
 __global__ __launch_bounds__(64 * W) void row_product_kernel(Int8Args a)
 {
@@ -635,8 +635,8 @@ int launch_row_product(const Int8Args& a, hipStream_t s)
 
 // ---------------------------------------------------------------- which kernel
 
-// Microseconds that a product is estimated to take.  The constants are fitted to launches of 20 sizes of M by 16 of K and N (1 to
-// 8192 tokens, K 128 to 16384, N 10 to 16384, weights that do not stay in a cache), each to what is near the fastest there: over
+// Microseconds that a product is estimated to take.  The constants are fitted to launches of 20 sizes of M by 16 of K and N but the two
+// largest products, 318 (1 to 8192 tokens, K 128 to 16384, N 10 to 16384, weights that do not stay in a cache), each to what is near the fastest there: over
 // these the kernel of the least estimate takes 1.0 % more than the fastest one, 26 % at most
 // (512 x 16384 -> 512).  Depth pays where a CU has a tile or two (64 x 64 at 256 x 4096 -> 4096: 14.5 us by two steps, 10.0 by four),
 // two steps where workgroups that share a CU hide each other's waits (128 x 128 at 2048 x 4096 -> 4096: 32.7 by two, 35.2 by three).
@@ -717,7 +717,8 @@ int launch_product(Kernel kernel, const Int8Args& a, hipStream_t s)
 }
 
 // An input that is not quantised yet takes a launch of its own, 2.5 to 3.9 us more on the GPU and 2.75 on the host (kQuantise counts
-// some of that), or every workgroup of a row kernel quantises its 16 rows for itself while its first weights are on their way.  Fitted to
+// some of that), or every workgroup of a row kernel quantises its 16 rows for itself: it loads them, then asks for its first weights, and
+// works the scales and whole numbers out while these are on their way.  Fitted to
 // 114 sizes (1 to 593 tokens, K 128 to 4096, N 10 to 12288), the rule takes 0.5 % more than the fastest one call after another, 1.6 % in
 // a graph.  1 x 2048 -> 4288 5.7 us against 8.9, 1 x 4096 -> 12288 12.5 against 15.3, 101 x 384 -> 256 5.0 against 8.9;
 // 593 x 384 -> 1280 would take 11.3 against 8.7.

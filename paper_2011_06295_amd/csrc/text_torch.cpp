@@ -26,7 +26,7 @@ int type_of(at::ScalarType t)
     return t == at::kFloat ? SC_F32 : t == at::kHalf ? SC_F16 : t == at::kBFloat16 ? SC_BF16 : -1;
 }
 
-// What ends in a Python exception; `value`: a ValueError.
+// What ends in a ValueError.
 struct Refused {
     const char* what;
 };
