@@ -8,34 +8,15 @@
 #include <utility>
 
 #include "text_ops.h"
+#include "tiles.h"
 
 namespace sc {
 
 namespace {
 
-enum { kF32 = 0, kF16 = 1, kBF16 = 2, kI8 = 3 };   // SC_F32, SC_F16, SC_BF16, SC_I8
-
 constexpr float kTiny = 0x1p-100f;   // a row whose largest size is below this counts as zeros (127 / a would overflow from 2^-121)
 
 // ---------------------------------------------------------------- rows to 8-bit integers
-
-template <class T>
-struct Piece {     // what one load of 16 bytes holds, from any element on (the hardware splits what crosses a line)
-    static constexpr int kCount = 16 / sizeof(T);
-    typedef T type __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
-};
-
-// Elements k .. k + kCount - 1 of a row; zeros past its end.
-template <class T>
-__device__ __forceinline__ typename Piece<T>::type load_piece(const T* row, int k, int K)
-{
-    typedef typename Piece<T>::type V;
-    if (k + Piece<T>::kCount <= K) return *reinterpret_cast<const V*>(row + k);
-    V v;
-#pragma unroll
-    for (int e = 0; e < Piece<T>::kCount; ++e) v[e] = k + e < K ? row[k + e] : (T)0.f;
-    return v;
-}
 
 // The largest size of a piece and of what came before, as a bit pattern: patterns order as the sizes do, and a NaN lies above all.
 // 16-bit types go two by two (two patterns a word until size_of).
@@ -158,39 +139,6 @@ int launch_quantize(const void* x, int8_t* q, float* scale, int rows, int K, lon
 
 // ---------------------------------------------------------------- product, tiles through LDS
 
-typedef int int4v __attribute__((ext_vector_type(4)));
-#define SC_LDS __attribute__((address_space(3)))
-
-template <class F, int... I>
-__device__ __forceinline__ void each_of(F&& f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
-// f(0) .. f(N - 1), each with its number as a constant: loops that have to be unrolled whole, however long.
-template <int N, class F>
-__device__ __forceinline__ void each(F&& f) { each_of(f, std::make_integer_sequence<int, N>{}); }
-
-// 16 bytes a lane from memory to LDS at `lds` + 16 * lane; bytes past the descriptor's end arrive as zeros.  Not the builtin:
-// the compiler waits for every load of that kind before any later read of LDS, here the reads wait where they have to.
-// A load to LDS may read m0 one wait state after a scalar instruction wrote it at the earliest; the compiler adds none inside an asm block.
-// (It notes that it keeps m0 for itself, which it does not across an operation that needs it.)
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void load_to_lds(int4v descriptor, unsigned offset, unsigned base, unsigned lds)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" :: "s"(lds), "v"(offset), "s"(descriptor), "s"(base) : "m0", "memory");
-}
-
-// The same, 4 bytes a lane.
-__device__ __forceinline__ void load_word_to_lds(int4v descriptor, unsigned offset, unsigned lds)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" :: "s"(lds), "v"(offset), "s"(descriptor) : "m0", "memory");
-}
-#pragma clang diagnostic pop
-
-__device__ __forceinline__ int4v descriptor_of(const void* p, long long bytes)
-{
-    const uint64_t b = reinterpret_cast<uint64_t>(p);
-    return int4v{(int)b, (int)(b >> 32) & 0xffff, (int)bytes, 0x00020000};
-}
-
 // c += a * b over 16 x 16 outputs and 64 bytes: lane l holds bytes 16 * (l / 16) .. + 15 of row l % 16 of a and of b, and rows
 // 4 * (l / 16) .. + 3 of c at column l % 16.  The sums stay in accumulation registers (as a builtin they were copied and spilled).
 __device__ __forceinline__ void multiply(int4v& c, int4v a, int4v b)
@@ -205,19 +153,6 @@ __device__ __forceinline__ float output_of(int sum, float x_scale, float w_scale
     float v = fmaf((float)sum * x_scale, w_scale, bias);
     asm("" : "+v"(v));
     return relu && v < 0.f ? 0.f : v;
-}
-
-// The tile that a workgroup takes: workgroups go round the eight XCDs, so each gets a run of tiles of its own, which goes down kGroup
-// tiles before it goes across: the 32 that an XCD's CUs hold at one a CU are 4 by 8 tiles that share rows of x and of w.
-__device__ __forceinline__ void tile_of(unsigned block, unsigned tiles, int down, int across, int& tm, int& tn)
-{
-    const unsigned xcd = block % 8, share = tiles / 8, rest = tiles % 8;
-    const unsigned tile = xcd * share + (xcd < rest ? xcd : rest) + block / 8;
-    constexpr int kGroup = 4;
-    const unsigned per_group = kGroup * (unsigned)across, group = tile / per_group, in = tile % per_group;
-    const int rows = min(kGroup, down - (int)group * kGroup);
-    tm = (int)group * kGroup + (int)(in % (unsigned)rows);
-    tn = (int)(in / (unsigned)rows);
 }
 
 // Large tiles: a workgroup has a CU to itself, so it walks over tiles, `stride` apart, and loads the next one's first steps before it
@@ -257,6 +192,7 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 || S > 2 ? 1 : 2) void 
     int4v from_x, from_w;
     unsigned xdst = lds0, wdst = lds0 + S * kX, tile = blockIdx.x;
     int next_m = 0, next_n = 0, step = 0, set = 0;      // what is loaded: a step of a tile, whose scales go to `set`
+    unsigned at = 0;                                    // where it begins in its rows
     auto enter = [&]() {
         int tm, tn;
         tile_of(tile, tiles, down, across, tm, tn);
@@ -274,7 +210,9 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 || S > 2 ? 1 : 2) void 
             load_word_to_lds(descriptor_of(x_scale + next_m, xs), threadIdx.x * 4, (unsigned)(uintptr_t)(SC_LDS float*)token_scale[set] + wave * 256);
     };
     auto advance = [&]() {
+        at += 128;
         if (++step < steps) return;
+        at = 0;
         tile += stride;
         if (kWalks<MB, NB> && tile < tiles) {
             step = 0;
@@ -285,8 +223,8 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 || S > 2 ? 1 : 2) void 
         }
     };
     auto load = [&](int i) {
-        if (i < kLoadsX) load_to_lds(from_x, offset[i], step * 128, xdst + (wave * kLoadsX + i) * 1024);
-        else load_to_lds(from_w, offset[i], step * 128, wdst + (wave * kLoadsW + i - kLoadsX) * 1024);
+        if (i < kLoadsX) load_to_lds(from_x, offset[i], at, xdst + (wave * kLoadsX + i) * 1024);
+        else load_to_lds(from_w, offset[i], at, wdst + (wave * kLoadsW + i - kLoadsX) * 1024);
     };
     enter();
     int m0 = next_m, n0 = next_n, done = set;
@@ -523,9 +461,10 @@ __global__ __launch_bounds__(64 * W) void row_product_kernel(Int8Args a)
     auto load = [&](int slot, int unit) {
         from_w[2] = unit < units ? bytes_w : 0;
         from_x[2] = unit < units ? bytes_x : 0;
+        const unsigned at = unit < units ? unit * 128u : 0u;
         each<kLoads>([&](auto load) {
             constexpr int l = load, block = l < kLoadsX ? l / 2 : (l - kLoadsX) / 2;
-            load_to_lds(l < kLoadsX ? from_x : from_w, offset[l & 1] + block * 16u * a.pitch, unit * 128, lds0 + slot * kUnit + l * 1024);
+            load_to_lds(l < kLoadsX ? from_x : from_w, offset[l & 1] + block * 16u * a.pitch, at, lds0 + slot * kUnit + l * 1024);
         });
     };
     each<D>([&](auto d) { load(d, wave + d * W); });
