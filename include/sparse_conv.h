@@ -424,6 +424,122 @@ int sparse_conv_int8_linear(const void* x, const float* x_scale, const signed ch
                             void* out, int M, int N, int K, long long ldx, long long ldo, int in_dtype, int out_dtype,
                             unsigned flags, void* workspace, long long workspace_bytes, void* stream);
 
+/* What a layer applies to its sums: nothing, max(z, 0), z Phi(z) with the normal distribution's Phi = (1 + erf(z / sqrt 2)) / 2,
+ * or z / (1 + exp(-z)). */
+enum { SC_ACT_NONE = 0, SC_ACT_RELU = 1, SC_ACT_GELU = 2, SC_ACT_SILU = 3 };
+
+/*
+ * sparse_conv_linear - fully connected layer:
+ *   z[m][n] = sum_k x[m][k] * w[n][k] + bias[n],  out[m][n] = act(z[m][n]) + residual[m][n].
+ *   x         [M][K], ldx elements from one row to the next (ldx >= K).
+ *   w         [N][K], ldw from one row to the next.
+ *   bias      fp32 [N] or NULL.
+ *   residual  [M][N], ldr from one row to the next, or NULL; it may be `out` itself (same address and ldr = ldo).
+ *   out       [M][N], ldo from one row to the next.
+ *   z         [M][N] without gaps, or NULL: receives what goes into the activation, rounded, as the gradient needs it.
+ *   dtype     of x, w, residual, out and z: SC_F32, SC_F16 or SC_BF16.
+ *   workspace of at least the bytes that sparse_conv_linear_workspace reports for the same arguments (it looks at x and w for
+ *             their alignment alone).  Arrays at multiples of 16 bytes whose rows are whole multiples of 16 bytes apart and long
+ *             are read as they are; others are copied there first.
+ * Products are summed, and everything behind them is computed, in fp32; out and z are rounded once.  Apart from residual = out no
+ * array that is written may overlap another (what lies between rows counts as theirs).  The same arguments give the same bits.
+ * An infinity or a NaN in a row of x or of w reaches no other row or column of the output.  M may be 0 (no-op).
+ * SC_EINVAL: a null or misaligned pointer (to its own element size), N or K below 1, a distance between rows that is too small, an
+ * unknown type or activation, a workspace that is too small.  SC_EUNSUPPORTED: M, N or K above 2^20, a distance of 2^31 or more.
+ */
+int sparse_conv_linear_workspace(const void* x, const void* w, int M, int N, int K, long long ldx, long long ldw, int dtype,
+                                 long long* bytes);
+int sparse_conv_linear(const void* x, const void* w, const float* bias, const void* residual, void* out, void* z, int M, int N, int K,
+                       long long ldx, long long ldw, long long ldr, long long ldo, int dtype, int activation, void* workspace,
+                       long long workspace_bytes, void* stream);
+
+/* sparse_conv_linear_backward adds to what grad_w and grad_bias hold. */
+enum { SC_LINEAR_ACCUMULATE = 1u };
+
+/*
+ * sparse_conv_linear_backward - gradients of sparse_conv_linear.  With d[m][n] = grad[m][n] * act'(z[m][n]):
+ *   grad_x[m][k] = sum_n d[m][n] w[n][k],  grad_w[n][k] = sum_m d[m][n] x[m][k],  grad_bias[n] = sum_m d[m][n].
+ *   grad       [M][N], ldg from one row to the next: the gradient of out (which is the residual's gradient as well).
+ *   z          [M][N] as sparse_conv_linear left it; not read for SC_ACT_NONE.  (The slope of SC_ACT_RELU at 0 is 0.)
+ *   x, w       as there; x is read for grad_w alone, w for grad_x alone.
+ *   grad_x     [M][K] without gaps, or NULL if it is not wanted; grad_w [N][K] likewise; grad_bias fp32 [N] likewise.
+ *   flags      0 or SC_LINEAR_ACCUMULATE.
+ *   workspace  as there; the same gradients have to be wanted (the three pointers are compared with NULL).
+ * Sums in fp32.  d is rounded to dtype before it is multiplied (grad_bias sums what was not rounded).  No array that is written may
+ * overlap another.  With M = 0, grad_w and grad_bias are set to zero (or left alone with SC_LINEAR_ACCUMULATE).  Status codes as above.
+ */
+int sparse_conv_linear_backward_workspace(const void* grad, const void* x, const void* w, const void* grad_x, const void* grad_w,
+                                          const void* grad_bias, int M, int N, int K, long long ldg, long long ldx, long long ldw,
+                                          int dtype, int activation, long long* bytes);
+int sparse_conv_linear_backward(const void* grad, const void* z, const void* x, const void* w, void* grad_x, void* grad_w,
+                                float* grad_bias, int M, int N, int K, long long ldg, long long ldx, long long ldw, int dtype,
+                                int activation, unsigned flags, void* workspace, long long workspace_bytes, void* stream);
+
+/* sparse_conv_cross_entropy: labels are 64-bit integers instead of 32-bit ones. */
+enum { SC_LOSS_LABELS_64 = 1u };
+
+/*
+ * sparse_conv_cross_entropy - loss of a classifier and the gradient of its logits.  With s = scale * weights[m]:
+ *   loss[m] = s * (log(sum_c exp(logits[m][c])) - logits[m][labels[m]]),
+ *   grad[m][c] = s * (exp(logits[m][c]) / sum_c' exp(logits[m][c']) - (c == labels[m])).
+ *   logits   [rows][classes] of dtype (SC_F32, SC_F16, SC_BF16), ldl elements from one row to the next.
+ *   labels   [rows], signed 32-bit integers (64-bit with SC_LOSS_LABELS_64).
+ *   weights  fp32 [rows] or NULL (ones).
+ *   loss     fp32 [rows].
+ *   grad     [rows][classes] of dtype, ldg from one row to the next, or NULL; it may be `logits` itself (same address and ldg = ldl).
+ * A row whose label lies outside 0..classes-1, or whose s is 0, has loss 0 and a gradient of zeros, and its logits are not read.
+ * Minus infinity forbids a class; a row that holds a NaN or plus infinity, or nothing but minus infinities, gives NaN in its own loss and
+ * gradient.  Computed in fp32; the gradient is rounded once.  No other overlap of what is written.  rows may be 0 (no-op).
+ * SC_EINVAL: a null or misaligned pointer, classes below 1, a distance between rows that is too small, an unknown type or flag.
+ * SC_EUNSUPPORTED: classes or rows of 2^31 - 2^20 or more, rows * ldl or rows * ldg above 2^46, 2^22 rows or more of 256 pieces of 16
+ * bytes or more (2^26 of shorter ones).
+ */
+int sparse_conv_cross_entropy(const void* logits, const void* labels, const float* weights, float* loss, void* grad, int rows,
+                              int classes, long long ldl, long long ldg, int dtype, float scale, unsigned flags, void* stream);
+
+/* 8-bit numbers of 4 exponent and 3 fraction bits (largest 448), for the states of sparse_conv_adamw. */
+enum { SC_E4M3 = 4 };
+
+/* Elements that share a scale in a state of 8 bits; the last block of a tensor may be shorter. */
+#define SC_ADAMW_BLOCK 256
+
+/* One tensor of a step: DEVICE arrays of `count` elements. */
+typedef struct {
+    void* param;        /* of param_dtype, read and written */
+    const void* grad;   /* of grad_dtype */
+    void* m;            /* first moment, of state_dtype, read and written */
+    void* v;            /* second moment */
+    float* m_scale;     /* states of 8 bits: fp32 [count / SC_ADAMW_BLOCK, rounded up]; else not used */
+    float* v_scale;
+    float* master;      /* fp32 weights that the step is applied to, param receives them rounded; or NULL, then param is stepped itself */
+    long long count;    /* may be 0 */
+} sparse_conv_adamw_tensor;
+
+/*
+ * sparse_conv_adamw - an AdamW step over many tensors, in few launches.  For each element, with g = grad_scale * grad, all in fp32:
+ *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
+ *   p = (1 - rate * decay) p - rate * (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps),   t = step.
+ *   tensors      HOST array, read by the call; its tensors are of the same types, all with `master` or all without, and none of
+ *                their arrays may overlap another, but gradients each other.
+ *   param_dtype  SC_F32, SC_F16 or SC_BF16; grad_dtype SC_F32 or param_dtype (any of the three where param_dtype is SC_F32).
+ *   state_dtype  SC_F32, or SC_E4M3: a state is its number of 8 bits times its block's scale.  A scale is the block's largest
+ *                size / 448; m is rounded to the nearest number, v up or down by chance, so that what it should be is kept on average
+ *                (by numbers that an element's place in its tensor and the step alone give: the same arguments give the same bits), and
+ *                not to zero.  A block whose largest size is below 2^-100 counts as zeros.  A gradient that is no finite number spoils its block.
+ *   step         the number of this step, from 1.
+ *   counted      NULL, or DEVICE memory that sparse_conv_adamw_count filled: the step's number is taken from there, and `step` not looked at.
+ * SC_EINVAL: a null or misaligned pointer, a negative count, betas outside 0 <= beta < 1, rate, eps or decay negative or no finite number,
+ * step below 1, unknown types.
+ */
+int sparse_conv_adamw(const sparse_conv_adamw_tensor* tensors, int count, int param_dtype, int grad_dtype, int state_dtype, double rate,
+                      double beta1, double beta2, double eps, double decay, double grad_scale, long long step, const void* counted,
+                      void* stream);
+
+/* For steps in a captured graph: adds 1 to *steps (DEVICE) and leaves in `counted` (DEVICE, SC_ADAMW_COUNTED_BYTES at a multiple of 16)
+ * what a step of that number needs. */
+#define SC_ADAMW_COUNTED_BYTES 16
+int sparse_conv_adamw_count(long long* steps, void* counted, double beta1, double beta2, void* stream);
+
 /* HIP error code of the last failing runtime call made through this handle (0 if none). */
 int sparse_conv_last_hip_error(sparse_conv_t h);
 

@@ -20,6 +20,12 @@ SC_FLAG_UNIFY_NNZ = 1
 SC_EPILOGUE_RELU = 1
 SC_EPILOGUE_MAXPOOL2 = 2
 SC_EMBED_CHANNELS_FIRST, SC_EMBED_TOKENS_64, SC_EMBED_ACCUMULATE = 1, 2, 4
+SC_ACT_NONE, SC_ACT_RELU, SC_ACT_GELU, SC_ACT_SILU = 0, 1, 2, 3
+SC_LINEAR_ACCUMULATE = 1
+SC_LOSS_LABELS_64 = 1
+SC_E4M3 = 4
+SC_ADAMW_BLOCK = 256
+SC_ADAMW_COUNTED_BYTES = 16
 
 # SPARSECONV_LIBRARY names another build of the same library (e.g. an instrumented one)
 LIB_PATH = os.environ.get("SPARSECONV_LIBRARY") or os.path.join(
@@ -33,8 +39,15 @@ EXPORTS = (
     "sparse_conv_probe_lds_read", "sparse_conv_probe_copy",
     "sparse_conv_embed", "sparse_conv_embed_backward_workspace", "sparse_conv_embed_backward",
     "sparse_conv_int8_quantize", "sparse_conv_int8_linear_workspace", "sparse_conv_int8_linear",
+    "sparse_conv_linear_workspace", "sparse_conv_linear", "sparse_conv_linear_backward_workspace", "sparse_conv_linear_backward",
+    "sparse_conv_cross_entropy", "sparse_conv_adamw", "sparse_conv_adamw_count",
     "sparse_conv_last_hip_error", "sparse_conv_strerror", "sparse_conv_destroy",
 )
+
+
+class AdamwTensor(C.Structure):
+    """sparse_conv_adamw_tensor: DEVICE arrays of one tensor of an AdamW step."""
+    _fields_ = [(name, C.c_void_p) for name in ("param", "grad", "m", "v", "m_scale", "v_scale", "master")] + [("count", C.c_longlong)]
 
 
 class SparseConvError(RuntimeError):
@@ -84,6 +97,14 @@ def _load():
     lib.sparse_conv_int8_quantize.argtypes = [vp, vp, vp, n, n, ll, n, vp]
     lib.sparse_conv_int8_linear_workspace.argtypes = [n, n, n, n, n, C.POINTER(ll)]
     lib.sparse_conv_int8_linear.argtypes = [vp, vp, vp, vp, vp, vp, n, n, n, ll, ll, n, n, flags, vp, ll, vp]
+    f64 = C.c_double
+    lib.sparse_conv_linear_workspace.argtypes = [vp, vp, n, n, n, ll, ll, n, C.POINTER(ll)]
+    lib.sparse_conv_linear.argtypes = [vp, vp, vp, vp, vp, vp, n, n, n, ll, ll, ll, ll, n, n, vp, ll, vp]
+    lib.sparse_conv_linear_backward_workspace.argtypes = [vp, vp, vp, vp, vp, vp, n, n, n, ll, ll, ll, n, n, C.POINTER(ll)]
+    lib.sparse_conv_linear_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, n, n, n, ll, ll, ll, n, n, flags, vp, ll, vp]
+    lib.sparse_conv_cross_entropy.argtypes = [vp, vp, vp, vp, vp, n, n, ll, ll, n, f32, flags, vp]
+    lib.sparse_conv_adamw.argtypes = [C.POINTER(AdamwTensor), n, n, n, n, f64, f64, f64, f64, f64, f64, ll, vp, vp]
+    lib.sparse_conv_adamw_count.argtypes = [vp, vp, f64, f64, vp]
     lib.sparse_conv_last_hip_error.argtypes = [vp]
     lib.sparse_conv_strerror.argtypes = [C.c_int]
     lib.sparse_conv_strerror.restype = C.c_char_p
@@ -320,6 +341,61 @@ def sparse_conv_int8_linear(x_ptr: int, x_scale_ptr: int, w_ptr: int, w_scale_pt
     _check(_lib.sparse_conv_int8_linear(x_ptr, x_scale_ptr or None, w_ptr, w_scale_ptr, bias_ptr or None, out_ptr, M, N, K, ldx, ldo,
                                         in_dtype, out_dtype, flags, workspace_ptr or None, workspace_bytes, stream or None),
            "sparse_conv_int8_linear")
+
+
+def sparse_conv_linear_workspace(x_ptr: int, w_ptr: int, M: int, N: int, K: int, ldx: int, ldw: int, dtype: int) -> int:
+    """Bytes of scratch memory that sparse_conv_linear needs for these arguments."""
+    n = C.c_longlong(0)
+    _check(_lib.sparse_conv_linear_workspace(x_ptr, w_ptr, M, N, K, ldx, ldw, dtype, C.byref(n)), "sparse_conv_linear_workspace")
+    return int(n.value)
+
+
+def sparse_conv_linear(x_ptr: int, w_ptr: int, bias_ptr: int, residual_ptr: int, out_ptr: int, z_ptr: int, M: int, N: int, K: int, ldx: int,
+                       ldw: int, ldr: int, ldo: int, dtype: int, activation: int = SC_ACT_NONE, workspace_ptr: int = 0,
+                       workspace_bytes: int = 0, stream: int = 0) -> None:
+    """Enqueue the fully connected layer on DEVICE x [M][K] and w [N][K] into DEVICE out [M][N] (and z, what goes into the activation)."""
+    _check(_lib.sparse_conv_linear(x_ptr, w_ptr, bias_ptr or None, residual_ptr or None, out_ptr, z_ptr or None, M, N, K, ldx, ldw, ldr, ldo,
+                                   dtype, activation, workspace_ptr or None, workspace_bytes, stream or None), "sparse_conv_linear")
+
+
+def sparse_conv_linear_backward_workspace(grad_ptr: int, x_ptr: int, w_ptr: int, grad_x_ptr: int, grad_w_ptr: int, grad_bias_ptr: int, M: int,
+                                          N: int, K: int, ldg: int, ldx: int, ldw: int, dtype: int, activation: int = SC_ACT_NONE) -> int:
+    """Bytes of scratch memory that sparse_conv_linear_backward needs for these arguments."""
+    n = C.c_longlong(0)
+    _check(_lib.sparse_conv_linear_backward_workspace(grad_ptr, x_ptr, w_ptr, grad_x_ptr or None, grad_w_ptr or None, grad_bias_ptr or None,
+                                                      M, N, K, ldg, ldx, ldw, dtype, activation, C.byref(n)),
+           "sparse_conv_linear_backward_workspace")
+    return int(n.value)
+
+
+def sparse_conv_linear_backward(grad_ptr: int, z_ptr: int, x_ptr: int, w_ptr: int, grad_x_ptr: int, grad_w_ptr: int, grad_bias_ptr: int, M: int,
+                                N: int, K: int, ldg: int, ldx: int, ldw: int, dtype: int, activation: int = SC_ACT_NONE, flags: int = 0,
+                                workspace_ptr: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    """Enqueue the layer's gradients: those whose pointers are not 0."""
+    _check(_lib.sparse_conv_linear_backward(grad_ptr, z_ptr or None, x_ptr, w_ptr, grad_x_ptr or None, grad_w_ptr or None, grad_bias_ptr or None,
+                                            M, N, K, ldg, ldx, ldw, dtype, activation, flags, workspace_ptr or None, workspace_bytes,
+                                            stream or None), "sparse_conv_linear_backward")
+
+
+def sparse_conv_cross_entropy(logits_ptr: int, labels_ptr: int, weights_ptr: int, loss_ptr: int, grad_ptr: int, rows: int, classes: int, ldl: int,
+                              ldg: int, dtype: int, scale: float = 1.0, flags: int = 0, stream: int = 0) -> None:
+    """Enqueue the losses of DEVICE logits [rows][classes] and, with grad_ptr, the gradient of the logits."""
+    _check(_lib.sparse_conv_cross_entropy(logits_ptr, labels_ptr, weights_ptr or None, loss_ptr, grad_ptr or None, rows, classes, ldl, ldg, dtype,
+                                          scale, flags, stream or None), "sparse_conv_cross_entropy")
+
+
+def sparse_conv_adamw(tensors: Sequence[AdamwTensor], param_dtype: int, grad_dtype: int, state_dtype: int, rate: float, beta1: float,
+                      beta2: float, eps: float, decay: float, grad_scale: float = 1.0, step: int = 1, counted_ptr: int = 0,
+                      stream: int = 0) -> None:
+    """Enqueue an AdamW step over DEVICE tensors."""
+    array = (AdamwTensor * len(tensors))(*tensors)
+    _check(_lib.sparse_conv_adamw(array, len(tensors), param_dtype, grad_dtype, state_dtype, rate, beta1, beta2, eps, decay, grad_scale, step,
+                                  counted_ptr or None, stream or None), "sparse_conv_adamw")
+
+
+def sparse_conv_adamw_count(steps_ptr: int, counted_ptr: int, beta1: float, beta2: float, stream: int = 0) -> None:
+    """Enqueue the count of a step in DEVICE memory, and what a step of that number needs."""
+    _check(_lib.sparse_conv_adamw_count(steps_ptr, counted_ptr, beta1, beta2, stream or None), "sparse_conv_adamw_count")
 
 
 def sparse_conv_destroy(handle: Optional[int]) -> None:

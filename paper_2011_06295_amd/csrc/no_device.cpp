@@ -22,4 +22,12 @@ int launch_int8_linear(int, int, const Int8Args&, char*, void*) { return (int)hi
 long long embed_grad_workspace(const EmbedGradArgs& a, int) { return a.dim % 2 ? 16ll * a.sentences * a.words : 0; }
 long long int8_workspace(int M, int, int K, int in_dtype, int) { return in_dtype < 3 && K % 2 ? (long long)M * K : 0; }
 
+int launch_linear(int, const LinearArgs&, char*, void*) { return (int)hipErrorNotSupported; }
+int launch_linear_grad(int, const LinearGradArgs&, char*, void*) { return (int)hipErrorNotSupported; }
+int launch_loss(int, const LossArgs&, void*) { return (int)hipErrorNotSupported; }
+int launch_adamw(const AdamwTensor*, int, int, int, bool, const AdamwRule&, void*) { return (int)hipErrorNotSupported; }
+int launch_adamw_count(long long*, AdamwCounted*, double, double, void*) { return (int)hipErrorNotSupported; }
+long long linear_workspace(const LinearArgs& a, int) { return a.K % 2 ? 16ll * a.M * a.K : 0; }
+long long linear_grad_workspace(const LinearGradArgs& a, int) { return a.K % 2 ? 16ll * a.M * a.K : 0; }
+
 }  // namespace sc

@@ -48,6 +48,36 @@ int check_int8(int M, int N, int K, int in_dtype, int out_dtype)
     return SC_OK;
 }
 
+constexpr int kMostLinear = 1 << 20;
+constexpr long long kMostApart = 1ll << 31;
+
+// An array: `bytes` from p on, whose elements have `element` bytes.
+struct Array {
+    const void* p;
+    long long bytes;
+    int element;
+};
+bool missing(const Array& a) { return !a.p || !aligned(a.p, a.element); }
+bool overlap(const Array& a, const Array& b) { return a.p && b.p && overlap(a.p, a.bytes, b.p, b.bytes); }
+
+long long rows_bytes(long long rows, long long cols, long long ld, int b) { return rows > 0 ? ((rows - 1) * ld + cols) * b : 0; }
+
+// Sizes that both directions of the layer share; ld: distances between rows of x, w, and of the output or its gradient.
+int check_linear(int M, int N, int K, long long ldx, long long ldw, long long ldo, int dtype, int activation)
+{
+    if (M < 0 || N < 1 || K < 1 || ldx < K || ldw < K || ldo < N || !is_float(dtype) || activation < SC_ACT_NONE || activation > SC_ACT_SILU) return SC_EINVAL;
+    if (M > kMostLinear || N > kMostLinear || K > kMostLinear || ldx >= kMostApart || ldw >= kMostApart || ldo >= kMostApart) return SC_EUNSUPPORTED;
+    return SC_OK;
+}
+
+static_assert(sizeof(sc::AdamwTensor) == sizeof(sparse_conv_adamw_tensor) && offsetof(sc::AdamwTensor, count) == offsetof(sparse_conv_adamw_tensor, count) &&
+                  offsetof(sc::AdamwTensor, v_scale) == offsetof(sparse_conv_adamw_tensor, v_scale),
+              "the same structure");
+static_assert(sizeof(sc::AdamwCounted) == SC_ADAMW_COUNTED_BYTES, "what the header says");
+
+bool is_beta(double b) { return b >= 0.0 && b < 1.0; }
+bool is_amount(double a) { return a >= 0.0 && a <= 3.4e38; }
+
 int status(int launched) { return launched == 0 ? SC_OK : launched == sc::kTooLarge ? SC_EUNSUPPORTED : SC_EHIP; }
 
 }  // namespace
@@ -155,6 +185,155 @@ int sparse_conv_int8_linear(const void* x, const float* x_scale, const signed ch
     const sc::Int8Args a{x, x_scale, reinterpret_cast<const int8_t*>(w), w_scale, bias, out, M, N, K, (int)pitch, ldx, ldo,
                          (flags & SC_EPILOGUE_RELU) != 0};
     return status(sc::launch_int8_linear(in_dtype, out_dtype, a, static_cast<char*>(workspace), stream));
+}
+
+int sparse_conv_linear_workspace(const void* x, const void* w, int M, int N, int K, long long ldx, long long ldw, int dtype, long long* bytes)
+{
+    if (!bytes) return SC_EINVAL;
+    const int rc = check_linear(M, N, K, ldx, ldw, N, dtype, SC_ACT_NONE);
+    if (rc != SC_OK) return rc;
+    *bytes = 0;
+    if (M == 0) return SC_OK;
+    sc::LinearArgs a{};
+    a.x = x; a.w = w; a.M = M; a.N = N; a.K = K; a.ldx = ldx; a.ldw = ldw;
+    *bytes = sc::linear_workspace(a, dtype);
+    return SC_OK;
+}
+
+int sparse_conv_linear(const void* x, const void* w, const float* bias, const void* residual, void* out, void* z, int M, int N, int K,
+                       long long ldx, long long ldw, long long ldr, long long ldo, int dtype, int activation, void* workspace,
+                       long long workspace_bytes, void* stream)
+{
+    int rc = check_linear(M, N, K, ldx, ldw, ldo, dtype, activation);
+    if (rc == SC_OK && residual) rc = check_linear(M, N, K, ldx, ldw, ldr, dtype, activation);
+    if (rc != SC_OK) return rc;
+    if (M == 0) return SC_OK;
+    const int b = type_bytes(dtype);
+    const Array ax{x, rows_bytes(M, K, ldx, b), b}, aw{w, rows_bytes(N, K, ldw, b), b}, ab{bias, 4ll * N, 4}, ar{residual, rows_bytes(M, N, ldr, b), b},
+        ao{out, rows_bytes(M, N, ldo, b), b}, az{z, rows_bytes(M, N, N, b), b};
+    if (missing(ax) || missing(aw) || missing(ao) || (bias && missing(ab)) || (residual && missing(ar)) || (z && missing(az))) return SC_EINVAL;
+    if (overlap(ao, ax) || overlap(ao, aw) || overlap(ao, ab) || overlap(ao, az) || (overlap(ao, ar) && !(residual == out && ldr == ldo)) ||
+        overlap(az, ax) || overlap(az, aw) || overlap(az, ab) || overlap(az, ar)) return SC_EINVAL;
+    const sc::LinearArgs a{x, w, bias, residual, out, z, ldx, ldw, ldr, ldo, M, N, K, activation};
+    const long long need = sc::linear_workspace(a, dtype);
+    const Array work{workspace, need, 16};
+    if (need > 0 && (missing(work) || workspace_bytes < need || overlap(work, ax) || overlap(work, aw) || overlap(work, ab) || overlap(work, ar) ||
+                     overlap(work, ao) || overlap(work, az))) return SC_EINVAL;
+    return status(sc::launch_linear(dtype, a, static_cast<char*>(workspace), stream));
+}
+
+int sparse_conv_linear_backward_workspace(const void* grad, const void* x, const void* w, const void* grad_x, const void* grad_w,
+                                          const void* grad_bias, int M, int N, int K, long long ldg, long long ldx, long long ldw,
+                                          int dtype, int activation, long long* bytes)
+{
+    if (!bytes) return SC_EINVAL;
+    const int rc = check_linear(M, N, K, ldx, ldw, ldg, dtype, activation);
+    if (rc != SC_OK) return rc;
+    *bytes = 0;
+    if (M == 0) return SC_OK;
+    sc::LinearGradArgs a{};
+    a.grad = grad; a.x = x; a.w = w; a.M = M; a.N = N; a.K = K; a.ldg = ldg; a.ldx = ldx; a.ldw = ldw; a.act = activation;
+    a.grad_x = const_cast<void*>(grad_x);
+    a.grad_w = const_cast<void*>(grad_w);
+    a.grad_bias = static_cast<float*>(const_cast<void*>(grad_bias));
+    *bytes = sc::linear_grad_workspace(a, dtype);
+    return SC_OK;
+}
+
+int sparse_conv_linear_backward(const void* grad, const void* z, const void* x, const void* w, void* grad_x, void* grad_w,
+                                float* grad_bias, int M, int N, int K, long long ldg, long long ldx, long long ldw, int dtype,
+                                int activation, unsigned flags, void* workspace, long long workspace_bytes, void* stream)
+{
+    const int rc = check_linear(M, N, K, ldx, ldw, ldg, dtype, activation);
+    if (rc != SC_OK) return rc;
+    if (flags & ~static_cast<unsigned>(SC_LINEAR_ACCUMULATE)) return SC_EINVAL;
+    const int b = type_bytes(dtype);
+    if (activation == SC_ACT_NONE) z = nullptr;
+    if (!grad_w) x = nullptr;
+    if (!grad_x) w = nullptr;
+    const Array ag{grad, rows_bytes(M, N, ldg, b), b}, az{z, rows_bytes(M, N, N, b), b}, ax{x, rows_bytes(M, K, ldx, b), b}, aw{w, rows_bytes(N, K, ldw, b), b},
+        gx{grad_x, rows_bytes(M, K, K, b), b}, gw{grad_w, rows_bytes(N, K, K, b), b}, gb{grad_bias, 4ll * N, 4};
+    if ((grad_x && missing(gx)) || (grad_w && missing(gw)) || (grad_bias && missing(gb))) return SC_EINVAL;
+    if (M > 0 && ((missing(ag) && (grad_x || grad_w || grad_bias)) || (activation != SC_ACT_NONE && missing(az)) || (grad_w && missing(ax)) || (grad_x && missing(aw)))) return SC_EINVAL;
+    const Array written[] = {gx, gw, gb}, read[] = {ag, az, ax, aw};
+    for (int i = 0; i < 3; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (overlap(written[i], written[j])) return SC_EINVAL;
+        for (const Array& r : read)
+            if (overlap(written[i], r)) return SC_EINVAL;
+    }
+    sc::LinearGradArgs a{grad, z, x, w, grad_x, grad_w, grad_bias, ldg, ldx, ldw, M, N, K, activation, (flags & SC_LINEAR_ACCUMULATE) != 0};
+    if (M == 0) {
+        if (a.accumulate) return SC_OK;
+        return status(sc::launch_linear_grad(dtype, a, nullptr, stream));
+    }
+    const long long need = sc::linear_grad_workspace(a, dtype);
+    const Array work{workspace, need, 16};
+    if (need > 0) {
+        if (missing(work) || workspace_bytes < need) return SC_EINVAL;
+        for (const Array& r : read)
+            if (overlap(work, r)) return SC_EINVAL;
+        for (const Array& r : written)
+            if (overlap(work, r)) return SC_EINVAL;
+    }
+    return status(sc::launch_linear_grad(dtype, a, static_cast<char*>(workspace), stream));
+}
+
+int sparse_conv_cross_entropy(const void* logits, const void* labels, const float* weights, float* loss, void* grad, int rows,
+                              int classes, long long ldl, long long ldg, int dtype, float scale, unsigned flags, void* stream)
+{
+    if (rows < 0 || classes < 1 || ldl < classes || (grad && ldg < classes) || !is_float(dtype) || (flags & ~static_cast<unsigned>(SC_LOSS_LABELS_64))) return SC_EINVAL;
+    constexpr int kMostClasses = 0x7fffffff - (1 << 20);
+    if (classes > kMostClasses || rows > kMostClasses || too_many(rows, ldl) || (grad && too_many(rows, ldg))) return SC_EUNSUPPORTED;
+    if (rows == 0) return SC_OK;
+    const int b = type_bytes(dtype), lb = (flags & SC_LOSS_LABELS_64) ? 8 : 4;
+    const Array al{logits, rows_bytes(rows, classes, ldl, b), b}, an{labels, (long long)rows * lb, lb}, aw{weights, rows * 4ll, 4}, as{loss, rows * 4ll, 4},
+        ag{grad, rows_bytes(rows, classes, ldg, b), b};
+    if (missing(al) || missing(an) || missing(as) || (weights && missing(aw)) || (grad && missing(ag))) return SC_EINVAL;
+    if (overlap(as, al) || overlap(as, an) || overlap(as, aw) || overlap(as, ag) || overlap(ag, an) || overlap(ag, aw) ||
+        (overlap(ag, al) && !(grad == logits && ldg == ldl))) return SC_EINVAL;
+    const sc::LossArgs a{logits, labels, weights, loss, grad, ldl, ldg, rows, classes, scale, (flags & SC_LOSS_LABELS_64) != 0};
+    return status(sc::launch_loss(dtype, a, stream));
+}
+
+int sparse_conv_adamw(const sparse_conv_adamw_tensor* tensors, int count, int param_dtype, int grad_dtype, int state_dtype, double rate,
+                      double beta1, double beta2, double eps, double decay, double grad_scale, long long step, const void* counted,
+                      void* stream)
+{
+    if (count < 0 || (count > 0 && !tensors) || !is_float(param_dtype) || !is_float(grad_dtype) || (state_dtype != SC_F32 && state_dtype != SC_E4M3)) return SC_EINVAL;
+    if (param_dtype != SC_F32 && grad_dtype != SC_F32 && grad_dtype != param_dtype) return SC_EINVAL;
+    if (!is_amount(rate) || !is_amount(eps) || !is_amount(decay) || !is_beta(beta1) || !is_beta(beta2) || !std::isfinite(grad_scale)) return SC_EINVAL;
+    if (counted ? !aligned(counted, 16) : step < 1) return SC_EINVAL;
+    const bool small = state_dtype == SC_E4M3;
+    for (int i = 0; i < count; ++i) {
+        const sparse_conv_adamw_tensor& t = tensors[i];
+        if (t.count < 0 || (t.master != nullptr) != (tensors[0].master != nullptr)) return SC_EINVAL;
+        if (t.count > kMaxElements) return SC_EUNSUPPORTED;
+        if (t.count == 0) continue;
+        const int pb = type_bytes(param_dtype), gb = type_bytes(grad_dtype), sb = small ? 1 : 4;
+        const long long scales = (t.count + SC_ADAMW_BLOCK - 1) / SC_ADAMW_BLOCK * 4;
+        const Array arrays[] = {{t.param, t.count * pb, pb}, {t.grad, t.count * gb, gb}, {t.m, t.count * sb, sb}, {t.v, t.count * sb, sb},
+                                {t.master, t.count * 4, 4}, {small ? t.m_scale : nullptr, scales, 4}, {small ? t.v_scale : nullptr, scales, 4}};
+        for (int j = 0; j < 7; ++j) {
+            if (j == 4 ? t.master && missing(arrays[j]) : (j < 4 || small) && missing(arrays[j])) return SC_EINVAL;
+            for (int k = 0; k < j; ++k)
+                if (overlap(arrays[j], arrays[k])) return SC_EINVAL;
+        }
+    }
+    if (count == 0) return SC_OK;
+    sc::AdamwRule rule{(float)rate, (float)(1.0 - rate * decay), (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps,
+                       (float)grad_scale, 1.f, 1.f, (unsigned)step, static_cast<const sc::AdamwCounted*>(counted)};
+    if (!counted) {
+        rule.c1 = (float)(1.0 / (1.0 - std::pow(beta1, (double)step)));
+        rule.c2 = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
+    }
+    return status(sc::launch_adamw(reinterpret_cast<const sc::AdamwTensor*>(tensors), count, param_dtype, grad_dtype, small, rule, stream));
+}
+
+int sparse_conv_adamw_count(long long* steps, void* counted, double beta1, double beta2, void* stream)
+{
+    if (!steps || !counted || !aligned(steps, 8) || !aligned(counted, 16) || overlap(steps, 8, counted, SC_ADAMW_COUNTED_BYTES) || !is_beta(beta1) || !is_beta(beta2)) return SC_EINVAL;
+    return status(sc::launch_adamw_count(steps, static_cast<sc::AdamwCounted*>(counted), std::log(beta1), std::log(beta2), stream));
 }
 
 }  // extern "C"

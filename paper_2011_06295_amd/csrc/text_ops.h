@@ -56,4 +56,59 @@ int int8_own_kernel(int M, int N, int K, int in_dtype);      // of the kernel th
 long long int8_workspace(int M, int N, int K, int in_dtype, int out_dtype);
 int launch_int8_linear(int in_dtype, int out_dtype, const Int8Args& a, char* workspace, void* stream);
 
+
+struct LinearArgs {
+    const void *x, *w;     // [M][ldx], [N][ldw]
+    const float* bias;     // or null
+    const void* residual;  // [M][ldr] or null
+    void *out, *z;         // [M][ldo]; [M][N] or null
+    long long ldx, ldw, ldr, ldo;
+    int M, N, K, act;
+};
+long long linear_workspace(const LinearArgs& a, int dtype);
+int launch_linear(int dtype, const LinearArgs& a, char* workspace, void* stream);
+
+struct LinearGradArgs {
+    const void *grad, *z, *x, *w;      // [M][ldg], [M][N] or null, [M][ldx], [N][ldw]
+    void *grad_x, *grad_w;             // [M][K], [N][K], either or null
+    float* grad_bias;                  // [N] or null
+    long long ldg, ldx, ldw;
+    int M, N, K, act;
+    bool accumulate;
+};
+long long linear_grad_workspace(const LinearGradArgs& a, int dtype);
+int launch_linear_grad(int dtype, const LinearGradArgs& a, char* workspace, void* stream);
+
+struct LossArgs {
+    const void *logits, *labels;       // [rows][ldl], [rows]
+    const float* weights;              // [rows] or null
+    float* loss;                       // [rows]
+    void* grad;                        // [rows][ldg] or null
+    long long ldl, ldg;
+    int rows, classes;
+    float scale;
+    bool wide;                         // 64-bit labels
+};
+int launch_loss(int dtype, const LossArgs& a, void* stream);
+
+// Exactly sparse_conv_adamw_tensor of the public header.
+struct AdamwTensor {
+    void* param;
+    const void* grad;
+    void *m, *v;
+    float *m_scale, *v_scale, *master;
+    long long count;
+};
+struct AdamwCounted {      // what a step on a count in device memory reads
+    float c1, c2;
+    unsigned step, unused;
+};
+struct AdamwRule {
+    float rate, keep, beta1, rest1, beta2, rest2, eps, grad_scale, c1, c2;      // keep = 1 - rate decay; rest = 1 - beta
+    unsigned step;
+    const AdamwCounted* counted;       // or null; else c1, c2 and step are there
+};
+int launch_adamw(const AdamwTensor* tensors, int count, int param_dtype, int grad_dtype, bool small, const AdamwRule& rule, void* stream);
+int launch_adamw_count(long long* count, AdamwCounted* counted, double log_beta1, double log_beta2, void* stream);
+
 }  // namespace sc

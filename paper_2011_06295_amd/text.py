@@ -1,10 +1,11 @@
-"""A text model around the sparse convolutions: word vectors, their gradient and a fully connected layer in 8-bit integers.
+"""A text model around the sparse convolutions: word vectors, their gradient and a fully connected layer in 8-bit integers; and what trains
+the layers behind the convolutions: a fully connected layer with its gradients, a classifier's loss, AdamW steps.
 
-`Embedding` and `Int8Linear` call the library's operators (include/sparse_conv.h) on PyTorch tensors.  A call's tensors are checked,
+`Embedding`, `Int8Linear`, `Linear`, `cross_entropy` and `AdamW` call the library's operators (include/sparse_conv.h) on PyTorch tensors.  A call's tensors are checked,
 and its output and scratch memory allocated, by csrc/text_torch.cpp: calls of few tokens are bound by the host.  There is no fallback.
 
 Autograd does not record these calls: their outputs have no gradient function, also where a table or an input requires a gradient.
-`Embedding.backward` is called by the program itself.  A write into a given `out` raises that tensor's version.
+`Embedding.backward` and `Linear.backward` are called by the program itself.  A write into a given `out` raises that tensor's version.
 """
 from __future__ import annotations
 
@@ -29,7 +30,8 @@ def _bind():
     import ctypes as C
     lib = B.raw_library()
     _calls.bind(*(C.cast(getattr(lib, "sparse_conv_" + name), C.c_void_p).value for name in (
-        "embed", "embed_backward_workspace", "embed_backward", "int8_linear_workspace", "int8_linear")))
+        "embed", "embed_backward_workspace", "embed_backward", "int8_linear_workspace", "int8_linear", "linear_workspace", "linear",
+        "linear_backward_workspace", "linear_backward", "cross_entropy", "adamw", "adamw_count")))
 
 
 _bind()
@@ -147,3 +149,128 @@ class Int8Linear:
         if out.__class__ is int:
             B._check(out, "sparse_conv_int8_linear")
         return out
+
+
+_ACTIVATIONS = {None: B.SC_ACT_NONE, "relu": B.SC_ACT_RELU, "gelu": B.SC_ACT_GELU, "silu": B.SC_ACT_SILU}
+
+
+class Linear:
+    """Fully connected layer act(x W^T + bias) + residual in the weight's type, summed in fp32, and its gradients.  The weight and the bias are
+    read when a call runs: a step that changes them in place needs no new layer.  Autograd does not record the calls: `backward` is called
+    by the program itself."""
+
+    def __init__(self, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, activation: Optional[str] = None):
+        """weight: CUDA tensor [N][K] of fp32, binary16 or bfloat16 (kept, not copied; rows may lie apart); bias: fp32 [N] or None;
+        activation: None, "relu", "gelu" (x Phi(x)) or "silu"."""
+        if not weight.is_cuda or weight.dtype not in _DTYPES or weight.dim() != 2 or min(weight.shape) < 1 or (weight.stride(1) != 1 and weight.shape[1] > 1):
+            raise ValueError("weight must be a CUDA tensor [N][K] of fp32, binary16 or bfloat16 whose rows are contiguous")
+        if bias is not None and (bias.shape != weight.shape[:1] or bias.dtype != torch.float32 or bias.device != weight.device or not bias.is_contiguous()):
+            raise ValueError("bias must be a contiguous fp32 tensor [N] on the weight's device")
+        if activation not in _ACTIVATIONS:
+            raise ValueError('activation must be None, "relu", "gelu" or "silu"')
+        self.weight, self.bias, self.activation = weight, bias, activation
+        self.N, self.K = weight.shape
+        self._act = _ACTIVATIONS[activation]
+        self._device = weight.get_device()
+
+    def forward(self, x, residual=None, keep: bool = False, out=None):
+        """[..., N] of x [..., K] (contiguous, or [M][K] with contiguous rows at any stride), plus residual [..., N], which may be `out` itself.
+        keep: (output, z), z what went into the activation, as `backward` needs it."""
+        if self._device != _current_device():      # the library's calls run on the current device
+            with torch.cuda.device(self._device):
+                return self.forward(x, residual, keep, out)
+        out = _calls.layer(x, self.weight, self.bias, residual, out, keep, self._act, _current_stream(self._device))
+        if out.__class__ is int:
+            B._check(out, "sparse_conv_linear")
+        return out
+
+    def backward(self, grad, x, z=None, grad_x=True, grad_weight=True, grad_bias=True, accumulate: bool = False):
+        """(gradient of x, of the weight, of the bias (fp32)) from the gradient of the output, which is the residual's as well.  x: what
+        forward was given (None where grad_weight is False); z: what it kept, needed with an activation.  Each of the three is made (True), left out
+        (False, None comes back) or written to the tensor given; accumulate: the weight's and the bias's are added to those tensors."""
+        if self._device != _current_device():
+            with torch.cuda.device(self._device):
+                return self.backward(grad, x, z, grad_x, grad_weight, grad_bias, accumulate)
+        if self.bias is None and grad_bias is True:
+            grad_bias = False
+        out = _calls.layer_backward(grad, x, self.weight, z, grad_x, grad_weight, grad_bias, accumulate, self._act, _current_stream(self._device))
+        if out.__class__ is int:
+            B._check(out, "sparse_conv_linear_backward")
+        return out
+
+
+def cross_entropy(logits, labels, weights=None, grad=True, scale: float = 1.0):
+    """(losses fp32 [...], gradient of their sum towards the logits [..., classes] or None) of logits [..., classes] and labels [...]:
+    scale * weights * -log of the softmax at the label.  A row whose label is no class, or whose weight is 0, counts for nothing.
+    grad: True, False or the tensor to write to, which may be `logits` itself.  Autograd does not record the call."""
+    if not isinstance(logits, torch.Tensor) or not logits.is_cuda:
+        raise ValueError("logits must be a CUDA tensor [..., classes] of fp32, binary16 or bfloat16")
+    device = logits.get_device()
+    if device != _current_device():
+        with torch.cuda.device(device):
+            return cross_entropy(logits, labels, weights, grad, scale)
+    out = _calls.cross_entropy(logits, labels, weights, grad, float(scale), _current_stream(device))
+    if out.__class__ is int:
+        B._check(out, "sparse_conv_cross_entropy")
+    return out
+
+
+class AdamW:
+    """AdamW steps over many tensors at once, in place: m = b1 m + (1 - b1) g, v = b2 v + (1 - b2) g^2,
+    p = (1 - rate decay) p - rate (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps), in fp32.
+
+    States (`m`, `v`, with 8 bits `m_scale` and `v_scale`, with master `master`) are one array each for all tensors; tensor i's begin at element
+    `begins[i]`, a whole number of blocks of 256.  They are zero at first and can be copied out and in, with `steps`, the number of
+    steps taken."""
+
+    def __init__(self, params, rate: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, decay: float = 0.01, bits: int = 32, master: bool = False,
+                 counted: bool = False):
+        """params: contiguous CUDA tensors of one type (fp32, binary16, bfloat16) and device.  bits: 32, or 8: numbers of 8 bits (e4m3)
+        with an fp32 scale for each block of 256.  master: steps apply to fp32 weights kept here, the parameters receive them rounded
+        (else a 16-bit parameter loses every change below half its own rounding).  counted: the number of steps is counted in device
+        memory, for steps recorded in a graph (`steps` is then a tensor)."""
+        self.params = list(params)
+        if not self.params or any(not isinstance(p, torch.Tensor) or not p.is_cuda or p.dtype not in _DTYPES or not p.is_contiguous() for p in self.params):
+            raise ValueError("params must be contiguous CUDA tensors of fp32, binary16 or bfloat16")
+        first = self.params[0]
+        if any(p.dtype != first.dtype or p.device != first.device for p in self.params):
+            raise ValueError("params must be of one type and on one device (an optimizer for each)")
+        spans = sorted((p.data_ptr(), p.data_ptr() + p.numel() * p.element_size()) for p in self.params if p.numel())
+        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+            raise ValueError("params must not share memory")
+        if bits not in (8, 32):
+            raise ValueError("bits must be 8 or 32")
+        beta1, beta2 = (float(b) for b in betas)
+        self.rate, self.betas, self.eps, self.decay, self.bits = float(rate), (beta1, beta2), float(eps), float(decay), bits
+        if not (0.0 <= beta1 < 1.0 and 0.0 <= beta2 < 1.0 and self.rate >= 0.0 and self.eps >= 0.0 and self.decay >= 0.0):
+            raise ValueError("rate, eps and decay must not be negative, betas at least 0 and below 1")
+        self.begins = [0]
+        for p in self.params:
+            self.begins.append(self.begins[-1] + -(-p.numel() // B.SC_ADAMW_BLOCK) * B.SC_ADAMW_BLOCK)
+        total, device = self.begins.pop(), first.device
+        self.m, self.v = (torch.zeros(total, dtype=torch.float32 if bits == 32 else torch.float8_e4m3fn, device=device) for _ in range(2))
+        self.m_scale = self.v_scale = self.master = None
+        if bits == 8:
+            self.m_scale, self.v_scale = (torch.zeros(total // B.SC_ADAMW_BLOCK, device=device) for _ in range(2))
+        if master:
+            self.master = torch.zeros(total, device=device)
+            for begin, p in zip(self.begins, self.params):
+                self.master[begin:begin + p.numel()].copy_(p.detach().reshape(-1))
+        self.steps = torch.zeros(1, dtype=torch.int64, device=device) if counted else 0
+        self._counted = torch.zeros(B.SC_ADAMW_COUNTED_BYTES // 4, device=device) if counted else None
+        self._device = first.get_device()
+
+    def step(self, grads, scale: float = 1.0):
+        """One step on scale * grads: a contiguous tensor like each parameter (all fp32 or of the parameters' type; any of the three types where
+        parameters are fp32), or None, which leaves the parameter and its states alone."""
+        if self._device != _current_device():
+            with torch.cuda.device(self._device):
+                return self.step(grads, scale)
+        grads = grads if isinstance(grads, list) else list(grads)
+        counted = None if self._counted is None else (self.steps, self._counted)
+        rule = (self.rate, *self.betas, self.eps, self.decay, scale)
+        rc = _calls.adamw(self.params, grads, self.m, self.v, self.m_scale, self.v_scale, self.master, counted, rule,
+                          self.steps + 1 if counted is None else 1, _current_stream(self._device))
+        B._check(rc, "sparse_conv_adamw")
+        if counted is None:
+            self.steps += 1
