@@ -39,24 +39,53 @@ struct ProductArgs {
 
 // ---------------------------------------------------------------- activations
 
-__device__ __forceinline__ float activate(float z, int act)
+constexpr float kLog2e = 1.4426950408889634f;
+
+constexpr float kNormal[7] = {-2.302209377e+00f, -1.048351228e-01f, 9.404921002e-05f, 1.595799404e-04f, -1.143983536e-05f, 3.816313949e-07f, -5.067239961e-09f};
+
+// The normal distribution's Phi.  log(Phi(z) / Phi(-z)) is odd and smooth: z times a polynomial of z^2, fitted here up to |z| = 5.5 for
+// the least error of Phi, 1.3e-7 (beyond, Phi is within 1e-7 of 0 or 1, and the polynomial goes on towards infinity).  Two transcendental
+// instructions, where erff takes the longest part of an epilogue.
+__device__ __forceinline__ float normal(float z)
 {
-    if (act == kRelu) return z < 0.f ? 0.f : z;
-    if (act == kGelu) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-    if (act == kSilu) return z / (1.f + __expf(-z));
+    const float u = z * z;
+    float p = kNormal[6];
+#pragma unroll
+    for (int i = 5; i >= 0; --i) p = fmaf(p, u, kNormal[i]);
+    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(p * z));
+}
+
+__device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * z)); }
+
+template <int kAct>
+__device__ __forceinline__ float activate(float z)
+{
+    if (kAct == kRelu) return z < 0.f ? 0.f : z;
+    if (kAct == kGelu) return z * normal(z);
+    if (kAct == kSilu) return z * logistic(z);
     return z;
 }
 
 // The derivative.
-__device__ __forceinline__ float slope(float z, int act)
+template <int kAct>
+__device__ __forceinline__ float slope(float z)
 {
-    if (act == kRelu) return z > 0.f ? 1.f : z == z ? 0.f : z;
-    if (act == kGelu) return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * __expf(-0.5f * z * z) * 0.39894228040143268f;
-    if (act == kSilu) {
-        const float s = 1.f / (1.f + __expf(-z));
-        return s * (1.f + z * (1.f - s));
+    if (kAct == kRelu) return z > 0.f ? 1.f : z == z ? 0.f : z;
+    if (kAct == kGelu) return fmaf(z * 0.39894228040143268f, __builtin_amdgcn_exp2f(-0.5f * kLog2e * z * z), normal(z));
+    if (kAct == kSilu) {
+        const float s = logistic(z);
+        return s * fmaf(z, 1.f - s, 1.f);
     }
     return 1.f;
+}
+
+// f with the activation as a constant: one branch for all the elements that it takes.
+template <class F>
+__device__ __forceinline__ void with_activation(int act, F&& f)
+{
+    if (act == kRelu) f(std::integral_constant<int, kRelu>{});
+    else if (act == kGelu) f(std::integral_constant<int, kGelu>{});
+    else if (act == kSilu) f(std::integral_constant<int, kSilu>{});
 }
 
 // ---------------------------------------------------------------- products
@@ -109,9 +138,10 @@ __device__ __forceinline__ void finish(const ProductArgs& a, const float (&sum)[
                 if (e < count) to[e] = y[e];
     };
     if (a.z) store(static_cast<T*>(a.z) + (size_t)m * a.N + n);
-    if (a.act != kNone)
+    with_activation(a.act, [&](auto act) {
 #pragma unroll
-        for (int e = 0; e < C; ++e) v[e] = activate(v[e], a.act);
+        for (int e = 0; e < C; ++e) v[e] = activate<act>(v[e]);
+    });
     if (a.residual) {
         const T* from = static_cast<const T*>(a.residual) + (size_t)m * a.ldr + n;
         if (count >= C) {
@@ -477,6 +507,413 @@ __global__ __launch_bounds__(256) void linear_join_kernel(ProductArgs a)
     finish<T, 4>(a, sum, bias, m, n, a.N - n);
 }
 
+// ---------------------------------------------------------------- products of arrays as they lie
+
+// One operand: element (i, c) at p[i * ld + c] (its rows lie along the sum) or, "turned", at p[c * ld + i].  z: or null, else the element is
+// p's times the activation's slope at z's, rounded; z has no gaps.
+struct Side {
+    const void *p, *z;
+    long long ld, ldz;
+    int count;                          // of i
+};
+
+// kRows i by 128 bytes of c of an operand, a thread's share: pieces of 16 bytes, from any element on.  Loads are issued by no branch at all, so that
+// those of several steps can be in flight (after one the compiler waits for all that came before): a piece that would reach outside is the nearest
+// one inside, and `put` moves it into place, with zeros for c past the sum's end.  Outputs of i's that are not there are never stored.
+// kFew: the operand has rows of less than a piece, which are loaded one by one.
+template <class T, int kRows, bool kTurned, bool kSlope, bool kFew>
+struct Share {
+    static constexpr int kCount = 16 / sizeof(T), kC = 128 / sizeof(T), kPieces = kRows * 8 / 256;
+    typedef typename Piece<T>::type V;
+    V v[kPieces], z[kSlope ? kPieces : 1];
+
+    // Turned: pairs of pieces, of c and c + 1, so that words of two (pairs of words, for fp32) go to LDS.
+    static __device__ __forceinline__ void place(int t, int& i, int& c)
+    {
+        if constexpr (kTurned) {
+            constexpr int kAcross = kRows / kCount;      // pieces of one c
+            const int pair = t / 2 * 256 + (int)threadIdx.x;
+            i = pair % kAcross * kCount;
+            c = pair / kAcross * 2 + t % 2;
+        } else {
+            const int piece = t * 256 + (int)threadIdx.x;
+            i = piece / 8;
+            c = piece % 8 * kCount;
+        }
+    }
+
+    // How far a piece of a turned operand begins before its i, to end within the operand.
+    static __device__ __forceinline__ int back(int count, int i) { return max(i + kCount - count, 0); }
+
+    static __device__ __forceinline__ V load(const T* from, long long ld, int count, int i, int c, int c_end)
+    {
+        V v;
+        if constexpr (kTurned) {
+            const T* row = from + (size_t)min(c, c_end - 1) * ld;
+            if constexpr (kFew) {
+#pragma unroll
+                for (int e = 0; e < kCount; ++e) v[e] = row[max(min(i + e - back(count, i), count - 1), 0)];
+            } else {
+                v = *reinterpret_cast<const V*>(row + min(i, count - kCount));
+            }
+        } else {
+            const T* row = from + (size_t)min(i, count - 1) * ld;
+            if constexpr (kFew) {
+#pragma unroll
+                for (int e = 0; e < kCount; ++e) v[e] = row[min(c + e, c_end - 1)];
+            } else {
+                v = *reinterpret_cast<const V*>(row + min(c, c_end - kCount));
+            }
+        }
+        return v;
+    }
+
+    __device__ __forceinline__ void fetch(const Side& s, int i0, int c0, int c_end)
+    {
+#pragma unroll
+        for (int t = 0; t < kPieces; ++t) {
+            int i, c;
+            place(t, i, c);
+            v[t] = load(static_cast<const T*>(s.p), s.ld, s.count, i0 + i, c0 + c, c_end);
+            if constexpr (kSlope) z[t] = load(static_cast<const T*>(s.z), s.ldz, s.count, i0 + i, c0 + c, c_end);
+        }
+    }
+
+    // The last step: a piece of a row moves down, and what lies past the end becomes zero.
+    static __device__ __forceinline__ void end(V& v, int c, int c_end)
+    {
+        if constexpr (kTurned || kFew) {
+#pragma unroll
+            for (int e = 0; e < kCount; ++e) v[e] = c + (kTurned ? 0 : e) < c_end ? v[e] : (T)0.f;
+        } else {
+            const int moved = max(c - (c_end - kCount), 0);
+            const unsigned __int128 bits = __builtin_bit_cast(unsigned __int128, v);
+            v = __builtin_bit_cast(V, moved < kCount ? bits >> (moved * 8 * (int)sizeof(T)) : (unsigned __int128)0);
+        }
+    }
+
+    // Multiplies by the slope; what is not rounded yet is added to `sums`, an element of the thread's pairs of pieces each (turned alone).
+    __device__ __forceinline__ void apply(int act, float* sums)
+    {
+        auto all = [&](auto act) {
+#pragma unroll
+            for (int t = 0; t < kPieces; ++t)
+#pragma unroll
+                for (int e = 0; e < kCount; ++e) {
+                    float g = (float)v[t][e];
+                    if constexpr (act != kNone) {
+                        g *= slope<act>((float)z[t][e]);
+                        v[t][e] = (T)g;
+                    }
+                    if constexpr (kTurned) sums[t / 2 * kCount + e] += g;
+                }
+        };
+        if constexpr (kSlope) with_activation(act, all);
+        else all(std::integral_constant<int, kNone>{});
+    }
+
+    // Row i of LDS is 128 bytes along c, its pieces permuted by the row as in the tile kernel, and by 16 rows more for what is turned.
+    static __device__ __forceinline__ int turn_of(int i) { return ((i >> 1) ^ (i >> 4)) & 7; }
+
+    // kSums: the sums of what goes to LDS are wanted.
+    template <bool kSums>
+    __device__ __forceinline__ void put(const Side& s, int act, int i0, int c0, int c_end, char* to, float* sums)
+    {
+        if (c0 + kC > c_end)
+#pragma unroll
+            for (int t = 0; t < kPieces; ++t) {
+                int i, c;
+                place(t, i, c);
+                end(v[t], c0 + c, c_end);
+                if constexpr (kSlope) end(z[t], c0 + c, c_end);
+            }
+        if constexpr (kSlope || kSums) apply(act, sums);
+#pragma unroll
+        for (int t = 0; t < kPieces; t += kTurned ? 2 : 1) {
+            int i, c;
+            place(t, i, c);
+            if constexpr (!kTurned) {
+                typedef T A __attribute__((ext_vector_type(16 / sizeof(T))));
+                *reinterpret_cast<A*>(to + i * 128 + (((c / kCount) ^ turn_of(i)) << 4)) = v[t];
+            } else {
+                const int byte = c * (int)sizeof(T), first = back(s.count, i0 + i);      // (i's that an earlier piece has as well)
+#pragma unroll
+                for (int e = 0; e < kCount; ++e) {
+                    typedef T two __attribute__((ext_vector_type(2)));
+                    const int row = i + e - first;
+                    if (e >= first) *reinterpret_cast<two*>(to + row * 128 + (((byte >> 4) ^ turn_of(row)) << 4) + (byte & 15)) = two{v[t][e], v[t + 1][e]};
+                }
+            }
+        }
+    }
+};
+
+// 32 I by 32 J sums of a workgroup of four wavefronts, over c of c_begin .. c_end - 1.  The bytes of the kAhead steps that follow are on their way to
+// registers while one is multiplied from LDS (two buffers, a barrier a step): a step takes 0.2 us of work, its loads 1 us and more.
+constexpr int kAhead = 3;
+
+template <class T, int I, int J, bool kTurnedA, bool kTurnedB, bool kSlope, bool kFew>
+__device__ __forceinline__ void direct_tile(const Side& a, const Side& b, int act, int i0, int j0, int c_begin, int c_end, char* lds, float4v (&acc)[I][J], float* sums)
+{
+    constexpr int kA = 32 * I * 128, kBuffer = kA + 32 * J * 128, kC = 128 / sizeof(T);
+    Share<T, 32 * I, kTurnedA, kSlope, kFew> of_a[kAhead];
+    Share<T, 32 * J, kTurnedB, false, kFew> of_b[kAhead];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4, wi = wave & 1, wj = wave >> 1;
+    each<kAhead>([&](auto d) {
+        of_a[d].fetch(a, i0, c_begin + d * kC, c_end);
+        of_b[d].fetch(b, j0, c_begin + d * kC, c_end);
+    });
+    int buffer = 0;
+    for (int first = c_begin; first < c_end; first += kAhead * kC)
+        each<kAhead>([&](auto d) {      // (what lies past the end is zeros: the steps of a round are not skipped, whose loads would have to be waited for)
+            const int c = first + d * kC;
+            of_a[d].template put<kTurnedA>(a, act, i0, c, c_end, lds + buffer, sums);
+            of_b[d].template put<false>(b, act, j0, c, c_end, lds + buffer + kA, nullptr);
+            __syncthreads();
+            of_a[d].fetch(a, i0, c + kAhead * kC, c_end);
+            of_b[d].fetch(b, j0, c + kAhead * kC, c_end);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                int4v fa[I], fb[J];
+#pragma unroll
+                for (int i = 0; i < I; ++i) {
+                    const int row = (wi * I + i) * 16 + r;
+                    fa[i] = *reinterpret_cast<const int4v*>(lds + buffer + row * 128 + (((h * 4 + q) ^ of_a[d].turn_of(row)) << 4));
+                }
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    const int row = (wj * J + j) * 16 + r;
+                    fb[j] = *reinterpret_cast<const int4v*>(lds + buffer + kA + row * 128 + (((h * 4 + q) ^ of_b[d].turn_of(row)) << 4));
+                }
+#pragma unroll
+                for (int i = 0; i < I; ++i)
+#pragma unroll
+                    for (int j = 0; j < J; ++j) acc[i][j] = multiplied<T>(acc[i][j], fb[j], fa[i]);
+            }
+            buffer = kBuffer - buffer;
+        });
+}
+
+// A tile's sums to the output (or to its part's sums): lane l holds row l % 16 of a's block and rows 4 (l / 16) .. + 3 of b's.
+template <class T, int I, int J>
+__device__ __forceinline__ void direct_store(const ProductArgs& a, int part, int m0, int n0, const float4v (&acc)[I][J])
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4, wi = wave & 1, wj = wave >> 1;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        const int n = n0 + (wj * J + j) * 16 + q * 4;
+        if (n >= a.N) continue;
+        float bias[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bias[e] = a.bias && n + e < a.N ? a.bias[n + e] : 0.f;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int m = m0 + (wi * I + i) * 16 + r;
+            if (m >= a.M) continue;
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = acc[i][j][e];
+            if (a.partial) {
+                float* to = a.partial + ((size_t)part * a.M + m) * a.N + n;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (n + e < a.N) to[e] = v[e];
+            } else {
+                finish<T, 4>(a, v, bias, m, n, a.N - n);
+            }
+        }
+    }
+}
+
+template <int I, int J>
+__device__ __forceinline__ void zero(float4v (&acc)[I][J])
+{
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+        for (int j = 0; j < J; ++j) acc[i][j] = float4v{0.f, 0.f, 0.f, 0.f};
+}
+
+// The layer on rows at any address, a part of the sum a workgroup.  `a` says where the output goes; a.steps: of 128 bytes, a part.
+template <class T, int I, int J, bool kFew>
+__global__ __launch_bounds__(256) void linear_direct_kernel(ProductArgs a, int K, long long ldx, long long ldw)
+{
+    __shared__ __attribute__((aligned(256))) char lds[2 * 32 * (I + J) * 128];
+    const int across = (a.N + 32 * J - 1) / (32 * J), down = (a.M + 32 * I - 1) / (32 * I), tile = (int)(blockIdx.x % (unsigned)(across * down)), part = (int)(blockIdx.x / (unsigned)(across * down));
+    const int m0 = tile % down * 32 * I, n0 = tile / down * 32 * J;
+    constexpr int kC = 128 / sizeof(T);
+    float4v acc[I][J];
+    zero(acc);
+    direct_tile<T, I, J, false, false, false, kFew>(Side{a.x, nullptr, ldx, 0, a.M}, Side{a.w, nullptr, ldw, 0, a.N}, kNone, m0, n0, part * a.steps * kC,
+                                              min(K, (part + 1) * a.steps * kC), lds, acc, nullptr);
+    direct_store<T, I, J>(a, part, m0, n0, acc);
+}
+
+// Both gradients in one launch: the first `tiles_x` workgroups take grad_x = d w (sum over N), the others grad_w = d^T x (over M) and, in the
+// tiles of the first columns, the sums of d for the bias.
+struct DirectGradArgs {
+    const void *grad, *z, *x, *w;
+    void *grad_x, *grad_w;
+    float *grad_bias, *partial_x, *partial_w, *partial_bias;      // partial: of parts, or null
+    long long ldg, ldx, ldw;
+    const float* sums;                                            // or null: of d over 64 rows each, [(M + 63) / 64][N] (d itself is then `grad`)
+    int M, N, K, act, accumulate, steps_x, steps_w;               // steps of 128 bytes, a part
+    unsigned tiles_x;
+};
+
+template <class T, int I, int J, bool kSlope, bool kFew>
+__global__ __launch_bounds__(256) void linear_direct_grad_kernel(DirectGradArgs a)
+{
+    __shared__ __attribute__((aligned(256))) char lds[2 * 32 * (I + J) * 128];
+    constexpr int kC = 128 / sizeof(T), kCount = 16 / sizeof(T), kSums = I * kCount / 2;      // a thread's pairs of pieces hold I / 2 times kCount i's
+    static_assert(I % 2 == 0, "pieces come in pairs");
+    const int across = (a.K + 32 * J - 1) / (32 * J);
+    const Side d_rows{a.grad, a.z, a.ldg, a.N, a.M}, d_turned{a.grad, a.z, a.ldg, a.N, a.N};
+    float4v acc[I][J];
+    zero(acc);
+    ProductArgs out{};
+    if (blockIdx.x < a.tiles_x) {
+        const int down = (a.M + 32 * I - 1) / (32 * I), tile = (int)(blockIdx.x % (unsigned)(across * down)), part = (int)(blockIdx.x / (unsigned)(across * down));
+        const int m0 = tile % down * 32 * I, k0 = tile / down * 32 * J;
+        direct_tile<T, I, J, false, true, kSlope, kFew>(d_rows, Side{a.w, nullptr, a.ldw, 0, a.K}, a.act, m0, k0, part * a.steps_x * kC, min(a.N, (part + 1) * a.steps_x * kC), lds, acc, nullptr);
+        out.out = a.grad_x;
+        out.partial = a.partial_x;
+        out.M = a.M;
+        out.N = a.K;
+        out.ldo = a.K;
+        direct_store<T, I, J>(out, part, m0, k0, acc);
+        return;
+    }
+    const unsigned block = blockIdx.x - a.tiles_x;
+    const int down = (a.N + 32 * I - 1) / (32 * I), tiles_w = down * (a.grad_w ? across : 1), tile = (int)(block % (unsigned)tiles_w), part = (int)(block / (unsigned)tiles_w);
+    const int n0 = tile % down * 32 * I, k0 = tile / down * 32 * J;
+    float sums[kSums] = {};
+    direct_tile<T, I, J, true, true, kSlope, kFew>(d_turned, a.grad_w ? Side{a.x, nullptr, a.ldx, 0, a.K} : d_turned, a.act, n0, k0, part * a.steps_w * kC, min(a.M, (part + 1) * a.steps_w * kC), lds, acc, sums);
+    out.out = a.grad_w;
+    out.residual = a.accumulate ? a.grad_w : nullptr;
+    out.partial = a.partial_w;
+    out.M = a.N;
+    out.N = a.K;
+    out.ldo = out.ldr = a.K;
+    if (a.grad_w) direct_store<T, I, J>(out, part, n0, k0, acc);
+    if (!a.grad_bias || k0 != 0) return;
+    if (a.sums) {
+        constexpr int kGroups = 256 / (32 * I);
+        if (part != 0) return;
+        const int column = threadIdx.x % (32 * I), group = threadIdx.x / (32 * I), n = n0 + column, count = (a.M + 63) / 64;
+        float* of = reinterpret_cast<float*>(lds);
+        float total = 0.f;
+        if (n < a.N)
+#pragma unroll 8
+            for (int i = group; i < count; i += kGroups) total += a.sums[(size_t)i * a.N + n];
+        __syncthreads();
+        of[threadIdx.x] = total;
+        __syncthreads();
+        if (group != 0 || n >= a.N) return;
+        total = 0.f;
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) total += of[g * 32 * I + column];
+        a.grad_bias[n] = a.accumulate ? a.grad_bias[n] + total : total;
+        return;
+    }
+    // The threads that hold the same i's lie kAcross apart; their sums are added in order.
+    constexpr int kAcross = 32 * I / kCount, kApart = 256 / kAcross;
+    static_assert(kApart >= 1, "a thread a piece");
+    float* of = reinterpret_cast<float*>(lds);
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < kSums; ++e) {
+        const int pair = e / kCount * 256 + (int)threadIdx.x, i = pair % kAcross * kCount, first = max(n0 + i + kCount - a.N, 0);
+        if (e % kCount >= first) of[(pair / kAcross) * (32 * I) + i + e % kCount - first] = sums[e];      // (places as in Share)
+    }
+    __syncthreads();
+    if ((int)threadIdx.x >= 32 * I || n0 + (int)threadIdx.x >= a.N) return;
+    float total = 0.f;
+    for (int p = 0; p < kApart * (kSums / kCount); ++p) total += of[p * 32 * I + threadIdx.x];
+    const int n = n0 + threadIdx.x;
+    if (a.partial_bias) a.partial_bias[(size_t)part * a.N + n] = total;
+    else a.grad_bias[n] = a.accumulate ? a.grad_bias[n] + total : total;
+}
+
+// Very few rows of x: a wavefront (S wavefronts, that share the sum) takes C rows of w and all R of x, 16 bytes a lane of each at a time.
+template <class T, int R, int C, int S>
+__global__ __launch_bounds__(256) void linear_dot_kernel(ProductArgs a, int K, long long ldx, long long ldw)
+{
+    typedef typename Piece<T>::type V;
+    constexpr int kCount = 16 / sizeof(T), kAhead = R * C <= 2 ? 4 : 2;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n0 = (int)(blockIdx.x * (4 / S) + wave / S) * C;
+    const T* x = static_cast<const T*>(a.x);
+    const T* w = static_cast<const T*>(a.w);
+    float sum[R][C] = {};
+    auto add = [&](const V (&xv)[R], const V (&wv)[C]) {
+#pragma unroll
+        for (int e = 0; e < kCount; ++e)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int c = 0; c < C; ++c) sum[r][c] = fmaf((float)xv[r][e], (float)wv[c][e], sum[r][c]);
+    };
+    const T* row[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) row[c] = w + (size_t)min(n0 + c, a.N - 1) * ldw;
+    constexpr int kStep = 64 * kCount * S;
+    int k = ((wave % S) * 64 + lane) * kCount;
+    for (; k + (kAhead - 1) * kStep + kCount <= K; k += kAhead * kStep) {
+        V xv[kAhead][R], wv[kAhead][C];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) wv[u][c] = *reinterpret_cast<const V*>(row[c] + k + u * kStep);
+#pragma unroll
+            for (int r = 0; r < R; ++r) xv[u][r] = *reinterpret_cast<const V*>(x + (size_t)min(r, a.M - 1) * ldx + k + u * kStep);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) add(xv[u], wv[u]);
+    }
+    for (; k < K; k += kStep) {
+        V xv[R], wv[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) wv[c] = load_piece<T>(row[c], k, K);
+#pragma unroll
+        for (int r = 0; r < R; ++r) xv[r] = load_piece<T>(x + (size_t)min(r, a.M - 1) * ldx, k, K);
+        add(xv, wv);
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int d = 32; d > 0; d /= 2) sum[r][c] += __shfl_xor(sum[r][c], d);
+    if constexpr (S > 1) {
+        __shared__ float of[4][R * C];
+        if (lane == 0)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int c = 0; c < C; ++c) of[wave][r * C + c] = sum[r][c];
+        __syncthreads();
+        if (wave % S != 0) return;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                sum[r][c] = 0.f;
+#pragma unroll
+                for (int i = 0; i < S; ++i) sum[r][c] += of[wave + i][r * C + c];
+            }
+    }
+    // Lane r finishes row r.
+    float v[C], bias[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        v[c] = sum[0][c];
+#pragma unroll
+        for (int r = 1; r < R; ++r) v[c] = lane == r ? sum[r][c] : v[c];
+        bias[c] = a.bias && n0 + c < a.N ? a.bias[n0 + c] : 0.f;
+    }
+    if (lane < min(R, a.M) && n0 < a.N) finish<T, C>(a, v, bias, lane, n0, a.N - n0);
+}
+
 // ---------------------------------------------------------------- which kernel
 
 double pieces_of(int n, int size) { return (double)((n + size - 1) / size); }
@@ -521,14 +958,14 @@ double tile_estimate(const TileRule& r, int M, int N, int parts, double bytes, d
 struct Choice {
     Kernel kernel;
     int parts, steps;
+    double us;
 };
 
 Choice choose(int dtype, int M, int N, int row_bytes)
 {
     const double f = dtype == kF32 ? 8.0 : 1.0, bytes = row_bytes;
     const int all = (row_bytes + 127) / 128;
-    Choice best{kRow11, 1, all};
-    double least = 0.0;
+    Choice best{kRow11, 1, all, 0.0};
     for (int k = 0; k < kKernels; ++k) {
         if (k == kTile88 && dtype == kF32) continue;
         for (int parts = 1; parts <= (k < kTile22 ? 1 : 64); parts *= 2) {
@@ -536,13 +973,19 @@ Choice choose(int dtype, int M, int N, int row_bytes)
             if (parts > 1 && steps < 8) break;
             if (k == kTile88 && steps < kStepsToWalk) break;
             const double us = k < kTile22 ? row_estimate(kRowRules[k], M, N, bytes, f) : tile_estimate(kTileRules[k - kTile22], M, N, parts, bytes, f);
-            if ((k == 0 && parts == 1) || us < least) {
-                best = Choice{(Kernel)k, (all + steps - 1) / steps, steps};
-                least = us;
-            }
+            if ((k == 0 && parts == 1) || us < best.us) best = Choice{(Kernel)k, (all + steps - 1) / steps, steps, us};
         }
     }
     return best;
+}
+
+// Parts of a sum of `all` steps, so that `tiles` workgroups a part are `wanted` in all, of `least` steps each or more.
+int parts_of(double tiles, int all, double wanted, int least)
+{
+    int parts = 1;
+    while (parts < 64 && tiles * parts * 2 <= wanted && (all + 2 * parts - 1) / (2 * parts) >= least) parts *= 2;
+    const int steps = (all + parts - 1) / parts;
+    return (all + steps - 1) / steps;
 }
 
 template <class T, int MB, int NB, int S>
@@ -596,16 +1039,11 @@ int launch_join(const ProductArgs& a, hipStream_t s)
 
 long long round_up(long long n, long long to) { return (n + to - 1) / to * to; }
 
-long long partial_bytes(int dtype, int M, int N, int row_bytes)
-{
-    const Choice c = choose(dtype, M, N, row_bytes);
-    return c.parts > 1 ? round_up(4ll * c.parts * M * N, 256) : 0;
-}
+long long partial_bytes(int parts, int M, int N) { return parts > 1 ? round_up(4ll * parts * M * N, 256) : 0; }
 
 // The product of rows that are laid out; partial: scratch memory of partial_bytes.
-int product(int dtype, ProductArgs a, char* partial, hipStream_t s)
+int product(int dtype, const Choice& c, ProductArgs a, char* partial, hipStream_t s)
 {
-    const Choice c = choose(dtype, a.M, a.N, a.row_bytes);
     a.parts = c.parts;
     a.steps = c.steps;
     a.partial = c.parts > 1 ? reinterpret_cast<float*>(partial) : nullptr;
@@ -653,16 +1091,25 @@ __global__ __launch_bounds__(256) void linear_lay_kernel(LayArgs a)
             for (int e = 0; e < kCount; ++e) g[e] = (float)v[e];
             if (a.z) {
                 const V z = load_piece<T>(static_cast<const T*>(a.z) + (size_t)row * a.cols, col, a.cols);
+                with_activation(a.act, [&](auto act) {
 #pragma unroll
-                for (int e = 0; e < kCount; ++e) {
-                    g[e] = col + e < a.cols ? g[e] * slope((float)z[e], a.act) : 0.f;
-                    v[e] = (T)g[e];
-                }
+                    for (int e = 0; e < kCount; ++e) {
+                        g[e] = col + e < a.cols ? g[e] * slope<act>((float)z[e]) : 0.f;
+                        v[e] = (T)g[e];
+                    }
+                });
             }
 #pragma unroll
             for (int e = 0; e < kCount; ++e) total[e] += g[e];
         }
-        if (a.copy && row < a.rows && col < a.copy_pitch) *reinterpret_cast<A*>(static_cast<T*>(a.copy) + (size_t)row * a.copy_pitch + col) = v;
+        if (a.copy && row < a.rows && col < a.copy_pitch) {      // (a pitch of no whole pieces: no zeros behind the row)
+            T* const to = static_cast<T*>(a.copy) + (size_t)row * a.copy_pitch + col;
+            if (col + kCount <= a.copy_pitch) *reinterpret_cast<V*>(to) = v;
+            else
+#pragma unroll
+                for (int e = 0; e < kCount; ++e)
+                    if (col + e < a.copy_pitch) to[e] = v[e];
+        }
         if (a.turned)
 #pragma unroll
             for (int e = 0; e < kCount; ++e) tile[in][piece * kCount + e] = v[e];
@@ -722,15 +1169,18 @@ int launch_zeros(void* a, long long a_bytes, void* b, long long b_bytes, hipStre
     return (int)hipGetLastError();
 }
 
-int launch_lay(int dtype, const LayArgs& a, hipStream_t s)
+template <class T>
+int launch_lay_of(const LayArgs& a, hipStream_t s)
 {
     const long long groups = ((a.rows + 63ll) / 64) * ((a.cols + 63ll) / 64);
     if ((unsigned long long)groups > most_groups(256)) return kTooLarge;
-    const dim3 grid((unsigned)groups), block(256);
-    if (dtype == kF32) hipLaunchKernelGGL(linear_lay_kernel<float>, grid, block, 0, s, a);
-    else if (dtype == kF16) hipLaunchKernelGGL(linear_lay_kernel<_Float16>, grid, block, 0, s, a);
-    else hipLaunchKernelGGL(linear_lay_kernel<__bf16>, grid, block, 0, s, a);
+    hipLaunchKernelGGL(linear_lay_kernel<T>, dim3((unsigned)groups), dim3(256), 0, s, a);
     return (int)hipGetLastError();
+}
+
+int launch_lay(int dtype, const LayArgs& a, hipStream_t s)
+{
+    return dtype == kF32 ? launch_lay_of<float>(a, s) : dtype == kF16 ? launch_lay_of<_Float16>(a, s) : launch_lay_of<__bf16>(a, s);
 }
 
 int bytes_of(int dtype) { return dtype == kF32 ? 4 : 2; }
@@ -746,52 +1196,136 @@ bool laid_out(const void* p, long long ld, int rows, int cols, int b)
 long long pitch_of(long long cols, int b) { return round_up(cols, 16 / b); }
 long long laid_bytes(long long rows, long long cols, int b) { return round_up(rows * pitch_of(cols, b) * b, 256); }
 
+// How the layer is computed: very few rows by linear_dot_kernel; rows at odd addresses, or too few steps to pay for laying them out, by
+// linear_direct_kernel; else from rows that are laid out.
+enum Way { kDot, kDirect, kLaid };
+
+struct LinearPlan {
+    Way way;
+    Choice laid;            // of kLaid
+    int parts, steps;       // of kDirect
+    bool lay_x, lay_w;
+    long long x, w, end;    // bytes of scratch memory: where w's copy and the parts begin, and all
+};
+
+double lay_estimate(double bytes) { return 3.0 + bytes / 4e6; }
+
+// A direct launch whose tiles take `work` steps in all, `longest` of them one after another at most.  turned: the gradients' operands.
+double direct_estimate(int dtype, double work, int longest, bool turned)
+{
+    const double alone = dtype == kF32 ? 0.74 : turned ? 0.42 : 0.34, shared = dtype == kF32 ? (turned ? 0.66 : 0.53) : turned ? 0.42 : 0.25;
+    return 4.5 + std::max(longest * alone, work / 256.0 * shared);
+}
+
+// Parts of a sum, and the launch that adds them up.
+double join_estimate(int parts, double outputs) { return parts > 1 ? 3.0 + 4.0 * outputs * (parts + 1) / 4e6 : 0.0; }
+
+LinearPlan plan_of(const LinearArgs& a, int dtype)
+{
+    const int b = bytes_of(dtype), row_bytes = (int)pitch_of(a.K, b) * b, all = (row_bytes + 127) / 128;
+    LinearPlan p{};
+    p.lay_x = !laid_out(a.x, a.ldx, a.M, a.K, b);
+    p.lay_w = !laid_out(a.w, a.ldw, a.N, a.K, b);
+    // (Two rows that are laid out, or four of fp32: 4096 -> 4096 8.6 us either way in bfloat16, 13.8 and 14.7 in fp32; eight of them 24 and 8.5.
+    // Eight that are not: 1001 -> 1001 6.8 and 9.5.)
+    if (a.M <= (p.lay_x || p.lay_w ? 8 : dtype == kF32 ? 4 : 2)) {
+        p.way = kDot;
+        return p;
+    }
+    const double tiles = pieces_of(a.M, 64) * pieces_of(a.N, 64);
+    p.parts = parts_of(tiles, all, 256.0, 8);
+    p.steps = (all + p.parts - 1) / p.parts;
+    p.laid = choose(dtype, a.M, a.N, row_bytes);
+    const double laid = p.laid.us + (p.lay_x ? lay_estimate(2.0 * a.M * row_bytes) : 0.0) + (p.lay_w ? lay_estimate(2.0 * a.N * row_bytes) : 0.0);
+    const double direct = direct_estimate(dtype, tiles * all, p.steps, false) + join_estimate(p.parts, (double)a.M * a.N);
+    if (direct < laid) {
+        p.way = kDirect;
+        p.end = partial_bytes(p.parts, a.M, a.N);
+        return p;
+    }
+    p.way = kLaid;
+    p.x = p.lay_x ? laid_bytes(a.M, a.K, b) : 0;
+    p.w = p.x + (p.lay_w ? laid_bytes(a.N, a.K, b) : 0);
+    p.end = p.w + partial_bytes(p.laid.parts, a.M, a.N);
+    return p;
+}
+
+template <class T, int R, int C>
+int launch_dot(const ProductArgs& a, const LinearArgs& l, hipStream_t s)
+{
+    // (wavefronts that share a sum where there are too few rows of w for every SIMD to have some)
+    const long long groups = (a.N + C - 1ll) / C;
+    if (groups <= 512) hipLaunchKernelGGL((linear_dot_kernel<T, R, C, 4>), dim3((unsigned)groups), dim3(256), 0, s, a, l.K, l.ldx, l.ldw);
+    else hipLaunchKernelGGL((linear_dot_kernel<T, R, C, 1>), dim3((unsigned)((groups + 3) / 4)), dim3(256), 0, s, a, l.K, l.ldx, l.ldw);
+    return (int)hipGetLastError();
+}
+
+template <class T>
+int launch_way(const LinearPlan& p, ProductArgs a, const LinearArgs& l, char* workspace, hipStream_t s)
+{
+    if (p.way == kDot) {
+        if (l.M == 1) return launch_dot<T, 1, 2>(a, l, s);
+        if (l.M == 2) return launch_dot<T, 2, 2>(a, l, s);
+        if (l.M <= 4) return launch_dot<T, 4, 2>(a, l, s);
+        return launch_dot<T, 8, 2>(a, l, s);
+    }
+    a.parts = p.parts;
+    a.steps = p.steps;
+    a.partial = p.parts > 1 ? reinterpret_cast<float*>(workspace) : nullptr;
+    const long long groups = (a.M + 63ll) / 64 * ((a.N + 63ll) / 64) * p.parts;
+    if ((unsigned long long)groups > most_groups(256)) return kTooLarge;
+    if (l.K < (int)(16 / sizeof(T))) hipLaunchKernelGGL((linear_direct_kernel<T, 2, 2, true>), dim3((unsigned)groups), dim3(256), 0, s, a, l.K, l.ldx, l.ldw);
+    else hipLaunchKernelGGL((linear_direct_kernel<T, 2, 2, false>), dim3((unsigned)groups), dim3(256), 0, s, a, l.K, l.ldx, l.ldw);
+    const int e = (int)hipGetLastError();
+    return e != 0 || p.parts == 1 ? e : launch_join<T>(a, s);
+}
+
 }  // namespace
 
-long long linear_workspace(const LinearArgs& a, int dtype)
-{
-    const int b = bytes_of(dtype);
-    long long bytes = 0;
-    if (!laid_out(a.x, a.ldx, a.M, a.K, b)) bytes += laid_bytes(a.M, a.K, b);
-    if (!laid_out(a.w, a.ldw, a.N, a.K, b)) bytes += laid_bytes(a.N, a.K, b);
-    return bytes + partial_bytes(dtype, a.M, a.N, (int)pitch_of(a.K, b) * b);
-}
+long long linear_workspace(const LinearArgs& a, int dtype) { return plan_of(a, dtype).end; }
 
 int launch_linear(int dtype, const LinearArgs& a, char* workspace, void* stream)
 {
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const int b = bytes_of(dtype), row_bytes = (int)pitch_of(a.K, b) * b;
+    const LinearPlan plan = plan_of(a, dtype);
     ProductArgs p{a.x, a.w, a.bias, a.residual, a.out, a.z, nullptr, a.M, a.N, row_bytes, (int)(a.M > 1 ? a.ldx * b : row_bytes), (int)(a.N > 1 ? a.ldw * b : row_bytes),
                   a.act, 0, 1, a.ldr, a.ldo};
-    if (!laid_out(a.x, a.ldx, a.M, a.K, b)) {
+    if (plan.way != kLaid)
+        return dtype == kF32 ? launch_way<float>(plan, p, a, workspace, s) : dtype == kF16 ? launch_way<_Float16>(plan, p, a, workspace, s) : launch_way<__bf16>(plan, p, a, workspace, s);
+    if (plan.lay_x) {
         const int e = launch_lay(dtype, LayArgs{a.x, nullptr, workspace, nullptr, nullptr, a.ldx, a.M, a.K, row_bytes / b, 0, 0}, s);
         if (e != 0) return e;
         p.x = workspace;
         p.x_pitch = row_bytes;
-        workspace += laid_bytes(a.M, a.K, b);
     }
-    if (!laid_out(a.w, a.ldw, a.N, a.K, b)) {
-        const int e = launch_lay(dtype, LayArgs{a.w, nullptr, workspace, nullptr, nullptr, a.ldw, a.N, a.K, row_bytes / b, 0, 0}, s);
+    if (plan.lay_w) {
+        const int e = launch_lay(dtype, LayArgs{a.w, nullptr, workspace + plan.x, nullptr, nullptr, a.ldw, a.N, a.K, row_bytes / b, 0, 0}, s);
         if (e != 0) return e;
-        p.w = workspace;
+        p.w = workspace + plan.x;
         p.w_pitch = row_bytes;
-        workspace += laid_bytes(a.N, a.K, b);
     }
-    return product(dtype, p, workspace, s);
+    return product(dtype, plan.laid, p, workspace + plan.w, s);
 }
 
 namespace {
 
-// Where the pieces of a backward pass lie in its scratch memory.
-struct GradLayout {
+// How the gradients are computed, and where the pieces of a pass lie in its scratch memory.
+struct GradPlan {
+    bool direct, formed;                                     // direct; and the gradient behind the activation is formed by a launch before
+    int parts_x, parts_w, steps_x, steps_w;
+    long long sums_x, sums_w, sums_bias;
+    // laid out
     bool own_dz;                                             // the gradient behind the activation is formed (else grad is it)
-    long long dz, dz_turned, x_turned, w_turned, sums, partial, end;
+    Choice x, w;
+    long long dz, dz_turned, x_turned, w_turned, sums, partial;
+    long long end;
 };
 
-GradLayout layout_of(const LinearGradArgs& a, int dtype)
+GradPlan plan_of(const LinearGradArgs& a, int dtype)
 {
-    const int b = bytes_of(dtype);
-    GradLayout l{};
+    const int b = bytes_of(dtype), count = 128 / b;
+    GradPlan l{};
     l.own_dz = a.act != kNone || !laid_out(a.grad, a.ldg, a.M, a.N, b);
     long long at = 0;
     auto take = [&](bool wanted, long long bytes) {
@@ -799,30 +1333,116 @@ GradLayout layout_of(const LinearGradArgs& a, int dtype)
         if (wanted) at += round_up(bytes, 256);
         return here;
     };
+    double laid = 0.0, direct = 0.0;
+    // (Chosen as if all three were wanted: a gradient's bits do not depend on which others are.)
+    l.x = choose(dtype, a.M, a.K, (int)pitch_of(a.N, b) * b);
+    l.w = choose(dtype, a.N, a.K, (int)pitch_of(a.M, b) * b);
+    laid = l.x.us + l.w.us + lay_estimate(2.0 * a.N * a.K * b) + lay_estimate(2.0 * a.M * a.K * b) + lay_estimate(3.0 * a.M * a.N * b) + 3.0;
+    const double tiles_x = pieces_of(a.M, 64) * pieces_of(a.K, 64), tiles_w = pieces_of(a.N, 64) * pieces_of(a.K, 64);
+    const int all_x = (a.N + count - 1) / count, all_w = (a.M + count - 1) / count;
+    l.parts_x = parts_of(tiles_x, all_x, 256.0, 8);
+    l.parts_w = parts_of(tiles_w, all_w, 256.0, 8);
+    l.steps_x = (all_x + l.parts_x - 1) / l.parts_x;
+    l.steps_w = (all_w + l.parts_w - 1) / l.parts_w;
+    const double work = tiles_x * all_x + tiles_w * all_w, form = lay_estimate(3.0 * a.M * a.N * b) + 1.5;
+    direct = direct_estimate(dtype, work, std::max(l.steps_x, l.steps_w), true) + join_estimate(l.parts_x, (double)a.M * a.K) + join_estimate(l.parts_w, (double)a.N * a.K);
+    // (Where the slope is worked out as the tiles are loaded, every tile along K does it anew.)
+    const double anew = a.act == kNone ? 0.0 : std::max(work / 256.0, (double)std::max(l.steps_x, l.steps_w)) * (a.act == kRelu ? 0.26 : 0.38) * (dtype == kF32 ? 0.5 : 1.0);
+    l.formed = anew > form;
+    direct += std::min(anew, form);
+    if (direct < laid) {
+        l.direct = true;
+        l.dz = take(l.formed, (long long)a.M * a.N * b);
+        l.sums = take(l.formed && a.grad_bias, (a.M + 63ll) / 64 * a.N * 4);
+        l.sums_x = take(a.grad_x, partial_bytes(l.parts_x, a.M, a.K));
+        l.sums_w = take(a.grad_w, partial_bytes(l.parts_w, a.N, a.K));
+        l.sums_bias = take(a.grad_bias && l.parts_w > 1 && !l.formed, 4ll * l.parts_w * a.N);
+        l.end = at;
+        return l;
+    }
     l.dz = take(a.grad_x && l.own_dz, laid_bytes(a.M, a.N, b));
     l.dz_turned = take(a.grad_w, laid_bytes(a.N, a.M, b));
     l.x_turned = take(a.grad_w, laid_bytes(a.K, a.M, b));
     l.w_turned = take(a.grad_x, laid_bytes(a.K, a.N, b));
     l.sums = take(a.grad_bias, (a.M + 63ll) / 64 * a.N * 4);
-    const long long px = a.grad_x ? partial_bytes(dtype, a.M, a.K, (int)pitch_of(a.N, b) * b) : 0;
-    const long long pw = a.grad_w ? partial_bytes(dtype, a.N, a.K, (int)pitch_of(a.M, b) * b) : 0;
-    l.partial = take(true, std::max(px, pw));
+    l.partial = take(true, std::max(a.grad_x ? partial_bytes(l.x.parts, a.M, a.K) : 0, a.grad_w ? partial_bytes(l.w.parts, a.N, a.K) : 0));
     l.end = at;
     return l;
 }
 
+int launch_bias(const float* sums, float* out, int count, int N, bool accumulate, hipStream_t s)
+{
+    hipLaunchKernelGGL(linear_bias_kernel, dim3((unsigned)((N + 15) / 16)), dim3(256), 0, s, sums, out, count, N, (int)accumulate);
+    return (int)hipGetLastError();
+}
+
+template <class T>
+int launch_direct_grad(const GradPlan& l, const LinearGradArgs& a, char* workspace, hipStream_t s)
+{
+    const unsigned across = (unsigned)((a.K + 63) / 64);
+    const unsigned long long x = a.grad_x ? (a.M + 63ull) / 64 * across * l.parts_x : 0;
+    const unsigned long long w = a.grad_w || a.grad_bias ? (a.N + 63ull) / 64 * (a.grad_w ? across : 1u) * l.parts_w : 0;
+    if (x + w > most_groups(256)) return kTooLarge;
+    if (x + w == 0) return 0;
+    float* const px = a.grad_x && l.parts_x > 1 ? reinterpret_cast<float*>(workspace + l.sums_x) : nullptr;
+    float* const pw = a.grad_w && l.parts_w > 1 ? reinterpret_cast<float*>(workspace + l.sums_w) : nullptr;
+    float* const pb = a.grad_bias && l.parts_w > 1 && !l.formed ? reinterpret_cast<float*>(workspace + l.sums_bias) : nullptr;
+    DirectGradArgs d{a.grad, a.act != kNone ? a.z : nullptr, a.x, a.w, a.grad_x, a.grad_w, a.grad_bias, px, pw, pb, a.ldg, a.ldx, a.ldw, nullptr, a.M, a.N, a.K, a.act,
+                     a.accumulate, l.steps_x, l.steps_w, (unsigned)x};
+    int e = 0;
+    if (l.formed) {
+        float* const sums = a.grad_bias ? reinterpret_cast<float*>(workspace + l.sums) : nullptr;
+        e = launch_lay_of<T>(LayArgs{a.grad, a.z, workspace + l.dz, nullptr, sums, a.ldg, a.M, a.N, a.N, 0, a.act}, s);
+        if (e != 0) return e;
+        d.grad = workspace + l.dz;
+        d.z = nullptr;
+        d.ldg = a.N;
+        d.sums = sums;
+        d.act = kNone;
+    }
+    const dim3 grid((unsigned)(x + w)), block(256);
+    const bool few = std::min(a.N, a.K) < (int)(16 / sizeof(T));
+    if (d.z && few) hipLaunchKernelGGL((linear_direct_grad_kernel<T, 2, 2, true, true>), grid, block, 0, s, d);
+    else if (d.z) hipLaunchKernelGGL((linear_direct_grad_kernel<T, 2, 2, true, false>), grid, block, 0, s, d);
+    else if (few) hipLaunchKernelGGL((linear_direct_grad_kernel<T, 2, 2, false, true>), grid, block, 0, s, d);
+    else hipLaunchKernelGGL((linear_direct_grad_kernel<T, 2, 2, false, false>), grid, block, 0, s, d);
+    e = (int)hipGetLastError();
+    ProductArgs p{};
+    if (e == 0 && px) {
+        p.out = a.grad_x;
+        p.partial = px;
+        p.M = a.M;
+        p.N = a.K;
+        p.parts = l.parts_x;
+        p.ldo = a.K;
+        e = launch_join<T>(p, s);
+    }
+    if (e == 0 && pw) {
+        p.out = a.grad_w;
+        p.residual = a.accumulate ? a.grad_w : nullptr;
+        p.partial = pw;
+        p.M = a.N;
+        p.N = a.K;
+        p.parts = l.parts_w;
+        p.ldo = p.ldr = a.K;
+        e = launch_join<T>(p, s);
+    }
+    if (e == 0 && pb) e = launch_bias(pb, a.grad_bias, l.parts_w, a.N, a.accumulate, s);
+    return e;
+}
+
 }  // namespace
 
-long long linear_grad_workspace(const LinearGradArgs& a, int dtype) { return layout_of(a, dtype).end; }
+long long linear_grad_workspace(const LinearGradArgs& a, int dtype) { return plan_of(a, dtype).end; }
 
 int launch_linear_grad(int dtype, const LinearGradArgs& a, char* workspace, void* stream)
 {
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const int b = bytes_of(dtype);
-    if (a.M == 0) {      // sums of nothing
-        return launch_zeros(a.grad_w, (long long)a.N * a.K * b, a.grad_bias, a.N * 4ll, s);
-    }
-    const GradLayout l = layout_of(a, dtype);
+    if (a.M == 0) return launch_zeros(a.grad_w, (long long)a.N * a.K * b, a.grad_bias, a.N * 4ll, s);      // sums of nothing
+    const GradPlan l = plan_of(a, dtype);
+    if (l.direct)
+        return dtype == kF32 ? launch_direct_grad<float>(l, a, workspace, s) : dtype == kF16 ? launch_direct_grad<_Float16>(l, a, workspace, s) : launch_direct_grad<__bf16>(l, a, workspace, s);
     const int m_pitch = (int)pitch_of(a.M, b), n_pitch = (int)pitch_of(a.N, b);
     int e = 0;
     if ((a.grad_x && l.own_dz) || a.grad_w || a.grad_bias) {
@@ -830,24 +1450,20 @@ int launch_linear_grad(int dtype, const LinearGradArgs& a, char* workspace, void
                                       a.grad_bias ? reinterpret_cast<float*>(workspace + l.sums) : nullptr, a.ldg, a.M, a.N, n_pitch, m_pitch, a.act}, s);
         if (e != 0) return e;
     }
-    if (a.grad_bias) {
-        hipLaunchKernelGGL(linear_bias_kernel, dim3((unsigned)((a.N + 15) / 16)), dim3(256), 0, s, reinterpret_cast<const float*>(workspace + l.sums), a.grad_bias,
-                           (a.M + 63) / 64, a.N, (int)a.accumulate);
-        if ((e = (int)hipGetLastError()) != 0) return e;
-    }
+    if (a.grad_bias && (e = launch_bias(reinterpret_cast<const float*>(workspace + l.sums), a.grad_bias, (a.M + 63) / 64, a.N, a.accumulate, s)) != 0) return e;
     if (a.grad_x) {
         e = launch_lay(dtype, LayArgs{a.w, nullptr, nullptr, workspace + l.w_turned, nullptr, a.ldw, a.N, a.K, 0, n_pitch, 0}, s);
         if (e != 0) return e;
         const ProductArgs p{l.own_dz ? workspace + l.dz : a.grad, workspace + l.w_turned, nullptr, nullptr, a.grad_x, nullptr, nullptr, a.M, a.K, n_pitch * b,
                             l.own_dz || a.M == 1 ? n_pitch * b : (int)(a.ldg * b), n_pitch * b, kNone, 0, 1, 0, a.K};
-        if ((e = product(dtype, p, workspace + l.partial, s)) != 0) return e;
+        if ((e = product(dtype, l.x, p, workspace + l.partial, s)) != 0) return e;
     }
     if (a.grad_w) {
         e = launch_lay(dtype, LayArgs{a.x, nullptr, nullptr, workspace + l.x_turned, nullptr, a.ldx, a.M, a.K, 0, m_pitch, 0}, s);
         if (e != 0) return e;
         const ProductArgs p{workspace + l.dz_turned, workspace + l.x_turned, nullptr, a.accumulate ? a.grad_w : nullptr, a.grad_w, nullptr, nullptr, a.N, a.K, m_pitch * b,
                             m_pitch * b, m_pitch * b, kNone, 0, 1, a.K, a.K};
-        if ((e = product(dtype, p, workspace + l.partial, s)) != 0) return e;
+        if ((e = product(dtype, l.w, p, workspace + l.partial, s)) != 0) return e;
     }
     return 0;
 }
