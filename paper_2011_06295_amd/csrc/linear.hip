@@ -18,6 +18,7 @@ namespace {
 enum { kNone = 0, kRelu = 1, kGelu = 2, kSilu = 3 };   // SC_ACT_*
 
 typedef float float4v __attribute__((ext_vector_type(4)));
+typedef int int2v __attribute__((ext_vector_type(2)));
 
 // Elements of 16 bytes, as the matrix instructions take them.
 template <class T>
@@ -25,12 +26,12 @@ using Eight = T __attribute__((ext_vector_type(16 / sizeof(T))));
 
 // What a launch multiplies.  (Arguments past 112 bytes cost the host 0.75 us more.)
 struct ProductArgs {
-    const void *x, *w;              // rows of row_bytes bytes (a multiple of 16), x_pitch and w_pitch apart
+    const void *x, *w;              // rows along the sum, whole pieces of 16 bytes, x_pitch and w_pitch bytes apart; turned: see the tile kernel
     const float* bias;              // or null
     const void* residual;           // or null
     void *out, *z;                  // z: what goes into the activation, or null
     float* partial;                 // or null.  Else a part of k each: sums [part][M][N], and nothing of the above
-    int M, N, row_bytes, x_pitch, w_pitch;
+    int M, N, terms, x_pitch, w_pitch;      // terms: of a sum
     int act;
     int steps;                      // of 128 bytes, a part
     int parts;
@@ -157,8 +158,27 @@ __device__ __forceinline__ void finish(const ProductArgs& a, const float (&sum)[
     store(static_cast<T*>(a.out) + (size_t)m * a.ldo + n);
 }
 
+template <class T>
+__device__ __forceinline__ int bytes_of_rows(int terms) { return (terms * (int)sizeof(T) + 15) / 16 * 16; }
+
+// Four elements of each of 16 rows that lie along i, as four elements along c of each of 16 i's: lane l of 16 gives the address of elements
+// 4 (l % 4) .. + 3 of row l / 4, and gets rows 0 .. 3 of element l.
+__device__ __forceinline__ int2v read_turned(const char* at)
+{
+    typedef short short4v __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(int2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((SC_LDS short4v*)(SC_LDS char*)at));
+}
+
 // A load of a piece that lies past the rows' end: an offset that no descriptor reaches (they describe 2^31 bytes at most).
 __device__ __forceinline__ unsigned past(unsigned offset, unsigned beyond, int i) { return offset | ((beyond >> i) & 1u) << 31; }
+
+// What the number of a turned row's piece of 16 bytes is combined with (by exclusive or), row c of a tile of `length` i's.
+template <class T>
+__device__ __forceinline__ int swizzle_of(int c, int length)
+{
+    if (sizeof(T) == 4) return ((c >> 2) & 3) << 2;
+    return length == 64 ? (((c >> 1) & 1) | ((c >> 3) & 1) << 1) << 1 : ((c & 3) | ((c >> 3) & 1) << 2) << 1;
+}
 
 // Large tiles: a workgroup has a CU to itself, so it walks over tiles, `stride` apart, and loads the next one's first steps before it
 // finishes one.  (Three steps a tile at least: a barrier lies between what reads a tile's biases and what loads over them.)
@@ -167,11 +187,12 @@ constexpr bool kWalksOver = MB * NB >= 64;
 constexpr int kStepsToWalk = 3;
 
 // A tile of 16 MB WM rows of x by 16 NB WN rows of w, 128 bytes of each a step; WM x WN wavefronts with MB x NB blocks of 16 x 16 sums.
-// S steps are in LDS or on their way there.
-template <class T, int MB, int NB, int WM, int WN, int S>
+// S steps are in LDS or on their way there.  kTurnX, kTurnW: that operand is given the other way round, element (i, c) at c * pitch + i, as the
+// gradients need it: its step is a part of 128 / sizeof(T) such rows, which lie in LDS as they do in memory and are turned as they are read.
+template <class T, int MB, int NB, int WM, int WN, int S, bool kTurnX, bool kTurnW>
 __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 || S > 2 ? 1 : 2) void linear_tile_kernel(ProductArgs a, unsigned tiles, unsigned stride)
 {
-    constexpr int TM = 16 * MB * WM, TN = 16 * NB * WN, W = WM * WN;
+    constexpr int TM = 16 * MB * WM, TN = 16 * NB * WN, W = WM * WN, kC = 128 / sizeof(T);
     constexpr int kLoadsX = TM / 8 / W, kLoadsW = TN / 8 / W, kLoads = kLoadsX + kLoadsW;
     constexpr int kX = TM * 128, kW = TN * 128, kHalf = MB / 2;
     static_assert(MB % 2 == 0 && NB % 2 == 0, "blocks come in pairs");
@@ -181,20 +202,29 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 || S > 2 ? 1 : 2) void 
     __shared__ __attribute__((aligned(16))) float channel_bias[kSets][TN];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int down = (a.M + TM - 1) / TM, across = (a.N + TN - 1) / TN, steps = a.steps, all_steps = (a.row_bytes + 127) / 128;
+    const int row_bytes = bytes_of_rows<T>(a.terms);
+    const int down = (a.M + TM - 1) / TM, across = (a.N + TN - 1) / TN, steps = a.steps, all_steps = (row_bytes + 127) / 128;
     // A row of LDS is the 128 bytes of a row's step; its eight pieces of 16 bytes are permuted by the row, so that the 16 rows that a
     // read takes one piece of lie in 16 different groups of four banks.  A lane's load fetches the piece that belongs where it lands.
+    // Turned, a row of LDS is the tile's i's at one c, 32 bytes (64 of fp32) permuted by c so that the 16 (4) rows of a read lie in different banks.
     unsigned offset[kLoads], behind = 0;      // behind: bit i, load i's piece of the last step lies past the end of its row
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-        const int row = (wave * (i < kLoadsX ? kLoadsX : kLoadsW) + (i < kLoadsX ? i : i - kLoadsX)) * 8 + (lane >> 3);
-        const int turn = i < kLoadsX ? (row >> 1) & 7 : ((row >> 1) & 1) | ((row >> 3) & 3) << 1;
-        const int piece = ((lane & 7) ^ turn) << 4;
-        offset[i] = (unsigned)row * (i < kLoadsX ? a.x_pitch : a.w_pitch) + piece;
-        if ((all_steps - 1) * 128 + piece >= a.row_bytes) behind |= 1u << i;
+        const bool of_x = i < kLoadsX;
+        const int load = wave * (of_x ? kLoadsX : kLoadsW) + (of_x ? i : i - kLoadsX);
+        if (of_x ? kTurnX : kTurnW) {
+            const int pieces = (of_x ? TM : TN) * (int)sizeof(T) / 16, at = load * 64 + lane, c = at / pieces;
+            offset[i] = (unsigned)c * (of_x ? a.x_pitch : a.w_pitch) + ((at % pieces ^ swizzle_of<T>(c, of_x ? TM : TN)) << 4);
+        } else {
+            const int row = load * 8 + (lane >> 3);
+            const int turn = of_x || kTurnW ? (row >> 1) & 7 : ((row >> 1) & 1) | ((row >> 3) & 3) << 1;
+            const int piece = ((lane & 7) ^ turn) << 4;
+            offset[i] = (unsigned)row * (of_x ? a.x_pitch : a.w_pitch) + piece;
+            if ((all_steps - 1) * 128 + piece >= row_bytes) behind |= 1u << i;
+        }
     }
     const unsigned lds0 = (unsigned)(uintptr_t)(SC_LDS char*)lds;
-    int4v from_x, from_w;
+    int4v from_x = {0, 0, 0, 0}, from_w = from_x;
     int bytes_x = 0, bytes_w = 0;
     unsigned xdst = lds0, wdst = lds0 + S * kX, tile = blockIdx.x, beyond = 0;
     int next_m = 0, next_n = 0, next_part = 0, step = 0, end = 0, set = 0;      // what is loaded: a step of a tile, whose biases go to `set`
@@ -207,8 +237,8 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 || S > 2 ? 1 : 2) void 
         next_n = tn * TN;
         step = next_part * steps;
         end = step + steps;
-        from_x = descriptor_of(static_cast<const char*>(a.x) + (size_t)next_m * a.x_pitch, (long long)min(TM, a.M - next_m) * a.x_pitch);
-        from_w = descriptor_of(static_cast<const char*>(a.w) + (size_t)next_n * a.w_pitch, (long long)min(TN, a.N - next_n) * a.w_pitch);
+        if (!kTurnX) from_x = descriptor_of(static_cast<const char*>(a.x) + (size_t)next_m * a.x_pitch, (long long)min(TM, a.M - next_m) * a.x_pitch);
+        if (!kTurnW) from_w = descriptor_of(static_cast<const char*>(a.w) + (size_t)next_n * a.w_pitch, (long long)min(TN, a.N - next_n) * a.w_pitch);
         bytes_x = from_x[2];
         bytes_w = from_w[2];
         if (wave * 64 < TN) {
@@ -219,6 +249,20 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 || S > 2 ? 1 : 2) void 
         }
     };
     // (Each of these scalars is set in one place: with a branch for each reason to fetch nothing the compiler lost the descriptors' zeros.)
+    auto look = [&]() {
+        const bool there = step < min(end, all_steps);      // else zeros: past the last tile, or past the rows (in the last part)
+        const int c = there ? step * kC : 0, rows = min(kC, a.terms - c) - 1;
+        if (kTurnX)
+            from_x = descriptor_of(static_cast<const char*>(a.x) + (size_t)c * a.x_pitch + (size_t)next_m * sizeof(T),
+                                   there ? (long long)rows * a.x_pitch + bytes_of_rows<T>(a.M - next_m) : 0ll);
+        else from_x[2] = there ? bytes_x : 0;
+        if (kTurnW)
+            from_w = descriptor_of(static_cast<const char*>(a.w) + (size_t)c * a.w_pitch + (size_t)next_n * sizeof(T),
+                                   there ? (long long)rows * a.w_pitch + bytes_of_rows<T>(a.N - next_n) : 0ll);
+        else from_w[2] = there ? bytes_w : 0;
+        at = there ? step * 128 : 0;
+        beyond = step == all_steps - 1 ? behind : 0;
+    };
     auto advance = [&]() {
         if (++step == end) {
             tile += stride;
@@ -227,19 +271,14 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 || S > 2 ? 1 : 2) void 
                 enter();
             }
         }
-        const bool there = step < min(end, all_steps);      // else zeros: past the last tile, or past the rows (in the last part)
-        from_x[2] = there ? bytes_x : 0;
-        from_w[2] = there ? bytes_w : 0;
-        at = there ? step * 128 : 0;
-        beyond = step == all_steps - 1 ? behind : 0;
+        look();
     };
     auto load = [&](int i) {
-        if (i < kLoadsX) load_to_lds(from_x, past(offset[i], beyond, i), at, xdst + (wave * kLoadsX + i) * 1024);
-        else load_to_lds(from_w, past(offset[i], beyond, i), at, wdst + (wave * kLoadsW + i - kLoadsX) * 1024);
+        if (i < kLoadsX) load_to_lds(from_x, kTurnX ? offset[i] : past(offset[i], beyond, i), kTurnX ? 0 : at, xdst + (wave * kLoadsX + i) * 1024);
+        else load_to_lds(from_w, kTurnW ? offset[i] : past(offset[i], beyond, i), kTurnW ? 0 : at, wdst + (wave * kLoadsW + i - kLoadsX) * 1024);
     };
     enter();
-    at = step * 128;
-    beyond = step == all_steps - 1 ? behind : 0;
+    look();
     int m0 = next_m, n0 = next_n, part = next_part, done = set;
     each<S>([&](auto stage) {
         if constexpr (stage > 0) advance();
@@ -263,12 +302,37 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 || S > 2 ? 1 : 2) void 
     // Where a lane reads: its row of block 0 and its piece; the second 64 bytes of a step are four pieces on (an exclusive or).
     // Row r of a wavefront's block j of w stands for channel 32 (j / 2) + 8 (r / 4) + 4 (j % 2) + r % 4, so that a lane's sums of
     // two blocks are eight channels in a row.
+    // (Where w is turned, of channel 16 j + r: its reads would take twice the time.)  Turned, a lane reads four c's of 16 bits at once, or one of fp32.
     const int wm = wave % WM, wn = wave / WM, r = lane & 15, q = lane >> 4;
-    int xa0 = (wm * 16 * MB + r) * 128 + ((q ^ (r >> 1)) << 4), xa1 = xa0 ^ 64;
-    int wa0 = S * kX + (wn * 16 * NB + (r >> 2) * 8 + (r & 3)) * 128 + ((q ^ (r >> 1)) << 4), wa1 = wa0 ^ 64;
+    constexpr int kRowX = TM * (int)sizeof(T), kRowW = TN * (int)sizeof(T), kChunk = sizeof(T) == 2 ? 32 : 64;      // bytes of 16 i's
+    const int c_first = sizeof(T) == 2 ? 8 * q + (r >> 2) : 4 * q, in_chunk = sizeof(T) == 2 ? (r & 3) * 8 : r * 4;
+    auto turned = [&](int first_block, int row_length, int tile_length) {
+        return c_first * row_length + ((first_block * kChunk / 16) ^ swizzle_of<T>(c_first, tile_length)) * 16 + in_chunk;
+    };
+    int xa0 = kTurnX ? turned(wm * MB, kRowX, TM) : (wm * 16 * MB + r) * 128 + ((q ^ (r >> 1)) << 4), xa1 = kTurnX ? xa0 + kC / 2 * kRowX : xa0 ^ 64;
+    int wa0 = S * kX + (kTurnW ? turned(wn * NB, kRowW, TN) : (wn * 16 * NB + (r >> 2) * 8 + (r & 3)) * 128 + ((q ^ (r >> 1)) << 4));
+    int wa1 = kTurnW ? wa0 + kC / 2 * kRowW : wa0 ^ 64;
     int4v wf[2][NB], xf[2][MB];
-    auto read_w = [&](int h, int j) { wf[h][j] = *reinterpret_cast<const int4v*>(lds + (h ? wa1 : wa0) + ((j >> 1) * 32 + (j & 1) * 4) * 128); };
-    auto read_x = [&](int h, int i) { xf[h][i] = *reinterpret_cast<const int4v*>(lds + (h ? xa1 : xa0) + i * 2048); };
+    auto read = [&](int address, int block, int row_length) {      // turned: 16 i's of a block
+        const char* from = lds + (address ^ (block * kChunk));
+        if constexpr (sizeof(T) == 2) {
+            const int2v low = read_turned(from), high = read_turned(from + 4 * row_length);
+            return int4v{low[0], low[1], high[0], high[1]};
+        } else {
+            int4v v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const int*>(from + e * row_length);
+            return v;
+        }
+    };
+    auto read_w = [&](int h, int j) {
+        if constexpr (kTurnW) wf[h][j] = read(h ? wa1 : wa0, j, kRowW);
+        else wf[h][j] = *reinterpret_cast<const int4v*>(lds + (h ? wa1 : wa0) + ((j >> 1) * 32 + (j & 1) * 4) * 128);
+    };
+    auto read_x = [&](int h, int i) {
+        if constexpr (kTurnX) xf[h][i] = read(h ? xa1 : xa0, i, kRowX);
+        else xf[h][i] = *reinterpret_cast<const int4v*>(lds + (h ? xa1 : xa0) + i * 2048);
+    };
     asm volatile("s_waitcnt vmcnt(%0)" :: "n"((S - 1) * kLoads) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
@@ -344,34 +408,37 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 || S > 2 ? 1 : 2) void 
         // Bias, activation and residual, while the first steps of the next tile are on their way.  The last products are read: the matrix
         // unit's results need 18 clocks.
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
-        each<NB / 2>([&](auto pair) {
-            constexpr int j = 2 * pair;
-            const int tile_n = wn * 16 * NB + j * 16 + q * 8, n = n0 + tile_n;
-            float bias[8];
+        constexpr int kWide = kTurnW ? 4 : 8;      // channels in a row that a lane has
+        each<NB * 4 / kWide>([&](auto group) {
+            constexpr int j = group * kWide / 4;
+            const int tile_n = wn * 16 * NB + j * 16 + q * kWide, n = n0 + tile_n;
+            float bias[kWide];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) bias[e] = channel_bias[done][tile_n + e];
+            for (int e = 0; e < kWide; ++e) bias[e] = channel_bias[done][tile_n + e];
             each<MB>([&](auto block) {
                 constexpr int i = block;
                 const int m = m0 + (wm * MB + i) * 16 + r;
-                asm volatile("" : "+a"(acc[i][j]), "+a"(acc[i][j + 1]));
-                float v[8];
+                float v[kWide];
+                each<kWide / 4>([&](auto half) {
+                    asm volatile("" : "+a"(acc[i][j + half]));
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = acc[i][j + e / 4][e % 4];
-                acc[i][j] = acc[i][j + 1] = float4v{0.f, 0.f, 0.f, 0.f};
+                    for (int e = 0; e < 4; ++e) v[half * 4 + e] = acc[i][j + half][e];
+                    acc[i][j + half] = float4v{0.f, 0.f, 0.f, 0.f};
+                });
                 if (m >= a.M || n >= a.N) return;
                 if (a.partial) {
                     float* to = a.partial + ((size_t)part * a.M + m) * a.N + n;
                     typedef float four __attribute__((ext_vector_type(4), aligned(4)));
-                    if (n + 8 <= a.N) {
+                    if (n + kWide <= a.N) {
 #pragma unroll
-                        for (int c = 0; c < 2; ++c) reinterpret_cast<four*>(to)[c] = four{v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]};
+                        for (int c = 0; c < kWide / 4; ++c) reinterpret_cast<four*>(to)[c] = four{v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]};
                     } else {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
+                        for (int e = 0; e < kWide; ++e)
                             if (n + e < a.N) to[e] = v[e];
                     }
                 } else {
-                    finish<T, 8>(a, v, bias, m, n, a.N - n);
+                    finish<T, kWide>(a, v, bias, m, n, a.N - n);
                 }
             });
         });
@@ -398,7 +465,7 @@ __global__ __launch_bounds__(64 * W) void linear_row_kernel(ProductArgs a)
     const int r = lane & 15, q = lane >> 4;
     const int across = (a.N + kChannels - 1) / kChannels;
     const int m0 = (int)(blockIdx.x / across) * kTokens, n0 = (int)(blockIdx.x % across) * kChannels;
-    const int units = (a.row_bytes + 127) / 128;
+    const int row_bytes = bytes_of_rows<T>(a.terms), units = (row_bytes + 127) / 128;
 
     // Pieces of 16 bytes are permuted within the 128 bytes of a row as in the tile kernel.
     int4v from_w = descriptor_of(static_cast<const char*>(a.w) + (size_t)n0 * a.w_pitch, (long long)min(kChannels, a.N - n0) * a.w_pitch);
@@ -410,7 +477,7 @@ __global__ __launch_bounds__(64 * W) void linear_row_kernel(ProductArgs a)
     for (int o = 0; o < 2; ++o) {
         row[o] = (unsigned)(o * 8 + (lane >> 3));
         piece_of[o] = ((lane & 7) ^ ((o * 4 + (lane >> 4)) & 7)) << 4;
-        if ((units - 1) * 128 + (int)piece_of[o] >= a.row_bytes) behind |= 1u << o;
+        if ((units - 1) * 128 + (int)piece_of[o] >= row_bytes) behind |= 1u << o;
     }
     auto load = [&](int slot, int unit) {
         from_w[2] = unit < units ? bytes_w : 0;
@@ -961,19 +1028,22 @@ struct Choice {
     double us;
 };
 
-Choice choose(int dtype, int M, int N, int row_bytes)
+// turned: both operands or w alone (tile kernels take those).
+Choice choose(int dtype, int M, int N, int terms, bool turned)
 {
-    const double f = dtype == kF32 ? 8.0 : 1.0, bytes = row_bytes;
-    const int all = (row_bytes + 127) / 128;
-    Choice best{kRow11, 1, all, 0.0};
-    for (int k = 0; k < kKernels; ++k) {
+    const double f = dtype == kF32 ? 8.0 : 1.0;
+    const int row_bytes = (terms * (dtype == kF32 ? 4 : 2) + 15) / 16 * 16, all = (row_bytes + 127) / 128;
+    const double bytes = row_bytes;
+    Choice best{kKernels, 1, all, 0.0};
+    for (int k = turned ? kTile22 : 0; k < kKernels; ++k) {
         if (k == kTile88 && dtype == kF32) continue;
+        if (k == kDeep42 && turned) continue;
         for (int parts = 1; parts <= (k < kTile22 ? 1 : 64); parts *= 2) {
             const int steps = (all + parts - 1) / parts;
             if (parts > 1 && steps < 8) break;
             if (k == kTile88 && steps < kStepsToWalk) break;
             const double us = k < kTile22 ? row_estimate(kRowRules[k], M, N, bytes, f) : tile_estimate(kTileRules[k - kTile22], M, N, parts, bytes, f);
-            if ((k == 0 && parts == 1) || us < best.us) best = Choice{(Kernel)k, (all + steps - 1) / steps, steps, us};
+            if (best.kernel == kKernels || us < best.us) best = Choice{(Kernel)k, (all + steps - 1) / steps, steps, us};
         }
     }
     return best;
@@ -988,14 +1058,17 @@ int parts_of(double tiles, int all, double wanted, int least)
     return (all + steps - 1) / steps;
 }
 
-template <class T, int MB, int NB, int S>
+// Which operands are turned.
+enum Turned { kRows, kTurnedW, kTurnedBoth };
+
+template <class T, int MB, int NB, int S, Turned turned>
 int launch_tile(const ProductArgs& a, hipStream_t s)
 {
     const long long tiles = (long long)a.parts * ((a.M + 32ll * MB - 1) / (32 * MB)) * ((a.N + 32ll * NB - 1) / (32 * NB));
     const bool walks = kWalksOver<MB, NB> && a.steps >= kStepsToWalk;
     if (tiles >= (1ll << 31) || (!walks && (unsigned long long)tiles > most_groups(256))) return kTooLarge;
     const unsigned blocks = walks ? (unsigned)std::min(tiles, 256ll) : (unsigned)tiles;
-    hipLaunchKernelGGL((linear_tile_kernel<T, MB, NB, 2, 2, S>), dim3(blocks), dim3(256), 0, s, a, (unsigned)tiles, blocks);
+    hipLaunchKernelGGL((linear_tile_kernel<T, MB, NB, 2, 2, S, turned == kTurnedBoth, turned != kRows>), dim3(blocks), dim3(256), 0, s, a, (unsigned)tiles, blocks);
     return (int)hipGetLastError();
 }
 
@@ -1008,24 +1081,33 @@ int launch_row(const ProductArgs& a, hipStream_t s)
     return (int)hipGetLastError();
 }
 
-template <class T>
+template <class T, Turned turned>
 int launch_kernel(Kernel kernel, const ProductArgs& a, hipStream_t s)
 {
-    switch (kernel) {
+    if constexpr (turned == kRows) switch (kernel) {
         case kRow11: return launch_row<T, 1, 1, 8, 4>(a, s);
         case kRow21: return launch_row<T, 2, 1, 8, 2>(a, s);
         case kRow22: return launch_row<T, 2, 2, 4, 2>(a, s);
         case kRow41: return launch_row<T, 4, 1, 8, 1>(a, s);
         case kRow42: return launch_row<T, 4, 2, 4, 2>(a, s);
-        case kTile22: return launch_tile<T, 2, 2, 2>(a, s);
-        case kTile44: return launch_tile<T, 4, 4, 2>(a, s);
-        case kTile88:
-            if constexpr (sizeof(T) == 2) return launch_tile<T, 8, 8, 2>(a, s);
-            return kTooLarge;      // (never chosen)
-        case kDeep22: return launch_tile<T, 2, 2, 4>(a, s);
-        case kDeep42: return launch_tile<T, 4, 2, 4>(a, s);
-        default: return launch_tile<T, 4, 4, 3>(a, s);
+        case kDeep42: return launch_tile<T, 4, 2, 4, turned>(a, s);
+        default: break;
     }
+    if constexpr (sizeof(T) == 2)
+        if (kernel == kTile88) return launch_tile<T, 8, 8, 2, turned>(a, s);
+    switch (kernel) {
+        case kTile22: return launch_tile<T, 2, 2, 2, turned>(a, s);
+        case kTile44: return launch_tile<T, 4, 4, 2, turned>(a, s);
+        case kDeep22: return launch_tile<T, 2, 2, 4, turned>(a, s);
+        default: return launch_tile<T, 4, 4, 3, turned>(a, s);
+    }
+}
+
+template <class T>
+int launch_kernel(Kernel kernel, Turned turned, const ProductArgs& a, hipStream_t s)
+{
+    if (turned == kRows) return launch_kernel<T, kRows>(kernel, a, s);
+    return turned == kTurnedW ? launch_kernel<T, kTurnedW>(kernel, a, s) : launch_kernel<T, kTurnedBoth>(kernel, a, s);
 }
 
 template <class T>
@@ -1041,29 +1123,28 @@ long long round_up(long long n, long long to) { return (n + to - 1) / to * to; }
 
 long long partial_bytes(int parts, int M, int N) { return parts > 1 ? round_up(4ll * parts * M * N, 256) : 0; }
 
-// The product of rows that are laid out; partial: scratch memory of partial_bytes.
-int product(int dtype, const Choice& c, ProductArgs a, char* partial, hipStream_t s)
+// The product of operands that are laid out; partial: scratch memory of partial_bytes.
+int product(int dtype, const Choice& c, Turned turned, ProductArgs a, char* partial, hipStream_t s)
 {
     a.parts = c.parts;
     a.steps = c.steps;
     a.partial = c.parts > 1 ? reinterpret_cast<float*>(partial) : nullptr;
-    int e = dtype == kF32 ? launch_kernel<float>(c.kernel, a, s) : dtype == kF16 ? launch_kernel<_Float16>(c.kernel, a, s) : launch_kernel<__bf16>(c.kernel, a, s);
+    int e = dtype == kF32 ? launch_kernel<float>(c.kernel, turned, a, s) : dtype == kF16 ? launch_kernel<_Float16>(c.kernel, turned, a, s) : launch_kernel<__bf16>(c.kernel, turned, a, s);
     if (e != 0 || c.parts == 1) return e;
     return dtype == kF32 ? launch_join<float>(a, s) : dtype == kF16 ? launch_join<_Float16>(a, s) : launch_join<__bf16>(a, s);
 }
 
 // ---------------------------------------------------------------- rows laid out
 
-// Tiles of 64 x 64 elements of [rows][cols] (ld elements from one row to the next), each of: `copy`, rows of copy_pitch elements as they
-// are; `turned`, columns as rows of turned_pitch elements; both with zeros up to the pitch.  With an activation the elements are first
-// multiplied by its derivative at z, in fp32, and rounded once; column_sums [tiles down][cols] receives the sums over the
-// tile's rows of what was not rounded.
+// Tiles of 64 x 64 elements of [rows][cols] (ld elements from one row to the next) to `copy` (or null), rows of copy_pitch elements with zeros behind
+// what is there.  With an activation the elements are first multiplied by its slope at z (no gaps), in fp32, and rounded once; column_sums
+// [tiles down][cols] (or null) receives the sums over the tile's rows of what was not rounded.
 struct LayArgs {
     const void *from, *z;
-    void *copy, *turned;
+    void* copy;
     float* column_sums;
     long long ld;
-    int rows, cols, copy_pitch, turned_pitch, act;
+    int rows, cols, copy_pitch, act;
 };
 
 template <class T>
@@ -1071,68 +1152,64 @@ __global__ __launch_bounds__(256) void linear_lay_kernel(LayArgs a)
 {
     constexpr int kCount = 16 / sizeof(T), kPer = 64 / kCount, kTurns = 64 * kPer / 256;      // pieces a row of the tile; a thread's pieces
     typedef typename Piece<T>::type V;
-    typedef T A __attribute__((ext_vector_type(16 / sizeof(T))));
-    constexpr int kPitch = 64 + 16 / sizeof(T) / 2 + 1;
-    __shared__ T tile[64][kPitch];
     __shared__ float sums[256 / kPer][64];
-    const int across = (a.cols + 63) / 64, tr = (int)(blockIdx.x / (unsigned)across), tc = (int)(blockIdx.x % (unsigned)across);
+    const int across = (max(a.cols, a.copy_pitch) + 63) / 64, tr = (int)(blockIdx.x / (unsigned)across), tc = (int)(blockIdx.x % (unsigned)across);
     const int piece = threadIdx.x % kPer, first = threadIdx.x / kPer, col = tc * 64 + piece * kCount;
     float total[kCount] = {};
+    V v[kTurns], z[kTurns];
+    // (All loads first.  A piece that ends past its row is the last one within it, moved down.)
+    const int from = min(col, a.cols - kCount), moved = col - from;
+    auto whole = [&](const T* row) {
+        if (a.cols < kCount) return load_piece<T>(row, col, a.cols);
+        return *reinterpret_cast<const V*>(row + from);
+    };
+    auto place = [&](V& v) {
+        if (a.cols < kCount || moved <= 0) return;
+        const unsigned __int128 bits = __builtin_bit_cast(unsigned __int128, v);
+        v = __builtin_bit_cast(V, moved < kCount ? bits >> (moved * 8 * (int)sizeof(T)) : (unsigned __int128)0);
+    };
 #pragma unroll
-    for (int t = 0; t < kTurns; ++t) {
-        const int in = first + t * (256 / kPer), row = tr * 64 + in;
-        V v;
+    for (int t = 0; t < kTurns; ++t) v[t] = whole(static_cast<const T*>(a.from) + (size_t)min(tr * 64 + first + t * (256 / kPer), a.rows - 1) * a.ld);
+    if (a.z)
 #pragma unroll
-        for (int e = 0; e < kCount; ++e) v[e] = (T)0.f;
-        if (row < a.rows && col < a.cols) {
-            v = load_piece<T>(static_cast<const T*>(a.from) + (size_t)row * a.ld, col, a.cols);
-            float g[kCount];
+        for (int t = 0; t < kTurns; ++t) z[t] = whole(static_cast<const T*>(a.z) + (size_t)min(tr * 64 + first + t * (256 / kPer), a.rows - 1) * a.cols);
+    auto all = [&](auto act) {
 #pragma unroll
-            for (int e = 0; e < kCount; ++e) g[e] = (float)v[e];
-            if (a.z) {
-                const V z = load_piece<T>(static_cast<const T*>(a.z) + (size_t)row * a.cols, col, a.cols);
-                with_activation(a.act, [&](auto act) {
+        for (int t = 0; t < kTurns; ++t) {
+            const int row = tr * 64 + first + t * (256 / kPer);
+            if (row >= a.rows) break;
+            place(v[t]);
+            if constexpr (act != kNone) place(z[t]);
 #pragma unroll
-                    for (int e = 0; e < kCount; ++e) {
-                        g[e] = col + e < a.cols ? g[e] * slope<act>((float)z[e]) : 0.f;
-                        v[e] = (T)g[e];
-                    }
-                });
+            for (int e = 0; e < kCount; ++e) {
+                float g = (float)v[t][e];
+                if constexpr (act != kNone) {
+                    g = col + e < a.cols ? g * slope<act>((float)z[t][e]) : 0.f;
+                    v[t][e] = (T)g;
+                }
+                total[e] += g;
             }
+            if (a.copy && col < a.copy_pitch) {
+                T* const to = static_cast<T*>(a.copy) + (size_t)row * a.copy_pitch + col;
+                if (col + kCount <= a.copy_pitch) *reinterpret_cast<V*>(to) = v[t];
+                else
 #pragma unroll
-            for (int e = 0; e < kCount; ++e) total[e] += g[e];
+                    for (int e = 0; e < kCount; ++e)
+                        if (col + e < a.copy_pitch) to[e] = v[t][e];
+            }
         }
-        if (a.copy && row < a.rows && col < a.copy_pitch) {      // (a pitch of no whole pieces: no zeros behind the row)
-            T* const to = static_cast<T*>(a.copy) + (size_t)row * a.copy_pitch + col;
-            if (col + kCount <= a.copy_pitch) *reinterpret_cast<V*>(to) = v;
-            else
+    };
+    if (a.z) with_activation(a.act, all);
+    else all(std::integral_constant<int, kNone>{});
+    if (!a.column_sums) return;
 #pragma unroll
-                for (int e = 0; e < kCount; ++e)
-                    if (col + e < a.copy_pitch) to[e] = v[e];
-        }
-        if (a.turned)
-#pragma unroll
-            for (int e = 0; e < kCount; ++e) tile[in][piece * kCount + e] = v[e];
-    }
-    if (a.column_sums)
-#pragma unroll
-        for (int e = 0; e < kCount; ++e) sums[first][piece * kCount + e] = total[e];
+    for (int e = 0; e < kCount; ++e) sums[first][piece * kCount + e] = total[e];
     __syncthreads();
-    if (a.column_sums && threadIdx.x < 64 && tc * 64 + (int)threadIdx.x < a.cols) {
+    if (threadIdx.x < 64 && tc * 64 + (int)threadIdx.x < a.cols) {
         float s = 0.f;
 #pragma unroll
         for (int i = 0; i < 256 / kPer; ++i) s += sums[i][threadIdx.x];
         a.column_sums[(size_t)tr * a.cols + tc * 64 + threadIdx.x] = s;
-    }
-    if (!a.turned) return;
-#pragma unroll
-    for (int t = 0; t < kTurns; ++t) {
-        const int in = first + t * (256 / kPer), to = tc * 64 + in, at = tr * 64 + piece * kCount;
-        if (to >= a.cols || at >= a.turned_pitch) continue;
-        A v;
-#pragma unroll
-        for (int e = 0; e < kCount; ++e) v[e] = tile[piece * kCount + e][in];
-        *reinterpret_cast<A*>(static_cast<T*>(a.turned) + (size_t)to * a.turned_pitch + at) = v;
     }
 }
 
@@ -1172,7 +1249,7 @@ int launch_zeros(void* a, long long a_bytes, void* b, long long b_bytes, hipStre
 template <class T>
 int launch_lay_of(const LayArgs& a, hipStream_t s)
 {
-    const long long groups = ((a.rows + 63ll) / 64) * ((a.cols + 63ll) / 64);
+    const long long groups = ((a.rows + 63ll) / 64) * ((std::max(a.cols, a.copy_pitch) + 63ll) / 64);
     if ((unsigned long long)groups > most_groups(256)) return kTooLarge;
     hipLaunchKernelGGL(linear_lay_kernel<T>, dim3((unsigned)groups), dim3(256), 0, s, a);
     return (int)hipGetLastError();
@@ -1235,7 +1312,7 @@ LinearPlan plan_of(const LinearArgs& a, int dtype)
     const double tiles = pieces_of(a.M, 64) * pieces_of(a.N, 64);
     p.parts = parts_of(tiles, all, 256.0, 8);
     p.steps = (all + p.parts - 1) / p.parts;
-    p.laid = choose(dtype, a.M, a.N, row_bytes);
+    p.laid = choose(dtype, a.M, a.N, a.K, false);
     const double laid = p.laid.us + (p.lay_x ? lay_estimate(2.0 * a.M * row_bytes) : 0.0) + (p.lay_w ? lay_estimate(2.0 * a.N * row_bytes) : 0.0);
     const double direct = direct_estimate(dtype, tiles * all, p.steps, false) + join_estimate(p.parts, (double)a.M * a.N);
     if (direct < laid) {
@@ -1289,23 +1366,23 @@ int launch_linear(int dtype, const LinearArgs& a, char* workspace, void* stream)
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const int b = bytes_of(dtype), row_bytes = (int)pitch_of(a.K, b) * b;
     const LinearPlan plan = plan_of(a, dtype);
-    ProductArgs p{a.x, a.w, a.bias, a.residual, a.out, a.z, nullptr, a.M, a.N, row_bytes, (int)(a.M > 1 ? a.ldx * b : row_bytes), (int)(a.N > 1 ? a.ldw * b : row_bytes),
+    ProductArgs p{a.x, a.w, a.bias, a.residual, a.out, a.z, nullptr, a.M, a.N, a.K, (int)(a.M > 1 ? a.ldx * b : row_bytes), (int)(a.N > 1 ? a.ldw * b : row_bytes),
                   a.act, 0, 1, a.ldr, a.ldo};
     if (plan.way != kLaid)
         return dtype == kF32 ? launch_way<float>(plan, p, a, workspace, s) : dtype == kF16 ? launch_way<_Float16>(plan, p, a, workspace, s) : launch_way<__bf16>(plan, p, a, workspace, s);
     if (plan.lay_x) {
-        const int e = launch_lay(dtype, LayArgs{a.x, nullptr, workspace, nullptr, nullptr, a.ldx, a.M, a.K, row_bytes / b, 0, 0}, s);
+        const int e = launch_lay(dtype, LayArgs{a.x, nullptr, workspace, nullptr, a.ldx, a.M, a.K, row_bytes / b, kNone}, s);
         if (e != 0) return e;
         p.x = workspace;
         p.x_pitch = row_bytes;
     }
     if (plan.lay_w) {
-        const int e = launch_lay(dtype, LayArgs{a.w, nullptr, workspace + plan.x, nullptr, nullptr, a.ldw, a.N, a.K, row_bytes / b, 0, 0}, s);
+        const int e = launch_lay(dtype, LayArgs{a.w, nullptr, workspace + plan.x, nullptr, a.ldw, a.N, a.K, row_bytes / b, kNone}, s);
         if (e != 0) return e;
         p.w = workspace + plan.x;
         p.w_pitch = row_bytes;
     }
-    return product(dtype, plan.laid, p, workspace + plan.w, s);
+    return product(dtype, plan.laid, kRows, p, workspace + plan.w, s);
 }
 
 namespace {
@@ -1316,9 +1393,9 @@ struct GradPlan {
     int parts_x, parts_w, steps_x, steps_w;
     long long sums_x, sums_w, sums_bias;
     // laid out
-    bool own_dz;                                             // the gradient behind the activation is formed (else grad is it)
+    bool own_dz, lay_x, lay_w;                               // the gradient behind the activation is formed (else grad is it); x, w are copied
     Choice x, w;
-    long long dz, dz_turned, x_turned, w_turned, sums, partial;
+    long long dz, x_at, w_at, sums, partial;
     long long end;
 };
 
@@ -1327,6 +1404,8 @@ GradPlan plan_of(const LinearGradArgs& a, int dtype)
     const int b = bytes_of(dtype), count = 128 / b;
     GradPlan l{};
     l.own_dz = a.act != kNone || !laid_out(a.grad, a.ldg, a.M, a.N, b);
+    l.lay_x = a.grad_w && !laid_out(a.x, a.ldx, a.M, a.K, b);
+    l.lay_w = a.grad_x && !laid_out(a.w, a.ldw, a.N, a.K, b);
     long long at = 0;
     auto take = [&](bool wanted, long long bytes) {
         const long long here = at;
@@ -1335,9 +1414,10 @@ GradPlan plan_of(const LinearGradArgs& a, int dtype)
     };
     double laid = 0.0, direct = 0.0;
     // (Chosen as if all three were wanted: a gradient's bits do not depend on which others are.)
-    l.x = choose(dtype, a.M, a.K, (int)pitch_of(a.N, b) * b);
-    l.w = choose(dtype, a.N, a.K, (int)pitch_of(a.M, b) * b);
-    laid = l.x.us + l.w.us + lay_estimate(2.0 * a.N * a.K * b) + lay_estimate(2.0 * a.M * a.K * b) + lay_estimate(3.0 * a.M * a.N * b) + 3.0;
+    l.x = choose(dtype, a.M, a.K, a.N, true);
+    l.w = choose(dtype, a.N, a.K, a.M, true);
+    laid = l.x.us + l.w.us + lay_estimate((l.own_dz ? 3.0 : 1.0) * a.M * a.N * b) + 3.0;
+    if (a.K * b % 16 != 0) laid += lay_estimate(2.0 * a.N * a.K * b) + lay_estimate(2.0 * a.M * a.K * b);
     const double tiles_x = pieces_of(a.M, 64) * pieces_of(a.K, 64), tiles_w = pieces_of(a.N, 64) * pieces_of(a.K, 64);
     const int all_x = (a.N + count - 1) / count, all_w = (a.M + count - 1) / count;
     l.parts_x = parts_of(tiles_x, all_x, 256.0, 8);
@@ -1360,10 +1440,9 @@ GradPlan plan_of(const LinearGradArgs& a, int dtype)
         l.end = at;
         return l;
     }
-    l.dz = take(a.grad_x && l.own_dz, laid_bytes(a.M, a.N, b));
-    l.dz_turned = take(a.grad_w, laid_bytes(a.N, a.M, b));
-    l.x_turned = take(a.grad_w, laid_bytes(a.K, a.M, b));
-    l.w_turned = take(a.grad_x, laid_bytes(a.K, a.N, b));
+    l.dz = take(l.own_dz && (a.grad_x || a.grad_w), laid_bytes(a.M, a.N, b));
+    l.x_at = take(l.lay_x, laid_bytes(a.M, a.K, b));
+    l.w_at = take(l.lay_w, laid_bytes(a.N, a.K, b));
     l.sums = take(a.grad_bias, (a.M + 63ll) / 64 * a.N * 4);
     l.partial = take(true, std::max(a.grad_x ? partial_bytes(l.x.parts, a.M, a.K) : 0, a.grad_w ? partial_bytes(l.w.parts, a.N, a.K) : 0));
     l.end = at;
@@ -1392,7 +1471,7 @@ int launch_direct_grad(const GradPlan& l, const LinearGradArgs& a, char* workspa
     int e = 0;
     if (l.formed) {
         float* const sums = a.grad_bias ? reinterpret_cast<float*>(workspace + l.sums) : nullptr;
-        e = launch_lay_of<T>(LayArgs{a.grad, a.z, workspace + l.dz, nullptr, sums, a.ldg, a.M, a.N, a.N, 0, a.act}, s);
+        e = launch_lay_of<T>(LayArgs{a.grad, a.z, workspace + l.dz, sums, a.ldg, a.M, a.N, a.N, a.act}, s);
         if (e != 0) return e;
         d.grad = workspace + l.dz;
         d.z = nullptr;
@@ -1443,27 +1522,38 @@ int launch_linear_grad(int dtype, const LinearGradArgs& a, char* workspace, void
     const GradPlan l = plan_of(a, dtype);
     if (l.direct)
         return dtype == kF32 ? launch_direct_grad<float>(l, a, workspace, s) : dtype == kF16 ? launch_direct_grad<_Float16>(l, a, workspace, s) : launch_direct_grad<__bf16>(l, a, workspace, s);
-    const int m_pitch = (int)pitch_of(a.M, b), n_pitch = (int)pitch_of(a.N, b);
+    const int k_pitch = (int)pitch_of(a.K, b), n_pitch = (int)pitch_of(a.N, b);
     int e = 0;
-    if ((a.grad_x && l.own_dz) || a.grad_w || a.grad_bias) {
-        e = launch_lay(dtype, LayArgs{a.grad, a.act != kNone ? a.z : nullptr, a.grad_x && l.own_dz ? workspace + l.dz : nullptr, a.grad_w ? workspace + l.dz_turned : nullptr,
-                                      a.grad_bias ? reinterpret_cast<float*>(workspace + l.sums) : nullptr, a.ldg, a.M, a.N, n_pitch, m_pitch, a.act}, s);
+    const void *d = a.grad, *x = a.x, *w = a.w;
+    int d_bytes = (int)(a.M > 1 ? a.ldg * b : n_pitch * b), x_bytes = (int)(a.M > 1 ? a.ldx * b : k_pitch * b), w_bytes = (int)(a.N > 1 ? a.ldw * b : k_pitch * b);
+    const bool form = l.own_dz && (a.grad_x || a.grad_w);
+    if (form || a.grad_bias) {
+        e = launch_lay(dtype, LayArgs{a.grad, a.act != kNone ? a.z : nullptr, form ? workspace + l.dz : nullptr, a.grad_bias ? reinterpret_cast<float*>(workspace + l.sums) : nullptr,
+                                      a.ldg, a.M, a.N, n_pitch, a.act}, s);
         if (e != 0) return e;
+        if (form) {
+            d = workspace + l.dz;
+            d_bytes = n_pitch * b;
+        }
     }
     if (a.grad_bias && (e = launch_bias(reinterpret_cast<const float*>(workspace + l.sums), a.grad_bias, (a.M + 63) / 64, a.N, a.accumulate, s)) != 0) return e;
+    if (l.lay_x) {
+        if ((e = launch_lay(dtype, LayArgs{a.x, nullptr, workspace + l.x_at, nullptr, a.ldx, a.M, a.K, k_pitch, kNone}, s)) != 0) return e;
+        x = workspace + l.x_at;
+        x_bytes = k_pitch * b;
+    }
+    if (l.lay_w) {
+        if ((e = launch_lay(dtype, LayArgs{a.w, nullptr, workspace + l.w_at, nullptr, a.ldw, a.N, a.K, k_pitch, kNone}, s)) != 0) return e;
+        w = workspace + l.w_at;
+        w_bytes = k_pitch * b;
+    }
     if (a.grad_x) {
-        e = launch_lay(dtype, LayArgs{a.w, nullptr, nullptr, workspace + l.w_turned, nullptr, a.ldw, a.N, a.K, 0, n_pitch, 0}, s);
-        if (e != 0) return e;
-        const ProductArgs p{l.own_dz ? workspace + l.dz : a.grad, workspace + l.w_turned, nullptr, nullptr, a.grad_x, nullptr, nullptr, a.M, a.K, n_pitch * b,
-                            l.own_dz || a.M == 1 ? n_pitch * b : (int)(a.ldg * b), n_pitch * b, kNone, 0, 1, 0, a.K};
-        if ((e = product(dtype, l.x, p, workspace + l.partial, s)) != 0) return e;
+        const ProductArgs p{d, w, nullptr, nullptr, a.grad_x, nullptr, nullptr, a.M, a.K, a.N, d_bytes, w_bytes, kNone, 0, 1, 0, a.K};
+        if ((e = product(dtype, l.x, kTurnedW, p, workspace + l.partial, s)) != 0) return e;
     }
     if (a.grad_w) {
-        e = launch_lay(dtype, LayArgs{a.x, nullptr, nullptr, workspace + l.x_turned, nullptr, a.ldx, a.M, a.K, 0, m_pitch, 0}, s);
-        if (e != 0) return e;
-        const ProductArgs p{workspace + l.dz_turned, workspace + l.x_turned, nullptr, a.accumulate ? a.grad_w : nullptr, a.grad_w, nullptr, nullptr, a.N, a.K, m_pitch * b,
-                            m_pitch * b, m_pitch * b, kNone, 0, 1, a.K, a.K};
-        if ((e = product(dtype, l.w, p, workspace + l.partial, s)) != 0) return e;
+        const ProductArgs p{d, x, nullptr, a.accumulate ? a.grad_w : nullptr, a.grad_w, nullptr, nullptr, a.N, a.K, a.M, d_bytes, x_bytes, kNone, 0, 1, a.K, a.K};
+        if ((e = product(dtype, l.w, kTurnedBoth, p, workspace + l.partial, s)) != 0) return e;
     }
     return 0;
 }
