@@ -18,6 +18,7 @@ namespace {
 enum { kNone = 0, kRelu = 1, kGelu = 2, kSilu = 3 };   // SC_ACT_*
 
 typedef float float4v __attribute__((ext_vector_type(4)));
+typedef float float16v __attribute__((ext_vector_type(16)));
 typedef int int2v __attribute__((ext_vector_type(2)));
 
 // Elements of 16 bytes, as the matrix instructions take them.
@@ -104,6 +105,15 @@ __device__ __forceinline__ void multiply(float4v& c, int4v w, int4v x)
     else asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(w), "v"(x));
 }
 
+// The same over 32 x 32 outputs and 16 k's of 16 bits: lane l holds k = 8 (l / 32) .. + 7 of row l % 32 of each, and of w's rows 8 a + 4 (l / 32) + e
+// (a, e = 0 .. 3) the sums at column l % 32.
+template <class T, int e>
+__device__ __forceinline__ void multiply(float16v& c, int4v w, int4v x)
+{
+    if constexpr (std::is_same<T, _Float16>::value) asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+a"(c) : "v"(w), "v"(x));
+    else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(w), "v"(x));
+}
+
 // The same by the compiler's builtins, for kernels whose sums take few registers.
 template <class T>
 __device__ __forceinline__ float4v multiplied(float4v c, int4v w, int4v x)
@@ -121,7 +131,8 @@ __device__ __forceinline__ float4v multiplied(float4v c, int4v w, int4v x)
 }
 
 // C sums of a row (n .. n + C - 1 of row m, of which `count` are there) to the output: bias, activation, residual, in fp32 and rounded once.
-template <class T, int C>
+// kInside: all are there; kPlain: there is no activation, no residual and no z.
+template <class T, int C, bool kInside = false, bool kPlain = false>
 __device__ __forceinline__ void finish(const ProductArgs& a, const float (&sum)[C], const float (&bias)[C], int m, int n, int count)
 {
     typedef T V __attribute__((ext_vector_type(C), aligned(sizeof(T))));
@@ -132,27 +143,29 @@ __device__ __forceinline__ void finish(const ProductArgs& a, const float (&sum)[
         V y;
 #pragma unroll
         for (int e = 0; e < C; ++e) y[e] = (T)v[e];
-        if (count >= C) *reinterpret_cast<V*>(to) = y;
+        if (kInside || count >= C) *reinterpret_cast<V*>(to) = y;
         else
 #pragma unroll
             for (int e = 0; e < C; ++e)
                 if (e < count) to[e] = y[e];
     };
-    if (a.z) store(static_cast<T*>(a.z) + (size_t)m * a.N + n);
-    with_activation(a.act, [&](auto act) {
+    if constexpr (!kPlain) {
+        if (a.z) store(static_cast<T*>(a.z) + (size_t)m * a.N + n);
+        with_activation(a.act, [&](auto act) {
 #pragma unroll
-        for (int e = 0; e < C; ++e) v[e] = activate<act>(v[e]);
-    });
-    if (a.residual) {
-        const T* from = static_cast<const T*>(a.residual) + (size_t)m * a.ldr + n;
-        if (count >= C) {
-            const V r = *reinterpret_cast<const V*>(from);
+            for (int e = 0; e < C; ++e) v[e] = activate<act>(v[e]);
+        });
+        if (a.residual) {
+            const T* from = static_cast<const T*>(a.residual) + (size_t)m * a.ldr + n;
+            if (kInside || count >= C) {
+                const V r = *reinterpret_cast<const V*>(from);
 #pragma unroll
-            for (int e = 0; e < C; ++e) v[e] += (float)r[e];
-        } else {
+                for (int e = 0; e < C; ++e) v[e] += (float)r[e];
+            } else {
 #pragma unroll
-            for (int e = 0; e < C; ++e)
-                if (e < count) v[e] += (float)from[e];
+                for (int e = 0; e < C; ++e)
+                    if (e < count) v[e] += (float)from[e];
+            }
         }
     }
     store(static_cast<T*>(a.out) + (size_t)m * a.ldo + n);
@@ -172,33 +185,44 @@ __device__ __forceinline__ int2v read_turned(const char* at)
 // A load of a piece that lies past the rows' end: an offset that no descriptor reaches (they describe 2^31 bytes at most).
 __device__ __forceinline__ unsigned past(unsigned offset, unsigned beyond, int i) { return offset | ((beyond >> i) & 1u) << 31; }
 
-// What the number of a turned row's piece of 16 bytes is combined with (by exclusive or), row c of a tile of `length` i's.
-template <class T>
+// What the number of a turned row's piece of 16 bytes is combined with (by exclusive or), row c of a tile of `length` i's, blocks of B.
+template <class T, int B>
 __device__ __forceinline__ int swizzle_of(int c, int length)
 {
     if (sizeof(T) == 4) return ((c >> 2) & 3) << 2;
+    if (B == 32) return (length == 64 ? (c >> 1) & 1 : c & 3) << 2;
     return length == 64 ? (((c >> 1) & 1) | ((c >> 3) & 1) << 1) << 1 : ((c & 3) | ((c >> 3) & 1) << 2) << 1;
 }
+
+// The row of a block of B rows of w that row r of a matrix instruction takes, so that a lane's sums are of channels in a row (8 of two blocks of 16, 16
+// of a block of 32), counted over two blocks of 16; and what a row's pieces are permuted by.
+template <int B>
+__device__ __forceinline__ int channel_of(int r) { return B == 32 ? ((r >> 2) & 1) * 16 + (r >> 3) * 4 + (r & 3) : (r >> 2) * 8 + (r & 3); }
+template <int B>
+__device__ __forceinline__ int turn_of_w(int row) { return B == 32 ? ((row >> 1) & 3) | ((row >> 4) & 1) << 2 : ((row >> 1) & 1) | ((row >> 3) & 3) << 1; }
 
 // Large tiles: a workgroup has a CU to itself, so it walks over tiles, `stride` apart, and loads the next one's first steps before it
 // finishes one.  (Three steps a tile at least: a barrier lies between what reads a tile's biases and what loads over them.)
 template <int MB, int NB>
-constexpr bool kWalksOver = MB * NB >= 64;
+constexpr bool kWalksOver = MB * NB >= 64;      // (blocks of 16)
 constexpr int kStepsToWalk = 3;
 
 // A tile of 16 MB WM rows of x by 16 NB WN rows of w, 128 bytes of each a step; WM x WN wavefronts with MB x NB blocks of 16 x 16 sums.
 // S steps are in LDS or on their way there.  kTurnX, kTurnW: that operand is given the other way round, element (i, c) at c * pitch + i, as the
 // gradients need it: its step is a part of 128 / sizeof(T) such rows, which lie in LDS as they do in memory and are turned as they are read.
-template <class T, int MB, int NB, int WM, int WN, int S, bool kTurnX, bool kTurnW>
-__global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 || S > 2 ? 1 : 2) void linear_tile_kernel(ProductArgs a, unsigned tiles, unsigned stride)
+// Blocks of the matrix instructions are of B x B sums (32 of 16-bit types where a wavefront has 64 x 64 sums or more: half the operands a product).
+template <class T, int MB16, int NB16, int WM, int WN, int S, bool kTurnX, bool kTurnW>
+__global__ __launch_bounds__(64 * WM * WN, MB16 * NB16 >= 64 || S > 2 ? 1 : 2) void linear_tile_kernel(ProductArgs a, unsigned tiles, unsigned stride)
 {
-    constexpr int TM = 16 * MB * WM, TN = 16 * NB * WN, W = WM * WN, kC = 128 / sizeof(T);
+    constexpr int B = sizeof(T) == 2 && MB16 * NB16 >= 16 ? 32 : 16, MB = MB16 * 16 / B, NB = NB16 * 16 / B, kGroups = B / 16;      // groups of k's of a half step
+    typedef typename std::conditional<B == 32, float16v, float4v>::type Sums;
+    constexpr int TM = B * MB * WM, TN = B * NB * WN, W = WM * WN, kC = 128 / sizeof(T);
     constexpr int kLoadsX = TM / 8 / W, kLoadsW = TN / 8 / W, kLoads = kLoadsX + kLoadsW;
-    constexpr int kX = TM * 128, kW = TN * 128, kHalf = MB / 2;
-    static_assert(MB % 2 == 0 && NB % 2 == 0, "blocks come in pairs");
+    constexpr int kX = TM * 128, kW = TN * 128, FX = MB * kGroups, FW = NB * kGroups, kHalf = FX / 2;      // pieces of a half step that a lane reads
+    static_assert(MB16 % 2 == 0 && NB16 % 2 == 0, "blocks come in pairs");
     static_assert(TN % 64 == 0 && TN <= 64 * W, "a bias a thread");
     __shared__ __attribute__((aligned(256))) char lds[S * (kX + kW)];
-    constexpr int kSets = kWalksOver<MB, NB> ? 2 : 1;      // the tile that is finished, and the next one
+    constexpr int kSets = kWalksOver<MB16, NB16> ? 2 : 1;      // the tile that is finished, and the next one
     __shared__ __attribute__((aligned(16))) float channel_bias[kSets][TN];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -214,10 +238,10 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 || S > 2 ? 1 : 2) void 
         const int load = wave * (of_x ? kLoadsX : kLoadsW) + (of_x ? i : i - kLoadsX);
         if (of_x ? kTurnX : kTurnW) {
             const int pieces = (of_x ? TM : TN) * (int)sizeof(T) / 16, at = load * 64 + lane, c = at / pieces;
-            offset[i] = (unsigned)c * (of_x ? a.x_pitch : a.w_pitch) + ((at % pieces ^ swizzle_of<T>(c, of_x ? TM : TN)) << 4);
+            offset[i] = (unsigned)c * (of_x ? a.x_pitch : a.w_pitch) + ((at % pieces ^ swizzle_of<T, B>(c, of_x ? TM : TN)) << 4);
         } else {
             const int row = load * 8 + (lane >> 3);
-            const int turn = of_x || kTurnW ? (row >> 1) & 7 : ((row >> 1) & 1) | ((row >> 3) & 3) << 1;
+            const int turn = of_x ? (row >> 1) & 7 : turn_of_w<B>(row);
             const int piece = ((lane & 7) ^ turn) << 4;
             offset[i] = (unsigned)row * (of_x ? a.x_pitch : a.w_pitch) + piece;
             if ((all_steps - 1) * 128 + piece >= row_bytes) behind |= 1u << i;
@@ -266,7 +290,7 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 || S > 2 ? 1 : 2) void 
     auto advance = [&]() {
         if (++step == end) {
             tile += stride;
-            if (kWalksOver<MB, NB> && tile < tiles) {
+            if (kWalksOver<MB16, NB16> && tile < tiles) {
                 set ^= 1;
                 enter();
             }
@@ -290,30 +314,41 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 || S > 2 ? 1 : 2) void 
     xdst -= S * kX;
     wdst -= S * kW;
 
-    float4v acc[MB][NB];
+    Sums acc[MB][NB];
+    auto clear = [&](Sums& c) {
+#pragma unroll
+        for (int e = 0; e < B * B / 64; ++e) c[e] = 0.f;
+    };
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
-            acc[i][j] = float4v{0.f, 0.f, 0.f, 0.f};
+            clear(acc[i][j]);
             asm volatile("" : "+a"(acc[i][j]));
         }
 
-    // Where a lane reads: its row of block 0 and its piece; the second 64 bytes of a step are four pieces on (an exclusive or).
-    // Row r of a wavefront's block j of w stands for channel 32 (j / 2) + 8 (r / 4) + 4 (j % 2) + r % 4, so that a lane's sums of
-    // two blocks are eight channels in a row.
-    // (Where w is turned, of channel 16 j + r: its reads would take twice the time.)  Turned, a lane reads four c's of 16 bits at once, or one of fp32.
-    const int wm = wave % WM, wn = wave / WM, r = lane & 15, q = lane >> 4;
-    constexpr int kRowX = TM * (int)sizeof(T), kRowW = TN * (int)sizeof(T), kChunk = sizeof(T) == 2 ? 32 : 64;      // bytes of 16 i's
-    const int c_first = sizeof(T) == 2 ? 8 * q + (r >> 2) : 4 * q, in_chunk = sizeof(T) == 2 ? (r & 3) * 8 : r * 4;
+    // Where a lane reads: its row of block 0 and its piece; the second 64 bytes of a step are four pieces on, the second k's of 32 x 32 blocks two (an
+    // exclusive or).  (Where w is turned, r stands for channel r of a block: its reads would take twice the time.)  Turned, a lane reads four c's
+    // of 16 bits at once, or one of fp32.
+    const int wm = wave % WM, wn = wave / WM, r = lane % B, q = lane / B;
+    constexpr int kRowX = TM * (int)sizeof(T), kRowW = TN * (int)sizeof(T), kChunk = B * (int)sizeof(T);      // bytes of a block's i's
+    const int c_first = sizeof(T) == 2 ? 8 * q + ((lane & 15) >> 2) : 4 * q, in_chunk = sizeof(T) == 2 ? (B == 32 ? (lane & 16) * 2 : 0) + (lane & 3) * 8 : r * 4;
     auto turned = [&](int first_block, int row_length, int tile_length) {
-        return c_first * row_length + ((first_block * kChunk / 16) ^ swizzle_of<T>(c_first, tile_length)) * 16 + in_chunk;
+        return c_first * row_length + ((first_block * kChunk / 16) ^ swizzle_of<T, B>(c_first, tile_length)) * 16 + in_chunk;
     };
-    int xa0 = kTurnX ? turned(wm * MB, kRowX, TM) : (wm * 16 * MB + r) * 128 + ((q ^ (r >> 1)) << 4), xa1 = kTurnX ? xa0 + kC / 2 * kRowX : xa0 ^ 64;
-    int wa0 = S * kX + (kTurnW ? turned(wn * NB, kRowW, TN) : (wn * 16 * NB + (r >> 2) * 8 + (r & 3)) * 128 + ((q ^ (r >> 1)) << 4));
-    int wa1 = kTurnW ? wa0 + kC / 2 * kRowW : wa0 ^ 64;
-    int4v wf[2][NB], xf[2][MB];
-    auto read = [&](int address, int block, int row_length) {      // turned: 16 i's of a block
+    const int w_row = channel_of<B>(r);
+    int xa[2][kGroups], wa[2][kGroups];
+    xa[0][0] = kTurnX ? turned(wm * MB, kRowX, TM) : (wm * B * MB + r) * 128 + ((q ^ ((r >> 1) & 7)) << 4);
+    wa[0][0] = S * kX + (kTurnW ? turned(wn * NB, kRowW, TN) : (wn * B * NB + w_row) * 128 + ((q ^ turn_of_w<B>(w_row)) << 4));
+    each<2 * kGroups>([&](auto n) {
+        constexpr int h = n / kGroups, g = n % kGroups, c = (h * kGroups + g) * (kC / 2 / kGroups), pieces = h * 64 + g * 32;
+        if constexpr (n > 0) {
+            xa[h][g] = kTurnX ? xa[0][0] + c * kRowX : xa[0][0] ^ pieces;
+            wa[h][g] = kTurnW ? wa[0][0] + c * kRowW : wa[0][0] ^ pieces;
+        }
+    });
+    int4v wf[2][FW], xf[2][FX];
+    auto read = [&](int address, int block, int row_length) {      // turned: a block's i's
         const char* from = lds + (address ^ (block * kChunk));
         if constexpr (sizeof(T) == 2) {
             const int2v low = read_turned(from), high = read_turned(from + 4 * row_length);
@@ -325,24 +360,26 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 || S > 2 ? 1 : 2) void 
             return v;
         }
     };
-    auto read_w = [&](int h, int j) {
-        if constexpr (kTurnW) wf[h][j] = read(h ? wa1 : wa0, j, kRowW);
-        else wf[h][j] = *reinterpret_cast<const int4v*>(lds + (h ? wa1 : wa0) + ((j >> 1) * 32 + (j & 1) * 4) * 128);
+    auto read_w = [&](int h, int u) {
+        const int g = u / NB, j = u % NB;
+        if constexpr (kTurnW) wf[h][u] = read(wa[h][g], j, kRowW);
+        else wf[h][u] = *reinterpret_cast<const int4v*>(lds + wa[h][g] + (B == 32 ? j * 32 : (j >> 1) * 32 + (j & 1) * 4) * 128);
     };
-    auto read_x = [&](int h, int i) {
-        if constexpr (kTurnX) xf[h][i] = read(h ? xa1 : xa0, i, kRowX);
-        else xf[h][i] = *reinterpret_cast<const int4v*>(lds + (h ? xa1 : xa0) + i * 2048);
+    auto read_x = [&](int h, int u) {
+        const int g = u / MB, i = u % MB;
+        if constexpr (kTurnX) xf[h][u] = read(xa[h][g], i, kRowX);
+        else xf[h][u] = *reinterpret_cast<const int4v*>(lds + xa[h][g] + i * B * 128);
     };
     asm volatile("s_waitcnt vmcnt(%0)" :: "n"((S - 1) * kLoads) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 #pragma unroll
-    for (int j = 0; j < NB; ++j) read_w(0, j);
+    for (int j = 0; j < FW; ++j) read_w(0, j);
 #pragma unroll
     for (int i = 0; i < kHalf; ++i) read_x(0, i);
     __builtin_amdgcn_sched_barrier(0);
 
-    // A step is two halves of MB x NB products, 64 bytes each.  In the first, all that the second needs is read, one read every few
+    // A step is two halves, 64 bytes each.  In the first, all that the second needs is read, one read every few
     // products (a wavefront is alone on its SIMD and issues in order: reads or loads in a row leave the matrix unit without work).
     // Then nothing reads this buffer any more and, spread over the second half, it is loaded with the bytes of the step that is S on.
     // Halfway through, those of the next step (loaded S - 1 steps before) are waited for, and the first half's operands are read.
@@ -352,19 +389,19 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 || S > 2 ? 1 : 2) void 
             advance();
             const int dx = buffer == S - 1 ? (1 - S) * kX : kX, dw = buffer == S - 1 ? (1 - S) * kW : kW;      // to the next step's buffer
             buffer = buffer == S - 1 ? 0 : buffer + 1;
-            constexpr int kBlocks = MB * NB, kSlots = kBlocks * kSub<T>, kTurn = kSlots / 2;
+            constexpr int kProducts = FX * NB, kSlots = kProducts * kSub<T>, kTurn = kSlots / 2;      // (product t is of x's piece t / NB and of w's of the same k's)
             each<kSlots>([&](auto slot) {
-                constexpr int t = slot, i = t % kBlocks / NB, j = t % NB, kOps = kHalf + NB + MB;
-                multiply<T, t / kBlocks>(acc[i][j], wf[0][j], xf[0][i]);
-                if constexpr (t < kBlocks) {
-                    constexpr int first = (t * kOps + kBlocks - 1) / kBlocks, last = ((t + 1) * kOps + kBlocks - 1) / kBlocks;
+                constexpr int t = slot, u = t % kProducts / NB, j = t % NB, kOps = kHalf + FW + FX;
+                multiply<T, t / kProducts>(acc[u % MB][j], wf[0][u / MB * NB + j], xf[0][u]);
+                if constexpr (t < kProducts) {
+                    constexpr int first = (t * kOps + kProducts - 1) / kProducts, last = ((t + 1) * kOps + kProducts - 1) / kProducts;
                     each<last - first>([&](auto n) {
                         constexpr int o = first + n;
                         if constexpr (o < 2 * kHalf && o % 2 == 0) read_x(0, kHalf + o / 2);
                         else {
-                            constexpr int u = o < 2 * kHalf ? o / 2 : o - kHalf;
-                            if constexpr (u < NB) read_w(1, u);
-                            else read_x(1, u - NB);
+                            constexpr int v = o < 2 * kHalf ? o / 2 : o - kHalf;
+                            if constexpr (v < FW) read_w(1, v);
+                            else read_x(1, v - FW);
                         }
                     });
                 }
@@ -375,28 +412,31 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 || S > 2 ? 1 : 2) void 
             asm volatile("" ::: "memory");
             __builtin_amdgcn_sched_barrier(0);
             each<kSlots>([&](auto slot) {
-                constexpr int t = slot, i = t % kBlocks / NB, j = t % NB;
+                constexpr int t = slot, u = t % kProducts / NB, j = t % NB;
                 if constexpr (t == kTurn) {
                     constexpr int kIssued = (kTurn * kLoads + kSlots - 1) / kSlots;
                     asm volatile("s_waitcnt vmcnt(%0)" :: "n"(kIssued + (S - 2) * kLoads) : "memory");
                     __builtin_amdgcn_s_barrier();
                     asm volatile("" ::: "memory");
-                    xa0 += dx;
-                    xa1 += dx;
-                    wa0 += dw;
-                    wa1 += dw;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int g = 0; g < kGroups; ++g) {
+                            xa[h][g] += dx;
+                            wa[h][g] += dw;
+                        }
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                multiply<T, t / kBlocks>(acc[i][j], wf[1][j], xf[1][i]);
+                multiply<T, t / kProducts>(acc[u % MB][j], wf[1][u / MB * NB + j], xf[1][u]);
                 constexpr int first = (t * kLoads + kSlots - 1) / kSlots, last = ((t + 1) * kLoads + kSlots - 1) / kSlots;
                 each<last - first>([&](auto n) { load(first + n); });
                 if constexpr (t >= kTurn) {
-                    constexpr int kReads = NB + kHalf, kRoom = kSlots - kTurn, v = t - kTurn;
+                    constexpr int kReads = FW + kHalf, kRoom = kSlots - kTurn, v = t - kTurn;
                     constexpr int from = (v * kReads + kRoom - 1) / kRoom, to = ((v + 1) * kReads + kRoom - 1) / kRoom;
                     each<to - from>([&](auto n) {
                         constexpr int o = from + n;
-                        if constexpr (o < NB) read_w(0, o);
-                        else read_x(0, o - NB);
+                        if constexpr (o < FW) read_w(0, o);
+                        else read_x(0, o - FW);
                     });
                 }
                 __builtin_amdgcn_sched_barrier(0);
@@ -408,41 +448,58 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 || S > 2 ? 1 : 2) void 
         // Bias, activation and residual, while the first steps of the next tile are on their way.  The last products are read: the matrix
         // unit's results need 18 clocks.
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
-        constexpr int kWide = kTurnW ? 4 : 8;      // channels in a row that a lane has
-        each<NB * 4 / kWide>([&](auto group) {
-            constexpr int j = group * kWide / 4;
-            const int tile_n = wn * 16 * NB + j * 16 + q * kWide, n = n0 + tile_n;
-            float bias[kWide];
+        // A lane's channels of a unit, and how many of them lie in a row: 8 and 8 of two blocks of 16, 16 and 16 of a block of 32; 4 at once where w is turned.
+        constexpr int kUnit = B == 32 ? 16 : kTurnW ? 4 : 8, kWide = kTurnW ? 4 : 8, kPerUnit = B == 16 && !kTurnW ? 2 : 1;
+        auto epilogue = [&](auto inside, auto plain) {
+            each<NB / kPerUnit>([&](auto unit) {
+                constexpr int j = unit * kPerUnit;
+                auto channel = [&](int run) { return wn * B * NB + j * B + (B == 32 ? (kTurnW ? run * 8 + q * 4 : q * 16 + run * 8) : q * kWide); };
+                float bias[kUnit];
 #pragma unroll
-            for (int e = 0; e < kWide; ++e) bias[e] = channel_bias[done][tile_n + e];
-            each<MB>([&](auto block) {
-                constexpr int i = block;
-                const int m = m0 + (wm * MB + i) * 16 + r;
-                float v[kWide];
-                each<kWide / 4>([&](auto half) {
-                    asm volatile("" : "+a"(acc[i][j + half]));
+                for (int e = 0; e < kUnit; ++e) bias[e] = channel_bias[done][channel(e / kWide) + e % kWide];
+                each<MB>([&](auto block) {
+                    constexpr int i = block;
+                    const int m = m0 + (wm * MB + i) * B + r;
+                    float v[kUnit];
+                    each<kPerUnit>([&](auto of) {
+                        Sums& c = acc[i][j + of];
+                        asm volatile("" : "+a"(c));
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[half * 4 + e] = acc[i][j + half][e];
-                    acc[i][j + half] = float4v{0.f, 0.f, 0.f, 0.f};
+                        for (int e = 0; e < kUnit / kPerUnit; ++e) v[of * (kUnit / kPerUnit) + e] = c[e];
+                        clear(c);
+                    });
+                    if (!inside && m >= a.M) return;
+                    each<kUnit / kWide>([&](auto run) {
+                        const int n = n0 + channel(run);
+                        if (!inside && n >= a.N) return;
+                        float sum[kWide], more[kWide];
+#pragma unroll
+                        for (int e = 0; e < kWide; ++e) {
+                            sum[e] = v[run * kWide + e];
+                            more[e] = bias[run * kWide + e];
+                        }
+                        if (!plain && a.partial) {
+                            float* to = a.partial + ((size_t)part * a.M + m) * a.N + n;
+                            typedef float four __attribute__((ext_vector_type(4), aligned(4)));
+                            if (inside || n + kWide <= a.N) {
+#pragma unroll
+                                for (int c = 0; c < kWide / 4; ++c) reinterpret_cast<four*>(to)[c] = four{sum[4 * c], sum[4 * c + 1], sum[4 * c + 2], sum[4 * c + 3]};
+                            } else {
+#pragma unroll
+                                for (int e = 0; e < kWide; ++e)
+                                    if (n + e < a.N) to[e] = sum[e];
+                            }
+                        } else {
+                            finish<T, kWide, inside, plain>(a, sum, more, m, n, a.N - n);
+                        }
+                    });
                 });
-                if (m >= a.M || n >= a.N) return;
-                if (a.partial) {
-                    float* to = a.partial + ((size_t)part * a.M + m) * a.N + n;
-                    typedef float four __attribute__((ext_vector_type(4), aligned(4)));
-                    if (n + kWide <= a.N) {
-#pragma unroll
-                        for (int c = 0; c < kWide / 4; ++c) reinterpret_cast<four*>(to)[c] = four{v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]};
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < kWide; ++e)
-                            if (n + e < a.N) to[e] = v[e];
-                    }
-                } else {
-                    finish<T, kWide>(a, v, bias, m, n, a.N - n);
-                }
             });
-        });
-        if (!kWalksOver<MB, NB>) break;
+        };
+        if (m0 + TM > a.M || n0 + TN > a.N) epilogue(std::false_type{}, std::false_type{});
+        else if (a.partial || a.act != kNone || a.residual || a.z) epilogue(std::true_type{}, std::false_type{});
+        else epilogue(std::true_type{}, std::true_type{});
+        if (!kWalksOver<MB16, NB16>) break;
         m0 = next_m;
         n0 = next_n;
         part = next_part;
