@@ -12,7 +12,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsparseconv.so")
 TORCH_LIB = os.path.join(HERE, "_text_torch.so")
 SOURCES = ["kernels.hip", "matrix_f32.hip", "matrix_f16.hip", "probes.hip", "api.cpp", "plan.cpp", "matrix_plan.cpp", "host_csr.cpp",
-           "embed.hip", "int8.hip", "linear.hip", "loss.hip", "adamw.hip", "text_api.cpp"]
+           "embed.hip", "int8.hip", "linear.hip", "linear_laid_f32.hip", "linear_laid_f16.hip", "linear_laid_bf16.hip",
+           "loss.hip", "adamw.hip", "text_api.cpp"]
 
 # packed fp32 VALU forms are switched off for the device pass (the host pass
 # prints a harmless "not a recognized feature" note for the same flag)

@@ -8,601 +8,11 @@
 #include <algorithm>
 #include <cmath>
 
-#include "text_ops.h"
-#include "tiles.h"
+#include "linear.h"
 
 namespace sc {
 
 namespace {
-
-enum { kNone = 0, kRelu = 1, kGelu = 2, kSilu = 3 };   // SC_ACT_*
-
-typedef float float4v __attribute__((ext_vector_type(4)));
-typedef float float16v __attribute__((ext_vector_type(16)));
-typedef int int2v __attribute__((ext_vector_type(2)));
-
-// Elements of 16 bytes, as the matrix instructions take them.
-template <class T>
-using Eight = T __attribute__((ext_vector_type(16 / sizeof(T))));
-
-// What a launch multiplies.  (Arguments past 112 bytes cost the host 0.75 us more.)
-struct ProductArgs {
-    const void *x, *w;              // rows along the sum, whole pieces of 16 bytes, x_pitch and w_pitch bytes apart; turned: see the tile kernel
-    const float* bias;              // or null
-    const void* residual;           // or null
-    void *out, *z;                  // z: what goes into the activation, or null
-    float* partial;                 // or null.  Else a part of k each: sums [part][M][N], and nothing of the above
-    int M, N, terms, x_pitch, w_pitch;      // terms: of a sum
-    int act;
-    int steps;                      // of 128 bytes, a part
-    int parts;
-    long long ldr, ldo;             // elements; z has N
-};
-
-// ---------------------------------------------------------------- activations
-
-constexpr float kLog2e = 1.4426950408889634f;
-
-constexpr float kNormal[7] = {-2.302209377e+00f, -1.048351228e-01f, 9.404921002e-05f, 1.595799404e-04f, -1.143983536e-05f, 3.816313949e-07f, -5.067239961e-09f};
-
-// The normal distribution's Phi.  log(Phi(z) / Phi(-z)) is odd and smooth: z times a polynomial of z^2, fitted here up to |z| = 5.5 for
-// the least error of Phi, 1.3e-7 (beyond, Phi is within 1e-7 of 0 or 1, and the polynomial goes on towards infinity).  Two transcendental
-// instructions, where erff takes the longest part of an epilogue.
-__device__ __forceinline__ float normal(float z)
-{
-    const float u = z * z;
-    float p = kNormal[6];
-#pragma unroll
-    for (int i = 5; i >= 0; --i) p = fmaf(p, u, kNormal[i]);
-    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(p * z));
-}
-
-__device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * z)); }
-
-template <int kAct>
-__device__ __forceinline__ float activate(float z)
-{
-    if (kAct == kRelu) return z < 0.f ? 0.f : z;
-    if (kAct == kGelu) return z * normal(z);
-    if (kAct == kSilu) return z * logistic(z);
-    return z;
-}
-
-// The derivative.
-template <int kAct>
-__device__ __forceinline__ float slope(float z)
-{
-    if (kAct == kRelu) return z > 0.f ? 1.f : z == z ? 0.f : z;
-    if (kAct == kGelu) return fmaf(z * 0.39894228040143268f, __builtin_amdgcn_exp2f(-0.5f * kLog2e * z * z), normal(z));
-    if (kAct == kSilu) {
-        const float s = logistic(z);
-        return s * fmaf(z, 1.f - s, 1.f);
-    }
-    return 1.f;
-}
-
-// f with the activation as a constant: one branch for all the elements that it takes.
-template <class F>
-__device__ __forceinline__ void with_activation(int act, F&& f)
-{
-    if (act == kRelu) f(std::integral_constant<int, kRelu>{});
-    else if (act == kGelu) f(std::integral_constant<int, kGelu>{});
-    else if (act == kSilu) f(std::integral_constant<int, kSilu>{});
-}
-
-// ---------------------------------------------------------------- products
-
-// A piece of 16 bytes of x and of w: lane l holds k = its share l / 16 of row l % 16 of each, and rows 4 (l / 16) .. + 3 of w's 16 at
-// column l % 16 (of x) of the sums.  fp32 pieces take four instructions, e = 0 .. 3.  The sums stay in accumulation registers.
-template <class T>
-constexpr int kSub = sizeof(T) == 4 ? 4 : 1;
-
-template <class T, int e>
-__device__ __forceinline__ void multiply(float4v& c, int4v w, int4v x)
-{
-    if constexpr (std::is_same<T, float>::value) asm volatile("v_mfma_f32_16x16x4_f32 %0, %1, %2, %0" : "+a"(c) : "v"(w[e]), "v"(x[e]));
-    else if constexpr (std::is_same<T, _Float16>::value) asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(w), "v"(x));
-    else asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(w), "v"(x));
-}
-
-// The same over 32 x 32 outputs and 16 k's of 16 bits: lane l holds k = 8 (l / 32) .. + 7 of row l % 32 of each, and of w's rows 8 a + 4 (l / 32) + e
-// (a, e = 0 .. 3) the sums at column l % 32.
-template <class T, int e>
-__device__ __forceinline__ void multiply(float16v& c, int4v w, int4v x)
-{
-    if constexpr (std::is_same<T, _Float16>::value) asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+a"(c) : "v"(w), "v"(x));
-    else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(w), "v"(x));
-}
-
-// The same by the compiler's builtins, for kernels whose sums take few registers.
-template <class T>
-__device__ __forceinline__ float4v multiplied(float4v c, int4v w, int4v x)
-{
-    if constexpr (std::is_same<T, float>::value) {
-        const float4v a = __builtin_bit_cast(float4v, w), b = __builtin_bit_cast(float4v, x);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
-        return c;
-    } else if constexpr (std::is_same<T, _Float16>::value) {
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(Eight<_Float16>, w), __builtin_bit_cast(Eight<_Float16>, x), c, 0, 0, 0);
-    } else {
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Eight<__bf16>, w), __builtin_bit_cast(Eight<__bf16>, x), c, 0, 0, 0);
-    }
-}
-
-// C sums of a row (n .. n + C - 1 of row m, of which `count` are there) to the output: bias, activation, residual, in fp32 and rounded once.
-// kInside: all are there; kPlain: there is no activation, no residual and no z.
-template <class T, int C, bool kInside = false, bool kPlain = false>
-__device__ __forceinline__ void finish(const ProductArgs& a, const float (&sum)[C], const float (&bias)[C], int m, int n, int count)
-{
-    typedef T V __attribute__((ext_vector_type(C), aligned(sizeof(T))));
-    float v[C];
-#pragma unroll
-    for (int e = 0; e < C; ++e) v[e] = sum[e] + bias[e];
-    auto store = [&](T* to) {
-        V y;
-#pragma unroll
-        for (int e = 0; e < C; ++e) y[e] = (T)v[e];
-        if (kInside || count >= C) *reinterpret_cast<V*>(to) = y;
-        else
-#pragma unroll
-            for (int e = 0; e < C; ++e)
-                if (e < count) to[e] = y[e];
-    };
-    if constexpr (!kPlain) {
-        if (a.z) store(static_cast<T*>(a.z) + (size_t)m * a.N + n);
-        with_activation(a.act, [&](auto act) {
-#pragma unroll
-            for (int e = 0; e < C; ++e) v[e] = activate<act>(v[e]);
-        });
-        if (a.residual) {
-            const T* from = static_cast<const T*>(a.residual) + (size_t)m * a.ldr + n;
-            if (kInside || count >= C) {
-                const V r = *reinterpret_cast<const V*>(from);
-#pragma unroll
-                for (int e = 0; e < C; ++e) v[e] += (float)r[e];
-            } else {
-#pragma unroll
-                for (int e = 0; e < C; ++e)
-                    if (e < count) v[e] += (float)from[e];
-            }
-        }
-    }
-    store(static_cast<T*>(a.out) + (size_t)m * a.ldo + n);
-}
-
-template <class T>
-__device__ __forceinline__ int bytes_of_rows(int terms) { return (terms * (int)sizeof(T) + 15) / 16 * 16; }
-
-// Four elements of each of 16 rows that lie along i, as four elements along c of each of 16 i's: lane l of 16 gives the address of elements
-// 4 (l % 4) .. + 3 of row l / 4, and gets rows 0 .. 3 of element l.
-__device__ __forceinline__ int2v read_turned(const char* at)
-{
-    typedef short short4v __attribute__((ext_vector_type(4)));
-    return __builtin_bit_cast(int2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((SC_LDS short4v*)(SC_LDS char*)at));
-}
-
-// A load of a piece that lies past the rows' end: an offset that no descriptor reaches (they describe 2^31 bytes at most).
-__device__ __forceinline__ unsigned past(unsigned offset, unsigned beyond, int i) { return offset | ((beyond >> i) & 1u) << 31; }
-
-// What the number of a turned row's piece of 16 bytes is combined with (by exclusive or), row c of a tile of `length` i's, blocks of B.
-template <class T, int B>
-__device__ __forceinline__ int swizzle_of(int c, int length)
-{
-    if (sizeof(T) == 4) return ((c >> 2) & 3) << 2;
-    if (B == 32) return (length == 64 ? (c >> 1) & 1 : c & 3) << 2;
-    return length == 64 ? (((c >> 1) & 1) | ((c >> 3) & 1) << 1) << 1 : ((c & 3) | ((c >> 3) & 1) << 2) << 1;
-}
-
-// The row of a block of B rows of w that row r of a matrix instruction takes, so that a lane's sums are of channels in a row (8 of two blocks of 16, 16
-// of a block of 32), counted over two blocks of 16; and what a row's pieces are permuted by.
-template <int B>
-__device__ __forceinline__ int channel_of(int r) { return B == 32 ? ((r >> 2) & 1) * 16 + (r >> 3) * 4 + (r & 3) : (r >> 2) * 8 + (r & 3); }
-template <int B>
-__device__ __forceinline__ int turn_of_w(int row) { return B == 32 ? ((row >> 1) & 3) | ((row >> 4) & 1) << 2 : ((row >> 1) & 1) | ((row >> 3) & 3) << 1; }
-
-// Large tiles: a workgroup has a CU to itself, so it walks over tiles, `stride` apart, and loads the next one's first steps before it
-// finishes one.  (Three steps a tile at least: a barrier lies between what reads a tile's biases and what loads over them.)
-template <int MB, int NB>
-constexpr bool kWalksOver = MB * NB >= 64;      // (blocks of 16)
-constexpr int kStepsToWalk = 3;
-
-// A tile of 16 MB WM rows of x by 16 NB WN rows of w, 128 bytes of each a step; WM x WN wavefronts with MB x NB blocks of 16 x 16 sums.
-// S steps are in LDS or on their way there.  kTurnX, kTurnW: that operand is given the other way round, element (i, c) at c * pitch + i, as the
-// gradients need it: its step is a part of 128 / sizeof(T) such rows, which lie in LDS as they do in memory and are turned as they are read.
-// Blocks of the matrix instructions are of B x B sums (32 of 16-bit types where a wavefront has 64 x 64 sums or more: half the operands a product).
-template <class T, int MB16, int NB16, int WM, int WN, int S, bool kTurnX, bool kTurnW>
-__global__ __launch_bounds__(64 * WM * WN, MB16 * NB16 >= 64 || S > 2 ? 1 : 2) void linear_tile_kernel(ProductArgs a, unsigned tiles, unsigned stride)
-{
-    constexpr int B = sizeof(T) == 2 && MB16 * NB16 >= 16 ? 32 : 16, MB = MB16 * 16 / B, NB = NB16 * 16 / B, kGroups = B / 16;      // groups of k's of a half step
-    typedef typename std::conditional<B == 32, float16v, float4v>::type Sums;
-    constexpr int TM = B * MB * WM, TN = B * NB * WN, W = WM * WN, kC = 128 / sizeof(T);
-    constexpr int kLoadsX = TM / 8 / W, kLoadsW = TN / 8 / W, kLoads = kLoadsX + kLoadsW;
-    constexpr int kX = TM * 128, kW = TN * 128, FX = MB * kGroups, FW = NB * kGroups, kHalf = FX / 2;      // pieces of a half step that a lane reads
-    static_assert(MB16 % 2 == 0 && NB16 % 2 == 0, "blocks come in pairs");
-    static_assert(TN % 64 == 0 && TN <= 64 * W, "a bias a thread");
-    __shared__ __attribute__((aligned(256))) char lds[S * (kX + kW)];
-    constexpr int kSets = kWalksOver<MB16, NB16> ? 2 : 1;      // the tile that is finished, and the next one
-    __shared__ __attribute__((aligned(16))) float channel_bias[kSets][TN];
-
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int row_bytes = bytes_of_rows<T>(a.terms);
-    const int down = (a.M + TM - 1) / TM, across = (a.N + TN - 1) / TN, steps = a.steps, all_steps = (row_bytes + 127) / 128;
-    // A row of LDS is the 128 bytes of a row's step; its eight pieces of 16 bytes are permuted by the row, so that the 16 rows that a
-    // read takes one piece of lie in 16 different groups of four banks.  A lane's load fetches the piece that belongs where it lands.
-    // Turned, a row of LDS is the tile's i's at one c, 32 bytes (64 of fp32) permuted by c so that the 16 (4) rows of a read lie in different banks.
-    unsigned offset[kLoads], behind = 0;      // behind: bit i, load i's piece of the last step lies past the end of its row
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-        const bool of_x = i < kLoadsX;
-        const int load = wave * (of_x ? kLoadsX : kLoadsW) + (of_x ? i : i - kLoadsX);
-        if (of_x ? kTurnX : kTurnW) {
-            const int pieces = (of_x ? TM : TN) * (int)sizeof(T) / 16, at = load * 64 + lane, c = at / pieces;
-            offset[i] = (unsigned)c * (of_x ? a.x_pitch : a.w_pitch) + ((at % pieces ^ swizzle_of<T, B>(c, of_x ? TM : TN)) << 4);
-        } else {
-            const int row = load * 8 + (lane >> 3);
-            const int turn = of_x ? (row >> 1) & 7 : turn_of_w<B>(row);
-            const int piece = ((lane & 7) ^ turn) << 4;
-            offset[i] = (unsigned)row * (of_x ? a.x_pitch : a.w_pitch) + piece;
-            if ((all_steps - 1) * 128 + piece >= row_bytes) behind |= 1u << i;
-        }
-    }
-    const unsigned lds0 = (unsigned)(uintptr_t)(SC_LDS char*)lds;
-    int4v from_x = {0, 0, 0, 0}, from_w = from_x;
-    int bytes_x = 0, bytes_w = 0;
-    unsigned xdst = lds0, wdst = lds0 + S * kX, tile = blockIdx.x, beyond = 0;
-    int next_m = 0, next_n = 0, next_part = 0, step = 0, end = 0, set = 0;      // what is loaded: a step of a tile, whose biases go to `set`
-    unsigned at = 0;                                                            // where it begins in its rows
-    auto enter = [&]() {
-        int tm, tn;
-        tile_of(tile, tiles, down * a.parts, across, tm, tn);      // (the parts of a tile as further tiles below it)
-        next_part = tm / down;
-        next_m = (tm - next_part * down) * TM;
-        next_n = tn * TN;
-        step = next_part * steps;
-        end = step + steps;
-        if (!kTurnX) from_x = descriptor_of(static_cast<const char*>(a.x) + (size_t)next_m * a.x_pitch, (long long)min(TM, a.M - next_m) * a.x_pitch);
-        if (!kTurnW) from_w = descriptor_of(static_cast<const char*>(a.w) + (size_t)next_n * a.w_pitch, (long long)min(TN, a.N - next_n) * a.w_pitch);
-        bytes_x = from_x[2];
-        bytes_w = from_w[2];
-        if (wave * 64 < TN) {
-            if (a.bias)
-                load_word_to_lds(descriptor_of(a.bias + next_n, min(TN, a.N - next_n) * 4ll), threadIdx.x * 4,
-                                 (unsigned)(uintptr_t)(SC_LDS float*)channel_bias[set] + wave * 256);
-            else channel_bias[set][threadIdx.x] = 0.f;
-        }
-    };
-    // (Each of these scalars is set in one place: with a branch for each reason to fetch nothing the compiler lost the descriptors' zeros.)
-    auto look = [&]() {
-        const bool there = step < min(end, all_steps);      // else zeros: past the last tile, or past the rows (in the last part)
-        const int c = there ? step * kC : 0, rows = min(kC, a.terms - c) - 1;
-        if (kTurnX)
-            from_x = descriptor_of(static_cast<const char*>(a.x) + (size_t)c * a.x_pitch + (size_t)next_m * sizeof(T),
-                                   there ? (long long)rows * a.x_pitch + bytes_of_rows<T>(a.M - next_m) : 0ll);
-        else from_x[2] = there ? bytes_x : 0;
-        if (kTurnW)
-            from_w = descriptor_of(static_cast<const char*>(a.w) + (size_t)c * a.w_pitch + (size_t)next_n * sizeof(T),
-                                   there ? (long long)rows * a.w_pitch + bytes_of_rows<T>(a.N - next_n) : 0ll);
-        else from_w[2] = there ? bytes_w : 0;
-        at = there ? step * 128 : 0;
-        beyond = step == all_steps - 1 ? behind : 0;
-    };
-    auto advance = [&]() {
-        if (++step == end) {
-            tile += stride;
-            if (kWalksOver<MB16, NB16> && tile < tiles) {
-                set ^= 1;
-                enter();
-            }
-        }
-        look();
-    };
-    auto load = [&](int i) {
-        if (i < kLoadsX) load_to_lds(from_x, kTurnX ? offset[i] : past(offset[i], beyond, i), kTurnX ? 0 : at, xdst + (wave * kLoadsX + i) * 1024);
-        else load_to_lds(from_w, kTurnW ? offset[i] : past(offset[i], beyond, i), kTurnW ? 0 : at, wdst + (wave * kLoadsW + i - kLoadsX) * 1024);
-    };
-    enter();
-    look();
-    int m0 = next_m, n0 = next_n, part = next_part, done = set;
-    each<S>([&](auto stage) {
-        if constexpr (stage > 0) advance();
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) load(i);
-        xdst += kX;
-        wdst += kW;
-    });
-    xdst -= S * kX;
-    wdst -= S * kW;
-
-    Sums acc[MB][NB];
-    auto clear = [&](Sums& c) {
-#pragma unroll
-        for (int e = 0; e < B * B / 64; ++e) c[e] = 0.f;
-    };
-#pragma unroll
-    for (int i = 0; i < MB; ++i)
-#pragma unroll
-        for (int j = 0; j < NB; ++j) {
-            clear(acc[i][j]);
-            asm volatile("" : "+a"(acc[i][j]));
-        }
-
-    // Where a lane reads: its row of block 0 and its piece; the second 64 bytes of a step are four pieces on, the second k's of 32 x 32 blocks two (an
-    // exclusive or).  (Where w is turned, r stands for channel r of a block: its reads would take twice the time.)  Turned, a lane reads four c's
-    // of 16 bits at once, or one of fp32.
-    const int wm = wave % WM, wn = wave / WM, r = lane % B, q = lane / B;
-    constexpr int kRowX = TM * (int)sizeof(T), kRowW = TN * (int)sizeof(T), kChunk = B * (int)sizeof(T);      // bytes of a block's i's
-    const int c_first = sizeof(T) == 2 ? 8 * q + ((lane & 15) >> 2) : 4 * q, in_chunk = sizeof(T) == 2 ? (B == 32 ? (lane & 16) * 2 : 0) + (lane & 3) * 8 : r * 4;
-    auto turned = [&](int first_block, int row_length, int tile_length) {
-        return c_first * row_length + ((first_block * kChunk / 16) ^ swizzle_of<T, B>(c_first, tile_length)) * 16 + in_chunk;
-    };
-    const int w_row = channel_of<B>(r);
-    int xa[2][kGroups], wa[2][kGroups];
-    xa[0][0] = kTurnX ? turned(wm * MB, kRowX, TM) : (wm * B * MB + r) * 128 + ((q ^ ((r >> 1) & 7)) << 4);
-    wa[0][0] = S * kX + (kTurnW ? turned(wn * NB, kRowW, TN) : (wn * B * NB + w_row) * 128 + ((q ^ turn_of_w<B>(w_row)) << 4));
-    each<2 * kGroups>([&](auto n) {
-        constexpr int h = n / kGroups, g = n % kGroups, c = (h * kGroups + g) * (kC / 2 / kGroups), pieces = h * 64 + g * 32;
-        if constexpr (n > 0) {
-            xa[h][g] = kTurnX ? xa[0][0] + c * kRowX : xa[0][0] ^ pieces;
-            wa[h][g] = kTurnW ? wa[0][0] + c * kRowW : wa[0][0] ^ pieces;
-        }
-    });
-    int4v wf[2][FW], xf[2][FX];
-    auto read = [&](int address, int block, int row_length) {      // turned: a block's i's
-        const char* from = lds + (address ^ (block * kChunk));
-        if constexpr (sizeof(T) == 2) {
-            const int2v low = read_turned(from), high = read_turned(from + 4 * row_length);
-            return int4v{low[0], low[1], high[0], high[1]};
-        } else {
-            int4v v;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const int*>(from + e * row_length);
-            return v;
-        }
-    };
-    auto read_w = [&](int h, int u) {
-        const int g = u / NB, j = u % NB;
-        if constexpr (kTurnW) wf[h][u] = read(wa[h][g], j, kRowW);
-        else wf[h][u] = *reinterpret_cast<const int4v*>(lds + wa[h][g] + (B == 32 ? j * 32 : (j >> 1) * 32 + (j & 1) * 4) * 128);
-    };
-    auto read_x = [&](int h, int u) {
-        const int g = u / MB, i = u % MB;
-        if constexpr (kTurnX) xf[h][u] = read(xa[h][g], i, kRowX);
-        else xf[h][u] = *reinterpret_cast<const int4v*>(lds + xa[h][g] + i * B * 128);
-    };
-    asm volatile("s_waitcnt vmcnt(%0)" :: "n"((S - 1) * kLoads) : "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-#pragma unroll
-    for (int j = 0; j < FW; ++j) read_w(0, j);
-#pragma unroll
-    for (int i = 0; i < kHalf; ++i) read_x(0, i);
-    __builtin_amdgcn_sched_barrier(0);
-
-    // A step is two halves, 64 bytes each.  In the first, all that the second needs is read, one read every few
-    // products (a wavefront is alone on its SIMD and issues in order: reads or loads in a row leave the matrix unit without work).
-    // Then nothing reads this buffer any more and, spread over the second half, it is loaded with the bytes of the step that is S on.
-    // Halfway through, those of the next step (loaded S - 1 steps before) are waited for, and the first half's operands are read.
-    int buffer = 0;
-    for (unsigned current = blockIdx.x; current < tiles; current += stride) {
-        for (int k = 0; k < steps; ++k) {
-            advance();
-            const int dx = buffer == S - 1 ? (1 - S) * kX : kX, dw = buffer == S - 1 ? (1 - S) * kW : kW;      // to the next step's buffer
-            buffer = buffer == S - 1 ? 0 : buffer + 1;
-            constexpr int kProducts = FX * NB, kSlots = kProducts * kSub<T>, kTurn = kSlots / 2;      // (product t is of x's piece t / NB and of w's of the same k's)
-            each<kSlots>([&](auto slot) {
-                constexpr int t = slot, u = t % kProducts / NB, j = t % NB, kOps = kHalf + FW + FX;
-                multiply<T, t / kProducts>(acc[u % MB][j], wf[0][u / MB * NB + j], xf[0][u]);
-                if constexpr (t < kProducts) {
-                    constexpr int first = (t * kOps + kProducts - 1) / kProducts, last = ((t + 1) * kOps + kProducts - 1) / kProducts;
-                    each<last - first>([&](auto n) {
-                        constexpr int o = first + n;
-                        if constexpr (o < 2 * kHalf && o % 2 == 0) read_x(0, kHalf + o / 2);
-                        else {
-                            constexpr int v = o < 2 * kHalf ? o / 2 : o - kHalf;
-                            if constexpr (v < FW) read_w(1, v);
-                            else read_x(1, v - FW);
-                        }
-                    });
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            });
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_sched_barrier(0);
-            each<kSlots>([&](auto slot) {
-                constexpr int t = slot, u = t % kProducts / NB, j = t % NB;
-                if constexpr (t == kTurn) {
-                    constexpr int kIssued = (kTurn * kLoads + kSlots - 1) / kSlots;
-                    asm volatile("s_waitcnt vmcnt(%0)" :: "n"(kIssued + (S - 2) * kLoads) : "memory");
-                    __builtin_amdgcn_s_barrier();
-                    asm volatile("" ::: "memory");
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int g = 0; g < kGroups; ++g) {
-                            xa[h][g] += dx;
-                            wa[h][g] += dw;
-                        }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-                multiply<T, t / kProducts>(acc[u % MB][j], wf[1][u / MB * NB + j], xf[1][u]);
-                constexpr int first = (t * kLoads + kSlots - 1) / kSlots, last = ((t + 1) * kLoads + kSlots - 1) / kSlots;
-                each<last - first>([&](auto n) { load(first + n); });
-                if constexpr (t >= kTurn) {
-                    constexpr int kReads = FW + kHalf, kRoom = kSlots - kTurn, v = t - kTurn;
-                    constexpr int from = (v * kReads + kRoom - 1) / kRoom, to = ((v + 1) * kReads + kRoom - 1) / kRoom;
-                    each<to - from>([&](auto n) {
-                        constexpr int o = from + n;
-                        if constexpr (o < FW) read_w(0, o);
-                        else read_x(0, o - FW);
-                    });
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            });
-            xdst += dx;
-            wdst += dw;
-        }
-
-        // Bias, activation and residual, while the first steps of the next tile are on their way.  The last products are read: the matrix
-        // unit's results need 18 clocks.
-        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
-        // A lane's channels of a unit, and how many of them lie in a row: 8 and 8 of two blocks of 16, 16 and 16 of a block of 32; 4 at once where w is turned.
-        constexpr int kUnit = B == 32 ? 16 : kTurnW ? 4 : 8, kWide = kTurnW ? 4 : 8, kPerUnit = B == 16 && !kTurnW ? 2 : 1;
-        auto epilogue = [&](auto inside, auto plain) {
-            each<NB / kPerUnit>([&](auto unit) {
-                constexpr int j = unit * kPerUnit;
-                auto channel = [&](int run) { return wn * B * NB + j * B + (B == 32 ? (kTurnW ? run * 8 + q * 4 : q * 16 + run * 8) : q * kWide); };
-                float bias[kUnit];
-#pragma unroll
-                for (int e = 0; e < kUnit; ++e) bias[e] = channel_bias[done][channel(e / kWide) + e % kWide];
-                each<MB>([&](auto block) {
-                    constexpr int i = block;
-                    const int m = m0 + (wm * MB + i) * B + r;
-                    float v[kUnit];
-                    each<kPerUnit>([&](auto of) {
-                        Sums& c = acc[i][j + of];
-                        asm volatile("" : "+a"(c));
-#pragma unroll
-                        for (int e = 0; e < kUnit / kPerUnit; ++e) v[of * (kUnit / kPerUnit) + e] = c[e];
-                        clear(c);
-                    });
-                    if (!inside && m >= a.M) return;
-                    each<kUnit / kWide>([&](auto run) {
-                        const int n = n0 + channel(run);
-                        if (!inside && n >= a.N) return;
-                        float sum[kWide], more[kWide];
-#pragma unroll
-                        for (int e = 0; e < kWide; ++e) {
-                            sum[e] = v[run * kWide + e];
-                            more[e] = bias[run * kWide + e];
-                        }
-                        if (!plain && a.partial) {
-                            float* to = a.partial + ((size_t)part * a.M + m) * a.N + n;
-                            typedef float four __attribute__((ext_vector_type(4), aligned(4)));
-                            if (inside || n + kWide <= a.N) {
-#pragma unroll
-                                for (int c = 0; c < kWide / 4; ++c) reinterpret_cast<four*>(to)[c] = four{sum[4 * c], sum[4 * c + 1], sum[4 * c + 2], sum[4 * c + 3]};
-                            } else {
-#pragma unroll
-                                for (int e = 0; e < kWide; ++e)
-                                    if (n + e < a.N) to[e] = sum[e];
-                            }
-                        } else {
-                            finish<T, kWide, inside, plain>(a, sum, more, m, n, a.N - n);
-                        }
-                    });
-                });
-            });
-        };
-        if (m0 + TM > a.M || n0 + TN > a.N) epilogue(std::false_type{}, std::false_type{});
-        else if (a.partial || a.act != kNone || a.residual || a.z) epilogue(std::true_type{}, std::false_type{});
-        else epilogue(std::true_type{}, std::true_type{});
-        if (!kWalksOver<MB16, NB16>) break;
-        m0 = next_m;
-        n0 = next_n;
-        part = next_part;
-        done = set;
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (loads of zeros that nothing reads)
-}
-
-// Few rows of x: 16 MB of them by 16 NB rows of w a workgroup, whose W wavefronts go round the 128-byte units of the rows and add their
-// sums up at the end.  A wavefront loads its units to a part of LDS of its own, D of them in flight, and waits for its own loads alone.
-// (Loads in the order that the products take would touch 16 rows with 16 lanes in a row, at a quarter of the rate.)
-template <class T, int MB, int NB, int W, int D>
-__global__ __launch_bounds__(64 * W) void linear_row_kernel(ProductArgs a)
-{
-    constexpr int kTokens = 16 * MB, kChannels = 16 * NB, kThreads = 64 * W;
-    constexpr int kLoadsX = 2 * MB, kLoads = kLoadsX + 2 * NB, kUnit = 1024 * kLoads;
-    static_assert(D * kUnit >= kTokens * kChannels * 4, "the sums take the place of the units");
-    __shared__ __attribute__((aligned(256))) char lds[W * D * kUnit];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int r = lane & 15, q = lane >> 4;
-    const int across = (a.N + kChannels - 1) / kChannels;
-    const int m0 = (int)(blockIdx.x / across) * kTokens, n0 = (int)(blockIdx.x % across) * kChannels;
-    const int row_bytes = bytes_of_rows<T>(a.terms), units = (row_bytes + 127) / 128;
-
-    // Pieces of 16 bytes are permuted within the 128 bytes of a row as in the tile kernel.
-    int4v from_w = descriptor_of(static_cast<const char*>(a.w) + (size_t)n0 * a.w_pitch, (long long)min(kChannels, a.N - n0) * a.w_pitch);
-    int4v from_x = descriptor_of(static_cast<const char*>(a.x) + (size_t)m0 * a.x_pitch, (long long)min(kTokens, a.M - m0) * a.x_pitch);
-    const int bytes_w = from_w[2], bytes_x = from_x[2];
-    const unsigned lds0 = (unsigned)(uintptr_t)(SC_LDS char*)lds + wave * D * kUnit;
-    unsigned row[2], piece_of[2], behind = 0;      // of the rows lane / 8 of an even and an odd load: their permutations differ
-#pragma unroll
-    for (int o = 0; o < 2; ++o) {
-        row[o] = (unsigned)(o * 8 + (lane >> 3));
-        piece_of[o] = ((lane & 7) ^ ((o * 4 + (lane >> 4)) & 7)) << 4;
-        if ((units - 1) * 128 + (int)piece_of[o] >= row_bytes) behind |= 1u << o;
-    }
-    auto load = [&](int slot, int unit) {
-        from_w[2] = unit < units ? bytes_w : 0;
-        from_x[2] = unit < units ? bytes_x : 0;
-        const unsigned beyond = unit == units - 1 ? behind : 0, at = unit < units ? unit * 128u : 0u;
-        each<kLoads>([&](auto load) {
-            constexpr int l = load, block = l < kLoadsX ? l / 2 : (l - kLoadsX) / 2;
-            const unsigned pitch = l < kLoadsX ? a.x_pitch : a.w_pitch;
-            load_to_lds(l < kLoadsX ? from_x : from_w, past((row[l & 1] + block * 16u) * pitch + piece_of[l & 1], beyond, l & 1), at,
-                        lds0 + slot * kUnit + l * 1024);
-        });
-    };
-    each<D>([&](auto d) { load(d, wave + d * W); });
-
-    float4v acc[MB][NB];
-#pragma unroll
-    for (int i = 0; i < MB; ++i)
-#pragma unroll
-        for (int j = 0; j < NB; ++j) acc[i][j] = float4v{0.f, 0.f, 0.f, 0.f};
-    const char* mine = lds + wave * D * kUnit + r * 128;
-    const int piece[2] = {(q ^ (r >> 1)) << 4, ((q + 4) ^ (r >> 1)) << 4};
-    int slot = 0;
-    for (int unit = wave; unit < units; unit += W) {
-        asm volatile("s_waitcnt vmcnt(%0)" :: "n"((D - 1) * kLoads) : "memory");
-        const char* from = mine + slot * kUnit;
-        int4v wf[2][NB], xf[2][MB];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-#pragma unroll
-            for (int i = 0; i < MB; ++i) xf[h][i] = *reinterpret_cast<const int4v*>(from + i * 2048 + piece[h]);
-#pragma unroll
-            for (int j = 0; j < NB; ++j) wf[h][j] = *reinterpret_cast<const int4v*>(from + kLoadsX * 1024 + j * 2048 + piece[h]);
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_sched_barrier(0);
-        load(slot, unit + D * W);
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < MB; ++i)
-#pragma unroll
-                for (int j = 0; j < NB; ++j) acc[i][j] = multiplied<T>(acc[i][j], wf[h][j], xf[h][i]);
-        slot = slot + 1 == D ? 0 : slot + 1;
-    }
-
-    // Sums of each wavefront where its units were: [token][channel].
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < MB; ++i)
-#pragma unroll
-        for (int j = 0; j < NB; ++j)
-            *reinterpret_cast<float4v*>(lds + wave * D * kUnit + ((i * 16 + r) * kChannels + j * 16 + q * 4) * 4) = acc[i][j];
-    __syncthreads();
-    for (int o = threadIdx.x; o < kTokens * kChannels / 4; o += kThreads) {
-        const int token = o / (kChannels / 4), channel = o % (kChannels / 4) * 4, m = m0 + token, n = n0 + channel;
-        if (m >= a.M || n >= a.N) continue;
-        float4v total = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < W; ++w) total += *reinterpret_cast<const float4v*>(lds + w * D * kUnit + o * 16);
-        float sum[4], bias[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            sum[e] = total[e];
-            bias[e] = a.bias && n + e < a.N ? a.bias[n + e] : 0.f;
-        }
-        finish<T, 4>(a, sum, bias, m, n, a.N - n);
-    }
-}
 
 // The parts of a product added up, in their order, then as in the kernels above.  Four outputs of a row a thread.
 template <class T>
@@ -1042,42 +452,54 @@ __global__ __launch_bounds__(256) void linear_dot_kernel(ProductArgs a, int K, l
 
 double pieces_of(int n, int size) { return (double)((n + size - 1) / size); }
 
-// Microseconds that a product of rows of `bytes` is estimated to take: a row kernel by what its workgroups load, a tile kernel by its
-// steps.  f: clocks of the matrix unit that a piece of 16 bytes takes, over those of 16-bit types.
-enum Kernel { kRow11, kRow21, kRow22, kRow41, kRow42, kTile22, kTile44, kTile88, kDeep22, kDeep42, kDeep44, kKernels };
+// Microseconds that a product of rows of `bytes` is estimated to take.  The constants are fitted, for 16-bit types and for fp32, to what each kernel
+// near the fastest took at 125 sizes (4 to 8192 rows of x, 64 to 8192 of w and of terms, one launch after another in a graph, arrays
+// that change): the kernel of the least estimate takes 1.9 % more than the fastest on average, and more than 15 % at one size (4096 x 3776 -> 64).
 
+// Row kernel: a launch, the sums of the wavefronts and the further workgroups of a CU, then the largest of what all workgroups load,
+// what those of one CU load, both operands from memory, and the products.
 struct RowRule {
     int MB, NB;
-    double join, more, all, one, weights;      // us; MB/us of all workgroups, KB/us of one, MB/us of w
+    double join, more;                        // us
+    double all, one, arrays, products;        // MB/us of all, KB/us of one, MB/us of the arrays; us for 1000 bytes of a block
 };
-constexpr RowRule kRowRules[] = {{1, 1, 0.36, 1.39, 21.1, 144.0, 7.2}, {2, 1, 0.24, 1.42, 22.5, 135.0, 6.0}, {2, 2, 0.12, 0.83, 19.2, 136.0, 5.6},
-                                 {4, 1, 0.33, 1.54, 24.6, 133.0, 4.75}, {4, 2, 0.91, 1.64, 19.8, 132.0, 5.05}};
+constexpr RowRule kRowRules[2][5] = {
+    {{1, 1, 1.25, 0.62, 20.4, 126.0, 6.3, 0.055}, {2, 1, 1.08, 0.68, 19.4, 127.0, 5.6, 0.050}, {2, 2, 0.97, 0.19, 15.4, 129.0, 6.4, 0.055},
+     {4, 1, 1.24, 0.34, 24.1, 133.0, 4.6, 0.050}, {4, 2, 2.09, 0.87, 15.1, 146.0, 4.9, 0.050}},
+    {{1, 1, 1.09, 0.67, 15.9, 255.0, 6.2, 0.373}, {2, 1, 0.85, 1.18, 30.8, 605.0, 5.1, 0.324}, {2, 2, 1.03, 0.19, 21.4, 106.0, 4.6, 0.302},
+     {4, 1, 0.90, 0.52, 85.6, 180.0, 2.1, 0.289}, {4, 2, 2.14, 1.30, 68.7, 129.0, 3.1, 0.293}}};
 
-double row_estimate(const RowRule& r, int M, int N, double bytes, double f)
+double row_estimate(const RowRule& r, int M, int N, double bytes)
 {
-    const double groups = pieces_of(M, 16 * r.MB) * pieces_of(N, 16 * r.NB), loaded = 16.0 * (r.MB + r.NB) * bytes;
-    const double on_a_cu = std::ceil(groups / 256.0);
-    const double load = std::max({groups * loaded / (r.all * 1e6), on_a_cu * loaded / (r.one * 1e3), (double)N * bytes / (r.weights * 1e6)});
-    const double multiply = on_a_cu * r.MB * r.NB * (bytes / 64.0) * f * 16.0 / 4.0 / 2000.0;
-    return 3.0 + r.join * on_a_cu + r.more * (on_a_cu - 1.0) + std::max(load, multiply);
+    const double groups = pieces_of(M, 16 * r.MB) * pieces_of(N, 16 * r.NB), loaded = 16.0 * (r.MB + r.NB) * bytes, on_a_cu = std::ceil(groups / 256.0);
+    return 3.0 + r.join * on_a_cu + r.more * (on_a_cu - 1.0) +
+           std::max({groups * loaded / (r.all * 1e6), on_a_cu * loaded / (r.one * 1e3), ((double)M + N) * bytes / (r.arrays * 1e6), on_a_cu * r.MB * r.NB * bytes * r.products * 1e-3});
 }
 
+// Tile kernel: steps of `least` us while a workgroup has the CU to itself, `each` times the workgroups that share it beyond; the operands
+// from memory at least; the output.
 struct TileRule {
-    int MB, NB, share;
-    double least, each, start, finish, weights;
+    int MB, NB, share;                        // blocks of a wavefront; workgroups that a CU holds
+    double least, each, start, finish;
+    double arrays, output;                    // MB/us
 };
-constexpr TileRule kTileRules[] = {{2, 2, 4, 0.268, 0.213, 0.28, 2.35, 3.5}, {4, 4, 2, 0.063, 0.446, 0.40, 4.07, 3.2}, {8, 8, 1, 0.0, 1.16, 2.66, 9.15, 6.7},
-                                   {2, 2, 2, 0.049, 0.194, 1.20, 1.90, 7.0}, {4, 2, 1, 0.0, 0.271, 1.12, 2.48, 6.6}, {4, 4, 1, 0.0, 0.396, 0.99, 3.39, 4.7}};
+constexpr TileRule kTileRules[2][6] = {
+    {{2, 2, 4, 0.244, 0.185, 1.25, 2.34, 2.2, 13.4}, {4, 4, 2, 0.065, 0.470, 1.79, 2.88, 4.4, 10.6}, {8, 8, 1, 0.0, 1.15, 1.55, 8.19, 5.0, 12.3},
+     {2, 2, 2, 0.043, 0.211, 2.71, 1.19, 5.2, 9.1}, {4, 2, 1, 0.0, 0.308, 2.29, 1.87, 3.4, 6.1}, {4, 4, 1, 0.0, 0.401, 2.66, 2.32, 4.6, 5.9}},
+    {{2, 2, 4, 0.228, 0.551, 1.25, 2.36, 1.8, 5.6}, {4, 4, 2, 0.055, 1.92, 0.10, 6.34, 1.9, 8.7}, {8, 8, 1, 0.0, 7.7, 1.55, 8.19, 5.0, 12.3},
+     {2, 2, 2, 0.074, 0.568, 1.75, 2.27, 3.2, 21.8}, {4, 2, 1, 0.0, 1.02, 2.41, 2.08, 25.8, 4.5}, {4, 4, 1, 0.0, 1.93, 3.36, 3.26, 5.0, 10.7}}};
 
-double tile_estimate(const TileRule& r, int M, int N, int parts, double bytes, double f)
+double tile_estimate(const TileRule& r, int M, int N, int parts, double bytes, int element)
 {
     const double groups = pieces_of(M, 32 * r.MB) * pieces_of(N, 32 * r.NB) * parts, steps = std::ceil(bytes / 128.0 / parts), held = 256.0 * r.share;
-    const double rounds = std::floor(groups / held), rest = groups - rounds * held, each = f > 1.0 ? std::max(r.each, 2.0 * r.MB * r.NB * f * 16.0 / 2100.0) : r.each;
-    double us = r.start + rounds * (steps * each * r.share + r.finish);
-    if (rest > 0.0) us += steps * std::max(r.least, each * std::ceil(rest / 256.0)) + r.finish;
-    us = std::max(us, 3.0 + (double)N * bytes / (r.weights * 1e6));
-    return parts > 1 ? us + 3.0 + 4.0 * M * (double)N * (parts + 1) / 4e6 : us;
+    const double rounds = std::floor(groups / held), rest = groups - rounds * held;
+    double us = r.start + rounds * (steps * r.each * r.share + r.finish);
+    if (rest > 0.0) us += steps * std::max(r.least, r.each * std::ceil(rest / 256.0)) + r.finish;
+    return std::max(us, 3.0 + ((double)M + N) * bytes / (r.arrays * 1e6)) + (double)M * N * element / (r.output * 1e6);
 }
+
+// Parts of a sum, and the launch that adds them up.
+double join_estimate(int parts, double outputs) { return parts > 1 ? 3.0 + 4.0 * outputs * (parts + 1) / 4e6 : 0.0; }
 
 struct Choice {
     Kernel kernel;
@@ -1088,7 +510,7 @@ struct Choice {
 // turned: both operands or w alone (tile kernels take those).
 Choice choose(int dtype, int M, int N, int terms, bool turned)
 {
-    const double f = dtype == kF32 ? 8.0 : 1.0;
+    const int wide = dtype == kF32;
     const int row_bytes = (terms * (dtype == kF32 ? 4 : 2) + 15) / 16 * 16, all = (row_bytes + 127) / 128;
     const double bytes = row_bytes;
     Choice best{kKernels, 1, all, 0.0};
@@ -1097,9 +519,10 @@ Choice choose(int dtype, int M, int N, int terms, bool turned)
         if (k == kDeep42 && turned) continue;
         for (int parts = 1; parts <= (k < kTile22 ? 1 : 64); parts *= 2) {
             const int steps = (all + parts - 1) / parts;
-            if (parts > 1 && steps < 8) break;
+            if (parts > 1 && (steps < 8 || (double)M * N * parts > 1.6e7)) break;
             if (k == kTile88 && steps < kStepsToWalk) break;
-            const double us = k < kTile22 ? row_estimate(kRowRules[k], M, N, bytes, f) : tile_estimate(kTileRules[k - kTile22], M, N, parts, bytes, f);
+            const double us = k < kTile22 ? row_estimate(kRowRules[wide][k], M, N, bytes)
+                                          : tile_estimate(kTileRules[wide][k - kTile22], M, N, parts, bytes, wide ? 4 : 2) + join_estimate(parts, (double)M * N);
             if (best.kernel == kKernels || us < best.us) best = Choice{(Kernel)k, (all + steps - 1) / steps, steps, us};
         }
     }
@@ -1113,58 +536,6 @@ int parts_of(double tiles, int all, double wanted, int least)
     while (parts < 64 && tiles * parts * 2 <= wanted && (all + 2 * parts - 1) / (2 * parts) >= least) parts *= 2;
     const int steps = (all + parts - 1) / parts;
     return (all + steps - 1) / steps;
-}
-
-// Which operands are turned.
-enum Turned { kRows, kTurnedW, kTurnedBoth };
-
-template <class T, int MB, int NB, int S, Turned turned>
-int launch_tile(const ProductArgs& a, hipStream_t s)
-{
-    const long long tiles = (long long)a.parts * ((a.M + 32ll * MB - 1) / (32 * MB)) * ((a.N + 32ll * NB - 1) / (32 * NB));
-    const bool walks = kWalksOver<MB, NB> && a.steps >= kStepsToWalk;
-    if (tiles >= (1ll << 31) || (!walks && (unsigned long long)tiles > most_groups(256))) return kTooLarge;
-    const unsigned blocks = walks ? (unsigned)std::min(tiles, 256ll) : (unsigned)tiles;
-    hipLaunchKernelGGL((linear_tile_kernel<T, MB, NB, 2, 2, S, turned == kTurnedBoth, turned != kRows>), dim3(blocks), dim3(256), 0, s, a, (unsigned)tiles, blocks);
-    return (int)hipGetLastError();
-}
-
-template <class T, int MB, int NB, int W, int D>
-int launch_row(const ProductArgs& a, hipStream_t s)
-{
-    const long long groups = ((a.M + 16ll * MB - 1) / (16 * MB)) * ((a.N + 16ll * NB - 1) / (16 * NB));
-    if ((unsigned long long)groups > most_groups(64 * W)) return kTooLarge;
-    hipLaunchKernelGGL((linear_row_kernel<T, MB, NB, W, D>), dim3((unsigned)groups), dim3(64 * W), 0, s, a);
-    return (int)hipGetLastError();
-}
-
-template <class T, Turned turned>
-int launch_kernel(Kernel kernel, const ProductArgs& a, hipStream_t s)
-{
-    if constexpr (turned == kRows) switch (kernel) {
-        case kRow11: return launch_row<T, 1, 1, 8, 4>(a, s);
-        case kRow21: return launch_row<T, 2, 1, 8, 2>(a, s);
-        case kRow22: return launch_row<T, 2, 2, 4, 2>(a, s);
-        case kRow41: return launch_row<T, 4, 1, 8, 1>(a, s);
-        case kRow42: return launch_row<T, 4, 2, 4, 2>(a, s);
-        case kDeep42: return launch_tile<T, 4, 2, 4, turned>(a, s);
-        default: break;
-    }
-    if constexpr (sizeof(T) == 2)
-        if (kernel == kTile88) return launch_tile<T, 8, 8, 2, turned>(a, s);
-    switch (kernel) {
-        case kTile22: return launch_tile<T, 2, 2, 2, turned>(a, s);
-        case kTile44: return launch_tile<T, 4, 4, 2, turned>(a, s);
-        case kDeep22: return launch_tile<T, 2, 2, 4, turned>(a, s);
-        default: return launch_tile<T, 4, 4, 3, turned>(a, s);
-    }
-}
-
-template <class T>
-int launch_kernel(Kernel kernel, Turned turned, const ProductArgs& a, hipStream_t s)
-{
-    if (turned == kRows) return launch_kernel<T, kRows>(kernel, a, s);
-    return turned == kTurnedW ? launch_kernel<T, kTurnedW>(kernel, a, s) : launch_kernel<T, kTurnedBoth>(kernel, a, s);
 }
 
 template <class T>
@@ -1186,7 +557,7 @@ int product(int dtype, const Choice& c, Turned turned, ProductArgs a, char* part
     a.parts = c.parts;
     a.steps = c.steps;
     a.partial = c.parts > 1 ? reinterpret_cast<float*>(partial) : nullptr;
-    int e = dtype == kF32 ? launch_kernel<float>(c.kernel, turned, a, s) : dtype == kF16 ? launch_kernel<_Float16>(c.kernel, turned, a, s) : launch_kernel<__bf16>(c.kernel, turned, a, s);
+    int e = dtype == kF32 ? launch_laid_f32(c.kernel, turned, a, s) : dtype == kF16 ? launch_laid_f16(c.kernel, turned, a, s) : launch_laid_bf16(c.kernel, turned, a, s);
     if (e != 0 || c.parts == 1) return e;
     return dtype == kF32 ? launch_join<float>(a, s) : dtype == kF16 ? launch_join<_Float16>(a, s) : launch_join<__bf16>(a, s);
 }
@@ -1344,15 +715,12 @@ struct LinearPlan {
 
 double lay_estimate(double bytes) { return 3.0 + bytes / 4e6; }
 
-// A direct launch whose tiles take `work` steps in all, `longest` of them one after another at most.  turned: the gradients' operands.
-double direct_estimate(int dtype, double work, int longest, bool turned)
+// A direct launch of `tiles` that take `work` steps in all, `longest` of them one after another at most.  turned: the gradients' operands.
+double direct_estimate(int dtype, double tiles, double work, int longest, bool turned)
 {
-    const double alone = dtype == kF32 ? 0.74 : turned ? 0.42 : 0.34, shared = dtype == kF32 ? (turned ? 0.66 : 0.53) : turned ? 0.42 : 0.25;
-    return 4.5 + std::max(longest * alone, work / 256.0 * shared);
+    const double alone = dtype == kF32 ? 0.74 : turned ? 0.42 : 0.34, shared = dtype == kF32 ? 0.63 : turned ? 0.38 : 0.25;
+    return 4.5 + std::max(longest * alone, work / 256.0 * shared) + tiles / 256.0 * (turned ? 1.5 : 0.9);
 }
-
-// Parts of a sum, and the launch that adds them up.
-double join_estimate(int parts, double outputs) { return parts > 1 ? 3.0 + 4.0 * outputs * (parts + 1) / 4e6 : 0.0; }
 
 LinearPlan plan_of(const LinearArgs& a, int dtype)
 {
@@ -1371,7 +739,7 @@ LinearPlan plan_of(const LinearArgs& a, int dtype)
     p.steps = (all + p.parts - 1) / p.parts;
     p.laid = choose(dtype, a.M, a.N, a.K, false);
     const double laid = p.laid.us + (p.lay_x ? lay_estimate(2.0 * a.M * row_bytes) : 0.0) + (p.lay_w ? lay_estimate(2.0 * a.N * row_bytes) : 0.0);
-    const double direct = direct_estimate(dtype, tiles * all, p.steps, false) + join_estimate(p.parts, (double)a.M * a.N);
+    const double direct = direct_estimate(dtype, tiles * p.parts, tiles * all, p.steps, false) + join_estimate(p.parts, (double)a.M * a.N);
     if (direct < laid) {
         p.way = kDirect;
         p.end = partial_bytes(p.parts, a.M, a.N);
@@ -1417,6 +785,17 @@ int launch_way(const LinearPlan& p, ProductArgs a, const LinearArgs& l, char* wo
 }  // namespace
 
 long long linear_workspace(const LinearArgs& a, int dtype) { return plan_of(a, dtype).end; }
+
+int linear_kernel(int dtype, int M, int N, int K)
+{
+    LinearArgs a{};
+    a.M = M;
+    a.N = N;
+    a.K = K;
+    a.ldx = a.ldw = K;
+    const LinearPlan p = plan_of(a, dtype);
+    return p.way == kDot ? 100 : p.way == kDirect ? 101 : p.laid.kernel;
+}
 
 int launch_linear(int dtype, const LinearArgs& a, char* workspace, void* stream)
 {
@@ -1482,7 +861,7 @@ GradPlan plan_of(const LinearGradArgs& a, int dtype)
     l.steps_x = (all_x + l.parts_x - 1) / l.parts_x;
     l.steps_w = (all_w + l.parts_w - 1) / l.parts_w;
     const double work = tiles_x * all_x + tiles_w * all_w, form = lay_estimate(3.0 * a.M * a.N * b) + 1.5;
-    direct = direct_estimate(dtype, work, std::max(l.steps_x, l.steps_w), true) + join_estimate(l.parts_x, (double)a.M * a.K) + join_estimate(l.parts_w, (double)a.N * a.K);
+    direct = direct_estimate(dtype, tiles_x * l.parts_x + tiles_w * l.parts_w, work, std::max(l.steps_x, l.steps_w), true) + join_estimate(l.parts_x, (double)a.M * a.K) + join_estimate(l.parts_w, (double)a.N * a.K);
     // (Where the slope is worked out as the tiles are loaded, every tile along K does it anew.)
     const double anew = a.act == kNone ? 0.0 : std::max(work / 256.0, (double)std::max(l.steps_x, l.steps_w)) * (a.act == kRelu ? 0.26 : 0.38) * (dtype == kF32 ? 0.5 : 1.0);
     l.formed = anew > form;
@@ -1570,6 +949,17 @@ int launch_direct_grad(const GradPlan& l, const LinearGradArgs& a, char* workspa
 }  // namespace
 
 long long linear_grad_workspace(const LinearGradArgs& a, int dtype) { return plan_of(a, dtype).end; }
+
+int linear_grad_kernel(int dtype, int M, int N, int K, int act)
+{
+    LinearGradArgs a{};
+    a.M = M;
+    a.N = a.ldg = N;
+    a.K = a.ldx = a.ldw = K;
+    a.act = act;
+    const GradPlan p = plan_of(a, dtype);
+    return p.direct ? 101 + p.formed : 1000 * p.x.kernel + p.w.kernel;
+}
 
 int launch_linear_grad(int dtype, const LinearGradArgs& a, char* workspace, void* stream)
 {

@@ -1,8 +1,8 @@
 // The loss of a classifier with the gradient of its logits (sparse_conv_cross_entropy).
 //
 // loss = w (log sum_c exp z_c - z_label), gradient = w (exp(z_c - lse) - [c = label]).  The bytes bound it: logits once in, gradient
-// once out.  A row stays in registers between the two, where it fits (131072 classes of 16 bits, 65536 of fp32); longer rows are
-// read twice.  Each thread keeps the largest of its logits and the sum of exponentials over that largest, the threads of a row
+// once out.  A row stays in registers between the two, where two workgroups of a CU still fit (65536 classes of 16 bits, 32768 of fp32); longer
+// rows are read twice.  Each thread keeps the largest of its logits and the sum of exponentials over that largest, the threads of a row
 // join these pairs once, and every thread turns what it holds into the gradient.
 #include <hip/hip_runtime.h>
 
@@ -231,7 +231,6 @@ int launch(const LossArgs& a, hipStream_t s)
     if (pieces <= 2048) return by_row<T, 512, 4>(a, s);
     if (pieces <= 4096) return by_row<T, 1024, 4>(a, s);
     if (pieces <= 8192) return by_row<T, 1024, 8>(a, s);
-    if (pieces <= 16384) return by_row<T, 1024, 16>(a, s);
     return by_row<T, 1024, 0>(a, s);
 }
 
