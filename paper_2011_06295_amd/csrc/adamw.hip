@@ -49,7 +49,7 @@ __device__ __forceinline__ float factor_of(float largest, float& scale)
 {
     const bool zeros = largest < 0x1p-100f;
     scale = zeros ? 0.f : largest * (1.f / 448.f);
-    return zeros ? 0.f : 448.f / largest;
+    return zeros ? 0.f : 448.f * (1.f / largest);
 }
 
 // y >= 0 to four binary digits, up or down by chance, so that what the steps add up to stays right on average: with the nearest number
@@ -60,6 +60,15 @@ __device__ __forceinline__ float by_chance(float y, float noise)
     const float step = __uint_as_float((unsigned)(127 + exponent) << 23), inverse = __uint_as_float((unsigned)(127 - exponent) << 23);
     const float whole = floorf(fmaf(y, inverse, noise)) * step;
     return y > 0.f ? fminf(fmaxf(whole, 0x1p-9f), 448.f) : 0.f;
+}
+
+// The moments, every operation rounded by itself: the numbers of 8 bits are those of the definition done in fp32 step by step, also where a value lies next to
+// the border between two of them.
+__device__ __forceinline__ void update(const AdamwRule& rule, float g, float& m, float& v)
+{
+#pragma clang fp contract(off)
+    m = rule.beta1 * m + rule.rest1 * g;
+    v = rule.beta2 * v + rule.rest2 * (g * g);
 }
 
 template <class T>
@@ -170,9 +179,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwLaunch a)
         float most_m = 0.f, most_v = 0.f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float d = g[b][e] * rule.grad_scale;
-            m[b][e] = rule.beta1 * m[b][e] + rule.rest1 * d;
-            v[b][e] = rule.beta2 * v[b][e] + rule.rest2 * (d * d);
+            update(rule, g[b][e] * rule.grad_scale, m[b][e], v[b][e]);
             const float root = __builtin_amdgcn_sqrtf(v[b][e]) * rule.c2 + rule.eps;
             p[b][e] = p[b][e] * rule.keep - rule.rate * rule.c1 * m[b][e] * __builtin_amdgcn_rcpf(root);
             if (kSmall) {

@@ -156,6 +156,46 @@ __device__ __forceinline__ void finish(const ProductArgs& a, const float (&sum)[
     store(static_cast<T*>(a.out) + (size_t)m * a.ldo + n);
 }
 
+// Four elements of each of 16 rows that lie along i, as four elements along c of each of 16 i's: lane l of 16 gives the address of elements
+// 4 (l % 4) .. + 3 of row l / 4, and gets rows 0 .. 3 of element l.
+__device__ __forceinline__ int2v read_turned(const char* at)
+{
+    typedef short short4v __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(int2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((SC_LDS short4v*)(SC_LDS char*)at));
+}
+
+// What the number of a turned row's piece of 16 bytes is combined with (by exclusive or), row c of a tile of `length` i's.
+template <class T>
+__device__ __forceinline__ int swizzle_of(int c, int length)
+{
+    if (sizeof(T) == 4) return ((c >> 2) & 3) << 2;
+    return length == 64 ? (((c >> 1) & 1) | ((c >> 3) & 1) << 1) << 1 : ((c & 3) | ((c >> 3) & 1) << 2) << 1;
+}
+
+// Where a lane reads the i's of a block of 16 of a turned tile of `length` i's, whose rows lie in LDS as in memory but for that permutation; further blocks of
+// a wavefront by exclusive or of 16 sizeof(T) times their number.
+template <class T>
+__device__ __forceinline__ int turned_address(int lane, int block, int length)
+{
+    const int r = lane & 15, q = lane >> 4, c = sizeof(T) == 2 ? 8 * q + (r >> 2) : 4 * q;
+    return c * length * (int)sizeof(T) + ((block * (int)sizeof(T)) ^ swizzle_of<T>(c, length)) * 16 + (sizeof(T) == 2 ? (r & 3) * 8 : r * 4);
+}
+
+// A lane's 16 bytes along c of its i there: four c's of 16 bits at once, or one of fp32.
+template <class T>
+__device__ __forceinline__ int4v read_block(const char* at, int row_length)
+{
+    if constexpr (sizeof(T) == 2) {
+        const int2v low = read_turned(at), high = read_turned(at + 4 * row_length);
+        return int4v{low[0], low[1], high[0], high[1]};
+    } else {
+        int4v v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const int*>(at + e * row_length);
+        return v;
+    }
+}
+
 }  // namespace
 
 }  // namespace sc

@@ -58,46 +58,27 @@ struct Side {
 template <class T, int kRows, bool kTurned, bool kSlope, bool kFew>
 struct Share {
     static constexpr int kCount = 16 / sizeof(T), kC = 128 / sizeof(T), kPieces = kRows * 8 / 256;
+    static constexpr int kAcross = kTurned ? kRows / kCount : 8, kLength = kTurned ? kRows * (int)sizeof(T) : 128;      // pieces, bytes of a row in LDS
     typedef typename Piece<T>::type V;
     V v[kPieces], z[kSlope ? kPieces : 1];
 
-    // Turned: pairs of pieces, of c and c + 1, so that words of two (pairs of words, for fp32) go to LDS.
+    // The first i and c of piece t.  (Turned, all pieces of a thread are of the same i's.)
     static __device__ __forceinline__ void place(int t, int& i, int& c)
     {
-        if constexpr (kTurned) {
-            constexpr int kAcross = kRows / kCount;      // pieces of one c
-            const int pair = t / 2 * 256 + (int)threadIdx.x;
-            i = pair % kAcross * kCount;
-            c = pair / kAcross * 2 + t % 2;
-        } else {
-            const int piece = t * 256 + (int)threadIdx.x;
-            i = piece / 8;
-            c = piece % 8 * kCount;
-        }
+        const int piece = t * 256 + (int)threadIdx.x, along = piece % kAcross * kCount, row = piece / kAcross;
+        i = kTurned ? along : row;
+        c = kTurned ? row : along;
     }
 
-    // How far a piece of a turned operand begins before its i, to end within the operand.
-    static __device__ __forceinline__ int back(int count, int i) { return max(i + kCount - count, 0); }
-
-    static __device__ __forceinline__ V load(const T* from, long long ld, int count, int i, int c, int c_end)
+    // Element `along` on of a row of `length`.
+    static __device__ __forceinline__ V load(const T* row, int along, int length)
     {
         V v;
-        if constexpr (kTurned) {
-            const T* row = from + (size_t)min(c, c_end - 1) * ld;
-            if constexpr (kFew) {
+        if constexpr (kFew) {
 #pragma unroll
-                for (int e = 0; e < kCount; ++e) v[e] = row[max(min(i + e - back(count, i), count - 1), 0)];
-            } else {
-                v = *reinterpret_cast<const V*>(row + min(i, count - kCount));
-            }
+            for (int e = 0; e < kCount; ++e) v[e] = row[min(along + e, length - 1)];
         } else {
-            const T* row = from + (size_t)min(i, count - 1) * ld;
-            if constexpr (kFew) {
-#pragma unroll
-                for (int e = 0; e < kCount; ++e) v[e] = row[min(c + e, c_end - 1)];
-            } else {
-                v = *reinterpret_cast<const V*>(row + min(c, c_end - kCount));
-            }
+            v = *reinterpret_cast<const V*>(row + min(along, length - kCount));
         }
         return v;
     }
@@ -108,25 +89,48 @@ struct Share {
         for (int t = 0; t < kPieces; ++t) {
             int i, c;
             place(t, i, c);
-            v[t] = load(static_cast<const T*>(s.p), s.ld, s.count, i0 + i, c0 + c, c_end);
-            if constexpr (kSlope) z[t] = load(static_cast<const T*>(s.z), s.ldz, s.count, i0 + i, c0 + c, c_end);
+            i += i0;
+            c += c0;
+            const size_t row = kTurned ? min(c, c_end - 1) : min(i, s.count - 1);
+            const int along = kTurned ? i : c, length = kTurned ? s.count : c_end;
+            v[t] = load(static_cast<const T*>(s.p) + row * s.ld, along, length);
+            if constexpr (kSlope) z[t] = load(static_cast<const T*>(s.z) + row * s.ldz, along, length);
         }
     }
 
-    // The last step: a piece of a row moves down, and what lies past the end becomes zero.
-    static __device__ __forceinline__ void end(V& v, int c, int c_end)
+    // A piece that was loaded from before its place moves there; zeros behind the row's end (kFew: what was loaded there becomes zero).
+    static __device__ __forceinline__ void move(V& v, int along, int length)
     {
-        if constexpr (kTurned || kFew) {
+        if constexpr (kFew) {
 #pragma unroll
-            for (int e = 0; e < kCount; ++e) v[e] = c + (kTurned ? 0 : e) < c_end ? v[e] : (T)0.f;
+            for (int e = 0; e < kCount; ++e) v[e] = along + e < length ? v[e] : (T)0.f;
         } else {
-            const int moved = max(c - (c_end - kCount), 0);
+            const int moved = max(along - (length - kCount), 0);
             const unsigned __int128 bits = __builtin_bit_cast(unsigned __int128, v);
             v = __builtin_bit_cast(V, moved < kCount ? bits >> (moved * 8 * (int)sizeof(T)) : (unsigned __int128)0);
         }
     }
 
-    // Multiplies by the slope; what is not rounded yet is added to `sums`, an element of the thread's pairs of pieces each (turned alone).
+    __device__ __forceinline__ void end(const Side& s, int i0, int c0, int c_end)
+    {
+        const bool last = c0 + kC > c_end, edge = kTurned && i0 + kRows > s.count;
+        if (!last && !edge) return;
+#pragma unroll
+        for (int t = 0; t < kPieces; ++t) {
+            int i, c;
+            place(t, i, c);
+            auto all = [&](V& v) {
+                if (kTurned ? edge : last) move(v, kTurned ? i0 + i : c0 + c, kTurned ? s.count : c_end);
+                if (kTurned && last)
+#pragma unroll
+                    for (int e = 0; e < kCount; ++e) v[e] = c0 + c < c_end ? v[e] : (T)0.f;
+            };
+            all(v[t]);
+            if constexpr (kSlope) all(z[t]);
+        }
+    }
+
+    // Multiplies by the slope; what is not rounded yet is added to `sums`, an element of the thread's pieces each (turned alone).
     __device__ __forceinline__ void apply(int act, float* sums)
     {
         auto all = [&](auto act) {
@@ -139,45 +143,26 @@ struct Share {
                         g *= slope<act>((float)z[t][e]);
                         v[t][e] = (T)g;
                     }
-                    if constexpr (kTurned) sums[t / 2 * kCount + e] += g;
+                    if constexpr (kTurned) sums[e] += g;
                 }
         };
         if constexpr (kSlope) with_activation(act, all);
         else all(std::integral_constant<int, kNone>{});
     }
 
-    // Row i of LDS is 128 bytes along c, its pieces permuted by the row as in the tile kernel, and by 16 rows more for what is turned.
-    static __device__ __forceinline__ int turn_of(int i) { return ((i >> 1) ^ (i >> 4)) & 7; }
-
-    // kSums: the sums of what goes to LDS are wanted.
+    // kSums: the sums of what goes to LDS are wanted.  Rows lie along c there, 128 bytes, their pieces permuted by the row, or as they do in memory.
     template <bool kSums>
     __device__ __forceinline__ void put(const Side& s, int act, int i0, int c0, int c_end, char* to, float* sums)
     {
-        if (c0 + kC > c_end)
-#pragma unroll
-            for (int t = 0; t < kPieces; ++t) {
-                int i, c;
-                place(t, i, c);
-                end(v[t], c0 + c, c_end);
-                if constexpr (kSlope) end(z[t], c0 + c, c_end);
-            }
+        end(s, i0, c0, c_end);
         if constexpr (kSlope || kSums) apply(act, sums);
+        typedef T A __attribute__((ext_vector_type(16 / sizeof(T))));
 #pragma unroll
-        for (int t = 0; t < kPieces; t += kTurned ? 2 : 1) {
+        for (int t = 0; t < kPieces; ++t) {
             int i, c;
             place(t, i, c);
-            if constexpr (!kTurned) {
-                typedef T A __attribute__((ext_vector_type(16 / sizeof(T))));
-                *reinterpret_cast<A*>(to + i * 128 + (((c / kCount) ^ turn_of(i)) << 4)) = v[t];
-            } else {
-                const int byte = c * (int)sizeof(T), first = back(s.count, i0 + i);      // (i's that an earlier piece has as well)
-#pragma unroll
-                for (int e = 0; e < kCount; ++e) {
-                    typedef T two __attribute__((ext_vector_type(2)));
-                    const int row = i + e - first;
-                    if (e >= first) *reinterpret_cast<two*>(to + row * 128 + (((byte >> 4) ^ turn_of(row)) << 4) + (byte & 15)) = two{v[t][e], v[t + 1][e]};
-                }
-            }
+            const int row = kTurned ? c : i, piece = (kTurned ? i : c) / kCount, turn = kTurned ? swizzle_of<T>(c, kRows) : (i >> 1) & 7;
+            *reinterpret_cast<A*>(to + row * kLength + ((piece ^ turn) << 4)) = v[t];
         }
     }
 };
@@ -190,9 +175,13 @@ template <class T, int I, int J, bool kTurnedA, bool kTurnedB, bool kSlope, bool
 __device__ __forceinline__ void direct_tile(const Side& a, const Side& b, int act, int i0, int j0, int c_begin, int c_end, char* lds, float4v (&acc)[I][J], float* sums)
 {
     constexpr int kA = 32 * I * 128, kBuffer = kA + 32 * J * 128, kC = 128 / sizeof(T);
-    Share<T, 32 * I, kTurnedA, kSlope, kFew> of_a[kAhead];
-    Share<T, 32 * J, kTurnedB, false, kFew> of_b[kAhead];
+    typedef Share<T, 32 * I, kTurnedA, kSlope, kFew> A;
+    typedef Share<T, 32 * J, kTurnedB, false, kFew> B;
+    A of_a[kAhead];
+    B of_b[kAhead];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4, wi = wave & 1, wj = wave >> 1;
+    const int a_at = kTurnedA ? turned_address<T>(lane, wi * I, 32 * I) : (wi * I * 16 + r) * 128 + ((q ^ (r >> 1)) << 4);
+    const int b_at = kA + (kTurnedB ? turned_address<T>(lane, wj * J, 32 * J) : (wj * J * 16 + r) * 128 + ((q ^ (r >> 1)) << 4));
     each<kAhead>([&](auto d) {
         of_a[d].fetch(a, i0, c_begin + d * kC, c_end);
         of_b[d].fetch(b, j0, c_begin + d * kC, c_end);
@@ -206,19 +195,17 @@ __device__ __forceinline__ void direct_tile(const Side& a, const Side& b, int ac
             __syncthreads();
             of_a[d].fetch(a, i0, c + kAhead * kC, c_end);
             of_b[d].fetch(b, j0, c + kAhead * kC, c_end);
+            auto read = [&](auto turned, int at, int h, int block, int length) {
+                if constexpr (turned) return read_block<T>(lds + buffer + ((at + h * (kC / 2) * length) ^ (block * 16 * (int)sizeof(T))), length);
+                else return *reinterpret_cast<const int4v*>(lds + buffer + (at ^ (h * 64)) + block * 2048);
+            };
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 int4v fa[I], fb[J];
 #pragma unroll
-                for (int i = 0; i < I; ++i) {
-                    const int row = (wi * I + i) * 16 + r;
-                    fa[i] = *reinterpret_cast<const int4v*>(lds + buffer + row * 128 + (((h * 4 + q) ^ of_a[d].turn_of(row)) << 4));
-                }
+                for (int i = 0; i < I; ++i) fa[i] = read(std::integral_constant<bool, kTurnedA>{}, a_at, h, i, A::kLength);
 #pragma unroll
-                for (int j = 0; j < J; ++j) {
-                    const int row = (wj * J + j) * 16 + r;
-                    fb[j] = *reinterpret_cast<const int4v*>(lds + buffer + kA + row * 128 + (((h * 4 + q) ^ of_b[d].turn_of(row)) << 4));
-                }
+                for (int j = 0; j < J; ++j) fb[j] = read(std::integral_constant<bool, kTurnedB>{}, b_at, h, j, B::kLength);
 #pragma unroll
                 for (int i = 0; i < I; ++i)
 #pragma unroll
@@ -299,8 +286,7 @@ template <class T, int I, int J, bool kSlope, bool kFew>
 __global__ __launch_bounds__(256) void linear_direct_grad_kernel(DirectGradArgs a)
 {
     __shared__ __attribute__((aligned(256))) char lds[2 * 32 * (I + J) * 128];
-    constexpr int kC = 128 / sizeof(T), kCount = 16 / sizeof(T), kSums = I * kCount / 2;      // a thread's pairs of pieces hold I / 2 times kCount i's
-    static_assert(I % 2 == 0, "pieces come in pairs");
+    constexpr int kC = 128 / sizeof(T), kCount = 16 / sizeof(T);
     const int across = (a.K + 32 * J - 1) / (32 * J);
     const Side d_rows{a.grad, a.z, a.ldg, a.N, a.M}, d_turned{a.grad, a.z, a.ldg, a.N, a.N};
     float4v acc[I][J];
@@ -321,7 +307,7 @@ __global__ __launch_bounds__(256) void linear_direct_grad_kernel(DirectGradArgs 
     const unsigned block = blockIdx.x - a.tiles_x;
     const int down = (a.N + 32 * I - 1) / (32 * I), tiles_w = down * (a.grad_w ? across : 1), tile = (int)(block % (unsigned)tiles_w), part = (int)(block / (unsigned)tiles_w);
     const int n0 = tile % down * 32 * I, k0 = tile / down * 32 * J;
-    float sums[kSums] = {};
+    float sums[kCount] = {};
     direct_tile<T, I, J, true, true, kSlope, kFew>(d_turned, a.grad_w ? Side{a.x, nullptr, a.ldx, 0, a.K} : d_turned, a.act, n0, k0, part * a.steps_w * kC, min(a.M, (part + 1) * a.steps_w * kC), lds, acc, sums);
     out.out = a.grad_w;
     out.residual = a.accumulate ? a.grad_w : nullptr;
@@ -351,19 +337,17 @@ __global__ __launch_bounds__(256) void linear_direct_grad_kernel(DirectGradArgs 
         return;
     }
     // The threads that hold the same i's lie kAcross apart; their sums are added in order.
-    constexpr int kAcross = 32 * I / kCount, kApart = 256 / kAcross;
-    static_assert(kApart >= 1, "a thread a piece");
+    constexpr int kAcross = 32 * I / kCount;
+    static_assert(256 % kAcross == 0, "a thread's pieces are of the same i's");
     float* of = reinterpret_cast<float*>(lds);
     __syncthreads();
 #pragma unroll
-    for (int e = 0; e < kSums; ++e) {
-        const int pair = e / kCount * 256 + (int)threadIdx.x, i = pair % kAcross * kCount, first = max(n0 + i + kCount - a.N, 0);
-        if (e % kCount >= first) of[(pair / kAcross) * (32 * I) + i + e % kCount - first] = sums[e];      // (places as in Share)
-    }
+    for (int e = 0; e < kCount; ++e) of[threadIdx.x / kAcross * (32 * I) + threadIdx.x % kAcross * kCount + e] = sums[e];
     __syncthreads();
     if ((int)threadIdx.x >= 32 * I || n0 + (int)threadIdx.x >= a.N) return;
     float total = 0.f;
-    for (int p = 0; p < kApart * (kSums / kCount); ++p) total += of[p * 32 * I + threadIdx.x];
+#pragma unroll
+    for (int p = 0; p < 256 / kAcross; ++p) total += of[p * 32 * I + threadIdx.x];
     const int n = n0 + threadIdx.x;
     if (a.partial_bias) a.partial_bias[(size_t)part * a.N + n] = total;
     else a.grad_bias[n] = a.accumulate ? a.grad_bias[n] + total : total;
@@ -718,8 +702,8 @@ double lay_estimate(double bytes) { return 3.0 + bytes / 4e6; }
 // A direct launch of `tiles` that take `work` steps in all, `longest` of them one after another at most.  turned: the gradients' operands.
 double direct_estimate(int dtype, double tiles, double work, int longest, bool turned)
 {
-    const double alone = dtype == kF32 ? 0.74 : turned ? 0.42 : 0.34, shared = dtype == kF32 ? 0.63 : turned ? 0.38 : 0.25;
-    return 4.5 + std::max(longest * alone, work / 256.0 * shared) + tiles / 256.0 * (turned ? 1.5 : 0.9);
+    const double alone = dtype == kF32 ? 0.74 : 0.34, shared = dtype == kF32 ? (turned ? 0.60 : 0.63) : turned ? 0.28 : 0.25;
+    return 4.5 + std::max(longest * alone, work / 256.0 * shared) + tiles / 256.0 * (turned ? 1.2 : 0.9);
 }
 
 LinearPlan plan_of(const LinearArgs& a, int dtype)
@@ -863,7 +847,7 @@ GradPlan plan_of(const LinearGradArgs& a, int dtype)
     const double work = tiles_x * all_x + tiles_w * all_w, form = lay_estimate(3.0 * a.M * a.N * b) + 1.5;
     direct = direct_estimate(dtype, tiles_x * l.parts_x + tiles_w * l.parts_w, work, std::max(l.steps_x, l.steps_w), true) + join_estimate(l.parts_x, (double)a.M * a.K) + join_estimate(l.parts_w, (double)a.N * a.K);
     // (Where the slope is worked out as the tiles are loaded, every tile along K does it anew.)
-    const double anew = a.act == kNone ? 0.0 : std::max(work / 256.0, (double)std::max(l.steps_x, l.steps_w)) * (a.act == kRelu ? 0.26 : 0.38) * (dtype == kF32 ? 0.5 : 1.0);
+    const double anew = a.act == kNone ? 0.0 : std::max(work / 256.0, (double)std::max(l.steps_x, l.steps_w)) * (a.act == kRelu ? 0.20 : 0.36) * (dtype == kF32 ? 0.5 : 1.0);
     l.formed = anew > form;
     direct += std::min(anew, form);
     if (direct < laid) {

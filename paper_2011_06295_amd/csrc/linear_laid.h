@@ -26,24 +26,8 @@ __device__ __forceinline__ void multiply(float4v& c, int4v w, int4v x)
 template <class T>
 __device__ __forceinline__ int bytes_of_rows(int terms) { return (terms * (int)sizeof(T) + 15) / 16 * 16; }
 
-// Four elements of each of 16 rows that lie along i, as four elements along c of each of 16 i's: lane l of 16 gives the address of elements
-// 4 (l % 4) .. + 3 of row l / 4, and gets rows 0 .. 3 of element l.
-__device__ __forceinline__ int2v read_turned(const char* at)
-{
-    typedef short short4v __attribute__((ext_vector_type(4)));
-    return __builtin_bit_cast(int2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((SC_LDS short4v*)(SC_LDS char*)at));
-}
-
 // A load of a piece that lies past the rows' end: an offset that no descriptor reaches (they describe 2^31 bytes at most).
 __device__ __forceinline__ unsigned past(unsigned offset, unsigned beyond, int i) { return offset | ((beyond >> i) & 1u) << 31; }
-
-// What the number of a turned row's piece of 16 bytes is combined with (by exclusive or), row c of a tile of `length` i's.
-template <class T>
-__device__ __forceinline__ int swizzle_of(int c, int length)
-{
-    if (sizeof(T) == 4) return ((c >> 2) & 3) << 2;
-    return length == 64 ? (((c >> 1) & 1) | ((c >> 3) & 1) << 1) << 1 : ((c & 3) | ((c >> 3) & 1) << 2) << 1;
-}
 
 // Large tiles: a workgroup has a CU to itself, so it walks over tiles, `stride` apart, and loads the next one's first steps before it
 // finishes one.  (Three steps a tile at least: a barrier lies between what reads a tile's biases and what loads over them.)
@@ -170,32 +154,16 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 || S > 2 ? 1 : 2) void 
     // four c's of 16 bits at once, or one of fp32.
     const int wm = wave % WM, wn = wave / WM, r = lane & 15, q = lane >> 4;
     constexpr int kRowX = TM * (int)sizeof(T), kRowW = TN * (int)sizeof(T), kChunk = 16 * (int)sizeof(T);      // bytes of a block's i's
-    const int c_first = sizeof(T) == 2 ? 8 * q + (r >> 2) : 4 * q, in_chunk = sizeof(T) == 2 ? (r & 3) * 8 : r * 4;
-    auto turned = [&](int first_block, int row_length, int tile_length) {
-        return c_first * row_length + ((first_block * kChunk / 16) ^ swizzle_of<T>(c_first, tile_length)) * 16 + in_chunk;
-    };
-    int xa0 = kTurnX ? turned(wm * MB, kRowX, TM) : (wm * 16 * MB + r) * 128 + ((q ^ (r >> 1)) << 4), xa1 = kTurnX ? xa0 + kC / 2 * kRowX : xa0 ^ 64;
-    int wa0 = S * kX + (kTurnW ? turned(wn * NB, kRowW, TN) : (wn * 16 * NB + (r >> 2) * 8 + (r & 3)) * 128 + ((q ^ (r >> 1)) << 4));
+    int xa0 = kTurnX ? turned_address<T>(lane, wm * MB, TM) : (wm * 16 * MB + r) * 128 + ((q ^ (r >> 1)) << 4), xa1 = kTurnX ? xa0 + kC / 2 * kRowX : xa0 ^ 64;
+    int wa0 = S * kX + (kTurnW ? turned_address<T>(lane, wn * NB, TN) : (wn * 16 * NB + (r >> 2) * 8 + (r & 3)) * 128 + ((q ^ (r >> 1)) << 4));
     int wa1 = kTurnW ? wa0 + kC / 2 * kRowW : wa0 ^ 64;
     int4v wf[2][NB], xf[2][MB];
-    auto read = [&](int address, int block, int row_length) {      // turned: 16 i's of a block
-        const char* from = lds + (address ^ (block * kChunk));
-        if constexpr (sizeof(T) == 2) {
-            const int2v low = read_turned(from), high = read_turned(from + 4 * row_length);
-            return int4v{low[0], low[1], high[0], high[1]};
-        } else {
-            int4v v;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const int*>(from + e * row_length);
-            return v;
-        }
-    };
     auto read_w = [&](int h, int j) {
-        if constexpr (kTurnW) wf[h][j] = read(h ? wa1 : wa0, j, kRowW);
+        if constexpr (kTurnW) wf[h][j] = read_block<T>(lds + ((h ? wa1 : wa0) ^ (j * kChunk)), kRowW);
         else wf[h][j] = *reinterpret_cast<const int4v*>(lds + (h ? wa1 : wa0) + ((j >> 1) * 32 + (j & 1) * 4) * 128);
     };
     auto read_x = [&](int h, int i) {
-        if constexpr (kTurnX) xf[h][i] = read(h ? xa1 : xa0, i, kRowX);
+        if constexpr (kTurnX) xf[h][i] = read_block<T>(lds + ((h ? xa1 : xa0) ^ (i * kChunk)), kRowX);
         else xf[h][i] = *reinterpret_cast<const int4v*>(lds + (h ? xa1 : xa0) + i * 2048);
     };
     asm volatile("s_waitcnt vmcnt(%0)" :: "n"((S - 1) * kLoads) : "memory");
