@@ -536,6 +536,64 @@ def test_adamw_in_a_graph_counts_its_steps():
         assert int(opt.steps) == plain.steps == 5
 
 
+# ---------------------------------------------------------------- the model that runs them together
+
+def _small_model(seed, **more):
+    import torch
+    from paper_2011_06295_amd import text_model
+    rng = np.random.default_rng(seed)
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    vocab, dim, classes, width = 400, 40, 5, 30
+    filters = [((rng.standard_normal((12, dim, 1, s)) * 0.3).astype(np.float32), (rng.random((12, dim, 1, s)) < 0.3).astype(np.uint8),
+                (rng.standard_normal(12) * 0.1).astype(np.float32)) for s in (2, 3)]
+    table = torch.randn((vocab, dim), generator=gen, device="cuda")
+    table[0] = 0.0
+    hidden, classifier = torch.randn((width, 24), generator=gen, device="cuda") * 0.3, torch.randn((classes, width), generator=gen, device="cuda") * 0.3
+    model = text_model.ClassifierModel(table, filters, hidden, classifier, **more)
+    model.hidden.bias.copy_(torch.randn(width, generator=gen, device="cuda") * 0.1)
+    tokens, labels = text_model.sentences(9, 21, vocab, classes, seed=seed)
+    return model, filters, tokens, labels
+
+
+@pytest.mark.parametrize("activation", ["relu", "gelu", "silu"])
+def test_model_s_gradients_against_64_bits(activation):
+    """fp32 features, bounded by 1e-5 of their largest (the convolutions' own tolerance), go through two layers, the loss and back: 4e-5 of each
+    gradient's largest."""
+    import torch
+    model, filters, tokens, labels = _small_model(41, activation=activation)
+    losses, grads = model.gradients(tokens, labels)
+    leaves = [t.double().cpu().requires_grad_(True) for t in (model.words.table, model.hidden.weight, model.hidden.bias, model.classifier.weight, model.classifier.bias)]
+    table, w1, b1, w2, b2 = leaves
+    x = table[tokens.cpu()].permute(0, 2, 1)[:, :, None]
+    features = torch.cat([torch.relu(torch.nn.functional.conv2d(x, torch.from_numpy(w * m).double(), torch.from_numpy(b).double())).squeeze(2).amax(2) for w, m, b in filters], 1)
+    logits = _act(features @ w1.t() + b1, activation) @ w2.t() + b2
+    each = torch.nn.functional.cross_entropy(logits, labels.cpu(), reduction="none") / len(tokens)
+    each.sum().backward()
+    assert float((losses.double().cpu() - each.detach()).abs().max()) <= 4e-5 * float(each.detach().max())
+    leaves[0].grad[0] = 0.0          # the padding word
+    for got, leaf in zip(grads, leaves):
+        assert float((got.double().cpu() - leaf.grad).abs().max()) <= 4e-5 * float(leaf.grad.abs().max()), got.shape
+    model.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_model_s_step_moves_its_parameters_by_the_optimizer_s_rule(bits):
+    """The first step: the sign of each gradient times the rate, but where the gradient is as small as eps; decay."""
+    import torch
+    model, _, tokens, labels = _small_model(42, bits=bits, rate=1e-2, decay=0.1)
+    parameters = model.optimizer.params
+    before = [p.double() for p in parameters]
+    _, grads = model.gradients(tokens, labels)
+    first = float(model.train_step(tokens, labels))
+    for p, p0, g in zip(parameters, before, grads):
+        g = g.double()
+        ref = p0 * (1 - 1e-2 * 0.1) - 1e-2 * g / (g.abs() + 1e-8)
+        _within(p, ref, 4 * E * p0.abs() + 16 * E * 1e-2 + E * ref.abs(), p.shape)
+    assert float(model.words.table[0].abs().max()) == 0.0
+    assert math.isfinite(first) and math.isfinite(float(model.train_step(tokens, labels)))
+    model.close()
+
+
 # ---------------------------------------------------------------- streams, graphs, refusals
 
 def test_layer_and_loss_on_another_stream_and_in_a_graph():
