@@ -445,7 +445,8 @@ enum { SC_ACT_NONE = 0, SC_ACT_RELU = 1, SC_ACT_GELU = 2, SC_ACT_SILU = 3 };
  * array that is written may overlap another (what lies between rows counts as theirs).  The same arguments give the same bits.
  * An infinity or a NaN in a row of x or of w reaches no other row or column of the output.  M may be 0 (no-op).
  * SC_EINVAL: a null or misaligned pointer (to its own element size), N or K below 1, a distance between rows that is too small, an
- * unknown type or activation, a workspace that is too small.  SC_EUNSUPPORTED: M, N or K above 2^20, a distance of 2^31 or more.
+ * unknown type or activation, a workspace that is too small.  SC_EUNSUPPORTED: M, N or K above 2^20, a distance of 2^31 or more, an array of
+ * 2^24 - 1 tiles of 64 x 64 elements or more (about 2^36 elements).
  */
 int sparse_conv_linear_workspace(const void* x, const void* w, int M, int N, int K, long long ldx, long long ldw, int dtype,
                                  long long* bytes);
@@ -529,7 +530,7 @@ typedef struct {
  *   step         the number of this step, from 1.
  *   counted      NULL, or DEVICE memory that sparse_conv_adamw_count filled: the step's number is taken from there, and `step` not looked at.
  * SC_EINVAL: a null or misaligned pointer, a negative count, betas outside 0 <= beta < 1, rate, eps or decay negative or no finite number,
- * step below 1, unknown types.
+ * step below 1, unknown types.  SC_EUNSUPPORTED: more than 2^34 elements in a tensor.
  */
 int sparse_conv_adamw(const sparse_conv_adamw_tensor* tensors, int count, int param_dtype, int grad_dtype, int state_dtype, double rate,
                       double beta1, double beta2, double eps, double decay, double grad_scale, long long step, const void* counted,

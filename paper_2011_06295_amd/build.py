@@ -111,9 +111,17 @@ def build_sanitize_text(verbose: bool = False) -> str:
     return exe
 
 
+def build_sanitize_train(verbose: bool = False) -> str:
+    """The same for the entry points of the layer, the loss and the AdamW step (text_api.cpp) and tests/sanitize/train_driver.cpp."""
+    exe = os.path.join(_build_dir(), "sanitize_train_driver")
+    _run_all([_sanitized("train_driver.cpp", exe, ("text_api.cpp", "no_device.cpp"))], verbose)
+    return exe
+
+
 if __name__ == "__main__":
     if "--sanitize" in sys.argv[1:]:
         print(build_sanitize(verbose=True))
         print(build_sanitize_text(verbose=True))
+        print(build_sanitize_train(verbose=True))
     else:
         print(build(verbose=True))

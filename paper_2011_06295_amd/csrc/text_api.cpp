@@ -49,6 +49,8 @@ int check_int8(int M, int N, int K, int in_dtype, int out_dtype)
 }
 
 constexpr int kMostLinear = 1 << 20;
+constexpr long long kMostTiles = (1ll << 24) - 1;
+constexpr long long kMostStep = 1ll << 34;      // elements of a tensor: workgroups of 2048 each
 constexpr long long kMostApart = 1ll << 31;
 
 // An array: `bytes` from p on, whose elements have `element` bytes.
@@ -67,6 +69,9 @@ int check_linear(int M, int N, int K, long long ldx, long long ldw, long long ld
 {
     if (M < 0 || N < 1 || K < 1 || ldx < K || ldw < K || ldo < N || !is_float(dtype) || activation < SC_ACT_NONE || activation > SC_ACT_SILU) return SC_EINVAL;
     if (M > kMostLinear || N > kMostLinear || K > kMostLinear || ldx >= kMostApart || ldw >= kMostApart || ldo >= kMostApart) return SC_EUNSUPPORTED;
+    // (Tiles of 64 x 64 of each array: what a launch of 256 threads a tile can count.)
+    const long long m = (M + 63) / 64, n = (N + 63) / 64, k = (K + 63) / 64;
+    if (m * n >= kMostTiles || m * k >= kMostTiles || n * k >= kMostTiles) return SC_EUNSUPPORTED;
     return SC_OK;
 }
 
@@ -209,7 +214,7 @@ int sparse_conv_linear(const void* x, const void* w, const float* bias, const vo
     if (rc != SC_OK) return rc;
     if (M == 0) return SC_OK;
     const int b = type_bytes(dtype);
-    const Array ax{x, rows_bytes(M, K, ldx, b), b}, aw{w, rows_bytes(N, K, ldw, b), b}, ab{bias, 4ll * N, 4}, ar{residual, rows_bytes(M, N, ldr, b), b},
+    const Array ax{x, rows_bytes(M, K, ldx, b), b}, aw{w, rows_bytes(N, K, ldw, b), b}, ab{bias, 4ll * N, 4}, ar{residual, residual ? rows_bytes(M, N, ldr, b) : 0, b},
         ao{out, rows_bytes(M, N, ldo, b), b}, az{z, rows_bytes(M, N, N, b), b};
     if (missing(ax) || missing(aw) || missing(ao) || (bias && missing(ab)) || (residual && missing(ar)) || (z && missing(az))) return SC_EINVAL;
     if (overlap(ao, ax) || overlap(ao, aw) || overlap(ao, ab) || overlap(ao, az) || (overlap(ao, ar) && !(residual == out && ldr == ldo)) ||
@@ -288,7 +293,7 @@ int sparse_conv_cross_entropy(const void* logits, const void* labels, const floa
     if (rows == 0) return SC_OK;
     const int b = type_bytes(dtype), lb = (flags & SC_LOSS_LABELS_64) ? 8 : 4;
     const Array al{logits, rows_bytes(rows, classes, ldl, b), b}, an{labels, (long long)rows * lb, lb}, aw{weights, rows * 4ll, 4}, as{loss, rows * 4ll, 4},
-        ag{grad, rows_bytes(rows, classes, ldg, b), b};
+        ag{grad, grad ? rows_bytes(rows, classes, ldg, b) : 0, b};
     if (missing(al) || missing(an) || missing(as) || (weights && missing(aw)) || (grad && missing(ag))) return SC_EINVAL;
     if (overlap(as, al) || overlap(as, an) || overlap(as, aw) || overlap(as, ag) || overlap(ag, an) || overlap(ag, aw) ||
         (overlap(ag, al) && !(grad == logits && ldg == ldl))) return SC_EINVAL;
@@ -308,7 +313,7 @@ int sparse_conv_adamw(const sparse_conv_adamw_tensor* tensors, int count, int pa
     for (int i = 0; i < count; ++i) {
         const sparse_conv_adamw_tensor& t = tensors[i];
         if (t.count < 0 || (t.master != nullptr) != (tensors[0].master != nullptr)) return SC_EINVAL;
-        if (t.count > kMaxElements) return SC_EUNSUPPORTED;
+        if (t.count > kMostStep) return SC_EUNSUPPORTED;
         if (t.count == 0) continue;
         const int pb = type_bytes(param_dtype), gb = type_bytes(grad_dtype), sb = small ? 1 : 4;
         const long long scales = (t.count + SC_ADAMW_BLOCK - 1) / SC_ADAMW_BLOCK * 4;

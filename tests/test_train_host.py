@@ -29,6 +29,7 @@ def test_layer_limits_workspace_and_empty_calls():
         assert _linear(**big) == B.SC_EUNSUPPORTED
     for name in ("ldx", "ldw", "ldo"):
         assert _linear(**{name: 1 << 31}) == B.SC_EUNSUPPORTED
+    assert _linear(M=1 << 20, N=1 << 16, ldo=1 << 16) == B.SC_EUNSUPPORTED and _linear(N=1 << 20, K=1 << 16, ldx=1 << 16, ldw=1 << 16, ldo=1 << 20) == B.SC_EUNSUPPORTED
     assert _linear(M=0, x=None) == B.SC_OK
     n = C.c_longlong(-1)
 
@@ -129,7 +130,7 @@ def test_step_limits_and_empty_calls():
     assert _adamw([]) == B.SC_OK
     assert _adamw([_tensor(count=0, param=None, grad=None, m=None, v=None)] * 3) == B.SC_OK
     assert _adamw([_tensor(), _tensor(master=1 << 50)]) == B.SC_EINVAL           # all with, or all without
-    assert _adamw([_tensor(count=1 << 47)]) == B.SC_EUNSUPPORTED
+    assert _adamw([_tensor(count=(1 << 34) + 1)]) == B.SC_EUNSUPPORTED
     for args in ((None, Z, 0.9, 0.9), (X, None, 0.9, 0.9), (X + 4, Z, 0.9, 0.9), (X, Z + 8, 0.9, 0.9), (X, X, 0.9, 0.9), (X, Z, 1.0, 0.9), (X, Z, 0.9, -1.0)):
         assert LIB.sparse_conv_adamw_count(*args, None) == B.SC_EINVAL
 
