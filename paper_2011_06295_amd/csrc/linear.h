@@ -168,7 +168,8 @@ __device__ __forceinline__ int2v read_turned(const char* at)
 template <class T>
 __device__ __forceinline__ int swizzle_of(int c, int length)
 {
-    if (sizeof(T) == 4) return ((c >> 2) & 3) << 2;
+    if (sizeof(T) == 4) return ((c >> 2) & (length == 32 ? 1 : 3)) << 2;
+    if (length == 32) return ((c >> 3) & 1) << 1;
     return length == 64 ? (((c >> 1) & 1) | ((c >> 3) & 1) << 1) << 1 : ((c & 3) | ((c >> 3) & 1) << 2) << 1;
 }
 

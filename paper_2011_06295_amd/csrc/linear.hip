@@ -437,8 +437,8 @@ __global__ __launch_bounds__(256) void linear_dot_kernel(ProductArgs a, int K, l
 double pieces_of(int n, int size) { return (double)((n + size - 1) / size); }
 
 // Microseconds that a product of rows of `bytes` is estimated to take.  The constants are fitted, for 16-bit types and for fp32, to what each kernel
-// near the fastest took at 125 sizes (4 to 8192 rows of x, 64 to 8192 of w and of terms, one launch after another in a graph, arrays
-// that change): the kernel of the least estimate takes 1.9 % more than the fastest on average, and more than 15 % at one size (4096 x 3776 -> 64).
+// near the fastest took at 159 sizes (4 to 8192 rows of x, 64 to 8192 of w and of terms, one launch after another in a graph, arrays
+// that change): the kernel of the least estimate takes 1.1 % more than the fastest on average, and at most 21 % (40 x 7552 -> 3712 bfloat16).
 
 // Row kernel: a launch, the sums of the wavefronts and the further workgroups of a CU, then the largest of what all workgroups load,
 // what those of one CU load, both operands from memory, and the products.
@@ -448,10 +448,10 @@ struct RowRule {
     double all, one, arrays, products;        // MB/us of all, KB/us of one, MB/us of the arrays; us for 1000 bytes of a block
 };
 constexpr RowRule kRowRules[2][5] = {
-    {{1, 1, 1.25, 0.62, 20.4, 126.0, 6.3, 0.055}, {2, 1, 1.08, 0.68, 19.4, 127.0, 5.6, 0.050}, {2, 2, 0.97, 0.19, 15.4, 129.0, 6.4, 0.055},
-     {4, 1, 1.24, 0.34, 24.1, 133.0, 4.6, 0.050}, {4, 2, 2.09, 0.87, 15.1, 146.0, 4.9, 0.050}},
-    {{1, 1, 1.09, 0.67, 15.9, 255.0, 6.2, 0.373}, {2, 1, 0.85, 1.18, 30.8, 605.0, 5.1, 0.324}, {2, 2, 1.03, 0.19, 21.4, 106.0, 4.6, 0.302},
-     {4, 1, 0.90, 0.52, 85.6, 180.0, 2.1, 0.289}, {4, 2, 2.14, 1.30, 68.7, 129.0, 3.1, 0.293}}};
+    {{1, 1, 1.22, 0.603, 17.9, 137.0, 6.23, 0.0547}, {2, 1, 0.746, 0.317, 21.6, 129.0, 5.98, 0.0479}, {2, 2, 1.86, 0.573, 14.8, 132.0, 6.73, 0.0479},
+     {4, 1, 0.899, 0.344, 21.1, 139.0, 4.77, 0.05}, {4, 2, 2.04, 0.601, 16.1, 121.0, 6.32, 0.0499}},
+    {{1, 1, 1.15, 0.769, 16.3, 174.0, 4.99, 0.356}, {2, 1, 0.66, 0.317, 14.9, 66.9, 4.09, 0.358}, {2, 2, 1.56, 1.54, 28.8, 182.0, 4.61, 0.287},
+     {4, 1, 0.829, 0.344, 48.2, 119.0, 4.34, 0.331}, {4, 2, 2.13, 1.37, 10.0, 166.0, 6.05, 0.289}}};
 
 double row_estimate(const RowRule& r, int M, int N, double bytes)
 {
@@ -468,10 +468,10 @@ struct TileRule {
     double arrays, output;                    // MB/us
 };
 constexpr TileRule kTileRules[2][6] = {
-    {{2, 2, 4, 0.244, 0.185, 1.25, 2.34, 2.2, 13.4}, {4, 4, 2, 0.065, 0.470, 1.79, 2.88, 4.4, 10.6}, {8, 8, 1, 0.0, 1.15, 1.55, 8.19, 5.0, 12.3},
-     {2, 2, 2, 0.043, 0.211, 2.71, 1.19, 5.2, 9.1}, {4, 2, 1, 0.0, 0.308, 2.29, 1.87, 3.4, 6.1}, {4, 4, 1, 0.0, 0.401, 2.66, 2.32, 4.6, 5.9}},
-    {{2, 2, 4, 0.228, 0.551, 1.25, 2.36, 1.8, 5.6}, {4, 4, 2, 0.055, 1.92, 0.10, 6.34, 1.9, 8.7}, {8, 8, 1, 0.0, 7.7, 1.55, 8.19, 5.0, 12.3},
-     {2, 2, 2, 0.074, 0.568, 1.75, 2.27, 3.2, 21.8}, {4, 2, 1, 0.0, 1.02, 2.41, 2.08, 25.8, 4.5}, {4, 4, 1, 0.0, 1.93, 3.36, 3.26, 5.0, 10.7}}};
+    {{2, 2, 4, 0.223, 0.176, 1.25, 2.34, 1.58, 8.54}, {4, 4, 2, 0.063, 0.438, 1.79, 3.18, 4.61, 20.3}, {8, 8, 1, 0.00878, 1.15, 7.83, 2.04, 5.5, 6.17},
+     {2, 2, 2, 0.043, 0.203, 2.63, 1.29, 5.17, 15.3}, {4, 2, 1, 0.0104, 0.297, 2.55, 1.58, 9.4, 5.15}, {4, 4, 1, 0.01, 0.429, 2.87, 2.09, 5.56, 7.34}},
+    {{2, 2, 4, 0.268, 0.535, 1.25, 2.51, 1.72, 26.0}, {4, 4, 2, 0.0675, 1.91, 1.79, 3.91, 2.04, 6.97}, {8, 8, 1, 0.0, 7.7, 1.55, 8.19, 5.0, 12.3},
+     {2, 2, 2, 0.043, 0.56, 2.35, 1.82, 29.1, 89.6}, {4, 2, 1, 0.015, 1.02, 2.82, 1.52, 4.47, 4.46}, {4, 4, 1, 0.01, 1.91, 1.57, 4.43, 2.0, 13.1}}};
 
 double tile_estimate(const TileRule& r, int M, int N, int parts, double bytes, int element)
 {
@@ -483,7 +483,7 @@ double tile_estimate(const TileRule& r, int M, int N, int parts, double bytes, i
 }
 
 // Parts of a sum, and the launch that adds them up.
-double join_estimate(int parts, double outputs) { return parts > 1 ? 3.0 + 4.0 * outputs * (parts + 1) / 4e6 : 0.0; }
+double join_estimate(int parts, double outputs) { return parts > 1 ? 3.5 + 4.0 * outputs * (parts + 1) / 4e6 : 0.0; }
 
 struct Choice {
     Kernel kernel;
@@ -511,15 +511,6 @@ Choice choose(int dtype, int M, int N, int terms, bool turned)
         }
     }
     return best;
-}
-
-// Parts of a sum of `all` steps, so that `tiles` workgroups a part are `wanted` in all, of `least` steps each or more.
-int parts_of(double tiles, int all, double wanted, int least)
-{
-    int parts = 1;
-    while (parts < 64 && tiles * parts * 2 <= wanted && (all + 2 * parts - 1) / (2 * parts) >= least) parts *= 2;
-    const int steps = (all + parts - 1) / parts;
-    return (all + steps - 1) / steps;
 }
 
 template <class T>
@@ -692,18 +683,38 @@ enum Way { kDot, kDirect, kLaid };
 struct LinearPlan {
     Way way;
     Choice laid;            // of kLaid
-    int parts, steps;       // of kDirect
+    bool small;             // kDirect: tiles of 32 x 32
+    int parts, steps;
     bool lay_x, lay_w;
     long long x, w, end;    // bytes of scratch memory: where w's copy and the parts begin, and all
 };
 
 double lay_estimate(double bytes) { return 3.0 + bytes / 4e6; }
 
-// A direct launch of `tiles` that take `work` steps in all, `longest` of them one after another at most.  turned: the gradients' operands.
-double direct_estimate(int dtype, double tiles, double work, int longest, bool turned)
+// A direct launch of `tiles` that take `work` steps in all, `longest` of them one after another at most.  turned: the gradients' operands; small: tiles of
+// 32 x 32 instead of 64 x 64 (faster until they are several for each CU: gradients of 128 x 200 -> 256 fp32 6.4 us against 9.9, of 1024 x 1024 -> 1024
+// bfloat16 24.9 against 16.6).
+double direct_estimate(int dtype, bool turned, bool small, double tiles, double work, int longest)
 {
-    const double alone = dtype == kF32 ? 0.74 : 0.34, shared = dtype == kF32 ? (turned ? 0.60 : 0.63) : turned ? 0.28 : 0.25;
-    return 4.5 + std::max(longest * alone, work / 256.0 * shared) + tiles / 256.0 * (turned ? 1.2 : 0.9);
+    const bool wide = dtype == kF32;
+    const double alone = small ? (wide ? 0.26 : 0.21) : wide ? 0.74 : 0.34;
+    const double shared = small ? (wide ? 0.23 : turned ? 0.15 : 0.20) : wide ? (turned ? 0.60 : 0.63) : turned ? 0.28 : 0.25;
+    return (small ? 3.7 : 4.5) + std::max(longest * alone, work / 256.0 * shared) + tiles / 256.0 * (turned ? 1.2 : 0.9) * (small ? 0.5 : 1.0);
+}
+
+// Parts of a sum of `all` steps, one for each workgroup: their number is a power of two but where the last would be empty.
+int parts_of(int all, int wanted)
+{
+    const int steps = (all + wanted - 1) / wanted;
+    return (all + steps - 1) / steps;
+}
+
+// f(small, parts) for both tiles and all parts of a sum that are looked at: `all` steps, `tiles(size)` of them a part.
+template <class Tiles, class F>
+void each_split(int all, Tiles&& tiles, F&& f)
+{
+    for (int small = 0; small < 2; ++small)
+        for (int parts = 1; parts <= 64 && (parts == 1 || (all >= 8 * parts && tiles(small ? 32 : 64) * parts <= 512.0)); parts *= 2) f(small != 0, parts_of(all, parts));
 }
 
 LinearPlan plan_of(const LinearArgs& a, int dtype)
@@ -718,12 +729,19 @@ LinearPlan plan_of(const LinearArgs& a, int dtype)
         p.way = kDot;
         return p;
     }
-    const double tiles = pieces_of(a.M, 64) * pieces_of(a.N, 64);
-    p.parts = parts_of(tiles, all, 256.0, 8);
-    p.steps = (all + p.parts - 1) / p.parts;
+    double direct = -1.0;
+    auto tiles = [&](int size) { return pieces_of(a.M, size) * pieces_of(a.N, size); };
+    each_split(all, tiles, [&](bool small, int parts) {
+        const int steps = (all + parts - 1) / parts;
+        const double count = tiles(small ? 32 : 64), us = direct_estimate(dtype, false, small, count * parts, count * all, steps) + join_estimate(parts, (double)a.M * a.N);
+        if (direct >= 0.0 && us >= direct) return;
+        direct = us;
+        p.small = small;
+        p.parts = parts;
+        p.steps = steps;
+    });
     p.laid = choose(dtype, a.M, a.N, a.K, false);
     const double laid = p.laid.us + (p.lay_x ? lay_estimate(2.0 * a.M * row_bytes) : 0.0) + (p.lay_w ? lay_estimate(2.0 * a.N * row_bytes) : 0.0);
-    const double direct = direct_estimate(dtype, tiles * p.parts, tiles * all, p.steps, false) + join_estimate(p.parts, (double)a.M * a.N);
     if (direct < laid) {
         p.way = kDirect;
         p.end = partial_bytes(p.parts, a.M, a.N);
@@ -758,10 +776,14 @@ int launch_way(const LinearPlan& p, ProductArgs a, const LinearArgs& l, char* wo
     a.parts = p.parts;
     a.steps = p.steps;
     a.partial = p.parts > 1 ? reinterpret_cast<float*>(workspace) : nullptr;
-    const long long groups = (a.M + 63ll) / 64 * ((a.N + 63ll) / 64) * p.parts;
+    const long long tile = p.small ? 32 : 64, groups = (a.M + tile - 1) / tile * ((a.N + tile - 1) / tile) * p.parts;
     if ((unsigned long long)groups > most_groups(256)) return kTooLarge;
-    if (l.K < (int)(16 / sizeof(T))) hipLaunchKernelGGL((linear_direct_kernel<T, 2, 2, true>), dim3((unsigned)groups), dim3(256), 0, s, a, l.K, l.ldx, l.ldw);
-    else hipLaunchKernelGGL((linear_direct_kernel<T, 2, 2, false>), dim3((unsigned)groups), dim3(256), 0, s, a, l.K, l.ldx, l.ldw);
+    const dim3 grid((unsigned)groups), block(256);
+    const bool few = l.K < (int)(16 / sizeof(T));
+    if (p.small && few) hipLaunchKernelGGL((linear_direct_kernel<T, 1, 1, true>), grid, block, 0, s, a, l.K, l.ldx, l.ldw);
+    else if (p.small) hipLaunchKernelGGL((linear_direct_kernel<T, 1, 1, false>), grid, block, 0, s, a, l.K, l.ldx, l.ldw);
+    else if (few) hipLaunchKernelGGL((linear_direct_kernel<T, 2, 2, true>), grid, block, 0, s, a, l.K, l.ldx, l.ldw);
+    else hipLaunchKernelGGL((linear_direct_kernel<T, 2, 2, false>), grid, block, 0, s, a, l.K, l.ldx, l.ldw);
     const int e = (int)hipGetLastError();
     return e != 0 || p.parts == 1 ? e : launch_join<T>(a, s);
 }
@@ -778,7 +800,7 @@ int linear_kernel(int dtype, int M, int N, int K)
     a.K = K;
     a.ldx = a.ldw = K;
     const LinearPlan p = plan_of(a, dtype);
-    return p.way == kDot ? 100 : p.way == kDirect ? 101 : p.laid.kernel;
+    return p.way == kDot ? 100 : p.way == kDirect ? (p.small ? 103 : 101) : p.laid.kernel;
 }
 
 int launch_linear(int dtype, const LinearArgs& a, char* workspace, void* stream)
@@ -809,7 +831,7 @@ namespace {
 
 // How the gradients are computed, and where the pieces of a pass lie in its scratch memory.
 struct GradPlan {
-    bool direct, formed;                                     // direct; and the gradient behind the activation is formed by a launch before
+    bool direct, formed, small;                              // direct; the gradient behind the activation is formed by a launch before; tiles of 32 x 32
     int parts_x, parts_w, steps_x, steps_w;
     long long sums_x, sums_w, sums_bias;
     // laid out
@@ -832,24 +854,35 @@ GradPlan plan_of(const LinearGradArgs& a, int dtype)
         if (wanted) at += round_up(bytes, 256);
         return here;
     };
-    double laid = 0.0, direct = 0.0;
+    double laid = 0.0, direct = -1.0;
     // (Chosen as if all three were wanted: a gradient's bits do not depend on which others are.)
     l.x = choose(dtype, a.M, a.K, a.N, true);
     l.w = choose(dtype, a.N, a.K, a.M, true);
     laid = l.x.us + l.w.us + lay_estimate((l.own_dz ? 3.0 : 1.0) * a.M * a.N * b) + 3.0;
     if (a.K * b % 16 != 0) laid += lay_estimate(2.0 * a.N * a.K * b) + lay_estimate(2.0 * a.M * a.K * b);
-    const double tiles_x = pieces_of(a.M, 64) * pieces_of(a.K, 64), tiles_w = pieces_of(a.N, 64) * pieces_of(a.K, 64);
     const int all_x = (a.N + count - 1) / count, all_w = (a.M + count - 1) / count;
-    l.parts_x = parts_of(tiles_x, all_x, 256.0, 8);
-    l.parts_w = parts_of(tiles_w, all_w, 256.0, 8);
-    l.steps_x = (all_x + l.parts_x - 1) / l.parts_x;
-    l.steps_w = (all_w + l.parts_w - 1) / l.parts_w;
-    const double work = tiles_x * all_x + tiles_w * all_w, form = lay_estimate(3.0 * a.M * a.N * b) + 1.5;
-    direct = direct_estimate(dtype, tiles_x * l.parts_x + tiles_w * l.parts_w, work, std::max(l.steps_x, l.steps_w), true) + join_estimate(l.parts_x, (double)a.M * a.K) + join_estimate(l.parts_w, (double)a.N * a.K);
-    // (Where the slope is worked out as the tiles are loaded, every tile along K does it anew.)
-    const double anew = a.act == kNone ? 0.0 : std::max(work / 256.0, (double)std::max(l.steps_x, l.steps_w)) * (a.act == kRelu ? 0.20 : 0.36) * (dtype == kF32 ? 0.5 : 1.0);
-    l.formed = anew > form;
-    direct += std::min(anew, form);
+    const double form = lay_estimate(3.0 * a.M * a.N * b) + 1.5;
+    auto tiles_x = [&](int size) { return pieces_of(a.M, size) * pieces_of(a.K, size); };
+    auto tiles_w = [&](int size) { return pieces_of(a.N, size) * pieces_of(a.K, size); };
+    each_split(all_x, tiles_x, [&](bool small, int parts_x) {
+        each_split(all_w, tiles_w, [&](bool small_w, int parts_w) {
+            if (small != small_w) return;
+            const double x = tiles_x(small ? 32 : 64), w = tiles_w(small ? 32 : 64), work = x * all_x + w * all_w;
+            const int steps_x = (all_x + parts_x - 1) / parts_x, steps_w = (all_w + parts_w - 1) / parts_w, longest = std::max(steps_x, steps_w);
+            // (Where the slope is worked out as the tiles are loaded, every tile along K does it anew.)
+            const double anew = a.act == kNone ? 0.0 : std::max(work / 256.0, (double)longest) * (a.act == kRelu ? 0.28 : 0.38) * (dtype == kF32 ? 0.5 : 1.0) * (small ? 0.8 : 1.0);
+            const double us = direct_estimate(dtype, true, small, x * parts_x + w * parts_w, work, longest) + join_estimate(parts_x, (double)a.M * a.K) +
+                              join_estimate(parts_w, (double)a.N * a.K) + std::min(anew, form);
+            if (direct >= 0.0 && us >= direct) return;
+            direct = us;
+            l.small = small;
+            l.formed = anew > form;
+            l.parts_x = parts_x;
+            l.parts_w = parts_w;
+            l.steps_x = steps_x;
+            l.steps_w = steps_w;
+        });
+    });
     if (direct < laid) {
         l.direct = true;
         l.dz = take(l.formed, (long long)a.M * a.N * b);
@@ -878,9 +911,9 @@ int launch_bias(const float* sums, float* out, int count, int N, bool accumulate
 template <class T>
 int launch_direct_grad(const GradPlan& l, const LinearGradArgs& a, char* workspace, hipStream_t s)
 {
-    const unsigned across = (unsigned)((a.K + 63) / 64);
-    const unsigned long long x = a.grad_x ? (a.M + 63ull) / 64 * across * l.parts_x : 0;
-    const unsigned long long w = a.grad_w || a.grad_bias ? (a.N + 63ull) / 64 * (a.grad_w ? across : 1u) * l.parts_w : 0;
+    const unsigned long long tile = l.small ? 32 : 64, across = (a.K + tile - 1) / tile;
+    const unsigned long long x = a.grad_x ? (a.M + tile - 1) / tile * across * l.parts_x : 0;
+    const unsigned long long w = a.grad_w || a.grad_bias ? (a.N + tile - 1) / tile * (a.grad_w ? across : 1ull) * l.parts_w : 0;
     if (x + w > most_groups(256)) return kTooLarge;
     if (x + w == 0) return 0;
     float* const px = a.grad_x && l.parts_x > 1 ? reinterpret_cast<float*>(workspace + l.sums_x) : nullptr;
@@ -901,10 +934,14 @@ int launch_direct_grad(const GradPlan& l, const LinearGradArgs& a, char* workspa
     }
     const dim3 grid((unsigned)(x + w)), block(256);
     const bool few = std::min(a.N, a.K) < (int)(16 / sizeof(T));
-    if (d.z && few) hipLaunchKernelGGL((linear_direct_grad_kernel<T, 2, 2, true, true>), grid, block, 0, s, d);
-    else if (d.z) hipLaunchKernelGGL((linear_direct_grad_kernel<T, 2, 2, true, false>), grid, block, 0, s, d);
-    else if (few) hipLaunchKernelGGL((linear_direct_grad_kernel<T, 2, 2, false, true>), grid, block, 0, s, d);
-    else hipLaunchKernelGGL((linear_direct_grad_kernel<T, 2, 2, false, false>), grid, block, 0, s, d);
+    auto enqueue = [&](auto slope, auto few_of) {
+        if (l.small) hipLaunchKernelGGL((linear_direct_grad_kernel<T, 1, 1, decltype(slope)::value, decltype(few_of)::value>), grid, block, 0, s, d);
+        else hipLaunchKernelGGL((linear_direct_grad_kernel<T, 2, 2, decltype(slope)::value, decltype(few_of)::value>), grid, block, 0, s, d);
+    };
+    if (d.z && few) enqueue(std::true_type{}, std::true_type{});
+    else if (d.z) enqueue(std::true_type{}, std::false_type{});
+    else if (few) enqueue(std::false_type{}, std::true_type{});
+    else enqueue(std::false_type{}, std::false_type{});
     e = (int)hipGetLastError();
     ProductArgs p{};
     if (e == 0 && px) {

@@ -411,9 +411,9 @@ int launch_kernel(Kernel kernel, const ProductArgs& a, hipStream_t s)
 {
     if constexpr (turned == kRows) switch (kernel) {
         case kRow11: return launch_row<T, 1, 1, 8, 4>(a, s);
-        case kRow21: return launch_row<T, 2, 1, 8, 2>(a, s);
-        case kRow22: return launch_row<T, 2, 2, 4, 2>(a, s);
-        case kRow41: return launch_row<T, 4, 1, 8, 1>(a, s);
+        case kRow21: return launch_row<T, 2, 1, 4, 3>(a, s);
+        case kRow22: return launch_row<T, 2, 2, 8, 2>(a, s);
+        case kRow41: return launch_row<T, 4, 1, 4, 2>(a, s);
         case kRow42: return launch_row<T, 4, 2, 4, 2>(a, s);
         case kDeep42: return launch_tile<T, 4, 2, 4, turned>(a, s);
         default: break;

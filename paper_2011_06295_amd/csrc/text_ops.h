@@ -69,7 +69,7 @@ long long linear_workspace(const LinearArgs& a, int dtype);
 int launch_linear(int dtype, const LinearArgs& a, char* workspace, void* stream);
 
 // (For tests: every kernel is to be reached.)  Of operands without gaps at multiples of 16 bytes: the number of the kernel, 100 for very few rows, 101 for
-// arrays as they lie; of the gradients 101, 102 where d is formed before, else 1000 * grad_x's + grad_w's.
+// arrays as they lie (103: in tiles of 32 x 32); of the gradients 101, 102 where d is formed before, else 1000 * grad_x's + grad_w's.
 int linear_kernel(int dtype, int M, int N, int K);
 int linear_grad_kernel(int dtype, int M, int N, int K, int act);
 
