@@ -438,7 +438,8 @@ double pieces_of(int n, int size) { return (double)((n + size - 1) / size); }
 
 // Microseconds that a product of rows of `bytes` is estimated to take.  The constants are fitted, for 16-bit types and for fp32, to what each kernel
 // near the fastest took at 159 sizes (4 to 8192 rows of x, 64 to 8192 of w and of terms, one launch after another in a graph, arrays
-// that change): the kernel of the least estimate takes 1.1 % more than the fastest on average, and at most 21 % (40 x 7552 -> 3712 bfloat16).
+// that change): the kernel of the least estimate takes 1.1 % more than the fastest on average, and at most 21 % (40 x 7552 -> 3712 bfloat16).  (By hand: 5.8 for
+// the arrays of 2 x 2 in 16 bits, where the fit has 6.73: 24 rows of 4096 terms by 8192 take 18.2 us there and 14.8 in 2 x 1 when the weights come from HBM.)
 
 // Row kernel: a launch, the sums of the wavefronts and the further workgroups of a CU, then the largest of what all workgroups load,
 // what those of one CU load, both operands from memory, and the products.
@@ -448,7 +449,7 @@ struct RowRule {
     double all, one, arrays, products;        // MB/us of all, KB/us of one, MB/us of the arrays; us for 1000 bytes of a block
 };
 constexpr RowRule kRowRules[2][5] = {
-    {{1, 1, 1.22, 0.603, 17.9, 137.0, 6.23, 0.0547}, {2, 1, 0.746, 0.317, 21.6, 129.0, 5.98, 0.0479}, {2, 2, 1.86, 0.573, 14.8, 132.0, 6.73, 0.0479},
+    {{1, 1, 1.22, 0.603, 17.9, 137.0, 6.23, 0.0547}, {2, 1, 0.746, 0.317, 21.6, 129.0, 5.98, 0.0479}, {2, 2, 1.86, 0.573, 14.8, 132.0, 5.8, 0.0479},
      {4, 1, 0.899, 0.344, 21.1, 139.0, 4.77, 0.05}, {4, 2, 2.04, 0.601, 16.1, 121.0, 6.32, 0.0499}},
     {{1, 1, 1.15, 0.769, 16.3, 174.0, 4.99, 0.356}, {2, 1, 0.66, 0.317, 14.9, 66.9, 4.09, 0.358}, {2, 2, 1.56, 1.54, 28.8, 182.0, 4.61, 0.287},
      {4, 1, 0.829, 0.344, 48.2, 119.0, 4.34, 0.331}, {4, 2, 2.13, 1.37, 10.0, 166.0, 6.05, 0.289}}};
@@ -691,15 +692,15 @@ struct LinearPlan {
 
 double lay_estimate(double bytes) { return 3.0 + bytes / 4e6; }
 
-// A direct launch of `tiles` that take `work` steps in all, `longest` of them one after another at most.  turned: the gradients' operands; small: tiles of
+// A direct launch of `tiles` that take `work` steps in all, `longest` of them one after another at most, of arrays of `bytes`.  turned: the gradients' operands; small: tiles of
 // 32 x 32 instead of 64 x 64 (faster until they are several for each CU: gradients of 128 x 200 -> 256 fp32 6.4 us against 9.9, of 1024 x 1024 -> 1024
 // bfloat16 24.9 against 16.6).
-double direct_estimate(int dtype, bool turned, bool small, double tiles, double work, int longest)
+double direct_estimate(int dtype, bool turned, bool small, double tiles, double work, int longest, double bytes)
 {
     const bool wide = dtype == kF32;
     const double alone = small ? (wide ? 0.26 : 0.21) : wide ? 0.74 : 0.34;
     const double shared = small ? (wide ? 0.23 : turned ? 0.15 : 0.20) : wide ? (turned ? 0.60 : 0.63) : turned ? 0.28 : 0.25;
-    return (small ? 3.7 : 4.5) + std::max(longest * alone, work / 256.0 * shared) + tiles / 256.0 * (turned ? 1.2 : 0.9) * (small ? 0.5 : 1.0);
+    return (small ? 3.7 : 4.5) + std::max({longest * alone, work / 256.0 * shared, bytes / 5.2e6}) + tiles / 256.0 * (turned ? 1.2 : 0.9) * (small ? 0.5 : 1.0);
 }
 
 // Parts of a sum of `all` steps, one for each workgroup: their number is a power of two but where the last would be empty.
@@ -733,7 +734,7 @@ LinearPlan plan_of(const LinearArgs& a, int dtype)
     auto tiles = [&](int size) { return pieces_of(a.M, size) * pieces_of(a.N, size); };
     each_split(all, tiles, [&](bool small, int parts) {
         const int steps = (all + parts - 1) / parts;
-        const double count = tiles(small ? 32 : 64), us = direct_estimate(dtype, false, small, count * parts, count * all, steps) + join_estimate(parts, (double)a.M * a.N);
+        const double count = tiles(small ? 32 : 64), us = direct_estimate(dtype, false, small, count * parts, count * all, steps, ((double)a.M + a.N) * row_bytes) + join_estimate(parts, (double)a.M * a.N);
         if (direct >= 0.0 && us >= direct) return;
         direct = us;
         p.small = small;
@@ -864,6 +865,7 @@ GradPlan plan_of(const LinearGradArgs& a, int dtype)
     const double form = lay_estimate(3.0 * a.M * a.N * b) + 1.5;
     auto tiles_x = [&](int size) { return pieces_of(a.M, size) * pieces_of(a.K, size); };
     auto tiles_w = [&](int size) { return pieces_of(a.N, size) * pieces_of(a.K, size); };
+    const double bytes = ((double)a.M * a.N * (a.act == kNone ? 1 : 2) + (double)a.M * a.K + (double)a.N * a.K) * b;
     each_split(all_x, tiles_x, [&](bool small, int parts_x) {
         each_split(all_w, tiles_w, [&](bool small_w, int parts_w) {
             if (small != small_w) return;
@@ -871,7 +873,7 @@ GradPlan plan_of(const LinearGradArgs& a, int dtype)
             const int steps_x = (all_x + parts_x - 1) / parts_x, steps_w = (all_w + parts_w - 1) / parts_w, longest = std::max(steps_x, steps_w);
             // (Where the slope is worked out as the tiles are loaded, every tile along K does it anew.)
             const double anew = a.act == kNone ? 0.0 : std::max(work / 256.0, (double)longest) * (a.act == kRelu ? 0.28 : 0.38) * (dtype == kF32 ? 0.5 : 1.0) * (small ? 0.8 : 1.0);
-            const double us = direct_estimate(dtype, true, small, x * parts_x + w * parts_w, work, longest) + join_estimate(parts_x, (double)a.M * a.K) +
+            const double us = direct_estimate(dtype, true, small, x * parts_x + w * parts_w, work, longest, bytes) + join_estimate(parts_x, (double)a.M * a.K) +
                               join_estimate(parts_w, (double)a.N * a.K) + std::min(anew, form);
             if (direct >= 0.0 && us >= direct) return;
             direct = us;
