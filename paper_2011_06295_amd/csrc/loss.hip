@@ -1,9 +1,10 @@
 // The loss of a classifier with the gradient of its logits (sparse_conv_cross_entropy).
 //
-// loss = w (log sum_c exp z_c - z_label), gradient = w (exp(z_c - lse) - [c = label]).  The bytes bound it: logits once in, gradient
+// loss = w (log sum_c exp z_c - z_label), gradient = w (exp(z_c - log sum exp z) - [c = label]).  The bytes bound it: logits once in, gradient
 // once out.  A row stays in registers between the two, where two workgroups of a CU still fit (65536 classes of 16 bits, 32768 of fp32); longer
 // rows are read twice.  Each thread keeps the largest of its logits and the sum of exponentials over that largest, the threads of a row
-// join these pairs once, and every thread turns what it holds into the gradient.
+// join these pairs once, and every thread turns what it holds into the gradient.  4096 x 65536 bfloat16 with masked classes and rows takes 228 us (1.07 GB,
+// 4.7 TB/s; 209 at the rate of a large copy); 128 x 6 fp32 5.8, of which the GPU works 2.1 and the host the rest.
 #include <hip/hip_runtime.h>
 
 #include "text_ops.h"
@@ -12,6 +13,8 @@
 namespace sc {
 
 namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
 
 struct Pair {      // the largest logit and the sum of exp(z - largest)
     float most, sum;
@@ -70,13 +73,13 @@ __device__ __forceinline__ Pair add(Pair p, typename Piece<T>::type v)
 }
 
 template <class T>
-__device__ __forceinline__ void store_gradient(T* row, int c, int classes, typename Piece<T>::type v, float lse, const Row& r)
+__device__ __forceinline__ void store_gradient(T* row, int c, int classes, typename Piece<T>::type v, float most, float log2_sum, const Row& r)
 {
     typedef typename Piece<T>::type V;
     V y;
 #pragma unroll
     for (int e = 0; e < Piece<T>::kCount; ++e) {
-        const float p = __expf((float)v[e] - lse);
+        const float p = __builtin_amdgcn_exp2f(fmaf((float)v[e] - most, kLog2e, -log2_sum));      // (far from zero most + log_sum would lose the logarithm's digits)
         y[e] = (T)(r.weight * (c + e == r.label ? p - 1.f : p));
     }
     if (c + Piece<T>::kCount <= classes) *reinterpret_cast<V*>(row + c) = y;
@@ -127,15 +130,15 @@ __global__ __launch_bounds__(256) void loss_lanes_kernel(LossArgs a)
 #pragma unroll
     for (int d = kLanes / 2; d > 0; d /= 2) p = join(p, {__shfl_xor(p.most, d), __shfl_xor(p.sum, d)});
     labelled = __shfl(labelled, max(r.label, 0) / kCount % kLanes, kLanes);
-    const float lse = logf(p.sum) + p.most;
+    const float log_sum = logf(p.sum), log2_sum = log_sum * kLog2e;
     if (at >= a.rows) return;
-    if (lane == 0) a.loss[row] = r.counts ? r.weight * ((p.most - labelled) + logf(p.sum)) : 0.f;
+    if (lane == 0) a.loss[row] = r.counts ? r.weight * ((p.most - labelled) + log_sum) : 0.f;
     if (!a.grad) return;
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
         const int c = (i * kLanes + lane) * kCount;
         if (c >= a.classes) break;
-        if (r.counts) store_gradient<T>(to, c, a.classes, kept[i], lse, r);
+        if (r.counts) store_gradient<T>(to, c, a.classes, kept[i], p.most, log2_sum, r);
         else store_zeros<T>(to, c, a.classes);
     }
 }
@@ -190,15 +193,15 @@ __global__ __launch_bounds__(kThreads) void loss_row_kernel(LossArgs a)
     p = of_wave[0];
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) p = join(p, of_wave[w]);
-    const float log_sum = logf(p.sum), lse = log_sum + p.most;
+    const float log_sum = logf(p.sum), log2_sum = log_sum * kLog2e;
     if (threadIdx.x == 0) a.loss[row] = r.weight * ((p.most - labelled) + log_sum);
     if (!a.grad) return;
     if constexpr (kPieces > 0) {
 #pragma unroll
         for (int i = 0; i < kPieces; ++i)
-            if (first + i * (int)kStep < a.classes) store_gradient<T>(to, first + i * (int)kStep, a.classes, kept[i], lse, r);
+            if (first + i * (int)kStep < a.classes) store_gradient<T>(to, first + i * (int)kStep, a.classes, kept[i], p.most, log2_sum, r);
     } else {
-        for (long long c = first; c < a.classes; c += kStep) store_gradient<T>(to, (int)c, a.classes, load_logits<T>(from, (int)c, a.classes), lse, r);
+        for (long long c = first; c < a.classes; c += kStep) store_gradient<T>(to, (int)c, a.classes, load_logits<T>(from, (int)c, a.classes), p.most, log2_sum, r);
     }
 }
 

@@ -341,6 +341,30 @@ def test_loss(dtype):
         _check_loss(logits, labels, weights, (1.0, 0.37)[i % 2], dtype, (rows, classes, dtype), in_place=i % 2 == 0)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_loss_of_logits_far_from_zero(dtype):
+    """Differences of logits are exact in fp32 here, so an offset of them all costs nothing."""
+    import torch
+    from paper_2011_06295_amd import text
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    for rows, classes, offset in ((40, 6, 30000.0), (7, 129, -30000.0), (5, 1025, 20000.0), (3, 4096, 50000.0), (2, 40001, -50000.0), (2, 131072, 30000.0)):
+        step = {"f32": 2.0 ** -6, "f16": 32.0, "bf16": 256.0}[dtype]
+        logits = (offset + step * torch.randint(-300 if dtype == "f32" else -2, 300 if dtype == "f32" else 3, (rows, classes), generator=gen, device="cuda")).to(_types()[dtype])
+        labels = torch.randint(0, classes, (rows,), generator=gen, device="cuda")
+        loss, grad = text.cross_entropy(logits, labels)
+        z = logits.double()
+        top = z.amax(1, keepdim=True)
+        lse, far = torch.logsumexp(z - top, 1, keepdim=True), top - z
+        of_sum = 2 * (168 + classes / 1024) * E
+        label = far.gather(1, labels[:, None])
+        ref = (lse + label)[:, 0]
+        _within(loss, ref, of_sum + 4 * E * (ref.abs() + lse[:, 0]) + TINY["f32"], (rows, classes))
+        p = torch.exp(-far - lse)
+        ref = p.scatter_add(1, labels[:, None], torch.full_like(label, -1.0))
+        off = p * (of_sum + 4 * E * (far + lse + 4)) + 4 * E * (ref.abs() + (p > 0.5))
+        _within(grad, ref, off + U[dtype] * (ref.abs() + off) + TINY[dtype], (rows, classes))
+
+
 def test_loss_of_rows_that_lie_apart():
     import torch
     from paper_2011_06295_amd import text
