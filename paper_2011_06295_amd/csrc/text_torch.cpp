@@ -574,7 +574,24 @@ PyObject* py_adamw(PyObject*, PyObject* const* args, Py_ssize_t count)
             require(steps.scalar_type() == at::kLong && steps.numel() == 1 && steps.device() == m.device() && room_of.is_contiguous() && room_of.device() == m.device() &&
                         room_of.numel() * room_of.element_size() >= SC_ADAMW_COUNTED_BYTES, "bad arguments");
             counted = room_of.data_ptr();
-            const int rc = adamw_count(static_cast<long long*>(steps.data_ptr()), room_of.data_ptr(), rule[1], rule[2], stream);
+            // (What the step would refuse must not count: its rule and types, then its arrays.)
+            int rc = adamw(nullptr, 0, param_dtype, grad_dtype, small ? SC_E4M3 : SC_F32, rule[0], rule[1], rule[2], rule[3], rule[4], rule[5], 1, counted, stream);
+            const int bytes_of[3] = {4, 2, 2};      // SC_F32, SC_F16, SC_BF16
+            for (const sparse_conv_adamw_tensor& t : list) {
+                const char *p = static_cast<const char*>(t.param), *g = static_cast<const char*>(t.grad);
+                const int64_t p_bytes = t.count * bytes_of[param_dtype], g_bytes = t.count * bytes_of[grad_dtype];
+                bool overlap = p < g + g_bytes && g < p + p_bytes;
+                for (int i = 2; i < 7; ++i) {
+                    if (args[i] == Py_None) continue;
+                    const at::Tensor& state = THPVariable_Unpack(args[i]);
+                    const char* from = static_cast<const char*>(state.data_ptr());
+                    const char* end = from + state.numel() * state.element_size();
+                    overlap = overlap || (p < end && from < p + p_bytes) || (g < end && from < g + g_bytes);
+                }
+                if (overlap) rc = SC_EINVAL;
+            }
+            if (rc != SC_OK) return PyLong_FromLong(rc);
+            rc = adamw_count(static_cast<long long*>(steps.data_ptr()), room_of.data_ptr(), rule[1], rule[2], stream);
             if (rc != SC_OK) return PyLong_FromLong(rc);
             written(steps);
         }

@@ -262,11 +262,14 @@ class AdamW:
 
     def step(self, grads, scale: float = 1.0):
         """One step on scale * grads: a contiguous tensor like each parameter (all fp32 or of the parameters' type; any of the three types where
-        parameters are fp32), or None, which leaves the parameter and its states alone."""
+        parameters are fp32), or None, which leaves the parameter and its states alone.  Rates and scale are kept by a graph as they were when
+        it was recorded."""
         if self._device != _current_device():
             with torch.cuda.device(self._device):
                 return self.step(grads, scale)
         grads = grads if isinstance(grads, list) else list(grads)
+        if self._counted is None and torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("a step recorded in a graph would keep its number in every replay: make the optimizer with counted=True")
         counted = None if self._counted is None else (self.steps, self._counted)
         rule = (self.rate, *self.betas, self.eps, self.decay, scale)
         rc = _calls.adamw(self.params, grads, self.m, self.v, self.m_scale, self.v_scale, self.master, counted, rule,

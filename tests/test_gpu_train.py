@@ -562,6 +562,35 @@ def test_adamw_in_a_graph_counts_its_steps():
         assert int(opt.steps) == plain.steps == 5
 
 
+def test_adamw_refused_steps_do_not_count_and_plain_ones_are_not_recorded():
+    import torch
+    from paper_2011_06295_amd import text
+    for bits in (32, 8):
+        for counted in (True, False):
+            p = torch.ones(600, device="cuda", dtype=torch.bfloat16)
+            opt = text.AdamW([p], bits=bits, counted=counted, master=True)
+            g = torch.ones(600, device="cuda", dtype=torch.bfloat16)
+            opt.step([g])
+            before = [t.clone() for t in (p, opt.m.view(torch.uint8), opt.master)]
+            for bad in ([g.half()], [p], [opt.master[:600]], [g[:599]], [g, g], [g.cpu()], [g.double()]):
+                with pytest.raises((ValueError, RuntimeError)):
+                    opt.step(bad)
+            with pytest.raises((ValueError, RuntimeError)):
+                opt.step([g], scale=math.inf)
+            opt.rate = -1.0
+            with pytest.raises((ValueError, RuntimeError)):
+                opt.step([g])
+            opt.rate = 1e-3
+            assert int(opt.steps) == 1 and all(torch.equal(a, b) for a, b in zip(before, (p, opt.m.view(torch.uint8), opt.master)))
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        q = p + 1
+        with pytest.raises(RuntimeError, match="counted"):
+            opt.step([g])
+    assert opt.steps == 1
+
+
 # ---------------------------------------------------------------- the model that runs them together
 
 def _small_model(seed, **more):
