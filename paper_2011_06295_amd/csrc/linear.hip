@@ -1,8 +1,17 @@
 // Fully connected layer with bias, activation and residual, and its gradients (sparse_conv_linear, sparse_conv_linear_backward).
 //
-// Every product here is out[m][n] = sum_k x[m][k] w[n][k] of two arrays whose rows lie along k, at multiples of 16 bytes.  What does
-// not come like that (odd rows; the transposes that the gradients need) is laid out in scratch memory first.  Products of 16-bit
-// numbers are summed in fp32 by the matrix cores, fp32 is multiplied in fp32.
+// z = x w^T + bias, out = act(z) + residual; with d = grad act'(z): grad_x = d w, grad_w = d^T x, grad_bias = sum_m d.  So every product is
+// out[m][n] = sum_k a[m][k] b[n][k] of operands whose rows lie along the sum, or the other way round ("turned").  Products of 16-bit numbers are
+// summed in fp32 by the matrix cores, fp32 is multiplied in fp32 (at most 152 TFLOP/s here).  d is rounded to the type of the operands once, since
+// the matrix cores take nothing else; the bias' sums take it before that.
+//
+// Four ways, chosen by what each is estimated to take (below):
+//   very few rows     linear_dot_kernel: the weights once from memory at 4.7 TB/s (1 x 4096 -> 4096 bfloat16 7.2 us);
+//   arrays as they lie  linear_direct_kernel, linear_direct_grad_kernel: one launch, tiles of 32 x 32 or 64 x 64, any address and either way round
+//                     (203 x 1001 -> 1111 fp32 13.0 us; both gradients of 128 x 200 -> 256 with relu 6.6 us);
+//   few rows          linear_row_kernel (linear_laid.h): the weights from memory (24 x 4096 -> 8192 float16 14.8 us, 4.6 TB/s);
+//   tiles             linear_tile_kernel (linear_laid.h): the matrix cores (8192 x 4096 -> 8192 bfloat16 with gelu and z kept 452 us, 1.22 PFLOP/s).
+// The last two load straight to LDS, which takes rows at multiples of 16 bytes; others are laid out in scratch memory first (linear_lay_kernel).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -14,7 +23,8 @@ namespace sc {
 
 namespace {
 
-// The parts of a product added up, in their order, then as in the kernels above.  Four outputs of a row a thread.
+// The parts of a product added up, in their order, then as in the kernels that do all of a sum.  Four outputs of a row a thread; bytes and a launch
+// bound it (about 3.5 us and 1 TB/s of partial sums on top of the product, with which the choice reckons).
 template <class T>
 __global__ __launch_bounds__(256) void linear_join_kernel(ProductArgs a)
 {
@@ -168,7 +178,8 @@ struct Share {
 };
 
 // 32 I by 32 J sums of a workgroup of four wavefronts, over c of c_begin .. c_end - 1.  The bytes of the kAhead steps that follow are on their way to
-// registers while one is multiplied from LDS (two buffers, a barrier a step): a step takes 0.2 us of work, its loads 1 us and more.
+// registers while one is multiplied from LDS (two buffers, a barrier a step): a step takes 0.2 us of work, its loads 1 us and more.  Latency bounds it where
+// a CU has one tile, so tiles are small (I = J = 1) while there are few: 24 x 1001 -> 1001 bfloat16 6.1 us in tiles of 32 x 32, 10.2 in 64 x 64.
 constexpr int kAhead = 3;
 
 template <class T, int I, int J, bool kTurnedA, bool kTurnedB, bool kSlope, bool kFew>
@@ -271,7 +282,8 @@ __global__ __launch_bounds__(256) void linear_direct_kernel(ProductArgs a, int K
 }
 
 // Both gradients in one launch: the first `tiles_x` workgroups take grad_x = d w (sum over N), the others grad_w = d^T x (over M) and, in the
-// tiles of the first columns, the sums of d for the bias.
+// tiles of the first columns, the sums of d for the bias.  One launch instead of up to six (d, two products, joins, sums): 128 x 200 -> 256 fp32
+// 6.4 us against 16.3 laid out.  Past about 2000 x 1000 -> 2000 what the tiles read again from L2 costs more than that.
 struct DirectGradArgs {
     const void *grad, *z, *x, *w;
     void *grad_x, *grad_w;
@@ -353,7 +365,8 @@ __global__ __launch_bounds__(256) void linear_direct_grad_kernel(DirectGradArgs 
     else a.grad_bias[n] = a.accumulate ? a.grad_bias[n] + total : total;
 }
 
-// Very few rows of x: a wavefront (S wavefronts, that share the sum) takes C rows of w and all R of x, 16 bytes a lane of each at a time.
+// Very few rows of x: a wavefront (S wavefronts, that share the sum) takes C rows of w and all R of x, 16 bytes a lane of each at a time.  The weights'
+// bytes bound it, and the latency of the first: 1 x 4096 -> 4096 bfloat16 7.2 us (33.6 MB, 6.55 at the rate of a large copy).
 template <class T, int R, int C, int S>
 __global__ __launch_bounds__(256) void linear_dot_kernel(ProductArgs a, int K, long long ldx, long long ldw)
 {
@@ -438,8 +451,9 @@ double pieces_of(int n, int size) { return (double)((n + size - 1) / size); }
 
 // Microseconds that a product of rows of `bytes` is estimated to take.  The constants are fitted, for 16-bit types and for fp32, to what each kernel
 // near the fastest took at 159 sizes (4 to 8192 rows of x, 64 to 8192 of w and of terms, one launch after another in a graph, arrays
-// that change): the kernel of the least estimate takes 1.1 % more than the fastest on average, and at most 21 % (40 x 7552 -> 3712 bfloat16).  (By hand: 5.8 for
-// the arrays of 2 x 2 in 16 bits, where the fit has 6.73: 24 rows of 4096 terms by 8192 take 18.2 us there and 14.8 in 2 x 1 when the weights come from HBM.)
+// that change): the kernel of the least estimate takes 1.1 % more than the fastest on average, and at most 21 % (40 x 7552 -> 3712 bfloat16).
+// One constant is not the fit's, for arrays that its repetitions held in the caches: 5.8 for 2 x 2 in 16 bits (6.73), since 24 x 4096 -> 8192
+// takes 18.2 us there and 14.8 in 2 x 1 with weights from HBM.
 
 // Row kernel: a launch, the sums of the wavefronts and the further workgroups of a CU, then the largest of what all workgroups load,
 // what those of one CU load, both operands from memory, and the products.
@@ -542,7 +556,8 @@ int product(int dtype, const Choice& c, Turned turned, ProductArgs a, char* part
 
 // Tiles of 64 x 64 elements of [rows][cols] (ld elements from one row to the next) to `copy` (or null), rows of copy_pitch elements with zeros behind
 // what is there.  With an activation the elements are first multiplied by its slope at z (no gaps), in fp32, and rounded once; column_sums
-// [tiles down][cols] (or null) receives the sums over the tile's rows of what was not rounded.
+// [tiles down][cols] (or null) receives the sums over the tile's rows of what was not rounded.  Bytes bound it: 8192 x 8192 bfloat16 with the slope
+// of gelu, 403 MB, 76 us (5.3 TB/s).
 struct LayArgs {
     const void *from, *z;
     void* copy;
@@ -692,9 +707,9 @@ struct LinearPlan {
 
 double lay_estimate(double bytes) { return 3.0 + bytes / 4e6; }
 
-// A direct launch of `tiles` that take `work` steps in all, `longest` of them one after another at most, of arrays of `bytes`.  turned: the gradients' operands; small: tiles of
-// 32 x 32 instead of 64 x 64 (faster until they are several for each CU: gradients of 128 x 200 -> 256 fp32 6.4 us against 9.9, of 1024 x 1024 -> 1024
-// bfloat16 24.9 against 16.6).
+// A direct launch of `tiles` that take `work` steps in all, `longest` of them one after another at most, of arrays of `bytes`.  turned: the gradients'
+// operands; small: tiles of 32 x 32 instead of 64 x 64 (faster until they are several for each CU: gradients of 128 x 200 -> 256 fp32 6.4 us against
+// 9.9, of 1024 x 1024 -> 1024 bfloat16 24.9 against 16.6).
 double direct_estimate(int dtype, bool turned, bool small, double tiles, double work, int longest, double bytes)
 {
     const bool wide = dtype == kF32;
