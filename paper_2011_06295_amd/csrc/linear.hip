@@ -61,14 +61,14 @@ struct Side {
     int count;                          // of i
 };
 
-// kRows i by 128 bytes of c of an operand, a thread's share: pieces of 16 bytes, from any element on.  Loads are issued by no branch at all, so that
+// kRows i by U units of 128 bytes of c of an operand, a thread's share: pieces of 16 bytes, from any element on.  Loads are issued by no branch at all, so that
 // those of several steps can be in flight (after one the compiler waits for all that came before): a piece that would reach outside is the nearest
 // one inside, and `put` moves it into place, with zeros for c past the sum's end.  Outputs of i's that are not there are never stored.
 // kFew: the operand has rows of less than a piece, which are loaded one by one.
-template <class T, int kRows, bool kTurned, bool kSlope, bool kFew>
+template <class T, int kRows, int U, bool kTurned, bool kSlope, bool kFew>
 struct Share {
-    static constexpr int kCount = 16 / sizeof(T), kC = 128 / sizeof(T), kPieces = kRows * 8 / 256;
-    static constexpr int kAcross = kTurned ? kRows / kCount : 8, kLength = kTurned ? kRows * (int)sizeof(T) : 128;      // pieces, bytes of a row in LDS
+    static constexpr int kCount = 16 / sizeof(T), kC = 128 * U / sizeof(T), kPieces = kRows * 8 * U / 256;
+    static constexpr int kAcross = kTurned ? kRows / kCount : 8 * U, kLength = kTurned ? kRows * (int)sizeof(T) : 128 * U;      // pieces, bytes of a row in LDS
     typedef typename Piece<T>::type V;
     V v[kPieces], z[kSlope ? kPieces : 1];
 
@@ -160,7 +160,7 @@ struct Share {
         else all(std::integral_constant<int, kNone>{});
     }
 
-    // kSums: the sums of what goes to LDS are wanted.  Rows lie along c there, 128 bytes, their pieces permuted by the row, or as they do in memory.
+    // kSums: the sums of what goes to LDS are wanted.  Rows lie along c there, U units, their pieces permuted by the row, or as they do in memory.
     template <bool kSums>
     __device__ __forceinline__ void put(const Side& s, int act, int i0, int c0, int c_end, char* to, float* sums)
     {
@@ -171,7 +171,7 @@ struct Share {
         for (int t = 0; t < kPieces; ++t) {
             int i, c;
             place(t, i, c);
-            const int row = kTurned ? c : i, piece = (kTurned ? i : c) / kCount, turn = kTurned ? swizzle_of<T>(c, kRows) : (i >> 1) & 7;
+            const int row = kTurned ? c : i, piece = (kTurned ? i : c) / kCount, turn = kTurned ? swizzle_of<T>(c, kRows) : U == 1 ? (i >> 1) & 7 : i & 15;
             *reinterpret_cast<A*>(to + row * kLength + ((piece ^ turn) << 4)) = v[t];
         }
     }
@@ -179,20 +179,23 @@ struct Share {
 
 // 32 I by 32 J sums of a workgroup of four wavefronts, over c of c_begin .. c_end - 1.  The bytes of the kAhead steps that follow are on their way to
 // registers while one is multiplied from LDS (two buffers, a barrier a step): a step takes 0.2 us of work, its loads 1 us and more.  Latency bounds it where
-// a CU has one tile, so tiles are small (I = J = 1) while there are few: 24 x 1001 -> 1001 bfloat16 6.1 us in tiles of 32 x 32, 10.2 in 64 x 64.
-constexpr int kAhead = 3;
+// a CU has one tile, so tiles are small (I = J = 1) while there are few: 24 x 1001 -> 1001 bfloat16 6.1 us in tiles of 32 x 32, 10.2 in 64 x 64.  Their steps are
+// of two units of 128 bytes, for half of the barriers: 203 x 1001 -> 1111 fp32 12.2 us, 13.8 in steps of one unit; gradients of 300 x 300 -> 300 with relu
+// 9.2 and 10.6.  (One step of those ahead: 18.1, three: 14.2; steps of four units: 16.4.  64 x 64: the same either way.)
+constexpr int units_of(int I, int J) { return I * J == 1 ? 2 : 1; }
+constexpr int ahead_of(int U) { return U == 1 ? 3 : 2; }
 
 template <class T, int I, int J, bool kTurnedA, bool kTurnedB, bool kSlope, bool kFew>
 __device__ __forceinline__ void direct_tile(const Side& a, const Side& b, int act, int i0, int j0, int c_begin, int c_end, char* lds, float4v (&acc)[I][J], float* sums)
 {
-    constexpr int kA = 32 * I * 128, kBuffer = kA + 32 * J * 128, kC = 128 / sizeof(T);
-    typedef Share<T, 32 * I, kTurnedA, kSlope, kFew> A;
-    typedef Share<T, 32 * J, kTurnedB, false, kFew> B;
+    constexpr int U = units_of(I, J), kAhead = ahead_of(U), kRow = 128 * U, kA = 32 * I * kRow, kBuffer = kA + 32 * J * kRow, kC = kRow / sizeof(T);
+    typedef Share<T, 32 * I, U, kTurnedA, kSlope, kFew> A;
+    typedef Share<T, 32 * J, U, kTurnedB, false, kFew> B;
     A of_a[kAhead];
     B of_b[kAhead];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4, wi = wave & 1, wj = wave >> 1;
-    const int a_at = kTurnedA ? turned_address<T>(lane, wi * I, 32 * I) : (wi * I * 16 + r) * 128 + ((q ^ (r >> 1)) << 4);
-    const int b_at = kA + (kTurnedB ? turned_address<T>(lane, wj * J, 32 * J) : (wj * J * 16 + r) * 128 + ((q ^ (r >> 1)) << 4));
+    const int turn = U == 1 ? r >> 1 : r, a_at = kTurnedA ? turned_address<T>(lane, wi * I, 32 * I) : (wi * I * 16 + r) * kRow + ((q ^ turn) << 4);
+    const int b_at = kA + (kTurnedB ? turned_address<T>(lane, wj * J, 32 * J) : (wj * J * 16 + r) * kRow + ((q ^ turn) << 4));
     each<kAhead>([&](auto d) {
         of_a[d].fetch(a, i0, c_begin + d * kC, c_end);
         of_b[d].fetch(b, j0, c_begin + d * kC, c_end);
@@ -207,11 +210,11 @@ __device__ __forceinline__ void direct_tile(const Side& a, const Side& b, int ac
             of_a[d].fetch(a, i0, c + kAhead * kC, c_end);
             of_b[d].fetch(b, j0, c + kAhead * kC, c_end);
             auto read = [&](auto turned, int at, int h, int block, int length) {
-                if constexpr (turned) return read_block<T>(lds + buffer + ((at + h * (kC / 2) * length) ^ (block * 16 * (int)sizeof(T))), length);
-                else return *reinterpret_cast<const int4v*>(lds + buffer + (at ^ (h * 64)) + block * 2048);
+                if constexpr (turned) return read_block<T>(lds + buffer + ((at + h * (64 / (int)sizeof(T)) * length) ^ (block * 16 * (int)sizeof(T))), length);
+                else return *reinterpret_cast<const int4v*>(lds + buffer + (at ^ (h * 64)) + block * 16 * kRow);
             };
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < 2 * U; ++h) {
                 int4v fa[I], fb[J];
 #pragma unroll
                 for (int i = 0; i < I; ++i) fa[i] = read(std::integral_constant<bool, kTurnedA>{}, a_at, h, i, A::kLength);
@@ -270,7 +273,7 @@ __device__ __forceinline__ void zero(float4v (&acc)[I][J])
 template <class T, int I, int J, bool kFew>
 __global__ __launch_bounds__(256) void linear_direct_kernel(ProductArgs a, int K, long long ldx, long long ldw)
 {
-    __shared__ __attribute__((aligned(256))) char lds[2 * 32 * (I + J) * 128];
+    __shared__ __attribute__((aligned(256))) char lds[2 * 32 * (I + J) * 128 * units_of(I, J)];
     const int across = (a.N + 32 * J - 1) / (32 * J), down = (a.M + 32 * I - 1) / (32 * I), tile = (int)(blockIdx.x % (unsigned)(across * down)), part = (int)(blockIdx.x / (unsigned)(across * down));
     const int m0 = tile % down * 32 * I, n0 = tile / down * 32 * J;
     constexpr int kC = 128 / sizeof(T);
@@ -297,7 +300,7 @@ struct DirectGradArgs {
 template <class T, int I, int J, bool kSlope, bool kFew>
 __global__ __launch_bounds__(256) void linear_direct_grad_kernel(DirectGradArgs a)
 {
-    __shared__ __attribute__((aligned(256))) char lds[2 * 32 * (I + J) * 128];
+    __shared__ __attribute__((aligned(256))) char lds[2 * 32 * (I + J) * 128 * units_of(I, J)];
     constexpr int kC = 128 / sizeof(T), kCount = 16 / sizeof(T);
     const int across = (a.K + 32 * J - 1) / (32 * J);
     const Side d_rows{a.grad, a.z, a.ldg, a.N, a.M}, d_turned{a.grad, a.z, a.ldg, a.N, a.N};
@@ -713,8 +716,8 @@ double lay_estimate(double bytes) { return 3.0 + bytes / 4e6; }
 double direct_estimate(int dtype, bool turned, bool small, double tiles, double work, int longest, double bytes)
 {
     const bool wide = dtype == kF32;
-    const double alone = small ? (wide ? 0.26 : 0.21) : wide ? 0.74 : 0.34;
-    const double shared = small ? (wide ? 0.23 : turned ? 0.15 : 0.20) : wide ? (turned ? 0.60 : 0.63) : turned ? 0.28 : 0.25;
+    const double alone = small ? (wide ? 0.24 : 0.20) : wide ? 0.74 : 0.34;
+    const double shared = small ? (wide ? 0.20 : turned ? 0.15 : 0.20) : wide ? (turned ? 0.60 : 0.63) : turned ? 0.28 : 0.25;
     return (small ? 3.7 : 4.5) + std::max({longest * alone, work / 256.0 * shared, bytes / 5.2e6}) + tiles / 256.0 * (turned ? 1.2 : 0.9) * (small ? 0.5 : 1.0);
 }
 
@@ -887,9 +890,9 @@ GradPlan plan_of(const LinearGradArgs& a, int dtype)
             const double x = tiles_x(small ? 32 : 64), w = tiles_w(small ? 32 : 64), work = x * all_x + w * all_w;
             const int steps_x = (all_x + parts_x - 1) / parts_x, steps_w = (all_w + parts_w - 1) / parts_w, longest = std::max(steps_x, steps_w);
             // (Where the slope is worked out as the tiles are loaded, every tile along K does it anew.)
-            const double anew = a.act == kNone ? 0.0 : std::max(work / 256.0, (double)longest) * (a.act == kRelu ? 0.28 : 0.38) * (dtype == kF32 ? 0.5 : 1.0) * (small ? 0.8 : 1.0);
+            const double anew = a.act == kNone ? 0.0 : std::max(work / 256.0, (double)longest) * (a.act == kRelu ? 0.42 : 0.50) * (dtype == kF32 ? 0.5 : 1.0) * (small ? 0.8 : 1.0);
             const double us = direct_estimate(dtype, true, small, x * parts_x + w * parts_w, work, longest, bytes) + join_estimate(parts_x, (double)a.M * a.K) +
-                              join_estimate(parts_w, (double)a.N * a.K) + std::min(anew, form);
+                              join_estimate(parts_w, (double)a.N * a.K) + 2.0 * ((parts_x > 1) + (parts_w > 1)) + std::min(anew, form);
             if (direct >= 0.0 && us >= direct) return;
             direct = us;
             l.small = small;

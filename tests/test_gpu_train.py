@@ -62,7 +62,8 @@ LAYERS = [  # M, K, N: every kernel (test_train_host.py), one token and row, odd
     (1, 1, 1), (1, 64, 10), (1, 4096, 640), (2, 7, 3), (3, 200, 6), (5, 1001, 70), (16, 64, 16), (17, 96, 33), (24, 2048, 520), (33, 128, 257),
     (40, 4096, 96), (64, 512, 64), (65, 72, 130), (100, 136, 1000), (128, 200, 256), (203, 1001, 1111), (250, 2048, 300), (256, 64, 512), (515, 328, 700),
     (1000, 40, 24), (64, 16384, 64), (300, 8192, 40), (700, 1500, 1100), (20, 520, 4100), (20, 264, 4100), (48, 136, 2100), (40, 64, 2100), (520, 264, 777), (48, 1032, 4100),
-    (40, 8192, 300), (20, 512, 8200), (900, 8192, 96), (8200, 264, 96), (4100, 512, 777), (264, 8192, 777), (20, 2048, 4160)]
+    (40, 8192, 300), (20, 512, 8200), (900, 8192, 96), (8200, 264, 96), (4100, 512, 777), (264, 8192, 777), (20, 2048, 4160), (880, 136, 520),
+    (360, 8192, 40), (880, 8192, 100)]
 LARGE_LAYERS = [(2048, 1024, 2048), (4200, 512, 4100), (2300, 264, 4097), (2300, 1001, 777), (8200, 520, 8264), (3000, 4096, 3000), (8192, 2048, 2048)]
 
 
