@@ -8,9 +8,9 @@
 // Four ways, chosen by what each is estimated to take (below):
 //   very few rows     linear_dot_kernel: the weights once from memory at 4.7 TB/s (1 x 4096 -> 4096 bfloat16 7.2 us);
 //   arrays as they lie  linear_direct_kernel, linear_direct_grad_kernel: one launch, tiles of 32 x 32 or 64 x 64, any address and either way round
-//                     (203 x 1001 -> 1111 fp32 13.0 us; both gradients of 128 x 200 -> 256 with relu 6.6 us);
+//                     (203 x 1001 -> 1111 fp32 11.2 us; both gradients of 128 x 200 -> 256 with relu 5.8 us);
 //   few rows          linear_row_kernel (linear_laid.h): the weights from memory (24 x 4096 -> 8192 float16 14.8 us, 4.6 TB/s);
-//   tiles             linear_tile_kernel (linear_laid.h): the matrix cores (8192 x 4096 -> 8192 bfloat16 with gelu and z kept 452 us, 1.22 PFLOP/s).
+//   tiles             linear_tile_kernel (linear_laid.h): the matrix cores (8192 x 4096 -> 8192 bfloat16 with gelu and z kept 450 us, 1.22 PFLOP/s).
 // The last two load straight to LDS, which takes rows at multiples of 16 bytes; others are laid out in scratch memory first (linear_lay_kernel).
 #include <hip/hip_runtime.h>
 
@@ -179,7 +179,7 @@ struct Share {
 
 // 32 I by 32 J sums of a workgroup of four wavefronts, over c of c_begin .. c_end - 1.  The bytes of the kAhead steps that follow are on their way to
 // registers while one is multiplied from LDS (two buffers, a barrier a step): a step takes 0.2 us of work, its loads 1 us and more.  Latency bounds it where
-// a CU has one tile, so tiles are small (I = J = 1) while there are few: 24 x 1001 -> 1001 bfloat16 6.1 us in tiles of 32 x 32, 10.2 in 64 x 64.  Their steps are
+// a CU has one tile, so tiles are small (I = J = 1) while there are few: 24 x 1001 -> 1001 bfloat16 5.8 us in tiles of 32 x 32, 10.2 in 64 x 64.  Their steps are
 // of two units of 128 bytes, for half of the barriers: 203 x 1001 -> 1111 fp32 12.2 us, 13.8 in steps of one unit; gradients of 300 x 300 -> 300 with relu
 // 9.2 and 10.6.  (One step of those ahead: 18.1, three: 14.2; steps of four units: 16.4.  64 x 64: the same either way.)
 constexpr int units_of(int I, int J) { return I * J == 1 ? 2 : 1; }
@@ -286,7 +286,7 @@ __global__ __launch_bounds__(256) void linear_direct_kernel(ProductArgs a, int K
 
 // Both gradients in one launch: the first `tiles_x` workgroups take grad_x = d w (sum over N), the others grad_w = d^T x (over M) and, in the
 // tiles of the first columns, the sums of d for the bias.  One launch instead of up to six (d, two products, joins, sums): 128 x 200 -> 256 fp32
-// 6.4 us against 16.3 laid out.  Past about 2000 x 1000 -> 2000 what the tiles read again from L2 costs more than that.
+// 5.1 us against 16.1 laid out.  Past about 2000 x 1000 -> 2000 what the tiles read again from L2 costs more than that.
 struct DirectGradArgs {
     const void *grad, *z, *x, *w;
     void *grad_x, *grad_w;
@@ -711,8 +711,8 @@ struct LinearPlan {
 double lay_estimate(double bytes) { return 3.0 + bytes / 4e6; }
 
 // A direct launch of `tiles` that take `work` steps in all, `longest` of them one after another at most, of arrays of `bytes`.  turned: the gradients'
-// operands; small: tiles of 32 x 32 instead of 64 x 64 (faster until they are several for each CU: gradients of 128 x 200 -> 256 fp32 6.4 us against
-// 9.9, of 1024 x 1024 -> 1024 bfloat16 24.9 against 16.6).
+// operands; small: tiles of 32 x 32 instead of 64 x 64 (faster until they are several for each CU: gradients of 128 x 200 -> 256 fp32 5.1 us against
+// 9.9, of 1024 x 1024 -> 1024 bfloat16 22.6 against 16.4).
 double direct_estimate(int dtype, bool turned, bool small, double tiles, double work, int longest, double bytes)
 {
     const bool wide = dtype == kF32;
