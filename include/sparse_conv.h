@@ -425,7 +425,7 @@ int sparse_conv_int8_linear(const void* x, const float* x_scale, const signed ch
                             unsigned flags, void* workspace, long long workspace_bytes, void* stream);
 
 /* What a layer applies to its sums: nothing, max(z, 0), z Phi(z) with the normal distribution's Phi = (1 + erf(z / sqrt 2)) / 2,
- * or z / (1 + exp(-z)). */
+ * or z / (1 + exp(-z)).  (Phi to an absolute 1.3e-7, as fp32 holds 1 + erf.) */
 enum { SC_ACT_NONE = 0, SC_ACT_RELU = 1, SC_ACT_GELU = 2, SC_ACT_SILU = 3 };
 
 /*
@@ -439,8 +439,8 @@ enum { SC_ACT_NONE = 0, SC_ACT_RELU = 1, SC_ACT_GELU = 2, SC_ACT_SILU = 3 };
  *   z         [M][N] without gaps, or NULL: receives what goes into the activation, rounded, as the gradient needs it.
  *   dtype     of x, w, residual, out and z: SC_F32, SC_F16 or SC_BF16.
  *   workspace of at least the bytes that sparse_conv_linear_workspace reports for the same arguments (it looks at x and w for
- *             their alignment alone).  Arrays at multiples of 16 bytes whose rows are whole multiples of 16 bytes apart and long
- *             are read as they are; others are copied there first.
+ *             their alignment alone).  Sums that several workgroups share are joined there, and arrays that do not lie at multiples of
+ *             16 bytes, with rows of whole multiples, are copied there first where that is faster.
  * Products are summed, and everything behind them is computed, in fp32; out and z are rounded once.  Apart from residual = out no
  * array that is written may overlap another (what lies between rows counts as theirs).  The same arguments give the same bits.
  * An infinity or a NaN in a row of x or of w reaches no other row or column of the output.  M may be 0 (no-op).
@@ -527,6 +527,7 @@ typedef struct {
  *                size / 448; m is rounded to the nearest number, v up or down by chance, so that what it should be is kept on average
  *                (by numbers that an element's place in its tensor and the step alone give: the same arguments give the same bits), and
  *                not to zero.  A block whose largest size is below 2^-100 counts as zeros.  A gradient that is no finite number spoils its block.
+ *   eps          with 0, an element that has had no gradient yet becomes NaN (0 / 0).
  *   step         the number of this step, from 1.
  *   counted      NULL, or DEVICE memory that sparse_conv_adamw_count filled: the step's number is taken from there, and `step` not looked at.
  * SC_EINVAL: a null or misaligned pointer, a negative count, betas outside 0 <= beta < 1, rate, eps or decay negative or no finite number,

@@ -523,6 +523,7 @@ PyObject* py_adamw(PyObject*, PyObject* const* args, Py_ssize_t count)
         const at::Tensor& v = tensor(args[3], "v must be a tensor");
         const bool small = m.scalar_type() == at::kFloat8_e4m3fn;
         const int64_t room = m.numel(), element = small ? 1 : 4;
+        const int state_dtype = small ? (int)SC_E4M3 : (int)SC_F32;
         auto is_state = [&](const at::Tensor& t, at::ScalarType type, int64_t n) { return t.is_cuda() && t.scalar_type() == type && t.dim() == 1 && t.size(0) == n && t.is_contiguous() && t.device() == m.device(); };
         const at::ScalarType type = small ? at::kFloat8_e4m3fn : at::kFloat;
         require(room % SC_ADAMW_BLOCK == 0 && is_state(m, type, room) && is_state(v, type, room), "states must be as the optimizer made them");
@@ -575,7 +576,7 @@ PyObject* py_adamw(PyObject*, PyObject* const* args, Py_ssize_t count)
                         room_of.numel() * room_of.element_size() >= SC_ADAMW_COUNTED_BYTES, "bad arguments");
             counted = room_of.data_ptr();
             // (What the step would refuse must not count: its rule and types, then its arrays.)
-            int rc = adamw(nullptr, 0, param_dtype, grad_dtype, small ? SC_E4M3 : SC_F32, rule[0], rule[1], rule[2], rule[3], rule[4], rule[5], 1, counted, stream);
+            int rc = adamw(nullptr, 0, param_dtype, grad_dtype, state_dtype, rule[0], rule[1], rule[2], rule[3], rule[4], rule[5], 1, counted, stream);
             const int bytes_of[3] = {4, 2, 2};      // SC_F32, SC_F16, SC_BF16
             for (const sparse_conv_adamw_tensor& t : list) {
                 const char *p = static_cast<const char*>(t.param), *g = static_cast<const char*>(t.grad);
@@ -595,7 +596,7 @@ PyObject* py_adamw(PyObject*, PyObject* const* args, Py_ssize_t count)
             if (rc != SC_OK) return PyLong_FromLong(rc);
             written(steps);
         }
-        const int rc = adamw(list.data(), (int)list.size(), param_dtype, grad_dtype, small ? SC_E4M3 : SC_F32, rule[0], rule[1], rule[2], rule[3], rule[4], rule[5],
+        const int rc = adamw(list.data(), (int)list.size(), param_dtype, grad_dtype, state_dtype, rule[0], rule[1], rule[2], rule[3], rule[4], rule[5],
                              PyLong_AsLongLong(args[9]), counted, stream);
         for (Py_ssize_t i = 0; i < tensors; ++i)
             if (PyList_GET_ITEM(args[1], i) != Py_None) written(THPVariable_Unpack(PyList_GET_ITEM(args[0], i)));
