@@ -811,15 +811,35 @@ int launch_way(const LinearPlan& p, ProductArgs a, const LinearArgs& l, char* wo
 
 long long linear_workspace(const LinearArgs& a, int dtype) { return plan_of(a, dtype).end; }
 
-int linear_kernel(int dtype, int M, int N, int K)
+namespace {
+
+// Operands without gaps at multiples of 16 bytes.
+LinearPlan plan_of(int dtype, int M, int N, int K)
 {
     LinearArgs a{};
     a.M = M;
     a.N = N;
     a.K = K;
     a.ldx = a.ldw = K;
-    const LinearPlan p = plan_of(a, dtype);
+    return plan_of(a, dtype);
+}
+
+bool few_of(int dtype, int terms) { return terms * bytes_of(dtype) < 16; }
+
+}  // namespace
+
+int linear_kernel(int dtype, int M, int N, int K)
+{
+    const LinearPlan p = plan_of(dtype, M, N, K);
     return p.way == kDot ? 100 : p.way == kDirect ? (p.small ? 103 : 101) : p.laid.kernel;
+}
+
+int linear_form(int dtype, int M, int N, int K)
+{
+    const LinearPlan p = plan_of(dtype, M, N, K);
+    if (p.way == kDot) return 0;
+    if (p.way == kLaid) return p.laid.parts > 1 ? 8 : 0;
+    return p.small + 2 * few_of(dtype, K) + 8 * (p.parts > 1);
 }
 
 int launch_linear(int dtype, const LinearArgs& a, char* workspace, void* stream)
@@ -991,15 +1011,31 @@ int launch_direct_grad(const GradPlan& l, const LinearGradArgs& a, char* workspa
 
 long long linear_grad_workspace(const LinearGradArgs& a, int dtype) { return plan_of(a, dtype).end; }
 
-int linear_grad_kernel(int dtype, int M, int N, int K, int act)
+namespace {
+
+GradPlan plan_of(int dtype, int M, int N, int K, int act)
 {
     LinearGradArgs a{};
     a.M = M;
     a.N = a.ldg = N;
     a.K = a.ldx = a.ldw = K;
     a.act = act;
-    const GradPlan p = plan_of(a, dtype);
+    return plan_of(a, dtype);
+}
+
+}  // namespace
+
+int linear_grad_kernel(int dtype, int M, int N, int K, int act)
+{
+    const GradPlan p = plan_of(dtype, M, N, K, act);
     return p.direct ? 101 + p.formed : 1000 * p.x.kernel + p.w.kernel;
+}
+
+int linear_grad_form(int dtype, int M, int N, int K, int act)
+{
+    const GradPlan p = plan_of(dtype, M, N, K, act);
+    if (!p.direct) return 8 * (p.x.parts > 1) + 16 * (p.w.parts > 1);
+    return p.small + 2 * few_of(dtype, std::min(N, K)) + 4 * (act != kNone && !p.formed) + 8 * (p.parts_x > 1) + 16 * (p.parts_w > 1);
 }
 
 int launch_linear_grad(int dtype, const LinearGradArgs& a, char* workspace, void* stream)

@@ -72,6 +72,10 @@ int launch_linear(int dtype, const LinearArgs& a, char* workspace, void* stream)
 // arrays as they lie (103: in tiles of 32 x 32); of the gradients 101, 102 where d is formed before, else 1000 * grad_x's + grad_w's.
 int linear_kernel(int dtype, int M, int N, int K);
 int linear_grad_kernel(int dtype, int M, int N, int K, int act);
+// Their forms: 1 tiles of 32 x 32, 2 rows of less than 16 bytes (both of one launch alone), 4 the slope is worked out as d is loaded, 8 the sums of the layer or
+// of grad_x are split, 16 those of grad_w are.
+int linear_form(int dtype, int M, int N, int K);
+int linear_grad_form(int dtype, int M, int N, int K, int act);
 
 struct LinearGradArgs {
     const void *grad, *z, *x, *w;      // [M][ldg], [M][N] or null, [M][ldx], [N][ldw]
