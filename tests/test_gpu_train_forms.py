@@ -1,11 +1,13 @@
 """Forms of the layer's and its gradients' kernels that ordinary sizes take (tiles of either size, the slope worked out as d is loaded, rows of less than
-16 bytes, sums split over workgroups), against 64 bits.
+16 bytes, sums split over workgroups), and gradients of arrays that lie apart and at odd addresses, against 64 bits.
 
 Bounds are those of test_gpu_train.py, which says where they come from.  test_train_forms_host.py checks that the sizes of both files reach
 every kernel in every form that sizes drawn at large take."""
+import math
+
 import pytest
 
-from test_gpu_train import _check_gradient, _check_layer
+from test_gpu_train import E, TINY, U, _act, _check_gradient, _check_layer, _mm, _slope, _types, _within
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +39,88 @@ def test_forms_of_the_gradients(dtype):
     for i, (M, K, N, act) in enumerate(FORM_GRADIENTS):
         print(f"form of the gradients {dtype} {M}x{K} -> {N} {act}", flush=True)
         _check_gradient(gen, M, K, N, dtype, act, i % 2 == 1)
+
+
+def _apart(gen, R, C, shift, gap, t, scale=1.0):
+    """(memory, [R][C] of it): rows C + gap elements apart from element `shift` on, NaN in all that is not theirs."""
+    import torch
+    store = torch.full((R * (C + gap) + shift + 8,), math.nan, dtype=t, device="cuda")
+    rows = store[shift:shift + R * (C + gap)].view(R, C + gap)[:, :C]
+    rows.copy_(torch.randn((R, C), generator=gen, device="cuda") * scale)
+    return store, rows
+
+
+# M, K, N: one launch in tiles of either size, with the slope worked out in it or before; laid out.
+APART = [(5, 64, 40), (37, 129, 66), (150, 256, 200), (300, 304, 300), (1021, 300, 77), (1000, 640, 776), (2100, 1032, 1040),
+         (3000, 2056, 2056), (4100, 4104, 4096)]
+WAYS = [  # shift and gap of grad, x, weight; 8 elements are 16 bytes or 32
+    ((0, 0), (0, 0), (0, 0)), ((8, 8), (8, 8), (8, 8)), ((1, 3), (0, 0), (0, 0)), ((0, 0), (1, 0), (0, 8)), ((0, 8), (0, 1), (0, 0)), ((0, 0), (0, 0), (2, 0)), ((0, 1), (3, 5), (1, 2))]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_gradients_of_rows_that_lie_apart_and_at_odd_addresses(dtype):
+    """Strided grad, x and weight, NaN between their rows; z, which has no gaps, and the gradients that are written at odd addresses."""
+    import torch
+    from paper_2011_06295_amd import text
+    t = _types()[dtype]
+    gen = torch.Generator(device="cuda").manual_seed(53)
+    for i, (M, K, N) in enumerate(APART):
+        for j, way in enumerate(WAYS):
+            act = (None, "relu", "gelu", "silu")[(i + j) % 4]
+            print(f"apart {dtype} {M}x{K} -> {N} {way} {act}", flush=True)
+            g, x, w = (_apart(gen, R, C, shift, gap, t, scale)[1] for (R, C, scale), (shift, gap) in zip(((M, N, 1.0), (M, K, 1.0), (N, K, 1.5 / math.sqrt(K))), way))
+            z = _apart(gen, 1, M * N, 1 + j % 3, 0, t, 2.0)[1].view(M, N)
+            stores, outs = zip(*(_apart(gen, 1, n, shift, 0, kind) for n, shift, kind in ((M * K, 1 + j % 2, t), (N * K, 3, t), (N, 1, torch.float32))))
+            before = [s.clone() for s in stores]
+            outs = [o.view(shape) for o, shape in zip(outs, ((M, K), (N, K), (N,)))]
+            gw0, gb0, accumulate = outs[1].double(), outs[2].double(), j % 2 == 1
+            layer = text.Linear(w, torch.zeros(N, device="cuda"), activation=act)
+            layer.backward(g, x, z if act else None, *outs, accumulate=accumulate)
+            d = g.double() * _slope(z.double(), act)
+            off = (9 * E * g.double().abs() if act in ("gelu", "silu") else 0.0) * torch.ones_like(d)
+            rounded = off + (U[dtype] * (d.abs() + off) + TINY[dtype] if act else 0.0)
+            what = (M, K, N, dtype, act, way)
+            for name, got, ref, size, wrong, count in (
+                    ("x", outs[0], d @ w.double(), d.abs() @ w.double().abs(), rounded @ w.double().abs(), N),
+                    ("weight", outs[1], d.t().contiguous() @ x.double(), d.t().abs().contiguous() @ x.double().abs(), rounded.t().contiguous() @ x.double().abs(), M)):
+                bound = wrong + 2 * (count + 2) * E * (size + wrong)
+                if accumulate and name == "weight":
+                    ref = ref + gw0
+                    bound = bound + E * (ref.abs() + bound)
+                _within(got, ref, bound + U[dtype] * (ref.abs() + bound) + TINY[dtype], what + (name,))
+            ref, bound = d.sum(0), off.sum(0) + 2 * (M + 2) * E * (d.abs() + off).sum(0)
+            if accumulate:
+                ref, bound = ref + gb0, bound + E * gb0.abs()
+            _within(outs[2], ref, bound + E * ref.abs() + TINY["f32"], what + ("bias",))
+            for store, was, out in zip(stores, before, outs):          # nothing else is written
+                first = out.storage_offset()
+                assert bool(torch.isnan(store[:first]).all()) and bool(torch.isnan(store[first + out.numel():]).all()) and store.shape == was.shape
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_large_layers_of_rows_that_lie_apart(dtype):
+    """Layers that are laid out: neither, one or both of x and the weight copied because of their address or distance alone; NaN between the rows."""
+    import torch
+    from paper_2011_06295_amd import binding as B
+    from paper_2011_06295_amd import text
+    t = _types()[dtype]
+    gen = torch.Generator(device="cuda").manual_seed(54)
+    for M, K, N in ((16, 2048, 4160), (900, 1024, 1304), (4100, 2048, 2056)):
+        copied = set()
+        for j, (_, of_x, of_w) in enumerate(WAYS):
+            act = (None, "relu", "gelu", "silu")[j % 4]
+            print(f"large apart {dtype} {M}x{K} -> {N} {of_x} {of_w} {act}", flush=True)
+            x, w = _apart(gen, M, K, *of_x, t)[1], _apart(gen, N, K, *of_w, t, 1.5 / math.sqrt(K))[1]
+            r = _apart(gen, M, N, 1, j, t)[1]
+            store, out = _apart(gen, M, N, 3, 2, t)
+            layer = text.Linear(w, None, activation=act)
+            layer.forward(x, residual=r, out=out)
+            z, off = _mm(x, w), 2 * (K + 2) * E * _mm(x.abs(), w.abs())
+            ref = _act(z, act) + r.double()
+            bound = 1.13 * off + (8 * E * (1 + z.abs()) if act in ("gelu", "silu") else 0.0) + E * ref.abs()
+            _within(out, ref, bound + U[dtype] * (ref.abs() + bound) + TINY[dtype], (M, K, N, dtype, of_x, of_w, act))
+            mask = torch.ones_like(store, dtype=torch.bool)
+            mask[3:3 + M * (N + 2)].view(M, N + 2)[:, :N] = False
+            assert bool(torch.isnan(store[mask]).all())
+            copied.add(B.sparse_conv_linear_workspace(x.data_ptr(), w.data_ptr(), M, N, K, x.stride(0), w.stride(0), {"f32": B.SC_F32, "f16": B.SC_F16, "bf16": B.SC_BF16}[dtype]))
+        assert M < 4100 or len(copied) == 4, copied
