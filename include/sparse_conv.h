@@ -461,7 +461,8 @@ enum { SC_LINEAR_ACCUMULATE = 1u };
  * sparse_conv_linear_backward - gradients of sparse_conv_linear.  With d[m][n] = grad[m][n] * act'(z[m][n]):
  *   grad_x[m][k] = sum_n d[m][n] w[n][k],  grad_w[n][k] = sum_m d[m][n] x[m][k],  grad_bias[n] = sum_m d[m][n].
  *   grad       [M][N], ldg from one row to the next: the gradient of out (which is the residual's gradient as well).
- *   z          [M][N] as sparse_conv_linear left it; not read for SC_ACT_NONE.  (The slope of SC_ACT_RELU at 0 is 0.)
+ *   z          [M][N] as sparse_conv_linear left it; not read for SC_ACT_NONE.  (The slope of SC_ACT_RELU at 0 is 0, and where
+ *              its slope is 0, d is 0 whatever grad holds.)
  *   x, w       as there; x is read for grad_w alone, w for grad_x alone.
  *   grad_x     [M][K] without gaps, or NULL if it is not wanted; grad_w [N][K] likewise; grad_bias fp32 [N] likewise.
  *   flags      0 or SC_LINEAR_ACCUMULATE.

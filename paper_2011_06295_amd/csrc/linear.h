@@ -79,13 +79,20 @@ __device__ __forceinline__ float activate(float z)
 template <int kAct>
 __device__ __forceinline__ float slope(float z)
 {
-    if (kAct == kRelu) return z > 0.f ? 1.f : z == z ? 0.f : z;
     if (kAct == kGelu) return fmaf(z * 0.39894228040143268f, __builtin_amdgcn_exp2f(-0.5f * kLog2e * z * z), normal(z));
     if (kAct == kSilu) {
         const float s = logistic(z);
         return s * fmaf(z, 1.f - s, 1.f);
     }
     return 1.f;
+}
+
+// A gradient g behind the activation.  ReLU passes it on or does not: a product with 0 would make a NaN of an infinite one.
+template <int kAct>
+__device__ __forceinline__ float behind(float g, float z)
+{
+    if (kAct == kRelu) return z > 0.f ? g : z == z ? 0.f : z;
+    return g * slope<kAct>(z);
 }
 
 // f with the activation as a constant: one branch for all the elements that it takes.

@@ -150,7 +150,7 @@ struct Share {
                 for (int e = 0; e < kCount; ++e) {
                     float g = (float)v[t][e];
                     if constexpr (act != kNone) {
-                        g *= slope<act>((float)z[t][e]);
+                        g = behind<act>(g, (float)z[t][e]);
                         v[t][e] = (T)g;
                     }
                     if constexpr (kTurned) sums[e] += g;
@@ -606,7 +606,7 @@ __global__ __launch_bounds__(256) void linear_lay_kernel(LayArgs a)
             for (int e = 0; e < kCount; ++e) {
                 float g = (float)v[t][e];
                 if constexpr (act != kNone) {
-                    g = col + e < a.cols ? g * slope<act>((float)z[t][e]) : 0.f;
+                    g = col + e < a.cols ? behind<act>(g, (float)z[t][e]) : 0.f;
                     v[t][e] = (T)g;
                 }
                 total[e] += g;

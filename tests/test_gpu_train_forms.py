@@ -7,7 +7,7 @@ import math
 
 import pytest
 
-from test_gpu_train import E, TINY, U, _act, _check_gradient, _check_layer, _mm, _slope, _types, _within
+from test_gpu_train import E, TINY, U, _act, _check_gradient, _check_layer, _layer_case, _mm, _slope, _types, _within
 
 pytestmark = pytest.mark.gpu
 
@@ -124,3 +124,30 @@ def test_large_layers_of_rows_that_lie_apart(dtype):
             assert bool(torch.isnan(store[mask]).all())
             copied.add(B.sparse_conv_linear_workspace(x.data_ptr(), w.data_ptr(), M, N, K, x.stride(0), w.stride(0), {"f32": B.SC_F32, "f16": B.SC_F16, "bf16": B.SC_BF16}[dtype]))
         assert M < 4100 or len(copied) == 4, copied
+
+
+# M, K, N: one launch in tiles of either size; d formed before it; laid out
+GRADIENT_WAYS = [(9, 40, 24), (300, 300, 300), (305, 2203, 253), (1021, 1001, 777), (4100, 2056, 4104)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_relu_stops_gradients_that_are_no_number(dtype):
+    """Where z is not above 0 the gradient behind a ReLU is 0, also of an infinity or a NaN: all gradients are those of a grad with zeros there."""
+    import torch
+    from paper_2011_06295_amd import text
+    gen = torch.Generator(device="cuda").manual_seed(55)
+    for M, K, N in GRADIENT_WAYS:
+        print(f"relu {dtype} {M}x{K} -> {N}", flush=True)
+        x, w, bias, g = _layer_case(gen, M, K, N, dtype, True)
+        z = torch.randn((M, N), generator=gen, device="cuda").to(_types()[dtype])
+        z[0, 0], z[1, 1], z[2, 2], z[3, 3] = 0.0, -1.0, -math.inf, 1.0
+        clean = torch.where(z > 0, g, torch.zeros_like(g))
+        g = torch.where(z > 0, g, torch.full_like(g, math.inf))
+        g[1, 1], g[2, 2] = -math.inf, math.nan
+        layer = text.Linear(w, bias, activation="relu")
+        for got, want in zip(layer.backward(g, x, z), layer.backward(clean, x, z)):
+            assert bool(torch.isfinite(want).all()) and torch.equal(got, want)
+        g[3, 3] = math.inf          # one that it passes on
+        gx, gw, gb = layer.backward(g, x, z)
+        assert not bool(torch.isfinite(gx[3]).any()) and not bool(torch.isfinite(gw[3]).any()) and float(gb[3]) == math.inf
+        assert bool(torch.isfinite(gx[4:]).all()) and bool(torch.isfinite(gw[4:]).all()) and bool(torch.isfinite(gb[4:]).all())
