@@ -462,7 +462,8 @@ enum { SC_LINEAR_ACCUMULATE = 1u };
  *   grad_x[m][k] = sum_n d[m][n] w[n][k],  grad_w[n][k] = sum_m d[m][n] x[m][k],  grad_bias[n] = sum_m d[m][n].
  *   grad       [M][N], ldg from one row to the next: the gradient of out (which is the residual's gradient as well).
  *   z          [M][N] as sparse_conv_linear left it; not read for SC_ACT_NONE.  (The slope of SC_ACT_RELU at 0 is 0, and where
- *              its slope is 0, d is 0 whatever grad holds.)
+ *              its slope is 0, d is 0 whatever grad holds.  The slopes of the others at
+ *              minus and plus infinity, which a z of 16 bits may have become, are 0 and 1.)
  *   x, w       as there; x is read for grad_w alone, w for grad_x alone.
  *   grad_x     [M][K] without gaps, or NULL if it is not wanted; grad_w [N][K] likewise; grad_bias fp32 [N] likewise.
  *   flags      0 or SC_LINEAR_ACCUMULATE.

@@ -75,10 +75,12 @@ __device__ __forceinline__ float activate(float z)
     return z;
 }
 
-// The derivative.
+// The derivative.  It is 0 or 1 to fp32 long before 128: infinities, which a z that is kept in 16 bits may have become, count as that (they would give 0 times
+// infinity).
 template <int kAct>
 __device__ __forceinline__ float slope(float z)
 {
+    z = z < -128.f ? -128.f : z > 128.f ? 128.f : z;
     if (kAct == kGelu) return fmaf(z * 0.39894228040143268f, __builtin_amdgcn_exp2f(-0.5f * kLog2e * z * z), normal(z));
     if (kAct == kSilu) {
         const float s = logistic(z);

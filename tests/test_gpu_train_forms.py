@@ -151,3 +151,29 @@ def test_relu_stops_gradients_that_are_no_number(dtype):
         gx, gw, gb = layer.backward(g, x, z)
         assert not bool(torch.isfinite(gx[3]).any()) and not bool(torch.isfinite(gw[3]).any()) and float(gb[3]) == math.inf
         assert bool(torch.isfinite(gx[4:]).all()) and bool(torch.isfinite(gw[4:]).all()) and bool(torch.isfinite(gb[4:]).all())
+
+
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+def test_slopes_of_what_went_past_16_bits(act):
+    """z outside binary16's range is kept as an infinity; the layer's output is 0 or as large, and the slope 0 or 1."""
+    import torch
+    from paper_2011_06295_amd import text
+    gen = torch.Generator(device="cuda").manual_seed(56)
+    for M, K, N in GRADIENT_WAYS:
+        print(f"past 16 bits {M}x{K} -> {N} {act}", flush=True)
+        x, w, bias, g = _layer_case(gen, M, K, N, "f16", True)
+        x[0], x[2], w[1] = 0.0, 0.0, 0.0
+        x[0, 0], x[2, 0], w[1, 0] = -3000.0, 3000.0, 40.0          # z of 120000 either way in column 1
+        w[2:, 0] = 0.0
+        w[0, 0] = 0.0
+        layer = text.Linear(w, bias, activation=act)
+        y, z = layer.forward(x, keep=True)
+        assert float(z[0, 1]) == -math.inf and float(z[2, 1]) == math.inf and float(y[0, 1]) == 0.0 and float(y[2, 1]) == math.inf
+        flat = z.clone()
+        flat[0, 1], flat[2, 1] = -60000.0, 60000.0          # slopes of 0 and 1 as well
+        got = layer.backward(g, x, z)
+        for a, b in zip(got, layer.backward(g, x, flat)):
+            assert bool(torch.isfinite(a).all()) and torch.equal(a, b)
+        z[4, 3] = math.nan
+        gx, gw, gb = layer.backward(g, x, z)
+        assert bool(torch.isnan(gx[4]).all()) and bool(torch.isnan(gw[3]).all()) and math.isnan(float(gb[3])) and torch.equal(gx[:4], got[0][:4]) and torch.equal(gx[5:], got[0][5:])
