@@ -521,7 +521,7 @@ typedef struct {
 /*
  * sparse_conv_adamw - an AdamW step over many tensors, in few launches.  For each element, with g = grad_scale * grad, all in fp32:
  *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
- *   p = (1 - rate * decay) p - rate * (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps),   t = step.
+ *   p = p - (rate * decay * p + rate * (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)),   t = step.
  *   tensors      HOST array, read by the call; its tensors are of the same types, all with `master` or all without, and none of
  *                their arrays may overlap another, but gradients each other.
  *   param_dtype  SC_F32, SC_F16 or SC_BF16; grad_dtype SC_F32 or param_dtype (any of the three where param_dtype is SC_F32).

@@ -326,7 +326,7 @@ int sparse_conv_adamw(const sparse_conv_adamw_tensor* tensors, int count, int pa
         }
     }
     if (count == 0) return SC_OK;
-    sc::AdamwRule rule{(float)rate, (float)(1.0 - rate * decay), (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps,
+    sc::AdamwRule rule{(float)rate, (float)(rate * decay), (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps,
                        (float)grad_scale, 1.f, 1.f, (unsigned)step, static_cast<const sc::AdamwCounted*>(counted)};
     if (!counted) {
         rule.c1 = (float)(1.0 / (1.0 - std::pow(beta1, (double)step)));

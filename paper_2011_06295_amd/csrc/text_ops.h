@@ -113,7 +113,7 @@ struct AdamwCounted {      // what a step on a count in device memory reads
     unsigned step, unused;
 };
 struct AdamwRule {
-    float rate, keep, beta1, rest1, beta2, rest2, eps, grad_scale, c1, c2;      // keep = 1 - rate decay; rest = 1 - beta
+    float rate, decay, beta1, rest1, beta2, rest2, eps, grad_scale, c1, c2;      // decay: times the rate; rest = 1 - beta
     unsigned step;
     const AdamwCounted* counted;       // or null; else c1, c2 and step are there
 };

@@ -177,3 +177,28 @@ def test_slopes_of_what_went_past_16_bits(act):
         z[4, 3] = math.nan
         gx, gw, gb = layer.backward(g, x, z)
         assert bool(torch.isnan(gx[4]).all()) and bool(torch.isnan(gw[3]).all()) and math.isnan(float(gb[3])) and torch.equal(gx[:4], got[0][:4]) and torch.equal(gx[5:], got[0][5:])
+
+
+# ---------------------------------------------------------------- AdamW
+
+@pytest.mark.parametrize("master", [False, True])
+def test_weight_decay_below_the_weights_own_rounding(master):
+    """What a step of a small rate takes off fp32 weights, on average over 2^22 of them.  A weight in 0.5 .. 1 moves in steps of 2^-24; updates of all sizes
+    up to the rate make each rounding as good as random, off by 2^-24 / sqrt(12) (and by a second one of that size at most), and their mean by
+    2^-24 / sqrt(6) / 2^11 = 1.2e-11.  Six times that is less than a hundredth of the decay, 1e-8 and more."""
+    import torch
+    from paper_2011_06295_amd import text
+    gen = torch.Generator(device="cuda").manual_seed(61)
+    for rate in (2e-6, 5e-6, 1e-5):
+        n, decay, eps = 1 << 22, 0.01, 1e-2
+        start = torch.rand(n, generator=gen, device="cuda") * 0.5 + 0.5
+        grad = 1e-2 * torch.randn(n, generator=gen, device="cuda")
+        p = start.to(torch.bfloat16) if master else start.clone()
+        opt = text.AdamW([p], rate=rate, eps=eps, decay=decay, master=master)
+        if master:
+            opt.master.copy_(start)
+        opt.step([grad])
+        moved = (opt.master if master else p).double() - start.double()
+        update = rate * grad.double() / (grad.double().abs() + eps)          # the first step: m over the root of v is the gradient over its size
+        took, ref = float((-moved - update).mean()), rate * decay * float(start.double().mean())
+        assert ref > 1.4e-8 and abs(took - ref) <= 8e-11 + 16 * E * rate, (rate, took, ref)
