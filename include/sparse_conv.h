@@ -529,11 +529,14 @@ typedef struct {
  *                size / 448; m is rounded to the nearest number, v up or down by chance, so that what it should be is kept on average
  *                (by numbers that an element's place in its tensor and the step alone give: the same arguments give the same bits), and
  *                not to zero.  A block whose largest size is below 2^-100 counts as zeros.  A gradient that is no finite number spoils its block.
+ *                A change of m below half a step between numbers, a 16th of it, is lost: with beta1 = 0.9 a steady gradient g may leave m anywhere
+ *                from 0.61 g to 2.25 g, and one that ends leaves up to 5 * 2^-9 of the scale.  Past 17/18 m would keep its value and its sign whatever
+ *                the gradient is, so states of 8 bits take beta1 up to 0.9 alone.
  *   eps          with 0, an element that has had no gradient yet becomes NaN (0 / 0).
  *   step         the number of this step, from 1.
  *   counted      NULL, or DEVICE memory that sparse_conv_adamw_count filled: the step's number is taken from there, and `step` not looked at.
  * SC_EINVAL: a null or misaligned pointer, a negative count, betas outside 0 <= beta < 1, rate, eps or decay negative or no finite number,
- * step below 1, unknown types.  SC_EUNSUPPORTED: more than 2^34 elements in a tensor.
+ * step below 1, unknown types.  SC_EUNSUPPORTED: more than 2^34 elements in a tensor, beta1 above 0.9 with states of 8 bits.
  */
 int sparse_conv_adamw(const sparse_conv_adamw_tensor* tensors, int count, int param_dtype, int grad_dtype, int state_dtype, double rate,
                       double beta1, double beta2, double eps, double decay, double grad_scale, long long step, const void* counted,

@@ -52,6 +52,9 @@ constexpr int kMostLinear = 1 << 20;
 constexpr long long kMostTiles = (1ll << 24) - 1;
 constexpr long long kMostStep = 1ll << 34;      // elements of a tensor: workgroups of 2048 each
 constexpr long long kMostApart = 1ll << 31;
+// First moments of 8 bits: (1 - beta1) times the moment has to be more than half a step between its numbers, a 18th at most, or it never changes; 0.9 leaves a
+// steady gradient's moment within a factor of 2.25.
+constexpr double kMostBeta1OfSmall = 0.9;
 
 // An array: `bytes` from p on, whose elements have `element` bytes.
 struct Array {
@@ -310,6 +313,7 @@ int sparse_conv_adamw(const sparse_conv_adamw_tensor* tensors, int count, int pa
     if (!is_amount(rate) || !is_amount(eps) || !is_amount(decay) || !is_beta(beta1) || !is_beta(beta2) || !std::isfinite(grad_scale)) return SC_EINVAL;
     if (counted ? !aligned(counted, 16) : step < 1) return SC_EINVAL;
     const bool small = state_dtype == SC_E4M3;
+    if (small && beta1 > kMostBeta1OfSmall) return SC_EUNSUPPORTED;
     for (int i = 0; i < count; ++i) {
         const sparse_conv_adamw_tensor& t = tensors[i];
         if (t.count < 0 || (t.master != nullptr) != (tensors[0].master != nullptr)) return SC_EINVAL;

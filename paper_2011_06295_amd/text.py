@@ -226,7 +226,8 @@ class AdamW:
     def __init__(self, params, rate: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, decay: float = 0.01, bits: int = 32, master: bool = False,
                  counted: bool = False):
         """params: contiguous CUDA tensors of one type (fp32, binary16, bfloat16) and device.  bits: 32, or 8: numbers of 8 bits (e4m3)
-        with an fp32 scale for each block of 256.  master: steps apply to fp32 weights kept here, the parameters receive them rounded
+        with an fp32 scale for each block of 256, and beta1 up to 0.9 (m is rounded to the nearest number, by which a steady gradient may leave it off by a factor
+        of 2.25; closer to 1 it would stop following).  master: steps apply to fp32 weights kept here, the parameters receive them rounded
         (else a 16-bit parameter loses every change below half its own rounding).  counted: the number of steps is counted in device
         memory, for steps recorded in a graph (`steps` is then a tensor)."""
         self.params = list(params)
@@ -244,6 +245,8 @@ class AdamW:
         self.rate, self.betas, self.eps, self.decay, self.bits = float(rate), (beta1, beta2), float(eps), float(decay), bits
         if not (0.0 <= beta1 < 1.0 and 0.0 <= beta2 < 1.0 and self.rate >= 0.0 and self.eps >= 0.0 and self.decay >= 0.0):
             raise ValueError("rate, eps and decay must not be negative, betas at least 0 and below 1")
+        if bits == 8 and beta1 > 0.9:      # a change of m by less than half a step between numbers of 8 bits is lost
+            raise ValueError("with states of 8 bits beta1 is 0.9 at most")
         self.begins = [0]
         for p in self.params:
             self.begins.append(self.begins[-1] + -(-p.numel() // B.SC_ADAMW_BLOCK) * B.SC_ADAMW_BLOCK)

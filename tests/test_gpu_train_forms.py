@@ -7,7 +7,7 @@ import math
 
 import pytest
 
-from test_gpu_train import E, TINY, U, _act, _check_gradient, _check_layer, _layer_case, _mm, _slope, _types, _within
+from test_gpu_train import E, TINY, U, _act, _check_gradient, _check_layer, _layer_case, _mm, _slope, _types, _values, _within
 
 pytestmark = pytest.mark.gpu
 
@@ -202,3 +202,37 @@ def test_weight_decay_below_the_weights_own_rounding(master):
         update = rate * grad.double() / (grad.double().abs() + eps)          # the first step: m over the root of v is the gradient over its size
         took, ref = float((-moved - update).mean()), rate * decay * float(start.double().mean())
         assert ref > 1.4e-8 and abs(took - ref) <= 8e-11 + 16 * E * rate, (rate, took, ref)
+
+
+def test_first_moments_of_8_bits_follow_the_gradient():
+    """m under steady gradients, after they turn, after they fall to a third and after they end, beside an element that keeps the block's scale.
+    m rests where (1 - b) |g - m| is half a step between numbers or less: a 16th of m where it has to grow, an 18th where it has to shrink (1.125 to 1); where the
+    steps are 2^-9 of the scale, (1 - b) times it within 2^-10.  The scale itself is off by an ulp or so a step."""
+    import torch
+    from paper_2011_06295_amd import text
+    for beta in (0.0, 0.5, 0.8, 0.9):
+        n = 8 * 256
+        size = torch.linspace(0.1, 0.9, n, device="cuda")
+        top = torch.arange(n, device="cuda") % 256 == 0
+        size[top] = 1.0
+        opt = text.AdamW([torch.zeros(n, device="cuda")], rate=0.0, betas=(beta, 0.999), bits=8)
+        slack, below, above = 1.001, 1 / (1 + 1 / 16 / (1 - beta)), 1 / (1 - 1 / 18 / (1 - beta))
+        for factor in (1.0, -1.0, 0.3, -0.3, 0.0):
+            g = torch.where(top, size, factor * size)
+            for _ in range(300):
+                opt.step([g])
+            m = _values(opt, "m")[~top]
+            if factor == 0.0:
+                assert float(m.abs().max()) <= 2.0 ** -10 / (1 - beta) * float(opt.m_scale.max()) * slack
+            else:
+                ratio = m / g.double()[~top]
+                assert below / slack <= float(ratio.min()) and float(ratio.max()) <= above * slack, (beta, factor)
+    for beta in (0.95, 0.99):
+        with pytest.raises(ValueError, match="beta1"):
+            text.AdamW([torch.zeros(8, device="cuda")], betas=(beta, 0.999), bits=8)
+        text.AdamW([torch.zeros(8, device="cuda")], betas=(beta, 0.999))
+        opt = text.AdamW([torch.zeros(8, device="cuda")], bits=8, counted=True)
+        opt.betas = (beta, 0.999)
+        with pytest.raises(RuntimeError):
+            opt.step([torch.ones(8, device="cuda")])
+        assert int(opt.steps) == 0

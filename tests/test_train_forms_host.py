@@ -1,4 +1,4 @@
-"""Every kernel of the layer and its gradients, in every form that sizes drawn at large take, is one that a GPU test compares with 64 bits.  Needs no GPU."""
+"""Every kernel of the layer and its gradients, in every form that sizes drawn at large take, is one that a GPU test compares with 64 bits; refusals.  Needs no GPU."""
 import ctypes as C
 import math
 import random
@@ -63,3 +63,14 @@ def test_drawn_sizes_take_no_form_that_is_not_tested(dtype):
     # (both tiles, with and without the slope in them, short rows, every way to split the sums)
     forms = {form for kind, _, form in gradients if kind == "both"}
     assert {f & 5 for f in forms} == {0, 1, 4, 5} and {f & 7 for f in forms} >= {2, 3, 6, 7} and {f & 24 for f in forms} == {0, 8, 16, 24}
+
+
+def test_first_moments_of_8_bits_need_a_beta_that_moves_them():
+    tensors = (B.AdamwTensor * 1)()
+
+    def step(beta1, state, count=0):
+        return LIB.sparse_conv_adamw(tensors, count, B.SC_F32, B.SC_F32, state, 1e-3, beta1, 0.999, 1e-8, 0.0, 1.0, 1, None, None)
+    for beta1 in (0.0, 0.5, 0.9):
+        assert step(beta1, B.SC_E4M3) == step(beta1, B.SC_F32) == B.SC_OK
+    for beta1 in (0.900001, 0.95, 0.99):
+        assert step(beta1, B.SC_E4M3) == step(beta1, B.SC_E4M3, 1) == B.SC_EUNSUPPORTED and step(beta1, B.SC_F32) == B.SC_OK
