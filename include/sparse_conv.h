@@ -527,8 +527,10 @@ typedef struct {
  *   param_dtype  SC_F32, SC_F16 or SC_BF16; grad_dtype SC_F32 or param_dtype (any of the three where param_dtype is SC_F32).
  *   state_dtype  SC_F32, or SC_E4M3: a state is its number of 8 bits times its block's scale.  A scale is the block's largest
  *                size / 448; m is rounded to the nearest number, v up or down by chance, so that what it should be is kept on average
- *                (by numbers that an element's place in its tensor and the step alone give: the same arguments give the same bits), and
- *                not to zero.  A block whose largest size is below 2^-100 counts as zeros.  A gradient that is no finite number spoils its block.
+ *                (by numbers that an element's place in its tensor and the step alone give: the same arguments give the same bits).
+ *                The smallest number that v takes above zero is 2^-9: an element whose v is less than 2^-9 of the scale, a 229376th of the block's
+ *                largest, is held there, so that it moves by less than it would with its own v.
+ *                A block whose largest size is below 2^-100 counts as zeros.  A gradient that is no finite number spoils its block.
  *                A change of m below half a step between numbers, a 16th of it, is lost: with beta1 = 0.9 a steady gradient g may leave m anywhere
  *                from 0.61 g to 2.25 g, and one that ends leaves up to 5 * 2^-9 of the scale.  Past 17/18 m would keep its value and its sign whatever
  *                the gradient is, so states of 8 bits take beta1 up to 0.9 alone.

@@ -56,7 +56,8 @@ __device__ __forceinline__ float factor_of(float largest, float& scale)
 }
 
 // y >= 0 to four binary digits, up or down by chance, so that what the steps add up to stays right on average: with the nearest number
-// a state that changes by a thousandth a step would stay where it is.  What is there stays above zero (a step divides by its root).
+// a state that changes by a thousandth a step would stay where it is.  What is there stays above zero (a step divides by its root),
+// so that below the smallest number the average is too large: it is the smallest number.
 __device__ __forceinline__ float by_chance(float y, float noise)
 {
     const int exponent = max((int)(__float_as_uint(y) >> 23) - 127 - 3, -9);

@@ -236,3 +236,25 @@ def test_first_moments_of_8_bits_follow_the_gradient():
         with pytest.raises(RuntimeError):
             opt.step([torch.ones(8, device="cuda")])
         assert int(opt.steps) == 0
+
+
+def test_second_moments_of_8_bits_keep_their_average_down_to_the_smallest_number():
+    """One step from zero, v of each size beside an element that sets the block's scale to 1 / 448 of its own.  On average what it should be, within six deviations of
+    65280 roundings, half a step each at most; below the smallest number, 2^-9 of the scale, that number."""
+    import torch
+    from paper_2011_06295_amd import text
+    n = 256 * 256
+    top = torch.arange(n, device="cuda") % 256 == 0
+    for times in (1e-3, 0.1, 0.9, 1.1, 1.5, 2.7, 7.3, 1000.0):          # v over the smallest number
+        g = torch.full((n,), math.sqrt(times / 229376.0), device="cuda")
+        g[top] = 1.0
+        opt = text.AdamW([torch.zeros(n, device="cuda")], rate=0.0, betas=(0.9, 0.5), bits=8)
+        opt.step([g])
+        v, scale = _values(opt, "v")[~top], float(opt.v_scale[0])
+        smallest = scale * 2.0 ** -9
+        assert abs(float(_values(opt, "v")[top].min()) - 0.5) <= 4 * E
+        if times < 1.0:
+            assert bool((v == smallest).all())
+        else:
+            step = smallest * max(1.0, 2.0 ** (math.floor(math.log2(times)) - 3))
+            assert abs(float(v.mean()) - 0.5 * times / 229376.0) <= 6 * 0.5 * step / math.sqrt(65280.0) + 1e-6 * float(v.mean()), times
