@@ -9,7 +9,7 @@
 //   very few rows     linear_dot_kernel: the weights once from memory at 4.7 TB/s (1 x 4096 -> 4096 bfloat16 7.2 us);
 //   arrays as they lie  linear_direct_kernel, linear_direct_grad_kernel: one launch, tiles of 32 x 32 or 64 x 64, any address and either way round
 //                     (203 x 1001 -> 1111 fp32 11.2 us; both gradients of 128 x 200 -> 256 with relu 5.8 us);
-//   few rows          linear_row_kernel (linear_laid.h): the weights from memory (24 x 4096 -> 8192 float16 14.8 us, 4.6 TB/s);
+//   few rows          linear_row_kernel (linear_laid.h): the weights from memory (24 x 4096 -> 8192 float16 14.8 us, three sets of weights in turn);
 //   tiles             linear_tile_kernel (linear_laid.h): the matrix cores (8192 x 4096 -> 8192 bfloat16 with gelu and z kept 450 us, 1.22 PFLOP/s).
 // The last two load straight to LDS, which takes rows at multiples of 16 bytes; others are laid out in scratch memory first (linear_lay_kernel).
 #include <hip/hip_runtime.h>
@@ -452,11 +452,12 @@ __global__ __launch_bounds__(256) void linear_dot_kernel(ProductArgs a, int K, l
 
 double pieces_of(int n, int size) { return (double)((n + size - 1) / size); }
 
-// Microseconds that a product of rows of `bytes` is estimated to take.  The constants are fitted, for 16-bit types and for fp32, to what each kernel
-// near the fastest took at 159 sizes (4 to 8192 rows of x, 64 to 8192 of w and of terms, one launch after another in a graph, arrays
-// that change): the kernel of the least estimate takes 1.1 % more than the fastest on average, and at most 21 % (40 x 7552 -> 3712 bfloat16).
-// One constant is not the fit's, for arrays that its repetitions held in the caches: 5.8 for 2 x 2 in 16 bits (6.73), since 24 x 4096 -> 8192
-// takes 18.2 us there and 14.8 in 2 x 1 with weights from HBM.
+// Microseconds that a product of rows of `bytes` is estimated to take.  The constants are fitted, for 16-bit types and for fp32, to what each kernel near the fastest
+// took at 159 sizes (4 to 8192 rows of x, 64 to 8192 of w and of terms), one launch after another in a graph, on three sets of arrays in turn; those of the 2 x 2
+// row kernel of 16 bits at 98 more, of 5 to 128 rows, there also with weights that all come from HBM.  At other sizes, without an activation, what the estimates
+// choose took more than the fastest by: 5 to 128 rows (294 products) 2.3 % on average on three sets in turn, 2.6 % from HBM, at most 43 % (5 x 256 -> 4544 bfloat16 4.7 us, 3.3 in tiles
+// of 32 x 32); 160 to 8192 rows in 16 bits (60) 1.5 %, at most 17 %; in fp32 (56) 6 %, at most 43 % (1024 x 2304 -> 1088 85 us, 59 by the 4 x 1 row
+// kernel).  What the epilogue does is not in the estimates.
 
 // Row kernel: a launch, the sums of the wavefronts and the further workgroups of a CU, then the largest of what all workgroups load,
 // what those of one CU load, both operands from memory, and the products.
@@ -466,7 +467,7 @@ struct RowRule {
     double all, one, arrays, products;        // MB/us of all, KB/us of one, MB/us of the arrays; us for 1000 bytes of a block
 };
 constexpr RowRule kRowRules[2][5] = {
-    {{1, 1, 1.22, 0.603, 17.9, 137.0, 6.23, 0.0547}, {2, 1, 0.746, 0.317, 21.6, 129.0, 5.98, 0.0479}, {2, 2, 1.86, 0.573, 14.8, 132.0, 5.8, 0.0479},
+    {{1, 1, 1.22, 0.603, 17.9, 137.0, 6.23, 0.0547}, {2, 1, 0.746, 0.317, 21.6, 129.0, 5.98, 0.0479}, {2, 2, 1.5, 1.01, 13.2, 120.0, 5.22, 0.0478},
      {4, 1, 0.899, 0.344, 21.1, 139.0, 4.77, 0.05}, {4, 2, 2.04, 0.601, 16.1, 121.0, 6.32, 0.0499}},
     {{1, 1, 1.15, 0.769, 16.3, 174.0, 4.99, 0.356}, {2, 1, 0.66, 0.317, 14.9, 66.9, 4.09, 0.358}, {2, 2, 1.56, 1.54, 28.8, 182.0, 4.61, 0.287},
      {4, 1, 0.829, 0.344, 48.2, 119.0, 4.34, 0.331}, {4, 2, 2.13, 1.37, 10.0, 166.0, 6.05, 0.289}}};

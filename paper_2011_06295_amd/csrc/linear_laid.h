@@ -297,8 +297,8 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 || S > 2 ? 1 : 2) void 
 // Few rows of x: 16 MB of them by 16 NB rows of w a workgroup, whose W wavefronts go round the 128-byte units of the rows and add their
 // sums up at the end.  A wavefront loads its units to a part of LDS of its own, D of them in flight, and waits for its own loads alone.
 // (Loads in the order that the products take would touch 16 rows with 16 lanes in a row, at a quarter of the rate.)  The weights' bytes bound it, as far
-// as enough of them are on their way: two workgroups of 72 KB a CU (2 x 1 blocks, 4 wavefronts, 3 deep) take 24 x 4096 -> 8192 float16 from HBM in
-// 14.8 us, one of 128 KB (2 x 2, 8 wavefronts, 2 deep) in 18.2, two of 64 KB (2 x 2, 4 wavefronts, 2 deep) in 19.9.
+// as enough of them are on their way: for 24 x 4096 -> 8192 in 16 bits two workgroups of 72 KB a CU (2 x 1 blocks, 4 wavefronts, 3 deep) take 15.2 us on three sets
+// of weights in turn, which the caches hold in part, one of 128 KB (2 x 2, 8 wavefronts, 2 deep) 16.4; from HBM alone both take 17 to 18.5.
 template <class T, int MB, int NB, int W, int D>
 __global__ __launch_bounds__(64 * W) void linear_row_kernel(ProductArgs a)
 {
