@@ -5,11 +5,11 @@
 // summed in fp32 by the matrix cores, fp32 is multiplied in fp32 (at most 152 TFLOP/s here).  d is rounded to the type of the operands once, since
 // the matrix cores take nothing else; the bias' sums take it before that.
 //
-// Four ways, chosen by what each is estimated to take (below):
+// Four ways, chosen by what each is estimated to take (below).  Times here and there: one call after another in a graph, three sets of arrays in turn.
 //   very few rows     linear_dot_kernel: the weights once from memory at 4.7 TB/s (1 x 4096 -> 4096 bfloat16 7.2 us);
 //   arrays as they lie  linear_direct_kernel, linear_direct_grad_kernel: one launch, tiles of 32 x 32 or 64 x 64, any address and either way round
-//                     (203 x 1001 -> 1111 fp32 11.2 us; both gradients of 128 x 200 -> 256 with relu 5.8 us);
-//   few rows          linear_row_kernel (linear_laid.h): the weights from memory (24 x 4096 -> 8192 float16 14.8 us, three sets of weights in turn);
+//                     (203 x 1001 -> 1111 fp32 11.2 us; both gradients of 128 x 200 -> 256 with relu 5.2 us);
+//   few rows          linear_row_kernel (linear_laid.h): the weights from memory (24 x 4096 -> 8192 float16 14.6 us; 17.3 where the caches hold none of them);
 //   tiles             linear_tile_kernel (linear_laid.h): the matrix cores (8192 x 4096 -> 8192 bfloat16 with gelu and z kept 450 us, 1.22 PFLOP/s).
 // The last two load straight to LDS, which takes rows at multiples of 16 bytes; others are laid out in scratch memory first (linear_lay_kernel).
 #include <hip/hip_runtime.h>
@@ -179,9 +179,10 @@ struct Share {
 
 // 32 I by 32 J sums of a workgroup of four wavefronts, over c of c_begin .. c_end - 1.  The bytes of the kAhead steps that follow are on their way to
 // registers while one is multiplied from LDS (two buffers, a barrier a step): a step takes 0.2 us of work, its loads 1 us and more.  Latency bounds it where
-// a CU has one tile, so tiles are small (I = J = 1) while there are few: 24 x 1001 -> 1001 bfloat16 5.8 us in tiles of 32 x 32, 10.2 in 64 x 64.  Their steps are
-// of two units of 128 bytes, for half of the barriers: 203 x 1001 -> 1111 fp32 12.2 us, 13.8 in steps of one unit; gradients of 300 x 300 -> 300 with relu
-// 9.2 and 10.6.  (One step of those ahead: 18.1, three: 14.2; steps of four units: 16.4.  64 x 64: the same either way.)
+// a CU has one tile, so tiles are small (I = J = 1) while there are few: 24 x 1001 -> 1001 bfloat16 5.2 us in tiles of 32 x 32, 9.6 in 64 x 64.  Their steps are
+// of two units of 128 bytes, for half of the barriers: 203 x 1001 -> 1111 fp32 11.2 us, 12.9 in steps of one unit; fp32 gradients of 300 x 300 -> 300 with relu
+// 8.5 and 9.8 (in bfloat16 7.3 and 6.5), of 128 x 1024 -> 1024 12.5 and 17.5.  (One step of those ahead or three, and steps of four units, were 16 to 48 %
+// slower at the first.  64 x 64: the same either way.)
 constexpr int units_of(int I, int J) { return I * J == 1 ? 2 : 1; }
 constexpr int ahead_of(int U) { return U == 1 ? 3 : 2; }
 
@@ -286,7 +287,8 @@ __global__ __launch_bounds__(256) void linear_direct_kernel(ProductArgs a, int K
 
 // Both gradients in one launch: the first `tiles_x` workgroups take grad_x = d w (sum over N), the others grad_w = d^T x (over M) and, in the
 // tiles of the first columns, the sums of d for the bias.  One launch instead of up to six (d, two products, joins, sums): 128 x 200 -> 256 fp32
-// 5.1 us against 16.1 laid out.  Past about 2000 x 1000 -> 2000 what the tiles read again from L2 costs more than that.
+// 4.5 us without an activation against 15.6 laid out, 5.2 with relu against 16.5.  Past about 2000 x 1000 -> 2000 (46 to 48 us either way) what the tiles read again
+// from L2 costs more than that.
 struct DirectGradArgs {
     const void *grad, *z, *x, *w;
     void *grad_x, *grad_w;
@@ -453,11 +455,11 @@ __global__ __launch_bounds__(256) void linear_dot_kernel(ProductArgs a, int K, l
 double pieces_of(int n, int size) { return (double)((n + size - 1) / size); }
 
 // Microseconds that a product of rows of `bytes` is estimated to take.  The constants are fitted, for 16-bit types and for fp32, to what each kernel near the fastest
-// took at 159 sizes (4 to 8192 rows of x, 64 to 8192 of w and of terms), one launch after another in a graph, on three sets of arrays in turn; those of the 2 x 2
-// row kernel of 16 bits at 98 more, of 5 to 128 rows, there also with weights that all come from HBM.  At other sizes, without an activation, what the estimates
-// choose took more than the fastest by: 5 to 128 rows (294 products) 2.3 % on average on three sets in turn, 2.6 % from HBM, at most 43 % (5 x 256 -> 4544 bfloat16 4.7 us, 3.3 in tiles
-// of 32 x 32); 160 to 8192 rows in 16 bits (60) 1.5 %, at most 17 %; in fp32 (56) 6 %, at most 43 % (1024 x 2304 -> 1088 85 us, 59 by the 4 x 1 row
-// kernel).  What the epilogue does is not in the estimates.
+// took at 159 sizes (4 to 8192 rows of x, 64 to 8192 of w and of terms), on three sets of arrays in turn; those of the 2 x 2 row kernel of 16 bits
+// at 98 more, of 5 to 128 rows, there also with weights that all come from HBM.  Without an activation, what the estimates choose took more than the fastest
+// by: at 147 sizes of 5 to 128 rows, the 98 among them, 2.3 % on average on three sets in turn, 2.6 % from HBM, at most 43 % (5 x 256 -> 4544 bfloat16 4.7 us, 3.3 in
+// tiles of 32 x 32); at others of 160 to 8192 rows 1.5 % in 16 bits (60), at most 17 %, and 6 % in fp32 (56), at most 43 % (1024 x 2304 -> 1088 85 us, 59 by
+// the 4 x 1 row kernel).  What the epilogue does is not in the estimates.
 
 // Row kernel: a launch, the sums of the wavefronts and the further workgroups of a CU, then the largest of what all workgroups load,
 // what those of one CU load, both operands from memory, and the products.
@@ -561,7 +563,7 @@ int product(int dtype, const Choice& c, Turned turned, ProductArgs a, char* part
 // Tiles of 64 x 64 elements of [rows][cols] (ld elements from one row to the next) to `copy` (or null), rows of copy_pitch elements with zeros behind
 // what is there.  With an activation the elements are first multiplied by its slope at z (no gaps), in fp32, and rounded once; column_sums
 // [tiles down][cols] (or null) receives the sums over the tile's rows of what was not rounded.  Bytes bound it: 8192 x 8192 bfloat16 with the slope
-// of gelu, 403 MB, 76 us (5.3 TB/s).
+// of gelu, 403 MB, 77 us (5.2 TB/s).
 struct LayArgs {
     const void *from, *z;
     void* copy;
@@ -712,8 +714,9 @@ struct LinearPlan {
 double lay_estimate(double bytes) { return 3.0 + bytes / 4e6; }
 
 // A direct launch of `tiles` that take `work` steps in all, `longest` of them one after another at most, of arrays of `bytes`.  turned: the gradients'
-// operands; small: tiles of 32 x 32 instead of 64 x 64 (faster until they are several for each CU: gradients of 128 x 200 -> 256 fp32 5.1 us against
-// 9.9, of 1024 x 1024 -> 1024 bfloat16 22.6 against 16.4).
+// operands; small: tiles of 32 x 32 instead of 64 x 64 (faster until they are several for each CU: gradients of 128 x 200 -> 256 fp32 4.5 us against
+// 9.3, of 1024 x 1024 -> 1024 bfloat16 21.7 against 15.2).  Outputs, z and residuals are not in `bytes`, and rows at odd addresses count as others do (gradients of
+// 1021 x 1001 -> 777 float16 with silu: 20 us estimated, 25.8 taken).
 double direct_estimate(int dtype, bool turned, bool small, double tiles, double work, int longest, double bytes)
 {
     const bool wide = dtype == kF32;
@@ -743,8 +746,8 @@ LinearPlan plan_of(const LinearArgs& a, int dtype)
     LinearPlan p{};
     p.lay_x = !laid_out(a.x, a.ldx, a.M, a.K, b);
     p.lay_w = !laid_out(a.w, a.ldw, a.N, a.K, b);
-    // (Two rows that are laid out, or four of fp32: 4096 -> 4096 8.6 us either way in bfloat16, 13.8 and 14.7 in fp32; eight of them 24 and 8.5.
-    // Eight that are not: 1001 -> 1001 6.8 and 9.5.)
+    // (Two rows that are laid out, or four of fp32: 4096 -> 4096 8.1 us and 8.4 by the other kernels in bfloat16, 13.1 and 14.6 in fp32; four in bfloat16 9.2 and
+    // 8.5.  Eight that are not: 1001 -> 1001 6.3 and 5.3 in bfloat16, 5.5 and 8.2 in fp32.)
     if (a.M <= (p.lay_x || p.lay_w ? 8 : dtype == kF32 ? 4 : 2)) {
         p.way = kDot;
         return p;

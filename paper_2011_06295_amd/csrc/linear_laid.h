@@ -37,7 +37,7 @@ constexpr bool kWalksOver = MB * NB >= 64;
 // A tile of 16 MB WM rows of x by 16 NB WN rows of w, 128 bytes of each a step; WM x WN wavefronts with MB x NB blocks of 16 x 16 sums.
 // S steps are in LDS or on their way there.  kTurnX, kTurnW: that operand is given the other way round, element (i, c) at c * pitch + i, as the
 // gradients need it: its step is a part of 128 / sizeof(T) such rows, which lie in LDS as they do in memory and are turned as they are read.
-// The matrix cores bound it: 550 GFLOP of bfloat16, 8192 x 4096 -> 8192, take 399 us a gradient (1.38 PFLOP/s; the largest tiles, 256 x 256 of four
+// The matrix cores bound it: 550 GFLOP of bfloat16, 8192 x 4096 -> 8192, take 391 us a gradient (1.41 PFLOP/s; the largest tiles, 256 x 256 of four
 // wavefronts, which read 1 / 64 of a byte from L2 a product) and 450 as a layer that applies gelu and keeps z, about
 // 17 more vector instructions an output, which nothing hides with one wavefront a SIMD.  (Counted: the matrix cores are busy in 70 and 59 % of the CUs' clocks, at 2.0 GHz;
 // no bank conflicts.)
@@ -297,8 +297,8 @@ __global__ __launch_bounds__(64 * WM * WN, MB * NB >= 64 || S > 2 ? 1 : 2) void 
 // Few rows of x: 16 MB of them by 16 NB rows of w a workgroup, whose W wavefronts go round the 128-byte units of the rows and add their
 // sums up at the end.  A wavefront loads its units to a part of LDS of its own, D of them in flight, and waits for its own loads alone.
 // (Loads in the order that the products take would touch 16 rows with 16 lanes in a row, at a quarter of the rate.)  The weights' bytes bound it, as far
-// as enough of them are on their way: for 24 x 4096 -> 8192 in 16 bits two workgroups of 72 KB a CU (2 x 1 blocks, 4 wavefronts, 3 deep) take 15.2 us on three sets
-// of weights in turn, which the caches hold in part, one of 128 KB (2 x 2, 8 wavefronts, 2 deep) 16.4; from HBM alone both take 17 to 18.5.
+// as enough of them are on their way: for 24 x 4096 -> 8192 in 16 bits two workgroups of 72 KB a CU (2 x 1 blocks, 4 wavefronts, 3 deep) take 14.5 us on three sets
+// of weights in turn, which the caches hold in part, one of 128 KB (2 x 2, 8 wavefronts, 2 deep) 15.7; on 16 sets, from HBM, 17.3 and 17.0 (3.9 TB/s).
 template <class T, int MB, int NB, int W, int D>
 __global__ __launch_bounds__(64 * W) void linear_row_kernel(ProductArgs a)
 {

@@ -3,8 +3,8 @@
 // loss = w (log sum_c exp z_c - z_label), gradient = w (exp(z_c - log sum exp z) - [c = label]).  The bytes bound it: logits once in, gradient
 // once out.  A row stays in registers between the two, where two workgroups of a CU still fit (65536 classes of 16 bits, 32768 of fp32); longer
 // rows are read twice.  Each thread keeps the largest of its logits and the sum of exponentials over that largest, the threads of a row
-// join these pairs once, and every thread turns what it holds into the gradient.  4096 x 65536 bfloat16 with masked classes and rows takes 228 us (1.07 GB,
-// 4.7 TB/s; 209 at the rate of a large copy); 128 x 6 fp32 5.8, of which the GPU works 2.1 and the host the rest.
+// join these pairs once, and every thread turns what it holds into the gradient.  4096 x 65536 bfloat16 with masked classes and rows takes 230 us (1.07 GB,
+// 4.7 TB/s; 209 at the rate of a large copy); 128 x 6 fp32 5.9, of which the GPU works 2.3 and the host the rest.
 #include <hip/hip_runtime.h>
 
 #include "text_ops.h"
