@@ -902,6 +902,7 @@ GradPlan plan_of(const LinearGradArgs& a, int dtype)
     l.x = choose(dtype, a.M, a.K, a.N, true);
     l.w = choose(dtype, a.N, a.K, a.M, true);
     laid = l.x.us + l.w.us + lay_estimate((l.own_dz ? 3.0 : 1.0) * a.M * a.N * b) + 3.0;
+    // (Copies that an address or a distance alone makes necessary are not priced: x's and w's are not known where their gradients are not wanted.)
     if (a.K * b % 16 != 0) laid += lay_estimate(2.0 * a.N * a.K * b) + lay_estimate(2.0 * a.M * a.K * b);
     const int all_x = (a.N + count - 1) / count, all_w = (a.M + count - 1) / count;
     const double form = lay_estimate(3.0 * a.M * a.N * b) + 1.5;
