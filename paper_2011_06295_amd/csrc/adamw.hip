@@ -4,9 +4,10 @@
 // and c2 = 1 / sqrt(1 - b2^t); all in fp32.  Decay and update are added before p is rounded: a factor 1 - rate decay would itself be rounded to 2^-24,
 // which is all of the decay from a rate decay of 3e-8 down.  The bytes bound it: each array once in and once out.
 // 6.1 million fp32 parameters take 27.6 us (170 MB, which the caches hold in part), 33 million of float16 with 32-bit weights beside 191 (927 MB,
-// 4.85 TB/s, four launches), 336 million of bfloat16 with states of 8 bits 707 (3.38 GB, 4.8 TB/s).
+// 4.85 TB/s, four launches), 336 million of bfloat16 with states of 8 bits 719 (3.38 GB, 4.7 TB/s).
 #include <hip/hip_runtime.h>
 
+#include <cfloat>
 #include <cmath>
 
 #include "text_ops.h"
@@ -185,7 +186,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwLaunch a)
         for (int e = 0; e < 4; ++e) {
             update(rule, g[b][e] * rule.grad_scale, m[b][e], v[b][e]);
             const float root = __builtin_amdgcn_sqrtf(v[b][e]) * rule.c2 + rule.eps;
-            p[b][e] -= fmaf(rule.decay, p[b][e], rule.rate * rule.c1 * m[b][e] * __builtin_amdgcn_rcpf(root));
+            const float change = rule.rate * rule.c1 * m[b][e] * __builtin_amdgcn_rcpf(root);
+            p[b][e] -= fmaf(rule.decay, __builtin_amdgcn_fmed3f(p[b][e], -FLT_MAX, FLT_MAX), change);      // (an infinite weight stays what it is)
             if (kSmall) {
                 most_m = fmaxf(most_m, fabsf(m[b][e]));
                 most_v = fmaxf(most_v, v[b][e]);

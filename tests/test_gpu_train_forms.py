@@ -204,6 +204,29 @@ def test_weight_decay_below_the_weights_own_rounding(master):
         assert ref > 1.4e-8 and abs(took - ref) <= 8e-11 + 16 * E * rate, (rate, took, ref)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_infinite_weights_stay(dtype):
+    """Places that a program has masked by infinities, with gradients of zero and others, with and without decay."""
+    import torch
+    from paper_2011_06295_amd import text
+    for bits in (8, 32):
+        for master in (False, True):
+            for decay in (0.0, 0.01):
+                p = torch.ones(600, dtype=_types()[dtype], device="cuda")
+                p[3], p[4], p[300], p[301] = -math.inf, math.inf, -math.inf, math.inf
+                g = torch.ones_like(p)
+                g[:5] = 0.0
+                kept = p.clone()
+                opt = text.AdamW([p], rate=1e-2, decay=decay, bits=bits, master=master)
+                for _ in range(3):
+                    opt.step([g])
+                infinite = torch.isinf(kept)
+                assert torch.equal(p[infinite], kept[infinite]) and bool(torch.isfinite(p[~infinite]).all()) and float(p[100]) < 1.0
+                g[301] = math.nan
+                opt.step([g])
+                assert math.isnan(float(p[301])) and float(p[3]) == -math.inf
+
+
 def test_first_moments_of_8_bits_follow_the_gradient():
     """m under steady gradients, after they turn, after they fall to a third and after they end, beside an element that keeps the block's scale.
     m rests where (1 - b) |g - m| is half a step between numbers or less: a 16th of m where it has to grow, an 18th where it has to shrink (1.125 to 1); where the
